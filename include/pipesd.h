@@ -300,6 +300,90 @@ int32_t pipesd_debug_attn_slots(pipesd_ctx *ctx, int32_t rows_per_kv_head, int32
 int32_t pipesd_debug_attn_split(int32_t total_keys, int32_t page_size, const int32_t *resident_ctas, int32_t units,
                                 int32_t *out3);
 
+/* ---- shaped sampling: temperature, top-k, top-p, min-p ----
+ *
+ * What stands around the verify pass where requests are sampled with settings: the pending token after a prompt, a draft model's
+ * tokens together with the rows q that they came from, and the acceptance rule for a target sampled the same way (Sec. 2.2, with
+ * the shaped distribution as p: the output then follows it exactly).  These calls need no context: every array is in device memory
+ * (plain pointers), all work is enqueued on cuda_stream with that stream's device current, nothing is allocated, nothing waits,
+ * and all of them can be captured into a graph.  They keep no state: calls on several streams or from several threads do not
+ * disturb one another unless they share outputs or scratch.
+ *
+ * A row's ids are ordered by logit, highest first, equal ones by id, lowest first.  With w_j = exp((l_j - max) / temperature)
+ * (temperature 0: 1 for the first of the order, 0 for the others) there are kept, in this order: top-k, the first top_k ids
+ * (top_k <= 0: all); top-p, of these the shortest prefix that holds at least top_p of their mass; min-p, of these the ids with
+ * w_j >= min_p.  The distribution is the kept w divided by their sum.  -inf is a logit that is never drawn.
+ * Weights are fp64, sums whole numbers of 2^-45 of the most likely id's weight: the same inputs give the same outputs, bit for bit. */
+#define PIPESD_F32 0
+#define PIPESD_BF16 1
+
+typedef struct pipesd_shaping {
+    float temperature; /* >= 0, finite                    */
+    int32_t top_k;     /* <= 0: off                       */
+    float top_p;       /* > 0; >= 1: off                  */
+    float min_p;       /* 0..1; 0: off                    */
+} pipesd_shaping;
+
+/* One token per row: the first id whose running probability, in id order, exceeds u[row] (0 <= u < 1).  logits: [rows, vocab] of
+ * `dtype`, row_stride elements between rows, vocab up to 2^18.  shaping, u: [rows].  probs (nullable): fp32 [rows, vocab] with
+ * probs_stride, the distributions that the tokens were drawn from -- the q of a draft step.  A row without a distribution (no finite
+ * logit, a NaN or +inf among them, settings or u out of range) gets token -1 and probabilities 0. */
+int32_t pipesd_sample(const void *logits, int32_t dtype, int64_t row_stride, int32_t rows, int32_t vocab,
+                      const pipesd_shaping *shaping, const float *u, int32_t *tokens, float *probs, int64_t probs_stride,
+                      void *cuda_stream);
+
+/* The accept/correct rule for n_req requests whose targets are shaped.  Request r has the rows row0[r] .. row0[r+1]-1 of logits
+ * ([rows, vocab]; row0: n_req + 1 entries from 0 to rows): one for each of its k drafts, and the extra-token row.  Draft i of
+ * request r is drafts[row0[r] - r + i], the distribution that it was drawn from row row0[r] - r + i of q (fp32, q_stride elements
+ * between rows; both have rows - n_req entries and may be null where that is 0).  u: [rows], per request k acceptance tests and
+ * the final draw.  shaping: [n_req].  A draft x is accepted while u < min(1, p(x) / q(x)); a correction comes from norm(max(0, p - q)),
+ * from p where that is 0 everywhere.  A row that has no distribution (see pipesd_sample) accepts nothing and gives next_token -1;
+ * so does a request whose row0 entries make no sense.  scratch: pipesd_accept_scratch_bytes(rows) bytes, 8-byte aligned. */
+uint64_t pipesd_accept_scratch_bytes(int32_t rows);
+int32_t pipesd_accept(const void *logits, int32_t dtype, int64_t row_stride, int32_t n_req, int32_t rows, int32_t vocab,
+                      const int32_t *row0, const pipesd_shaping *shaping, const float *q, int64_t q_stride,
+                      const int32_t *drafts, const float *u, int32_t *n_accepted, int32_t *next_token, void *scratch,
+                      void *cuda_stream);
+
+/* ---- a K/V cache in 4 bits ----
+ *
+ * One layer's paged cache at 5 bits per value, scales included: 160 bytes per position and head of 128 instead of 512.  The columns
+ * of a (position, head) row are cut into groups of 32 with a zero z = bf16(min) and a scale s = bf16((max - z) / 15); a value x is
+ * held as c = clamp(rint((x - z) / s), 0, 15) and stands for s * c + z.  Values beyond +-2^48 are held as that, a NaN as 0.
+ * Calls, streams, threads and graphs as for pipesd_sample; all arrays are in device memory.
+ *
+ * Where rows go: request r has the rows row0[r] .. row0[r+1]-1 of a call (row0: n_req + 1 entries from 0 to rows), and row i of it
+ * is position base[r] + i.  table: [n_req, max_pages] page ids; an id outside 0..n_pages-1 is a page that is not there: rows that
+ * belong to it are dropped, and attention sees no position of it.  So are rows behind position max_pages * page_size.  No two
+ * requests of an append may share a page that gets rows. */
+typedef struct pipesd_kv4_cfg {
+    int32_t n_kv_heads;
+    int32_t head_dim;  /* 64 or 128                                            */
+    int32_t page_size; /* positions: a multiple of 16, up to 4096              */
+    int32_t n_pages;   /* in the pool                                          */
+    int32_t max_pages; /* columns of the table; max_pages * page_size <= 2^30  */
+    int32_t reserved;  /* must be 0                                            */
+} pipesd_kv4_cfg;
+
+/* Bytes of a layer's pool (16-byte aligned, contents irrelevant at first; 0 for a bad cfg). */
+uint64_t pipesd_kv4_pool_bytes(const pipesd_kv4_cfg *cfg);
+/* Quantises rows of K and V ([rows, n_kv_heads, head_dim] of `dtype`, k_stride and v_stride elements between rows) into their
+ * positions; whatever else the pages hold stays as it is. */
+int32_t pipesd_kv4_append(const pipesd_kv4_cfg *cfg, void *pool, const void *k, const void *v, int32_t dtype, int64_t k_stride,
+                          int64_t v_stride, int32_t n_req, int32_t rows, const int32_t *row0, const int32_t *base,
+                          const int32_t *table, void *cuda_stream);
+/* The values that the rows' positions hold: fp32 [rows, n_kv_heads, head_dim] each, 16-byte aligned; 0 where no page is. */
+int32_t pipesd_kv4_read(const pipesd_kv4_cfg *cfg, const void *pool, float *k, float *v, int32_t n_req, int32_t rows,
+                        const int32_t *row0, const int32_t *base, const int32_t *table, void *cuda_stream);
+/* out[row] = softmax(scale * q . k) v over positions 0 .. base[r] + i of the request (its new rows appended before): a single
+ * token, the k+1 rows of a verification, or a prompt.  q, out: [rows, n_q_heads, head_dim] of `dtype` with q_stride, out_stride;
+ * n_q_heads a multiple of n_kv_heads; scale > 0.  bf16: products of bf16 with fp32 sums; fp32: operands carry 16 bits of mantissa.
+ * A row that sees no position gives 0.  scratch: pipesd_kv4_attend_scratch_bytes(cfg) bytes, 16-byte aligned. */
+uint64_t pipesd_kv4_attend_scratch_bytes(const pipesd_kv4_cfg *cfg);
+int32_t pipesd_kv4_attend(const pipesd_kv4_cfg *cfg, const void *pool, const void *q, void *out, int32_t dtype, int64_t q_stride,
+                          int64_t out_stride, int32_t n_q_heads, float scale, int32_t n_req, int32_t rows, const int32_t *row0,
+                          const int32_t *base, const int32_t *table, void *scratch, void *cuda_stream);
+
 /* ---- the edge-side scheduling model (host code only; no device work) ----
  *
  * The verify pass above is what the cloud runs; what decides WHEN it runs and how the draft tokens reach it is the

@@ -21,9 +21,11 @@ STATIC_SCRATCH_BYTES = 8 << 20
 MODE_STOCHASTIC, MODE_GREEDY = 0, 1
 Q_HOST, AUTOCOMMIT, CHAIN = 1, 2, 4
 TOKEN_PENDING = -1
+F32, BF16 = 0, 1
 DISCARDED = 1
 
 i32, u32, u64, f32, vp = ctypes.c_int32, ctypes.c_uint32, ctypes.c_uint64, ctypes.c_float, ctypes.c_void_p
+i64 = ctypes.c_int64
 
 
 class ModelCfg(ctypes.Structure):
@@ -63,6 +65,10 @@ class ProfileInfo(ctypes.Structure):
                 ("gemm_ms", ctypes.c_double), ("gemm_bytes", ctypes.c_double)]
 
 
+class Kv4Cfg(ctypes.Structure):
+    _fields_ = [(n, i32) for n in ("n_kv_heads", "head_dim", "page_size", "n_pages", "max_pages", "reserved")]
+
+
 # name -> (restype, argtypes); mirrors include/pipesd.h one to one
 _SIGNATURES = {
     "pipesd_strerror": (ctypes.c_char_p, [i32]),
@@ -90,6 +96,14 @@ _SIGNATURES = {
     "pipesd_gemm_pack": (i32, [vp, vp, i32, i32, vp]),
     "pipesd_gemm_run": (i32, [vp, vp, vp, vp, i32, i32, i32, vp]),
     "pipesd_gemm_run_static": (i32, [vp, vp, vp, i32, i32, i32, vp]),
+    "pipesd_sample": (i32, [vp, i32, i64, i32, i32, vp, vp, vp, vp, i64, vp]),
+    "pipesd_accept_scratch_bytes": (u64, [i32]),
+    "pipesd_accept": (i32, [vp, i32, i64, i32, i32, i32, vp, vp, vp, i64, vp, vp, vp, vp, vp, vp]),
+    "pipesd_kv4_pool_bytes": (u64, [ctypes.POINTER(Kv4Cfg)]),
+    "pipesd_kv4_append": (i32, [ctypes.POINTER(Kv4Cfg), vp, vp, vp, i32, i64, i64, i32, i32, vp, vp, vp, vp]),
+    "pipesd_kv4_read": (i32, [ctypes.POINTER(Kv4Cfg), vp, vp, vp, i32, i32, vp, vp, vp, vp]),
+    "pipesd_kv4_attend_scratch_bytes": (u64, [ctypes.POINTER(Kv4Cfg)]),
+    "pipesd_kv4_attend": (i32, [ctypes.POINTER(Kv4Cfg), vp, vp, vp, i32, i64, i64, i32, f32, i32, i32, vp, vp, vp, vp, vp]),
     "pipesd_sched_round_time": (i32, [i32, ctypes.c_double, ctypes.c_double, ctypes.c_double, vp, i32,
                                       ctypes.POINTER(ctypes.c_double)]),
     "pipesd_sched_optimal_batching": (i32, [i32, ctypes.c_double, ctypes.c_double, ctypes.c_double, vp,
@@ -424,6 +438,193 @@ def debug_attn_split(total_keys: int, page_size: int, resident_ctas, units: int)
     if rc != 0:
         raise PipesdError(rc, "pipesd_debug_attn_split")
     return tuple(out)
+
+
+# ---- shaped sampling and acceptance, on device tensors (no context)
+class _on:
+    """The device as the current one, and `stream` (None: its current stream) as the one that allocations belong to."""
+
+    __slots__ = ("index", "stream", "scopes")
+
+    def __init__(self, device, stream):
+        self.index, self.stream, self.scopes = device.index, stream, None
+
+    def __enter__(self):
+        import torch
+        if self.stream is None and torch.cuda.current_device() == self.index:        # (the usual call: nothing to switch)
+            return torch._C._cuda_getCurrentRawStream(self.index)
+        import contextlib
+        self.scopes = contextlib.ExitStack()
+        self.scopes.enter_context(torch.cuda.device(self.index))
+        if self.stream is not None:
+            self.scopes.enter_context(torch.cuda.stream(self.stream))
+        return torch.cuda.current_stream(self.index).cuda_stream
+
+    def __exit__(self, *exc):
+        if self.scopes is not None:
+            self.scopes.close()
+
+
+def _rows_of(t, name, width=None):
+    """Row stride of a 2-d or 3-d CUDA tensor whose rows are contiguous."""
+    assert t.is_cuda and t.dim() >= 2, f"{name}: a CUDA tensor of rows"
+    inner = 1
+    for d in range(t.dim() - 1, 0, -1):
+        assert t.shape[d] == 1 or t.stride(d) == inner, f"{name}: rows must be contiguous"
+        inner *= t.shape[d]
+    assert width is None or inner == width, f"{name}: rows of {width} elements expected"
+    assert t.shape[0] <= 1 or t.stride(0) >= inner, f"{name}: rows overlap"
+    return t.stride(0) if t.shape[0] > 1 else inner
+
+
+def _dtype_of(t, name):
+    import torch
+    assert t.dtype in (torch.float32, torch.bfloat16), f"{name}: fp32 or bf16"
+    return F32 if t.dtype == torch.float32 else BF16
+
+
+def _vector(t, n, dtype, device, name):
+    assert t.device == device and t.dtype == dtype and t.numel() == n and t.is_contiguous(), f"{name}: {n} contiguous {dtype} on {device} expected"
+    return t.data_ptr()
+
+
+def shaping(n: int, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, device="cuda"):
+    """Settings of n rows (sample) or requests (accept), each given as one number or n of them: an int32 tensor [n, 4] that
+    holds pipesd_shaping entries."""
+    import torch
+    a = np.empty((n, 4), np.int32)
+    t, p, m = (np.broadcast_to(np.asarray(x, np.float32), (n,)) for x in (temperature, top_p, min_p))
+    if not (np.isfinite(t).all() and (t >= 0).all()):
+        raise ValueError("temperature: finite numbers >= 0")
+    if not (p > 0).all():
+        raise ValueError("top_p: numbers > 0")
+    if not ((m >= 0) & (m <= 1)).all():
+        raise ValueError("min_p: numbers of [0, 1]")
+    a[:, 0], a[:, 1], a[:, 2], a[:, 3] = t.view(np.int32), np.broadcast_to(np.asarray(top_k, np.int32), (n,)), p.view(np.int32), m.view(np.int32)
+    return torch.from_numpy(a).to(device)
+
+
+def sample(logits, shaping, u, *, probs=None, tokens=None, stream=None):
+    """pipesd_sample: one token per row of logits [rows, vocab] (fp32 or bf16, any row stride), settings from shaping(),
+    uniforms u [rows] (fp32).  probs: an fp32 tensor [rows, vocab] that receives the distributions.  Returns the tokens (int32)."""
+    import torch
+    rows, vocab = logits.shape
+    dev = logits.device
+    ld = _rows_of(logits, "logits")
+    pl = 0
+    if probs is not None:
+        assert probs.dtype == torch.float32 and tuple(probs.shape) == (rows, vocab) and probs.device == dev
+        pl = _rows_of(probs, "probs")
+    with _on(dev, stream) as st:
+        if tokens is None:
+            tokens = torch.empty(rows, dtype=torch.int32, device=dev)
+        rc = lib().pipesd_sample(logits.data_ptr(), _dtype_of(logits, "logits"), ld, rows, vocab, _vector(shaping, 4 * rows, torch.int32, dev, "shaping"),
+                                 _vector(u, rows, torch.float32, dev, "u"), _vector(tokens, rows, torch.int32, dev, "tokens"),
+                                 probs.data_ptr() if probs is not None else None, pl, st)
+    if rc != OK:
+        raise PipesdError(rc, "pipesd_sample")
+    return tokens
+
+
+def accept(logits, row0, shaping, q, drafts, u, *, stream=None):
+    """pipesd_accept: the acceptance rule for shaped targets.  row0: int32 [n_req + 1]; shaping: of the requests; q: fp32
+    [rows - n_req, vocab]; drafts: int32 [rows - n_req]; u: fp32 [rows].  Returns (n_accepted, next_token), int32 [n_req] each."""
+    import torch
+    rows, vocab = logits.shape
+    dev = logits.device
+    n_req = row0.numel() - 1
+    ld = _rows_of(logits, "logits")
+    ql, qp, dp = 0, None, None
+    if rows > n_req:
+        assert q.dtype == torch.float32 and tuple(q.shape) == (rows - n_req, vocab) and q.device == dev
+        ql, qp, dp = _rows_of(q, "q"), q.data_ptr(), _vector(drafts, rows - n_req, torch.int32, dev, "drafts")
+    with _on(dev, stream) as st:
+        out = torch.empty((2, max(n_req, 0)), dtype=torch.int32, device=dev)
+        scratch = torch.empty(int(lib().pipesd_accept_scratch_bytes(rows)), dtype=torch.uint8, device=dev)
+        rc = lib().pipesd_accept(logits.data_ptr(), _dtype_of(logits, "logits"), ld, n_req, rows, vocab, _vector(row0, n_req + 1, torch.int32, dev, "row0"),
+                                 _vector(shaping, 4 * n_req, torch.int32, dev, "shaping"), qp, ql, dp, _vector(u, rows, torch.float32, dev, "u"),
+                                 out[0].data_ptr(), out[1].data_ptr(), scratch.data_ptr(), st)
+    if rc != OK:
+        raise PipesdError(rc, "pipesd_accept")
+    return out[0], out[1]
+
+
+class Kv4Cache:
+    """One layer's paged K/V cache in 4 bits (pipesd_kv4_*).  The pool is a uint8 tensor [pages, KV heads, units, bytes], the
+    caller's or one of n_pages pages made here; requests, positions and page tables are the caller's, as device tensors:
+
+      row0   int32 [n_req + 1]            request r has rows row0[r] .. row0[r+1]-1 of the call
+      base   int32 [n_req]                position of its first row
+      table  int32 [n_req, max_pages]     its pages; -1 where there is none
+    """
+
+    def __init__(self, n_kv_heads: int, head_dim: int, *, n_pages: int | None = None, pool=None, page_size: int = 16, device="cuda"):
+        import torch
+        if pool is None:
+            cfg = Kv4Cfg(n_kv_heads, head_dim, page_size, n_pages or 0, 1, 0)
+            size = int(lib().pipesd_kv4_pool_bytes(ctypes.byref(cfg)))
+            if size == 0:
+                raise PipesdError(E_INVALID, "pipesd_kv4_pool_bytes")
+            pool = torch.zeros(size, dtype=torch.uint8, device=device)
+        elif n_pages is None:
+            n_pages = pool.shape[0]
+        cfg = Kv4Cfg(n_kv_heads, head_dim, page_size, n_pages, 1, 0)
+        size = int(lib().pipesd_kv4_pool_bytes(ctypes.byref(cfg)))
+        if size == 0:
+            raise PipesdError(E_INVALID, "pipesd_kv4_pool_bytes")
+        assert pool.is_cuda and pool.dtype == torch.uint8 and pool.is_contiguous() and pool.numel() == size, f"pool: {size} contiguous bytes expected"
+        self.pool, self.n_kv_heads, self.head_dim, self.page_size, self.n_pages = pool, n_kv_heads, head_dim, page_size, n_pages
+        self._scratch_bytes = int(lib().pipesd_kv4_attend_scratch_bytes(ctypes.byref(cfg)))
+
+    def _where(self, rows, row0, base, table):
+        import torch
+        n_req, dev = base.numel(), self.pool.device
+        assert table.dim() == 2 and table.shape[0] == n_req, "table: [n_req, max_pages]"
+        cfg = Kv4Cfg(self.n_kv_heads, self.head_dim, self.page_size, self.n_pages, table.shape[1], 0)
+        return cfg, (n_req, rows, _vector(row0, n_req + 1, torch.int32, dev, "row0"), _vector(base, n_req, torch.int32, dev, "base"),
+                     _vector(table, table.numel(), torch.int32, dev, "table"))
+
+    def append(self, k, v, row0, base, table, *, stream=None):
+        """Quantises the rows k, v [rows, KV heads, head_dim] (fp32 or bf16) into their positions."""
+        dev = self.pool.device
+        shape = (k.shape[0], self.n_kv_heads, self.head_dim)
+        assert tuple(k.shape) == shape == tuple(v.shape) and k.dtype == v.dtype and k.device == dev == v.device, f"k, v: two alike of {shape} on {dev}"
+        cfg, where = self._where(k.shape[0], row0, base, table)
+        with _on(dev, stream) as st:
+            rc = lib().pipesd_kv4_append(ctypes.byref(cfg), self.pool.data_ptr(), k.data_ptr(), v.data_ptr(), _dtype_of(k, "k"), _rows_of(k, "k"), _rows_of(v, "v"),
+                                         *where, st)
+        if rc != OK:
+            raise PipesdError(rc, "pipesd_kv4_append")
+
+    def read(self, rows: int, row0, base, table, *, stream=None):
+        """The values at the rows' positions, fp32 [rows, KV heads, head_dim] of K and of V."""
+        import torch
+        dev = self.pool.device
+        cfg, where = self._where(rows, row0, base, table)
+        with _on(dev, stream) as st:
+            k, v = (torch.empty((rows, self.n_kv_heads, self.head_dim), device=dev) for _ in range(2))
+            rc = lib().pipesd_kv4_read(ctypes.byref(cfg), self.pool.data_ptr(), k.data_ptr(), v.data_ptr(), *where, st)
+        if rc != OK:
+            raise PipesdError(rc, "pipesd_kv4_read")
+        return k, v
+
+    def attend(self, q, row0, base, table, *, scale=None, out=None, stream=None):
+        """Attention of the rows q [rows, query heads, head_dim] (fp32 or bf16; appended before) over their requests' positions.
+        scale: head_dim ** -0.5 unless given."""
+        import torch
+        dev = self.pool.device
+        assert q.dim() == 3 and q.shape[2] == self.head_dim and q.device == dev, f"q: [rows, query heads, {self.head_dim}] on {dev}"
+        cfg, where = self._where(q.shape[0], row0, base, table)
+        with _on(dev, stream) as st:
+            if out is None:
+                out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+            scratch = torch.empty(self._scratch_bytes, dtype=torch.uint8, device=dev)
+            assert out.shape == q.shape and out.dtype == q.dtype and out.device == dev, "out: like q"
+            rc = lib().pipesd_kv4_attend(ctypes.byref(cfg), self.pool.data_ptr(), q.data_ptr(), out.data_ptr(), _dtype_of(q, "q"), _rows_of(q, "q"), _rows_of(out, "out"),
+                                         q.shape[1], self.head_dim ** -0.5 if scale is None else scale, *where, scratch.data_ptr(), st)
+        if rc != OK:
+            raise PipesdError(rc, "pipesd_kv4_attend")
+        return out
 
 
 # ---- the edge-side scheduling model (host code of the library)

@@ -9,11 +9,11 @@ HERE = Path(__file__).resolve().parent
 CSRC = HERE / "csrc"
 LIB = HERE / "libpipesd.so"
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-              "-shared", "-Xcompiler", "-fPIC", "--use_fast_math=false"]
+              "-shared", "-Xcompiler", "-fPIC", "--threads", "0", "--use_fast_math=false"]
 
 
 def _sources():
-    return sorted(CSRC.glob("*.cu")) , sorted(list(CSRC.glob("*.cuh")) + [HERE.parent / "include" / "pipesd.h"])
+    return sorted(CSRC.rglob("*.cu")), sorted(list(CSRC.rglob("*.cuh")) + [HERE.parent / "include" / "pipesd.h"])
 
 
 def build_cuda(force: bool = False, verbose: bool = False) -> Path:

@@ -1,0 +1,216 @@
+// A paged K/V cache held in 4 bits, and the attention of short chunks of query rows over it.
+//
+// Values: the columns of a (position, head) row are cut into groups of 32 that share a zero z = bf16(min) and a scale
+// s = bf16((max - z) / 15); a value is held as the code c = clamp(rint((x - z) / s), 0, 15) and stands for s * c + z.
+//
+// Layout of one layer: [page][KV head][unit], a unit being 16 positions of one head in 20 * HD contiguous bytes:
+//   K codes   8 HD   [position 16][t 4][group]      32-bit words, nibble p = column 32 group + 8 t + p
+//   K s, z    2 HD   [position 16][group]           bf16 pairs
+//   V codes   8 HD   [tile / 4][g 8][t 4][tile % 4] words, tile = 16 columns; nibble p = column 16 tile + g + 8 (p & 1) of position
+//                                                   2 t + (p >> 2) + 8 (p >> 1 & 1)
+//   V s       HD     [group][position 16]           bf16
+//   V z       HD     [group][position 16]           bf16
+// Both code orders are those of the A operand of mma.m16n8k16 (lane 4 g + t): a word ANDed with 0x000f000f is a register of
+// the operand, the same after shifts by 8, and with 0x00f000f0 another one.  Read as bf16 such a register holds the whole numbers
+// n < 256 times 2^-133 (subnormals: the exponent fields 0 and 1 are one linear range), so that a code needs one AND (and a shift for
+// every second one) and no conversion.  The factor 16 of the odd nibbles goes into Q, or into the step that centres V's codes.
+#pragma once
+#include "../common.cuh"
+
+namespace pipesd {
+
+constexpr int kKv4Unit = 16;                       // positions of a unit
+constexpr int kKv4Group = 32;                      // columns of a scale
+constexpr float kKv4Limit = 281474976710656.f;     // 2^48: larger values are held as this; a NaN as 0
+
+__host__ __device__ constexpr int kv4_unit_bytes(int hd) { return 20 * hd; }
+__host__ __device__ constexpr int kv4_k_scales(int hd) { return 8 * hd; }
+__host__ __device__ constexpr int kv4_v_codes(int hd) { return 10 * hd; }
+__host__ __device__ constexpr int kv4_v_scales(int hd) { return 18 * hd; }
+
+// Where the requests of a call are: request r has the rows row0[r] .. row0[r + 1] - 1, at the positions base[r] ... of its pages.
+struct Kv4Where {
+    const int32_t *row0, *base, *table;
+    int n_req, rows, n_pages, max_pages, page_size, Hkv;
+};
+
+// New rows and base of a request; a request whose numbers make no sense has none.
+__device__ __forceinline__ int kv4_rows(const Kv4Where& w, int r, int& first, int& base) {
+    first = w.row0[r];
+    base = w.base[r];
+    const int end = w.row0[r + 1];
+    if (first < 0 || end < first || end > w.rows || base < 0) return 0;
+    return min(end - first, max(0, w.max_pages * w.page_size - base));      // rows behind the table's last position are dropped
+}
+
+// Address of a unit of a request, or null where no page is mapped.
+__device__ __forceinline__ unsigned char* kv4_unit(unsigned char* pool, const Kv4Where& w, int r, int head, int unit, int hd) {
+    const int pos = unit * kKv4Unit, page = w.table[(size_t)r * w.max_pages + pos / w.page_size];
+    if (page < 0 || page >= w.n_pages) return nullptr;
+    return pool + (((size_t)page * w.Hkv + head) * (w.page_size / kKv4Unit) + pos % w.page_size / kKv4Unit) * kv4_unit_bytes(hd);
+}
+
+__device__ __forceinline__ float kv4_in(float x) { return x == x ? fminf(fmaxf(x, -kKv4Limit), kKv4Limit) : 0.f; }
+__device__ __forceinline__ void kv4_load8(const float* p, float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = kv4_in(p[i]);
+}
+__device__ __forceinline__ void kv4_load8(const uint16_t* p, float (&x)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = kv4_in(bf16_bits_to_f32(p[i]));
+}
+
+struct Kv4AppendArgs {
+    Kv4Where w;
+    const void *k, *v;
+    long long k_stride, v_stride;      // elements between rows
+    unsigned char* pool;
+};
+
+// One CTA per (unit that gets new rows, KV head): 8 columns of a row per thread; four neighbouring threads hold a group.
+// A unit's V words hold two to eight positions each, so the CTA owns the unit and keeps the nibbles of the positions before its rows.
+constexpr int kKv4AppendThreads = 256;
+template <int HD, typename T>
+__global__ void __launch_bounds__(kKv4AppendThreads) kv4_append_kernel(const Kv4AppendArgs a) {
+    constexpr int kPieces = HD / 8, kGroups = HD / kKv4Group, kTasks = kKv4Unit * kPieces;
+    __shared__ int s_req, s_unit;
+    __shared__ uint32_t codes[kKv4Unit][HD / 8];           // of V: [position][8 columns]
+    __shared__ uint32_t s_sz[kKv4Unit][kGroups];
+    const int tid = threadIdx.x, head = blockIdx.y;
+    if (tid < 32) {                                        // the blockIdx.x-th unit of the requests' units in order
+        int left = blockIdx.x, found = -1, unit = 0;
+        for (int r0 = 0; r0 < a.w.n_req && found < 0; r0 += 32) {
+            int first, base = 0, n = 0;
+            if (r0 + tid < a.w.n_req) n = kv4_rows(a.w, r0 + tid, first, base);
+            const int u0 = base / kKv4Unit, cnt = n > 0 ? (base + n - 1) / kKv4Unit - u0 + 1 : 0;
+            int inc = cnt;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int t = __shfl_up_sync(0xffffffffu, inc, o);
+                if (tid >= o) inc += t;
+            }
+            const unsigned hit = __ballot_sync(0xffffffffu, left < inc);
+            if (hit) {
+                const int l = __ffs(hit) - 1;
+                found = r0 + l;
+                unit = __shfl_sync(0xffffffffu, u0 + left - (inc - cnt), l);
+            } else {
+                left -= __shfl_sync(0xffffffffu, inc, 31);
+            }
+        }
+        if (tid == 0) { s_req = found; s_unit = unit; }
+    }
+    __syncthreads();
+    const int req = s_req, unit = s_unit;
+    if (req < 0) return;
+    int first, base;
+    const int n = kv4_rows(a.w, req, first, base);
+    unsigned char* dst = kv4_unit(a.pool, a.w, req, head, unit, HD);
+    if (!dst) return;                                      // no page there: the rows are dropped
+    const int lo = max(0, base - unit * kKv4Unit), hi = min(kKv4Unit, base + n - unit * kKv4Unit);     // new positions of the unit
+    for (int task = tid; task < 2 * kTasks; task += kKv4AppendThreads) {
+        const int kv = task / kTasks, slot = task % kTasks / kPieces, piece = task % kPieces;
+        if (slot < lo || slot >= hi) continue;             // the four threads of a group leave together
+        const size_t row = (size_t)(first + unit * kKv4Unit + slot - base);
+        const T* src = static_cast<const T*>(kv ? a.v : a.k) + row * (kv ? a.v_stride : a.k_stride) + (size_t)head * HD + piece * 8;
+        float x[8];
+        kv4_load8(src, x);
+        float mn = x[0], mx = x[0];
+#pragma unroll
+        for (int i = 1; i < 8; ++i) { mn = fminf(mn, x[i]); mx = fmaxf(mx, x[i]); }
+        const unsigned quad = 0xfu << (tid & 28);
+#pragma unroll
+        for (int o = 1; o < 4; o <<= 1) {
+            mn = fminf(mn, __shfl_xor_sync(quad, mn, o));
+            mx = fmaxf(mx, __shfl_xor_sync(quad, mx, o));
+        }
+        const uint16_t zb = f32_to_bf16_bits(mn);
+        const double z = (double)bf16_bits_to_f32(zb);
+        const uint16_t sb = f32_to_bf16_bits((float)(((double)mx - z) / 15.0));
+        const double s = (double)bf16_bits_to_f32(sb);
+        uint32_t word = 0;
+        if (s > 0.0)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) word |= (uint32_t)fmin(fmax(rint(((double)x[i] - z) / s), 0.0), 15.0) << (4 * i);
+        const int group = piece >> 2, t = piece & 3;
+        if (kv == 0) {
+            *reinterpret_cast<uint32_t*>(dst + slot * (HD / 2) + (t * kGroups + group) * 4) = word;
+            if (t == 0) *reinterpret_cast<uint32_t*>(dst + kv4_k_scales(HD) + (slot * kGroups + group) * 4) = pack2(sb, zb);
+        } else {
+            codes[slot][piece] = word;
+            if (t == 0) s_sz[slot][group] = pack2(sb, zb);
+        }
+    }
+    __syncthreads();
+    if (tid < kKv4Unit * kGroups) {
+        const int group = tid / kKv4Unit, slot = tid % kKv4Unit;
+        if (slot >= lo && slot < hi) {
+            const uint32_t sz = s_sz[slot][group];
+            reinterpret_cast<uint16_t*>(dst + kv4_v_scales(HD))[tid] = (uint16_t)sz;
+            reinterpret_cast<uint16_t*>(dst + kv4_v_scales(HD) + HD)[tid] = (uint16_t)(sz >> 16);
+        }
+    }
+    for (int i = tid; i < 2 * HD; i += kKv4AppendThreads) {
+        const int tile = i / 128 * 4 + i % 4, lane = i / 4 % 32, g = lane / 4, t = lane % 4;
+        uint32_t* p = reinterpret_cast<uint32_t*>(dst + kv4_v_codes(HD)) + i;
+        uint32_t word = 0, fresh = 0;
+#pragma unroll
+        for (int nib = 0; nib < 8; ++nib) {
+            const int slot = 2 * t + (nib >> 2) + 8 * (nib >> 1 & 1);
+            if (slot < lo || slot >= hi) continue;
+            fresh |= 15u << (4 * nib);
+            word |= (codes[slot][tile * 2 + (nib & 1)] >> (4 * g) & 15u) << (4 * nib);
+        }
+        if (fresh) *p = fresh == 0xffffffffu ? word : (*p & ~fresh) | word;
+    }
+}
+
+struct Kv4ReadArgs {
+    Kv4Where w;
+    unsigned char* pool;
+    float *k, *v;              // [rows][Hkv][HD]
+};
+
+// The values of the positions that belong to the rows: one warp per (row, KV head) and step; 0 where no page is mapped.
+template <int HD>
+__global__ void __launch_bounds__(256) kv4_read_kernel(const Kv4ReadArgs a) {
+    constexpr int kPieces = HD / 8, kGroups = HD / kKv4Group;
+    const int row = blockIdx.x;
+    __shared__ int s_req;
+    if (threadIdx.x == 0) s_req = -1;
+    __syncthreads();
+    for (int i = threadIdx.x; i < a.w.n_req; i += 256)
+        if (a.w.row0[i] <= row && row < a.w.row0[i + 1]) s_req = i;
+    __syncthreads();
+    if (s_req < 0) return;
+    int first, base;
+    const int n = kv4_rows(a.w, s_req, first, base), pos = base + row - first;
+    const bool in = row - first < n;
+    for (int task = threadIdx.x; task < 2 * a.w.Hkv * kPieces; task += 256) {
+        const int kv = task / (a.w.Hkv * kPieces), head = task / kPieces % a.w.Hkv, piece = task % kPieces, group = piece >> 2, slot = pos % kKv4Unit;
+        const unsigned char* u = in ? kv4_unit(a.pool, a.w, s_req, head, pos / kKv4Unit, HD) : nullptr;
+        float x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = 0.f;
+        if (u && kv == 0) {
+            const uint32_t word = *reinterpret_cast<const uint32_t*>(u + slot * (HD / 2) + ((piece & 3) * kGroups + group) * 4);
+            const uint32_t sz = *reinterpret_cast<const uint32_t*>(u + kv4_k_scales(HD) + (slot * kGroups + group) * 4);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = fmaf((float)(word >> (4 * i) & 15u), __uint_as_float(sz << 16), __uint_as_float(sz & 0xffff0000u));
+        } else if (u) {
+            const uint16_t* sz = reinterpret_cast<const uint16_t*>(u + kv4_v_scales(HD)) + group * kKv4Unit + slot;
+            const float s = bf16_bits_to_f32(sz[0]), z = bf16_bits_to_f32(sz[HD / 2]);
+            const int tile = piece >> 1, nib = (piece & 1) + 2 * (slot >> 3) + 4 * (slot & 1), t = slot % 8 / 2;
+#pragma unroll
+            for (int g = 0; g < 8; ++g) {
+                const uint32_t word = reinterpret_cast<const uint32_t*>(u + kv4_v_codes(HD))[(tile / 4 * 32 + g * 4 + t) * 4 + tile % 4];
+                x[g] = fmaf((float)(word >> (4 * nib) & 15u), s, z);
+            }
+        }
+        float4* out = reinterpret_cast<float4*>((kv ? a.v : a.k) + ((size_t)row * a.w.Hkv + head) * HD + piece * 8);
+        out[0] = make_float4(x[0], x[1], x[2], x[3]);
+        out[1] = make_float4(x[4], x[5], x[6], x[7]);
+    }
+}
+
+}  // namespace pipesd
