@@ -1,0 +1,294 @@
+"""Shaped sampling and acceptance (pipesd_sample, pipesd_accept) against 64-bit numpy."""
+import numpy as np
+import pytest
+
+from oracle import serving
+
+pytestmark = pytest.mark.gpu
+
+NEAR = 1e-9     # masses are rounded to 2^-46 of the most likely id's weight: over 2^18 ids a border moves by less than this
+
+
+def _cuda(a, dtype=None):
+    import torch
+    t = torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    return t if dtype is None else t.to(dtype)
+
+
+def _rng_rows(rng, rows, vocab, kind):
+    if kind == "peaked":
+        x = rng.standard_normal((rows, vocab)) * 2
+        for r in range(rows):
+            x[r, rng.integers(0, vocab, 20)] += rng.uniform(2, 9, 20)
+    elif kind == "flat":
+        x = rng.standard_normal((rows, vocab)) * 0.01
+    elif kind == "ties":
+        x = rng.integers(-2, 3, (rows, vocab)).astype(np.float64)
+    elif kind == "equal":
+        x = np.full((rows, vocab), -0.0)
+        x[:, ::2] = 0.0
+    elif kind == "banned":      # most of the row masked: -inf and the type's lowest value
+        x = rng.standard_normal((rows, vocab)) * 3
+        x[rng.random((rows, vocab)) < 0.9] = -np.inf
+        x[rng.random((rows, vocab)) < 0.5] = -3.3e38
+        x[:, rng.integers(0, vocab)] = 0.25
+    else:                       # a huge range
+        x = rng.standard_normal((rows, vocab)) * 1e4
+    return x.astype(np.float32)
+
+
+def _settings(rng, rows, vocab):
+    t = rng.choice([0.0, 1.0, 0.7, 0.3, 1.7, 1e-6, 50.0], rows)
+    k = rng.choice([0, 0, 1, 2, 40, vocab - 1, vocab, vocab + 5, -3], rows)
+    p = rng.choice([1.0, 1.0, 2.0, 0.9, 0.5, 0.999, 1 - 2.0 ** -24, 1e-6], rows)
+    m = rng.choice([0.0, 0.0, 0.05, 0.5, 1.0, 1e-6], rows)
+    return t.astype(np.float32), k.astype(np.int32), p.astype(np.float32), m.astype(np.float32)
+
+
+def _check(logits, settings, u, tokens, probs=None):
+    for r in range(len(logits)):
+        s = [v[r] for v in settings]
+        w = serving.shaped(logits[r], *s)
+        if w is None or not 0 <= u[r] < 1:
+            assert tokens[r] == -1
+            if probs is not None:
+                assert (probs[r] == 0).all()
+            continue
+        token, margin = serving.draw(w, u[r])
+        assert tokens[r] == token or margin < NEAR, f"row {r}: {tokens[r]} for {token}, settings {s}, margin {margin}"
+        if probs is not None:
+            want = w / w.sum()
+            # one rounding to fp32 (2^-24) and the sum's 2^-46 per id; below fp32's range the values are its subnormals
+            assert (np.abs(probs[r] - want) <= want * (2.0 ** -24 + len(w) * 2.0 ** -46) + 2.0 ** -149).all(), f"row {r}: settings {s}"
+
+
+@pytest.mark.parametrize("kind", ["peaked", "flat", "ties", "equal", "banned", "range"])
+@pytest.mark.parametrize("rows,vocab", [(7, 1), (7, 2), (9, 31), (40, 33), (33, 1000), (6, 4099), (17, 8192), (5, 32000), (40, 32001), (3, 50257)])
+def test_sample_matches(rows, vocab, kind):
+    import torch
+    from paper_2605_13319_b200 import binding
+    rng = np.random.default_rng(vocab * 7 + rows)
+    x, settings = _rng_rows(rng, rows, vocab, kind), _settings(rng, rows, vocab)
+    u = (rng.integers(0, 1 << 24, rows) * 2.0 ** -24).astype(np.float32)
+    u[0], u[-1] = 0.0, 1 - 2.0 ** -24
+    t, k, p, m = settings
+    shaping = binding.shaping(rows, temperature=t, top_k=k, top_p=p, min_p=m)
+    for dtype in (torch.float32, torch.bfloat16):
+        logits = _cuda(x, dtype)
+        probs = torch.full((rows, vocab), float("nan"), device="cuda")
+        tokens = binding.sample(logits, shaping, _cuda(u), probs=probs)
+        again = binding.sample(logits, shaping, _cuda(u))
+        assert torch.equal(tokens, again)
+        _check(logits.float().cpu().numpy(), settings, u, tokens.cpu().numpy(), probs.cpu().numpy())
+
+
+@pytest.mark.parametrize("rows", [1, 2, 30, 60, 130, 320])
+def test_sample_large_vocabulary_every_cluster_size(rows):
+    """The number of CTAs per row follows the number of rows; results do not."""
+    import torch
+    from paper_2605_13319_b200 import binding
+    rng = np.random.default_rng(rows)
+    vocab = 128256
+    x = torch.randn((rows, vocab), generator=torch.Generator("cuda").manual_seed(rows), device="cuda") * 2
+    settings = _settings(rng, rows, vocab)
+    u = (rng.integers(0, 1 << 24, rows) * 2.0 ** -24).astype(np.float32)
+    t, k, p, m = settings
+    shaping = binding.shaping(rows, temperature=t, top_k=k, top_p=p, min_p=m)
+    tokens = binding.sample(x, shaping, _cuda(u))
+    some = rng.permutation(rows)[:12]
+    _check(x[some].cpu().numpy(), [v[some] for v in settings], u[some], tokens.cpu().numpy()[some])
+    for r in some[:3]:     # a row alone
+        assert binding.sample(x[r:r + 1], shaping[r:r + 1].contiguous(), _cuda(u[r:r + 1])).item() == tokens[r].item()
+
+
+def test_sample_most_ids_there_can_be():
+    import torch
+    from paper_2605_13319_b200 import binding
+    x = torch.randn((2, 1 << 18), generator=torch.Generator("cuda").manual_seed(3), device="cuda")
+    x[1] = 1.5                                                       # all alike: the sum is 2^63
+    u = np.array([0.37, 0.75], np.float32)
+    tokens = binding.sample(x, binding.shaping(2, top_p=[0.9, 1.0]), _cuda(u)).cpu().numpy()
+    _check(x.cpu().numpy(), [np.float32([1, 1]), np.int32([0, 0]), np.float32([0.9, 1]), np.float32([0, 0])], u, tokens)
+    assert tokens[1] == 3 << 16
+
+
+def test_sample_rows_without_a_distribution():
+    import torch
+    from paper_2605_13319_b200 import binding
+    V, rows = 5000, 14
+    x = np.random.default_rng(0).standard_normal((rows, V)).astype(np.float32)
+    x[0] = -np.inf
+    x[1, 4999] = np.nan
+    x[2, 17] = np.inf
+    x[3, 0] = -np.nan
+    u = np.full(rows, 0.5, np.float32)
+    u[4], u[5], u[6] = 1.0, -0.1, np.nan
+    shaping = binding.shaping(rows)
+    bits = shaping.cpu().numpy().copy()
+    for r, (col, v) in {7: (0, -1.0), 8: (0, np.nan), 9: (0, np.inf), 10: (2, 0.0), 11: (2, np.nan), 12: (3, 1.01)}.items():
+        bits[r, col] = np.float32(v).view(np.int32)
+    probs = torch.full((rows, V), 7.0, device="cuda")
+    tokens = binding.sample(_cuda(x), _cuda(bits), _cuda(u), probs=probs).cpu().numpy()
+    assert (tokens[:13] == -1).all() and 0 <= tokens[13] < V
+    assert (probs[:13] == 0).all() and abs(probs[13].sum().item() - 1) < 1e-5
+
+
+@pytest.mark.parametrize("offset,ld", [(0, 1024), (1, 1031), (3, 1001), (4, 1004)])
+def test_sample_strides_and_what_lies_between_rows(offset, ld):
+    import torch
+    from paper_2605_13319_b200 import binding
+    rows, V = 9, 1000
+    rng = np.random.default_rng(ld)
+    settings = _settings(rng, rows, V)
+    u = (rng.integers(0, 1 << 24, rows) * 2.0 ** -24).astype(np.float32)
+    t, k, p, m = settings
+    shaping = binding.shaping(rows, temperature=t, top_k=k, top_p=p, min_p=m)
+    for dtype in (torch.float32, torch.bfloat16):
+        flat = torch.full((rows * ld + offset + 8,), float("nan"), device="cuda", dtype=dtype)          # NaN wherever there is no logit
+        logits = flat[offset:].as_strided((rows, V), (ld, 1))
+        logits.copy_(_cuda(_rng_rows(rng, rows, V, "peaked")))
+        out = torch.full((rows * ld + offset + 8,), 5.0, device="cuda")
+        probs = out[offset:].as_strided((rows, V), (ld, 1))
+        tokens = binding.sample(logits, shaping, _cuda(u), probs=probs)
+        _check(logits.float().cpu().numpy(), settings, u, tokens.cpu().numpy(), probs.cpu().numpy())
+        probs.fill_(5.0)
+        assert (out == 5.0).all()
+
+
+def test_sample_in_a_graph_and_on_other_streams():
+    import torch
+    from paper_2605_13319_b200 import binding
+    rows, V = 20, 32000
+    g = torch.Generator("cuda").manual_seed(1)
+    logits, u = torch.randn((rows, V), generator=g, device="cuda") * 2, torch.rand(rows, generator=g, device="cuda")
+    shaping, tokens = binding.shaping(rows, top_p=0.8, top_k=1000), torch.zeros(rows, dtype=torch.int32, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        binding.sample(logits, shaping, u, tokens=tokens)
+    for seed in (2, 3):
+        logits.copy_(torch.randn((rows, V), generator=g, device="cuda") * 2)
+        graph.replay()
+        want = binding.sample(logits, shaping, u)
+        assert torch.equal(tokens, want)
+        streams = [torch.cuda.Stream() for _ in range(3)]
+        torch.cuda.synchronize()
+        got = [binding.sample(logits, shaping, u, stream=s) for s in streams for _ in range(4)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, want) for x in got)
+
+
+# --------------------------------------------------------------------------- acceptance
+def _rounds(rng, ks, vocab, sharp):
+    """Logits of all rows, q and drafts (from q) of all drafts, uniforms."""
+    rows = sum(ks) + len(ks)
+    logits = (rng.standard_normal((rows, vocab)) * 2).astype(np.float32)
+    q, drafts, at = [], [], 0
+    for k in ks:
+        for i in range(k):
+            e = logits[at + i].astype(np.float64) + sharp * rng.standard_normal(vocab)
+            e = np.exp(e - e.max())
+            e[e < np.sort(e)[-min(vocab, 50)]] = 0
+            q.append((e / e.sum()).astype(np.float32))
+            drafts.append(rng.choice(vocab, p=e / e.sum()))
+        at += k + 1
+    u = (rng.integers(0, 1 << 24, rows) * 2.0 ** -24).astype(np.float32)
+    return logits, np.array(q, np.float32).reshape(-1, vocab), np.array(drafts, np.int32), u
+
+
+@pytest.mark.parametrize("vocab", [16, 1000, 1024, 32000, 50257])
+@pytest.mark.parametrize("ks", [[1], [8], [0, 3, 16, 1, 0, 5, 2], [31, 40]])
+def test_accept_matches(vocab, ks):
+    import torch
+    from paper_2605_13319_b200 import binding
+    rng = np.random.default_rng(vocab + len(ks))
+    for trial, sharp in enumerate([0.1, 0.7, 2.0]):
+        logits, q, drafts, u = _rounds(rng, ks, vocab, sharp)
+        row0 = np.concatenate([[0], np.cumsum(np.array(ks) + 1)]).astype(np.int32)
+        t, k, p, m = _settings(rng, len(ks), vocab)
+        if trial == 0:
+            t, k, p, m = (np.full(len(ks), v) for v in (np.float32(1), np.int32(0), np.float32(1), np.float32(0)))
+        shaping = binding.shaping(len(ks), temperature=t, top_k=k, top_p=p, min_p=m)
+        for dtype in (torch.float32, torch.bfloat16):
+            dev = _cuda(logits, dtype)
+            n, token = binding.accept(dev, _cuda(row0), shaping, _cuda(q), _cuda(drafts), _cuda(u))
+            n2, token2 = binding.accept(dev, _cuda(row0), shaping, _cuda(q), _cuda(drafts), _cuda(u))
+            assert torch.equal(n, n2) and torch.equal(token, token2)
+            x = dev.float().cpu().numpy()
+            for r in range(len(ks)):
+                a, b, first = row0[r], row0[r + 1], row0[r] - r
+                want = serving.accept(x[a:b], (t[r], k[r], p[r], m[r]), q[first:first + ks[r]], drafts[first:first + ks[r]], u[a:b])
+                assert (n[r].item(), token[r].item()) == want[:2] or want[2] < NEAR, (r, want)
+
+
+def test_accept_without_drafts_and_odd_requests():
+    import torch
+    from paper_2605_13319_b200 import binding
+    rng = np.random.default_rng(5)
+    V, n = 3001, 6
+    x = rng.standard_normal((n, V)).astype(np.float32)
+    u = rng.random(n).astype(np.float32)
+    s = binding.shaping(n, top_k=20)
+    got, token = binding.accept(_cuda(x), torch.arange(n + 1, dtype=torch.int32, device="cuda"), s, None, None, _cuda(u))
+    assert (got == 0).all() and torch.equal(token, binding.sample(_cuda(x), s, _cuda(u)))
+    # P = q wherever q is: nothing is left to correct with, a rejected draft (outside of the vocabulary) falls back to P
+    row = rng.standard_normal((2, V)).astype(np.float32)
+    P = serving.shaped(row[0], 1.0, 20)
+    q = np.where(P > 0, 1.0, 0.0).astype(np.float32)[None]
+    for draft in (-1, V, 1 << 30):
+        u2 = np.array([0.0, 0.6], np.float32)
+        got, token = binding.accept(_cuda(row), _cuda(np.int32([0, 2])), binding.shaping(1, top_k=20), _cuda(q), _cuda(np.int32([draft])), _cuda(u2))
+        assert got.item() == 0 and token.item() == serving.draw(P, u2[1])[0]
+    # a row without a distribution ends the round there; a bad final uniform gives no token; entries of row0 that make no sense: no round
+    rows = rng.standard_normal((9, V)).astype(np.float32)
+    rows[1] = -np.inf
+    qq = np.full((6, V), 1e-9, np.float32)                          # accepts any draft of the support
+    drafts = rows[[0, 1, 3, 4, 6, 7]].argmax(1).astype(np.int32)
+    u3 = np.full(9, 0.5, np.float32)
+    u3[5] = np.nan
+    s3 = binding.shaping(3)
+    got, token = binding.accept(_cuda(rows), _cuda(np.int32([0, 3, 6, 9])), s3, _cuda(qq), _cuda(drafts), _cuda(u3))
+    assert got.tolist() == [1, 2, 2] and token[0].item() == -1 and token[1].item() == -1 and token[2].item() >= 0
+    for bad in ([0, 3, 2, 9], [-1, 3, 6, 9], [0, 3, 6, 12], [0, 0, 6, 9]):
+        got, token = binding.accept(_cuda(rows), _cuda(np.int32(bad)), s3, _cuda(qq), _cuda(drafts), _cuda(u3))
+        for r in range(3):
+            if bad[r] < 0 or bad[r + 1] > 9 or bad[r + 1] <= bad[r]:
+                assert got[r].item() == 0 and token[r].item() == -1
+
+
+def test_greedy_settings_are_the_greedy_rule():
+    import torch
+    from paper_2605_13319_b200 import binding
+    rng = np.random.default_rng(8)
+    V, k = 1024, 6
+    for cut in range(k + 1):
+        x = rng.standard_normal((k + 1, V)).astype(np.float32)
+        drafts = x.argmax(1)[:k].astype(np.int32)
+        if cut < k:
+            drafts[cut] = (drafts[cut] + 5) % V
+        q = np.zeros((k, V), np.float32)
+        q[np.arange(k), drafts] = 1
+        u = rng.random(k + 1).astype(np.float32)
+        n, token = binding.accept(_cuda(x), _cuda(np.int32([0, k + 1])), binding.shaping(1, temperature=0.0), _cuda(q), _cuda(drafts), _cuda(u))
+        assert (n.item(), token.item()) == (cut, x[cut].argmax())
+
+
+def test_draft_and_accept_leave_the_target_distribution():
+    """One draft per request, sampled by pipesd_sample with its settings, verified by pipesd_accept with the target's: the first
+    emitted token follows the target's shaped distribution whatever the draft's is."""
+    import torch
+    from paper_2605_13319_b200 import binding
+    V, n = 24, 40000
+    g = torch.Generator("cuda").manual_seed(4)
+    edge, target, bonus = (torch.randn(V, generator=g, device="cuda") * 1.5 for _ in range(3))
+    q = torch.empty((n, V), device="cuda")
+    drafts = binding.sample(edge.expand(n, V).contiguous(), binding.shaping(n, temperature=0.8, top_k=12), torch.rand(n, generator=g, device="cuda"), probs=q)
+    logits = torch.stack([target, bonus]).repeat(n, 1)
+    row0 = torch.arange(0, 2 * n + 1, 2, dtype=torch.int32, device="cuda")
+    acc, token = binding.accept(logits, row0, binding.shaping(n, temperature=1.2, top_p=0.9), q, drafts, torch.rand(2 * n, generator=g, device="cuda"))
+    first = torch.where(acc == 1, drafts, token).cpu().numpy()
+    w = serving.shaped(target.cpu().numpy(), 1.2, 0, 0.9)
+    P = w / w.sum()
+    share = np.bincount(first, minlength=V) / n
+    assert (share[P == 0] == 0).all()
+    assert (np.abs(share - P) <= 5 * np.sqrt(P * (1 - P) / n) + 1e-12).all()      # five standard deviations of a frequency
+    assert 0 < acc.float().mean().item() < 1
