@@ -42,8 +42,34 @@ __device__ __forceinline__ unsigned long long order_key(float l, int id) {
     return (unsigned long long)s << 32 | (uint32_t)~id;
 }
 
+__device__ __forceinline__ float key_logit(unsigned long long key) {
+    const uint32_t b = (uint32_t)(key >> 32);
+    return __uint_as_float(b & 0x80000000u ? b ^ 0x80000000u : ~b);
+}
+
 __device__ __forceinline__ double shape_exponent(float l, const RowShape& r) { return fmax(((double)l - r.m) * r.c, -1000.0); }
-__device__ __forceinline__ unsigned long long shape_mass(double y) { return (unsigned long long)__double2ull_rn(exp2(y) * kMassOne); }
+// 2^y for -1000 <= y <= 0: whole part into the exponent, the rest by a polynomial of degree 10 (interpolation at the Chebyshev
+// nodes of [-1/2, 1/2], coefficients computed in 70 digits: relative error 3e-16, 2^0 = 1 exactly).
+__device__ __forceinline__ double shape_exp2(double y) {
+    const double big = 6755399441055744.0;         // 1.5 * 2^52: the sum's low bits are the rounded y
+    const double n = y + big, r = y - (n - big);
+    double p = 7.072585949269223e-09;
+    p = fma(p, r, 1.0208690299958306e-07);
+    p = fma(p, r, 1.321544258792169e-06);
+    p = fma(p, r, 1.5252657260200837e-05);
+    p = fma(p, r, 0.0001540353044173605);
+    p = fma(p, r, 0.0013333558230164974);
+    p = fma(p, r, 0.009618129107606888);
+    p = fma(p, r, 0.05550410866444772);
+    p = fma(p, r, 0.24022650695910097);
+    p = fma(p, r, 0.69314718055995);
+    p = fma(p, r, 1.0);
+    return __hiloint2double(__double2hiint(p) + (__double2loint(n) << 20), __double2loint(p));
+}
+// A weight as a whole number of 2^-45: 128 + w has exactly those last bits.
+__device__ __forceinline__ unsigned long long shape_mass(double y) {
+    return (unsigned long long)(__double_as_longlong(shape_exp2(y) + 128.0) - __double_as_longlong(128.0));
+}
 __device__ __forceinline__ bool shape_keeps(float l, int id, const RowShape& r) {
     return order_key(l, id) >= r.bound && shape_exponent(l, r) >= r.y_min;
 }
@@ -86,12 +112,27 @@ __device__ __forceinline__ unsigned long long shape_peer(const unsigned long lon
     asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(dsmem_addr(smem_u32(p), (uint32_t)rank)) : "memory");
     return v;
 }
+template <int C>
+__device__ __forceinline__ int shape_peer_i32(const int* p, int rank) {
+    if (C == 1) return *p;
+    int v;
+    asm volatile("ld.shared::cluster.s32 %0, [%1];" : "=r"(v) : "r"(dsmem_addr(smem_u32(p), (uint32_t)rank)) : "memory");
+    return v;
+}
 
+constexpr int kShapeList = 1024;                   // ids that are dealt with one by one
+constexpr int kDrawBatch = 4;
 struct ShapeSmem {
-    unsigned long long hist[2][kShapeBins];        // a level's bins; levels take turns, so that one barrier per level is enough
-    unsigned long long part[kShapeWarps];
-    unsigned long long cta[2];                     // what the other CTAs of the cluster read: key maximum, kept mass
-    unsigned long long found[3];                   // bin, sum above it, level's sum
+    union {                                        // bins of a row: of the first pass (32 bits) and of the second one, or of a digit
+        struct { uint32_t coarse[kShapeBins]; unsigned long long fine[kShapeBins / 2]; };
+        unsigned long long digit[kShapeBins];
+    };
+    unsigned long long own[kShapeList];            // keys that this CTA collected
+    unsigned long long keys[kShapeList], mass[kShapeList];     // the cluster's, and their masses
+    unsigned long long part[kShapeWarps], part2[kShapeWarps];
+    unsigned long long cta[4];                     // what the other CTAs of the cluster read: key maximum, kept mass, masses of a window
+    unsigned long long found[3];
+    int n_own, window[2];
 };
 
 // Walks this warp's ids of the row, VEC neighbours per lane and step, kBatch steps' loads in flight together.
@@ -120,24 +161,47 @@ __device__ __forceinline__ void shape_walk(const T* row, int j0, int j1, F&& f) 
     }
 }
 
-// The key at which a running sum over the order, of ones (kMass false) or of masses, first reaches `need`: everything from it upwards
-// is kept.  Radix descent over the key's digits (32 bits of logit, 22 of id), among keys >= floor_.  Returns floor_ if the whole sum stays
-// below `need`.
+// Sum (kMax: maximum) over the CTA; every thread gets it.  `part` is not used again before the next barrier but one.
+template <bool kMax>
+__device__ __forceinline__ unsigned long long cta_reduce_u64(unsigned long long v, unsigned long long* part) {
+    v = kMax ? warp_max_u64(v) : warp_sum_u64(v);
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = part[0];
+#pragma unroll
+    for (int w = 1; w < kShapeWarps; ++w) v = kMax ? (part[w] > v ? part[w] : v) : v + part[w];
+    return v;
+}
+
+// Finding the bound.  A cut of the order is the key at which a running sum over it (of ones: top-k; of masses: top-p) first reaches
+// `need`; everything from there upwards is kept.
+//
+// The usual way has two or three passes over the row.  First bins of equal width in the logit, counted by 32-bit atomics; for
+// masses a bin adds up w / (weight of its middle), which lies within 1 / 128 of 1, as whole numbers of 2^-13: its mass is then known
+// to kShapeSlack.  That settles a window of bins that holds the cut for certain, mostly one.  For top-k the window is exact.
+// Then, unless top-k's window is short, a pass that computes the masses proper: their sums above, in and below the window, and in
+// kFine finer bins of it (64-bit atomics, few of them).  What is left, the ids of one fine bin, is collected and compared
+// with each other.  Where more than kShapeList ids are left (thousands of equal logits, a cut in the far tail) shape_select_digits
+// takes over, which needs no luck: digit by digit over the whole key.
+constexpr int kShapeFine = kShapeBins / 2;
+constexpr double kShapeSlack = 1e-4;               // half a step of 2^-13 (6.1e-5), and what fp32 loses of the bin's position (4e-6) and weight
+constexpr float kShapeWidth = 64.f;                // bins per unit of the exponent (top-p) or of the logit (top-k)
+
 template <int C, bool kMass, typename T, int VEC>
-__device__ unsigned long long shape_select(const T* row, int j0, int j1, const RowShape& r, unsigned long long floor_, unsigned long long need,
-                                           double need_share, ShapeSmem& sm, int& turn) {
+__device__ __noinline__ unsigned long long shape_select_digits(const T* row, int j0, int j1, const RowShape& r, unsigned long long floor_, unsigned long long need,
+                                                               double need_share, ShapeSmem& sm) {
     const int tid = threadIdx.x;
     unsigned long long prefix = 0;
     int known = 0;                                 // leading bits of the key that are settled
-    constexpr int kBits[5] = {11, 11, 10, 11, 11};
 #pragma unroll 1
-    for (int level = 0; level < 5; ++level) {
-        if (level == 3) {                          // ids are below 2^22: ten more bits are ones
+    for (int level = 0; level < 5; ++level) {      // 32 bits of logit: 11, 11, 10; ids: 11, 11, above them ten ones
+        if (level == 3) {
             prefix = prefix << 10 | 1023u;
             known += 10;
         }
-        const int bits = kBits[level], shift = 64 - known - bits;
-        unsigned long long* hist = sm.hist[turn & 1];
+        const int bits = level == 2 ? 10 : 11, shift = 64 - known - bits;
+        unsigned long long* hist = sm.digit;
+        shape_sync<C>();                           // nobody reads what was here before
         for (int b = tid; b < kShapeBins; b += kShapeThreads) hist[b] = 0;
         __syncthreads();
         shape_walk<T, VEC>(row, j0, j1, [&](float l, int id) {
@@ -167,7 +231,6 @@ __device__ unsigned long long shape_select(const T* row, int j0, int j1, const R
             all += sm.part[w];
         }
         if (level == 0 && kMass) need = (unsigned long long)ceil(need_share * (double)all);
-        if (level == 0 && (all < need || need == 0)) return floor_;     // the same in every thread of the cluster
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if (above < need && need <= above + mine[i]) {
@@ -180,10 +243,300 @@ __device__ unsigned long long shape_select(const T* row, int j0, int j1, const R
         prefix = prefix << bits | sm.found[0];
         need -= sm.found[1];
         known += bits;
-        ++turn;
-        __syncthreads();
     }
+    shape_sync<C>();
     return prefix;
+}
+
+// The row's place among bins of equal width from the maximum downwards; the last bin takes everything below.
+struct ShapeBins {
+    float m, inv;                                  // maximum, bins per unit of the logit
+    __device__ __forceinline__ float at(float l) const { return (m - l) * inv; }
+    __device__ __forceinline__ int bin(float l) const { return (int)fminf(at(l), (float)(kShapeBins - 1)); }
+};
+
+// Keys that `wanted` says yes to: collected by every CTA, then put together in all of them (order arbitrary).  Returns their number;
+// above kShapeList none are there.
+template <int C, typename T, int VEC, typename F>
+__device__ int shape_collect(const T* row, int j0, int j1, ShapeSmem& sm, F&& wanted) {
+    const int tid = threadIdx.x;
+    if (tid == 0) sm.n_own = 0;
+    __syncthreads();
+    shape_walk<T, VEC>(row, j0, j1, [&](float l, int id) {
+        if (!wanted(l, id)) return;
+        const int i = atomicAdd(&sm.n_own, 1);
+        if (i < kShapeList) sm.own[i] = order_key(l, id);
+    });
+    shape_sync<C>();
+    int n = 0;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int theirs = shape_peer_i32<C>(&sm.n_own, c);
+        if (n + theirs <= kShapeList)
+            for (int i = tid; i < theirs; i += kShapeThreads) sm.keys[n + i] = shape_peer<C>(sm.own + i, c);
+        n += theirs;
+    }
+    __syncthreads();
+    return n;
+}
+
+// First pass: bins of the keys from floor_ on, each CTA its own.
+template <bool kMass, typename T, int VEC>
+__device__ __forceinline__ void shape_coarse(const T* row, int j0, int j1, const ShapeBins& bins, unsigned long long floor_, ShapeSmem& sm) {
+    for (int b = threadIdx.x; b < kShapeBins; b += kShapeThreads) sm.coarse[b] = 0;
+    __syncthreads();
+    shape_walk<T, VEC>(row, j0, j1, [&](float l, int id) {
+        if (floor_ && order_key(l, id) < floor_) return;
+        const float x = fminf(bins.at(l), (float)(kShapeBins - 1));
+        const int b = (int)x;
+        uint32_t add = 1;
+        if (kMass) {                               // exp(-d) to the second order, |d| <= 1 / 128
+            const float d = (x - (float)b - 0.5f) * (1.f / kShapeWidth);
+            add = (uint32_t)(fmaf(fmaf(0.5f, d, -1.f), d, 1.f) * 8192.f + 0.5f);
+        }
+        atomicAdd(sm.coarse + b, add);
+    });
+}
+
+// Top-k, k < V: the bound, or (kept few enough) also the list of at least all kept keys in sm.keys, *listed of them.
+template <int C, typename T, int VEC>
+__device__ unsigned long long shape_top_k(const T* row, int j0, int j1, const RowShape& r, int k, ShapeSmem& sm, int* listed) {
+    const int tid = threadIdx.x;
+    const ShapeBins bins = {(float)r.m, kShapeWidth};
+    *listed = 0;
+    shape_coarse<false, T, VEC>(row, j0, j1, bins, 0ull, sm);
+    shape_sync<C>();
+    unsigned mine[4], sum = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        mine[i] = 0;
+#pragma unroll
+        for (int c = 0; c < C; ++c) mine[i] += (unsigned)shape_peer_i32<C>(reinterpret_cast<const int*>(sm.coarse + tid * 4 + i), c);
+        sum += mine[i];
+    }
+    const unsigned long long incl = warp_scan_u64(sum);
+    if ((tid & 31) == 31) sm.part[tid >> 5] = incl;
+    __syncthreads();
+    unsigned long long above = incl - sum;
+    for (int w = 0; w < tid >> 5; ++w) above += sm.part[w];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (above < (unsigned)k && (unsigned)k <= above + mine[i]) {
+            sm.found[0] = (unsigned long long)(tid * 4 + i);
+            sm.found[1] = above;
+            sm.found[2] = mine[i];
+        }
+        above += mine[i];
+    }
+    __syncthreads();
+    const int cut = (int)sm.found[0], before = (int)sm.found[1], in = (int)sm.found[2];
+    if (before + in <= kShapeList) {               // all that may be kept
+        *listed = shape_collect<C, T, VEC>(row, j0, j1, sm, [&](float l, int) { return bins.bin(l) <= cut; });
+        return 0ull;
+    }
+    if (in > kShapeList) return shape_select_digits<C, false, T, VEC>(row, j0, j1, r, 0ull, (unsigned long long)k, 0.0, sm);
+    const int n = shape_collect<C, T, VEC>(row, j0, j1, sm, [&](float l, int) { return bins.bin(l) == cut; });
+    unsigned long long low = 0;                    // inverted: the smallest kept key as a maximum
+    for (int i = tid; i < n; i += kShapeThreads) {
+        int rank = before;
+        for (int j = 0; j < n; ++j) rank += sm.keys[j] > sm.keys[i];
+        if (rank < k && ~sm.keys[i] > low) low = ~sm.keys[i];
+    }
+    const unsigned long long bound = ~cta_reduce_u64<true>(low, sm.part2);
+    shape_sync<C>();
+    return bound;
+}
+
+// Top-p, 0 < p < 1, among the keys from floor_ on: the bound.
+template <int C, typename T, int VEC>
+__device__ unsigned long long shape_top_p(const T* row, int j0, int j1, const RowShape& r, unsigned long long floor_, float share, ShapeSmem& sm) {
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const ShapeBins bins = {(float)r.m, (float)(r.c * (0.6931471805599453 * kShapeWidth))};
+    if (!(bins.inv < 1e30f)) return shape_select_digits<C, true, T, VEC>(row, j0, j1, r, floor_, 0ull, (double)share, sm);
+    shape_coarse<true, T, VEC>(row, j0, j1, bins, floor_, sm);
+    shape_sync<C>();
+    // the bins' masses from the maximum downwards
+    double mine[4], sum = 0.0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        unsigned long long t = 0;
+#pragma unroll
+        for (int c = 0; c < C; ++c) t += (unsigned)shape_peer_i32<C>(reinterpret_cast<const int*>(sm.coarse + tid * 4 + i), c);
+        mine[i] = (double)t * shape_exp2(((double)(tid * 4 + i) + 0.5) * (-1.4426950408889634 / kShapeWidth)) * (1.0 / 8192.0);
+        sum += mine[i];
+    }
+    double incl = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const double t = __shfl_up_sync(0xffffffffu, incl, o);
+        if (lane >= o) incl += t;
+    }
+    if (lane == 31) sm.part[warp] = (unsigned long long)__double_as_longlong(incl);
+    if (tid == 0) { sm.window[0] = kShapeBins; sm.window[1] = -1; }
+    __syncthreads();
+    double above = incl - sum, all = 0.0;
+#pragma unroll
+    for (int w = 0; w < kShapeWarps; ++w) {
+        const double t = __longlong_as_double((long long)sm.part[w]);
+        if (w < warp) above += t;
+        all += t;
+    }
+    // The cut is in bin b if prefix(b - 1) < p Z <= prefix(b); what is known of a prefix is off by kShapeSlack of itself, and so is what
+    // is known of a suffix (plus what the last bin holds, below 2^18 e^-31), so that a p close to 1 is as sharp as one close to 0.
+    constexpr double kUp = 1.0 + 3.0 * kShapeSlack, kDown = 1.0 - 3.0 * kShapeSlack, kTail = 1e-8;
+    const double p = (double)share, cut_above = p * all, cut_below = (1.0 - p) * all;
+    int lo = kShapeBins, hi = -1;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const double upto = above + mine[i], below = fmax(all - above, 0.0), after = fmax(all - upto, 0.0);
+        if (above * kDown - kTail < cut_above && upto * kUp + kTail >= cut_above && below * kUp + kTail > cut_below && after * kDown - kTail <= cut_below) {
+            lo = min(lo, tid * 4 + i);
+            hi = max(hi, tid * 4 + i);
+        }
+        above = upto;
+    }
+    if (hi >= 0) {
+        atomicMin(&sm.window[0], lo);
+        atomicMax(&sm.window[1], hi);
+    }
+    for (int i = tid; i < kShapeFine; i += kShapeThreads) sm.fine[i] = 0;
+    __syncthreads();
+    lo = sm.window[0];
+    hi = sm.window[1];
+    if (hi < 0) return shape_select_digits<C, true, T, VEC>(row, j0, j1, r, floor_, 0ull, (double)share, sm);
+    // ---- the masses proper: above the window, all, and by fine bins of the window
+    const float from = (float)lo, to = hi == kShapeBins - 1 ? INFINITY : (float)(hi + 1), steps = (float)kShapeFine / (float)(hi + 1 - lo);
+    auto fine_of = [&](float x) { return (int)fminf((x - from) * steps, (float)(kShapeFine - 1)); };
+    unsigned long long m_above = 0, m_all = 0;
+    shape_walk<T, VEC>(row, j0, j1, [&](float l, int id) {
+        if (floor_ && order_key(l, id) < floor_) return;
+        const unsigned long long w = shape_mass(shape_exponent(l, r));
+        const float x = bins.at(l);
+        m_all += w;
+        if (x < from) m_above += w;
+        else if (x < to && w) atomicAdd(sm.fine + fine_of(x), w);
+    });
+    m_all = warp_sum_u64(m_all);
+    m_above = warp_sum_u64(m_above);
+    if (lane == 0) { sm.part[warp] = m_all; sm.part2[warp] = m_above; }
+    __syncthreads();
+    if (tid == 0) {
+        unsigned long long x = 0, y = 0;
+        for (int w = 0; w < kShapeWarps; ++w) { x += sm.part[w]; y += sm.part2[w]; }
+        sm.cta[2] = x;
+        sm.cta[3] = y;
+        sm.found[0] = ~0ull;
+    }
+    shape_sync<C>();
+    m_all = m_above = 0;
+#pragma unroll
+    for (int c = 0; c < C; ++c) { m_all += shape_peer<C>(&sm.cta[2], c); m_above += shape_peer<C>(&sm.cta[3], c); }
+    const unsigned long long need = (unsigned long long)ceil(p * (double)m_all);
+    unsigned long long f[2], fsum = 0;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        f[i] = 0;
+#pragma unroll
+        for (int c = 0; c < C; ++c) f[i] += shape_peer<C>(sm.fine + tid * 2 + i, c);
+        fsum += f[i];
+    }
+    const unsigned long long fincl = warp_scan_u64(fsum);
+    if (lane == 31) sm.part[warp] = fincl;
+    __syncthreads();
+    unsigned long long run = m_above + fincl - fsum;
+    for (int w = 0; w < warp; ++w) run += sm.part[w];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        if (run < need && need <= run + f[i]) {
+            sm.found[0] = (unsigned long long)(tid * 2 + i);
+            sm.found[1] = run;
+        }
+        run += f[i];
+    }
+    __syncthreads();
+    const unsigned long long before = sm.found[1];
+    const int cut = (int)sm.found[0];
+    if (sm.found[0] == ~0ull) return shape_select_digits<C, true, T, VEC>(row, j0, j1, r, floor_, 0ull, p, sm);
+    const int n = shape_collect<C, T, VEC>(row, j0, j1, sm, [&](float l, int id) {
+        const float x = bins.at(l);
+        return x >= from && x < to && fine_of(x) == cut && !(floor_ && order_key(l, id) < floor_);
+    });
+    if (n > kShapeList) return shape_select_digits<C, true, T, VEC>(row, j0, j1, r, floor_, 0ull, p, sm);
+    for (int i = tid; i < n; i += kShapeThreads) sm.mass[i] = shape_mass(shape_exponent(key_logit(sm.keys[i]), r));
+    __syncthreads();
+    unsigned long long low = 0;
+    for (int i = tid; i < n; i += kShapeThreads) {
+        unsigned long long t = before;
+        for (int j = 0; j < n; ++j) t += sm.keys[j] > sm.keys[i] ? sm.mass[j] : 0ull;
+        if (t < need && ~sm.keys[i] > low) low = ~sm.keys[i];
+    }
+    const unsigned long long bound = ~cta_reduce_u64<true>(low, sm.part2);
+    shape_sync<C>();
+    return bound;
+}
+
+// The rest of a row whose kept ids are all among sm.keys[0 .. n): top-k by rank, top-p, min-p, and the token (-1: no u).  Every CTA of
+// the cluster computes the same.
+__device__ __forceinline__ int shape_from_list(RowShape& r, const Shaping& s, int n, float u, ShapeSmem& sm, unsigned long long& total) {
+    const int tid = threadIdx.x;
+    constexpr int kMine = kShapeList / kShapeThreads;
+    for (int i = tid; i < n; i += kShapeThreads) sm.mass[i] = shape_mass(shape_exponent(key_logit(sm.keys[i]), r));
+    __syncthreads();
+    unsigned long long before[kMine], sum = 0;
+    bool kept[kMine];
+#pragma unroll
+    for (int e = 0; e < kMine; ++e) {
+        const int i = tid + e * kShapeThreads;
+        int rank = 0;
+        before[e] = 0;
+        kept[e] = false;
+        if (i < n) {
+            const unsigned long long key = sm.keys[i];
+            for (int j = 0; j < n; ++j) {
+                const bool up = sm.keys[j] > key;
+                rank += up;
+                before[e] += up ? sm.mass[j] : 0ull;
+            }
+            kept[e] = rank < s.k;
+            if (kept[e]) sum += sm.mass[i];
+        }
+    }
+    if (s.p < 1.f) {
+        const unsigned long long all = cta_reduce_u64<false>(sum, sm.part);
+        const unsigned long long need = (unsigned long long)ceil((double)s.p * (double)all);
+#pragma unroll
+        for (int e = 0; e < kMine; ++e) kept[e] = kept[e] && before[e] < need;
+    }
+    sum = 0;
+    unsigned long long low = 0;
+#pragma unroll
+    for (int e = 0; e < kMine; ++e) {
+        const int i = tid + e * kShapeThreads;
+        kept[e] = kept[e] && shape_exponent(key_logit(sm.keys[i]), r) >= r.y_min;
+        if (kept[e]) {
+            sum += sm.mass[i];
+            low = ~sm.keys[i] > low ? ~sm.keys[i] : low;
+        }
+    }
+    r.bound = ~cta_reduce_u64<true>(low, sm.part2);
+    __syncthreads();
+    total = cta_reduce_u64<false>(sum, sm.part);
+    if (tid == 0) sm.window[0] = -1;
+    __syncthreads();
+    if (!(u >= 0.f)) return -1;
+    // in id order: an id's low key bits are its complement
+    const unsigned long long target = (unsigned long long)floor((double)u * (double)total);
+#pragma unroll
+    for (int e = 0; e < kMine; ++e) {
+        const int i = tid + e * kShapeThreads;
+        if (!kept[e]) continue;
+        const uint32_t id = (uint32_t)sm.keys[i];
+        unsigned long long run = 0;
+        for (int j = 0; j < n; ++j) run += sm.keys[j] >= r.bound && (uint32_t)sm.keys[j] > id ? sm.mass[j] : 0ull;
+        if (run <= target && target < run + sm.mass[i]) sm.window[0] = (int)~id;
+    }
+    __syncthreads();
+    return sm.window[0];
 }
 
 // One row: its shape, and with kDraw its token and, where asked for, its probabilities.
@@ -202,93 +555,133 @@ __device__ void shape_row(const T* row, int V, const Shaping s, float u, int32_t
         bad |= !(l < INFINITY);
         if (l > best) { best = l; best_id = id; }
     });
-    unsigned long long top = bad ? ~0ull : best_id < V ? order_key(best, best_id) : 0ull;
-    top = warp_max_u64(top);
-    if (lane == 0) sm.part[warp] = top;
-    __syncthreads();
-    if (warp == 0) {
-        top = warp_max_u64(lane < kShapeWarps ? sm.part[lane] : 0ull);
-        if (lane == 0) sm.cta[0] = top;
-    }
-    shape_sync<C>();
-    top = 0;
+    unsigned long long top = cta_reduce_u64<true>(bad ? ~0ull : best_id < V ? order_key(best, best_id) : 0ull, sm.part);
+    if (C > 1) {
+        if (tid == 0) sm.cta[0] = top;
+        cluster_sync_all();
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-        const unsigned long long t = shape_peer<C>(&sm.cta[0], c);
-        top = t > top ? t : top;
+        for (int c = 0; c < C; ++c) {
+            const unsigned long long t = shape_peer<C>(&sm.cta[0], c);
+            top = t > top ? t : top;
+        }
     }
 
     RowShape r;
+    r.bound = 0;
+    r.m = r.c = r.y_min = 0.0;
     const bool sane = s.t >= 0.f && s.t < INFINITY && s.p > 0.f && s.mp >= 0.f && s.mp <= 1.f && (!kDraw || (u >= 0.f && u < 1.f));
     const bool empty = top == 0ull || top == ~0ull || !sane;          // uniform over the cluster
-    unsigned long long mass = 0;
+    unsigned long long total = 0;
+    int drawn = -1, listed = 0;
+    bool done = empty;                             // token and total are known (to every CTA)
     if (!empty) {
-        const uint32_t b = (uint32_t)(top >> 32);
-        r.m = (double)__uint_as_float(b & 0x80000000u ? b ^ 0x80000000u : ~b);
+        r.m = (double)key_logit(top);
         r.c = s.t > 0.f ? 1.4426950408889634074 / (double)s.t : 0.0;
         r.y_min = s.mp > 0.f ? log2((double)s.mp) : -INFINITY;
-        r.bound = 0;
         if (s.t == 0.f) {
             r.bound = top;
+            total = 1ull << 45;
+            drawn = (int)~(uint32_t)top;
+            done = true;
         } else {
-            int turn = 0;
-            if (s.k > 0 && s.k < V) r.bound = shape_select<C, false, T, VEC>(row, j0, j1, r, 0ull, (unsigned long long)s.k, 0.0, sm, turn);
-            if (s.p < 1.f) r.bound = shape_select<C, true, T, VEC>(row, j0, j1, r, r.bound, 0ull, (double)s.p, sm, turn);
+            if (s.k > 0 && s.k < V) r.bound = shape_top_k<C, T, VEC>(row, j0, j1, r, s.k, sm, &listed);
+            if (listed) {
+                drawn = shape_from_list(r, s, listed, kDraw ? u : -1.f, sm, total);
+                done = true;
+            } else if (s.p < 1.f) {
+                r.bound = shape_top_p<C, T, VEC>(row, j0, j1, r, r.bound, s.p, sm);
+            }
         }
+    }
+    if (!done) {
         // ---- mass of what is kept: this warp's, the CTA's, the row's
+        unsigned long long mass = 0;
         shape_walk<T, VEC>(row, j0, j1, [&](float l, int id) {
             if (shape_keeps(l, id, r)) mass += shape_mass(shape_exponent(l, r));
         });
         mass = warp_sum_u64(mass);
-    }
-    __syncthreads();
-    if (lane == 0) sm.part[warp] = mass;
-    __syncthreads();
-    if (tid == 0) {
-        unsigned long long t = 0;
-        for (int w = 0; w < kShapeWarps; ++w) t += sm.part[w];
-        sm.cta[1] = t;
-    }
-    shape_sync<C>();
-    unsigned long long total = 0, before = 0;
+        __syncthreads();
+        if (lane == 0) sm.part[warp] = mass;
+        __syncthreads();
+        unsigned long long before = 0, mine = 0;
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-        const unsigned long long t = shape_peer<C>(&sm.cta[1], c);
-        if (c < rank) before += t;
-        total += t;
-    }
-    for (int w = 0; w < warp; ++w) before += sm.part[w];
-    if (out && rank == 0 && tid == 0) {
-        r.total = empty ? 0ull : total;
-        *out = r;
-    }
-    if (kDraw) {
-        if (empty) {
-            if (rank == 0 && tid == 0) *token = -1;
-            if (probs)
-                for (int j = j0 + lane; j < j1; j += 32) probs[j] = 0.f;
-        } else {
+        for (int w = 0; w < kShapeWarps; ++w) {
+            if (w < warp) before += sm.part[w];
+            mine += sm.part[w];
+        }
+        total = mine;
+        if (C > 1) {
+            if (tid == 0) sm.cta[1] = mine;
+            cluster_sync_all();
+            total = 0;
+#pragma unroll
+            for (int c = 0; c < C; ++c) {
+                const unsigned long long t = shape_peer<C>(&sm.cta[1], c);
+                if (c < rank) before += t;
+                total += t;
+            }
+        }
+        if (kDraw) {
             // first id whose running mass exceeds u * total: in the one warp whose share of the sum holds it
             const unsigned long long target = (unsigned long long)floor((double)u * (double)total);
             if (before <= target && target < before + mass) {
                 unsigned long long run = before;
-                for (int j = j0; j < j1; j += 32) {
-                    const int id = j + lane;
-                    const float l = id < j1 ? logit_f32(row[id]) : -INFINITY;
-                    const unsigned long long w = id < j1 && shape_keeps(l, id, r) ? shape_mass(shape_exponent(l, r)) : 0ull;
-                    const unsigned long long incl = run + warp_scan_u64(w);
-                    const unsigned hit = __ballot_sync(0xffffffffu, incl > target);
-                    if (hit) {
-                        if (lane == 0) *token = j + __ffs(hit) - 1;
-                        break;
+                for (int j = j0; j < j1; j += 32 * kDrawBatch) {
+                    unsigned long long w[kDrawBatch];
+#pragma unroll
+                    for (int b = 0; b < kDrawBatch; ++b) {
+                        const int id = j + b * 32 + lane;
+                        const float l = id < j1 ? logit_f32(row[id]) : -INFINITY;
+                        w[b] = id < j1 && shape_keeps(l, id, r) ? shape_mass(shape_exponent(l, r)) : 0ull;
                     }
-                    run = __shfl_sync(0xffffffffu, incl, 31);
+                    bool hit = false;
+#pragma unroll
+                    for (int b = 0; b < kDrawBatch; ++b) {
+                        if (hit) continue;
+                        const unsigned long long incl = run + warp_scan_u64(w[b]);
+                        const unsigned over = __ballot_sync(0xffffffffu, incl > target);
+                        if (over) {
+                            if (lane == 0) *token = j + b * 32 + __ffs(over) - 1;
+                            hit = true;
+                        }
+                        run = __shfl_sync(0xffffffffu, incl, 31);
+                    }
+                    if (hit) break;
                 }
             }
-            if (probs) {
-                const double scale = kMassOne / (double)total;
+        }
+    }
+    if (out && rank == 0 && tid == 0) {
+        r.total = total;
+        *out = r;
+    }
+    if (kDraw) {
+        if (done && rank == 0 && tid == 0) *token = drawn;
+        if (probs) {
+            const double scale = done && empty ? 0.0 : kMassOne / (double)total;
+            if (done) {                            // few ids, or none: zeros first
+                if (VEC > 1 && ((uintptr_t)probs & 15) == 0)
+                    for (int j = j0 + lane * 4; j < j1; j += 128) {
+                        if (j + 4 <= j1) *reinterpret_cast<float4*>(probs + j) = make_float4(0.f, 0.f, 0.f, 0.f);
+                        else
+                            for (int i = j; i < j1; ++i) probs[i] = 0.f;
+                    }
+                else
+                    for (int j = j0 + lane; j < j1; j += 32) probs[j] = 0.f;
+                __syncthreads();
+                const int c0 = min(V, rank * kShapeWarps * per), c1 = min(V, c0 + kShapeWarps * per);     // this CTA's ids
+                if (listed) {
+                    for (int i = tid; i < listed; i += kShapeThreads) {
+                        const unsigned long long key = sm.keys[i];
+                        const int id = (int)~(uint32_t)key;
+                        if (key >= r.bound && id >= c0 && id < c1) probs[id] = (float)(shape_exp2(shape_exponent(key_logit(key), r)) * scale);
+                    }
+                } else if (!empty && tid == 0 && drawn >= c0 && drawn < c1) {
+                    probs[drawn] = 1.f;
+                }
+            } else {
                 shape_walk<T, VEC>(row, j0, j1, [&](float l, int id) {
-                    probs[id] = shape_keeps(l, id, r) ? (float)(exp2(shape_exponent(l, r)) * scale) : 0.f;
+                    probs[id] = shape_keeps(l, id, r) ? (float)(shape_exp2(shape_exponent(l, r)) * scale) : 0.f;
                 });
             }
         }
@@ -369,7 +762,7 @@ __global__ void __launch_bounds__(kAcceptThreads) accept_shaped_kernel(const Acc
     const T* logits = static_cast<const T*>(a.logits) + (size_t)first * a.stride;
     auto prob = [&](const T* row, const RowShape& r, int id, double scale) {
         const float l = logit_f32(row[id]);
-        return shape_keeps(l, id, r) ? exp2(shape_exponent(l, r)) * scale : 0.0;
+        return shape_keeps(l, id, r) ? shape_exp2(shape_exponent(l, r)) * scale : 0.0;
     };
     if (tid == 0) s_first = k;
     __syncthreads();
