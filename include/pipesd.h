@@ -318,7 +318,7 @@ int32_t pipesd_debug_attn_split(int32_t total_keys, int32_t page_size, const int
 #define PIPESD_BF16 1
 
 typedef struct pipesd_shaping {
-    float temperature; /* >= 0, finite                    */
+    float temperature; /* 0..1e30                         */
     int32_t top_k;     /* <= 0: off                       */
     float top_p;       /* > 0; >= 1: off                  */
     float min_p;       /* 0..1; 0: off                    */

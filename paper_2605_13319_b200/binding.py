@@ -494,8 +494,8 @@ def shaping(n: int, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, device="c
     import torch
     a = np.empty((n, 4), np.int32)
     t, p, m = (np.broadcast_to(np.asarray(x, np.float32), (n,)) for x in (temperature, top_p, min_p))
-    if not (np.isfinite(t).all() and (t >= 0).all()):
-        raise ValueError("temperature: finite numbers >= 0")
+    if not ((t >= 0) & (t <= 1e30)).all():
+        raise ValueError("temperature: numbers of [0, 1e30]")
     if not (p > 0).all():
         raise ValueError("top_p: numbers > 0")
     if not ((m >= 0) & (m <= 1)).all():

@@ -10,10 +10,11 @@ namespace {
 
 static_assert(sizeof(Shaping) == sizeof(pipesd_shaping), "pipesd_shaping is read as it is");
 
-// CTAs of a row: as many as leave the device one wave (two CTAs of kShapeThreads per SM), each with at least 4096 ids.
+// CTAs of a row: as many as leave the device one wave, each with at least 4096 ids.  Two CTAs fit an SM, but clusters do not fill
+// every group of SMs to its last place.
 int shape_cluster(int rows, int V) {
     int c = 8;
-    while (c > 1 && ((long long)rows * c > 2 * 148 || V < c * 4096)) c /= 2;
+    while (c > 1 && ((long long)rows * c > 256 || V < c * 4096)) c /= 2;
     return c;
 }
 

@@ -21,19 +21,26 @@ constexpr int kShapeThreads = 512;
 constexpr int kShapeWarps = kShapeThreads / 32;
 constexpr int kShapeBins = 2048;
 constexpr int kShapeMaxVocab = 1 << 18;
+constexpr float kShapeMaxT = 1e30f;                // beyond, even the lowest logit would have to be weighed against -inf
 constexpr double kMassOne = 35184372088832.0;      // 2^45
 
 struct Shaping { float t; int k; float p, mp; };   // pipesd_shaping
 
-// What the rest of a call needs to know about a row: P_id = exp2((l - m) * c) / (total * 2^-45) where key >= bound and the exponent
-// is >= y_min.  total = 0: the row has no distribution (no finite logit, a NaN or +inf among them, settings out of range).
+// What the rest of a call needs to know about a row: P_id = exp2((l - m) * c) / (total * 2^-45) where the id's key is >= bound, that is
+// where l > cut or l = cut and id <= cut_id.  total = 0: the row has no distribution (no finite logit, a NaN or +inf among them,
+// settings out of range).
 struct RowShape {
-    double m, c, y_min;
-    unsigned long long bound, total;
+    double m, c;
+    unsigned long long total;
+    float cut;
+    int cut_id;
 };
 
 __device__ __forceinline__ float logit_f32(float v) { return v; }
 __device__ __forceinline__ float logit_f32(uint16_t v) { return bf16_bits_to_f32(v); }
+template <typename T> __device__ __forceinline__ T logit_none();
+template <> __device__ __forceinline__ float logit_none<float>() { return -INFINITY; }
+template <> __device__ __forceinline__ uint16_t logit_none<uint16_t>() { return 0xff80; }
 
 // Position in the order as a number: larger = earlier.  The addition makes -0 a +0, so that the two tie.
 __device__ __forceinline__ unsigned long long order_key(float l, int id) {
@@ -47,32 +54,33 @@ __device__ __forceinline__ float key_logit(unsigned long long key) {
     return __uint_as_float(b & 0x80000000u ? b ^ 0x80000000u : ~b);
 }
 
-__device__ __forceinline__ double shape_exponent(float l, const RowShape& r) { return fmax(((double)l - r.m) * r.c, -1000.0); }
-// 2^y for -1000 <= y <= 0: whole part into the exponent, the rest by a polynomial of degree 10 (interpolation at the Chebyshev
-// nodes of [-1/2, 1/2], coefficients computed in 70 digits: relative error 3e-16, 2^0 = 1 exactly).
+// Exponent of the weight of a logit that r keeps (which has one of at least -1000).
+__device__ __forceinline__ double shape_exponent(float l, const RowShape& r) { return ((double)l - r.m) * r.c; }
+// The lowest logit with an exponent of about -990 or more.  What lies below has no mass, whatever the settings keep of it: the bound
+// of a row is never lower.
+__device__ __forceinline__ float shape_low(double m, double c) {
+    const float l = (float)fmax(m - 990.0 / c, -3.4028234e38);
+    return ((double)l - m) * c < -1000.0 ? nextafterf(l, INFINITY) : l;
+}
+// 2^y for -1000 <= y <= 0: whole part into the exponent, the rest by a polynomial of degree 9 (interpolation at the Chebyshev
+// nodes of [-1/2, 1/2], coefficients computed in 70 digits: relative error 1.8e-14, less than a step of the masses).  Coefficients
+// are read as constant operands: as literals each costs two moves.
+__constant__ double kExp2Poly[10] = {1.0000000000000135, 0.6931471805599462, 0.2402265069564034, 0.05550410866465167, 0.009618129193934313,
+                                     0.0013333558200794592, 0.0001540343375125101, 1.5252672924850737e-05, 1.325964524488711e-06, 1.0205905413765595e-07};
 __device__ __forceinline__ double shape_exp2(double y) {
     const double big = 6755399441055744.0;         // 1.5 * 2^52: the sum's low bits are the rounded y
     const double n = y + big, r = y - (n - big);
-    double p = 7.072585949269223e-09;
-    p = fma(p, r, 1.0208690299958306e-07);
-    p = fma(p, r, 1.321544258792169e-06);
-    p = fma(p, r, 1.5252657260200837e-05);
-    p = fma(p, r, 0.0001540353044173605);
-    p = fma(p, r, 0.0013333558230164974);
-    p = fma(p, r, 0.009618129107606888);
-    p = fma(p, r, 0.05550410866444772);
-    p = fma(p, r, 0.24022650695910097);
-    p = fma(p, r, 0.69314718055995);
-    p = fma(p, r, 1.0);
+    double p = kExp2Poly[9];
+#pragma unroll
+    for (int i = 8; i >= 0; --i) p = fma(p, r, kExp2Poly[i]);
     return __hiloint2double(__double2hiint(p) + (__double2loint(n) << 20), __double2loint(p));
 }
-// A weight as a whole number of 2^-45: 128 + w has exactly those last bits.
-__device__ __forceinline__ unsigned long long shape_mass(double y) {
-    return (unsigned long long)(__double_as_longlong(shape_exp2(y) + 128.0) - __double_as_longlong(128.0));
-}
-__device__ __forceinline__ bool shape_keeps(float l, int id, const RowShape& r) {
-    return order_key(l, id) >= r.bound && shape_exponent(l, r) >= r.y_min;
-}
+// A weight as a whole number of 2^-45: 128 + w has exactly those last bits.  (Sums may add the bits as they are and take the 128s away
+// in the end: whole numbers modulo 2^64.)
+constexpr unsigned long long kMassBase = 0x4060000000000000ull;          // 128.0
+__device__ __forceinline__ unsigned long long shape_mass_bits(double y) { return (unsigned long long)__double_as_longlong(shape_exp2(y) + 128.0); }
+__device__ __forceinline__ unsigned long long shape_mass(double y) { return shape_mass_bits(y) - kMassBase; }
+__device__ __forceinline__ bool shape_keeps(float l, int id, const RowShape& r) { return l > r.cut || (l == r.cut && id <= r.cut_id); }
 
 __device__ __forceinline__ unsigned long long warp_sum_u64(unsigned long long v) {
 #pragma unroll
@@ -121,7 +129,6 @@ __device__ __forceinline__ int shape_peer_i32(const int* p, int rank) {
 }
 
 constexpr int kShapeList = 1024;                   // ids that are dealt with one by one
-constexpr int kDrawBatch = 4;
 struct ShapeSmem {
     union {                                        // bins of a row: of the first pass (32 bits) and of the second one, or of a digit
         struct { uint32_t coarse[kShapeBins]; unsigned long long fine[kShapeBins / 2]; };
@@ -135,30 +142,103 @@ struct ShapeSmem {
     int n_own, window[2];
 };
 
-// Walks this warp's ids of the row, VEC neighbours per lane and step, kBatch steps' loads in flight together.
+// Walks this warp's ids of the row, VEC neighbours per lane and group: f(logits, first id) for groups of ids first + [0, VEC), several
+// groups' loads in flight together.  All lanes call f together; what lies at or behind j1 comes as -inf.
 template <typename T, int VEC, typename F>
-__device__ __forceinline__ void shape_walk(const T* row, int j0, int j1, F&& f) {
+__device__ __forceinline__ void shape_groups(const T* row, int j0, int j1, F&& f) {
     constexpr int kBatch = VEC == 1 ? 8 : 4;
     const int lane = threadIdx.x & 31;
-    for (int j = j0 + lane * VEC; j < j1; j += 32 * VEC * kBatch) {
+    for (int j = j0; j < j1; j += 32 * VEC * kBatch) {
         T v[kBatch][VEC];
 #pragma unroll
         for (int b = 0; b < kBatch; ++b) {
-            const int i = j + b * 32 * VEC;
-            if (i >= j1) continue;
-            if (VEC == 1) v[b][0] = row[i];
-            else if (i + VEC <= j1) *reinterpret_cast<uint4*>(v[b]) = *reinterpret_cast<const uint4*>(row + i);
-            else
+            const int i = j + (b * 32 + lane) * VEC;
+            if (VEC > 1 && i + VEC <= j1) {
+                *reinterpret_cast<uint4*>(v[b]) = *reinterpret_cast<const uint4*>(row + i);
+            } else {
 #pragma unroll
-                for (int e = 0; e < VEC; ++e)
-                    if (i + e < j1) v[b][e] = row[i + e];
+                for (int e = 0; e < VEC; ++e) v[b][e] = i + e < j1 ? row[i + e] : logit_none<T>();
+            }
         }
+        if (VEC == 1) {                            // eight groups of one: as one group of eight, of ids 32 apart
+            float l[kBatch];
 #pragma unroll
-        for (int b = 0; b < kBatch; ++b)
+            for (int b = 0; b < kBatch; ++b) l[b] = logit_f32(v[b][0]);
+            f(l, j + lane);
+        } else {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e)
-                if (j + b * 32 * VEC + e < j1) f(logit_f32(v[b][e]), j + b * 32 * VEC + e);
+            for (int b = 0; b < kBatch; ++b) {
+                if (j + b * 32 * VEC >= j1) break;
+                float l[VEC];
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) l[e] = logit_f32(v[b][e]);
+                f(l, j + (b * 32 + lane) * VEC);
+            }
+        }
     }
+}
+// The ids of a group are first + kApart * e.
+template <int VEC>
+__device__ __forceinline__ constexpr int group_apart() { return VEC == 1 ? 32 : 1; }
+
+// The same id by id (lanes may diverge in f).
+template <typename T, int VEC, typename F>
+__device__ __forceinline__ void shape_walk(const T* row, int j0, int j1, F&& f) {
+    shape_groups<T, VEC>(row, j0, j1, [&](const auto& l, int first) {
+        constexpr int kN = sizeof(l) / 4;
+#pragma unroll
+        for (int e = 0; e < kN; ++e) {
+            const int id = first + e * group_apart<VEC>();
+            if (id < j1) f(l[e], id);
+        }
+    });
+}
+
+// Masses of the ids that r keeps: f(mass, logit, id), 0 for the others.  All of a group's exponentials side by side, without a branch
+// between them (one by one they cost six times as much: each is a chain of fifteen dependent fp64 operations); groups of which the warp
+// keeps nothing are skipped.
+template <typename T, int VEC, typename F>
+__device__ __forceinline__ void shape_masses(const T* row, int j0, int j1, const RowShape& r, F&& f) {
+    shape_groups<T, VEC>(row, j0, j1, [&](const auto& l, int first) {
+        constexpr int kN = sizeof(l) / 4;
+        bool keep[kN], any = false;
+#pragma unroll
+        for (int e = 0; e < kN; ++e) {
+            keep[e] = shape_keeps(l[e], first + e * group_apart<VEC>(), r);
+            any |= keep[e];
+        }
+        if (!__any_sync(0xffffffffu, any)) return;
+        unsigned long long w[kN];
+#pragma unroll
+        for (int e = 0; e < kN; ++e) w[e] = shape_mass(shape_exponent(keep[e] ? l[e] : r.cut, r));
+#pragma unroll
+        for (int e = 0; e < kN; ++e) f(keep[e] ? w[e] : 0ull, l[e], first + e * group_apart<VEC>());
+    });
+}
+
+// This lane's sum of them.  What is not kept is weighed as the maximum, and its 2^45 taken away again.
+template <typename T, int VEC>
+__device__ __forceinline__ unsigned long long shape_mass_sum(const T* row, int j0, int j1, const RowShape& r) {
+    unsigned long long sum = 0;
+    unsigned n = 0, others = 0;
+    const float m = (float)r.m;
+    shape_groups<T, VEC>(row, j0, j1, [&](const auto& l, int first) {
+        constexpr int kN = sizeof(l) / 4;
+        float x[kN];
+        unsigned cut = 0;
+#pragma unroll
+        for (int e = 0; e < kN; ++e) {
+            const bool keep = shape_keeps(l[e], first + e * group_apart<VEC>(), r);
+            x[e] = keep ? l[e] : m;
+            cut += !keep;
+        }
+        if (!__any_sync(0xffffffffu, cut < kN)) return;
+        n += kN;
+        others += cut;
+#pragma unroll
+        for (int e = 0; e < kN; ++e) sum += shape_mass_bits(shape_exponent(x[e], r));
+    });
+    return sum - n * kMassBase - ((unsigned long long)others << 45);
 }
 
 // Sum (kMax: maximum) over the CTA; every thread gets it.  `part` is not used again before the next barrier but one.
@@ -188,8 +268,8 @@ constexpr double kShapeSlack = 1e-4;               // half a step of 2^-13 (6.1e
 constexpr float kShapeWidth = 64.f;                // bins per unit of the exponent (top-p) or of the logit (top-k)
 
 template <int C, bool kMass, typename T, int VEC>
-__device__ __noinline__ unsigned long long shape_select_digits(const T* row, int j0, int j1, const RowShape& r, unsigned long long floor_, unsigned long long need,
-                                                               double need_share, ShapeSmem& sm) {
+__device__ __noinline__ unsigned long long shape_select_digits(const T* row, int j0, int j1, const RowShape& r, unsigned long long need, double need_share,
+                                                               ShapeSmem& sm) {
     const int tid = threadIdx.x;
     unsigned long long prefix = 0;
     int known = 0;                                 // leading bits of the key that are settled
@@ -206,7 +286,7 @@ __device__ __noinline__ unsigned long long shape_select_digits(const T* row, int
         __syncthreads();
         shape_walk<T, VEC>(row, j0, j1, [&](float l, int id) {
             const unsigned long long key = order_key(l, id);
-            if (key < floor_ || (known && key >> (64 - known) != prefix)) return;
+            if (!shape_keeps(l, id, r) || (known && key >> (64 - known) != prefix)) return;
             const unsigned long long add = kMass ? shape_mass(shape_exponent(l, r)) : 1ull;
             if (add) atomicAdd(hist + (size_t)((key >> shift) & ((1u << bits) - 1)), add);
         });
@@ -248,10 +328,11 @@ __device__ __noinline__ unsigned long long shape_select_digits(const T* row, int
     return prefix;
 }
 
-// The row's place among bins of equal width from the maximum downwards; the last bin takes everything below.
+// The row's place among bins of equal width from the maximum downwards; the last bin takes everything below.  No contraction: every
+// pass has to come to the same place.
 struct ShapeBins {
     float m, inv;                                  // maximum, bins per unit of the logit
-    __device__ __forceinline__ float at(float l) const { return (m - l) * inv; }
+    __device__ __forceinline__ float at(float l) const { return __fmul_rn(__fsub_rn(m, l), inv); }
     __device__ __forceinline__ int bin(float l) const { return (int)fminf(at(l), (float)(kShapeBins - 1)); }
 };
 
@@ -280,13 +361,13 @@ __device__ int shape_collect(const T* row, int j0, int j1, ShapeSmem& sm, F&& wa
     return n;
 }
 
-// First pass: bins of the keys from floor_ on, each CTA its own.
+// First pass: bins of the ids that r keeps, each CTA its own.
 template <bool kMass, typename T, int VEC>
-__device__ __forceinline__ void shape_coarse(const T* row, int j0, int j1, const ShapeBins& bins, unsigned long long floor_, ShapeSmem& sm) {
+__device__ __forceinline__ void shape_coarse(const T* row, int j0, int j1, const ShapeBins& bins, const RowShape& r, ShapeSmem& sm) {
     for (int b = threadIdx.x; b < kShapeBins; b += kShapeThreads) sm.coarse[b] = 0;
     __syncthreads();
     shape_walk<T, VEC>(row, j0, j1, [&](float l, int id) {
-        if (floor_ && order_key(l, id) < floor_) return;
+        if (!shape_keeps(l, id, r)) return;
         const float x = fminf(bins.at(l), (float)(kShapeBins - 1));
         const int b = (int)x;
         uint32_t add = 1;
@@ -304,7 +385,7 @@ __device__ unsigned long long shape_top_k(const T* row, int j0, int j1, const Ro
     const int tid = threadIdx.x;
     const ShapeBins bins = {(float)r.m, kShapeWidth};
     *listed = 0;
-    shape_coarse<false, T, VEC>(row, j0, j1, bins, 0ull, sm);
+    shape_coarse<false, T, VEC>(row, j0, j1, bins, r, sm);
     shape_sync<C>();
     unsigned mine[4], sum = 0;
 #pragma unroll
@@ -334,7 +415,7 @@ __device__ unsigned long long shape_top_k(const T* row, int j0, int j1, const Ro
         *listed = shape_collect<C, T, VEC>(row, j0, j1, sm, [&](float l, int) { return bins.bin(l) <= cut; });
         return 0ull;
     }
-    if (in > kShapeList) return shape_select_digits<C, false, T, VEC>(row, j0, j1, r, 0ull, (unsigned long long)k, 0.0, sm);
+    if (in > kShapeList) return shape_select_digits<C, false, T, VEC>(row, j0, j1, r, (unsigned long long)k, 0.0, sm);
     const int n = shape_collect<C, T, VEC>(row, j0, j1, sm, [&](float l, int) { return bins.bin(l) == cut; });
     unsigned long long low = 0;                    // inverted: the smallest kept key as a maximum
     for (int i = tid; i < n; i += kShapeThreads) {
@@ -347,13 +428,13 @@ __device__ unsigned long long shape_top_k(const T* row, int j0, int j1, const Ro
     return bound;
 }
 
-// Top-p, 0 < p < 1, among the keys from floor_ on: the bound.
+// Top-p, 0 < p < 1, among the ids that r keeps: the bound.
 template <int C, typename T, int VEC>
-__device__ unsigned long long shape_top_p(const T* row, int j0, int j1, const RowShape& r, unsigned long long floor_, float share, ShapeSmem& sm) {
+__device__ unsigned long long shape_top_p(const T* row, int j0, int j1, const RowShape& r, float share, ShapeSmem& sm) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const ShapeBins bins = {(float)r.m, (float)(r.c * (0.6931471805599453 * kShapeWidth))};
-    if (!(bins.inv < 1e30f)) return shape_select_digits<C, true, T, VEC>(row, j0, j1, r, floor_, 0ull, (double)share, sm);
-    shape_coarse<true, T, VEC>(row, j0, j1, bins, floor_, sm);
+    if (!(bins.inv < 1e30f)) return shape_select_digits<C, true, T, VEC>(row, j0, j1, r, 0ull, (double)share, sm);
+    shape_coarse<true, T, VEC>(row, j0, j1, bins, r, sm);
     shape_sync<C>();
     // the bins' masses from the maximum downwards
     double mine[4], sum = 0.0;
@@ -403,14 +484,12 @@ __device__ unsigned long long shape_top_p(const T* row, int j0, int j1, const Ro
     __syncthreads();
     lo = sm.window[0];
     hi = sm.window[1];
-    if (hi < 0) return shape_select_digits<C, true, T, VEC>(row, j0, j1, r, floor_, 0ull, (double)share, sm);
+    if (hi < 0) return shape_select_digits<C, true, T, VEC>(row, j0, j1, r, 0ull, (double)share, sm);
     // ---- the masses proper: above the window, all, and by fine bins of the window
     const float from = (float)lo, to = hi == kShapeBins - 1 ? INFINITY : (float)(hi + 1), steps = (float)kShapeFine / (float)(hi + 1 - lo);
-    auto fine_of = [&](float x) { return (int)fminf((x - from) * steps, (float)(kShapeFine - 1)); };
+    auto fine_of = [&](float x) { return (int)fminf(__fmul_rn(__fsub_rn(x, from), steps), (float)(kShapeFine - 1)); };
     unsigned long long m_above = 0, m_all = 0;
-    shape_walk<T, VEC>(row, j0, j1, [&](float l, int id) {
-        if (floor_ && order_key(l, id) < floor_) return;
-        const unsigned long long w = shape_mass(shape_exponent(l, r));
+    shape_masses<T, VEC>(row, j0, j1, r, [&](unsigned long long w, float l, int) {
         const float x = bins.at(l);
         m_all += w;
         if (x < from) m_above += w;
@@ -456,12 +535,12 @@ __device__ unsigned long long shape_top_p(const T* row, int j0, int j1, const Ro
     __syncthreads();
     const unsigned long long before = sm.found[1];
     const int cut = (int)sm.found[0];
-    if (sm.found[0] == ~0ull) return shape_select_digits<C, true, T, VEC>(row, j0, j1, r, floor_, 0ull, p, sm);
+    if (sm.found[0] == ~0ull) return shape_select_digits<C, true, T, VEC>(row, j0, j1, r, 0ull, p, sm);
     const int n = shape_collect<C, T, VEC>(row, j0, j1, sm, [&](float l, int id) {
         const float x = bins.at(l);
-        return x >= from && x < to && fine_of(x) == cut && !(floor_ && order_key(l, id) < floor_);
+        return x >= from && x < to && fine_of(x) == cut && shape_keeps(l, id, r);
     });
-    if (n > kShapeList) return shape_select_digits<C, true, T, VEC>(row, j0, j1, r, floor_, 0ull, p, sm);
+    if (n > kShapeList) return shape_select_digits<C, true, T, VEC>(row, j0, j1, r, 0ull, p, sm);
     for (int i = tid; i < n; i += kShapeThreads) sm.mass[i] = shape_mass(shape_exponent(key_logit(sm.keys[i]), r));
     __syncthreads();
     unsigned long long low = 0;
@@ -478,9 +557,13 @@ __device__ unsigned long long shape_top_p(const T* row, int j0, int j1, const Ro
 // The rest of a row whose kept ids are all among sm.keys[0 .. n): top-k by rank, top-p, min-p, and the token (-1: no u).  Every CTA of
 // the cluster computes the same.
 __device__ __forceinline__ int shape_from_list(RowShape& r, const Shaping& s, int n, float u, ShapeSmem& sm, unsigned long long& total) {
+    const float low = shape_low(r.m, r.c);
     const int tid = threadIdx.x;
     constexpr int kMine = kShapeList / kShapeThreads;
-    for (int i = tid; i < n; i += kShapeThreads) sm.mass[i] = shape_mass(shape_exponent(key_logit(sm.keys[i]), r));
+    for (int i = tid; i < n; i += kShapeThreads) {
+        const float l = key_logit(sm.keys[i]);
+        sm.mass[i] = l >= low ? shape_mass(shape_exponent(l, r)) : 0ull;
+    }
     __syncthreads();
     unsigned long long before[kMine], sum = 0;
     bool kept[kMine];
@@ -508,17 +591,19 @@ __device__ __forceinline__ int shape_from_list(RowShape& r, const Shaping& s, in
         for (int e = 0; e < kMine; ++e) kept[e] = kept[e] && before[e] < need;
     }
     sum = 0;
-    unsigned long long low = 0;
+    unsigned long long last = 0;                   // inverted: the smallest kept key as a maximum
 #pragma unroll
     for (int e = 0; e < kMine; ++e) {
         const int i = tid + e * kShapeThreads;
-        kept[e] = kept[e] && shape_exponent(key_logit(sm.keys[i]), r) >= r.y_min;
+        kept[e] = kept[e] && key_logit(sm.keys[i]) >= r.cut;      // (min-p, and what has no mass)
         if (kept[e]) {
             sum += sm.mass[i];
-            low = ~sm.keys[i] > low ? ~sm.keys[i] : low;
+            last = ~sm.keys[i] > last ? ~sm.keys[i] : last;
         }
     }
-    r.bound = ~cta_reduce_u64<true>(low, sm.part2);
+    const unsigned long long bound = ~cta_reduce_u64<true>(last, sm.part2);
+    r.cut = key_logit(bound);
+    r.cut_id = (int)~(uint32_t)bound;
     __syncthreads();
     total = cta_reduce_u64<false>(sum, sm.part);
     if (tid == 0) sm.window[0] = -1;
@@ -532,11 +617,23 @@ __device__ __forceinline__ int shape_from_list(RowShape& r, const Shaping& s, in
         if (!kept[e]) continue;
         const uint32_t id = (uint32_t)sm.keys[i];
         unsigned long long run = 0;
-        for (int j = 0; j < n; ++j) run += sm.keys[j] >= r.bound && (uint32_t)sm.keys[j] > id ? sm.mass[j] : 0ull;
+        for (int j = 0; j < n; ++j) run += sm.keys[j] >= bound && (uint32_t)sm.keys[j] > id ? sm.mass[j] : 0ull;
         if (run <= target && target < run + sm.mass[i]) sm.window[0] = (int)~id;
     }
     __syncthreads();
     return sm.window[0];
+}
+
+// The lowest logit whose weight is at least min_p: log2(min_p) is met or not met by an exponent as it is computed, so the quotient is
+// only a first guess.
+__device__ __forceinline__ float shape_min_p(float m, double c, double min_p) {
+    const double y = log2(min_p), guess = (double)m + y / c;
+    auto meets = [&](float l) { return ((double)l - (double)m) * c >= y; };
+    if (!(guess > -3.4e38)) return -INFINITY;
+    float l = (float)guess;
+    for (int i = 0; i < 4 && !meets(l); ++i) l = nextafterf(l, INFINITY);
+    for (int i = 0; i < 4 && meets(nextafterf(l, -INFINITY)); ++i) l = nextafterf(l, -INFINITY);
+    return l;
 }
 
 // One row: its shape, and with kDraw its token and, where asked for, its probabilities.
@@ -567,48 +664,59 @@ __device__ void shape_row(const T* row, int V, const Shaping s, float u, int32_t
     }
 
     RowShape r;
-    r.bound = 0;
-    r.m = r.c = r.y_min = 0.0;
-    const bool sane = s.t >= 0.f && s.t < INFINITY && s.p > 0.f && s.mp >= 0.f && s.mp <= 1.f && (!kDraw || (u >= 0.f && u < 1.f));
+    r.m = r.c = 0.0;
+    r.cut = -INFINITY;                             // keeps everything
+    r.cut_id = V;
+    const bool sane = s.t >= 0.f && s.t <= kShapeMaxT && s.p > 0.f && s.mp >= 0.f && s.mp <= 1.f && (!kDraw || (u >= 0.f && u < 1.f));
     const bool empty = top == 0ull || top == ~0ull || !sane;          // uniform over the cluster
     unsigned long long total = 0;
     int drawn = -1, listed = 0;
     bool done = empty;                             // token and total are known (to every CTA)
     if (!empty) {
-        r.m = (double)key_logit(top);
+        const float m = key_logit(top);
+        r.m = (double)m;
         r.c = s.t > 0.f ? 1.4426950408889634074 / (double)s.t : 0.0;
-        r.y_min = s.mp > 0.f ? log2((double)s.mp) : -INFINITY;
         if (s.t == 0.f) {
-            r.bound = top;
+            r.cut = m;
+            r.cut_id = drawn = (int)~(uint32_t)top;
             total = 1ull << 45;
-            drawn = (int)~(uint32_t)top;
             done = true;
         } else {
-            if (s.k > 0 && s.k < V) r.bound = shape_top_k<C, T, VEC>(row, j0, j1, r, s.k, sm, &listed);
+            float floor_ = shape_low(r.m, r.c);
+            if (s.mp > 0.f) floor_ = fmaxf(floor_, shape_min_p(m, r.c, (double)s.mp));
+            unsigned long long bound = 0;
+            if (s.k > 0 && s.k < V) bound = shape_top_k<C, T, VEC>(row, j0, j1, r, s.k, sm, &listed);
             if (listed) {
+                r.cut = floor_;
                 drawn = shape_from_list(r, s, listed, kDraw ? u : -1.f, sm, total);
                 done = true;
-            } else if (s.p < 1.f) {
-                r.bound = shape_top_p<C, T, VEC>(row, j0, j1, r, r.bound, s.p, sm);
+            } else {
+                auto keep_from = [&](float cut, int id) {
+                    if (cut > r.cut) { r.cut = cut; r.cut_id = id; }
+                };
+                auto keep_key = [&](unsigned long long b) { keep_from(key_logit(b), (int)~(uint32_t)b); };
+                if (bound) keep_key(bound);
+                keep_from(shape_low(r.m, r.c), V);
+                if (s.p < 1.f) {
+                    const unsigned long long b = shape_top_p<C, T, VEC>(row, j0, j1, r, s.p, sm);
+                    r.cut = key_logit(b);          // (among what was kept: never lower)
+                    r.cut_id = (int)~(uint32_t)b;
+                }
+                keep_from(floor_, V);
             }
         }
     }
     if (!done) {
         // ---- mass of what is kept: this warp's, the CTA's, the row's
         unsigned long long mass = 0;
-        shape_walk<T, VEC>(row, j0, j1, [&](float l, int id) {
-            if (shape_keeps(l, id, r)) mass += shape_mass(shape_exponent(l, r));
-        });
+        mass = shape_mass_sum<T, VEC>(row, j0, j1, r);
         mass = warp_sum_u64(mass);
         __syncthreads();
         if (lane == 0) sm.part[warp] = mass;
         __syncthreads();
-        unsigned long long before = 0, mine = 0;
+        unsigned long long mine = 0, before = 0;   // this CTA's mass, and that of the ids before its own
 #pragma unroll
-        for (int w = 0; w < kShapeWarps; ++w) {
-            if (w < warp) before += sm.part[w];
-            mine += sm.part[w];
-        }
+        for (int w = 0; w < kShapeWarps; ++w) mine += sm.part[w];
         total = mine;
         if (C > 1) {
             if (tid == 0) sm.cta[1] = mine;
@@ -622,31 +730,37 @@ __device__ void shape_row(const T* row, int V, const Shaping s, float u, int32_t
             }
         }
         if (kDraw) {
-            // first id whose running mass exceeds u * total: in the one warp whose share of the sum holds it
+            // First id whose running mass exceeds u * total.  It is among the ids of the one warp whose share of the sum holds the target; all
+            // warps of its CTA add those up once more, a part each, and one of them walks its part (a warp alone takes 50 us for a sixteenth
+            // of 128256 ids).
             const unsigned long long target = (unsigned long long)floor((double)u * (double)total);
-            if (before <= target && target < before + mass) {
-                unsigned long long run = before;
-                for (int j = j0; j < j1; j += 32 * kDrawBatch) {
-                    unsigned long long w[kDrawBatch];
-#pragma unroll
-                    for (int b = 0; b < kDrawBatch; ++b) {
-                        const int id = j + b * 32 + lane;
-                        const float l = id < j1 ? logit_f32(row[id]) : -INFINITY;
-                        w[b] = id < j1 && shape_keeps(l, id, r) ? shape_mass(shape_exponent(l, r)) : 0ull;
-                    }
-                    bool hit = false;
-#pragma unroll
-                    for (int b = 0; b < kDrawBatch; ++b) {
-                        if (hit) continue;
-                        const unsigned long long incl = run + warp_scan_u64(w[b]);
+            if (before <= target && target < before + mine) {
+                auto owner = [&](const unsigned long long* part, int& w) {
+                    for (w = 0; w < kShapeWarps - 1 && target >= before + part[w]; ++w) before += part[w];
+                };
+                int w;
+                owner(sm.part, w);
+                int o0 = min(V, (rank * kShapeWarps + w) * per), o1 = min(V, o0 + per);
+                const int sub = ((o1 - o0 + kShapeWarps - 1) / kShapeWarps + 31) / 32 * 32;
+                const int s0 = min(o1, o0 + warp * sub), s1 = min(o1, s0 + sub);
+                const unsigned long long some = warp_sum_u64(shape_mass_sum<T, 1>(row, s0, s1, r));
+                if (lane == 0) sm.part2[warp] = some;
+                __syncthreads();
+                owner(sm.part2, w);
+                if (w == warp) {
+                    unsigned long long run = before;
+                    for (int j = s0; j < s1; j += 32) {
+                        const int id = j + lane;
+                        const float l = id < s1 ? logit_f32(row[id]) : -INFINITY;
+                        const unsigned long long mass_ = shape_keeps(l, id, r) ? shape_mass(shape_exponent(l, r)) : 0ull;
+                        const unsigned long long incl = run + warp_scan_u64(mass_);
                         const unsigned over = __ballot_sync(0xffffffffu, incl > target);
                         if (over) {
-                            if (lane == 0) *token = j + b * 32 + __ffs(over) - 1;
-                            hit = true;
+                            if (lane == 0) *token = j + __ffs(over) - 1;
+                            break;
                         }
                         run = __shfl_sync(0xffffffffu, incl, 31);
                     }
-                    if (hit) break;
                 }
             }
         }
@@ -674,14 +788,37 @@ __device__ void shape_row(const T* row, int V, const Shaping s, float u, int32_t
                     for (int i = tid; i < listed; i += kShapeThreads) {
                         const unsigned long long key = sm.keys[i];
                         const int id = (int)~(uint32_t)key;
-                        if (key >= r.bound && id >= c0 && id < c1) probs[id] = (float)(shape_exp2(shape_exponent(key_logit(key), r)) * scale);
+                        if (shape_keeps(key_logit(key), id, r) && id >= c0 && id < c1) probs[id] = (float)(shape_exp2(shape_exponent(key_logit(key), r)) * scale);
                     }
                 } else if (!empty && tid == 0 && drawn >= c0 && drawn < c1) {
                     probs[drawn] = 1.f;
                 }
             } else {
-                shape_walk<T, VEC>(row, j0, j1, [&](float l, int id) {
-                    probs[id] = shape_keeps(l, id, r) ? (float)(shape_exp2(shape_exponent(l, r)) * scale) : 0.f;
+                shape_groups<T, VEC>(row, j0, j1, [&](const auto& l, int first) {
+                    constexpr int kN = sizeof(l) / 4;
+                    float p[kN];
+                    bool any = false;
+#pragma unroll
+                    for (int e = 0; e < kN; ++e) {
+                        p[e] = 0.f;
+                        any |= shape_keeps(l[e], first + e * group_apart<VEC>(), r);
+                    }
+                    if (__any_sync(0xffffffffu, any)) {
+#pragma unroll
+                        for (int e = 0; e < kN; ++e) p[e] = (float)(shape_exp2(shape_exponent(l[e], r)) * scale);
+#pragma unroll
+                        for (int e = 0; e < kN; ++e) p[e] = shape_keeps(l[e], first + e * group_apart<VEC>(), r) ? p[e] : 0.f;
+                    }
+                    if (VEC > 1 && ((uintptr_t)probs & 15) == 0 && first + kN <= j1) {
+#pragma unroll
+                        for (int e = 0; e < kN; e += 4) *reinterpret_cast<float4*>(probs + first + e) = make_float4(p[e], p[e + 1 < kN ? e + 1 : e], p[e + 2 < kN ? e + 2 : e], p[e + 3 < kN ? e + 3 : e]);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < kN; ++e) {
+                            const int id = first + e * group_apart<VEC>();
+                            if (id < j1) probs[id] = p[e];
+                        }
+                    }
                 });
             }
         }
@@ -762,7 +899,7 @@ __global__ void __launch_bounds__(kAcceptThreads) accept_shaped_kernel(const Acc
     const T* logits = static_cast<const T*>(a.logits) + (size_t)first * a.stride;
     auto prob = [&](const T* row, const RowShape& r, int id, double scale) {
         const float l = logit_f32(row[id]);
-        return shape_keeps(l, id, r) ? shape_exp2(shape_exponent(l, r)) * scale : 0.0;
+        return shape_keeps(l, id, r) ? __dmul_rn(shape_exp2(shape_exponent(l, r)), scale) : 0.0;       // (no contraction: the same in every pass)
     };
     if (tid == 0) s_first = k;
     __syncthreads();
