@@ -19,7 +19,7 @@ namespace pipesd {
 
 constexpr int kShapeThreads = 512;
 constexpr int kShapeWarps = kShapeThreads / 32;
-constexpr int kShapeBins = 2048;
+constexpr int kShapeBins = 4096, kShapeFine = 1024, kShapeDigit = 2048;
 constexpr int kShapeMaxVocab = 1 << 18;
 constexpr float kShapeMaxT = 1e30f;                // beyond, even the lowest logit would have to be weighed against -inf
 constexpr double kMassOne = 35184372088832.0;      // 2^45
@@ -130,16 +130,20 @@ __device__ __forceinline__ int shape_peer_i32(const int* p, int rank) {
 
 constexpr int kShapeList = 1024;                   // ids that are dealt with one by one
 struct ShapeSmem {
-    union {                                        // bins of a row: of the first pass (32 bits) and of the second one, or of a digit
-        struct { uint32_t coarse[kShapeBins]; unsigned long long fine[kShapeBins / 2]; };
-        unsigned long long digit[kShapeBins];
+    union {                                        // bins of a row, or of a digit
+        uint32_t coarse[kShapeBins];
+        unsigned long long digit[kShapeDigit];
+    };
+    union {
+        unsigned long long fine[kShapeFine];       // bins of a window
+        unsigned long long mass[kShapeList];       // masses of `keys`
     };
     unsigned long long own[kShapeList];            // keys that this CTA collected
-    unsigned long long keys[kShapeList], mass[kShapeList];     // the cluster's, and their masses
+    unsigned long long keys[kShapeList];           // the cluster's
     unsigned long long part[kShapeWarps], part2[kShapeWarps];
     unsigned long long cta[4];                     // what the other CTAs of the cluster read: key maximum, kept mass, masses of a window
     unsigned long long found[3];
-    int n_own, window[2];
+    int n_own, n_keys, window[2];
 };
 
 // Walks this warp's ids of the row, VEC neighbours per lane and group: f(logits, first id) for groups of ids first + [0, VEC), several
@@ -256,16 +260,18 @@ __device__ __forceinline__ unsigned long long cta_reduce_u64(unsigned long long 
 // Finding the bound.  A cut of the order is the key at which a running sum over it (of ones: top-k; of masses: top-p) first reaches
 // `need`; everything from there upwards is kept.
 //
-// The usual way has two or three passes over the row.  First bins of equal width in the logit, counted by 32-bit atomics; for
-// masses a bin adds up w / (weight of its middle), which lies within 1 / 128 of 1, as whole numbers of 2^-13: its mass is then known
-// to kShapeSlack.  That settles a window of bins that holds the cut for certain, mostly one.  For top-k the window is exact.
-// Then, unless top-k's window is short, a pass that computes the masses proper: their sums above, in and below the window, and in
-// kFine finer bins of it (64-bit atomics, few of them).  What is left, the ids of one fine bin, is collected and compared
-// with each other.  Where more than kShapeList ids are left (thousands of equal logits, a cut in the far tail) shape_select_digits
-// takes over, which needs no luck: digit by digit over the whole key.
-constexpr int kShapeFine = kShapeBins / 2;
-constexpr double kShapeSlack = 1e-4;               // half a step of 2^-13 (6.1e-5), and what fp32 loses of the bin's position (4e-6) and weight
+// The usual way has two passes over the row.  The first one, which also finds the maximum, counts bins of equal width in the logit with
+// 32-bit atomics, from kShapeUp units above the largest of the row's first ids downwards; for masses a bin adds up
+// w / (weight of its middle), which lies within 1 / 128 of 1, as whole numbers of 2^-13: its mass is then known to kShapeSlack.
+// That settles a window of bins that holds the cut for certain, mostly one; for top-k the bin itself.  Top-k's second pass collects the
+// ids of that bin, with those above it where they are few: these rows are finished from that list.  Top-p's computes the masses
+// proper: their sums above and in the window, and in kShapeFine finer bins of it (64-bit atomics, few of them), and keeps the window's
+// ids.  Those of the fine bin with the cut are compared with each other.
+// Where more ids are left than the lists hold (thousands of equal logits, a cut in the far tail) shape_select_digits takes over,
+// which needs no luck: digit by digit over the whole key.
+constexpr double kShapeSlack = 1e-4;               // half a step of 2^-13 (6.1e-5), and what fp32 loses of the places of bin and maximum (8e-6 each)
 constexpr float kShapeWidth = 64.f;                // bins per unit of the exponent (top-p) or of the logit (top-k)
+constexpr float kShapeUp = 20.f;                   // units: 44 remain below, e^-44 of the maximum over 2^18 ids is nothing
 
 template <int C, bool kMass, typename T, int VEC>
 __device__ __noinline__ unsigned long long shape_select_digits(const T* row, int j0, int j1, const RowShape& r, unsigned long long need, double need_share,
@@ -282,7 +288,7 @@ __device__ __noinline__ unsigned long long shape_select_digits(const T* row, int
         const int bits = level == 2 ? 10 : 11, shift = 64 - known - bits;
         unsigned long long* hist = sm.digit;
         shape_sync<C>();                           // nobody reads what was here before
-        for (int b = tid; b < kShapeBins; b += kShapeThreads) hist[b] = 0;
+        for (int b = tid; b < kShapeDigit; b += kShapeThreads) hist[b] = 0;
         __syncthreads();
         shape_walk<T, VEC>(row, j0, j1, [&](float l, int id) {
             const unsigned long long key = order_key(l, id);
@@ -295,7 +301,7 @@ __device__ __noinline__ unsigned long long shape_select_digits(const T* row, int
         unsigned long long mine[4], sum = 0;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int b = kShapeBins - 1 - (tid * 4 + i);
+            const int b = kShapeDigit - 1 - (tid * 4 + i);
             mine[i] = 0;
 #pragma unroll
             for (int c = 0; c < C; ++c) mine[i] += shape_peer<C>(hist + b, c);
@@ -314,7 +320,7 @@ __device__ __noinline__ unsigned long long shape_select_digits(const T* row, int
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             if (above < need && need <= above + mine[i]) {
-                sm.found[0] = (unsigned long long)(kShapeBins - 1 - (tid * 4 + i));
+                sm.found[0] = (unsigned long long)(kShapeDigit - 1 - (tid * 4 + i));
                 sm.found[1] = above;
             }
             above += mine[i];
@@ -328,82 +334,97 @@ __device__ __noinline__ unsigned long long shape_select_digits(const T* row, int
     return prefix;
 }
 
-// The row's place among bins of equal width from the maximum downwards; the last bin takes everything below.  No contraction: every
-// pass has to come to the same place.
+// The row's place among bins of equal width from `from` downwards; the first bin takes everything above, the last everything below.  No
+// contraction: every pass has to come to the same place.
 struct ShapeBins {
-    float m, inv;                                  // maximum, bins per unit of the logit
-    __device__ __forceinline__ float at(float l) const { return __fmul_rn(__fsub_rn(m, l), inv); }
-    __device__ __forceinline__ int bin(float l) const { return (int)fminf(at(l), (float)(kShapeBins - 1)); }
+    float from, inv;                               // bins per unit of the logit
+    __device__ __forceinline__ float at(float l) const { return __fmul_rn(__fsub_rn(from, l), inv); }
+    __device__ __forceinline__ float clamped(float l) const { return fminf(fmaxf(at(l), 0.f), (float)(kShapeBins - 1)); }
 };
-
-// Keys that `wanted` says yes to: collected by every CTA, then put together in all of them (order arbitrary).  Returns their number;
-// above kShapeList none are there.
-template <int C, typename T, int VEC, typename F>
-__device__ int shape_collect(const T* row, int j0, int j1, ShapeSmem& sm, F&& wanted) {
-    const int tid = threadIdx.x;
-    if (tid == 0) sm.n_own = 0;
-    __syncthreads();
-    shape_walk<T, VEC>(row, j0, j1, [&](float l, int id) {
-        if (!wanted(l, id)) return;
-        const int i = atomicAdd(&sm.n_own, 1);
-        if (i < kShapeList) sm.own[i] = order_key(l, id);
-    });
-    shape_sync<C>();
-    int n = 0;
-#pragma unroll
-    for (int c = 0; c < C; ++c) {
-        const int theirs = shape_peer_i32<C>(&sm.n_own, c);
-        if (n + theirs <= kShapeList)
-            for (int i = tid; i < theirs; i += kShapeThreads) sm.keys[n + i] = shape_peer<C>(sm.own + i, c);
-        n += theirs;
+template <bool kMass>
+__device__ __forceinline__ void shape_count(const ShapeBins& bins, float l, uint32_t* coarse) {
+    const float x = bins.clamped(l);
+    const int b = (int)x;
+    uint32_t add = 1;
+    if (kMass) {                                   // exp(-d) to the second order, |d| <= 1 / 128
+        const float d = (x - (float)b - 0.5f) * (1.f / kShapeWidth);
+        add = (uint32_t)(fmaf(fmaf(0.5f, d, -1.f), d, 1.f) * 8192.f + 0.5f);
     }
-    __syncthreads();
-    return n;
+    atomicAdd(coarse + b, add);
 }
-
-// First pass: bins of the ids that r keeps, each CTA its own.
+// Pass over the ids that r keeps for their bins alone: where the first pass began too low, or a second cut follows.
 template <bool kMass, typename T, int VEC>
-__device__ __forceinline__ void shape_coarse(const T* row, int j0, int j1, const ShapeBins& bins, const RowShape& r, ShapeSmem& sm) {
+__device__ __noinline__ void shape_coarse(const T* row, int j0, int j1, const ShapeBins bins, const RowShape& r, ShapeSmem& sm) {
     for (int b = threadIdx.x; b < kShapeBins; b += kShapeThreads) sm.coarse[b] = 0;
     __syncthreads();
     shape_walk<T, VEC>(row, j0, j1, [&](float l, int id) {
-        if (!shape_keeps(l, id, r)) return;
-        const float x = fminf(bins.at(l), (float)(kShapeBins - 1));
-        const int b = (int)x;
-        uint32_t add = 1;
-        if (kMass) {                               // exp(-d) to the second order, |d| <= 1 / 128
-            const float d = (x - (float)b - 0.5f) * (1.f / kShapeWidth);
-            add = (uint32_t)(fmaf(fmaf(0.5f, d, -1.f), d, 1.f) * 8192.f + 0.5f);
-        }
-        atomicAdd(sm.coarse + b, add);
+        if (shape_keeps(l, id, r)) shape_count<kMass>(bins, l, sm.coarse);
     });
 }
 
-// Top-k, k < V: the bound, or (kept few enough) also the list of at least all kept keys in sm.keys, *listed of them.
-template <int C, typename T, int VEC>
-__device__ unsigned long long shape_top_k(const T* row, int j0, int j1, const RowShape& r, int k, ShapeSmem& sm, int* listed) {
-    const int tid = threadIdx.x;
-    const ShapeBins bins = {(float)r.m, kShapeWidth};
-    *listed = 0;
-    shape_coarse<false, T, VEC>(row, j0, j1, bins, r, sm);
-    shape_sync<C>();
-    unsigned mine[4], sum = 0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        mine[i] = 0;
-#pragma unroll
-        for (int c = 0; c < C; ++c) mine[i] += (unsigned)shape_peer_i32<C>(reinterpret_cast<const int*>(sm.coarse + tid * 4 + i), c);
-        sum += mine[i];
+// Four neighbouring bins of all CTAs.
+template <int C>
+__device__ __forceinline__ void shape_bins4(const uint32_t* p, unsigned (&n)[4]) {
+    if (C == 1) {
+        const uint4 v = *reinterpret_cast<const uint4*>(p);
+        n[0] = v.x; n[1] = v.y; n[2] = v.z; n[3] = v.w;
+        return;
     }
+    n[0] = n[1] = n[2] = n[3] = 0;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        uint4 v;
+        asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(dsmem_addr(smem_u32(p), (uint32_t)c)) : "memory");
+        n[0] += v.x; n[1] += v.y; n[2] += v.z; n[3] += v.w;
+    }
+}
+
+// The CTAs' own lists, put together in all of them as far as `wanted` says so (order arbitrary; ends with a barrier of the CTA).
+// Returns the number in sm.keys; more than kShapeList: not all of them are there.
+template <int C, typename F>
+__device__ __forceinline__ int shape_gather(ShapeSmem& sm, F&& wanted) {
+    if (threadIdx.x == 0) sm.n_keys = 0;
+    __syncthreads();
+    bool over = false;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int theirs = shape_peer_i32<C>(&sm.n_own, c);
+        over |= theirs > kShapeList;
+        for (int i = threadIdx.x; i < min(theirs, kShapeList); i += kShapeThreads) {
+            const unsigned long long key = shape_peer<C>(sm.own + i, c);
+            if (!wanted(key)) continue;
+            const int at = atomicAdd(&sm.n_keys, 1);
+            if (at < kShapeList) sm.keys[at] = key;
+        }
+    }
+    __syncthreads();
+    return over ? kShapeList + 1 : sm.n_keys;
+}
+__device__ __forceinline__ void shape_keep_key(ShapeSmem& sm, float l, int id) {
+    const int i = atomicAdd(&sm.n_own, 1);
+    if (i < kShapeList) sm.own[i] = order_key(l, id);
+}
+
+// Top-k, k < V, behind the first pass and a barrier of the cluster: the bound, or (few enough) the list of at least all kept keys in
+// sm.keys, *listed of them.  sm.n_own = 0 at the start.
+template <int C, typename T, int VEC>
+__device__ unsigned long long shape_top_k(const T* row, int j0, int j1, const RowShape& r, const ShapeBins& bins, int k, ShapeSmem& sm, int* listed) {
+    const int tid = threadIdx.x;
+    *listed = 0;
+    unsigned mine[8], sum = 0;
+    shape_bins4<C>(sm.coarse + tid * 8, *reinterpret_cast<unsigned(*)[4]>(mine));
+    shape_bins4<C>(sm.coarse + tid * 8 + 4, *reinterpret_cast<unsigned(*)[4]>(mine + 4));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += mine[i];
     const unsigned long long incl = warp_scan_u64(sum);
     if ((tid & 31) == 31) sm.part[tid >> 5] = incl;
     __syncthreads();
     unsigned long long above = incl - sum;
     for (int w = 0; w < tid >> 5; ++w) above += sm.part[w];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 8; ++i) {
         if (above < (unsigned)k && (unsigned)k <= above + mine[i]) {
-            sm.found[0] = (unsigned long long)(tid * 4 + i);
+            sm.found[0] = (unsigned long long)(tid * 8 + i);
             sm.found[1] = above;
             sm.found[2] = mine[i];
         }
@@ -411,40 +432,52 @@ __device__ unsigned long long shape_top_k(const T* row, int j0, int j1, const Ro
     }
     __syncthreads();
     const int cut = (int)sm.found[0], before = (int)sm.found[1], in = (int)sm.found[2];
-    if (before + in <= kShapeList) {               // all that may be kept
-        *listed = shape_collect<C, T, VEC>(row, j0, j1, sm, [&](float l, int) { return bins.bin(l) <= cut; });
+    const bool all = before + in <= kShapeList;    // all that may be kept
+    if (in > kShapeList) return shape_select_digits<C, false, T, VEC>(row, j0, j1, r, (unsigned long long)k, 0.0, sm);
+    shape_walk<T, VEC>(row, j0, j1, [&](float l, int id) {
+        const int b = (int)bins.clamped(l);
+        if (all ? b <= cut : b == cut) shape_keep_key(sm, l, id);
+    });
+    shape_sync<C>();
+    const int n = shape_gather<C>(sm, [](unsigned long long) { return true; });
+    if (all) {
+        *listed = n;
         return 0ull;
     }
-    if (in > kShapeList) return shape_select_digits<C, false, T, VEC>(row, j0, j1, r, (unsigned long long)k, 0.0, sm);
-    const int n = shape_collect<C, T, VEC>(row, j0, j1, sm, [&](float l, int) { return bins.bin(l) == cut; });
-    unsigned long long low = 0;                    // inverted: the smallest kept key as a maximum
+    unsigned long long last = 0;                   // inverted: the smallest kept key as a maximum
     for (int i = tid; i < n; i += kShapeThreads) {
         int rank = before;
         for (int j = 0; j < n; ++j) rank += sm.keys[j] > sm.keys[i];
-        if (rank < k && ~sm.keys[i] > low) low = ~sm.keys[i];
+        if (rank < k && ~sm.keys[i] > last) last = ~sm.keys[i];
     }
-    const unsigned long long bound = ~cta_reduce_u64<true>(low, sm.part2);
+    const unsigned long long bound = ~cta_reduce_u64<true>(last, sm.part2);
     shape_sync<C>();
     return bound;
 }
 
-// Top-p, 0 < p < 1, among the ids that r keeps: the bound.
+// Top-p, 0 < p < 1, among the ids that r keeps, behind the first pass and a barrier of the cluster: the bound.  *parts: sm.part holds
+// the kept masses of this CTA's warps (whose ids are `per` each).  sm.n_own = 0 at the start.
 template <int C, typename T, int VEC>
-__device__ unsigned long long shape_top_p(const T* row, int j0, int j1, const RowShape& r, float share, ShapeSmem& sm) {
+__device__ unsigned long long shape_top_p(const T* row, int j0, int j1, const RowShape& r, const ShapeBins& bins, float share, ShapeSmem& sm, int per, bool* parts) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const ShapeBins bins = {(float)r.m, (float)(r.c * (0.6931471805599453 * kShapeWidth))};
-    if (!(bins.inv < 1e30f)) return shape_select_digits<C, true, T, VEC>(row, j0, j1, r, 0ull, (double)share, sm);
-    shape_coarse<true, T, VEC>(row, j0, j1, bins, r, sm);
-    shape_sync<C>();
-    // the bins' masses from the maximum downwards
-    double mine[4], sum = 0.0;
+    const double p = (double)share;
+    *parts = false;
+    // the bins' masses from the top downwards, relative to the maximum's weight
+    double mine[8], sum = 0.0;
+    {
+        const float at_m = bins.at((float)r.m);
+        double w = shape_exp2(fmin(((double)at_m - (double)(tid * 8) - 0.5) * (1.4426950408889634 / kShapeWidth), 1.0));
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        unsigned long long t = 0;
+        for (int h = 0; h < 2; ++h) {
+            unsigned n[4];
+            shape_bins4<C>(sm.coarse + tid * 8 + 4 * h, n);
 #pragma unroll
-        for (int c = 0; c < C; ++c) t += (unsigned)shape_peer_i32<C>(reinterpret_cast<const int*>(sm.coarse + tid * 4 + i), c);
-        mine[i] = (double)t * shape_exp2(((double)(tid * 4 + i) + 0.5) * (-1.4426950408889634 / kShapeWidth)) * (1.0 / 8192.0);
-        sum += mine[i];
+            for (int i = 0; i < 4; ++i) {
+                mine[4 * h + i] = (double)n[i] * w * (1.0 / 8192.0);
+                w *= 0.98449643700540845;          // exp(-1 / 64)
+                sum += mine[4 * h + i];
+            }
+        }
     }
     double incl = sum;
 #pragma unroll
@@ -454,6 +487,7 @@ __device__ unsigned long long shape_top_p(const T* row, int j0, int j1, const Ro
     }
     if (lane == 31) sm.part[warp] = (unsigned long long)__double_as_longlong(incl);
     if (tid == 0) { sm.window[0] = kShapeBins; sm.window[1] = -1; }
+    for (int i = tid; i < kShapeFine; i += kShapeThreads) sm.fine[i] = 0;
     __syncthreads();
     double above = incl - sum, all = 0.0;
 #pragma unroll
@@ -463,16 +497,16 @@ __device__ unsigned long long shape_top_p(const T* row, int j0, int j1, const Ro
         all += t;
     }
     // The cut is in bin b if prefix(b - 1) < p Z <= prefix(b); what is known of a prefix is off by kShapeSlack of itself, and so is what
-    // is known of a suffix (plus what the last bin holds, below 2^18 e^-31), so that a p close to 1 is as sharp as one close to 0.
-    constexpr double kUp = 1.0 + 3.0 * kShapeSlack, kDown = 1.0 - 3.0 * kShapeSlack, kTail = 1e-8;
-    const double p = (double)share, cut_above = p * all, cut_below = (1.0 - p) * all;
+    // is known of a suffix (plus what the last bin holds, below 2^18 e^-44), so that a p close to 1 is as sharp as one close to 0.
+    constexpr double kUp = 1.0 + 3.0 * kShapeSlack, kDown = 1.0 - 3.0 * kShapeSlack, kTail = 1e-9;
+    const double cut_above = p * all, cut_below = (1.0 - p) * all;
     int lo = kShapeBins, hi = -1;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 8; ++i) {
         const double upto = above + mine[i], below = fmax(all - above, 0.0), after = fmax(all - upto, 0.0);
         if (above * kDown - kTail < cut_above && upto * kUp + kTail >= cut_above && below * kUp + kTail > cut_below && after * kDown - kTail <= cut_below) {
-            lo = min(lo, tid * 4 + i);
-            hi = max(hi, tid * 4 + i);
+            lo = min(lo, tid * 8 + i);
+            hi = max(hi, tid * 8 + i);
         }
         above = upto;
     }
@@ -480,20 +514,23 @@ __device__ unsigned long long shape_top_p(const T* row, int j0, int j1, const Ro
         atomicMin(&sm.window[0], lo);
         atomicMax(&sm.window[1], hi);
     }
-    for (int i = tid; i < kShapeFine; i += kShapeThreads) sm.fine[i] = 0;
     __syncthreads();
     lo = sm.window[0];
     hi = sm.window[1];
-    if (hi < 0) return shape_select_digits<C, true, T, VEC>(row, j0, j1, r, 0ull, (double)share, sm);
+    if (hi < 0) return shape_select_digits<C, true, T, VEC>(row, j0, j1, r, 0ull, p, sm);
     // ---- the masses proper: above the window, all, and by fine bins of the window
-    const float from = (float)lo, to = hi == kShapeBins - 1 ? INFINITY : (float)(hi + 1), steps = (float)kShapeFine / (float)(hi + 1 - lo);
-    auto fine_of = [&](float x) { return (int)fminf(__fmul_rn(__fsub_rn(x, from), steps), (float)(kShapeFine - 1)); };
+    const float from = lo == 0 ? -INFINITY : (float)lo, to = hi == kShapeBins - 1 ? INFINITY : (float)(hi + 1);
+    const float steps = (float)kShapeFine / (float)(hi + 1 - lo);
+    auto fine_of = [&](float x) { return (int)fminf(fmaxf(__fmul_rn(__fsub_rn(x, (float)lo), steps), 0.f), (float)(kShapeFine - 1)); };
     unsigned long long m_above = 0, m_all = 0;
-    shape_masses<T, VEC>(row, j0, j1, r, [&](unsigned long long w, float l, int) {
+    shape_masses<T, VEC>(row, j0, j1, r, [&](unsigned long long w, float l, int id) {
         const float x = bins.at(l);
         m_all += w;
         if (x < from) m_above += w;
-        else if (x < to && w) atomicAdd(sm.fine + fine_of(x), w);
+        else if (x < to && w) {
+            atomicAdd(sm.fine + fine_of(x), w);
+            shape_keep_key(sm, l, id);
+        }
     });
     m_all = warp_sum_u64(m_all);
     m_above = warp_sum_u64(m_above);
@@ -507,9 +544,10 @@ __device__ unsigned long long shape_top_p(const T* row, int j0, int j1, const Ro
         sm.found[0] = ~0ull;
     }
     shape_sync<C>();
-    m_all = m_above = 0;
+    m_all = 0;
+    unsigned long long run = 0;
 #pragma unroll
-    for (int c = 0; c < C; ++c) { m_all += shape_peer<C>(&sm.cta[2], c); m_above += shape_peer<C>(&sm.cta[3], c); }
+    for (int c = 0; c < C; ++c) { m_all += shape_peer<C>(&sm.cta[2], c); run += shape_peer<C>(&sm.cta[3], c); }
     const unsigned long long need = (unsigned long long)ceil(p * (double)m_all);
     unsigned long long f[2], fsum = 0;
 #pragma unroll
@@ -522,7 +560,7 @@ __device__ unsigned long long shape_top_p(const T* row, int j0, int j1, const Ro
     const unsigned long long fincl = warp_scan_u64(fsum);
     if (lane == 31) sm.part[warp] = fincl;
     __syncthreads();
-    unsigned long long run = m_above + fincl - fsum;
+    run += fincl - fsum;
     for (int w = 0; w < warp; ++w) run += sm.part[w];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -536,21 +574,32 @@ __device__ unsigned long long shape_top_p(const T* row, int j0, int j1, const Ro
     const unsigned long long before = sm.found[1];
     const int cut = (int)sm.found[0];
     if (sm.found[0] == ~0ull) return shape_select_digits<C, true, T, VEC>(row, j0, j1, r, 0ull, p, sm);
-    const int n = shape_collect<C, T, VEC>(row, j0, j1, sm, [&](float l, int id) {
-        const float x = bins.at(l);
-        return x >= from && x < to && fine_of(x) == cut && shape_keeps(l, id, r);
-    });
+    const int n = shape_gather<C>(sm, [&](unsigned long long key) { return fine_of(bins.at(key_logit(key))) == cut; });
+    shape_sync<C>();                               // the fine bins and the lists have been read
     if (n > kShapeList) return shape_select_digits<C, true, T, VEC>(row, j0, j1, r, 0ull, p, sm);
     for (int i = tid; i < n; i += kShapeThreads) sm.mass[i] = shape_mass(shape_exponent(key_logit(sm.keys[i]), r));
+    if (lane == 0) sm.part[warp] = 0;
     __syncthreads();
-    unsigned long long low = 0;
+    unsigned long long last = 0;                   // inverted: the smallest kept key as a maximum
     for (int i = tid; i < n; i += kShapeThreads) {
         unsigned long long t = before;
         for (int j = 0; j < n; ++j) t += sm.keys[j] > sm.keys[i] ? sm.mass[j] : 0ull;
-        if (t < need && ~sm.keys[i] > low) low = ~sm.keys[i];
+        if (t < need && ~sm.keys[i] > last) last = ~sm.keys[i];
     }
-    const unsigned long long bound = ~cta_reduce_u64<true>(low, sm.part2);
-    shape_sync<C>();
+    __syncthreads();
+    unsigned long long high = warp_max_u64(last);
+    if (lane == 0 && high) atomicMax(&sm.found[2], high);
+    // the window's kept ids, by the warps that they belong to
+    __syncthreads();
+    const unsigned long long bound = ~sm.found[2];
+    const int first = shape_rank<C>() * kShapeWarps * per;
+    for (int i = tid; i < sm.n_own; i += kShapeThreads) {
+        const unsigned long long key = sm.own[i];
+        if (key >= bound) atomicAdd(&sm.part[((int)~(uint32_t)key - first) / per], shape_mass(shape_exponent(key_logit(key), r)));
+    }
+    __syncthreads();
+    if (lane == 0) sm.part[warp] += sm.part2[warp];
+    *parts = true;
     return bound;
 }
 
@@ -644,14 +693,31 @@ __device__ void shape_row(const T* row, int V, const Shaping s, float u, int32_t
     const int per = ((V + C * kShapeWarps - 1) / (C * kShapeWarps) + kStep - 1) / kStep * kStep;     // ids of a warp
     const int j0 = min(V, (rank * kShapeWarps + warp) * per), j1 = min(V, j0 + per);
 
-    // ---- the first of the order; a NaN or +inf anywhere shows as the largest key there is
+    const bool sane = s.t >= 0.f && s.t <= kShapeMaxT && s.p > 0.f && s.mp >= 0.f && s.mp <= 1.f && (!kDraw || (u >= 0.f && u < 1.f));
+    const bool cut_k = sane && s.t > 0.f && s.k > 0 && s.k < V, cut_p = sane && s.t > 0.f && s.p < 1.f;
+    if (tid == 0) { sm.n_own = 0; sm.found[2] = 0; }
+    ShapeBins bins = {0.f, cut_k ? kShapeWidth : kShapeWidth / s.t};
+    if (cut_k || cut_p) {
+        for (int b = tid; b < kShapeBins; b += kShapeThreads) sm.coarse[b] = 0;
+        float first = -INFINITY;                   // of the row's first ids, the same in all CTAs
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (tid + i * kShapeThreads < V) first = fmaxf(first, logit_f32(row[tid + i * kShapeThreads]));
+        const unsigned long long f = cta_reduce_u64<true>(first > -INFINITY && first < INFINITY ? order_key(first, 0) : 0ull, sm.part2);
+        bins.from = (f ? key_logit(f) : 0.f) + (cut_k ? kShapeUp : kShapeUp * s.t);
+        if (!(bins.inv < 1e30f)) bins.inv = 1e30f; // (a tiny temperature: the bins are of no use, and found to be so)
+    }
+    // ---- first pass: the first of the order (a NaN or +inf anywhere shows as the largest key there is), and the bins
     float best = -INFINITY;
     int best_id = V;
     bool bad = false;
-    shape_walk<T, VEC>(row, j0, j1, [&](float l, int id) {
+    auto look = [&](float l, int id) {
         bad |= !(l < INFINITY);
         if (l > best) { best = l; best_id = id; }
-    });
+    };
+    if (cut_k) shape_walk<T, VEC>(row, j0, j1, [&](float l, int id) { look(l, id); shape_count<false>(bins, l, sm.coarse); });
+    else if (cut_p) shape_walk<T, VEC>(row, j0, j1, [&](float l, int id) { look(l, id); shape_count<true>(bins, l, sm.coarse); });
+    else shape_walk<T, VEC>(row, j0, j1, look);
     unsigned long long top = cta_reduce_u64<true>(bad ? ~0ull : best_id < V ? order_key(best, best_id) : 0ull, sm.part);
     if (C > 1) {
         if (tid == 0) sm.cta[0] = top;
@@ -667,10 +733,10 @@ __device__ void shape_row(const T* row, int V, const Shaping s, float u, int32_t
     r.m = r.c = 0.0;
     r.cut = -INFINITY;                             // keeps everything
     r.cut_id = V;
-    const bool sane = s.t >= 0.f && s.t <= kShapeMaxT && s.p > 0.f && s.mp >= 0.f && s.mp <= 1.f && (!kDraw || (u >= 0.f && u < 1.f));
     const bool empty = top == 0ull || top == ~0ull || !sane;          // uniform over the cluster
     unsigned long long total = 0;
     int drawn = -1, listed = 0;
+    bool parts = false;                            // sm.part holds the kept masses of this CTA's warps
     bool done = empty;                             // token and total are known (to every CTA)
     if (!empty) {
         const float m = key_logit(top);
@@ -684,8 +750,20 @@ __device__ void shape_row(const T* row, int V, const Shaping s, float u, int32_t
         } else {
             float floor_ = shape_low(r.m, r.c);
             if (s.mp > 0.f) floor_ = fmaxf(floor_, shape_min_p(m, r.c, (double)s.mp));
+            // the first pass' bins, unless the maximum lies above them
+            auto again = [&](float from, float inv) {
+                bins.from = from;
+                bins.inv = inv;
+            };
             unsigned long long bound = 0;
-            if (s.k > 0 && s.k < V) bound = shape_top_k<C, T, VEC>(row, j0, j1, r, s.k, sm, &listed);
+            if (cut_k) {
+                if (!(m <= bins.from)) {
+                    again(m, kShapeWidth);
+                    shape_coarse<false, T, VEC>(row, j0, j1, bins, r, sm);
+                    shape_sync<C>();
+                }
+                bound = shape_top_k<C, T, VEC>(row, j0, j1, r, bins, s.k, sm, &listed);
+            }
             if (listed) {
                 r.cut = floor_;
                 drawn = shape_from_list(r, s, listed, kDraw ? u : -1.f, sm, total);
@@ -697,11 +775,26 @@ __device__ void shape_row(const T* row, int V, const Shaping s, float u, int32_t
                 auto keep_key = [&](unsigned long long b) { keep_from(key_logit(b), (int)~(uint32_t)b); };
                 if (bound) keep_key(bound);
                 keep_from(shape_low(r.m, r.c), V);
-                if (s.p < 1.f) {
-                    const unsigned long long b = shape_top_p<C, T, VEC>(row, j0, j1, r, s.p, sm);
+                if (cut_p) {
+                    unsigned long long b;
+                    if (!(kShapeWidth / s.t < 1e30f)) {
+                        b = shape_select_digits<C, true, T, VEC>(row, j0, j1, r, 0ull, (double)s.p, sm);
+                    } else {
+                        if (cut_k || !(m <= bins.from)) {
+                            if (cut_k) {
+                                shape_sync<C>();   // (the lists of the first cut have been read)
+                                if (tid == 0) { sm.n_own = 0; sm.found[2] = 0; }
+                            }
+                            again(m, kShapeWidth / s.t);
+                            shape_coarse<true, T, VEC>(row, j0, j1, bins, r, sm);
+                            shape_sync<C>();
+                        }
+                        b = shape_top_p<C, T, VEC>(row, j0, j1, r, bins, s.p, sm, per, &parts);
+                    }
                     r.cut = key_logit(b);          // (among what was kept: never lower)
                     r.cut_id = (int)~(uint32_t)b;
                 }
+                if (floor_ > r.cut) parts = false;
                 keep_from(floor_, V);
             }
         }
@@ -709,10 +802,11 @@ __device__ void shape_row(const T* row, int V, const Shaping s, float u, int32_t
     if (!done) {
         // ---- mass of what is kept: this warp's, the CTA's, the row's
         unsigned long long mass = 0;
-        mass = shape_mass_sum<T, VEC>(row, j0, j1, r);
-        mass = warp_sum_u64(mass);
-        __syncthreads();
-        if (lane == 0) sm.part[warp] = mass;
+        if (!parts) {
+            mass = warp_sum_u64(shape_mass_sum<T, VEC>(row, j0, j1, r));
+            __syncthreads();
+            if (lane == 0) sm.part[warp] = mass;
+        }
         __syncthreads();
         unsigned long long mine = 0, before = 0;   // this CTA's mass, and that of the ids before its own
 #pragma unroll
