@@ -266,9 +266,9 @@ __device__ __forceinline__ unsigned long long cta_reduce_u64(unsigned long long 
 // That settles a window of bins that holds the cut for certain, mostly one; for top-k the bin itself.  Top-k's second pass collects the
 // ids of that bin, with those above it where they are few: these rows are finished from that list.  Top-p's computes the masses
 // proper: their sums above and in the window, and in kShapeFine finer bins of it (64-bit atomics, few of them), and keeps the window's
-// ids.  Those of the fine bin with the cut are compared with each other.
-// Where more ids are left than the lists hold (thousands of equal logits, a cut in the far tail) shape_select_digits takes over,
-// which needs no luck: digit by digit over the whole key.
+// ids (more than the list holds: a third pass collects those of one fine bin).  Those of the fine bin with the cut are compared with
+// each other.  Where even they are more than the lists hold (thousands of equal logits, a cut in the far tail) shape_select_digits
+// takes over, which needs no luck: digit by digit over the whole key.
 constexpr double kShapeSlack = 1e-4;               // half a step of 2^-13 (6.1e-5), and what fp32 loses of the places of bin and maximum (8e-6 each)
 constexpr float kShapeWidth = 64.f;                // bins per unit of the exponent (top-p) or of the logit (top-k)
 constexpr float kShapeUp = 20.f;                   // units: 44 remain below, e^-44 of the maximum over 2^18 ids is nothing
@@ -574,8 +574,20 @@ __device__ unsigned long long shape_top_p(const T* row, int j0, int j1, const Ro
     const unsigned long long before = sm.found[1];
     const int cut = (int)sm.found[0];
     if (sm.found[0] == ~0ull) return shape_select_digits<C, true, T, VEC>(row, j0, j1, r, 0ull, p, sm);
-    const int n = shape_gather<C>(sm, [&](unsigned long long key) { return fine_of(bins.at(key_logit(key))) == cut; });
+    int n = shape_gather<C>(sm, [&](unsigned long long key) { return fine_of(bins.at(key_logit(key))) == cut; });
     shape_sync<C>();                               // the fine bins and the lists have been read
+    const bool whole = n <= kShapeList;            // the window's ids are all in the lists
+    if (!whole) {                                  // another pass, for the fine bin's alone
+        if (tid == 0) sm.n_own = 0;
+        __syncthreads();
+        shape_walk<T, VEC>(row, j0, j1, [&](float l, int id) {
+            const float x = bins.at(l);
+            if (x >= from && x < to && fine_of(x) == cut && shape_keeps(l, id, r)) shape_keep_key(sm, l, id);
+        });
+        shape_sync<C>();
+        n = shape_gather<C>(sm, [](unsigned long long) { return true; });
+        shape_sync<C>();
+    }
     if (n > kShapeList) return shape_select_digits<C, true, T, VEC>(row, j0, j1, r, 0ull, p, sm);
     for (int i = tid; i < n; i += kShapeThreads) sm.mass[i] = shape_mass(shape_exponent(key_logit(sm.keys[i]), r));
     if (lane == 0) sm.part[warp] = 0;
@@ -592,6 +604,7 @@ __device__ unsigned long long shape_top_p(const T* row, int j0, int j1, const Ro
     // the window's kept ids, by the warps that they belong to
     __syncthreads();
     const unsigned long long bound = ~sm.found[2];
+    if (!whole) return bound;
     const int first = shape_rank<C>() * kShapeWarps * per;
     for (int i = tid; i < sm.n_own; i += kShapeThreads) {
         const unsigned long long key = sm.own[i];
