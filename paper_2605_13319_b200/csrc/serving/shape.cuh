@@ -19,7 +19,8 @@ namespace pipesd {
 
 constexpr int kShapeThreads = 512;
 constexpr int kShapeWarps = kShapeThreads / 32;
-constexpr int kShapeBins = 4096, kShapeFine = 1024, kShapeDigit = 2048;
+constexpr int kShapeBins = 4096, kShapeFine = 1024, kShapeDigit = 2048, kShapeSegs = 64;
+constexpr int kSegBins = kShapeBins / kShapeSegs, kSegFine = 32;      // bins of a segment
 constexpr int kShapeMaxVocab = 1 << 18;
 constexpr float kShapeMaxT = 1e30f;                // beyond, even the lowest logit would have to be weighed against -inf
 constexpr double kMassOne = 35184372088832.0;      // 2^45
@@ -141,6 +142,8 @@ struct ShapeSmem {
     unsigned long long own[kShapeList];            // keys that this CTA collected
     unsigned long long keys[kShapeList];           // the cluster's
     unsigned long long part[kShapeWarps], part2[kShapeWarps];
+    unsigned long long seg[kShapeSegs];            // sums of neighbouring bins: counts, or masses as doubles
+    unsigned long long fine_seg[kShapeFine / kSegFine];
     unsigned long long cta[4];                     // what the other CTAs of the cluster read: key maximum, kept mass, masses of a window
     unsigned long long found[3];
     int n_own, n_keys, window[2];
@@ -352,6 +355,34 @@ __device__ __forceinline__ void shape_count(const ShapeBins& bins, float l, uint
     }
     atomicAdd(coarse + b, add);
 }
+// Behind the pass and a barrier of the CTA: its bins' sums by segment, so that a cluster exchanges 64 numbers and then the bins of
+// one segment (all bins of all CTAs read by all of them take 20 us in a cluster of eight).  Masses are relative to a weight of 1 at the
+// first bin's upper end.
+constexpr double kBinShrink = 0.98449643700540845;       // exp(-1 / kShapeWidth)
+__device__ __forceinline__ double shape_bin_weight(int b) { return shape_exp2(((double)b + 0.5) * (-1.4426950408889634 / kShapeWidth)) * (1.0 / 8192.0); }
+template <bool kMass>
+__device__ __forceinline__ void shape_segments(ShapeSmem& sm) {
+    const int tid = threadIdx.x;
+    constexpr int kEach = kShapeBins / kShapeThreads;
+    uint32_t n[kEach];
+#pragma unroll
+    for (int i = 0; i < kEach; i += 4) *reinterpret_cast<uint4*>(n + i) = *reinterpret_cast<const uint4*>(sm.coarse + tid * kEach + i);
+    if (kMass) {
+        double w = shape_bin_weight(tid * kEach), sum = 0.0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) { sum += (double)n[i] * w; w *= kBinShrink; }
+#pragma unroll
+        for (int o = 1; o < kSegBins / kEach; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (tid % (kSegBins / kEach) == 0) sm.seg[tid / (kSegBins / kEach)] = (unsigned long long)__double_as_longlong(sum);
+    } else {
+        unsigned sum = 0;
+#pragma unroll
+        for (int i = 0; i < kEach; ++i) sum += n[i];
+#pragma unroll
+        for (int o = 1; o < kSegBins / kEach; o <<= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+        if (tid % (kSegBins / kEach) == 0) sm.seg[tid / (kSegBins / kEach)] = sum;
+    }
+}
 // Pass over the ids that r keeps for their bins alone: where the first pass began too low, or a second cut follows.
 template <bool kMass, typename T, int VEC>
 __device__ __noinline__ void shape_coarse(const T* row, int j0, int j1, const ShapeBins bins, const RowShape& r, ShapeSmem& sm) {
@@ -360,23 +391,38 @@ __device__ __noinline__ void shape_coarse(const T* row, int j0, int j1, const Sh
     shape_walk<T, VEC>(row, j0, j1, [&](float l, int id) {
         if (shape_keeps(l, id, r)) shape_count<kMass>(bins, l, sm.coarse);
     });
+    __syncthreads();
+    shape_segments<kMass>(sm);
 }
 
-// Four neighbouring bins of all CTAs.
 template <int C>
-__device__ __forceinline__ void shape_bins4(const uint32_t* p, unsigned (&n)[4]) {
-    if (C == 1) {
-        const uint4 v = *reinterpret_cast<const uint4*>(p);
-        n[0] = v.x; n[1] = v.y; n[2] = v.z; n[3] = v.w;
-        return;
-    }
-    n[0] = n[1] = n[2] = n[3] = 0;
+__device__ __forceinline__ unsigned shape_bin(const ShapeSmem& sm, int b) {
+    unsigned n = 0;
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-        uint4 v;
-        asm volatile("ld.shared::cluster.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(dsmem_addr(smem_u32(p), (uint32_t)c)) : "memory");
-        n[0] += v.x; n[1] += v.y; n[2] += v.z; n[3] += v.w;
+    for (int c = 0; c < C; ++c) n += (unsigned)shape_peer_i32<C>(reinterpret_cast<const int*>(sm.coarse + b), c);
+    return n;
+}
+__device__ __forceinline__ double warp_scan_f64(double v) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const double t = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += t;
     }
+    return v;
+}
+// The neighbours 2 lane, 2 lane + 1 among 64 counts in which the running sum first reaches need (whole warp; it does): their place and the sum
+// before it.
+__device__ __forceinline__ int shape_find2(unsigned long long a, unsigned long long b, unsigned long long need, unsigned long long& before, unsigned long long& in) {
+    const int lane = threadIdx.x & 31;
+    const unsigned long long incl = before + warp_scan_u64(a + b), start = incl - a - b;
+    const unsigned hit = __ballot_sync(0xffffffffu, need <= incl);
+    const int l = hit ? __ffs(hit) - 1 : 31;
+    const bool second = need > start + a;
+    const int at = __shfl_sync(0xffffffffu, 2 * lane + second, l);
+    before = __shfl_sync(0xffffffffu, second ? start + a : start, l);
+    in = __shfl_sync(0xffffffffu, second ? b : a, l);
+    return at;
 }
 
 // The CTAs' own lists, put together in all of them as far as `wanted` says so (order arbitrary; ends with a barrier of the CTA).
@@ -409,26 +455,19 @@ __device__ __forceinline__ void shape_keep_key(ShapeSmem& sm, float l, int id) {
 // sm.keys, *listed of them.  sm.n_own = 0 at the start.
 template <int C, typename T, int VEC>
 __device__ unsigned long long shape_top_k(const T* row, int j0, int j1, const RowShape& r, const ShapeBins& bins, int k, ShapeSmem& sm, int* listed) {
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, lane = tid & 31;
     *listed = 0;
-    unsigned mine[8], sum = 0;
-    shape_bins4<C>(sm.coarse + tid * 8, *reinterpret_cast<unsigned(*)[4]>(mine));
-    shape_bins4<C>(sm.coarse + tid * 8 + 4, *reinterpret_cast<unsigned(*)[4]>(mine + 4));
+    if (tid < 32) {                                // the segment, then its bin
+        unsigned long long n[2] = {0, 0}, above = 0, in;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum += mine[i];
-    const unsigned long long incl = warp_scan_u64(sum);
-    if ((tid & 31) == 31) sm.part[tid >> 5] = incl;
-    __syncthreads();
-    unsigned long long above = incl - sum;
-    for (int w = 0; w < tid >> 5; ++w) above += sm.part[w];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if (above < (unsigned)k && (unsigned)k <= above + mine[i]) {
-            sm.found[0] = (unsigned long long)(tid * 8 + i);
+        for (int c = 0; c < C; ++c) { n[0] += shape_peer<C>(sm.seg + 2 * lane, c); n[1] += shape_peer<C>(sm.seg + 2 * lane + 1, c); }
+        int at = shape_find2(n[0], n[1], (unsigned)k, above, in) * kSegBins;
+        at += shape_find2(shape_bin<C>(sm, at + 2 * lane), shape_bin<C>(sm, at + 2 * lane + 1), (unsigned)k, above, in);
+        if (lane == 0) {
+            sm.found[0] = (unsigned long long)at;
             sm.found[1] = above;
-            sm.found[2] = mine[i];
+            sm.found[2] = in;
         }
-        above += mine[i];
     }
     __syncthreads();
     const int cut = (int)sm.found[0], before = (int)sm.found[1], in = (int)sm.found[2];
@@ -462,61 +501,55 @@ __device__ unsigned long long shape_top_p(const T* row, int j0, int j1, const Ro
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const double p = (double)share;
     *parts = false;
-    // the bins' masses from the top downwards, relative to the maximum's weight
-    double mine[8], sum = 0.0;
-    {
-        const float at_m = bins.at((float)r.m);
-        double w = shape_exp2(fmin(((double)at_m - (double)(tid * 8) - 0.5) * (1.4426950408889634 / kShapeWidth), 1.0));
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            unsigned n[4];
-            shape_bins4<C>(sm.coarse + tid * 8 + 4 * h, n);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                mine[4 * h + i] = (double)n[i] * w * (1.0 / 8192.0);
-                w *= 0.98449643700540845;          // exp(-1 / 64)
-                sum += mine[4 * h + i];
-            }
-        }
-    }
-    double incl = sum;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-        const double t = __shfl_up_sync(0xffffffffu, incl, o);
-        if (lane >= o) incl += t;
-    }
-    if (lane == 31) sm.part[warp] = (unsigned long long)__double_as_longlong(incl);
-    if (tid == 0) { sm.window[0] = kShapeBins; sm.window[1] = -1; }
     for (int i = tid; i < kShapeFine; i += kShapeThreads) sm.fine[i] = 0;
-    __syncthreads();
-    double above = incl - sum, all = 0.0;
-#pragma unroll
-    for (int w = 0; w < kShapeWarps; ++w) {
-        const double t = __longlong_as_double((long long)sm.part[w]);
-        if (w < warp) above += t;
-        all += t;
-    }
     // The cut is in bin b if prefix(b - 1) < p Z <= prefix(b); what is known of a prefix is off by kShapeSlack of itself, and so is what
-    // is known of a suffix (plus what the last bin holds, below 2^18 e^-44), so that a p close to 1 is as sharp as one close to 0.
-    constexpr double kUp = 1.0 + 3.0 * kShapeSlack, kDown = 1.0 - 3.0 * kShapeSlack, kTail = 1e-9;
-    const double cut_above = p * all, cut_below = (1.0 - p) * all;
-    int lo = kShapeBins, hi = -1;
+    // is known of a suffix (plus what the last bin holds, below 2^18 e^-44 of the maximum), so that a p close to 1 is as sharp as one
+    // close to 0.  The same for segments of bins.
+    if (warp == 0) {
+        constexpr double kUp = 1.0 + 3.0 * kShapeSlack, kDown = 1.0 - 3.0 * kShapeSlack;
+        const double tail = 1e-9 * shape_exp2((double)bins.at((float)r.m) * (-1.4426950408889634 / kShapeWidth));
+        double n[2] = {0.0, 0.0};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const double upto = above + mine[i], below = fmax(all - above, 0.0), after = fmax(all - upto, 0.0);
-        if (above * kDown - kTail < cut_above && upto * kUp + kTail >= cut_above && below * kUp + kTail > cut_below && after * kDown - kTail <= cut_below) {
-            lo = min(lo, tid * 8 + i);
-            hi = max(hi, tid * 8 + i);
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) n[i] += __longlong_as_double((long long)shape_peer<C>(sm.seg + 2 * lane + i, c));
+        const double incl = warp_scan_f64(n[0] + n[1]), all = __shfl_sync(0xffffffffu, incl, 31), cut_above = p * all, cut_below = (1.0 - p) * all;
+        auto may = [&](double above, double upto) {
+            const double below = fmax(all - above, 0.0), after = fmax(all - upto, 0.0);
+            return above * kDown - tail < cut_above && upto * kUp + tail >= cut_above && below * kUp + tail > cut_below && after * kDown - tail <= cut_below;
+        };
+        auto widest = [&](int& lo, int& hi) {
+            lo = __reduce_min_sync(0xffffffffu, lo);
+            hi = __reduce_max_sync(0xffffffffu, hi);
+        };
+        const double s0 = incl - n[0] - n[1], s1 = incl - n[1];
+        int lo = kShapeBins, hi = -1;
+        if (may(s0, s1)) { lo = 2 * lane; hi = 2 * lane; }
+        if (may(s1, incl)) { lo = min(lo, 2 * lane + 1); hi = 2 * lane + 1; }
+        widest(lo, hi);
+        if (hi >= lo && hi - lo < 4) {             // its bins: 2, 4, ... neighbours a lane
+            double run = __shfl_sync(0xffffffffu, lo & 1 ? s1 : s0, lo >> 1);
+            const int first = lo * kSegBins, segs = hi - lo + 1;
+            int blo = kShapeBins, bhi = -1;
+            for (int q = 0; q < segs; ++q) {
+                const int b = first + q * kSegBins + 2 * lane;
+                const double w = shape_bin_weight(b), a0 = (double)shape_bin<C>(sm, b) * w, a1 = (double)shape_bin<C>(sm, b + 1) * (w * kBinShrink);
+                const double up = run + warp_scan_f64(a0 + a1), b0 = up - a0 - a1, b1 = up - a1;
+                if (may(b0, b1)) { blo = min(blo, b); bhi = max(bhi, b); }
+                if (may(b1, up)) { blo = min(blo, b + 1); bhi = max(bhi, b + 1); }
+                run = __shfl_sync(0xffffffffu, up, 31);
+            }
+            widest(blo, bhi);
+            lo = blo;
+            hi = bhi;
+        } else if (hi >= lo) {
+            lo *= kSegBins;
+            hi = hi * kSegBins + kSegBins - 1;
         }
-        above = upto;
-    }
-    if (hi >= 0) {
-        atomicMin(&sm.window[0], lo);
-        atomicMax(&sm.window[1], hi);
+        if (lane == 0) { sm.window[0] = lo; sm.window[1] = hi; }
     }
     __syncthreads();
-    lo = sm.window[0];
-    hi = sm.window[1];
+    const int lo = sm.window[0], hi = sm.window[1];
     if (hi < 0) return shape_select_digits<C, true, T, VEC>(row, j0, j1, r, 0ull, p, sm);
     // ---- the masses proper: above the window, all, and by fine bins of the window
     const float from = lo == 0 ? -INFINITY : (float)lo, to = hi == kShapeBins - 1 ? INFINITY : (float)(hi + 1);
@@ -536,12 +569,16 @@ __device__ unsigned long long shape_top_p(const T* row, int j0, int j1, const Ro
     m_above = warp_sum_u64(m_above);
     if (lane == 0) { sm.part[warp] = m_all; sm.part2[warp] = m_above; }
     __syncthreads();
-    if (tid == 0) {
-        unsigned long long x = 0, y = 0;
-        for (int w = 0; w < kShapeWarps; ++w) { x += sm.part[w]; y += sm.part2[w]; }
-        sm.cta[2] = x;
-        sm.cta[3] = y;
-        sm.found[0] = ~0ull;
+    {
+        unsigned long long t = sm.fine[2 * tid] + sm.fine[2 * tid + 1];
+#pragma unroll
+        for (int o = 1; o < kSegFine / 2; o <<= 1) t += __shfl_xor_sync(0xffffffffu, t, o);
+        if (tid % (kSegFine / 2) == 0) sm.fine_seg[tid / (kSegFine / 2)] = t;
+    }
+    if (warp == 0) {
+        m_all = warp_sum_u64(lane < kShapeWarps ? sm.part[lane] : 0ull);
+        m_above = warp_sum_u64(lane < kShapeWarps ? sm.part2[lane] : 0ull);
+        if (lane == 0) { sm.cta[2] = m_all; sm.cta[3] = m_above; }
     }
     shape_sync<C>();
     m_all = 0;
@@ -549,26 +586,28 @@ __device__ unsigned long long shape_top_p(const T* row, int j0, int j1, const Ro
 #pragma unroll
     for (int c = 0; c < C; ++c) { m_all += shape_peer<C>(&sm.cta[2], c); run += shape_peer<C>(&sm.cta[3], c); }
     const unsigned long long need = (unsigned long long)ceil(p * (double)m_all);
-    unsigned long long f[2], fsum = 0;
+    if (warp == 0) {                               // the segment of fine bins, then the bin
+        auto sum_of = [&](const unsigned long long* at) {
+            unsigned long long t = 0;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        f[i] = 0;
+            for (int c = 0; c < C; ++c) t += shape_peer<C>(at, c);
+            return t;
+        };
+        int at = 0;
+        bool in = run < need;
 #pragma unroll
-        for (int c = 0; c < C; ++c) f[i] += shape_peer<C>(sm.fine + tid * 2 + i, c);
-        fsum += f[i];
-    }
-    const unsigned long long fincl = warp_scan_u64(fsum);
-    if (lane == 31) sm.part[warp] = fincl;
-    __syncthreads();
-    run += fincl - fsum;
-    for (int w = 0; w < warp; ++w) run += sm.part[w];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        if (run < need && need <= run + f[i]) {
-            sm.found[0] = (unsigned long long)(tid * 2 + i);
+        for (int step = 0; step < 2; ++step) {
+            const unsigned long long mine = sum_of(step == 0 ? sm.fine_seg + lane : sm.fine + at * kSegFine + lane), incl = run + warp_scan_u64(mine);
+            const unsigned hit = __ballot_sync(0xffffffffu, need <= incl);
+            in = in && hit;
+            const int l = hit ? __ffs(hit) - 1 : 0;
+            at = at * kSegFine + l;
+            run = __shfl_sync(0xffffffffu, incl - mine, l);
+        }
+        if (lane == 0) {
+            sm.found[0] = in ? (unsigned long long)at : ~0ull;
             sm.found[1] = run;
         }
-        run += f[i];
     }
     __syncthreads();
     const unsigned long long before = sm.found[1];
@@ -732,9 +771,11 @@ __device__ void shape_row(const T* row, int V, const Shaping s, float u, int32_t
     else if (cut_p) shape_walk<T, VEC>(row, j0, j1, [&](float l, int id) { look(l, id); shape_count<true>(bins, l, sm.coarse); });
     else shape_walk<T, VEC>(row, j0, j1, look);
     unsigned long long top = cta_reduce_u64<true>(bad ? ~0ull : best_id < V ? order_key(best, best_id) : 0ull, sm.part);
+    if (cut_k) shape_segments<false>(sm);
+    else if (cut_p) shape_segments<true>(sm);
+    if (tid == 0) sm.cta[0] = top;
+    shape_sync<C>();
     if (C > 1) {
-        if (tid == 0) sm.cta[0] = top;
-        cluster_sync_all();
 #pragma unroll
         for (int c = 0; c < C; ++c) {
             const unsigned long long t = shape_peer<C>(&sm.cta[0], c);
