@@ -23,6 +23,11 @@ Kv4Where where_of(const pipesd_kv4_cfg* c, int n_req, int rows, const int32_t* r
 }
 bool dtype_ok(int32_t dtype) { return dtype == PIPESD_F32 || dtype == PIPESD_BF16; }
 bool aligned(const void* p, int32_t dtype) { return (uintptr_t)p % (dtype == PIPESD_F32 ? 4 : 2) == 0; }
+bool wide(const void* p, int64_t stride, int32_t rows, int32_t dtype) {
+    return (uintptr_t)p % 16 == 0 && (rows == 1 || stride * (dtype == PIPESD_F32 ? 4 : 2) % 16 == 0);
+}
+// n rows behind any base touch at most n / 16 + 2 units, and no more than n.
+int most_units(int32_t n_req, int32_t rows) { return (int)std::min<int64_t>(rows, rows / kKv4Unit + 2ll * n_req); }
 int32_t launched() { return cudaGetLastError() == cudaSuccess ? PIPESD_OK : PIPESD_E_CUDA; }
 
 using AttendFn = void (*)(Kv4AttendArgs);
@@ -78,10 +83,9 @@ int32_t pipesd_kv4_append(const pipesd_kv4_cfg* cfg, void* pool, const void* k, 
     if (!where_ok(cfg, pool, n_req, rows, row0, base, table) || !k || !v || !dtype_ok(dtype) || !aligned(k, dtype) || !aligned(v, dtype)) return PIPESD_E_INVALID;
     const int64_t width = (int64_t)cfg->n_kv_heads * cfg->head_dim;
     if (rows > 1 && (k_stride < width || v_stride < width)) return PIPESD_E_INVALID;
-    const Kv4AppendArgs a = {where_of(cfg, n_req, rows, row0, base, table), k, v, k_stride, v_stride, static_cast<unsigned char*>(pool)};
-    // n rows behind any base touch at most n / 16 + 2 units, and no more than n
-    const long long units = std::min<long long>(rows, rows / kKv4Unit + 2ll * n_req);
-    const dim3 grid((unsigned)units, (unsigned)cfg->n_kv_heads);
+    const Kv4AppendArgs a = {where_of(cfg, n_req, rows, row0, base, table), k, v, k_stride, v_stride, static_cast<unsigned char*>(pool),
+                             wide(k, k_stride, rows, dtype) && wide(v, v_stride, rows, dtype)};
+    const dim3 grid((unsigned)most_units(n_req, rows), (unsigned)cfg->n_kv_heads);
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (cfg->head_dim == 128) {
         if (dtype == PIPESD_F32) kv4_append_kernel<128, float><<<grid, kKv4AppendThreads, 0, st>>>(a);
@@ -96,9 +100,11 @@ int32_t pipesd_kv4_append(const pipesd_kv4_cfg* cfg, void* pool, const void* k, 
 int32_t pipesd_kv4_read(const pipesd_kv4_cfg* cfg, const void* pool, float* k, float* v, int32_t n_req, int32_t rows, const int32_t* row0,
                         const int32_t* base, const int32_t* table, void* cuda_stream) {
     if (!where_ok(cfg, pool, n_req, rows, row0, base, table) || !k || !v || (uintptr_t)k % 16 || (uintptr_t)v % 16) return PIPESD_E_INVALID;
-    const Kv4ReadArgs a = {where_of(cfg, n_req, rows, row0, base, table), static_cast<unsigned char*>(const_cast<void*>(pool)), k, v};
-    if (cfg->head_dim == 128) kv4_read_kernel<128><<<rows, 256, 0, (cudaStream_t)cuda_stream>>>(a);
-    else kv4_read_kernel<64><<<rows, 256, 0, (cudaStream_t)cuda_stream>>>(a);
+    const Kv4ReadArgs a = {where_of(cfg, n_req, rows, row0, base, table), static_cast<unsigned char*>(const_cast<void*>(pool)), k, v,
+                           most_units(n_req, rows)};
+    const dim3 grid((unsigned)(a.units + (rows + kKv4Unit - 1) / kKv4Unit), (unsigned)cfg->n_kv_heads);
+    if (cfg->head_dim == 128) kv4_read_kernel<128><<<grid, kKv4AppendThreads, 0, (cudaStream_t)cuda_stream>>>(a);
+    else kv4_read_kernel<64><<<grid, kKv4AppendThreads, 0, (cudaStream_t)cuda_stream>>>(a);
     return launched();
 }
 

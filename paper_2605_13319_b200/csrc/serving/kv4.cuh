@@ -51,13 +51,81 @@ __device__ __forceinline__ unsigned char* kv4_unit(unsigned char* pool, const Kv
 }
 
 __device__ __forceinline__ float kv4_in(float x) { return x == x ? fminf(fmaxf(x, -kKv4Limit), kKv4Limit) : 0.f; }
-__device__ __forceinline__ void kv4_load8(const float* p, float (&x)[8]) {
+// Eight neighbouring values; wide: in 16-byte pieces.
+__device__ __forceinline__ void kv4_load8(const float* p, bool wide, float (&x)[8]) {
+    if (wide) {
+        *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(p);
+        *reinterpret_cast<float4*>(x + 4) = *reinterpret_cast<const float4*>(p + 4);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = kv4_in(p[i]);
+        for (int i = 0; i < 8; ++i) x[i] = p[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = kv4_in(x[i]);
 }
-__device__ __forceinline__ void kv4_load8(const uint16_t* p, float (&x)[8]) {
+__device__ __forceinline__ void kv4_load8(const uint16_t* p, bool wide, float (&x)[8]) {
+    uint16_t h[8];
+    if (wide) {
+        *reinterpret_cast<uint4*>(h) = *reinterpret_cast<const uint4*>(p);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = kv4_in(bf16_bits_to_f32(p[i]));
+        for (int i = 0; i < 8; ++i) h[i] = p[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = kv4_in(bf16_bits_to_f32(h[i]));
+}
+
+// The n-th of the units that the requests' rows touch, in order (one warp; -1: there are not as many), and its number.
+__device__ __forceinline__ int kv4_nth_unit(const Kv4Where& w, int nth, int& unit) {
+    const int lane = threadIdx.x & 31;
+    unit = 0;
+    for (int r0 = 0; r0 < w.n_req; r0 += 32) {
+        int first, base = 0, n = 0;
+        if (r0 + lane < w.n_req) n = kv4_rows(w, r0 + lane, first, base);
+        const int u0 = base / kKv4Unit, cnt = n > 0 ? (base + n - 1) / kKv4Unit - u0 + 1 : 0;
+        int inc = cnt;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int t = __shfl_up_sync(0xffffffffu, inc, o);
+            if (lane >= o) inc += t;
+        }
+        const unsigned hit = __ballot_sync(0xffffffffu, nth < inc);
+        if (hit) {
+            const int l = __ffs(hit) - 1;
+            unit = __shfl_sync(0xffffffffu, u0 + nth - (inc - cnt), l);
+            return r0 + l;
+        }
+        nth -= __shfl_sync(0xffffffffu, inc, 31);
+    }
+    return -1;
+}
+
+// Scale of a group and codes of eight of its values, as the definition has them in exact arithmetic.  fp32 decides where it can: the
+// quotients are off by 2^-20 at most, so that only those within 1e-5 of a border (and a scale within four steps of one between two
+// bf16 values) need fp64.
+__device__ __forceinline__ uint16_t kv4_scale(float mx, float z) {
+    const float q = (mx - z) * (1.f / 15.f);
+    const uint32_t low = __float_as_uint(q) & 0xffffu;
+    if (low - 0x7ffcu > 8u && fabsf(q) > 1e-30f) return f32_to_bf16_bits(q);
+    return f32_to_bf16_bits((float)(((double)mx - (double)z) / 15.0));
+}
+__device__ __forceinline__ uint32_t kv4_codes(const float (&x)[8], float s, float z) {
+    if (!(s > 0.f)) return 0u;
+    uint32_t word = 0;
+    bool near = s < 1e-30f;                        // (its reciprocal, or the quotient's steps, may leave fp32's range)
+    const float inv = 1.f / s;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float t = (x[i] - z) * inv, n = rintf(t);
+        near |= fabsf(fabsf(t - n) - 0.5f) < 1e-5f;
+        word |= (uint32_t)fminf(fmaxf(n, 0.f), 15.f) << (4 * i);
+    }
+    if (near) {
+        word = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) word |= (uint32_t)fmin(fmax(rint(((double)x[i] - (double)z) / (double)s), 0.0), 15.0) << (4 * i);
+    }
+    return word;
 }
 
 struct Kv4AppendArgs {
@@ -65,6 +133,7 @@ struct Kv4AppendArgs {
     const void *k, *v;
     long long k_stride, v_stride;      // elements between rows
     unsigned char* pool;
+    bool wide;                         // rows and heads begin at multiples of 16 bytes
 };
 
 // One CTA per (unit that gets new rows, KV head): 8 columns of a row per thread; four neighbouring threads hold a group.
@@ -77,28 +146,10 @@ __global__ void __launch_bounds__(kKv4AppendThreads) kv4_append_kernel(const Kv4
     __shared__ uint32_t codes[kKv4Unit][HD / 8];           // of V: [position][8 columns]
     __shared__ uint32_t s_sz[kKv4Unit][kGroups];
     const int tid = threadIdx.x, head = blockIdx.y;
-    if (tid < 32) {                                        // the blockIdx.x-th unit of the requests' units in order
-        int left = blockIdx.x, found = -1, unit = 0;
-        for (int r0 = 0; r0 < a.w.n_req && found < 0; r0 += 32) {
-            int first, base = 0, n = 0;
-            if (r0 + tid < a.w.n_req) n = kv4_rows(a.w, r0 + tid, first, base);
-            const int u0 = base / kKv4Unit, cnt = n > 0 ? (base + n - 1) / kKv4Unit - u0 + 1 : 0;
-            int inc = cnt;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int t = __shfl_up_sync(0xffffffffu, inc, o);
-                if (tid >= o) inc += t;
-            }
-            const unsigned hit = __ballot_sync(0xffffffffu, left < inc);
-            if (hit) {
-                const int l = __ffs(hit) - 1;
-                found = r0 + l;
-                unit = __shfl_sync(0xffffffffu, u0 + left - (inc - cnt), l);
-            } else {
-                left -= __shfl_sync(0xffffffffu, inc, 31);
-            }
-        }
-        if (tid == 0) { s_req = found; s_unit = unit; }
+    if (tid < 32) {
+        int unit;
+        const int req = kv4_nth_unit(a.w, blockIdx.x, unit);
+        if (tid == 0) { s_req = req; s_unit = unit; }
     }
     __syncthreads();
     const int req = s_req, unit = s_unit;
@@ -114,7 +165,7 @@ __global__ void __launch_bounds__(kKv4AppendThreads) kv4_append_kernel(const Kv4
         const size_t row = (size_t)(first + unit * kKv4Unit + slot - base);
         const T* src = static_cast<const T*>(kv ? a.v : a.k) + row * (kv ? a.v_stride : a.k_stride) + (size_t)head * HD + piece * 8;
         float x[8];
-        kv4_load8(src, x);
+        kv4_load8(src, a.wide, x);
         float mn = x[0], mx = x[0];
 #pragma unroll
         for (int i = 1; i < 8; ++i) { mn = fminf(mn, x[i]); mx = fmaxf(mx, x[i]); }
@@ -125,13 +176,9 @@ __global__ void __launch_bounds__(kKv4AppendThreads) kv4_append_kernel(const Kv4
             mx = fmaxf(mx, __shfl_xor_sync(quad, mx, o));
         }
         const uint16_t zb = f32_to_bf16_bits(mn);
-        const double z = (double)bf16_bits_to_f32(zb);
-        const uint16_t sb = f32_to_bf16_bits((float)(((double)mx - z) / 15.0));
-        const double s = (double)bf16_bits_to_f32(sb);
-        uint32_t word = 0;
-        if (s > 0.0)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) word |= (uint32_t)fmin(fmax(rint(((double)x[i] - z) / s), 0.0), 15.0) << (4 * i);
+        const float z = bf16_bits_to_f32(zb);
+        const uint16_t sb = kv4_scale(mx, z);
+        const uint32_t word = kv4_codes(x, bf16_bits_to_f32(sb), z);
         const int group = piece >> 2, t = piece & 3;
         if (kv == 0) {
             *reinterpret_cast<uint32_t*>(dst + slot * (HD / 2) + (t * kGroups + group) * 4) = word;
@@ -169,47 +216,77 @@ struct Kv4ReadArgs {
     Kv4Where w;
     unsigned char* pool;
     float *k, *v;              // [rows][Hkv][HD]
+    int units;
 };
 
-// The values of the positions that belong to the rows: one warp per (row, KV head) and step; 0 where no page is mapped.
+// The values of the rows' positions.  CTAs below `units`: one (unit, KV head) each, 8 columns of a row per thread.  The others look for rows
+// that have no position in any unit (no page, behind the table's end, no request): zeros.
 template <int HD>
-__global__ void __launch_bounds__(256) kv4_read_kernel(const Kv4ReadArgs a) {
-    constexpr int kPieces = HD / 8, kGroups = HD / kKv4Group;
-    const int row = blockIdx.x;
-    __shared__ int s_req;
-    if (threadIdx.x == 0) s_req = -1;
+__global__ void __launch_bounds__(kKv4AppendThreads) kv4_read_kernel(const Kv4ReadArgs a) {
+    constexpr int kPieces = HD / 8, kGroups = HD / kKv4Group, kTasks = kKv4Unit * kPieces;
+    __shared__ int s_req, s_unit;
+    __shared__ __align__(16) uint32_t words[20 * HD / 4];
+    const int tid = threadIdx.x, head = blockIdx.y;
+    auto put = [&](int kv, size_t row, int piece, const float (&x)[8]) {
+        float4* out = reinterpret_cast<float4*>((kv ? a.v : a.k) + (row * a.w.Hkv + head) * HD + piece * 8);
+        out[0] = make_float4(x[0], x[1], x[2], x[3]);
+        out[1] = make_float4(x[4], x[5], x[6], x[7]);
+    };
+    const float none[8] = {};
+    if ((int)blockIdx.x >= a.units) {              // sixteen rows, sixteen threads each
+        __shared__ int has[kKv4Unit];
+        const int local = tid / kKv4Unit, row = ((int)blockIdx.x - a.units) * kKv4Unit + local;
+        if (tid < kKv4Unit) has[tid] = 0;
+        __syncthreads();
+        for (int r = tid % kKv4Unit; r < a.w.n_req; r += kKv4Unit) {
+            int first, base;
+            const int n = kv4_rows(a.w, r, first, base);
+            if (n > 0 && row >= first && row < first + n) has[local] = 1;
+        }
+        __syncthreads();
+        if (row < a.w.rows && !has[local])
+            for (int i = tid % kKv4Unit; i < 2 * kPieces; i += kKv4Unit) put(i / kPieces, row, i % kPieces, none);
+        return;
+    }
+    if (tid < 32) {
+        int unit;
+        const int req = kv4_nth_unit(a.w, blockIdx.x, unit);
+        if (tid == 0) { s_req = req; s_unit = unit; }
+    }
     __syncthreads();
-    for (int i = threadIdx.x; i < a.w.n_req; i += 256)
-        if (a.w.row0[i] <= row && row < a.w.row0[i + 1]) s_req = i;
-    __syncthreads();
-    if (s_req < 0) return;
+    const int req = s_req, unit = s_unit;
+    if (req < 0) return;
     int first, base;
-    const int n = kv4_rows(a.w, s_req, first, base), pos = base + row - first;
-    const bool in = row - first < n;
-    for (int task = threadIdx.x; task < 2 * a.w.Hkv * kPieces; task += 256) {
-        const int kv = task / (a.w.Hkv * kPieces), head = task / kPieces % a.w.Hkv, piece = task % kPieces, group = piece >> 2, slot = pos % kKv4Unit;
-        const unsigned char* u = in ? kv4_unit(a.pool, a.w, s_req, head, pos / kKv4Unit, HD) : nullptr;
+    const int n = kv4_rows(a.w, req, first, base);
+    const int lo = max(0, base - unit * kKv4Unit), hi = min(kKv4Unit, base + n - unit * kKv4Unit);
+    const unsigned char* u = kv4_unit(a.pool, a.w, req, head, unit, HD);
+    if (u)
+        for (int i = tid; i < 20 * HD / 16; i += kKv4AppendThreads) reinterpret_cast<uint4*>(words)[i] = reinterpret_cast<const uint4*>(u)[i];
+    __syncthreads();
+    for (int task = tid; task < 2 * kTasks; task += kKv4AppendThreads) {
+        const int kv = task / kTasks, slot = task % kTasks / kPieces, piece = task % kPieces, group = piece >> 2;
+        if (slot < lo || slot >= hi) continue;
+        const size_t row = (size_t)(first + unit * kKv4Unit + slot - base);
         float x[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = 0.f;
-        if (u && kv == 0) {
-            const uint32_t word = *reinterpret_cast<const uint32_t*>(u + slot * (HD / 2) + ((piece & 3) * kGroups + group) * 4);
-            const uint32_t sz = *reinterpret_cast<const uint32_t*>(u + kv4_k_scales(HD) + (slot * kGroups + group) * 4);
+        if (!u) {
+            put(kv, row, piece, none);
+            continue;
+        }
+        if (kv == 0) {
+            const uint32_t word = words[slot * (HD / 8) + (piece & 3) * kGroups + group], sz = words[kv4_k_scales(HD) / 4 + slot * kGroups + group];
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] = fmaf((float)(word >> (4 * i) & 15u), __uint_as_float(sz << 16), __uint_as_float(sz & 0xffff0000u));
-        } else if (u) {
-            const uint16_t* sz = reinterpret_cast<const uint16_t*>(u + kv4_v_scales(HD)) + group * kKv4Unit + slot;
+        } else {
+            const uint16_t* sz = reinterpret_cast<const uint16_t*>(words) + kv4_v_scales(HD) / 2 + group * kKv4Unit + slot;
             const float s = bf16_bits_to_f32(sz[0]), z = bf16_bits_to_f32(sz[HD / 2]);
             const int tile = piece >> 1, nib = (piece & 1) + 2 * (slot >> 3) + 4 * (slot & 1), t = slot % 8 / 2;
 #pragma unroll
             for (int g = 0; g < 8; ++g) {
-                const uint32_t word = reinterpret_cast<const uint32_t*>(u + kv4_v_codes(HD))[(tile / 4 * 32 + g * 4 + t) * 4 + tile % 4];
+                const uint32_t word = words[kv4_v_codes(HD) / 4 + (tile / 4 * 32 + g * 4 + t) * 4 + tile % 4];
                 x[g] = fmaf((float)(word >> (4 * nib) & 15u), s, z);
             }
         }
-        float4* out = reinterpret_cast<float4*>((kv ? a.v : a.k) + ((size_t)row * a.w.Hkv + head) * HD + piece * 8);
-        out[0] = make_float4(x[0], x[1], x[2], x[3]);
-        out[1] = make_float4(x[4], x[5], x[6], x[7]);
+        put(kv, row, piece, x);
     }
 }
 
