@@ -85,7 +85,9 @@ int32_t pipesd_kv4_append(const pipesd_kv4_cfg* cfg, void* pool, const void* k, 
     if (rows > 1 && (k_stride < width || v_stride < width)) return PIPESD_E_INVALID;
     const Kv4AppendArgs a = {where_of(cfg, n_req, rows, row0, base, table), k, v, k_stride, v_stride, static_cast<unsigned char*>(pool),
                              wide(k, k_stride, rows, dtype) && wide(v, v_stride, rows, dtype)};
-    const dim3 grid((unsigned)most_units(n_req, rows), (unsigned)cfg->n_kv_heads);
+    // enough CTAs to fill the device four times over; beyond that a CTA takes several heads of its unit
+    const int units = most_units(n_req, rows);
+    const dim3 grid((unsigned)units, (unsigned)std::min(cfg->n_kv_heads, std::max(1, 4 * 148 / units)));
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (cfg->head_dim == 128) {
         if (dtype == PIPESD_F32) kv4_append_kernel<128, float><<<grid, kKv4AppendThreads, 0, st>>>(a);

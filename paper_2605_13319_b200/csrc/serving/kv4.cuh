@@ -50,8 +50,7 @@ __device__ __forceinline__ unsigned char* kv4_unit(unsigned char* pool, const Kv
     return pool + (((size_t)page * w.Hkv + head) * (w.page_size / kKv4Unit) + pos % w.page_size / kKv4Unit) * kv4_unit_bytes(hd);
 }
 
-__device__ __forceinline__ float kv4_in(float x) { return x == x ? fminf(fmaxf(x, -kKv4Limit), kKv4Limit) : 0.f; }
-// Eight neighbouring values; wide: in 16-byte pieces.
+// Eight neighbouring values as they come (wide: in 16-byte pieces), and put within the limits: a NaN as 0.
 __device__ __forceinline__ void kv4_load8(const float* p, bool wide, float (&x)[8]) {
     if (wide) {
         *reinterpret_cast<float4*>(x) = *reinterpret_cast<const float4*>(p);
@@ -60,19 +59,25 @@ __device__ __forceinline__ void kv4_load8(const float* p, bool wide, float (&x)[
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = p[i];
     }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = kv4_in(x[i]);
 }
 __device__ __forceinline__ void kv4_load8(const uint16_t* p, bool wide, float (&x)[8]) {
-    uint16_t h[8];
+    uint32_t h[4];
     if (wide) {
         *reinterpret_cast<uint4*>(h) = *reinterpret_cast<const uint4*>(p);
     } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) h[i] = p[i];
+        for (int i = 0; i < 4; ++i) h[i] = pack2(p[2 * i], p[2 * i + 1]);
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = kv4_in(bf16_bits_to_f32(h[i]));
+    for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(h[i] << 16); x[2 * i + 1] = __uint_as_float(h[i] & 0xffff0000u); }
+}
+__device__ __forceinline__ void kv4_limit8(float (&x)[8]) {
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) most = max(most, __float_as_uint(x[i]) & 0x7fffffffu);
+    if (most <= __float_as_uint(kKv4Limit)) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = x[i] == x[i] ? fminf(fmaxf(x[i], -kKv4Limit), kKv4Limit) : 0.f;
 }
 
 // The n-th of the units that the requests' rows touch, in order (one warp; -1: there are not as many), and its number.
@@ -101,31 +106,38 @@ __device__ __forceinline__ int kv4_nth_unit(const Kv4Where& w, int nth, int& uni
 }
 
 // Scale of a group and codes of eight of its values, as the definition has them in exact arithmetic.  fp32 decides where it can: the
-// quotients are off by 2^-20 at most, so that only those within 1e-5 of a border (and a scale within four steps of one between two
-// bf16 values) need fp64.
+// quotients are off by 2^-20 at most, so that only those within 1e-5 of a border, and a scale within four steps of one between two
+// bf16 values, need more.
 __device__ __forceinline__ uint16_t kv4_scale(float mx, float z) {
     const float q = (mx - z) * (1.f / 15.f);
     const uint32_t low = __float_as_uint(q) & 0xffffu;
     if (low - 0x7ffcu > 8u && fabsf(q) > 1e-30f) return f32_to_bf16_bits(q);
     return f32_to_bf16_bits((float)(((double)mx - (double)z) / 15.0));
 }
+// A quotient near a border m + 1/2 (values of 8 bits fall on one every few hundred times): the sign of x - z - (m + 1/2) s, with the
+// difference's rounding error; the product is exact, 13 bits.
+__device__ __noinline__ float kv4_at_border(float x, float z, float s, float m) {
+    const float d = __fsub_rn(x, z), zz = __fsub_rn(d, x), err = __fadd_rn(__fsub_rn(x, __fsub_rn(d, zz)), -__fadd_rn(z, zz));
+    const float over = __fadd_rn(__fsub_rn(d, __fmul_rn(m + 0.5f, s)), err);
+    return over > 0.f || (over == 0.f && ((int)m & 1)) ? m + 1.f : m;
+}
 __device__ __forceinline__ uint32_t kv4_codes(const float (&x)[8], float s, float z) {
     if (!(s > 0.f)) return 0u;
     uint32_t word = 0;
-    bool near = s < 1e-30f;                        // (its reciprocal, or the quotient's steps, may leave fp32's range)
-    const float inv = 1.f / s;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float t = (x[i] - z) * inv, n = rintf(t);
-        near |= fabsf(fabsf(t - n) - 0.5f) < 1e-5f;
-        word |= (uint32_t)fminf(fmaxf(n, 0.f), 15.f) << (4 * i);
-    }
-    if (near) {
-        word = 0;
+    if (s < 1e-30f) {                              // its reciprocal, or the quotient's steps, may leave fp32's range
 #pragma unroll
         for (int i = 0; i < 8; ++i) word |= (uint32_t)fmin(fmax(rint(((double)x[i] - (double)z) / (double)s), 0.0), 15.0) << (4 * i);
+        return word;
     }
-    return word;
+    const float inv = __frcp_rn(s), big = 12582912.f;      // 1.5 * 2^23: the sum's last bits are the rounded quotient
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float t = fminf(fmaxf((x[i] - z) * inv, 0.f), 15.f);
+        float n = t + big;
+        if (fabsf(t - (n - big)) > 0.49999f) n = kv4_at_border(x[i], z, s, floorf(t)) + big;
+        word += __float_as_uint(n) << (4 * i);
+    }
+    return word - 0x4b400000u * 0x11111111u;       // the big ones' bits, shifted like the codes
 }
 
 struct Kv4AppendArgs {
@@ -136,79 +148,101 @@ struct Kv4AppendArgs {
     bool wide;                         // rows and heads begin at multiples of 16 bytes
 };
 
-// One CTA per (unit that gets new rows, KV head): 8 columns of a row per thread; four neighbouring threads hold a group.
-// A unit's V words hold two to eight positions each, so the CTA owns the unit and keeps the nibbles of the positions before its rows.
+// An 8 x 8 transpose of nibbles over the lanes whose numbers differ in the bits 0, 3 and 2: lane j of them (j made of these bits, in this
+// order) gets the j-th nibbles of all eight.
+__device__ __forceinline__ uint32_t kv4_transpose(uint32_t x) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int k = 0; k < 3; ++k) {
+        const int bit = k == 0 ? 1 : k == 1 ? 8 : 4, shift = 4 << k;
+        const uint32_t even = k == 0 ? 0x0f0f0f0fu : k == 1 ? 0x00ff00ffu : 0x0000ffffu;     // nibbles whose number has the bit k clear
+        const uint32_t y = __shfl_xor_sync(0xffffffffu, x, bit);
+        x = lane & bit ? (x & ~even) | ((y & ~even) >> shift) : (x & even) | ((y & even) << shift);
+    }
+    return x;
+}
+
+// A CTA takes a unit that gets new rows, and KV heads blockIdx.y, + gridDim.y, ...  A warp has one group of columns and eight of the unit's
+// positions (2t, 2t + 1, 2t + 8, 2t + 9 for two t), four lanes to a group, 8 columns each: what the words of V are made of, so that
+// nibbles change places within the warp and no barrier is needed.  V's words hold several positions: those that are not new keep theirs.
+// Bound: the latency of finding the unit and its page (three dependent loads) at few rows, instructions (about 15 a value) at many.
 constexpr int kKv4AppendThreads = 256;
 template <int HD, typename T>
 __global__ void __launch_bounds__(kKv4AppendThreads) kv4_append_kernel(const Kv4AppendArgs a) {
-    constexpr int kPieces = HD / 8, kGroups = HD / kKv4Group, kTasks = kKv4Unit * kPieces;
-    __shared__ int s_req, s_unit;
-    __shared__ uint32_t codes[kKv4Unit][HD / 8];           // of V: [position][8 columns]
-    __shared__ uint32_t s_sz[kKv4Unit][kGroups];
-    const int tid = threadIdx.x, head = blockIdx.y;
-    if (tid < 32) {
-        int unit;
-        const int req = kv4_nth_unit(a.w, blockIdx.x, unit);
-        if (tid == 0) { s_req = req; s_unit = unit; }
-    }
-    __syncthreads();
-    const int req = s_req, unit = s_unit;
+    constexpr int kGroups = HD / kKv4Group, kCombos = 2 * kGroups, kWarps = kKv4AppendThreads / 32;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    int unit;
+    const int req = kv4_nth_unit(a.w, blockIdx.x, unit);
     if (req < 0) return;
     int first, base;
     const int n = kv4_rows(a.w, req, first, base);
-    unsigned char* dst = kv4_unit(a.pool, a.w, req, head, unit, HD);
-    if (!dst) return;                                      // no page there: the rows are dropped
     const int lo = max(0, base - unit * kKv4Unit), hi = min(kKv4Unit, base + n - unit * kKv4Unit);     // new positions of the unit
-    for (int task = tid; task < 2 * kTasks; task += kKv4AppendThreads) {
-        const int kv = task / kTasks, slot = task % kTasks / kPieces, piece = task % kPieces;
-        if (slot < lo || slot >= hi) continue;             // the four threads of a group leave together
-        const size_t row = (size_t)(first + unit * kKv4Unit + slot - base);
-        const T* src = static_cast<const T*>(kv ? a.v : a.k) + row * (kv ? a.v_stride : a.k_stride) + (size_t)head * HD + piece * 8;
-        float x[8];
-        kv4_load8(src, a.wide, x);
-        float mn = x[0], mx = x[0];
+    const int combo = warp % kCombos, group = combo / 2;
+    const int piece = lane & 3, t = 2 * (combo & 1) + (lane >> 4), slot = 2 * t + (lane >> 2 & 1) + 8 * (lane >> 3 & 1);
+    const bool mine = slot >= lo && slot < hi;
+    const size_t row = (size_t)(first + unit * kKv4Unit + slot - base);
+    unsigned char* const unit0 = kv4_unit(a.pool, a.w, req, 0, unit, HD);
+    if (!unit0) return;                                    // no page there: the rows are dropped
+    const size_t head_bytes = (size_t)(a.w.page_size / kKv4Unit) * kv4_unit_bytes(HD);
+    constexpr int kKinds = kCombos == kWarps ? 2 : 1;      // of K and V, one warp does both or one
+    const int kind0 = kKinds == 2 ? 0 : warp / kCombos;
+    const size_t col = group * kKv4Group + piece * 8;
+    float next[kKinds][8];
+    auto fetch = [&](int head) {
 #pragma unroll
-        for (int i = 1; i < 8; ++i) { mn = fminf(mn, x[i]); mx = fmaxf(mx, x[i]); }
-        const unsigned quad = 0xfu << (tid & 28);
+        for (int i = 0; i < kKinds; ++i) {
+            const int kv = kind0 + i;
+            if (mine) kv4_load8(static_cast<const T*>(kv ? a.v : a.k) + row * (kv ? a.v_stride : a.k_stride) + (size_t)head * HD + col, a.wide, next[i]);
+        }
+    };
+    fetch(blockIdx.y);
+    for (int head = blockIdx.y; head < a.w.Hkv; head += gridDim.y) {
+        float x[kKinds][8];
 #pragma unroll
-        for (int o = 1; o < 4; o <<= 1) {
-            mn = fminf(mn, __shfl_xor_sync(quad, mn, o));
-            mx = fmaxf(mx, __shfl_xor_sync(quad, mx, o));
-        }
-        const uint16_t zb = f32_to_bf16_bits(mn);
-        const float z = bf16_bits_to_f32(zb);
-        const uint16_t sb = kv4_scale(mx, z);
-        const uint32_t word = kv4_codes(x, bf16_bits_to_f32(sb), z);
-        const int group = piece >> 2, t = piece & 3;
-        if (kv == 0) {
-            *reinterpret_cast<uint32_t*>(dst + slot * (HD / 2) + (t * kGroups + group) * 4) = word;
-            if (t == 0) *reinterpret_cast<uint32_t*>(dst + kv4_k_scales(HD) + (slot * kGroups + group) * 4) = pack2(sb, zb);
-        } else {
-            codes[slot][piece] = word;
-            if (t == 0) s_sz[slot][group] = pack2(sb, zb);
-        }
-    }
-    __syncthreads();
-    if (tid < kKv4Unit * kGroups) {
-        const int group = tid / kKv4Unit, slot = tid % kKv4Unit;
-        if (slot >= lo && slot < hi) {
-            const uint32_t sz = s_sz[slot][group];
-            reinterpret_cast<uint16_t*>(dst + kv4_v_scales(HD))[tid] = (uint16_t)sz;
-            reinterpret_cast<uint16_t*>(dst + kv4_v_scales(HD) + HD)[tid] = (uint16_t)(sz >> 16);
-        }
-    }
-    for (int i = tid; i < 2 * HD; i += kKv4AppendThreads) {
-        const int tile = i / 128 * 4 + i % 4, lane = i / 4 % 32, g = lane / 4, t = lane % 4;
-        uint32_t* p = reinterpret_cast<uint32_t*>(dst + kv4_v_codes(HD)) + i;
-        uint32_t word = 0, fresh = 0;
+        for (int i = 0; i < kKinds; ++i)
 #pragma unroll
-        for (int nib = 0; nib < 8; ++nib) {
-            const int slot = 2 * t + (nib >> 2) + 8 * (nib >> 1 & 1);
-            if (slot < lo || slot >= hi) continue;
-            fresh |= 15u << (4 * nib);
-            word |= (codes[slot][tile * 2 + (nib & 1)] >> (4 * g) & 15u) << (4 * nib);
+            for (int e = 0; e < 8; ++e) x[i][e] = mine ? next[i][e] : 0.f;
+        if (head + (int)gridDim.y < a.w.Hkv) fetch(head + gridDim.y);
+        unsigned char* dst = unit0 + head * head_bytes;
+#pragma unroll
+        for (int i = 0; i < kKinds; ++i) {
+            const int kv = kind0 + i;
+            kv4_limit8(x[i]);
+            float mn = x[i][0], mx = x[i][0];
+#pragma unroll
+            for (int e = 1; e < 8; ++e) { mn = fminf(mn, x[i][e]); mx = fmaxf(mx, x[i][e]); }
+#pragma unroll
+            for (int o = 1; o < 4; o <<= 1) {
+                mn = fminf(mn, __shfl_xor_sync(0xffffffffu, mn, o));
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+            }
+            const uint16_t zb = f32_to_bf16_bits(mn);
+            const float z = bf16_bits_to_f32(zb);
+            const uint16_t sb = kv4_scale(mx, z);
+            const uint32_t word = kv4_codes(x[i], bf16_bits_to_f32(sb), z);
+            if (kv == 0) {
+                if (mine) {
+                    *reinterpret_cast<uint32_t*>(dst + slot * (HD / 2) + (piece * kGroups + group) * 4) = word;
+                    if (piece == 0) *reinterpret_cast<uint32_t*>(dst + kv4_k_scales(HD) + (slot * kGroups + group) * 4) = pack2(sb, zb);
+                }
+            } else {
+                if (mine && piece == 0) {
+                    uint16_t* sz = reinterpret_cast<uint16_t*>(dst + kv4_v_scales(HD)) + group * kKv4Unit + slot;
+                    sz[0] = sb;
+                    sz[HD / 2] = zb;
+                }
+                const uint32_t turned = kv4_transpose(word);
+                const int g = (lane & 1) | (lane >> 2 & 2) | (lane & 4), tile = 2 * group + (piece >> 1);
+                uint32_t fresh = 0;
+#pragma unroll
+                for (int nib = 0; nib < 8; ++nib) {
+                    const int at = 2 * t + (nib >> 2) + 8 * (nib >> 1 & 1);
+                    if (at >= lo && at < hi) fresh |= 15u << (4 * nib);
+                }
+                uint32_t* p = reinterpret_cast<uint32_t*>(dst + kv4_v_codes(HD)) + (tile / 4 * 32 + g * 4 + t) * 4 + tile % 4;
+                if (fresh) *p = fresh == 0xffffffffu ? turned : (*p & ~fresh) | (turned & fresh);
+            }
         }
-        if (fresh) *p = fresh == 0xffffffffu ? word : (*p & ~fresh) | word;
     }
 }
 
