@@ -104,7 +104,9 @@ int32_t pipesd_kv4_read(const pipesd_kv4_cfg* cfg, const void* pool, float* k, f
     if (!where_ok(cfg, pool, n_req, rows, row0, base, table) || !k || !v || (uintptr_t)k % 16 || (uintptr_t)v % 16) return PIPESD_E_INVALID;
     const Kv4ReadArgs a = {where_of(cfg, n_req, rows, row0, base, table), static_cast<unsigned char*>(const_cast<void*>(pool)), k, v,
                            most_units(n_req, rows)};
-    const dim3 grid((unsigned)(a.units + (rows + kKv4Unit - 1) / kKv4Unit), (unsigned)cfg->n_kv_heads);
+    const int64_t ctas = (int64_t)a.units * cfg->n_kv_heads + (rows + kKv4Unit - 1) / kKv4Unit;
+    if (ctas > INT32_MAX) return PIPESD_E_INVALID;
+    const dim3 grid((unsigned)ctas);
     if (cfg->head_dim == 128) kv4_read_kernel<128><<<grid, kKv4AppendThreads, 0, (cudaStream_t)cuda_stream>>>(a);
     else kv4_read_kernel<64><<<grid, kKv4AppendThreads, 0, (cudaStream_t)cuda_stream>>>(a);
     return launched();

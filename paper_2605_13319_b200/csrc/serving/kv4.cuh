@@ -129,13 +129,23 @@ __device__ __forceinline__ uint32_t kv4_codes(const float (&x)[8], float s, floa
         for (int i = 0; i < 8; ++i) word |= (uint32_t)fmin(fmax(rint(((double)x[i] - (double)z) / (double)s), 0.0), 15.0) << (4 * i);
         return word;
     }
-    const float inv = __frcp_rn(s), big = 12582912.f;      // 1.5 * 2^23: the sum's last bits are the rounded quotient
+    float inv;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(inv) : "f"(s));
+    const float big = 12582912.f;                  // 1.5 * 2^23: the sum's last bits are the rounded quotient
+    uint32_t near = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const float t = fminf(fmaxf((x[i] - z) * inv, 0.f), 15.f);
-        float n = t + big;
-        if (fabsf(t - (n - big)) > 0.49999f) n = kv4_at_border(x[i], z, s, floorf(t)) + big;
+        const float t = fminf(fmaxf((x[i] - z) * inv, 0.f), 15.f), n = t + big;
+        if (fabsf(t - (n - big)) > 0.49999f) near |= 1u << i;
         word += __float_as_uint(n) << (4 * i);
+    }
+    if (near) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (near >> i & 1u) {
+                const float t = fminf(fmaxf((x[i] - z) * inv, 0.f), 15.f), n = kv4_at_border(x[i], z, s, floorf(t));
+                word += (uint32_t)((int)n - (int)rintf(t)) << (4 * i);
+            }
     }
     return word - 0x4b400000u * 0x11111111u;       // the big ones' bits, shifted like the codes
 }
@@ -253,23 +263,23 @@ struct Kv4ReadArgs {
     int units;
 };
 
-// The values of the rows' positions.  CTAs below `units`: one (unit, KV head) each, 8 columns of a row per thread.  The others look for rows
+// The values of the rows' positions.  The first units * Hkv CTAs: one (unit, KV head) each, 8 columns of a row per thread.  The others look for rows
 // that have no position in any unit (no page, behind the table's end, no request): zeros.
 template <int HD>
 __global__ void __launch_bounds__(kKv4AppendThreads) kv4_read_kernel(const Kv4ReadArgs a) {
     constexpr int kPieces = HD / 8, kGroups = HD / kKv4Group, kTasks = kKv4Unit * kPieces;
     __shared__ int s_req, s_unit;
     __shared__ __align__(16) uint32_t words[20 * HD / 4];
-    const int tid = threadIdx.x, head = blockIdx.y;
-    auto put = [&](int kv, size_t row, int piece, const float (&x)[8]) {
-        float4* out = reinterpret_cast<float4*>((kv ? a.v : a.k) + (row * a.w.Hkv + head) * HD + piece * 8);
+    const int tid = threadIdx.x, nth = blockIdx.x / a.w.Hkv, head = blockIdx.x % a.w.Hkv;
+    auto put = [&](int kv, size_t row, int h, int piece, const float (&x)[8]) {
+        float4* out = reinterpret_cast<float4*>((kv ? a.v : a.k) + (row * a.w.Hkv + h) * HD + piece * 8);
         out[0] = make_float4(x[0], x[1], x[2], x[3]);
         out[1] = make_float4(x[4], x[5], x[6], x[7]);
     };
     const float none[8] = {};
-    if ((int)blockIdx.x >= a.units) {              // sixteen rows, sixteen threads each
+    if (nth >= a.units) {                          // sixteen rows, sixteen threads each
         __shared__ int has[kKv4Unit];
-        const int local = tid / kKv4Unit, row = ((int)blockIdx.x - a.units) * kKv4Unit + local;
+        const int local = tid / kKv4Unit, row = ((int)blockIdx.x - a.units * a.w.Hkv) * kKv4Unit + local;
         if (tid < kKv4Unit) has[tid] = 0;
         __syncthreads();
         for (int r = tid % kKv4Unit; r < a.w.n_req; r += kKv4Unit) {
@@ -279,12 +289,12 @@ __global__ void __launch_bounds__(kKv4AppendThreads) kv4_read_kernel(const Kv4Re
         }
         __syncthreads();
         if (row < a.w.rows && !has[local])
-            for (int i = tid % kKv4Unit; i < 2 * kPieces; i += kKv4Unit) put(i / kPieces, row, i % kPieces, none);
+            for (int i = tid % kKv4Unit; i < 2 * a.w.Hkv * kPieces; i += kKv4Unit) put(i & 1, row, i / 2 / kPieces, i / 2 % kPieces, none);
         return;
     }
     if (tid < 32) {
         int unit;
-        const int req = kv4_nth_unit(a.w, blockIdx.x, unit);
+        const int req = kv4_nth_unit(a.w, nth, unit);
         if (tid == 0) { s_req = req; s_unit = unit; }
     }
     __syncthreads();
@@ -303,7 +313,7 @@ __global__ void __launch_bounds__(kKv4AppendThreads) kv4_read_kernel(const Kv4Re
         const size_t row = (size_t)(first + unit * kKv4Unit + slot - base);
         float x[8];
         if (!u) {
-            put(kv, row, piece, none);
+            put(kv, row, head, piece, none);
             continue;
         }
         if (kv == 0) {
@@ -320,7 +330,7 @@ __global__ void __launch_bounds__(kKv4AppendThreads) kv4_read_kernel(const Kv4Re
                 x[g] = fmaf((float)(word >> (4 * nib) & 15u), s, z);
             }
         }
-        put(kv, row, piece, x);
+        put(kv, row, head, piece, x);
     }
 }
 
