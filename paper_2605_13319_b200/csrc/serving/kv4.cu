@@ -65,7 +65,7 @@ int32_t attend_run(Kv4AttendArgs& a, int nt, cudaStream_t st) {
     attend_fn<HD, T>(nt)<<<a.ctas, kAttendThreads, attend_smem<HD, T>(nt), st>>>(a);
     if (cudaGetLastError() != cudaSuccess) return PIPESD_E_CUDA;
     const long long jobs = (long long)a.w.rows * a.Hq;
-    kv4_merge_kernel<HD, T><<<(unsigned)((jobs + 7) / 8), 256, 0, st>>>(a);
+    if (launch_pdl(kv4_merge_kernel<HD, T>, dim3((unsigned)((jobs + 7) / 8)), dim3(256), 0, st, a) != cudaSuccess) return PIPESD_E_CUDA;
     return launched();
 }
 

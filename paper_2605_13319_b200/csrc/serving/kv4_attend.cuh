@@ -3,7 +3,8 @@
 //
 // All query rows that share a KV head form one narrow operand (row = chunk row * G + query head of the group; 8 NT of them at a time).
 // Per unit of 16 positions, with keys and then value columns on the M side of mma.m16n8k16 (fp16 operands, fp32 sums):
-//   S^T[16 keys x rows] = sum over groups of s_key,group * (codes . Q_group) + z_key,group * (sum of Q over the group)
+//   S^T[16 keys x rows] = sum over groups of s_key,group * (codes . Q_group), and, by one more product (bf16), zeros . (sums of Q
+//                         over the groups, as three bf16 terms)
 //   O^T[HD x rows]     += (codes - 8)^T . (P * s_key,group),   and one more product [z + 8 s of the groups; ones] . P, which is the
 //                         middles' share of the output and the denominators, both of the very P (rounded) that P * s is made of.
 // No value is ever dequantised.  A key's code goes into the tensor cores as the subnormal that its bits are, n * 2^-24; Q is
@@ -87,7 +88,7 @@ template <int HD, int NT, bool kSplit>
 struct AttendSmem {
     static constexpr int kRows = 8 * NT, kGroups = HD / kKv4Group, kTerms = kSplit ? 2 : 1;
     uint2 q[HD / 16][NT][kTerms][32];              // B fragments
-    float qsum[kGroups][kRows];                    // sums of a group's (scaled) entries
+    uint2 qsum[NT][32];                            // sums of the groups' (scaled) entries as a B fragment, bf16: k = 4 term + group
     float qc[kRows];                               // what a row's scores are multiplied with
     int horizon[kRows];                            // last visible position; -1 for a row that is none
     float ref[kAttendWarps][kRows], sum[kAttendWarps][kRows];
@@ -170,6 +171,7 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 ? 2 : 1) kv4_attend_ke
     SM& sm = *reinterpret_cast<SM*>(smem_raw);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const int G = a.Hq / a.w.Hkv;
+    pdl_launch_dependents();
 
     if (lane == 0)
         for (int i = 0; i < kAttendStages; ++i) mbar_init(smem_u32(&sm.bars[warp][i]), 1);
@@ -211,58 +213,8 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 ? 2 : 1) kv4_attend_ke
         const int head = triple / groups, rho0 = triple % groups * kRows;
         const int n_rows = min(kRows, n * G - rho0);
 
-        // ---- queries of the triple: normalised, split, in fragment order; one warp per row
-        for (int row = warp; row < kRows; row += kAttendWarps) {
-            constexpr int kE = HD / 32;            // neighbouring columns of a lane
-            float x[kE];
-            float mx = 0.f;
-            const int rho = rho0 + row;
-            if (row < n_rows) {
-                const T* src = static_cast<const T*>(a.q) + (size_t)(first + rho / G) * a.q_stride + (size_t)(head * G + rho % G) * HD + lane * kE;
-#pragma unroll
-                for (int i = 0; i < kE; ++i) { x[i] = attend_in(src[i]); mx = fmaxf(mx, fabsf(x[i])); }
-            } else {
-#pragma unroll
-                for (int i = 0; i < kE; ++i) x[i] = 0.f;
-            }
-            mx = warp_max_f32(mx);
-            int e = 0;
-            if (mx > 0.f && mx < INFINITY) e = ilogbf(mx) + 1;                // |q| < 2^e
-            float part = 0.f;
-#pragma unroll
-            for (int i = 0; i < kE; ++i) {
-                const int d = lane * kE + i, grp = d / 32, tt = d % 32 / 8, p = d % 8;
-                // the odd nibbles come in as 16 codes
-                uint32_t hi, lo;
-                const float qs = ldexpf(x[i], 15 - e), down = p & 1 ? 0.0625f : 1.f;
-                attend_split(qs * down, 0.f, hi, lo);
-                part += (kSplit ? f16_lo(hi) + f16_lo(lo) : f16_lo(hi)) * (p & 1 ? 16.f : 1.f);
-                uint16_t* dst = reinterpret_cast<uint16_t*>(&sm.q[2 * grp + (p >> 1 & 1)][row / 8][0][row % 8 * 4 + tt]) + 2 * (p & 1) + (p >> 2);
-                dst[0] = (uint16_t)hi;
-                if (kSplit) dst[32 * 4] = (uint16_t)lo;
-            }
-#pragma unroll
-            for (int o = 1; o < 32 / kGroups; o <<= 1) part += __shfl_xor_sync(0xffffffffu, part, o);
-            if (lane % (32 / kGroups) == 0) sm.qsum[lane / (32 / kGroups)][row] = part;
-            if (lane == 0) {
-                sm.qc[row] = ldexpf(a.scale, e - 15);
-                sm.horizon[row] = row < n_rows ? base + rho / G : -1;
-            }
-        }
-        __syncthreads();
         const int seen_all = base + rho0 / G;                                // positions up to here are visible to every row
         const int seen_any = base + (rho0 + n_rows - 1) / G;
-        float o[kTiles][NT][4], zl[NT][4], ref[NT][2];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-#pragma unroll
-            for (int m = 0; m < kTiles; ++m)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[m][nt][i] = 0.f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) zl[nt][i] = 0.f;
-            ref[nt][0] = ref[nt][1] = kAttendNone;
-        }
         float unit_scale = 0.f;                    // 0: nothing seen yet
         const int ulast = min(u1, seen_any / kKv4Unit + 1);                  // units from here on are hidden from every row
         const unsigned char* mine = nullptr;       // lane i: where the unit (it & ~31) + i of this warp is
@@ -286,7 +238,75 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 ? 2 : 1) kv4_attend_ke
             }
             mapped = (mapped & ~(1u << st)) | (src ? 1u << st : 0u);
         };
-        for (int it = 0; it < min(n_it, kAttendStages); ++it) request(it);
+        for (int it = 0; it < min(n_it, kAttendStages); ++it) request(it);       // (on their way while the queries are laid out)
+        // ---- queries of the triple: normalised, split, in fragment order; one warp per row
+        for (int row = warp; row < kRows; row += kAttendWarps) {
+            constexpr int kE = HD / 32;            // neighbouring columns of a lane
+            float x[kE];
+            float mx = 0.f;
+            const int rho = rho0 + row;
+            if (row < n_rows) {
+                const T* src = static_cast<const T*>(a.q) + (size_t)(first + rho / G) * a.q_stride + (size_t)(head * G + rho % G) * HD + lane * kE;
+#pragma unroll
+                for (int i = 0; i < kE; ++i) { x[i] = attend_in(src[i]); mx = fmaxf(mx, fabsf(x[i])); }
+            } else {
+#pragma unroll
+                for (int i = 0; i < kE; ++i) x[i] = 0.f;
+            }
+            mx = warp_max_f32(mx);
+            int e = 0;
+            if (mx > 0.f && mx < INFINITY) e = ilogbf(mx) + 1;                // |q| < 2^e
+            // 2^(15 - e), which may leave fp32's range, as two factors
+            const int half = (15 - e) / 2;
+            const float up0 = __int_as_float((127 + half) << 23), up1 = __int_as_float((127 + 15 - e - half) << 23);
+            float part = 0.f;
+#pragma unroll
+            for (int i = 0; i < kE; ++i) {
+                const int d = lane * kE + i, grp = d / 32, tt = d % 32 / 8, p = d % 8;
+                // the odd nibbles come in as 16 codes
+                uint32_t hi, lo;
+                const float qs = x[i] * up0 * up1, down = p & 1 ? 0.0625f : 1.f;
+                attend_split(qs * down, 0.f, hi, lo);
+                part += (kSplit ? f16_lo(hi) + f16_lo(lo) : f16_lo(hi)) * (p & 1 ? 16.f : 1.f);
+                uint16_t* dst = reinterpret_cast<uint16_t*>(&sm.q[2 * grp + (p >> 1 & 1)][row / 8][0][row % 8 * 4 + tt]) + 2 * (p & 1) + (p >> 2);
+                dst[0] = (uint16_t)hi;
+                if (kSplit) dst[32 * 4] = (uint16_t)lo;
+            }
+#pragma unroll
+            for (int o = 1; o < 32 / kGroups; o <<= 1) part += __shfl_xor_sync(0xffffffffu, part, o);
+            if (lane % (32 / kGroups) == 0) {
+                // k = 4 term + group sits in lane 4 (row % 8) + k % 8 / 2, register k / 8, half k % 2; groups that are none and the
+                // fourth term are 0
+                const int grp = lane / (32 / kGroups);
+                float rest = part;
+#pragma unroll
+                for (int term = 0; term < 4; ++term) {
+                    const uint16_t h = term < 3 ? f32_to_bf16_bits(rest) : (uint16_t)0;
+                    rest -= bf16_bits_to_f32(h);
+#pragma unroll
+                    for (int k = 4 * term + grp; k < 4 * term + 4; k += kGroups) {
+                        uint16_t* dst = reinterpret_cast<uint16_t*>(&sm.qsum[row / 8][row % 8 * 4 + k % 8 / 2]) + 2 * (k / 8) + k % 2;
+                        *dst = k % 4 < kGroups ? h : (uint16_t)0;
+                    }
+                }
+            }
+            if (lane == 0) {
+                sm.qc[row] = ldexpf(a.scale, e - 15);
+                sm.horizon[row] = row < n_rows ? base + rho / G : -1;
+            }
+        }
+        __syncthreads();
+        float o[kTiles][NT][4], zl[NT][4], ref[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int m = 0; m < kTiles; ++m)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[m][nt][i] = 0.f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) zl[nt][i] = 0.f;
+            ref[nt][0] = ref[nt][1] = kAttendNone;
+        }
 #pragma unroll 1
         for (int it = 0; it < n_it; ++it) {
             const int st = it % kAttendStages, u = u0 + warp + kAttendWarps * it;
@@ -328,10 +348,23 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 ? 2 : 1) kv4_attend_ke
             }
             const float vmax = fmaxf(fmaxf(fabsf(vs[0]), fabsf(vs[1])), fmaxf(fabsf(vm[0]), fabsf(vm[1])));
             // ---- scores: [2 keys][2 rows] of each tile of 8 rows
+            uint4 zf;                              // zeros of both keys: groups 2 (t % 2), + 1
+            {
+                const bool odd = kGroups == 4 && (t & 1);
+                zf.x = __byte_perm(odd ? ksz[0][kGroups - 2] : ksz[0][0], odd ? ksz[0][kGroups - 1] : ksz[0][1], 0x7632);
+                zf.y = __byte_perm(odd ? ksz[1][kGroups - 2] : ksz[1][0], odd ? ksz[1][kGroups - 1] : ksz[1][1], 0x7632);
+                if (kGroups == 2 && (t & 1)) zf.x = zf.y = 0u;
+                zf.z = t < 2 ? zf.x : 0u;          // (k from 12 on: nothing)
+                zf.w = t < 2 ? zf.y : 0u;
+            }
             float s[NT][4];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 float zq[4] = {0.f, 0.f, 0.f, 0.f};
+                {
+                    const uint2 b = sm.qsum[nt][lane];
+                    mma_bf16_16816(zq, zf, b.x, b.y);
+                }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) s[nt][i] = 0.f;
 #pragma unroll
@@ -347,12 +380,9 @@ __global__ void __launch_bounds__(kAttendThreads, NT == 1 ? 2 : 1) kv4_attend_ke
                             attend_mma(acc, af, b.x, b.y);
                         }
                     }
-                    const float2 qs = *reinterpret_cast<const float2*>(&sm.qsum[grp][nt * 8 + 2 * t]);
-                    const float s0 = bf16_lo(ksz[0][grp]), z0 = bf16_hi(ksz[0][grp]), s1 = bf16_lo(ksz[1][grp]), z1 = bf16_hi(ksz[1][grp]);
+                    const float s0 = bf16_lo(ksz[0][grp]), s1 = bf16_lo(ksz[1][grp]);
                     s[nt][0] = fmaf(s0, acc[0], s[nt][0]); s[nt][1] = fmaf(s0, acc[1], s[nt][1]);
                     s[nt][2] = fmaf(s1, acc[2], s[nt][2]); s[nt][3] = fmaf(s1, acc[3], s[nt][3]);
-                    zq[0] = fmaf(z0, qs.x, zq[0]); zq[1] = fmaf(z0, qs.y, zq[1]);
-                    zq[2] = fmaf(z1, qs.x, zq[2]); zq[3] = fmaf(z1, qs.y, zq[3]);
                 }
                 const float2 qc = *reinterpret_cast<const float2*>(&sm.qc[nt * 8 + 2 * t]);
 #pragma unroll
@@ -532,25 +562,28 @@ __global__ void __launch_bounds__(256) kv4_merge_kernel(const Kv4AttendArgs a) {
     constexpr int kE = HD / 32;
     const int lane = threadIdx.x & 31;
     const long long job = (long long)blockIdx.x * 8 + (threadIdx.x >> 5);
-    if (job >= (long long)a.w.rows * a.Hq) return;
-    const int row = (int)(job / a.Hq), qh = (int)(job % a.Hq), G = a.Hq / a.w.Hkv;
+    const bool in = job < (long long)a.w.rows * a.Hq;
+    const int row = in ? (int)(job / a.Hq) : -1, qh = in ? (int)(job % a.Hq) : 0, G = a.Hq / a.w.Hkv;
     int req = -1;
     for (int r0 = 0; r0 < a.w.n_req && req < 0; r0 += 32) {
-        const int r = r0 + lane;
-        const unsigned hit = __ballot_sync(0xffffffffu, r < a.w.n_req && a.w.row0[min(r, a.w.n_req - 1)] <= row && row < a.w.row0[min(r, a.w.n_req - 1) + 1]);
-        if (hit) req = r0 + __ffs(hit) - 1;
+        const int r = min(r0 + lane, a.w.n_req - 1);
+        const unsigned hit = __ballot_sync(0xffffffffu, a.w.row0[r] <= row && row < a.w.row0[r + 1]);
+        if (hit) req = min(r0 + __ffs(hit) - 1, a.w.n_req - 1);
     }
-    if (req < 0) return;
     int n, first, base, units, groups;
-    attend_load(a, req, n, first, base, units, groups);
+    attend_load(a, req < 0 ? a.w.n_req : req, n, first, base, units, groups);
+    long long before;
+    const long long all = attend_total(a, req, before), share = attend_share(all, a.ctas);
+    // Launched with programmatic serialisation: behind this the shares are complete.  Every thread waits, those without work too: a grid that
+    // ended without could let its successor begin before its predecessor has ended.
+    pdl_wait();
+    if (req < 0) return;
     T* out = static_cast<T*>(a.out) + (size_t)row * a.out_stride + (size_t)qh * HD + lane * kE;
     if (row - first >= n) {                        // a row without a position: nothing to see
 #pragma unroll
         for (int i = 0; i < kE; ++i) attend_out(out + i, 0.f);
         return;
     }
-    long long before;
-    const long long all = attend_total(a, req, before), share = attend_share(all, a.ctas);
     const int rho = (row - first) * G + qh % G;
     const long long start = before + (long long)(qh / G * groups + rho / a.rows_cap) * units;
     const int c0 = (int)(start / share), c1 = (int)((start + units - 1) / share);
