@@ -465,26 +465,29 @@ class _on:
             self.scopes.close()
 
 
-def _rows_of(t, name, width=None):
-    """Row stride of a 2-d or 3-d CUDA tensor whose rows are contiguous."""
+def _rows_of(t, name):
+    """Elements between the rows of a CUDA tensor whose rows (all dimensions but the first) are contiguous."""
     assert t.is_cuda and t.dim() >= 2, f"{name}: a CUDA tensor of rows"
+    if t.is_contiguous():
+        return t.numel() // max(t.shape[0], 1)
     inner = 1
     for d in range(t.dim() - 1, 0, -1):
         assert t.shape[d] == 1 or t.stride(d) == inner, f"{name}: rows must be contiguous"
         inner *= t.shape[d]
-    assert width is None or inner == width, f"{name}: rows of {width} elements expected"
     assert t.shape[0] <= 1 or t.stride(0) >= inner, f"{name}: rows overlap"
     return t.stride(0) if t.shape[0] > 1 else inner
 
 
 def _dtype_of(t, name):
     import torch
-    assert t.dtype in (torch.float32, torch.bfloat16), f"{name}: fp32 or bf16"
-    return F32 if t.dtype == torch.float32 else BF16
+    if t.dtype is torch.float32:
+        return F32
+    assert t.dtype is torch.bfloat16, f"{name}: fp32 or bf16"
+    return BF16
 
 
 def _vector(t, n, dtype, device, name):
-    assert t.device == device and t.dtype == dtype and t.numel() == n and t.is_contiguous(), f"{name}: {n} contiguous {dtype} on {device} expected"
+    assert t.get_device() == device.index and t.dtype is dtype and t.numel() == n and t.is_contiguous(), f"{name}: {n} contiguous {dtype} on {device} expected"
     return t.data_ptr()
 
 
@@ -513,7 +516,7 @@ def sample(logits, shaping, u, *, probs=None, tokens=None, stream=None):
     ld = _rows_of(logits, "logits")
     pl = 0
     if probs is not None:
-        assert probs.dtype == torch.float32 and tuple(probs.shape) == (rows, vocab) and probs.device == dev
+        assert probs.dtype is torch.float32 and probs.shape == (rows, vocab) and probs.device == dev
         pl = _rows_of(probs, "probs")
     with _on(dev, stream) as st:
         if tokens is None:
@@ -533,20 +536,21 @@ def accept(logits, row0, shaping, q, drafts, u, *, stream=None):
     rows, vocab = logits.shape
     dev = logits.device
     n_req = row0.numel() - 1
+    assert n_req >= 1, "row0: a request at least"
     ld = _rows_of(logits, "logits")
     ql, qp, dp = 0, None, None
     if rows > n_req:
-        assert q.dtype == torch.float32 and tuple(q.shape) == (rows - n_req, vocab) and q.device == dev
+        assert q.dtype is torch.float32 and q.shape == (rows - n_req, vocab) and q.device == dev
         ql, qp, dp = _rows_of(q, "q"), q.data_ptr(), _vector(drafts, rows - n_req, torch.int32, dev, "drafts")
     with _on(dev, stream) as st:
-        out = torch.empty((2, max(n_req, 0)), dtype=torch.int32, device=dev)
+        n_accepted, next_token = torch.empty(n_req, dtype=torch.int32, device=dev), torch.empty(n_req, dtype=torch.int32, device=dev)
         scratch = torch.empty(int(lib().pipesd_accept_scratch_bytes(rows)), dtype=torch.uint8, device=dev)
         rc = lib().pipesd_accept(logits.data_ptr(), _dtype_of(logits, "logits"), ld, n_req, rows, vocab, _vector(row0, n_req + 1, torch.int32, dev, "row0"),
                                  _vector(shaping, 4 * n_req, torch.int32, dev, "shaping"), qp, ql, dp, _vector(u, rows, torch.float32, dev, "u"),
-                                 out[0].data_ptr(), out[1].data_ptr(), scratch.data_ptr(), st)
+                                 n_accepted.data_ptr(), next_token.data_ptr(), scratch.data_ptr(), st)
     if rc != OK:
         raise PipesdError(rc, "pipesd_accept")
-    return out[0], out[1]
+    return n_accepted, next_token
 
 
 class Kv4Cache:
@@ -575,12 +579,15 @@ class Kv4Cache:
         assert pool.is_cuda and pool.dtype == torch.uint8 and pool.is_contiguous() and pool.numel() == size, f"pool: {size} contiguous bytes expected"
         self.pool, self.n_kv_heads, self.head_dim, self.page_size, self.n_pages = pool, n_kv_heads, head_dim, page_size, n_pages
         self._scratch_bytes = int(lib().pipesd_kv4_attend_scratch_bytes(ctypes.byref(cfg)))
+        self._cfgs = {}        # by the width of the page table
 
     def _where(self, rows, row0, base, table):
         import torch
         n_req, dev = base.numel(), self.pool.device
         assert table.dim() == 2 and table.shape[0] == n_req, "table: [n_req, max_pages]"
-        cfg = Kv4Cfg(self.n_kv_heads, self.head_dim, self.page_size, self.n_pages, table.shape[1], 0)
+        cfg = self._cfgs.get(table.shape[1])
+        if cfg is None:
+            cfg = self._cfgs[table.shape[1]] = Kv4Cfg(self.n_kv_heads, self.head_dim, self.page_size, self.n_pages, table.shape[1], 0)
         return cfg, (n_req, rows, _vector(row0, n_req + 1, torch.int32, dev, "row0"), _vector(base, n_req, torch.int32, dev, "base"),
                      _vector(table, table.numel(), torch.int32, dev, "table"))
 
@@ -588,7 +595,7 @@ class Kv4Cache:
         """Quantises the rows k, v [rows, KV heads, head_dim] (fp32 or bf16) into their positions."""
         dev = self.pool.device
         shape = (k.shape[0], self.n_kv_heads, self.head_dim)
-        assert tuple(k.shape) == shape == tuple(v.shape) and k.dtype == v.dtype and k.device == dev == v.device, f"k, v: two alike of {shape} on {dev}"
+        assert k.shape == shape == v.shape and k.dtype is v.dtype and k.get_device() == dev.index == v.get_device(), f"k, v: two alike of {shape} on {dev}"
         cfg, where = self._where(k.shape[0], row0, base, table)
         with _on(dev, stream) as st:
             rc = lib().pipesd_kv4_append(ctypes.byref(cfg), self.pool.data_ptr(), k.data_ptr(), v.data_ptr(), _dtype_of(k, "k"), _rows_of(k, "k"), _rows_of(v, "v"),
@@ -613,13 +620,14 @@ class Kv4Cache:
         scale: head_dim ** -0.5 unless given."""
         import torch
         dev = self.pool.device
-        assert q.dim() == 3 and q.shape[2] == self.head_dim and q.device == dev, f"q: [rows, query heads, {self.head_dim}] on {dev}"
+        assert q.dim() == 3 and q.shape[2] == self.head_dim and q.get_device() == dev.index, f"q: [rows, query heads, {self.head_dim}] on {dev}"
         cfg, where = self._where(q.shape[0], row0, base, table)
         with _on(dev, stream) as st:
             if out is None:
                 out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+            else:
+                assert out.shape == q.shape and out.dtype is q.dtype and out.get_device() == dev.index, "out: like q"
             scratch = torch.empty(self._scratch_bytes, dtype=torch.uint8, device=dev)
-            assert out.shape == q.shape and out.dtype == q.dtype and out.device == dev, "out: like q"
             rc = lib().pipesd_kv4_attend(ctypes.byref(cfg), self.pool.data_ptr(), q.data_ptr(), out.data_ptr(), _dtype_of(q, "q"), _rows_of(q, "q"), _rows_of(out, "out"),
                                          q.shape[1], self.head_dim ** -0.5 if scale is None else scale, *where, scratch.data_ptr(), st)
         if rc != OK:

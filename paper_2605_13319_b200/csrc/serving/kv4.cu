@@ -65,7 +65,7 @@ int32_t attend_run(Kv4AttendArgs& a, int nt, cudaStream_t st) {
     attend_fn<HD, T>(nt)<<<a.ctas, kAttendThreads, attend_smem<HD, T>(nt), st>>>(a);
     if (cudaGetLastError() != cudaSuccess) return PIPESD_E_CUDA;
     const long long jobs = (long long)a.w.rows * a.Hq;
-    if (launch_pdl(kv4_merge_kernel<HD, T>, dim3((unsigned)((jobs + 7) / 8)), dim3(256), 0, st, a) != cudaSuccess) return PIPESD_E_CUDA;
+    if (launch_pdl(kv4_merge_kernel<HD, T>, dim3((unsigned)jobs), dim3(32 * kMergeWarps), 0, st, a) != cudaSuccess) return PIPESD_E_CUDA;
     return launched();
 }
 
@@ -125,7 +125,7 @@ int32_t pipesd_kv4_attend(const pipesd_kv4_cfg* cfg, const void* pool, const voi
         return PIPESD_E_INVALID;
     const int64_t width = (int64_t)n_q_heads * cfg->head_dim;
     if (rows > 1 && (q_stride < width || out_stride < width)) return PIPESD_E_INVALID;
-    if ((int64_t)rows * n_q_heads > (1ll << 33)) return PIPESD_E_INVALID;
+    if ((int64_t)rows * n_q_heads > INT32_MAX) return PIPESD_E_INVALID;
     if (!device_ready()) return PIPESD_E_CUDA;
     Kv4AttendArgs a = {};
     a.w = where_of(cfg, n_req, rows, row0, base, table);
