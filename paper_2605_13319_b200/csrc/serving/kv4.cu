@@ -33,12 +33,12 @@ int32_t launched() { return cudaGetLastError() == cudaSuccess ? PIPESD_OK : PIPE
 using AttendFn = void (*)(Kv4AttendArgs);
 template <int HD, typename T>
 AttendFn attend_fn(int nt) {
-    return nt == 1 ? kv4_attend_kernel<HD, 1, T> : nt == 2 ? kv4_attend_kernel<HD, 2, T> : kv4_attend_kernel<HD, 4, T>;
+    return nt == 1 ? kv4_attend_kernel<HD, 1, T> : kv4_attend_kernel<HD, 2, T>;
 }
 template <int HD, typename T>
 size_t attend_smem(int nt) {
     constexpr bool s = sizeof(T) == 4;
-    return nt == 1 ? sizeof(AttendSmem<HD, 1, s>) : nt == 2 ? sizeof(AttendSmem<HD, 2, s>) : sizeof(AttendSmem<HD, 4, s>);
+    return nt == 1 ? sizeof(AttendSmem<HD, 1, s>) : sizeof(AttendSmem<HD, 2, s>);
 }
 
 // Shared-memory limits belong to a device: set once for each, with that device current.
@@ -47,7 +47,7 @@ std::mutex g_mu;
 bool g_ready[kDevices] = {false};
 template <int HD, typename T>
 bool attend_attrs() {
-    for (int nt : {1, 2, 4})
+    for (int nt : {1, 2})
         if (cudaFuncSetAttribute((const void*)attend_fn<HD, T>(nt), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)attend_smem<HD, T>(nt)) != cudaSuccess)
             return false;
     return true;
@@ -60,9 +60,14 @@ bool device_ready() {
     return g_ready[dev];
 }
 
+// Tiles of eight query rows that a CTA takes of a KV head's: two unless that pads the rows by a fifth and more.  us with one and two (8
+// requests of 2000 to 4000 positions, 32 heads of 128; bf16, fp32): 4 rows 45 58, 56 80; 9 rows 77 66, 99 87; 17 rows 110 115, 142 158; over 8 KV
+// heads: 36 rows 54 53, 68 70; 68 rows 87 80, 112 107.
+int attend_row_tiles(int64_t rows) { return (rows + 15) / 16 * 16 * 5 <= (rows + 7) / 8 * 8 * 6 ? 2 : 1; }
+
 template <int HD, typename T>
 int32_t attend_run(Kv4AttendArgs& a, int nt, cudaStream_t st) {
-    attend_fn<HD, T>(nt)<<<a.ctas, kAttendThreads, attend_smem<HD, T>(nt), st>>>(a);
+    attend_fn<HD, T>(nt)<<<a.ctas, 32 * attend_warps(nt), attend_smem<HD, T>(nt), st>>>(a);
     if (cudaGetLastError() != cudaSuccess) return PIPESD_E_CUDA;
     const long long jobs = (long long)a.w.rows * a.Hq;
     if (launch_pdl(kv4_merge_kernel<HD, T>, dim3((unsigned)jobs), dim3(32 * kMergeWarps), 0, st, a) != cudaSuccess) return PIPESD_E_CUDA;
@@ -114,7 +119,8 @@ int32_t pipesd_kv4_read(const pipesd_kv4_cfg* cfg, const void* pool, float* k, f
 
 uint64_t pipesd_kv4_attend_scratch_bytes(const pipesd_kv4_cfg* cfg) {
     if (!cfg_ok(cfg)) return 0;
-    return (uint64_t)2 * kAttendSms * 8 * kAttendMaxTiles * (cfg->head_dim + 2) * 4;
+    // two shares per CTA, each of 8 rows per tile
+    return (uint64_t)2 * kAttendSms * std::max(8 * attend_ctas_per_sm(1), 16 * attend_ctas_per_sm(2)) * (cfg->head_dim + 2) * 4;
 }
 
 int32_t pipesd_kv4_attend(const pipesd_kv4_cfg* cfg, const void* pool, const void* q, void* out, int32_t dtype, int64_t q_stride, int64_t out_stride,
@@ -137,10 +143,9 @@ int32_t pipesd_kv4_attend(const pipesd_kv4_cfg* cfg, const void* pool, const voi
     a.Hq = n_q_heads;
     a.scale = scale * 1.4426950408889634f;
     a.parts = static_cast<float*>(scratch);
-    const int per_head = (rows + n_req - 1) / n_req * (n_q_heads / cfg->n_kv_heads);      // query rows of a KV head, in the mean
-    const int nt = per_head <= 8 ? 1 : per_head <= 16 ? 2 : 4;
+    const int nt = attend_row_tiles((int64_t)(rows + n_req - 1) / n_req * (n_q_heads / cfg->n_kv_heads));      // by the mean
     a.rows_cap = 8 * nt;
-    a.ctas = kAttendSms * (nt == 1 ? 2 : 1);
+    a.ctas = kAttendSms * attend_ctas_per_sm(nt);
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (cfg->head_dim == 128) return dtype == PIPESD_F32 ? attend_run<128, float>(a, nt, st) : attend_run<128, uint16_t>(a, nt, st);
     return dtype == PIPESD_F32 ? attend_run<64, float>(a, nt, st) : attend_run<64, uint16_t>(a, nt, st);

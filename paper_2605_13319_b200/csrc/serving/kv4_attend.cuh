@@ -24,10 +24,12 @@
 
 namespace pipesd {
 
-constexpr int kAttendWarps = 8;
-constexpr int kAttendThreads = 32 * kAttendWarps;
-constexpr int kAttendMaxTiles = 4;                 // row tiles of a CTA
+// Row tiles of a CTA (NT), and what fits an SM: sixteen warps of 128 registers with one, twelve of 168 with two (which unpack a unit's codes
+// for twice the rows).  More, at one CTA of eight warps per SM, were slower at every number of rows.
+__host__ __device__ constexpr int attend_warps(int nt) { return nt == 1 ? 8 : 4; }
+__host__ __device__ constexpr int attend_ctas_per_sm(int nt) { return nt == 1 ? 2 : 3; }
 constexpr int kAttendSms = 148;
+constexpr int kAttendMinUnits = 8;                 // of a CTA
 constexpr float kAttendNone = -1e30f;              // reference of a row that has seen nothing
 constexpr float kAttendExcess = 4.f;               // log2 units by which a score may exceed its row's reference: P <= 16
 constexpr float kAttendScaleExcess = 64.f;         // factor by which a scale may exceed its warp's unit: P * s <= 2^10
@@ -78,15 +80,15 @@ __device__ __forceinline__ long long attend_total(const Kv4AttendArgs& a, int up
     }
     return all;
 }
-// Units of a CTA: an equal share, at least one per warp.
+// Units of a CTA: an equal share, at least kAttendMinUnits.
 __device__ __forceinline__ long long attend_share(long long all, int ctas) {
     const long long per = (all + ctas - 1) / ctas;
-    return per < kAttendWarps ? kAttendWarps : per;
+    return per < kAttendMinUnits ? kAttendMinUnits : per;
 }
 
 template <int HD, int NT, bool kSplit>
 struct AttendSmem {
-    static constexpr int kRows = 8 * NT, kGroups = HD / kKv4Group, kTerms = kSplit ? 2 : 1;
+    static constexpr int kRows = 8 * NT, kGroups = HD / kKv4Group, kTerms = kSplit ? 2 : 1, kAttendWarps = attend_warps(NT);
     uint2 q[HD / 16][NT][kTerms][32];              // B fragments
     uint2 qsum[NT][32];                            // sums of the groups' (scaled) entries as a B fragment, bf16: k = 4 term + group
     float qc[kRows];                               // what a row's scores are multiplied with
@@ -161,12 +163,13 @@ __device__ __forceinline__ void attend_out(uint16_t* p, float v) { *p = f32_to_b
 // Power of two (as its float) that a unit's scales and middles up to m are taken relative to.
 __device__ __forceinline__ float attend_unit_scale(float m) { return __uint_as_float(max(__float_as_uint(m) & 0x7f800000u, 27u << 23)); }
 
-// grid: a.ctas, block kAttendThreads, dynamic shared memory: one AttendSmem.
+// grid: a.ctas, block 32 attend_warps(NT), dynamic shared memory: one AttendSmem.
 template <int HD, int NT, typename T>
-__global__ void __launch_bounds__(kAttendThreads, NT == 1 ? 2 : 1) kv4_attend_kernel(const Kv4AttendArgs a) {
+__global__ void __launch_bounds__(32 * attend_warps(NT), attend_ctas_per_sm(NT)) kv4_attend_kernel(const Kv4AttendArgs a) {
     constexpr bool kSplit = sizeof(T) == 4;
     using SM = AttendSmem<HD, NT, kSplit>;
     constexpr int kGroups = SM::kGroups, kRows = SM::kRows, kTerms = SM::kTerms, kTiles = HD / 16;
+    constexpr int kAttendWarps = SM::kAttendWarps, kAttendThreads = 32 * kAttendWarps;
     extern __shared__ __align__(16) unsigned char smem_raw[];
     SM& sm = *reinterpret_cast<SM*>(smem_raw);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
