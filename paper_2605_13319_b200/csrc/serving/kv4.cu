@@ -143,7 +143,10 @@ int32_t pipesd_kv4_attend(const pipesd_kv4_cfg* cfg, const void* pool, const voi
     a.Hq = n_q_heads;
     a.scale = scale * 1.4426950408889634f;
     a.parts = static_cast<float*>(scratch);
-    const int nt = attend_row_tiles((int64_t)(rows + n_req - 1) / n_req * (n_q_heads / cfg->n_kv_heads));      // by the mean
+    // two tiles where the rows suit them and there is work for all CTAs: the page table bounds it (1 request, 2048 positions, 32 heads, 9 rows:
+    // 19 us with one, 23 with two)
+    const int64_t most = (int64_t)n_req * cfg->max_pages * (cfg->page_size / kKv4Unit) * cfg->n_kv_heads;
+    const int nt = most < 16384 ? 1 : attend_row_tiles((int64_t)(rows + n_req - 1) / n_req * (n_q_heads / cfg->n_kv_heads));      // rows in the mean
     a.rows_cap = 8 * nt;
     a.ctas = kAttendSms * attend_ctas_per_sm(nt);
     cudaStream_t st = (cudaStream_t)cuda_stream;

@@ -32,9 +32,12 @@ constexpr int kAttendSms = 148;
 constexpr int kAttendMinUnits = 8;                 // of a CTA
 constexpr float kAttendNone = -1e30f;              // reference of a row that has seen nothing
 constexpr float kAttendExcess = 4.f;               // log2 units by which a score may exceed its row's reference: P <= 16
-constexpr float kAttendScaleExcess = 64.f;         // factor by which a scale may exceed its warp's unit: P * s <= 2^10
+constexpr float kAttendScaleExcess = 64.f;         // factor by which a scale may exceed its warp's unit
+// fp16 has 40 binades for a number and its second term: P is taken times 2^6 (up to 2^10), scales times 1 / 4 (up to 2^5: their 8 bits are exact
+// down to 2^-16 of the first unit's; products up to 2^15), middles times 2^8 (up to 2^15).
+constexpr float kAttendUpP = 6.f, kAttendUpScale = 0.25f, kAttendUpMiddle = 256.f;
 constexpr int kAttendStages = 4;
-constexpr float kTwo9 = 512.f, kTwo24 = 16777216.f;
+constexpr float kTwo9 = 512.f, kTwoM24 = 5.9604644775390625e-8f;
 
 struct Kv4AttendArgs {
     Kv4Where w;
@@ -45,7 +48,7 @@ struct Kv4AttendArgs {
     int Hq;
     float scale;               // times log2(e)
     float* parts;              // [2 * CTAs][8 NT (HD + 2)]
-    int ctas, rows_cap;        // rows_cap = 8 NT
+    int ctas, rows_cap;        // rows_cap: query rows of a triple
 };
 
 // What a request adds to the flat sequence of units: units per triple and triples.
@@ -81,9 +84,44 @@ __device__ __forceinline__ long long attend_total(const Kv4AttendArgs& a, int up
     return all;
 }
 // Units of a CTA: an equal share, at least kAttendMinUnits.
-__device__ __forceinline__ long long attend_share(long long all, int ctas) {
-    const long long per = (all + ctas - 1) / ctas;
+__device__ __forceinline__ long long attend_share(const Kv4AttendArgs& a, long long all) {
+    const long long per = (all + a.ctas - 1) / a.ctas;
     return per < kAttendMinUnits ? kAttendMinUnits : per;
+}
+// This CTA's range [f, f_end) of the flat sequence, and where it begins: `off` units into request `req`.  False: it has none.  (Whole
+// warps; the sums over the first 32 requests are kept for the search.)
+__device__ __forceinline__ bool attend_begin(const Kv4AttendArgs& a, long long& f, long long& f_end, int& req, long long& off) {
+    const int lane = threadIdx.x & 31;
+    auto chunk = [&](int r0, long long& mine) {
+        int n, first, base, units, groups;
+        attend_load(a, r0 + lane, n, first, base, units, groups);
+        mine = (long long)units * groups * a.w.Hkv;
+        return warp_scan_i64(mine);
+    };
+    long long mine0;
+    const long long inc0 = chunk(0, mine0);
+    long long all = __shfl_sync(0xffffffffu, inc0, 31);
+    for (int r0 = 32; r0 < a.w.n_req; r0 += 32) {
+        long long mine;
+        all += __shfl_sync(0xffffffffu, chunk(r0, mine), 31);
+    }
+    const long long share = attend_share(a, all);
+    f = (long long)blockIdx.x * share;
+    f_end = f + share < all ? f + share : all;
+    if (f >= f_end) return false;
+    long long left = f;
+    for (int r0 = 0;; r0 += 32) {
+        long long mine = mine0, inc = inc0;
+        if (r0 > 0) inc = chunk(r0, mine);
+        const unsigned hit = __ballot_sync(0xffffffffu, left < inc);
+        if (hit) {
+            const int l = __ffs(hit) - 1;
+            req = r0 + l;
+            off = left - __shfl_sync(0xffffffffu, inc - mine, l);
+            return true;
+        }
+        left -= __shfl_sync(0xffffffffu, inc, 31);
+    }
 }
 
 template <int HD, int NT, bool kSplit>
@@ -119,6 +157,11 @@ __device__ __forceinline__ uint32_t attend_transpose(uint32_t v) {       // 8 x 
 __device__ __forceinline__ uint32_t attend_mul2(uint32_t a, uint32_t b) {
     uint32_t r;
     asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t attend_fma2(uint32_t a, uint32_t b, uint32_t c) {
+    uint32_t r;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(a), "r"(b), "r"(c));
     return r;
 }
 __device__ __forceinline__ uint32_t attend_pack(float x, float y) {      // fp16 pair, the first in the low half
@@ -160,6 +203,17 @@ __device__ __forceinline__ float attend_in(uint16_t v) { return bf16_bits_to_f32
 __device__ __forceinline__ void attend_out(float* p, float v) { *p = v; }
 __device__ __forceinline__ void attend_out(uint16_t* p, float v) { *p = f32_to_bf16_bits(v); }
 
+template <bool kBf16>
+__device__ __forceinline__ void attend_mma_first(float (&c)[4], const uint4& a, uint32_t b0, uint32_t b1) {      // D = A . B
+    if (kBf16)
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};\n"
+                     : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+                     : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1), "f"(0.f));
+    else
+        asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};\n"
+                     : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+                     : "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b0), "r"(b1), "f"(0.f));
+}
 // Power of two (as its float) that a unit's scales and middles up to m are taken relative to.
 __device__ __forceinline__ float attend_unit_scale(float m) { return __uint_as_float(max(__float_as_uint(m) & 0x7f800000u, 27u << 23)); }
 
@@ -182,31 +236,10 @@ __global__ void __launch_bounds__(32 * attend_warps(NT), attend_ctas_per_sm(NT))
     __syncwarp();
     uint32_t parity = 0, mapped = 0;               // of the ring's barriers; which of its units are there
     bool failed = false;
-    // ---- this CTA's range of the flat sequence, and where it begins
-    long long unused;
-    const long long all = attend_total(a, -1, unused), share = attend_share(all, a.ctas);
-    long long f = (long long)blockIdx.x * share;
-    const long long f_end = f + share < all ? f + share : all;
-    if (f >= f_end) return;
+    long long f, f_end, off;
+    int req;
+    if (!attend_begin(a, f, f_end, req, off)) return;
     const long long f_cta = f;
-    int req = 0;
-    long long off = 0;                             // of f inside its request
-    {
-        long long left = f;
-        for (int r0 = 0;; r0 += 32) {
-            int n, first, base, units, groups;
-            attend_load(a, r0 + lane, n, first, base, units, groups);
-            const long long mine = (long long)units * groups * a.w.Hkv, inc = warp_scan_i64(mine);
-            const unsigned hit = __ballot_sync(0xffffffffu, left < inc);
-            if (hit) {
-                const int l = __ffs(hit) - 1;
-                req = r0 + l;
-                off = left - __shfl_sync(0xffffffffu, inc - mine, l);
-                break;
-            }
-            left -= __shfl_sync(0xffffffffu, inc, 31);
-        }
-    }
     while (f < f_end) {
         int n, first, base, units, groups;
         attend_load(a, req, n, first, base, units, groups);
@@ -281,7 +314,7 @@ __global__ void __launch_bounds__(32 * attend_warps(NT), attend_ctas_per_sm(NT))
                 // k = 4 term + group sits in lane 4 (row % 8) + k % 8 / 2, register k / 8, half k % 2; groups that are none and the
                 // fourth term are 0
                 const int grp = lane / (32 / kGroups);
-                float rest = part;
+                float rest = part * kTwoM24;       // (as the products with codes * 2^-24 are)
 #pragma unroll
                 for (int term = 0; term < 4; ++term) {
                     const uint16_t h = term < 3 ? f32_to_bf16_bits(rest) : (uint16_t)0;
@@ -294,7 +327,7 @@ __global__ void __launch_bounds__(32 * attend_warps(NT), attend_ctas_per_sm(NT))
                 }
             }
             if (lane == 0) {
-                sm.qc[row] = ldexpf(a.scale, e - 15);
+                sm.qc[row] = ldexpf(a.scale, e - 15 + 24);
                 sm.horizon[row] = row < n_rows ? base + rho / G : -1;
             }
         }
@@ -308,14 +341,14 @@ __global__ void __launch_bounds__(32 * attend_warps(NT), attend_ctas_per_sm(NT))
                 for (int i = 0; i < 4; ++i) o[m][nt][i] = 0.f;
 #pragma unroll
             for (int i = 0; i < 4; ++i) zl[nt][i] = 0.f;
-            ref[nt][0] = ref[nt][1] = kAttendNone;
+            ref[nt][0] = ref[nt][1] = 0.f;
         }
 #pragma unroll 1
         for (int it = 0; it < n_it; ++it) {
             const int st = it % kAttendStages, u = u0 + warp + kAttendWarps * it;
             const unsigned char* up = sm.ring[warp][st];
             const bool there = mapped >> st & 1u;
-            if (!mbar_wait(smem_u32(&sm.bars[warp][st]), parity >> st & 1u)) failed = true;
+            failed = failed || !mbar_wait(smem_u32(&sm.bars[warp][st]), parity >> st & 1u);
             parity ^= 1u << st;
             if (!there) {
                 if (it + kAttendStages < n_it) request(it + kAttendStages);
@@ -350,7 +383,7 @@ __global__ void __launch_bounds__(32 * attend_warps(NT), attend_ctas_per_sm(NT))
                 vm[0] = fmaf(8.f, vs[0], bf16_lo(zw)); vm[1] = fmaf(8.f, vs[1], bf16_hi(zw));
             }
             const float vmax = fmaxf(fmaxf(fabsf(vs[0]), fabsf(vs[1])), fmaxf(fabsf(vm[0]), fabsf(vm[1])));
-            // ---- scores: [2 keys][2 rows] of each tile of 8 rows
+            // ---- scores relative to the rows' references: [2 keys][2 rows] of each tile of 8 rows
             uint4 zf;                              // zeros of both keys: groups 2 (t % 2), + 1
             {
                 const bool odd = kGroups == 4 && (t & 1);
@@ -363,16 +396,13 @@ __global__ void __launch_bounds__(32 * attend_warps(NT), attend_ctas_per_sm(NT))
             float s[NT][4];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                float zq[4] = {0.f, 0.f, 0.f, 0.f};
                 {
                     const uint2 b = sm.qsum[nt][lane];
-                    mma_bf16_16816(zq, zf, b.x, b.y);
+                    attend_mma_first<true>(s[nt], zf, b.x, b.y);
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[nt][i] = 0.f;
-#pragma unroll
                 for (int grp = 0; grp < kGroups; ++grp) {
-                    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+                    float acc[4];
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const uint32_t w0 = kw[0][grp] >> (8 * h), w1 = kw[1][grp] >> (8 * h);
@@ -380,7 +410,8 @@ __global__ void __launch_bounds__(32 * attend_warps(NT), attend_ctas_per_sm(NT))
 #pragma unroll
                         for (int term = 0; term < kTerms; ++term) {
                             const uint2 b = sm.q[2 * grp + h][nt][term][lane];
-                            attend_mma(acc, af, b.x, b.y);
+                            if (h + term == 0) attend_mma_first<false>(acc, af, b.x, b.y);
+                            else attend_mma(acc, af, b.x, b.y);
                         }
                     }
                     const float s0 = bf16_lo(ksz[0][grp]), s1 = bf16_lo(ksz[1][grp]);
@@ -389,7 +420,7 @@ __global__ void __launch_bounds__(32 * attend_warps(NT), attend_ctas_per_sm(NT))
                 }
                 const float2 qc = *reinterpret_cast<const float2*>(&sm.qc[nt * 8 + 2 * t]);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[nt][i] = fmaf(s[nt][i], kTwo24, zq[i]) * (i & 1 ? qc.y : qc.x);
+                for (int i = 0; i < 4; ++i) s[nt][i] = fmaf(s[nt][i], i & 1 ? qc.y : qc.x, -ref[nt][i & 1]);
                 if (edge) {
                     const int2 hz = *reinterpret_cast<const int2*>(&sm.horizon[nt * 8 + 2 * t]);
 #pragma unroll
@@ -402,10 +433,11 @@ __global__ void __launch_bounds__(32 * attend_warps(NT), attend_ctas_per_sm(NT))
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) over |= s[nt][i] > ref[nt][i & 1] + kAttendExcess;
+                for (int i = 0; i < 4; ++i) over |= s[nt][i] > kAttendExcess;
             if (__any_sync(0xffffffffu, over)) {
                 const float fit = attend_unit_scale(warp_max_f32(vmax));
                 const float to = fmaxf(fit, unit_scale), shrink = unit_scale / to;
+                const bool first_unit = unit_scale == 0.f;
                 unit_scale = to;
 #pragma unroll
                 for (int nt = 0; nt < NT; ++nt)
@@ -414,9 +446,12 @@ __global__ void __launch_bounds__(32 * attend_warps(NT), attend_ctas_per_sm(NT))
                         float m = fmaxf(s[nt][c], s[nt][2 + c]);
 #pragma unroll
                         for (int x = 4; x < 32; x <<= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, x));
-                        m = fmaxf(m, ref[nt][c]);
-                        const float factor = attend_exp2(ref[nt][c] - m);
-                        ref[nt][c] = m;
+                        // how far the reference moves: up, or (of the first unit) to the unit's maximum
+                        m = first_unit && m > -INFINITY ? m : fmaxf(m, 0.f);
+                        const float factor = first_unit ? 1.f : attend_exp2(-m);
+                        ref[nt][c] += m;
+                        s[nt][c] -= m;
+                        s[nt][2 + c] -= m;
                         zl[nt][c] *= g == 4 ? factor : factor * shrink;      // (row 4: the denominators; rows from 8 on are not used)
 #pragma unroll
                         for (int i = 0; i < 2; ++i)
@@ -428,9 +463,10 @@ __global__ void __launch_bounds__(32 * attend_warps(NT), attend_ctas_per_sm(NT))
             uint32_t s16, m16, m16_lo = 0u, s16w[kGroups][2];
             {
                 const float inv = __uint_as_float((254u << 23) - __float_as_uint(unit_scale));       // 1 / unit_scale
-                s16 = attend_pack(vs[0] * inv, vs[1] * inv);                                          // (8 bits: exact)
-                if (kSplit) attend_split(vm[0] * inv, vm[1] * inv, m16, m16_lo);
-                else m16 = attend_pack(vm[0] * inv, vm[1] * inv);
+                const float inv_s = inv * kAttendUpScale, inv_m = inv * kAttendUpMiddle;
+                s16 = attend_pack(vs[0] * inv_s, vs[1] * inv_s);                                      // (8 bits: exact)
+                if (kSplit) attend_split(vm[0] * inv_m, vm[1] * inv_m, m16, m16_lo);
+                else m16 = attend_pack(vm[0] * inv_m, vm[1] * inv_m);
             }
 #pragma unroll
             for (int grp = 0; grp < kGroups; ++grp)
@@ -442,7 +478,7 @@ __global__ void __launch_bounds__(32 * attend_warps(NT), attend_ctas_per_sm(NT))
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) p[nt][i] = attend_exp2(s[nt][i] - ref[nt][i & 1]);
+                for (int i = 0; i < 4; ++i) p[nt][i] = attend_exp2(s[nt][i] + kAttendUpP);
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const uint32_t hi = attend_pack(p[nt][2 * i], p[nt][2 * i + 1]);
@@ -484,10 +520,12 @@ __global__ void __launch_bounds__(32 * attend_warps(NT), attend_ctas_per_sm(NT))
                 for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        if (kSplit) {              // (hi + lo) * s in fp32, split again
-                            const float x = (f16_lo(ph[nt][i]) + f16_lo(pl[nt][i])) * f16_lo(s16w[grp][i]);
-                            const float y = (f16_hi(ph[nt][i]) + f16_hi(pl[nt][i])) * f16_hi(s16w[grp][i]);
-                            attend_split(x, y, b[nt][0][i], b[nt][kTerms - 1][i]);
+                        if (kSplit) {              // (hi + lo) * s: what the product rounds off goes to the second term
+                            uint32_t hi, lo;
+                            hi = attend_mul2(ph[nt][i], s16w[grp][i]);
+                            lo = attend_fma2(ph[nt][i], s16w[grp][i], hi ^ 0x80008000u);
+                            b[nt][0][i] = hi;
+                            b[nt][kTerms - 1][i] = attend_fma2(pl[nt][i], s16w[grp][i], lo);
                         } else {
                             b[nt][0][i] = attend_mul2(ph[nt][i], s16w[grp][i]);
                         }
@@ -512,8 +550,11 @@ __global__ void __launch_bounds__(32 * attend_warps(NT), attend_ctas_per_sm(NT))
         // ---- the warps' shares: outputs with the middles' part, references, denominators
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt) {
-            if (g == 0) *reinterpret_cast<float2*>(&sm.ref[warp][nt * 8 + 2 * t]) = make_float2(ref[nt][0], ref[nt][1]);
-            if (g == 4) *reinterpret_cast<float2*>(&sm.sum[warp][nt * 8 + 2 * t]) = make_float2(zl[nt][0], zl[nt][1]);
+            if (g == 4) {
+                *reinterpret_cast<float2*>(&sm.ref[warp][nt * 8 + 2 * t]) =
+                    make_float2(zl[nt][0] == 0.f ? kAttendNone : ref[nt][0], zl[nt][1] == 0.f ? kAttendNone : ref[nt][1]);
+                *reinterpret_cast<float2*>(&sm.sum[warp][nt * 8 + 2 * t]) = make_float2(zl[nt][0], zl[nt][1]);
+            }
 #pragma unroll
             for (int grp = 0; grp < kGroups; ++grp) {
                 const float z[2] = {__shfl_sync(0xffffffffu, zl[nt][0], grp * 4 + t), __shfl_sync(0xffffffffu, zl[nt][1], grp * 4 + t)};
@@ -522,7 +563,7 @@ __global__ void __launch_bounds__(32 * attend_warps(NT), attend_ctas_per_sm(NT))
 #pragma unroll
                     for (int i = 0; i < 4; ++i)
                         sm.o[warp][nt * 8 + 2 * t + (i & 1)][(2 * grp + h) * 16 + g + 8 * (i >> 1)] =
-                            fmaf(o[2 * grp + h][nt][i], kTwo9, z[i & 1]) * unit_scale;
+                            fmaf(o[2 * grp + h][nt][i], kTwo9 * kAttendUpMiddle / kAttendUpScale, z[i & 1]) * (unit_scale / kAttendUpMiddle);
             }
         }
         __syncthreads();
@@ -577,7 +618,7 @@ __global__ void __launch_bounds__(32 * kMergeWarps) kv4_merge_kernel(const Kv4At
     int n, first, base, units, groups;
     attend_load(a, req < 0 ? a.w.n_req : req, n, first, base, units, groups);
     long long before;
-    const long long all = attend_total(a, req, before), share = attend_share(all, a.ctas);
+    const long long all = attend_total(a, req, before), share = attend_share(a, all);
     // Launched with programmatic serialisation: behind this the shares are complete.  Every thread waits, those without work too: a grid that
     // ended without could let its successor begin before its predecessor has ended.
     pdl_wait();
