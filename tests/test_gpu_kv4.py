@@ -377,3 +377,46 @@ def test_serving_round_together():
         assert (n.item(), token.item()) == want[:2] or want[2] < 1e-9
         length += 1 + n.item()
         pending = token.clone()
+
+
+def test_rows_of_no_request():
+    """Rows behind the last request's: attention leaves them, reads give 0, appends drop them."""
+    import torch
+    rng = np.random.default_rng(4)
+    c = Case(rng, [3, 2], [20, 0], 2, 128)
+    c.fill(rng)                                                              # (positions 0..19 of request 0 are part of its cache)
+    k, v = (_rows(rng, 8, 2, 128, torch.float32) for _ in range(2))
+    c.cache.append(k, v, *c.where)
+    c.write_ref(k.double().cpu().numpy(), v.double().cpu().numpy())
+    assert np.array_equal(c.pool.cpu().numpy(), c.ref.pool)
+    got = c.cache.read(8, *c.where)
+    assert all((x[5:] == 0).all() and (x[3:5] != 0).any() for x in got)
+    for dtype in (torch.bfloat16, torch.float32):
+        q = _rows(rng, 8, 4, 128, dtype)
+        out = torch.full_like(q, 9.0)
+        c.cache.attend(q, *c.where, out=out)
+        assert (out[5:] == 9.0).all() and torch.isfinite(out).all() and (out[:5] != 9.0).any()
+
+
+def test_exact_ties_of_codes():
+    """bf16 rows put quotients exactly on borders every few hundred values: to even, as in exact arithmetic."""
+    import torch
+    from paper_2605_13319_b200 import binding
+    n = 4096
+    g = torch.Generator("cuda").manual_seed(0)
+    where = (torch.tensor([0, n], dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda"),
+             torch.arange(n // 16, dtype=torch.int32, device="cuda")[None])
+    for dtype in (torch.bfloat16, torch.float32):
+        ties = 0
+        for std, off in ((1.0, 0.0), (0.01, 3.0), (100.0, 1.0), (1e-20, 0.0)):
+            k = (torch.randn((n, 2, 128), generator=g, device="cuda") * std + off).to(dtype)
+            cache = binding.Kv4Cache(2, 128, n_pages=n // 16)
+            cache.append(k, k, *where)
+            x = k.double().unflatten(-1, (-1, 32))
+            z = x.amin(-1, keepdim=True).bfloat16().double()
+            s = ((x.amax(-1, keepdim=True) - z) / 15).bfloat16().double()
+            q = (x - z) / torch.where(s > 0, s, 1.0)
+            ties += int(((q - q.floor()) == 0.5).sum())
+            want = (torch.round(q).clamp(0, 15) * (s > 0) * s + z).flatten(-2).float()
+            assert all(torch.equal(y, want) for y in cache.read(n, *where))
+        assert ties > 100 or dtype == torch.float32

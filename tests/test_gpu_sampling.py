@@ -292,3 +292,55 @@ def test_draft_and_accept_leave_the_target_distribution():
     assert (share[P == 0] == 0).all()
     assert (np.abs(share - P) <= 5 * np.sqrt(P * (1 - P) / n) + 1e-12).all()      # five standard deviations of a frequency
     assert 0 < acc.float().mean().item() < 1
+
+
+def test_accept_in_a_graph_and_on_other_streams():
+    import torch
+    from paper_2605_13319_b200 import binding
+    rng = np.random.default_rng(12)
+    ks, V = [4, 0, 7], 8000
+    logits, q, drafts, u = (_cuda(a) for a in _rounds(rng, ks, V, 0.7))
+    row0 = _cuda(np.concatenate([[0], np.cumsum(np.array(ks) + 1)]).astype(np.int32))
+    shaping = binding.shaping(3, temperature=[1.0, 0.8, 0.0], top_k=[0, 50, 0], top_p=[0.9, 1.0, 1.0])
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        captured = binding.accept(logits, row0, shaping, q, drafts, u)
+    for _ in range(3):
+        u.copy_(torch.rand(u.shape, device="cuda"))
+        graph.replay()
+        want = binding.accept(logits, row0, shaping, q, drafts, u)
+        torch.cuda.synchronize()
+        got = [binding.accept(logits, row0, shaping, q, drafts, u, stream=s) for s in [torch.cuda.Stream() for _ in range(3)]]
+        torch.cuda.synchronize()
+        for a in [captured] + got:
+            assert torch.equal(a[0], want[0]) and torch.equal(a[1], want[1])
+
+
+@pytest.mark.parametrize("vocab", [40000, 128256])
+def test_sample_windows_that_overflow_their_lists(vocab):
+    """More ids than a list holds near a cut: dense flat tails (a third pass), thousands of equal logits at the cut (digit by digit)
+    and a maximum far above the row's first ids (bins anew)."""
+    import torch
+    from paper_2605_13319_b200 import binding
+    g = torch.Generator("cuda").manual_seed(vocab)
+    rows = []
+    for std in (0.05, 0.3):
+        rows.append(torch.randn(vocab, generator=g, device="cuda") * std)
+    rows.append(torch.randint(0, 3, (vocab,), generator=g, device="cuda").float())
+    x = torch.randn(vocab, generator=g, device="cuda")
+    x[-1] = 200.0
+    rows.append(x)
+    x = torch.randn(vocab, generator=g, device="cuda") * 2 - 500.0
+    x[:4000] = -900.0
+    rows.append(x)
+    logits = torch.stack(rows)
+    n = len(rows)
+    rng = np.random.default_rng(7)
+    for t, k, p, m in ((1.0, 0, 0.9, 0.0), (1.0, 0, 0.31, 0.0), (1.3, 5000, 1.0, 0.0), (0.9, 30000, 0.95, 0.0), (1.0, 1100, 0.5, 0.2), (60.0, 0, 0.999, 0.0), (0.02, 0, 0.99, 0.0)):
+        u = (rng.integers(0, 1 << 24, n) * 2.0 ** -24).astype(np.float32)
+        s = [np.full(n, v, d) for v, d in ((t, np.float32), (k, np.int32), (p, np.float32), (m, np.float32))]
+        probs = torch.empty_like(logits)
+        for dtype in (torch.float32, torch.bfloat16):
+            y = logits.to(dtype)
+            tokens = binding.sample(y, binding.shaping(n, temperature=t, top_k=k, top_p=p, min_p=m), _cuda(u), probs=probs)
+            _check(y.float().cpu().numpy(), s, u, tokens.cpu().numpy(), probs.cpu().numpy())
