@@ -13,7 +13,8 @@
 // its rounding as well.  fp16 keeps 11 bits of P and of P * s; the scales and middles are taken relative to a power of two that
 // fits the warp's first unit, and rescaled (like a row's exponentials, which are relative to a score of that unit) when one
 // exceeds it by 2^6 (2^4).
-// fp32 queries and outputs (kSplit): Q, P, P * s and the middles as two fp16 terms each, 22 bits of mantissa.
+// fp32 queries and outputs (kSplit): Q, P, P * s and the middles as two fp16 terms each, 22 bits of mantissa; a unit's products go to the
+// running sums by ordinary additions, which round to nearest (the tensor pipe truncates where it adds: error 2.1e-6 over long caches).
 // Work: the units of all (request, KV head, row group) triples in a row, cut into equal ranges, one per CTA; the warps of a CTA take
 // its units in turn.  A triple that one CTA has whole is finished there; of others each CTA leaves (O, reference, denominator),
 // which kv4_merge_kernel adds up in CTA order.  No atomics, no state between calls.
@@ -403,16 +404,17 @@ __global__ void __launch_bounds__(32 * attend_warps(NT), attend_ctas_per_sm(NT))
 #pragma unroll
                 for (int grp = 0; grp < kGroups; ++grp) {
                     float acc[4];
+                    uint4 af[2];
 #pragma unroll
                     for (int h = 0; h < 2; ++h) {
                         const uint32_t w0 = kw[0][grp] >> (8 * h), w1 = kw[1][grp] >> (8 * h);
-                        const uint4 af = make_uint4(w0 & 0x000f000fu, w1 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x00f000f0u);
+                        af[h] = make_uint4(w0 & 0x000f000fu, w1 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x00f000f0u);
+                    }
 #pragma unroll
-                        for (int term = 0; term < kTerms; ++term) {
-                            const uint2 b = sm.q[2 * grp + h][nt][term][lane];
-                            if (h + term == 0) attend_mma_first<false>(acc, af, b.x, b.y);
-                            else attend_mma(acc, af, b.x, b.y);
-                        }
+                    for (int i = 0; i < 2 * kTerms; ++i) {     // the small terms first: the sum is truncated at every step
+                        const uint2 b = sm.q[2 * grp + i % 2][nt][kTerms - 1 - i / 2][lane];
+                        if (i == 0) attend_mma_first<false>(acc, af[0], b.x, b.y);
+                        else attend_mma(acc, af[i % 2], b.x, b.y);
                     }
                     const float s0 = bf16_lo(ksz[0][grp]), s1 = bf16_lo(ksz[1][grp]);
                     s[nt][0] = fmaf(s0, acc[0], s[nt][0]); s[nt][1] = fmaf(s0, acc[1], s[nt][1]);
@@ -502,10 +504,15 @@ __global__ void __launch_bounds__(32 * attend_warps(NT), attend_ctas_per_sm(NT))
             }
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                attend_mma(zl[nt], az, ph[nt][0], ph[nt][1]);
                 if (kSplit) {
-                    attend_mma(zl[nt], az, pl[nt][0], pl[nt][1]);
-                    attend_mma(zl[nt], azl, ph[nt][0], ph[nt][1]);
+                    float x[4];
+                    attend_mma_first<false>(x, az, pl[nt][0], pl[nt][1]);
+                    attend_mma(x, azl, ph[nt][0], ph[nt][1]);
+                    attend_mma(x, az, ph[nt][0], ph[nt][1]);
+                    zl[nt][0] += x[0];
+                    zl[nt][1] += x[1];
+                } else {
+                    attend_mma(zl[nt], az, ph[nt][0], ph[nt][1]);
                 }
             }
             uint32_t vw[kTiles];                   // a word per tile
@@ -536,9 +543,17 @@ __global__ void __launch_bounds__(32 * attend_warps(NT), attend_ctas_per_sm(NT))
                     const uint4 af = make_uint4(attend_centre<false>(w0 & 0x000f000fu), attend_centre<true>(w0 & 0x00f000f0u),
                                                 attend_centre<false>(w1 & 0x000f000fu), attend_centre<true>(w1 & 0x00f000f0u));
 #pragma unroll
-                    for (int nt = 0; nt < NT; ++nt)
+                    for (int nt = 0; nt < NT; ++nt) {
+                        if (kSplit) {
+                            float x[4];
+                            attend_mma_first<false>(x, af, b[nt][kTerms - 1][0], b[nt][kTerms - 1][1]);
+                            attend_mma(x, af, b[nt][0][0], b[nt][0][1]);
 #pragma unroll
-                        for (int term = 0; term < kTerms; ++term) attend_mma(o[2 * grp + h][nt], af, b[nt][term][0], b[nt][term][1]);
+                            for (int i = 0; i < 4; ++i) o[2 * grp + h][nt][i] += x[i];
+                        } else {
+                            attend_mma(o[2 * grp + h][nt], af, b[nt][0][0], b[nt][0][1]);
+                        }
+                    }
                 }
             }
         }
