@@ -193,59 +193,66 @@ template <typename T, int VEC, typename F>
 __device__ __forceinline__ void shape_walk(const T* row, int j0, int j1, F&& f) {
     shape_groups<T, VEC>(row, j0, j1, [&](const auto& l, int first) {
         constexpr int kN = sizeof(l) / 4;
+        const int lane = threadIdx.x & 31;
+        if (first - lane * (VEC == 1 ? 1 : VEC) + 32 * kN <= j1) {           // the whole warp's group is inside
 #pragma unroll
-        for (int e = 0; e < kN; ++e) {
-            const int id = first + e * group_apart<VEC>();
-            if (id < j1) f(l[e], id);
+            for (int e = 0; e < kN; ++e) f(l[e], first + e * group_apart<VEC>());
+        } else {
+#pragma unroll
+            for (int e = 0; e < kN; ++e) {
+                const int id = first + e * group_apart<VEC>();
+                if (id < j1) f(l[e], id);
+            }
         }
     });
 }
 
-// Masses of the ids that r keeps: f(mass, logit, id), 0 for the others.  All of a group's exponentials side by side, without a branch
-// between them (one by one they cost six times as much: each is a chain of fifteen dependent fp64 operations); groups of which the warp
-// keeps nothing are skipped.
-template <typename T, int VEC, typename F>
+// Whether r keeps an id; kTies: of the ids with just the cut's logit some may be cut (else cut_id is behind all ids).
+template <bool kTies>
+__device__ __forceinline__ bool shape_kept(float l, int id, const RowShape& r) { return kTies ? shape_keeps(l, id, r) : l >= r.cut; }
+
+// Masses of the ids that r keeps, as shape_mass_bits: f(bits, kept, logit, id); what is not kept is weighed as the maximum.  All of a
+// group's exponentials side by side, without a branch between them (one by one they are chains of fifteen dependent fp64 operations);
+// groups of which the warp keeps nothing are skipped.
+template <bool kTies, typename T, int VEC, typename F>
 __device__ __forceinline__ void shape_masses(const T* row, int j0, int j1, const RowShape& r, F&& f) {
+    const float m = (float)r.m;
     shape_groups<T, VEC>(row, j0, j1, [&](const auto& l, int first) {
         constexpr int kN = sizeof(l) / 4;
         bool keep[kN], any = false;
 #pragma unroll
         for (int e = 0; e < kN; ++e) {
-            keep[e] = shape_keeps(l[e], first + e * group_apart<VEC>(), r);
+            keep[e] = shape_kept<kTies>(l[e], first + e * group_apart<VEC>(), r);
             any |= keep[e];
         }
         if (!__any_sync(0xffffffffu, any)) return;
         unsigned long long w[kN];
 #pragma unroll
-        for (int e = 0; e < kN; ++e) w[e] = shape_mass(shape_exponent(keep[e] ? l[e] : r.cut, r));
+        for (int e = 0; e < kN; ++e) w[e] = shape_mass_bits(shape_exponent(keep[e] ? l[e] : m, r));
 #pragma unroll
-        for (int e = 0; e < kN; ++e) f(keep[e] ? w[e] : 0ull, l[e], first + e * group_apart<VEC>());
+        for (int e = 0; e < kN; ++e) f(w[e], keep[e], l[e], first + e * group_apart<VEC>());
     });
 }
-
-// This lane's sum of them.  What is not kept is weighed as the maximum, and its 2^45 taken away again.
-template <typename T, int VEC>
-__device__ __forceinline__ unsigned long long shape_mass_sum(const T* row, int j0, int j1, const RowShape& r) {
-    unsigned long long sum = 0;
+// A sum of them: the 128s, and the 2^45 of the others, are taken away in the end.
+struct MassSum {
+    unsigned long long bits = 0;
     unsigned n = 0, others = 0;
-    const float m = (float)r.m;
-    shape_groups<T, VEC>(row, j0, j1, [&](const auto& l, int first) {
-        constexpr int kN = sizeof(l) / 4;
-        float x[kN];
-        unsigned cut = 0;
-#pragma unroll
-        for (int e = 0; e < kN; ++e) {
-            const bool keep = shape_keeps(l[e], first + e * group_apart<VEC>(), r);
-            x[e] = keep ? l[e] : m;
-            cut += !keep;
-        }
-        if (!__any_sync(0xffffffffu, cut < kN)) return;
-        n += kN;
-        others += cut;
-#pragma unroll
-        for (int e = 0; e < kN; ++e) sum += shape_mass_bits(shape_exponent(x[e], r));
+    __device__ __forceinline__ unsigned long long total() const { return bits - n * kMassBase - ((unsigned long long)others << 45); }
+};
+// This lane's sum.
+template <bool kTies, typename T, int VEC>
+__device__ __forceinline__ unsigned long long shape_mass_sum_of(const T* row, int j0, int j1, const RowShape& r) {
+    MassSum sum;
+    shape_masses<kTies, T, VEC>(row, j0, j1, r, [&](unsigned long long w, bool keep, float, int) {
+        sum.bits += w;
+        ++sum.n;
+        sum.others += !keep;
     });
-    return sum - n * kMassBase - ((unsigned long long)others << 45);
+    return sum.total();
+}
+template <typename T, int VEC>
+__device__ __forceinline__ unsigned long long shape_mass_sum(const T* row, int j0, int j1, const RowShape& r, int V) {
+    return r.cut_id < V ? shape_mass_sum_of<true, T, VEC>(row, j0, j1, r) : shape_mass_sum_of<false, T, VEC>(row, j0, j1, r);
 }
 
 // Sum (kMax: maximum) over the CTA; every thread gets it.  `part` is not used again before the next barrier but one.
@@ -344,17 +351,20 @@ struct ShapeBins {
     __device__ __forceinline__ float at(float l) const { return __fmul_rn(__fsub_rn(from, l), inv); }
     __device__ __forceinline__ float clamped(float l) const { return fminf(fmaxf(at(l), 0.f), (float)(kShapeBins - 1)); }
 };
+// (The place's whole part by an addition that rounds towards zero, the weight's whole steps by one that rounds to nearest: the converters
+// take a quarter of the rate.)
 template <bool kMass>
 __device__ __forceinline__ void shape_count(const ShapeBins& bins, float l, uint32_t* coarse) {
-    const float x = bins.clamped(l);
-    const int b = (int)x;
+    const float big = 8388608.f, x = bins.clamped(l), b = __fadd_rz(x, big);
     uint32_t add = 1;
-    if (kMass) {                                   // exp(-d) to the second order, |d| <= 1 / 128
-        const float d = (x - (float)b - 0.5f) * (1.f / kShapeWidth);
-        add = (uint32_t)(fmaf(fmaf(0.5f, d, -1.f), d, 1.f) * 8192.f + 0.5f);
+    if (kMass) {                                   // exp(-d) to the second order, d = (f - 1/2) / 64, |d| <= 1 / 128, in steps of 2^-13
+        constexpr float d0 = 0.5f / kShapeWidth;
+        const float f = x - (b - big);
+        add = __float_as_uint(fmaf(f, fmaf(f, 4096.f / (kShapeWidth * kShapeWidth), -(8192.f + 8192.f * d0) / kShapeWidth), big + 8192.f * (1.f + d0 + 0.5f * d0 * d0))) - 0x4b000000u;
     }
-    atomicAdd(coarse + b, add);
+    atomicAdd(coarse + (__float_as_uint(b) - 0x4b000000u), add);
 }
+
 // Behind the pass and a barrier of the CTA: its bins' sums by segment, so that a cluster exchanges 64 numbers and then the bins of
 // one segment (all bins of all CTAs read by all of them take 20 us in a cluster of eight).  Masses are relative to a weight of 1 at the
 // first bin's upper end.
@@ -497,7 +507,7 @@ __device__ unsigned long long shape_top_k(const T* row, int j0, int j1, const Ro
 // Top-p, 0 < p < 1, among the ids that r keeps, behind the first pass and a barrier of the cluster: the bound.  *parts: sm.part holds
 // the kept masses of this CTA's warps (whose ids are `per` each).  sm.n_own = 0 at the start.
 template <int C, typename T, int VEC>
-__device__ unsigned long long shape_top_p(const T* row, int j0, int j1, const RowShape& r, const ShapeBins& bins, float share, ShapeSmem& sm, int per, bool* parts) {
+__device__ unsigned long long shape_top_p(const T* row, int j0, int j1, const RowShape& r, const ShapeBins& bins, float share, ShapeSmem& sm, int V, int per, bool* parts) {
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const double p = (double)share;
     *parts = false;
@@ -555,16 +565,23 @@ __device__ unsigned long long shape_top_p(const T* row, int j0, int j1, const Ro
     const float from = lo == 0 ? -INFINITY : (float)lo, to = hi == kShapeBins - 1 ? INFINITY : (float)(hi + 1);
     const float steps = (float)kShapeFine / (float)(hi + 1 - lo);
     auto fine_of = [&](float x) { return (int)fminf(fmaxf(__fmul_rn(__fsub_rn(x, (float)lo), steps), 0.f), (float)(kShapeFine - 1)); };
-    unsigned long long m_above = 0, m_all = 0;
-    shape_masses<T, VEC>(row, j0, j1, r, [&](unsigned long long w, float l, int id) {
+    MassSum s_all, s_above;
+    auto weigh = [&](unsigned long long w, bool keep, float l, int id) {
         const float x = bins.at(l);
-        m_all += w;
-        if (x < from) m_above += w;
-        else if (x < to && w) {
-            atomicAdd(sm.fine + fine_of(x), w);
+        s_all.bits += w;
+        ++s_all.n;
+        s_all.others += !keep;
+        if (x < from) {                            // (kept, or it would not be above a kept one)
+            s_above.bits += w;
+            ++s_above.n;
+        } else if (x < to && keep && w > kMassBase) {
+            atomicAdd(sm.fine + fine_of(x), w - kMassBase);
             shape_keep_key(sm, l, id);
         }
-    });
+    };
+    if (r.cut_id < V) shape_masses<true, T, VEC>(row, j0, j1, r, weigh);
+    else shape_masses<false, T, VEC>(row, j0, j1, r, weigh);
+    unsigned long long m_all = s_all.total(), m_above = s_above.total();
     m_all = warp_sum_u64(m_all);
     m_above = warp_sum_u64(m_above);
     if (lane == 0) { sm.part[warp] = m_all; sm.part2[warp] = m_above; }
@@ -761,16 +778,21 @@ __device__ void shape_row(const T* row, int V, const Shaping s, float u, int32_t
     }
     // ---- first pass: the first of the order (a NaN or +inf anywhere shows as the largest key there is), and the bins
     float best = -INFINITY;
-    int best_id = V;
+    int best_id = 0;                               // (only looked for where it is the row's token)
     bool bad = false;
-    auto look = [&](float l, int id) {
+    auto look = [&](float l) {
         bad |= !(l < INFINITY);
-        if (l > best) { best = l; best_id = id; }
+        best = fmaxf(best, l);
     };
-    if (cut_k) shape_walk<T, VEC>(row, j0, j1, [&](float l, int id) { look(l, id); shape_count<false>(bins, l, sm.coarse); });
-    else if (cut_p) shape_walk<T, VEC>(row, j0, j1, [&](float l, int id) { look(l, id); shape_count<true>(bins, l, sm.coarse); });
-    else shape_walk<T, VEC>(row, j0, j1, look);
-    unsigned long long top = cta_reduce_u64<true>(bad ? ~0ull : best_id < V ? order_key(best, best_id) : 0ull, sm.part);
+    if (cut_k) shape_walk<T, VEC>(row, j0, j1, [&](float l, int) { look(l); shape_count<false>(bins, l, sm.coarse); });
+    else if (cut_p) shape_walk<T, VEC>(row, j0, j1, [&](float l, int) { look(l); shape_count<true>(bins, l, sm.coarse); });
+    else if (s.t > 0.f) shape_walk<T, VEC>(row, j0, j1, [&](float l, int) { look(l); });
+    else
+        shape_walk<T, VEC>(row, j0, j1, [&](float l, int id) {
+            bad |= !(l < INFINITY);
+            if (l > best) { best = l; best_id = id; }
+        });
+    unsigned long long top = cta_reduce_u64<true>(bad ? ~0ull : best > -INFINITY ? order_key(best, best_id) : 0ull, sm.part);
     if (cut_k) shape_segments<false>(sm);
     else if (cut_p) shape_segments<true>(sm);
     if (tid == 0) sm.cta[0] = top;
@@ -843,7 +865,7 @@ __device__ void shape_row(const T* row, int V, const Shaping s, float u, int32_t
                             shape_coarse<true, T, VEC>(row, j0, j1, bins, r, sm);
                             shape_sync<C>();
                         }
-                        b = shape_top_p<C, T, VEC>(row, j0, j1, r, bins, s.p, sm, per, &parts);
+                        b = shape_top_p<C, T, VEC>(row, j0, j1, r, bins, s.p, sm, V, per, &parts);
                     }
                     r.cut = key_logit(b);          // (among what was kept: never lower)
                     r.cut_id = (int)~(uint32_t)b;
@@ -857,7 +879,7 @@ __device__ void shape_row(const T* row, int V, const Shaping s, float u, int32_t
         // ---- mass of what is kept: this warp's, the CTA's, the row's
         unsigned long long mass = 0;
         if (!parts) {
-            mass = warp_sum_u64(shape_mass_sum<T, VEC>(row, j0, j1, r));
+            mass = warp_sum_u64(shape_mass_sum<T, VEC>(row, j0, j1, r, V));
             __syncthreads();
             if (lane == 0) sm.part[warp] = mass;
         }
@@ -891,7 +913,7 @@ __device__ void shape_row(const T* row, int V, const Shaping s, float u, int32_t
                 int o0 = min(V, (rank * kShapeWarps + w) * per), o1 = min(V, o0 + per);
                 const int sub = ((o1 - o0 + kShapeWarps - 1) / kShapeWarps + 31) / 32 * 32;
                 const int s0 = min(o1, o0 + warp * sub), s1 = min(o1, s0 + sub);
-                const unsigned long long some = warp_sum_u64(shape_mass_sum<T, 1>(row, s0, s1, r));
+                const unsigned long long some = warp_sum_u64(shape_mass_sum<T, 1>(row, s0, s1, r, V));
                 if (lane == 0) sm.part2[warp] = some;
                 __syncthreads();
                 owner(sm.part2, w);
