@@ -999,8 +999,9 @@ __device__ void shape_row(const T* row, int V, const Shaping s, float u, int32_t
 struct ShapeArgs {
     const void* logits;
     long long stride;          // elements between rows
-    int V, rows;
-    const Shaping* shaping;    // [rows], or [n_req] with row0
+    int V, first, rows;        // rows first .. first + rows - 1
+    bool more;                 // the grid behind this one has the rest of the rows
+    const Shaping* shaping;    // of all rows, or [n_req] with row0
     const int32_t* row0;       // nullable: [n_req + 1]
     int n_req;
     const float* u;
@@ -1014,7 +1015,8 @@ struct ShapeArgs {
 template <int C, bool kDraw, typename T, int VEC>
 __global__ void __launch_bounds__(kShapeThreads, 2) shape_kernel(const ShapeArgs a) {
     __shared__ ShapeSmem sm;
-    const int row = blockIdx.x / C;
+    if (a.more) pdl_launch_dependents();
+    const int row = a.first + blockIdx.x / C;
     const T* lr = static_cast<const T*>(a.logits) + (size_t)row * a.stride;
     if (kDraw) {
         shape_row<C, true, T, VEC>(lr, a.V, a.shaping[row], a.u[row], a.tokens + row, a.probs ? a.probs + (size_t)row * a.probs_stride : nullptr,
@@ -1026,10 +1028,13 @@ __global__ void __launch_bounds__(kShapeThreads, 2) shape_kernel(const ShapeArgs
         for (int i = threadIdx.x; i < a.n_req; i += kShapeThreads)
             if (a.row0[i] <= row && row < a.row0[i + 1]) s_req = i;
         __syncthreads();
-        const int req = s_req;
-        if (req < 0) return;                       // a row that is no request's (the whole cluster leaves)
-        shape_row<C, false, T, VEC>(lr, a.V, a.shaping[req], 0.f, nullptr, nullptr, a.shapes + row, sm);
+        const int req = s_req;                     // (-1: a row that is no request's)
+        if (req >= 0) shape_row<C, false, T, VEC>(lr, a.V, a.shaping[req], 0.f, nullptr, nullptr, a.shapes + row, sm);
     }
+    // What follows may begin to launch, and waits for this grid before it reads.  (A grid of the rest of a call's rows runs beside the one
+    // before it, and ends after it.)
+    pdl_launch_dependents();
+    pdl_wait();
 }
 
 // ---- acceptance -----------------------------------------------------------------------------------------------------------
@@ -1048,14 +1053,15 @@ struct AcceptArgs {
 };
 
 constexpr int kAcceptThreads = 1024;
-constexpr int kAcceptCluster = 8;
+constexpr int kAcceptBatch = 8;                    // steps of 32 ids whose loads are in flight together
 
-// A cluster per request, grid (kAcceptCluster, n_req).  The tests are independent of one another: thread i takes draft i, the first
+// A cluster of kCluster CTAs per request, grid (kCluster, n_req).  The tests are independent of one another: thread i takes draft i, the first
 // failure counts.  The draw is an inverse CDF in id order over fp64 terms, max(0, P - q) or P: warp w of CTA r adds the ids
 // [(r * 32 + w) * R, + R) lane by lane, the totals are added in warp and rank order, and the one warp whose range
 // holds u * total walks it again.
-template <typename T>
+template <int kAcceptCluster, typename T>
 __global__ void __launch_bounds__(kAcceptThreads) accept_shaped_kernel(const AcceptArgs a) {
+    pdl_wait();                                    // launched with programmatic serialisation: the shapes must be there
     constexpr int kWarps = kAcceptThreads / 32;
     const int req = blockIdx.y, rank = (int)cluster_ctarank(), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     __shared__ int s_first;
@@ -1100,15 +1106,29 @@ __global__ void __launch_bounds__(kAcceptThreads) accept_shaped_kernel(const Acc
     const int j0 = min(a.V, (rank * kWarps + warp) * R), j1 = min(a.V, j0 + R);
     bool use_q = n < k;
     const float* qr = a.q + (size_t)(slot0 + (use_q ? n : 0)) * a.q_stride;
-    auto term = [&](int j) {
-        if (j >= j1) return 0.0;
-        const double p = prob(lr, r, j, scale);
-        return use_q ? fmax(0.0, p - (double)qr[j]) : p;
+    // The terms of kAcceptBatch steps of 32 ids, this lane's.  (One step at a time, each waits for the L2: 20 us for a walk of 16.)
+    auto terms = [&](int j, double (&t)[kAcceptBatch]) {
+        float l[kAcceptBatch], q[kAcceptBatch];
+#pragma unroll
+        for (int i = 0; i < kAcceptBatch; ++i) {
+            const bool in = j + 32 * i < j1;
+            l[i] = in ? logit_f32(lr[j + 32 * i]) : -INFINITY;
+            q[i] = in && use_q ? qr[j + 32 * i] : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < kAcceptBatch; ++i) {
+            t[i] = 0.0;
+            if (shape_keeps(l[i], j + 32 * i, r)) t[i] = fmax(0.0, __dmul_rn(shape_exp2(shape_exponent(l[i], r)), scale) - (double)q[i]);
+        }
     };
     for (int attempt = 0; attempt < 2; ++attempt) {
         double sum = 0.0;
-#pragma unroll 4
-        for (int j = j0 + lane; j < j1; j += 32) sum += term(j);
+        for (int j = j0 + lane; j < j1; j += 32 * kAcceptBatch) {
+            double t[kAcceptBatch];
+            terms(j, t);
+#pragma unroll
+            for (int i = 0; i < kAcceptBatch; ++i) sum += t[i];
+        }
         sum = warp_sum_d(sum);
         if (lane == 0) s_warp[warp] = sum;
         __syncthreads();
@@ -1145,19 +1165,25 @@ __global__ void __launch_bounds__(kAcceptThreads) accept_shaped_kernel(const Acc
         if (s_base + s_incl[warp] > target && !(start > target)) {        // one warp of the cluster
             double run = start;
             int token = -1, last = -1;
-            for (int j = j0; j < j1 && token < 0; j += 32) {
-                const double own = term(j + lane);
-                double inc = own;
-                const unsigned mass = __ballot_sync(0xffffffffu, inc > 0.0);
-                if (mass) last = j + 31 - __clz(mass);
+            for (int j = j0; j < j1 && token < 0; j += 32 * kAcceptBatch) {
+                double own[kAcceptBatch];
+                terms(j + lane, own);
 #pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const double t = __shfl_up_sync(0xffffffffu, inc, o);
-                    if (lane >= o) inc += t;
+                for (int i = 0; i < kAcceptBatch; ++i) {
+                    if (token >= 0) continue;
+                    double inc = own[i];
+                    const unsigned mass = __ballot_sync(0xffffffffu, inc > 0.0);
+                    if (!mass) continue;
+                    last = j + 32 * i + 31 - __clz(mass);
+#pragma unroll
+                    for (int o = 1; o < 32; o <<= 1) {
+                        const double t = __shfl_up_sync(0xffffffffu, inc, o);
+                        if (lane >= o) inc += t;
+                    }
+                    const unsigned hit = __ballot_sync(0xffffffffu, own[i] > 0.0 && run + inc > target);
+                    if (hit) token = j + 32 * i + __ffs(hit) - 1;
+                    run += __shfl_sync(0xffffffffu, inc, 31);
                 }
-                const unsigned hit = __ballot_sync(0xffffffffu, own > 0.0 && run + inc > target);
-                if (hit) token = j + __ffs(hit) - 1;
-                run += __shfl_sync(0xffffffffu, inc, 31);
             }
             if (token < 0) token = last;           // the walk's rounding fell short of the range's total
             if (lane == 0) { a.n_accepted[req] = n; a.next_token[req] = token; }
