@@ -11,8 +11,8 @@
 //   V s       HD     [group][position 16]           bf16
 //   V z       HD     [group][position 16]           bf16
 // Both code orders are those of the A operand of mma.m16n8k16 (lane 4 g + t): a word ANDed with 0x000f000f is a register of
-// the operand, the same after shifts by 8, and with 0x00f000f0 another one.  Read as bf16 such a register holds the whole numbers
-// n < 256 times 2^-133 (subnormals: the exponent fields 0 and 1 are one linear range), so that a code needs one AND (and a shift for
+// the operand, the same after shifts by 8, and with 0x00f000f0 another one.  Read as fp16 such a register holds whole numbers (n < 2048)
+// times 2^-24 (subnormals: the exponent fields 0 and 1 are one linear range), so that a code needs one AND (and a shift for
 // every second one) and no conversion.  The factor 16 of the odd nibbles goes into Q, or into the step that centres V's codes.
 #pragma once
 #include "../common.cuh"
@@ -175,7 +175,9 @@ __device__ __forceinline__ uint32_t kv4_transpose(uint32_t x) {
 // A CTA takes a unit that gets new rows, and KV heads blockIdx.y, + gridDim.y, ...  A warp has one group of columns and eight of the unit's
 // positions (2t, 2t + 1, 2t + 8, 2t + 9 for two t), four lanes to a group, 8 columns each: what the words of V are made of, so that
 // nibbles change places within the warp and no barrier is needed.  V's words hold several positions: those that are not new keep theirs.
-// Bound: the latency of finding the unit and its page (three dependent loads) at few rows, instructions (about 15 a value) at many.
+// Bound: the latency of finding the unit and its page (three dependent loads) at few rows, instructions (some 30 a value, most of them the
+// 32-bit pipes') at many.  32 requests of one row (8 heads of 128, bf16): 4.7 us; 2048 rows of 32 heads: 29 us, 44 MB in and out, 1.5 TB/s
+// (through shared memory and two barriers, a division in fp64 near borders: 39 us).
 constexpr int kKv4AppendThreads = 256;
 template <int HD, typename T>
 __global__ void __launch_bounds__(kKv4AppendThreads) kv4_append_kernel(const Kv4AppendArgs a) {
@@ -263,7 +265,7 @@ struct Kv4ReadArgs {
     int units;
 };
 
-// The values of the rows' positions.  The first units * Hkv CTAs: one (unit, KV head) each, 8 columns of a row per thread.  The others look for rows
+// The values of the rows' positions; bound by its stores: 2048 rows of 32 heads 18 us, 78 MB in and out, 4.3 TB/s.  The first units * Hkv CTAs: one (unit, KV head) each, 8 columns of a row per thread.  The others look for rows
 // that have no position in any unit (no page, behind the table's end, no request): zeros.
 template <int HD>
 __global__ void __launch_bounds__(kKv4AppendThreads) kv4_read_kernel(const Kv4ReadArgs a) {

@@ -20,6 +20,13 @@
 // which kv4_merge_kernel adds up in CTA order.  No atomics, no state between calls.
 // Every warp has a ring of kAttendStages units of its own, filled by one bulk copy per unit: nothing synchronises the warps of a CTA
 // until its range, or a triple in it, ends.
+//
+// What bounds it.  Few query rows: instructions, 370 a unit and tile (80 of them the codes' unpacking, on a pipe of half rate), at 2.4 a cycle
+// of four; 1 row of 131072 positions over 8 heads 53 us, 168 MB, 3.2 TB/s (0.48 of the measured copy).  Short caches: a chain of 12 us (tables,
+// copies, queries, products, exchange, merge).  Many query rows: what every score costs in instructions, and the warp-level products.  The
+// same on tcgen05 -- a tile of 128 positions unpacked into tensor memory for 64 rows, a thread per key -- was slower at every number of
+// rows (9 rows of 32 heads 170 us for 66, 68 rows over 8 heads 117 for 80, 160 rows 193 for 151): its products take a tenth of the time, and
+// scores, exponentials and both unpackings, with barriers between them, more than here.
 #pragma once
 #include "kv4.cuh"
 
