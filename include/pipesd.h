@@ -338,7 +338,8 @@ int32_t pipesd_sample(const void *logits, int32_t dtype, int64_t row_stride, int
  * between rows; both have rows - n_req entries and may be null where that is 0).  u: [rows], per request k acceptance tests and
  * the final draw.  shaping: [n_req].  A draft x is accepted while u < min(1, p(x) / q(x)); a correction comes from norm(max(0, p - q)),
  * from p where that is 0 everywhere.  A row that has no distribution (see pipesd_sample) accepts nothing and gives next_token -1;
- * so does a request whose row0 entries make no sense.  scratch: pipesd_accept_scratch_bytes(rows) bytes, 8-byte aligned. */
+ * so does a request whose row0 entries make no sense.  scratch: pipesd_accept_scratch_bytes(rows) bytes, 8-byte aligned, one for
+ * each of calls that may run at the same time. */
 uint64_t pipesd_accept_scratch_bytes(int32_t rows);
 int32_t pipesd_accept(const void *logits, int32_t dtype, int64_t row_stride, int32_t n_req, int32_t rows, int32_t vocab,
                       const int32_t *row0, const pipesd_shaping *shaping, const float *q, int64_t q_stride,
@@ -372,13 +373,16 @@ uint64_t pipesd_kv4_pool_bytes(const pipesd_kv4_cfg *cfg);
 int32_t pipesd_kv4_append(const pipesd_kv4_cfg *cfg, void *pool, const void *k, const void *v, int32_t dtype, int64_t k_stride,
                           int64_t v_stride, int32_t n_req, int32_t rows, const int32_t *row0, const int32_t *base,
                           const int32_t *table, void *cuda_stream);
-/* The values that the rows' positions hold: fp32 [rows, n_kv_heads, head_dim] each, 16-byte aligned; 0 where no page is. */
+/* The values that the rows' positions hold: fp32 [rows, n_kv_heads, head_dim] each, 16-byte aligned; 0 where no page is, and for rows
+ * of no request. */
 int32_t pipesd_kv4_read(const pipesd_kv4_cfg *cfg, const void *pool, float *k, float *v, int32_t n_req, int32_t rows,
                         const int32_t *row0, const int32_t *base, const int32_t *table, void *cuda_stream);
 /* out[row] = softmax(scale * q . k) v over positions 0 .. base[r] + i of the request (its new rows appended before): a single
  * token, the k+1 rows of a verification, or a prompt.  q, out: [rows, n_q_heads, head_dim] of `dtype` with q_stride, out_stride;
  * n_q_heads a multiple of n_kv_heads; scale > 0.  bf16: products of bf16 with fp32 sums; fp32: operands carry 16 bits of mantissa.
- * A row that sees no position gives 0.  scratch: pipesd_kv4_attend_scratch_bytes(cfg) bytes, 16-byte aligned. */
+ * A row that sees no position gives 0; rows of no request are left as they are.  out must not overlap q.  A value's bits are kept
+ * relative to the largest of its request's: down to 2^-16 of it all of them, then fewer.  scratch: pipesd_kv4_attend_scratch_bytes(cfg)
+ * bytes, 16-byte aligned; it holds nothing between calls, but two calls that may run at the same time need one each. */
 uint64_t pipesd_kv4_attend_scratch_bytes(const pipesd_kv4_cfg *cfg);
 int32_t pipesd_kv4_attend(const pipesd_kv4_cfg *cfg, const void *pool, const void *q, void *out, int32_t dtype, int64_t q_stride,
                           int64_t out_stride, int32_t n_q_heads, float scale, int32_t n_req, int32_t rows, const int32_t *row0,

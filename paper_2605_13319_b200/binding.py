@@ -543,7 +543,8 @@ def accept(logits, row0, shaping, q, drafts, u, *, stream=None):
         assert q.dtype is torch.float32 and q.shape == (rows - n_req, vocab) and q.device == dev
         ql, qp, dp = _rows_of(q, "q"), q.data_ptr(), _vector(drafts, rows - n_req, torch.int32, dev, "drafts")
     with _on(dev, stream) as st:
-        n_accepted, next_token = torch.empty(n_req, dtype=torch.int32, device=dev), torch.empty(n_req, dtype=torch.int32, device=dev)
+        n_accepted = torch.empty(n_req, dtype=torch.int32, device=dev)
+        next_token = torch.empty_like(n_accepted)
         scratch = torch.empty(int(lib().pipesd_accept_scratch_bytes(rows)), dtype=torch.uint8, device=dev)
         rc = lib().pipesd_accept(logits.data_ptr(), _dtype_of(logits, "logits"), ld, n_req, rows, vocab, _vector(row0, n_req + 1, torch.int32, dev, "row0"),
                                  _vector(shaping, 4 * n_req, torch.int32, dev, "shaping"), qp, ql, dp, _vector(u, rows, torch.float32, dev, "u"),
@@ -609,7 +610,8 @@ class Kv4Cache:
         dev = self.pool.device
         cfg, where = self._where(rows, row0, base, table)
         with _on(dev, stream) as st:
-            k, v = (torch.empty((rows, self.n_kv_heads, self.head_dim), device=dev) for _ in range(2))
+            k = torch.empty((rows, self.n_kv_heads, self.head_dim), dtype=torch.float32, device=dev)
+            v = torch.empty_like(k)
             rc = lib().pipesd_kv4_read(ctypes.byref(cfg), self.pool.data_ptr(), k.data_ptr(), v.data_ptr(), *where, st)
         if rc != OK:
             raise PipesdError(rc, "pipesd_kv4_read")

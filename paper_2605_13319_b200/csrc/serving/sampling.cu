@@ -46,7 +46,9 @@ cudaError_t launch_cluster(void (*kernel)(Args), dim3 grid, int threads, int C, 
     }
     cfg.attrs = attr;
     cfg.numAttrs = n;
-    return cudaLaunchKernelEx(&cfg, kernel, a);
+    const cudaError_t e = cudaLaunchKernelEx(&cfg, kernel, a);
+    if (e != cudaSuccess) (void)cudaGetLastError();          // (reported here, not by the next call)
+    return e;
 }
 
 template <bool kDraw, typename T, int VEC>

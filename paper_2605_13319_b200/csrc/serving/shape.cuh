@@ -1072,9 +1072,10 @@ __global__ void __launch_bounds__(kAcceptThreads) accept_shaped_kernel(const Acc
     const int req = blockIdx.y, rank = (int)cluster_ctarank(), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     __shared__ int s_first;
     __shared__ double s_warp[kWarps], s_incl[kWarps], s_cta[2][kAcceptCluster], s_base, s_total;
-    const int first = a.row0[req], k = a.row0[req + 1] - first - 1;
-    const int slot0 = first - req;                 // of the request's first draft
-    if (k < 0 || first < 0 || first + k >= a.rows || slot0 < 0 || slot0 + k > a.rows - a.n_req) {     // no such rows (the whole cluster leaves)
+    const int first = a.row0[req], end = a.row0[req + 1];
+    const bool sane = first >= req && end > first && end <= a.rows && end - req - 1 <= a.rows - a.n_req;       // (its drafts are there too)
+    const int k = sane ? end - first - 1 : 0, slot0 = sane ? first - req : 0;     // slot0: of the request's first draft
+    if (!sane) {                                   // no such rows (the whole cluster leaves)
         if (rank == 0 && tid == 0) { a.n_accepted[req] = 0; a.next_token[req] = -1; }
         return;
     }

@@ -248,7 +248,7 @@ def test_accept_without_drafts_and_odd_requests():
     s3 = binding.shaping(3)
     got, token = binding.accept(_cuda(rows), _cuda(np.int32([0, 3, 6, 9])), s3, _cuda(qq), _cuda(drafts), _cuda(u3))
     assert got.tolist() == [1, 2, 2] and token[0].item() == -1 and token[1].item() == -1 and token[2].item() >= 0
-    for bad in ([0, 3, 2, 9], [-1, 3, 6, 9], [0, 3, 6, 12], [0, 0, 6, 9]):
+    for bad in ([0, 3, 2, 9], [-1, 3, 6, 9], [0, 3, 6, 12], [0, 0, 6, 9], [5, -2 ** 31 + 3, 6, 9], [2 ** 31 - 1, -2 ** 31, 6, 9]):
         got, token = binding.accept(_cuda(rows), _cuda(np.int32(bad)), s3, _cuda(qq), _cuda(drafts), _cuda(u3))
         for r in range(3):
             if bad[r] < 0 or bad[r + 1] > 9 or bad[r + 1] <= bad[r]:
