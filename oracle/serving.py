@@ -1,4 +1,4 @@
-"""64-bit checkers of shaped sampling, shaped acceptance and the 4-bit K/V cache, from their definitions, in numpy.
+"""64-bit forms of shaped sampling, shaped acceptance and the 4-bit K/V cache, from their definitions, in numpy.
 
 TEST INFRASTRUCTURE ONLY: nothing of the product path imports this."""
 from __future__ import annotations

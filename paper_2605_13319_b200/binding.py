@@ -626,7 +626,7 @@ class Kv4Cache:
         cfg, where = self._where(q.shape[0], row0, base, table)
         with _on(dev, stream) as st:
             if out is None:
-                out = torch.empty(q.shape, dtype=q.dtype, device=dev)
+                out = torch.empty_like(q, memory_format=torch.contiguous_format)
             else:
                 assert out.shape == q.shape and out.dtype is q.dtype and out.get_device() == dev.index, "out: like q"
             scratch = torch.empty(self._scratch_bytes, dtype=torch.uint8, device=dev)

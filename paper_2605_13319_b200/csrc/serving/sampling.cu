@@ -124,8 +124,8 @@ int32_t pipesd_accept(const void* logits, int32_t dtype, int64_t row_stride, int
     s.shapes = static_cast<RowShape*>(scratch);
     if (launch_shape_any<false>(s, dtype, st) != cudaSuccess) return PIPESD_E_CUDA;
     AcceptArgs a = {logits, row_stride, vocab, rows, row0, n_req, q, q_stride, drafts, u, s.shapes, n_accepted, next_token};
-    // CTAs of a request: as many as leave every CTA an SM of its own
-    const int c = n_req * 8 <= 148 ? 8 : n_req * 4 <= 148 ? 4 : 2;
+    // CTAs of a request: as many as fit the device together, two to an SM
+    const int c = n_req * 8 <= 2 * 148 ? 8 : n_req * 4 <= 2 * 148 ? 4 : 2;
     const bool f32 = dtype == PIPESD_F32;
     const auto kernel = c == 8 ? (f32 ? accept_shaped_kernel<8, float> : accept_shaped_kernel<8, uint16_t>)
                       : c == 4 ? (f32 ? accept_shaped_kernel<4, float> : accept_shaped_kernel<4, uint16_t>)

@@ -1058,15 +1058,16 @@ struct AcceptArgs {
     int32_t *n_accepted, *next_token;
 };
 
-constexpr int kAcceptThreads = 1024;
+constexpr int kAcceptThreads = 512;
 constexpr int kAcceptBatch = 8;                    // steps of 32 ids whose loads are in flight together
 
 // A cluster of kCluster CTAs per request, grid (kCluster, n_req).  The tests are independent of one another: thread i takes draft i, the first
 // failure counts.  The draw is an inverse CDF in id order over fp64 terms, max(0, P - q) or P: warp w of CTA r adds the ids
-// [(r * 32 + w) * R, + R) lane by lane, the totals are added in warp and rank order, and the one warp whose range
-// holds u * total walks it again.
+// [(r * 16 + w) * R, + R) batch by batch of 256, the totals are added in warp and rank order, and the one warp whose range
+// holds u * total goes through the batch that does again.  Bound by the latencies of five dependent loads and by the fp64 terms: with 1024 threads
+// a CTA, one to an SM, and the whole range walked again, 310 rows of 128256 ids for 32 requests took 151 us, rows included; so 143.
 template <int kAcceptCluster, typename T>
-__global__ void __launch_bounds__(kAcceptThreads) accept_shaped_kernel(const AcceptArgs a) {
+__global__ void __launch_bounds__(kAcceptThreads, 2) accept_shaped_kernel(const AcceptArgs a) {
     pdl_wait();                                    // launched with programmatic serialisation: the shapes must be there
     constexpr int kWarps = kAcceptThreads / 32;
     const int req = blockIdx.y, rank = (int)cluster_ctarank(), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -1110,6 +1111,7 @@ __global__ void __launch_bounds__(kAcceptThreads) accept_shaped_kernel(const Acc
     const double scale = kMassOne / (double)r.total;
     constexpr int kAllWarps = kAcceptCluster * kWarps;
     const int R = ((a.V + kAllWarps - 1) / kAllWarps + 31) / 32 * 32;
+    static_assert(kShapeMaxVocab <= kAllWarps * 32 * 32 * kAcceptBatch, "a lane per batch");
     const int j0 = min(a.V, (rank * kWarps + warp) * R), j1 = min(a.V, j0 + R);
     bool use_q = n < k;
     const float* qr = a.q + (size_t)(slot0 + (use_q ? n : 0)) * a.q_stride;
@@ -1122,33 +1124,47 @@ __global__ void __launch_bounds__(kAcceptThreads) accept_shaped_kernel(const Acc
             l[i] = in ? logit_f32(lr[j + 32 * i]) : -INFINITY;
             q[i] = in && use_q ? qr[j + 32 * i] : 0.f;
         }
+        bool keep[kAcceptBatch], any = false;
 #pragma unroll
         for (int i = 0; i < kAcceptBatch; ++i) {
+            keep[i] = shape_keeps(l[i], j + 32 * i, r);
+            any |= keep[i];
             t[i] = 0.0;
-            if (shape_keeps(l[i], j + 32 * i, r)) t[i] = fmax(0.0, __dmul_rn(shape_exp2(shape_exponent(l[i], r)), scale) - (double)q[i]);
         }
+        if (!__any_sync(0xffffffffu, any)) return;
+        double w[kAcceptBatch];                    // side by side, without a branch between them
+#pragma unroll
+        for (int i = 0; i < kAcceptBatch; ++i) w[i] = __dmul_rn(shape_exp2(shape_exponent(keep[i] ? l[i] : r.cut, r)), scale);
+#pragma unroll
+        for (int i = 0; i < kAcceptBatch; ++i) t[i] = keep[i] ? fmax(0.0, w[i] - (double)q[i]) : 0.0;
     };
     for (int attempt = 0; attempt < 2; ++attempt) {
-        double sum = 0.0;
-        for (int j = j0 + lane; j < j1; j += 32 * kAcceptBatch) {
-            double t[kAcceptBatch];
-            terms(j, t);
+        double sum = 0.0, batch_sum = 0.0;         // lane b: the sum of batch b
+        int n_batch = 0;
+        for (int j = j0; j < j1; j += 32 * kAcceptBatch, ++n_batch) {     // (all lanes together)
+            double t[kAcceptBatch], part = 0.0;
+            terms(j + lane, t);
 #pragma unroll
-            for (int i = 0; i < kAcceptBatch; ++i) sum += t[i];
+            for (int i = 0; i < kAcceptBatch; ++i) part += t[i];
+            part = warp_sum_d(part);
+            if (lane == n_batch) batch_sum = part;
+            sum += part;
         }
-        sum = warp_sum_d(sum);
         if (lane == 0) s_warp[warp] = sum;
         __syncthreads();
         if (warp == 0) {
-            double inc = s_warp[lane];
+            double inc = 0.0, before = 0.0, all = 0.0;       // in order: a warp without mass ends where it starts, exactly
 #pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const double t = __shfl_up_sync(0xffffffffu, inc, o);
-                if (lane >= o) inc += t;
+            for (int i = 0; i < kWarps; ++i) {
+                if (i == lane) before = all;
+                all += s_warp[i];
+                if (i == lane) inc = all;
             }
-            const double before = __shfl_up_sync(0xffffffffu, inc, 1), all = __shfl_sync(0xffffffffu, inc, 31);
-            s_warp[lane] = lane ? before : 0.0;    // a warp's start is the previous one's end, exactly
-            s_incl[lane] = inc;
+            __syncwarp();
+            if (lane < kWarps) {
+                s_warp[lane] = before;
+                s_incl[lane] = inc;
+            }
             if (lane < kAcceptCluster)
                 asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(dsmem_addr(smem_u32(&s_cta[attempt][rank]), (uint32_t)lane)), "d"(all) : "memory");
         }
@@ -1170,29 +1186,37 @@ __global__ void __launch_bounds__(kAcceptThreads) accept_shaped_kernel(const Acc
         }
         const double target = (double)uk * total, start = s_base + s_warp[warp];
         if (s_base + s_incl[warp] > target && !(start > target)) {        // one warp of the cluster
-            double run = start;
-            int token = -1, last = -1;
-            for (int j = j0; j < j1 && token < 0; j += 32 * kAcceptBatch) {
-                double own[kAcceptBatch];
-                terms(j + lane, own);
-#pragma unroll
-                for (int i = 0; i < kAcceptBatch; ++i) {
-                    if (token >= 0) continue;
-                    double inc = own[i];
-                    const unsigned mass = __ballot_sync(0xffffffffu, inc > 0.0);
-                    if (!mass) continue;
-                    last = j + 32 * i + 31 - __clz(mass);
-#pragma unroll
-                    for (int o = 1; o < 32; o <<= 1) {
-                        const double t = __shfl_up_sync(0xffffffffu, inc, o);
-                        if (lane >= o) inc += t;
-                    }
-                    const unsigned hit = __ballot_sync(0xffffffffu, own[i] > 0.0 && run + inc > target);
-                    if (hit) token = j + 32 * i + __ffs(hit) - 1;
-                    run += __shfl_sync(0xffffffffu, inc, 31);
-                }
+            // its batch with the target (or, where rounding falls short of that, the last one with mass), then the id
+            double run = start, before = start;
+            int at = 0;
+            for (int i = 0; i < n_batch; ++i) {
+                const double part = __shfl_sync(0xffffffffu, batch_sum, i);
+                if (part > 0.0) { at = i; before = run; }
+                run += part;
+                if (part > 0.0 && run > target) break;
             }
-            if (token < 0) token = last;           // the walk's rounding fell short of the range's total
+            int token = -1, last = -1;
+            const int j = j0 + at * 32 * kAcceptBatch;
+            double own[kAcceptBatch];
+            terms(j + lane, own);
+            run = before;
+#pragma unroll
+            for (int i = 0; i < kAcceptBatch; ++i) {
+                if (token >= 0) continue;
+                double inc = own[i];
+                const unsigned mass = __ballot_sync(0xffffffffu, inc > 0.0);
+                if (!mass) continue;
+                last = j + 32 * i + 31 - __clz(mass);
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const double t = __shfl_up_sync(0xffffffffu, inc, o);
+                    if (lane >= o) inc += t;
+                }
+                const unsigned hit = __ballot_sync(0xffffffffu, own[i] > 0.0 && run + inc > target);
+                if (hit) token = j + 32 * i + __ffs(hit) - 1;
+                run += __shfl_sync(0xffffffffu, inc, 31);
+            }
+            if (token < 0) token = last;           // the walk's rounding fell short of the batch's total
             if (lane == 0) { a.n_accepted[req] = n; a.next_token[req] = token; }
         }
         break;

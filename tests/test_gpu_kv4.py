@@ -44,7 +44,7 @@ class Case:
                         self.ref.write(self.table[r], h, (base or self.base)[r] + i, kv, x[self.row(r, i), h])
 
     def fill(self, rng, spread=None):
-        """Values in every position before the new rows too (written by the checker, bytes sent over)."""
+        """Values in every position before the new rows too (written by the 64-bit form, bytes sent over)."""
         import torch
         for r, b in enumerate(self.base):
             for pos in range(b):
@@ -211,7 +211,7 @@ def test_attend_pages_that_are_not_there():
 
 
 def _big(seed, new, base, heads, kvh, hd, dtype, page=16):
-    """A case too large for the checker's loops, with a plain 64-bit form on the device."""
+    """A case too large for the 64-bit loops, with a plain 64-bit form on the device."""
     import torch
     from paper_2605_13319_b200 import binding
     g = torch.Generator("cuda").manual_seed(seed)
@@ -316,7 +316,7 @@ def test_attend_offsets_beyond_32_bits():
 def test_serving_round_together():
     """A model of one layer, served as these operators are meant to be: the prompt's K and V appended and attended, the output
     projected by the library's GEMM, the pending token sampled; then draft steps (sampled with their distributions), one
-    verification of all of them, and the cache rolled back to what was accepted.  Every step against the 64-bit checkers on the
+    verification of all of them, and the cache rolled back to what was accepted.  Every step against the 64-bit forms on the
     step's own inputs; the verification's outputs are those of single steps."""
     import torch
     from paper_2605_13319_b200 import binding
