@@ -90,9 +90,10 @@ int32_t pipesd_kv4_append(const pipesd_kv4_cfg* cfg, void* pool, const void* k, 
     if (rows > 1 && (k_stride < width || v_stride < width)) return PIPESD_E_INVALID;
     const Kv4AppendArgs a = {where_of(cfg, n_req, rows, row0, base, table), k, v, k_stride, v_stride, static_cast<unsigned char*>(pool),
                              wide(k, k_stride, rows, dtype) && wide(v, v_stride, rows, dtype)};
-    // enough CTAs to fill the device four times over; beyond that a CTA takes several heads of its unit
+    // CTAs for one wave and a half (four to an SM), beyond which a CTA takes several heads of its unit: 2048 rows 27.1 us with one wave, 25.9, 24.4
+    // with two; 5 requests of 100 to 700 rows in fp32 7.4, 7.2, 7.9
     const int units = most_units(n_req, rows);
-    const dim3 grid((unsigned)units, (unsigned)std::min(cfg->n_kv_heads, std::max(1, 4 * 148 / units)));
+    const dim3 grid((unsigned)units, (unsigned)std::min(cfg->n_kv_heads, std::max(1, 6 * 148 / units)));
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (cfg->head_dim == 128) {
         if (dtype == PIPESD_F32) kv4_append_kernel<128, float><<<grid, kKv4AppendThreads, 0, st>>>(a);

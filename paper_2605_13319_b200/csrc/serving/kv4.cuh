@@ -176,11 +176,11 @@ __device__ __forceinline__ uint32_t kv4_transpose(uint32_t x) {
 // positions (2t, 2t + 1, 2t + 8, 2t + 9 for two t), four lanes to a group, 8 columns each: what the words of V are made of, so that
 // nibbles change places within the warp and no barrier is needed.  V's words hold several positions: those that are not new keep theirs.
 // Bound: the latency of finding the unit and its page (three dependent loads) at few rows, instructions (some 30 a value, most of them the
-// 32-bit pipes') at many.  32 requests of one row (8 heads of 128, bf16): 4.7 us; 2048 rows of 32 heads: 29 us, 44 MB in and out, 1.5 TB/s
-// (through shared memory and two barriers, a division in fp64 near borders: 39 us).
+// 32-bit pipes') at many.  32 requests of one row (8 heads of 128, bf16): 4.7 us; 2048 rows of 32 heads: 26 us, 44 MB in and out, 1.7 TB/s
+// (through shared memory and two barriers, a division in fp64 near borders: 39 us; three CTAs to an SM instead of four: 28).
 constexpr int kKv4AppendThreads = 256;
 template <int HD, typename T>
-__global__ void __launch_bounds__(kKv4AppendThreads) kv4_append_kernel(const Kv4AppendArgs a) {
+__global__ void __launch_bounds__(kKv4AppendThreads, 4) kv4_append_kernel(const Kv4AppendArgs a) {
     constexpr int kGroups = HD / kKv4Group, kCombos = 2 * kGroups, kWarps = kKv4AppendThreads / 32;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int unit;
