@@ -327,7 +327,8 @@ typedef struct pipesd_shaping {
 /* One token per row: the first id whose running probability, in id order, exceeds u[row] (0 <= u < 1).  logits: [rows, vocab] of
  * `dtype`, row_stride elements between rows, vocab up to 2^18.  shaping, u: [rows].  probs (nullable): fp32 [rows, vocab] with
  * probs_stride, the distributions that the tokens were drawn from -- the q of a draft step.  A row without a distribution (no finite
- * logit, a NaN or +inf among them, settings or u out of range) gets token -1 and probabilities 0. */
+ * logit, a NaN or +inf among them, settings or u out of range) gets token -1 and probabilities 0.
+ * probs must not overlap logits: a row is read again while another part of it is written. */
 int32_t pipesd_sample(const void *logits, int32_t dtype, int64_t row_stride, int32_t rows, int32_t vocab,
                       const pipesd_shaping *shaping, const float *u, int32_t *tokens, float *probs, int64_t probs_stride,
                       void *cuda_stream);
@@ -355,8 +356,8 @@ int32_t pipesd_accept(const void *logits, int32_t dtype, int64_t row_stride, int
  *
  * Where rows go: request r has the rows row0[r] .. row0[r+1]-1 of a call (row0: n_req + 1 entries from 0 to rows), and row i of it
  * is position base[r] + i.  table: [n_req, max_pages] page ids; an id outside 0..n_pages-1 is a page that is not there: rows that
- * belong to it are dropped, and attention sees no position of it.  So are rows behind position max_pages * page_size.  No two
- * requests of an append may share a page that gets rows. */
+ * belong to it are dropped, and attention sees no position of it.  So are rows behind position max_pages * page_size.  A page
+ * that gets rows of an append is in one request's pages, once. */
 typedef struct pipesd_kv4_cfg {
     int32_t n_kv_heads;
     int32_t head_dim;  /* 64 or 128                                            */
@@ -379,8 +380,8 @@ int32_t pipesd_kv4_read(const pipesd_kv4_cfg *cfg, const void *pool, float *k, f
                         const int32_t *row0, const int32_t *base, const int32_t *table, void *cuda_stream);
 /* out[row] = softmax(scale * q . k) v over positions 0 .. base[r] + i of the request (its new rows appended before): a single
  * token, the k+1 rows of a verification, or a prompt.  q, out: [rows, n_q_heads, head_dim] of `dtype` with q_stride, out_stride;
- * n_q_heads a multiple of n_kv_heads; scale > 0.  bf16: products of bf16 with fp32 sums; fp32: operands carry 16 bits of mantissa.
- * A row that sees no position gives 0; rows of no request are left as they are.  out must not overlap q.  A value's bits are kept
+ * n_q_heads a multiple of n_kv_heads; scale > 0, and scale * |q| below 2^96.  bf16: products of bf16 with fp32 sums;
+ * fp32: operands carry 16 bits of mantissa.  A row that sees no position gives 0; rows of no request are left as they are.  out must not overlap q.  A value's bits are kept
  * relative to the largest of its request's: down to 2^-16 of it all of them, then fewer.  scratch: pipesd_kv4_attend_scratch_bytes(cfg)
  * bytes, 16-byte aligned; it holds nothing between calls, but two calls that may run at the same time need one each. */
 uint64_t pipesd_kv4_attend_scratch_bytes(const pipesd_kv4_cfg *cfg);

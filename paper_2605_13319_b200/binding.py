@@ -442,12 +442,15 @@ def debug_attn_split(total_keys: int, page_size: int, resident_ctas, units: int)
 
 # ---- shaped sampling and acceptance, on device tensors (no context)
 class _on:
-    """The device as the current one, and `stream` (None: its current stream) as the one that allocations belong to."""
+    """The device as the current one, and `stream` (None: its current stream) as the one that allocations belong to.  With a stream of
+    its own, a call keeps the memory of its tensors from being given out again while that stream may still use it: those that it is
+    given, and, for the current stream, those that it makes."""
 
-    __slots__ = ("index", "stream", "scopes")
+    __slots__ = ("index", "stream", "tensors", "scopes", "home")
 
-    def __init__(self, device, stream):
-        self.index, self.stream, self.scopes = device.index, stream, None
+    def __init__(self, device, stream, *tensors):
+        self.index, self.stream, self.tensors, self.scopes, self.home = device.index, stream, tensors, None, None
+        assert stream is None or stream.device == device, f"stream: one of {device} expected"
 
     def __enter__(self):
         import torch
@@ -457,12 +460,21 @@ class _on:
         self.scopes = contextlib.ExitStack()
         self.scopes.enter_context(torch.cuda.device(self.index))
         if self.stream is not None:
+            self.home = torch.cuda.current_stream(self.index)
+            for t in self.tensors:
+                if t is not None and t.is_cuda:
+                    t.record_stream(self.stream)
             self.scopes.enter_context(torch.cuda.stream(self.stream))
         return torch.cuda.current_stream(self.index).cuda_stream
 
     def __exit__(self, *exc):
         if self.scopes is not None:
             self.scopes.close()
+
+    def made(self, *tensors):
+        if self.home is not None:
+            for t in tensors:
+                t.record_stream(self.home)
 
 
 def _rows_of(t, name):
@@ -518,9 +530,11 @@ def sample(logits, shaping, u, *, probs=None, tokens=None, stream=None):
     if probs is not None:
         assert probs.dtype is torch.float32 and probs.shape == (rows, vocab) and probs.device == dev
         pl = _rows_of(probs, "probs")
-    with _on(dev, stream) as st:
+    on = _on(dev, stream, logits, shaping, u, probs, tokens)
+    with on as st:
         if tokens is None:
             tokens = torch.empty(rows, dtype=torch.int32, device=dev)
+            on.made(tokens)
         rc = lib().pipesd_sample(logits.data_ptr(), _dtype_of(logits, "logits"), ld, rows, vocab, _vector(shaping, 4 * rows, torch.int32, dev, "shaping"),
                                  _vector(u, rows, torch.float32, dev, "u"), _vector(tokens, rows, torch.int32, dev, "tokens"),
                                  probs.data_ptr() if probs is not None else None, pl, st)
@@ -540,11 +554,14 @@ def accept(logits, row0, shaping, q, drafts, u, *, stream=None):
     ld = _rows_of(logits, "logits")
     ql, qp, dp = 0, None, None
     if rows > n_req:
+        assert q is not None and drafts is not None, "q, drafts: of the rows beyond one per request"
         assert q.dtype is torch.float32 and q.shape == (rows - n_req, vocab) and q.device == dev
         ql, qp, dp = _rows_of(q, "q"), q.data_ptr(), _vector(drafts, rows - n_req, torch.int32, dev, "drafts")
-    with _on(dev, stream) as st:
+    on = _on(dev, stream, logits, row0, shaping, q, drafts, u)
+    with on as st:
         n_accepted = torch.empty(n_req, dtype=torch.int32, device=dev)
         next_token = torch.empty_like(n_accepted)
+        on.made(n_accepted, next_token)
         scratch = torch.empty(int(lib().pipesd_accept_scratch_bytes(rows)), dtype=torch.uint8, device=dev)
         rc = lib().pipesd_accept(logits.data_ptr(), _dtype_of(logits, "logits"), ld, n_req, rows, vocab, _vector(row0, n_req + 1, torch.int32, dev, "row0"),
                                  _vector(shaping, 4 * n_req, torch.int32, dev, "shaping"), qp, ql, dp, _vector(u, rows, torch.float32, dev, "u"),
@@ -598,7 +615,7 @@ class Kv4Cache:
         shape = (k.shape[0], self.n_kv_heads, self.head_dim)
         assert k.shape == shape == v.shape and k.dtype is v.dtype and k.get_device() == dev.index == v.get_device(), f"k, v: two alike of {shape} on {dev}"
         cfg, where = self._where(k.shape[0], row0, base, table)
-        with _on(dev, stream) as st:
+        with _on(dev, stream, self.pool, k, v, row0, base, table) as st:
             rc = lib().pipesd_kv4_append(ctypes.byref(cfg), self.pool.data_ptr(), k.data_ptr(), v.data_ptr(), _dtype_of(k, "k"), _rows_of(k, "k"), _rows_of(v, "v"),
                                          *where, st)
         if rc != OK:
@@ -609,9 +626,11 @@ class Kv4Cache:
         import torch
         dev = self.pool.device
         cfg, where = self._where(rows, row0, base, table)
-        with _on(dev, stream) as st:
+        on = _on(dev, stream, self.pool, row0, base, table)
+        with on as st:
             k = torch.empty((rows, self.n_kv_heads, self.head_dim), dtype=torch.float32, device=dev)
             v = torch.empty_like(k)
+            on.made(k, v)
             rc = lib().pipesd_kv4_read(ctypes.byref(cfg), self.pool.data_ptr(), k.data_ptr(), v.data_ptr(), *where, st)
         if rc != OK:
             raise PipesdError(rc, "pipesd_kv4_read")
@@ -624,9 +643,11 @@ class Kv4Cache:
         dev = self.pool.device
         assert q.dim() == 3 and q.shape[2] == self.head_dim and q.get_device() == dev.index, f"q: [rows, query heads, {self.head_dim}] on {dev}"
         cfg, where = self._where(q.shape[0], row0, base, table)
-        with _on(dev, stream) as st:
+        on = _on(dev, stream, self.pool, q, row0, base, table, out)
+        with on as st:
             if out is None:
                 out = torch.empty_like(q, memory_format=torch.contiguous_format)
+                on.made(out)
             else:
                 assert out.shape == q.shape and out.dtype is q.dtype and out.get_device() == dev.index, "out: like q"
             scratch = torch.empty(self._scratch_bytes, dtype=torch.uint8, device=dev)

@@ -89,7 +89,8 @@ extern "C" {
 
 int32_t pipesd_sample(const void* logits, int32_t dtype, int64_t row_stride, int32_t rows, int32_t vocab, const pipesd_shaping* shaping,
                       const float* u, int32_t* tokens, float* probs, int64_t probs_stride, void* cuda_stream) {
-    if (!rows_ok(logits, dtype, row_stride, rows, vocab) || !shaping || !u || !tokens || (probs && probs_stride < vocab)) return PIPESD_E_INVALID;
+    if (!rows_ok(logits, dtype, row_stride, rows, vocab) || !shaping || !u || !tokens || (probs && (probs_stride < vocab || probs == logits)))
+        return PIPESD_E_INVALID;
     ShapeArgs a = {};
     a.logits = logits;
     a.stride = row_stride;

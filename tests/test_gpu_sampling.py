@@ -177,6 +177,26 @@ def test_sample_in_a_graph_and_on_other_streams():
         assert all(torch.equal(x, want) for x in got)
 
 
+def test_inputs_that_are_let_go_while_another_stream_waits():
+    import torch
+    from paper_2605_13319_b200 import binding
+    rows, V = 20, 32000
+    g = torch.Generator("cuda").manual_seed(1)
+    logits, u = torch.randn((rows, V), generator=g, device="cuda") * 2, torch.rand(rows, generator=g, device="cuda")
+    shaping, side = binding.shaping(rows, top_p=0.8), torch.cuda.Stream()
+    want = binding.sample(logits, shaping, u)
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(20_000_000)
+    got = binding.sample(logits, shaping, u, stream=side)
+    place = logits.data_ptr()
+    del logits
+    others = [torch.zeros((rows, V), device="cuda") for _ in range(2)]
+    assert place not in [x.data_ptr() for x in others]
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)
+
+
 # --------------------------------------------------------------------------- acceptance
 def _rounds(rng, ks, vocab, sharp):
     """Logits of all rows, q and drafts (from q) of all drafts, uniforms."""

@@ -17,7 +17,7 @@ def sample(logits=P, dtype=binding.F32, stride=1024, rows=2, vocab=1024, shaping
 @pytest.mark.parametrize("bad", [
     dict(logits=None), dict(shaping=None), dict(u=None), dict(tokens=None), dict(dtype=2), dict(dtype=-1), dict(rows=0), dict(rows=-3),
     dict(vocab=0), dict(vocab=(1 << 18) + 1, stride=1 << 19), dict(stride=1023), dict(stride=-1024), dict(logits=P + 2),
-    dict(dtype=binding.BF16, logits=P + 1), dict(probs=P, probs_stride=1023),
+    dict(dtype=binding.BF16, logits=P + 1), dict(probs=P, probs_stride=1023), dict(probs=P, probs_stride=1024),
 ])
 def test_sample_refuses(bad):
     assert sample(**bad) == INVALID
@@ -88,3 +88,34 @@ def test_settings_are_checked_on_the_host():
                 dict(min_p=-0.1), dict(min_p=1.5), dict(min_p=float("nan"))):
         with pytest.raises(ValueError):
             binding.shaping(2, device="cpu", **bad)
+
+
+class _Tensor:
+    def __init__(self, cuda=True):
+        self.is_cuda, self.on = cuda, []
+
+    def record_stream(self, stream):
+        self.on.append(stream)
+
+
+def test_streams_belong_to_the_tensors_device():
+    import torch
+    other = type("Stream", (), {"device": torch.device("cuda", 1)})()
+    with pytest.raises(AssertionError, match="stream"):
+        binding._on(torch.device("cuda", 0), other)
+    binding._on(torch.device("cuda", 1), other)
+
+
+def test_memory_is_kept_for_a_stream_of_its_own(monkeypatch):
+    import contextlib
+    import torch
+    monkeypatch.setattr(torch.cuda, "device", lambda i: contextlib.nullcontext())
+    monkeypatch.setattr(torch.cuda, "stream", lambda s: contextlib.nullcontext())
+    home = type("Stream", (), {"cuda_stream": 7})()
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda i: home)
+    side = type("Stream", (), {"device": torch.device("cuda", 0)})()
+    given, on_host, made = _Tensor(), _Tensor(False), _Tensor()
+    on = binding._on(torch.device("cuda", 0), side, given, None, on_host)
+    with on as st:
+        on.made(made)
+    assert st == 7 and given.on == [side] and on_host.on == [] and made.on == [home]
