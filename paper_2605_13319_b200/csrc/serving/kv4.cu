@@ -70,7 +70,12 @@ int32_t attend_run(Kv4AttendArgs& a, int nt, cudaStream_t st) {
     attend_fn<HD, T>(nt)<<<a.ctas, 32 * attend_warps(nt), attend_smem<HD, T>(nt), st>>>(a);
     if (cudaGetLastError() != cudaSuccess) return PIPESD_E_CUDA;
     const long long jobs = (long long)a.w.rows * a.Hq;
-    if (launch_pdl(kv4_merge_kernel<HD, T>, dim3((unsigned)jobs), dim3(32 * kMergeWarps), 0, st, a) != cudaSuccess) return PIPESD_E_CUDA;
+    const bool many = jobs > kMergeWave;
+    a.heads = many ? (int)std::min<long long>(a.Hq, (jobs + kMergeWave * kMergeWarps - 1) / (kMergeWave * kMergeWarps)) : 1;
+    const long long blocks = (long long)a.w.rows * ((a.Hq + a.heads - 1) / a.heads);
+    if (launch_pdl(many ? kv4_merge_kernel<HD, 1, T> : kv4_merge_kernel<HD, kMergeWarps, T>, dim3((unsigned)(many ? (blocks + kMergeWarps - 1) / kMergeWarps : blocks)),
+                   dim3(32 * kMergeWarps), 0, st, a) != cudaSuccess)
+        return PIPESD_E_CUDA;
     return launched();
 }
 

@@ -56,7 +56,7 @@ struct Kv4AttendArgs {
     int Hq;
     float scale;               // times log2(e)
     float* parts;              // [2 * CTAs][8 NT (HD + 2)]
-    int ctas, rows_cap;        // rows_cap: query rows of a triple
+    int ctas, rows_cap, heads; // rows_cap: query rows of a triple; heads: of a row that a warp or CTA of the merge takes
 };
 
 // What a request adds to the flat sequence of units: units per triple and triples.
@@ -622,17 +622,22 @@ __global__ void __launch_bounds__(32 * attend_warps(NT), attend_ctas_per_sm(NT))
     }
 }
 
-// One CTA per (row, query head): adds up the shares of a triple that several CTAs had.  Warp w takes the shares w, w + 4, ...; the
-// warps' sums are added in their order.  (A warp for a row alone waits for the L2 once per four shares: 12 us for 37 of them.)
+// Adds up the shares of triples that several CTAs had, per (row, query head).  W warps each: a CTA per job, of which warp w takes the shares w,
+// w + 4, ..., and the warps' sums are added in their order (a warp for a row alone waits for the L2 once per four shares: 12 us for 37 of them).
+// W = 1: beyond a wave of such CTAs a warp per a.heads heads of a row, since what finds a job's shares costs more than the few that each then
+// has (us with four and one: 32 rows of 32 heads, one wave, 52.5 52.6; 64 rows 63.7 60; 155 rows in fp32 206 198; 2000 rows 705 606).
 constexpr int kMergeWarps = 4;
-template <int HD, typename T>
+constexpr int kMergeWave = 148 * 9;                // CTAs of it that the device holds (56 registers)
+template <int HD, int W, typename T>
 __global__ void __launch_bounds__(32 * kMergeWarps) kv4_merge_kernel(const Kv4AttendArgs a) {
     constexpr int kE = HD / 32;
-    __shared__ float s_v[kMergeWarps][HD], s_sum[kMergeWarps];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int row = (int)(blockIdx.x / a.Hq), qh = (int)(blockIdx.x % a.Hq), G = a.Hq / a.w.Hkv;
+    __shared__ float s_v[W][HD], s_sum[W];
+    const int lane = threadIdx.x & 31, warp = W == 1 ? 0 : threadIdx.x >> 5;
+    const long long job = W == 1 ? (long long)blockIdx.x * kMergeWarps + (threadIdx.x >> 5) : (long long)blockIdx.x;
+    const int blocks = (a.Hq + a.heads - 1) / a.heads, G = a.Hq / a.w.Hkv;       // (of heads)
+    const int row = (int)(job / blocks), q0 = (int)(job % blocks) * a.heads, q1 = min(a.Hq, q0 + a.heads);
     int req = -1;
-    for (int r0 = 0; r0 < a.w.n_req && req < 0; r0 += 32) {
+    for (int r0 = 0; row < a.w.rows && r0 < a.w.n_req && req < 0; r0 += 32) {    // (the last CTA's warps may have no row)
         const int r = min(r0 + lane, a.w.n_req - 1);
         const unsigned hit = __ballot_sync(0xffffffffu, a.w.row0[r] <= row && row < a.w.row0[r + 1]);
         if (hit) req = min(r0 + __ffs(hit) - 1, a.w.n_req - 1);
@@ -645,47 +650,49 @@ __global__ void __launch_bounds__(32 * kMergeWarps) kv4_merge_kernel(const Kv4At
     // ended without could let its successor begin before its predecessor has ended.
     pdl_wait();
     if (req < 0) return;
-    T* out = static_cast<T*>(a.out) + (size_t)row * a.out_stride + (size_t)qh * HD + lane * kE;
-    if (row - first >= n) {                        // a row without a position: nothing to see
-        if (warp == 0)
-#pragma unroll
-            for (int i = 0; i < kE; ++i) attend_out(out + i, 0.f);
-        return;
-    }
-    const int rho = (row - first) * G + qh % G;
-    const long long start = before + (long long)(qh / G * groups + rho / a.rows_cap) * units;
-    const int c0 = (int)(start / share), c1 = (int)((start + units - 1) / share);
-    if (c0 == c1) return;
-    const int local = rho % a.rows_cap;
     const size_t slot_size = (size_t)a.rows_cap * (HD + 2);
-    auto slot = [&](int c) { return a.parts + (size_t)(2 * c + (start > (long long)c * share ? 1 : 0)) * slot_size; };
-    float top = kAttendNone;
-    for (int c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, slot(c)[a.rows_cap * HD + local]);
-    top = warp_max_f32(top);
-    float v[kE] = {}, sum = 0.f;
+    for (int qh = q0; qh < q1; ++qh) {
+        T* out = static_cast<T*>(a.out) + (size_t)row * a.out_stride + (size_t)qh * HD + lane * kE;
+        if (row - first >= n) {                    // a row without a position: nothing to see
+            if (warp == 0)
+#pragma unroll
+                for (int i = 0; i < kE; ++i) attend_out(out + i, 0.f);
+            continue;
+        }
+        const int rho = (row - first) * G + qh % G;
+        const long long start = before + (long long)(qh / G * groups + rho / a.rows_cap) * units;
+        const int c0 = (int)(start / share), c1 = (int)((start + units - 1) / share);
+        if (c0 == c1) continue;
+        const int local = rho % a.rows_cap;
+        auto slot = [&](int c) { return a.parts + (size_t)(2 * c + (start > (long long)c * share ? 1 : 0)) * slot_size; };
+        float top = kAttendNone;
+        for (int c = c0 + lane; c <= c1; c += 32) top = fmaxf(top, slot(c)[a.rows_cap * HD + local]);
+        top = warp_max_f32(top);
+        float v[kE] = {}, sum = 0.f;
 #pragma unroll 4
-    for (int c = c0 + warp; c <= c1; c += kMergeWarps) {
-        const float* p = slot(c);
-        const float factor = attend_exp2(p[a.rows_cap * HD + local] - top);
+        for (int c = c0 + warp; c <= c1; c += W) {
+            const float* p = slot(c);
+            const float factor = attend_exp2(p[a.rows_cap * HD + local] - top);
 #pragma unroll
-        for (int i = 0; i < kE; ++i) v[i] = fmaf(factor, p[local * HD + lane * kE + i], v[i]);
-        sum = fmaf(factor, p[a.rows_cap * (HD + 1) + local], sum);
-    }
+            for (int i = 0; i < kE; ++i) v[i] = fmaf(factor, p[local * HD + lane * kE + i], v[i]);
+            sum = fmaf(factor, p[a.rows_cap * (HD + 1) + local], sum);
+        }
+        if (W > 1) {                               // (one head: a.heads is 1)
 #pragma unroll
-    for (int i = 0; i < kE; ++i) s_v[warp][lane * kE + i] = v[i];
-    if (lane == 0) s_sum[warp] = sum;
-    __syncthreads();
-    if (warp) return;
-    sum = 0.f;
+            for (int i = 0; i < kE; ++i) s_v[warp][lane * kE + i] = v[i];
+            if (lane == 0) s_sum[warp] = sum;
+            __syncthreads();
+            if (warp) return;
 #pragma unroll
-    for (int w = 0; w < kMergeWarps; ++w) sum += s_sum[w];
-    const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);
+            for (int w = 1; w < W; ++w) {
+                sum += s_sum[w];
 #pragma unroll
-    for (int i = 0; i < kE; ++i) {
-        float x = 0.f;
+                for (int i = 0; i < kE; ++i) v[i] += s_v[w][lane * kE + i];
+            }
+        }
+        const float inv = sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : sum);
 #pragma unroll
-        for (int w = 0; w < kMergeWarps; ++w) x += s_v[w][lane * kE + i];
-        attend_out(out + i, x * inv);
+        for (int i = 0; i < kE; ++i) attend_out(out + i, v[i] * inv);
     }
 }
 
