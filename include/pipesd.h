@@ -381,7 +381,7 @@ int32_t pipesd_kv4_read(const pipesd_kv4_cfg *cfg, const void *pool, float *k, f
 /* out[row] = softmax(scale * q . k) v over positions 0 .. base[r] + i of the request (its new rows appended before): a single
  * token, the k+1 rows of a verification, or a prompt.  q, out: [rows, n_q_heads, head_dim] of `dtype` with q_stride, out_stride;
  * n_q_heads a multiple of n_kv_heads; scale > 0, and scale * |q| below 2^96.  bf16: products of bf16 with fp32 sums;
- * fp32: operands carry 16 bits of mantissa.  A row that sees no position gives 0; rows of no request are left as they are.  out must not overlap q.  A value's bits are kept
+ * fp32: operands carry 22 bits of mantissa.  A row that sees no position gives 0; rows of no request are left as they are.  out must not overlap q.  A value's bits are kept
  * relative to the largest of its request's: down to 2^-16 of it all of them, then fewer.  scratch: pipesd_kv4_attend_scratch_bytes(cfg)
  * bytes, 16-byte aligned; it holds nothing between calls, but two calls that may run at the same time need one each. */
 uint64_t pipesd_kv4_attend_scratch_bytes(const pipesd_kv4_cfg *cfg);

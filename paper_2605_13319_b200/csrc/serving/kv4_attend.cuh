@@ -14,7 +14,9 @@
 // fits the warp's first unit, and rescaled (like a row's exponentials, which are relative to a score of that unit) when one
 // exceeds it by 2^6 (2^4).
 // fp32 queries and outputs (kSplit): Q, P, P * s and the middles as two fp16 terms each, 22 bits of mantissa; a unit's products go to the
-// running sums by ordinary additions, which round to nearest (the tensor pipe truncates where it adds: error 2.1e-6 over long caches).
+// running sums by ordinary additions, which round to nearest, and keys' codes are centred too, middles times sums of Q (fp32) added beside
+// (the tensor pipe truncates where it adds: error 2.1e-6 over long caches without either, 1.2e-6 with the additions, 2.5e-7 with both;
+// 155 ragged rows take 9 us of 206 more for the one, 3 of 201 for the other).  An exponential's argument stays near 0, P's power of two comes after.
 // Work: the units of all (request, KV head, row group) triples in a row, cut into equal ranges, one per CTA; the warps of a CTA take
 // its units in turn.  A triple that one CTA has whole is finished there; of others each CTA leaves (O, reference, denominator),
 // which kv4_merge_kernel adds up in CTA order.  No atomics, no state between calls.
@@ -43,7 +45,7 @@ constexpr float kAttendExcess = 4.f;               // log2 units by which a scor
 constexpr float kAttendScaleExcess = 64.f;         // factor by which a scale may exceed its warp's unit
 // fp16 has 40 binades for a number and its second term: P is taken times 2^6 (up to 2^10), scales times 1 / 4 (up to 2^5: their 8 bits are exact
 // down to 2^-16 of the first unit's; products up to 2^15), middles times 2^8 (up to 2^15).
-constexpr float kAttendUpP = 6.f, kAttendUpScale = 0.25f, kAttendUpMiddle = 256.f;
+constexpr float kAttendUpP = 6.f, kAttendUpPFactor = 64.f, kAttendUpScale = 0.25f, kAttendUpMiddle = 256.f;
 constexpr int kAttendStages = 4;
 constexpr float kTwo9 = 512.f, kTwoM24 = 5.9604644775390625e-8f;
 
@@ -136,7 +138,7 @@ template <int HD, int NT, bool kSplit>
 struct AttendSmem {
     static constexpr int kRows = 8 * NT, kGroups = HD / kKv4Group, kTerms = kSplit ? 2 : 1, kAttendWarps = attend_warps(NT);
     uint2 q[HD / 16][NT][kTerms][32];              // B fragments
-    uint2 qsum[NT][32];                            // sums of the groups' (scaled) entries as a B fragment, bf16: k = 4 term + group
+    uint2 qsum[NT][32];                            // sums of the groups' (scaled) entries as a B fragment, bf16: k = 4 term + group; kSplit: fp32 [group][row]
     float qc[kRows];                               // what a row's scores are multiplied with
     int horizon[kRows];                            // last visible position; -1 for a row that is none
     float ref[kAttendWarps][kRows], sum[kAttendWarps][kRows];
@@ -234,6 +236,7 @@ __global__ void __launch_bounds__(32 * attend_warps(NT), attend_ctas_per_sm(NT))
     constexpr int kAttendWarps = SM::kAttendWarps, kAttendThreads = 32 * kAttendWarps;
     extern __shared__ __align__(16) unsigned char smem_raw[];
     SM& sm = *reinterpret_cast<SM*>(smem_raw);
+    float* const qsums = reinterpret_cast<float*>(sm.qsum);
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
     const int G = a.Hq / a.w.Hkv;
     pdl_launch_dependents();
@@ -307,18 +310,20 @@ __global__ void __launch_bounds__(32 * attend_warps(NT), attend_ctas_per_sm(NT))
 #pragma unroll
             for (int i = 0; i < kE; ++i) {
                 const int d = lane * kE + i, grp = d / 32, tt = d % 32 / 8, p = d % 8;
-                // the odd nibbles come in as 16 codes
+                // the odd nibbles come in as 16 codes, unless codes are centred
                 uint32_t hi, lo;
-                const float qs = x[i] * up0 * up1, down = p & 1 ? 0.0625f : 1.f;
+                const float qs = x[i] * up0 * up1, down = !kSplit && (p & 1) ? 0.0625f : 1.f;
                 attend_split(qs * down, 0.f, hi, lo);
-                part += (kSplit ? f16_lo(hi) + f16_lo(lo) : f16_lo(hi)) * (p & 1 ? 16.f : 1.f);
+                part += kSplit ? f16_lo(hi) + f16_lo(lo) : f16_lo(hi) * (p & 1 ? 16.f : 1.f);
                 uint16_t* dst = reinterpret_cast<uint16_t*>(&sm.q[2 * grp + (p >> 1 & 1)][row / 8][0][row % 8 * 4 + tt]) + 2 * (p & 1) + (p >> 2);
                 dst[0] = (uint16_t)hi;
                 if (kSplit) dst[32 * 4] = (uint16_t)lo;
             }
 #pragma unroll
             for (int o = 1; o < 32 / kGroups; o <<= 1) part += __shfl_xor_sync(0xffffffffu, part, o);
-            if (lane % (32 / kGroups) == 0) {
+            if (kSplit) {
+                if (lane % (32 / kGroups) == 0) qsums[lane / (32 / kGroups) * kRows + row] = part * (1.f / kTwo9);       // (as the centred codes are)
+            } else if (lane % (32 / kGroups) == 0) {
                 // k = 4 term + group sits in lane 4 (row % 8) + k % 8 / 2, register k / 8, half k % 2; groups that are none and the
                 // fourth term are 0
                 const int grp = lane / (32 / kGroups);
@@ -335,7 +340,7 @@ __global__ void __launch_bounds__(32 * attend_warps(NT), attend_ctas_per_sm(NT))
                 }
             }
             if (lane == 0) {
-                sm.qc[row] = ldexpf(a.scale, e - 15 + 24);
+                sm.qc[row] = ldexpf(a.scale, e - 15 + (kSplit ? 9 : 24));
                 sm.horizon[row] = row < n_rows ? base + rho / G : -1;
             }
         }
@@ -393,7 +398,7 @@ __global__ void __launch_bounds__(32 * attend_warps(NT), attend_ctas_per_sm(NT))
             const float vmax = fmaxf(fmaxf(fabsf(vs[0]), fabsf(vs[1])), fmaxf(fabsf(vm[0]), fabsf(vm[1])));
             // ---- scores relative to the rows' references: [2 keys][2 rows] of each tile of 8 rows
             uint4 zf;                              // zeros of both keys: groups 2 (t % 2), + 1
-            {
+            if (!kSplit) {
                 const bool odd = kGroups == 4 && (t & 1);
                 zf.x = __byte_perm(odd ? ksz[0][kGroups - 2] : ksz[0][0], odd ? ksz[0][kGroups - 1] : ksz[0][1], 0x7632);
                 zf.y = __byte_perm(odd ? ksz[1][kGroups - 2] : ksz[1][0], odd ? ksz[1][kGroups - 1] : ksz[1][1], 0x7632);
@@ -404,7 +409,9 @@ __global__ void __launch_bounds__(32 * attend_warps(NT), attend_ctas_per_sm(NT))
             float s[NT][4];
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
-                {
+                if (kSplit) {
+                    s[nt][0] = s[nt][1] = s[nt][2] = s[nt][3] = 0.f;
+                } else {
                     const uint2 b = sm.qsum[nt][lane];
                     attend_mma_first<true>(s[nt], zf, b.x, b.y);
                 }
@@ -416,6 +423,7 @@ __global__ void __launch_bounds__(32 * attend_warps(NT), attend_ctas_per_sm(NT))
                     for (int h = 0; h < 2; ++h) {
                         const uint32_t w0 = kw[0][grp] >> (8 * h), w1 = kw[1][grp] >> (8 * h);
                         af[h] = make_uint4(w0 & 0x000f000fu, w1 & 0x000f000fu, w0 & 0x00f000f0u, w1 & 0x00f000f0u);
+                        if (kSplit) af[h] = make_uint4(attend_centre<false>(af[h].x), attend_centre<false>(af[h].y), attend_centre<true>(af[h].z), attend_centre<true>(af[h].w));
                     }
 #pragma unroll
                     for (int i = 0; i < 2 * kTerms; ++i) {     // the small terms first: the sum is truncated at every step
@@ -424,6 +432,12 @@ __global__ void __launch_bounds__(32 * attend_warps(NT), attend_ctas_per_sm(NT))
                         else attend_mma(acc, af[i % 2], b.x, b.y);
                     }
                     const float s0 = bf16_lo(ksz[0][grp]), s1 = bf16_lo(ksz[1][grp]);
+                    if (kSplit) {                  // the middles, z + 8 s
+                        const float2 b = *reinterpret_cast<const float2*>(&qsums[grp * kRows + nt * 8 + 2 * t]);
+                        const float m0 = fmaf(8.f, s0, bf16_hi(ksz[0][grp])), m1 = fmaf(8.f, s1, bf16_hi(ksz[1][grp]));
+                        s[nt][0] = fmaf(m0, b.x, s[nt][0]); s[nt][1] = fmaf(m0, b.y, s[nt][1]);
+                        s[nt][2] = fmaf(m1, b.x, s[nt][2]); s[nt][3] = fmaf(m1, b.y, s[nt][3]);
+                    }
                     s[nt][0] = fmaf(s0, acc[0], s[nt][0]); s[nt][1] = fmaf(s0, acc[1], s[nt][1]);
                     s[nt][2] = fmaf(s1, acc[2], s[nt][2]); s[nt][3] = fmaf(s1, acc[3], s[nt][3]);
                 }
@@ -487,7 +501,7 @@ __global__ void __launch_bounds__(32 * attend_warps(NT), attend_ctas_per_sm(NT))
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) p[nt][i] = attend_exp2(s[nt][i] + kAttendUpP);
+                for (int i = 0; i < 4; ++i) p[nt][i] = kSplit ? attend_exp2(s[nt][i]) * kAttendUpPFactor : attend_exp2(s[nt][i] + kAttendUpP);
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const uint32_t hi = attend_pack(p[nt][2 * i], p[nt][2 * i + 1]);

@@ -259,6 +259,16 @@ def test_attend_large(new, base, heads, kvh, hd):
         assert torch.equal(out, cache.attend(q, *where))                     # the same bits every time
 
 
+@pytest.mark.parametrize("new,base,heads,kvh,hd", [([1], [15], 8, 8, 128), ([1], [16000], 32, 8, 128), ([2, 9, 5], [4000, 500, 1], 32, 8, 128), ([17, 3], [700, 3000], 8, 8, 64)])
+def test_attend_fp32_keeps_what_fp32_has(new, base, heads, kvh, hd):
+    """Half steps of 22 bits (2^-23) for P, P s and the middles, twice that for Q's in scores of up to 2, an exponential off by 2^-22 at an
+    argument of up to 16 (half a step 2^-21, times ln 2): 2^-20 together, in the norm."""
+    import torch
+    cache, where, q, out, want = _big(sum(new), new, base, heads, kvh, hd, torch.float32)
+    rel = ((out.double() - want).norm() / want.norm()).item()
+    assert rel < 2.0 ** -20, rel
+
+
 def test_attend_strides_streams_and_graphs():
     import torch
     cache, where, q, out, _ = _big(3, [9, 1, 4], [700, 30, 2000], 16, 4, 128, torch.bfloat16)
