@@ -1068,7 +1068,9 @@ constexpr int kAcceptBatch = 8;                    // steps of 32 ids whose load
 // a CTA, one to an SM, and the whole range walked again, 310 rows of 128256 ids for 32 requests took 151 us, rows included; so 143.
 template <int kAcceptCluster, typename T>
 __global__ void __launch_bounds__(kAcceptThreads, 2) accept_shaped_kernel(const AcceptArgs a) {
+    cluster_started_arrive();                      // (totals are stored into the other CTAs below)
     pdl_wait();                                    // launched with programmatic serialisation: the shapes must be there
+    cluster_started_wait();
     constexpr int kWarps = kAcceptThreads / 32;
     const int req = blockIdx.y, rank = (int)cluster_ctarank(), tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     __shared__ int s_first;

@@ -364,3 +364,29 @@ def test_sample_windows_that_overflow_their_lists(vocab):
             y = logits.to(dtype)
             tokens = binding.sample(y, binding.shaping(n, temperature=t, top_k=k, top_p=p, min_p=m), _cuda(u), probs=probs)
             _check(y.float().cpu().numpy(), s, u, tokens.cpu().numpy(), probs.cpu().numpy())
+
+
+@pytest.mark.parametrize("n", [20, 60, 300])          # clusters of eight, four and two CTAs per request
+def test_accept_of_tiny_vocabularies_beside_other_work(n):
+    """Most warps have no ids, so that totals cross the cluster at once, while another stream keeps the SMs busy."""
+    import torch
+    from paper_2605_13319_b200 import binding
+    rng = np.random.default_rng(n)
+    ks, V = [int(k) for k in rng.integers(0, 4, n)], 16
+    logits, q, drafts, u = _rounds(rng, ks, V, 0.7)
+    row0 = np.concatenate([[0], np.cumsum(np.array(ks) + 1)]).astype(np.int32)
+    shaping = binding.shaping(n, temperature=0.9)
+    args = [_cuda(logits), _cuda(row0), shaping, _cuda(q), _cuda(drafts), _cuda(u)]
+    busy, busy_u, side = torch.randn((200, 32000), device="cuda"), torch.rand(200, device="cuda"), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    got = []
+    for _ in range(20):
+        binding.sample(busy, binding.shaping(200, top_p=0.9), busy_u, stream=side)
+        got.append(binding.accept(*args))
+    torch.cuda.synchronize()
+    for a, b in got:
+        assert torch.equal(a, got[0][0]) and torch.equal(b, got[0][1])
+    for r in range(n):
+        a, b, first = row0[r], row0[r + 1], row0[r] - r
+        want = serving.accept(logits[a:b], (0.9, 0, 1.0, 0.0), q[first:first + ks[r]], drafts[first:first + ks[r]], u[a:b])
+        assert (got[0][0][r].item(), got[0][1][r].item()) == want[:2] or want[2] < NEAR, (r, want)
