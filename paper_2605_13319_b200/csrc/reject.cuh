@@ -114,7 +114,9 @@ __global__ void __launch_bounds__(kSampleThreads) accept_sample_kernel(const flo
                                                                        const float* __restrict__ u_all,
                                                                        RejectOut* __restrict__ out,
                                                                        ReqState* __restrict__ req_state) {
+    cluster_started_arrive();     // (totals are stored into the other CTAs below)
     pdl_wait();      // launched with programmatic serialisation: the row statistics must be complete
+    cluster_started_wait();
     const int item = blockIdx.y, rank = (int)cluster_ctarank();
     const RejectItem it = items[item];
     if (it.mode == 2) return;                     // the whole cluster (one request) leaves together

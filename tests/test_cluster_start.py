@@ -19,7 +19,7 @@ def _kernel(file, name):
     return text[start:end if end >= 0 else len(text)]
 
 
-@pytest.mark.parametrize("file,name", [("serving/shape.cuh", "accept_shaped_kernel")])
+@pytest.mark.parametrize("file,name", [("serving/shape.cuh", "accept_shaped_kernel"), ("reject.cuh", "accept_sample_kernel")])
 def test_a_cluster_has_started_before_it_is_written_to(file, name):
     body = _kernel(file, name)
     remote, barrier = REMOTE.search(body), BARRIER.search(body)
