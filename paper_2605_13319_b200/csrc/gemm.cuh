@@ -256,6 +256,7 @@ __global__ void __launch_bounds__(kGemmThreads, kGemmCtasPerSm) gemm_wstream_ker
         fence_mbar_init();
     }
     __syncthreads();
+    if (a.S > 1) cluster_started_arrive();            // (partial tiles are stored into the other CTAs below)
     pdl_launch_dependents();
 
     // epilogue inputs that live in global memory are fetched right after the dependency wait, long before the
@@ -325,6 +326,7 @@ __global__ void __launch_bounds__(kGemmThreads, kGemmCtasPerSm) gemm_wstream_ker
             }
         }
         __syncwarp();
+        if (a.S > 1) cluster_started_wait();          // (every arrival is waited for)
     } else {
         // ---------------- consumers: warp w owns row tiles 2w and 2w+1 of the block
         if ((MODE == kResid || MODE == kQkvRope) && prefetch) {
@@ -406,6 +408,7 @@ __global__ void __launch_bounds__(kGemmThreads, kGemmCtasPerSm) gemm_wstream_ker
         // buffer: token-major rows of 16 floats, as the epilogue reads them.
         const int g = lane >> 2, t = lane & 3;
         const uint32_t recv_a = smem_u32(recv);
+        if (a.S > 1) cluster_started_wait();
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             const int tile = warp * 2 + j, owner = tile % a.S, q = tile / a.S;

@@ -19,7 +19,8 @@ def _kernel(file, name):
     return text[start:end if end >= 0 else len(text)]
 
 
-@pytest.mark.parametrize("file,name", [("serving/shape.cuh", "accept_shaped_kernel"), ("reject.cuh", "accept_sample_kernel")])
+@pytest.mark.parametrize("file,name", [("serving/shape.cuh", "accept_shaped_kernel"), ("reject.cuh", "accept_sample_kernel"),
+                                       ("gemm.cuh", "gemm_wstream_kernel"), ("gemm_dense.cuh", "gemm_dense_kernel")])
 def test_a_cluster_has_started_before_it_is_written_to(file, name):
     body = _kernel(file, name)
     remote, barrier = REMOTE.search(body), BARRIER.search(body)
@@ -27,4 +28,4 @@ def test_a_cluster_has_started_before_it_is_written_to(file, name):
     # a thread that waits has arrived, and whoever arrives waits: no return between the two
     arrive = body.find("cluster_started_arrive()")
     if arrive >= 0:
-        assert arrive < barrier.start() and "return" not in body[arrive:barrier.start()]
+        assert arrive < barrier.start() and "return;" not in body[arrive:barrier.start()]
