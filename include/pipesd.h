@@ -339,7 +339,8 @@ int32_t pipesd_sample(const void *logits, int32_t dtype, int64_t row_stride, int
  * between rows; both have rows - n_req entries and may be null where that is 0).  u: [rows], per request k acceptance tests and
  * the final draw.  shaping: [n_req].  A draft x is accepted while u < min(1, p(x) / q(x)); a correction comes from norm(max(0, p - q)),
  * from p where that is 0 everywhere.  A row that has no distribution (see pipesd_sample) accepts nothing and gives next_token -1;
- * so does a request whose row0 entries make no sense.  scratch: pipesd_accept_scratch_bytes(rows) bytes, 8-byte aligned, one for
+ * so does a request whose row0 entries make no sense: not 0 <= row0[r] - r, row0[r] < row0[r+1] <= rows with its drafts inside of q, or
+ * an entry before row0[r] larger than it.  scratch: pipesd_accept_scratch_bytes(rows) bytes, 8-byte aligned, one for
  * each of calls that may run at the same time. */
 uint64_t pipesd_accept_scratch_bytes(int32_t rows);
 int32_t pipesd_accept(const void *logits, int32_t dtype, int64_t row_stride, int32_t n_req, int32_t rows, int32_t vocab,

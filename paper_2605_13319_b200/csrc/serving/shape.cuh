@@ -1028,14 +1028,19 @@ __global__ void __launch_bounds__(kShapeThreads, 2) shape_kernel(const ShapeArgs
         shape_row<C, true, T, VEC>(lr, a.V, a.shaping[row], a.u[row], a.tokens + row, a.probs ? a.probs + (size_t)row * a.probs_stride : nullptr,
                                    nullptr, sm);
     } else {
+        // The lowest of the requests that claim the row (several may, where entries of row0 make no sense): the one that acceptance looks at,
+        // if there is one, and the same in all CTAs of the cluster, whose barriers go by its settings.
         __shared__ int s_req;
-        if (threadIdx.x == 0) s_req = -1;
+        if (threadIdx.x == 0) s_req = a.n_req;
         __syncthreads();
         for (int i = threadIdx.x; i < a.n_req; i += kShapeThreads)
-            if (a.row0[i] <= row && row < a.row0[i + 1]) s_req = i;
+            if (a.row0[i] <= row && row < a.row0[i + 1]) {
+                atomicMin(&s_req, i);
+                break;
+            }
         __syncthreads();
-        const int req = s_req;                     // (-1: a row that is no request's)
-        if (req >= 0) shape_row<C, false, T, VEC>(lr, a.V, a.shaping[req], 0.f, nullptr, nullptr, a.shapes + row, sm);
+        const int req = s_req;                     // (n_req: a row that is no request's)
+        if (req < a.n_req) shape_row<C, false, T, VEC>(lr, a.V, a.shaping[req], 0.f, nullptr, nullptr, a.shapes + row, sm);
     }
     // What follows may begin to launch, and waits for this grid before it reads.  (A grid of the rest of a call's rows runs beside the one
     // before it, and ends after it.)
@@ -1076,7 +1081,12 @@ __global__ void __launch_bounds__(kAcceptThreads, 2) accept_shaped_kernel(const 
     __shared__ int s_first;
     __shared__ double s_warp[kWarps], s_incl[kWarps], s_cta[2][kAcceptCluster], s_base, s_total;
     const int first = a.row0[req], end = a.row0[req + 1];
-    const bool sane = first >= req && end > first && end <= a.rows && end - req - 1 <= a.rows - a.n_req;       // (its drafts are there too)
+    // A request whose entries make sense: rows and drafts that are there, and no entry of an earlier request behind its first row, so that no
+    // two such requests share a row.
+    bool later = false;
+    for (int i = tid; i < req; i += kAcceptThreads) later |= a.row0[i] > first;
+    if (tid == 0) s_first = a.rows;
+    const bool sane = !__syncthreads_or(later) && first >= req && end > first && end <= a.rows && end - req - 1 <= a.rows - a.n_req;
     const int k = sane ? end - first - 1 : 0, slot0 = sane ? first - req : 0;     // slot0: of the request's first draft
     if (!sane) {                                   // no such rows (the whole cluster leaves)
         if (rank == 0 && tid == 0) { a.n_accepted[req] = 0; a.next_token[req] = -1; }
@@ -1087,8 +1097,6 @@ __global__ void __launch_bounds__(kAcceptThreads, 2) accept_shaped_kernel(const 
         const float l = logit_f32(row[id]);
         return shape_keeps(l, id, r) ? __dmul_rn(shape_exp2(shape_exponent(l, r)), scale) : 0.0;       // (no contraction: the same in every pass)
     };
-    if (tid == 0) s_first = k;
-    __syncthreads();
     for (int i = tid; i < k; i += kAcceptThreads) {
         const RowShape r = a.shapes[first + i];
         const int x = a.drafts[slot0 + i];
@@ -1102,7 +1110,7 @@ __global__ void __launch_bounds__(kAcceptThreads, 2) accept_shaped_kernel(const 
         if (!ok) atomicMin(&s_first, i);
     }
     __syncthreads();
-    const int n = s_first;
+    const int n = min(s_first, k);
     const RowShape r = a.shapes[first + n];
     const float uk = a.u[first + k];
     if (r.total == 0 || !(uk >= 0.f && uk < 1.f)) {

@@ -390,3 +390,41 @@ def test_accept_of_tiny_vocabularies_beside_other_work(n):
         a, b, first = row0[r], row0[r + 1], row0[r] - r
         want = serving.accept(logits[a:b], (0.9, 0, 1.0, 0.0), q[first:first + ks[r]], drafts[first:first + ks[r]], u[a:b])
         assert (got[0][0][r].item(), got[0][1][r].item()) == want[:2] or want[2] < NEAR, (r, want)
+
+
+@pytest.mark.parametrize("n", [3, 20, 45, 120])
+def test_accept_where_entries_of_row0_make_no_sense(n):
+    """Every request with settings of its own: those whose entries make sense get what they would get alone, the others (0, -1), however
+    many of them claim a row.  Rows go by clusters and by single CTAs, requests by clusters of eight, four and two."""
+    import torch
+    from paper_2605_13319_b200 import binding
+    rng = np.random.default_rng(n)
+    V, rows = 17000, 4 * n
+    logits = (rng.standard_normal((rows, V)) * 2).astype(np.float32)
+    q = np.full((rows - n, V), 2e-5, np.float32)
+    drafts = rng.integers(0, V, rows - n).astype(np.int32)
+    u = (rng.integers(0, 1 << 24, rows) * 2.0 ** -24).astype(np.float32)
+    t, k, p, m = (rng.choice(v, n) for v in ([0.0, 1.0, 0.7], [0, 0, 1, 40, 3000], [1.0, 0.9, 0.3], [0.0, 0.1]))
+    settings = [v.astype(d) for v, d in ((t, np.float32), (k, np.int32), (p, np.float32), (m, np.float32))]
+    shaping = binding.shaping(n, temperature=settings[0], top_k=settings[1], top_p=settings[2], min_p=settings[3])
+    good = np.arange(0, rows + 1, 4).astype(np.int32)
+    for trial in range(6):
+        row0 = good.copy()
+        if trial == 1:                                   # many requests claim the rows of others
+            row0[2::2] = 0
+        elif trial == 2:
+            row0[1:n:3] = rows
+        elif trial == 3:
+            row0[n // 2] = -7
+        elif trial == 4:
+            row0 = rng.integers(0, rows + 1, n + 1).astype(np.int32)
+        elif trial == 5:
+            row0 = rng.permutation(good)
+        got, token = (x.tolist() for x in binding.accept(_cuda(logits), _cuda(row0), shaping, _cuda(q), _cuda(drafts), _cuda(u)))
+        for r in range(n):
+            a, b, first = int(row0[r]), int(row0[r + 1]), int(row0[r]) - r
+            if not (0 <= first and a < b <= rows and b - r - 1 <= rows - n and (row0[:r] <= a).all()):
+                assert (got[r], token[r]) == (0, -1), (trial, r)
+            elif rng.random() < 30 / n:
+                want = serving.accept(logits[a:b], [v[r] for v in settings], q[first:first + b - a - 1], drafts[first:first + b - a - 1], u[a:b])
+                assert (got[r], token[r]) == want[:2] or want[2] < NEAR, (trial, r, want)
