@@ -338,7 +338,9 @@ int32_t pipesd_sample(const void *logits, int32_t dtype, int64_t row_stride, int
  * request r is drafts[row0[r] - r + i], the distribution that it was drawn from row row0[r] - r + i of q (fp32, q_stride elements
  * between rows; both have rows - n_req entries and may be null where that is 0).  u: [rows], per request k acceptance tests and
  * the final draw.  shaping: [n_req].  A draft x is accepted while u < min(1, p(x) / q(x)); a correction comes from norm(max(0, p - q)),
- * from p where that is 0 everywhere.  A row that has no distribution (see pipesd_sample) accepts nothing and gives next_token -1;
+ * from p where that is 0 everywhere.  A row that has no distribution (see pipesd_sample) accepts nothing and gives next_token -1.
+ * A draft that is no id, or whose u lies outside [0, 1), or whose q is a NaN or below 0 is not accepted; a correction from a row of q with
+ * such an entry at a kept id, or with a last u outside [0, 1), is next_token -1;
  * so does a request whose row0 entries make no sense: not 0 <= row0[r] - r, row0[r] < row0[r+1] <= rows with its drafts inside of q, or
  * an entry before row0[r] larger than it.  scratch: pipesd_accept_scratch_bytes(rows) bytes, 8-byte aligned, one for
  * each of calls that may run at the same time. */

@@ -70,9 +70,11 @@ def accept(logits, settings, q, drafts, u):
             ratio = min(P[x] / qx if qx > 0 else (np.inf if P[x] > 0 else 0.0), 1.0)
             if ratio < 1:
                 margin = min(margin, abs(float(u[i]) - ratio))
-            if float(u[i]) < ratio:
+            if qx >= 0 and 0 <= float(u[i]) < ratio:
                 continue
-        rest = np.maximum(P - np.asarray(q[i], np.float64), 0.0)
+        if not (np.asarray(q[i])[P > 0] >= 0).all():
+            return i, -1, margin
+        rest = np.maximum(P - np.asarray(q[i], np.float64), 0.0, where=P > 0, out=np.zeros_like(P))
         if rest.sum() > 0:
             P = rest
         break

@@ -1104,8 +1104,8 @@ __global__ void __launch_bounds__(kAcceptThreads, 2) accept_shaped_kernel(const 
         if (r.total && x >= 0 && x < a.V) {
             const double p = prob(logits + (size_t)i * a.stride, r, x, kMassOne / (double)r.total);
             const double q = (double)a.q[(size_t)(slot0 + i) * a.q_stride + x];
-            const double ratio = q > 0.0 ? p / q : (p > 0.0 ? INFINITY : 0.0);
-            ok = (double)a.u[first + i] < fmin(ratio, 1.0);
+            const double ratio = q > 0.0 ? p / q : (p > 0.0 ? INFINITY : 0.0), ui = (double)a.u[first + i];
+            ok = q >= 0.0 && ui >= 0.0 && ui < fmin(ratio, 1.0);         // (no NaN, and nothing below 0)
         }
         if (!ok) atomicMin(&s_first, i);
     }
@@ -1146,7 +1146,8 @@ __global__ void __launch_bounds__(kAcceptThreads, 2) accept_shaped_kernel(const 
 #pragma unroll
         for (int i = 0; i < kAcceptBatch; ++i) w[i] = __dmul_rn(shape_exp2(shape_exponent(keep[i] ? l[i] : r.cut, r)), scale);
 #pragma unroll
-        for (int i = 0; i < kAcceptBatch; ++i) t[i] = keep[i] ? fmax(0.0, w[i] - (double)q[i]) : 0.0;
+        for (int i = 0; i < kAcceptBatch; ++i)     // (a q that is no probability makes the sum a NaN)
+            t[i] = !keep[i] ? 0.0 : q[i] >= 0.f ? fmax(0.0, w[i] - (double)q[i]) : (double)NAN;
     };
     for (int attempt = 0; attempt < 2; ++attempt) {
         double sum = 0.0, batch_sum = 0.0;         // lane b: the sum of batch b
@@ -1189,6 +1190,10 @@ __global__ void __launch_bounds__(kAcceptThreads, 2) accept_shaped_kernel(const 
         }
         __syncthreads();
         const double total = s_total;
+        if (!(total < INFINITY)) {                 // a NaN, or below 0, among the q of the row: nothing to draw from
+            if (rank == 0 && tid == 0) { a.n_accepted[req] = n; a.next_token[req] = -1; }
+            return;
+        }
         if (use_q && !(total > 0.0)) {             // P <= q everywhere: the draw is from P
             use_q = false;
             __syncthreads();

@@ -428,3 +428,38 @@ def test_accept_where_entries_of_row0_make_no_sense(n):
             elif rng.random() < 30 / n:
                 want = serving.accept(logits[a:b], [v[r] for v in settings], q[first:first + b - a - 1], drafts[first:first + b - a - 1], u[a:b])
                 assert (got[r], token[r]) == want[:2] or want[2] < NEAR, (trial, r, want)
+
+
+@pytest.mark.parametrize("vocab", [40, 32000])
+def test_accept_where_q_or_u_are_no_probabilities(vocab):
+    """Every request has a result: NaN, infinities and numbers below 0 at the draft's q, elsewhere in its row, and among the uniforms."""
+    import torch
+    from paper_2605_13319_b200 import binding
+    rng = np.random.default_rng(vocab)
+    n = 24
+    logits, q, drafts, u = _rounds(rng, [2] * n, vocab, 0.3)
+    at_draft = [np.nan, -1.0, -np.inf, np.inf, -0.0, 0.0]
+    for r, v in enumerate(at_draft):                                 # the first draft's own
+        q[2 * r, drafts[2 * r]] = v
+    for r, v in enumerate([np.nan, -0.25, -np.inf, np.inf]):         # the whole row of a draft that is not accepted
+        q[2 * (6 + r)] = v
+        drafts[2 * (6 + r)] = -1
+    for r, v in enumerate([np.nan, -np.inf]):                        # one entry that top-k cuts, and one that it keeps
+        worst, best = logits[3 * (10 + r)].argmin(), logits[3 * (10 + r)].argmax()
+        q[2 * (10 + r), worst if r == 0 else best] = v
+        drafts[2 * (10 + r)] = vocab
+    for r, v in enumerate([np.nan, -0.5, -np.inf, 1.0, 2.0, np.inf]):        # a test's uniform
+        u[3 * (12 + r)] = v
+    for r, v in enumerate([np.nan, -0.5, 1.0, np.inf]):              # the last one
+        u[3 * (18 + r) + 2] = v
+    row0 = np.arange(0, 3 * n + 1, 3).astype(np.int32)
+    for k in (0, 10):
+        got, token = (x.tolist() for x in binding.accept(_cuda(logits), _cuda(row0), binding.shaping(n, top_k=k), _cuda(q), _cuda(drafts), _cuda(u)))
+        for r in range(n):
+            want = serving.accept(logits[3 * r:3 * r + 3], (1.0, k, 1.0, 0.0), q[2 * r:2 * r + 2], drafts[2 * r:2 * r + 2], u[3 * r:3 * r + 3])
+            assert (got[r], token[r]) == want[:2] or want[2] < NEAR, (k, r, want)
+            if r in (0, 1, 2, 3, 6, 7, 8, 9, 10, 11) or 12 <= r < 18:
+                assert got[r] == 0
+            if r in (6, 7, 8, 11) or 18 <= r < 22:
+                assert token[r] == -1
+        assert token[10] == -1 if k == 0 else token[10] >= 0
