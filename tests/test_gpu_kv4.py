@@ -430,3 +430,29 @@ def test_exact_ties_of_codes():
             want = (torch.round(q).clamp(0, 15) * (s > 0) * s + z).flatten(-2).float()
             assert all(torch.equal(y, want) for y in cache.read(n, *where))
         assert ties > 100 or dtype == torch.float32
+
+
+@pytest.mark.parametrize("hd,heads,kvh", [(64, 4, 1), (128, 2, 2), (128, 8, 2)])
+def test_attend_queries_that_are_no_numbers(hd, heads, kvh):
+    """A NaN or an infinity in a query makes its row of its head a NaN, and nothing else."""
+    import torch
+    rng = np.random.default_rng(hd + heads)
+    c = Case(rng, [5, 2], [90, 33], kvh, hd)
+    c.fill(rng)
+    k, v = (_rows(rng, c.rows, kvh, hd, torch.float32) for _ in range(2))
+    c.cache.append(k, v, *c.where)
+    c.write_ref(k.double().cpu().numpy(), v.double().cpu().numpy())
+    for dtype in (torch.bfloat16, torch.float32):
+        q = _rows(rng, c.rows, heads, hd, dtype)
+        clean = c.cache.attend(q, *c.where)
+        _attend_check(c, q, hd ** -0.5, clean)
+        bad = {(0, 0): float("nan"), (2, 1): float("inf"), (4, heads - 1): float("-inf"), (6, 0): float("nan")}
+        x = q.clone()
+        for (row, head), value in bad.items():
+            x[row, head, rng.integers(hd)] = value
+        x[4, heads - 1, :2] = float("inf")
+        out = c.cache.attend(x, *c.where)
+        for (row, head) in bad:
+            assert out[row, head].isnan().all()
+            out[row, head] = clean[row, head]
+        _attend_check(c, q, hd ** -0.5, out)

@@ -463,3 +463,30 @@ def test_accept_where_q_or_u_are_no_probabilities(vocab):
             if r in (6, 7, 8, 11) or 18 <= r < 22:
                 assert token[r] == -1
         assert token[10] == -1 if k == 0 else token[10] >= 0
+
+
+@pytest.mark.parametrize("n,vocab", [(20, 128256), (60, 32000), (60, 128256), (200, 32000), (200, 128256), (80, 1 << 18)])
+def test_accept_of_many_requests_over_whole_vocabularies(n, vocab):
+    """Clusters of eight, four and two CTAs per request, up to 32 batches of ids for a warp."""
+    import torch
+    from paper_2605_13319_b200 import binding
+    rng = np.random.default_rng(n + vocab)
+    g = torch.Generator("cuda").manual_seed(n)
+    ks = rng.integers(0, 4, n) if vocab < 1 << 18 else np.ones(n, int)
+    row0 = np.concatenate([[0], np.cumsum(ks + 1)]).astype(np.int32)
+    rows = int(row0[-1])
+    settings = _settings(rng, n, vocab)
+    settings[0][settings[0] == np.float32(1e-6)] = 1.0
+    shaping = binding.shaping(n, temperature=settings[0], top_k=settings[1], top_p=settings[2], min_p=settings[3])
+    u = (rng.integers(0, 1 << 24, rows) * 2.0 ** -24).astype(np.float32)
+    scored = np.setdiff1d(np.arange(rows), row0[1:] - 1)
+    for dtype in (torch.float32, torch.bfloat16):
+        logits = (torch.randn((rows, vocab), generator=g, device="cuda") * 2).to(dtype)
+        q = torch.softmax(logits[torch.from_numpy(scored).cuda()].float() + torch.randn((rows - n, vocab), generator=g, device="cuda"), 1)
+        drafts = torch.multinomial(q, 1, generator=g)[:, 0].int()
+        got, token = binding.accept(logits, _cuda(row0), shaping, q, drafts, _cuda(u))
+        for r in rng.permutation(n)[:8]:
+            a, b, first = int(row0[r]), int(row0[r + 1]), int(row0[r] - r)
+            mine = slice(first, first + int(ks[r]))
+            want = serving.accept(logits[a:b].float().cpu().numpy(), [v[r] for v in settings], q[mine].cpu().numpy(), drafts[mine].cpu().numpy(), u[a:b])
+            assert (got[r].item(), token[r].item()) == want[:2] or want[2] < NEAR, (r, want)
