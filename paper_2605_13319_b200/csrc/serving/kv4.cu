@@ -64,6 +64,12 @@ bool device_ready() {
 // requests of 2000 to 4000 positions, 32 heads of 128; bf16, fp32): 4 rows 45 58, 56 80; 9 rows 77 66, 99 87; 17 rows 110 115, 142 158; over 8 KV
 // heads: 36 rows 54 53, 68 70; 68 rows 87 80, 112 107.
 int attend_row_tiles(int64_t rows) { return (rows + 15) / 16 * 16 * 5 <= (rows + 7) / 8 * 8 * 6 ? 2 : 1; }
+// That where there is work for the CTAs of two: `units` of the page table (what the host knows of the lengths) times the row groups that read each,
+// `rows` of a KV head in the mean.  us with one and two tiles, bf16, one request, by units * groups: 9 rows of 32 heads behind 2048 positions
+// (8 thousand) 25 29; behind 8192 (33) 39 39; behind 16384 (66) 57 51; 9 rows over 8 heads behind 16384 (41) 43 47; 64 rows of 32 heads behind
+// 2048 (34) 39 41; 128 rows (70) 61 55; prompts of 512 rows (66) 78 68, of 2000 (1000) 620 430.
+constexpr int64_t kAttendTwoTiles = 49152;
+int attend_tiles(int64_t units, int64_t rows) { return units * ((rows + 7) / 8) < kAttendTwoTiles ? 1 : attend_row_tiles(rows); }
 
 template <int HD, typename T>
 int32_t attend_run(Kv4AttendArgs& a, int nt, cudaStream_t st) {
@@ -149,10 +155,8 @@ int32_t pipesd_kv4_attend(const pipesd_kv4_cfg* cfg, const void* pool, const voi
     a.Hq = n_q_heads;
     a.scale = scale * 1.4426950408889634f;
     a.parts = static_cast<float*>(scratch);
-    // two tiles where the rows suit them and there is work for all CTAs: the page table bounds it (1 request, 2048 positions, 32 heads, 9 rows:
-    // 19 us with one, 23 with two)
-    const int64_t most = (int64_t)n_req * cfg->max_pages * (cfg->page_size / kKv4Unit) * cfg->n_kv_heads;
-    const int nt = most < 16384 ? 1 : attend_row_tiles((int64_t)(rows + n_req - 1) / n_req * (n_q_heads / cfg->n_kv_heads));      // rows in the mean
+    const int nt = attend_tiles((int64_t)n_req * cfg->max_pages * (cfg->page_size / kKv4Unit) * cfg->n_kv_heads,
+                                (int64_t)(rows + n_req - 1) / n_req * (n_q_heads / cfg->n_kv_heads));
     a.rows_cap = 8 * nt;
     a.ctas = kAttendSms * attend_ctas_per_sm(nt);
     cudaStream_t st = (cudaStream_t)cuda_stream;

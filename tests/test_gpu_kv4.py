@@ -456,3 +456,84 @@ def test_attend_queries_that_are_no_numbers(hd, heads, kvh):
             assert out[row, head].isnan().all()
             out[row, head] = clean[row, head]
         _attend_check(c, q, hd ** -0.5, out)
+
+
+def _widen(c, units):
+    """The same requests with a page table wide enough for `units` units of all of them."""
+    import torch
+    per = c.page // 16 * c.kvh * len(c.new)
+    wide = np.full((len(c.new), -(-units // per)), -1, np.int32)
+    wide[:, :c.table.shape[1]] = c.table
+    c.table = wide
+    c.where[2] = torch.from_numpy(wide).cuda()
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+@pytest.mark.parametrize("heads,kvh,new,base,page", [
+    (2, 2, [9, 16, 11], [130, 0, 300], 16), (4, 1, [4, 3, 2, 3], [60, 250, 15, 1], 32), (8, 2, [9, 10, 8], [33, 200, 5], 48),
+    (7, 1, [5, 0, 7, 7], [16, 40, 100, 31], 16), (16, 2, [1, 3, 2], [90, 17, 400], 16), (3, 1, [16, 1, 11], [2, 500, 64], 64)])
+def test_attend_two_row_tiles(hd, heads, kvh, new, base, page):
+    """9 to 16, 33 to 48 or many query rows of a KV head in the mean and work for all CTAs, going by the page table: CTAs of two row tiles.
+    Ragged requests, of which one may have fewer rows than a tile, row groups that end inside a tile, units shared by several CTAs."""
+    import torch
+    rng = np.random.default_rng(hd + heads + sum(new) + sum(base))
+    mean = -(-sum(new) // len(new)) * heads // kvh
+    assert -(-mean // 16) * 16 * 5 <= -(-mean // 8) * 8 * 6
+    c = Case(rng, new, base, kvh, hd, page)
+    c.fill(rng)
+    _widen(c, 50000)
+    k, v = (_rows(rng, c.rows, kvh, hd, torch.float32) for _ in range(2))
+    c.cache.append(k, v, *c.where)
+    c.write_ref(k.double().cpu().numpy(), v.double().cpu().numpy())
+    for dtype in (torch.bfloat16, torch.float32):
+        q = _rows(rng, c.rows, heads, hd, dtype, 1.5)
+        out = torch.full_like(q, 7.0)
+        _attend_check(c, q, hd ** -0.5, c.cache.attend(q, *c.where, out=out))
+        x = q.clone()
+        x[1, 0, 3] = float("nan")
+        again = c.cache.attend(x, *c.where)
+        assert again[1, 0].isnan().all()
+        again[1, 0] = out[1, 0]
+        _attend_check(c, q, hd ** -0.5, again)
+
+
+@pytest.mark.parametrize("name,spread", [
+    ("growing scores", _by_position(lambda pos, kv: 1 + 0.03 * pos if kv == 0 else 1.0)),
+    ("growing values", _by_position(lambda pos, kv: 1.0 if kv == 0 else 2.0 ** (pos // 16 * 3 - 30))),
+    ("shrinking values", _by_position(lambda pos, kv: 1.0 if kv == 0 else 2.0 ** (20 - pos // 16 * 3))),
+    ("offset values", lambda rng, r, pos, h, kv: rng.standard_normal(128) * (1.0 if kv == 0 else 0.1) + (0.0 if kv == 0 else 7.0)),
+    ("zero values", lambda rng, r, pos, h, kv: rng.standard_normal(128) * (1 - kv))])
+def test_attend_ranges_of_two_row_tiles(name, spread):
+    import torch
+    rng = np.random.default_rng(len(name))
+    c = Case(rng, [6], [300], 1, 128)
+    c.fill(rng, spread)
+    _widen(c, 50000)
+    k, v = (torch.from_numpy(np.stack([spread(rng, 0, 300 + i, 0, kv) for i in range(6)]).astype(np.float32)[:, None]).cuda() for kv in range(2))
+    c.cache.append(k, v, *c.where)
+    c.write_ref(k.double().cpu().numpy(), v.double().cpu().numpy())
+    for dtype in (torch.bfloat16, torch.float32):
+        for std in (0.01, 2.0, 20.0):
+            q = _rows(rng, 6, 2, 128, dtype, std)                            # 12 query rows
+            _attend_check(c, q, 128 ** -0.5, c.cache.attend(q, *c.where))
+
+
+@pytest.mark.parametrize("new,base,heads,kvh,hd", [
+    ([150, 50], [1200, 3000], 35, 5, 64), ([170], [4000], 33, 11, 128), ([9] * 8, [int(x) for x in np.linspace(500, 4000, 8)], 32, 32, 128), ([700], [0], 32, 8, 128)])
+def test_attend_large_with_two_row_tiles(new, base, heads, kvh, hd):
+    """Also merges whose warps take several heads of a row, and a number of heads that those do not divide.  Bounds as for one row tile."""
+    import torch
+    for dtype, tol in ((torch.bfloat16, 2.0 ** -8), (torch.float32, 2.0 ** -20)):
+        cache, where, q, out, want = _big(sum(new), new, base, heads, kvh, hd, dtype)
+        rel = ((out.double() - want).norm() / want.norm()).item()
+        assert rel < tol, rel
+        assert torch.equal(out, cache.attend(q, *where))
+
+
+def test_a_prompt_does_not_go_by_the_width_of_the_page_table():
+    """2000 rows are work for all CTAs however narrow their table is: the same kernel and the same bits as with a wide one."""
+    import torch
+    cache, where, q, out, _ = _big(1, [2000], [0], 8, 8, 128, torch.bfloat16)
+    wide = torch.full((1, 4000), -1, dtype=torch.int32, device="cuda")
+    wide[:, :where[2].shape[1]] = where[2]
+    assert torch.equal(out, cache.attend(q, where[0], where[1], wide))
