@@ -10,7 +10,7 @@
 // and id.
 //
 // Masses are 64-bit whole numbers, w * 2^45 rounded to nearest: sums do not depend on their order, a prefix never decreases, and no
-// result changes between runs, cluster sizes or passes.  At most 2^18 ids, so a sum stays below 2^63; what rounding moves is
+// result changes between runs, cluster sizes or passes.  At most 2^18 ids, so a sum is at most 2^63; what rounding moves is
 // 2^-46 of the most likely id's weight per id, and an id below that has no mass at all.  Weights are evaluated in fp64: thresholds and
 // draws are whole decisions, and one in a few thousand of a flat row would fall on the other side of a border with fp32 weights.
 //
@@ -285,7 +285,8 @@ __device__ __forceinline__ unsigned long long cta_reduce_u64(unsigned long long 
 // ids (more than the list holds: a third pass collects those of one fine bin).  Those of the fine bin with the cut are compared with
 // each other.  Where even they are more than the lists hold (thousands of equal logits, a cut in the far tail) shape_select_digits
 // takes over, which needs no luck: digit by digit over the whole key.
-constexpr double kShapeSlack = 1e-4;               // half a step of 2^-13 (6.1e-5), and what fp32 loses of the places of bin and maximum (8e-6 each)
+constexpr double kShapeSlack = 1.1e-4;             // half a step of 2^-13 (6.1e-5), the quarter step that shape_count's constant is rounded by
+                                                   // (3.1e-5), and what fp32 loses of the places of bin and maximum (8e-6 each)
 constexpr float kShapeWidth = 64.f;                // bins per unit of the exponent (top-p) or of the logit (top-k)
 constexpr float kShapeUp = 20.f;                   // units: 44 remain below, e^-44 of the maximum over 2^18 ids is nothing
 
