@@ -354,7 +354,8 @@ int32_t pipesd_accept(const void *logits, int32_t dtype, int64_t row_stride, int
  *
  * One layer's paged cache at 5 bits per value, scales included: 160 bytes per position and head of 128 instead of 512.  The columns
  * of a (position, head) row are cut into groups of 32 with a zero z = bf16(min) and a scale s = bf16((max - z) / 15); a value x is
- * held as c = clamp(rint((x - z) / s), 0, 15) and stands for s * c + z.  Values beyond +-2^48 are held as that, a NaN as 0.
+ * held as c = clamp(rint((x - z) / s), 0, 15) and stands for s * c + z; where s is not above 0 (a group of one value, whose z may also be
+ * rounded above it) every code is 0 and stands for z.  Values beyond +-2^48 are held as that, a NaN as 0.
  * Calls, streams, threads and graphs as for pipesd_sample; all arrays are in device memory.
  *
  * Where rows go: request r has the rows row0[r] .. row0[r+1]-1 of a call (row0: n_req + 1 entries from 0 to rows), and row i of it
@@ -383,10 +384,13 @@ int32_t pipesd_kv4_read(const pipesd_kv4_cfg *cfg, const void *pool, float *k, f
                         const int32_t *row0, const int32_t *base, const int32_t *table, void *cuda_stream);
 /* out[row] = softmax(scale * q . k) v over positions 0 .. base[r] + i of the request (its new rows appended before): a single
  * token, the k+1 rows of a verification, or a prompt.  q, out: [rows, n_q_heads, head_dim] of `dtype` with q_stride, out_stride;
- * n_q_heads a multiple of n_kv_heads; scale > 0, and scale * |q| below 2^96.  bf16: products of bf16 with fp32 sums;
- * fp32: operands carry 22 bits of mantissa.  A row that sees no position gives 0; rows of no request are left as they are.  out must not overlap q.  A value's bits are kept
- * relative to the largest of its request's: down to 2^-16 of it all of them, then fewer.  scratch: pipesd_kv4_attend_scratch_bytes(cfg)
- * bytes, 16-byte aligned; it holds nothing between calls, but two calls that may run at the same time need one each. */
+ * n_q_heads a multiple of n_kv_heads; scale > 0, and scale * |q| below 2^96.  Sums are fp32.  bf16: q and codes enter the products as they
+ * are, probabilities, probabilities times scales, and z + 8 s of V as fp16 (11 bits), so that about an eighth of the outputs lie one bf16
+ * step beside the nearest one; fp32: q, probabilities and z + 8 s carry 22 bits of mantissa.  A row that sees no position gives 0, a head's
+ * row whose q has a NaN or an infinity a NaN; rows of no request are left as they are.  out must not overlap q.  A value's bits are
+ * kept relative to the largest of its request's: down to 2^-16 of it all of them, then fewer.  The order of sums goes by the lengths
+ * and by max_pages.  scratch: pipesd_kv4_attend_scratch_bytes(cfg) bytes, 16-byte aligned; it holds nothing between calls, but two
+ * calls that may run at the same time need one each. */
 uint64_t pipesd_kv4_attend_scratch_bytes(const pipesd_kv4_cfg *cfg);
 int32_t pipesd_kv4_attend(const pipesd_kv4_cfg *cfg, const void *pool, const void *q, void *out, int32_t dtype, int64_t q_stride,
                           int64_t out_stride, int32_t n_q_heads, float scale, int32_t n_req, int32_t rows, const int32_t *row0,

@@ -101,8 +101,10 @@ int32_t pipesd_kv4_append(const pipesd_kv4_cfg* cfg, void* pool, const void* k, 
     if (rows > 1 && (k_stride < width || v_stride < width)) return PIPESD_E_INVALID;
     const Kv4AppendArgs a = {where_of(cfg, n_req, rows, row0, base, table), k, v, k_stride, v_stride, static_cast<unsigned char*>(pool),
                              wide(k, k_stride, rows, dtype) && wide(v, v_stride, rows, dtype)};
-    // CTAs for one wave and a half (four to an SM), beyond which a CTA takes several heads of its unit: 2048 rows 27.1 us with one wave, 25.9, 24.4
-    // with two; 5 requests of 100 to 700 rows in fp32 7.4, 7.2, 7.9
+    // CTAs for one wave and a half (four to an SM), beyond which a CTA takes several heads of its unit.  us with one wave, one and a half, and two:
+    // 2048 rows of 32 heads of 128 in bf16 27.1, 25.9, 24.4; 5 requests of 100 to 700 rows of 8 heads of 64 in fp32 7.4, 7.2, 7.9; of 32 heads of
+    // 128 in bf16 (by graph, cold) 1000 rows 22.5, 22.5, 20.5, 4096 57, 59, 53, 8192 107, 107, 94; of 8 heads of 64 2048 rows 10, 12, 12,
+    // 4096 14, 16, 14.  Two waves gain a tenth at the largest and lose as much at the smaller ones.
     const int units = most_units(n_req, rows);
     const dim3 grid((unsigned)units, (unsigned)std::min(cfg->n_kv_heads, std::max(1, 6 * 148 / units)));
     cudaStream_t st = (cudaStream_t)cuda_stream;

@@ -1,7 +1,7 @@
 // A paged K/V cache held in 4 bits, and the attention of short chunks of query rows over it.
 //
 // Values: the columns of a (position, head) row are cut into groups of 32 that share a zero z = bf16(min) and a scale
-// s = bf16((max - z) / 15); a value is held as the code c = clamp(rint((x - z) / s), 0, 15) and stands for s * c + z.
+// s = bf16((max - z) / 15); a value is held as the code c = clamp(rint((x - z) / s), 0, 15) and stands for s * c + z (s <= 0: c = 0).
 //
 // Layout of one layer: [page][KV head][unit], a unit being 16 positions of one head in 20 * HD contiguous bytes:
 //   K codes   8 HD   [position 16][t 4][group]      32-bit words, nibble p = column 32 group + 8 t + p

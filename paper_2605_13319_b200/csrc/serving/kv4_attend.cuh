@@ -10,9 +10,10 @@
 // No value is ever dequantised.  A key's code goes into the tensor cores as the subnormal that its bits are, n * 2^-24; Q is
 // scaled by a power of two per row (largest entry near 2^15).  A value's code is centred on the way, by one fused multiply-add per
 // two codes (exact): outputs are means of many values, whose sum of uncentred codes would be hundreds of times the result and
-// its rounding as well.  fp16 keeps 11 bits of P and of P * s; the scales and middles are taken relative to a power of two that
-// fits the warp's first unit, and rescaled (like a row's exponentials, which are relative to a score of that unit) when one
-// exceeds it by 2^6 (2^4).
+// its rounding as well.  fp16 keeps 11 bits of P, of P * s and of the middles (bf16 outputs: an eighth of them one step beside the nearest,
+// error against 64 bits 1.68e-3 where rounding alone has 1.67e-3; a second term of P would double the values' products); the scales
+// and middles are taken relative to a power of two that fits the warp's first unit, and rescaled (like a row's exponentials, which are
+// relative to a score of that unit) when one exceeds it by 2^6 (2^4).
 // fp32 queries and outputs (kSplit): Q, P, P * s and the middles as two fp16 terms each, 22 bits of mantissa; a unit's products go to the
 // running sums by ordinary additions, which round to nearest, and keys' codes are centred too, middles times sums of Q (fp32) added beside
 // (the tensor pipe truncates where it adds: error 2.1e-6 over long caches without either, 1.2e-6 with the additions, 2.5e-7 with both;
@@ -639,7 +640,8 @@ __global__ void __launch_bounds__(32 * attend_warps(NT), attend_ctas_per_sm(NT))
 // Adds up the shares of triples that several CTAs had, per (row, query head).  W warps each: a CTA per job, of which warp w takes the shares w,
 // w + 4, ..., and the warps' sums are added in their order (a warp for a row alone waits for the L2 once per four shares: 12 us for 37 of them).
 // W = 1: beyond a wave of such CTAs a warp per a.heads heads of a row, since what finds a job's shares costs more than the few that each then
-// has (us with four and one: 32 rows of 32 heads, one wave, 52.5 52.6; 64 rows 63.7 60; 155 rows in fp32 206 198; 2000 rows 705 606).
+// has (us with four and one, CTAs of one row tile, heads of 128: 32 rows of 32 heads in bf16, one wave, 52.5 52.6; 64 rows 63.7 60; 155 rows
+// in fp32 206 198; a prompt of 2000 rows in bf16 705 606).
 constexpr int kMergeWarps = 4;
 constexpr int kMergeWave = 148 * 9;                // CTAs of it that the device holds (56 registers)
 template <int HD, int W, typename T>

@@ -11,8 +11,10 @@ namespace {
 static_assert(sizeof(Shaping) == sizeof(pipesd_shaping), "pipesd_shaping is read as it is");
 
 // CTAs of a row: as many as leave every CTA an SM of its own and 8000 ids.  us, top-p 0.9, by CTAs per row (1, 2, 4, 8): 1 row of 128256
-// 89, 55, 37, 29; 32 rows 94, 58, 39, 39; 128 rows 95, 85, 102, 147 (two CTAs fit an SM, but share its fp64 pipes, and clusters do not
-// fill every group of SMs to its last place); 16 rows of 32000 31, 25, 21, 25; of 8192 15, 17, 17, 22.
+// 89, 55, 37, 29; 32 rows 94, 58, 39, 39; 16 rows of 32000 31, 25, 21, 25; of 8192 15, 17, 17, 22.  Two CTAs on an SM pay or cost as the settings have
+// it, which the host does not know: 128 rows of 128256 with one and two CTAs (cold) unshaped 63 57, top-p 104 86, top-k 50 55 47, but top-k 1000
+// with top-p 158 256, since every CTA of a cluster ranks the whole list of kept ids.  (Clusters do not fill every group of SMs either: 37 rows of four
+// such CTAs take 236 where 24 rows take 133.)
 int shape_cluster(int rows, int V) {
     int c = 8;
     while (c > 1 && ((long long)rows * c > 148 || V < c * 8000)) c /= 2;

@@ -537,3 +537,28 @@ def test_a_prompt_does_not_go_by_the_width_of_the_page_table():
     wide = torch.full((1, 4000), -1, dtype=torch.int32, device="cuda")
     wide[:, :where[2].shape[1]] = where[2]
     assert torch.equal(out, cache.attend(q, where[0], where[1], wide))
+
+
+@pytest.mark.parametrize("hd", [64, 128])
+def test_groups_of_one_value(hd):
+    """Their zero, rounded to bf16, may lie above the value (a scale below 0) or on it (a scale of 0): code 0, which stands for the zero."""
+    import torch
+    rng = np.random.default_rng(hd)
+    c = Case(rng, [20], [0], 2, hd)
+    k, v = (_rows(rng, 20, 2, hd, torch.float32) for _ in range(2))
+    for x, i in ((k, 0), (v, 3)):
+        x[i] = 1.0059                                                        # (bf16: 1.0078)
+        x[i + 1] = -1.0059                                                   # (bf16: -1.0078, below it)
+        x[i + 2] = 1.5
+        x[i + 3, 0] = 77.77
+        x[i + 4, 1, 32:64] = 2.0 ** -20 * 1.0059
+    c.cache.append(k, v, *c.where)
+    c.write_ref(k.double().cpu().numpy(), v.double().cpu().numpy())
+    assert np.array_equal(c.pool.cpu().numpy(), c.ref.pool)
+    rk, rv = c.cache.read(20, *c.where)
+    assert (rk[0] == 1.0078125).all() and (rv[3] == 1.0078125).all() and (rk[2] == 1.5).all() and (rv[5] == 1.5).all()
+    scales = [float(serving.quantise(x[i, 0, :32].double().cpu().numpy())[1][0]) for x, i in ((k, 0), (k, 1), (k, 2))]
+    assert scales[0] < 0 < scales[1] and scales[2] == 0
+    for dtype in (torch.bfloat16, torch.float32):
+        q = _rows(rng, 20, 4, hd, dtype)
+        _attend_check(c, q, hd ** -0.5, c.cache.attend(q, *c.where))
