@@ -384,7 +384,7 @@ int32_t pipesd_kv4_read(const pipesd_kv4_cfg *cfg, const void *pool, float *k, f
                         const int32_t *row0, const int32_t *base, const int32_t *table, void *cuda_stream);
 /* out[row] = softmax(scale * q . k) v over positions 0 .. base[r] + i of the request (its new rows appended before): a single
  * token, the k+1 rows of a verification, or a prompt.  q, out: [rows, n_q_heads, head_dim] of `dtype` with q_stride, out_stride;
- * n_q_heads a multiple of n_kv_heads; scale > 0, and scale * |q| below 2^96.  Sums are fp32.  bf16: q and codes enter the products as they
+ * n_q_heads a multiple of n_kv_heads; scale > 0, scale * |q| below 2^96 and every score below 2^120 in magnitude.  Sums are fp32.  bf16: q and codes enter the products as they
  * are, probabilities, probabilities times scales, and z + 8 s of V as fp16 (11 bits), so that about an eighth of the outputs lie one bf16
  * step beside the nearest one; fp32: q, probabilities and z + 8 s carry 22 bits of mantissa.  A row that sees no position gives 0, a head's
  * row whose q has a NaN or an infinity a NaN; rows of no request are left as they are.  out must not overlap q.  A value's bits are

@@ -41,7 +41,7 @@ __host__ __device__ constexpr int attend_warps(int nt) { return nt == 1 ? 8 : 4;
 __host__ __device__ constexpr int attend_ctas_per_sm(int nt) { return nt == 1 ? 2 : 3; }
 constexpr int kAttendSms = 148;
 constexpr int kAttendMinUnits = 8;                 // of a CTA
-constexpr float kAttendNone = -1e30f;              // reference of a row that has seen nothing
+constexpr float kAttendNone = -3.3e38f;            // reference of a row that has seen nothing: below every score
 constexpr float kAttendExcess = 4.f;               // log2 units by which a score may exceed its row's reference: P <= 16
 constexpr float kAttendScaleExcess = 64.f;         // factor by which a scale may exceed its warp's unit
 // fp16 has 40 binades for a number and its second term: P is taken times 2^6 (up to 2^10), scales times 1 / 4 (up to 2^5: their 8 bits are exact

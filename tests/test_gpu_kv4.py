@@ -562,3 +562,27 @@ def test_groups_of_one_value(hd):
     for dtype in (torch.bfloat16, torch.float32):
         q = _rows(rng, 20, 4, hd, dtype)
         _attend_check(c, q, hd ** -0.5, c.cache.attend(q, *c.where))
+
+
+@pytest.mark.parametrize("units", [0, 50000])
+@pytest.mark.parametrize("hd", [64, 128])
+def test_attend_scores_far_below_zero(hd, units):
+    """scale * |q| just below 2^96 and keys that make every score -2^97 times their number of columns and less: still the softmax of
+    them, which is the value of the one key that is smallest.  Few positions (most warps see none) and many."""
+    import torch
+    rng = np.random.default_rng(hd)
+    for n in (12, 600):
+        c = Case(rng, [n], [0], 1, hd)
+        _widen(c, units or c.table.size)
+        k = torch.ones((n, 1, hd), device="cuda") * (2.0 + torch.arange(n, device="cuda") % 8)[:, None, None]
+        k[n // 2] = 1.0
+        v = _rows(rng, n, 1, hd, torch.float32)
+        c.cache.append(k, v, *c.where)
+        _, held = c.cache.read(n, *c.where)
+        for dtype in (torch.bfloat16, torch.float32):
+            q = torch.full((n, 2, hd), -7.5e28, device="cuda").to(dtype)
+            out = c.cache.attend(q, *c.where, scale=1.0)[n // 2:]
+            want = held[n // 2].expand(n - n // 2, 2, hd)
+            size = held[n // 2].abs().max() * 2.2                            # s |c - 8| + |z + 8 s|: 16 / 15 and 1 times the largest, and the roundings of s and z
+            assert torch.isfinite(out).all()
+            assert ((out.float() - want).abs() <= 2.0 ** -8 * want.abs() + 4 * 2.0 ** -11 * size).all()
