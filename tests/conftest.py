@@ -36,3 +36,21 @@ def _collect_after_gpu_test(request):
     if "gpu" in request.node.keywords:
         import gc
         gc.collect()
+
+
+@pytest.fixture(scope="session", autouse=True)
+def _what_takes_its_time_once(request):
+    """What takes its time once: memory for a stream of torch's pool (its allocator asks the driver: 0.4 ms, but 20 to 100 where other users
+    of the machine allocate) and loading a library's kernel (zeros 8 ms).  Done ahead of tests that count on what a stream of theirs is
+    still doing (10 ms of sleep); a block of every stream is held, since a capture empties the cache."""
+    import torch
+    blocks = []
+    if torch.cuda.is_available() and any("gpu" in it.keywords for it in request.session.items):
+        torch.cuda._sleep(1)
+        torch.zeros((64, 1024), device="cuda")
+        for stream in [torch.cuda.Stream() for _ in range(32)]:              # (the pool's, in turn)
+            with torch.cuda.stream(stream):
+                blocks.append(torch.empty(1, device="cuda"))
+        torch.cuda.synchronize()
+    yield
+    blocks.clear()
