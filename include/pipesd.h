@@ -340,9 +340,8 @@ int32_t pipesd_sample(const void *logits, int32_t dtype, int64_t row_stride, int
  * the final draw.  shaping: [n_req].  A draft x is accepted while u < min(1, p(x) / q(x)); a correction comes from norm(max(0, p - q)),
  * from p where that is 0 everywhere.  A row that has no distribution (see pipesd_sample) accepts nothing and gives next_token -1.
  * A draft that is no id, or whose u lies outside [0, 1), or whose q is a NaN or below 0 is not accepted; a correction from a row of q with
- * such an entry at a kept id, or with a last u outside [0, 1), is next_token -1;
- * so does a request whose row0 entries make no sense: not 0 <= row0[r] - r, row0[r] < row0[r+1] <= rows with its drafts inside of q, or
- * an entry before row0[r] larger than it.  scratch: pipesd_accept_scratch_bytes(rows) bytes, 8-byte aligned, one for
+ * such an entry at a kept id, or with a last u outside [0, 1), is next_token -1.  A request whose row0 entries make no sense gets 0 and
+ * -1: r <= row0[r] < row0[r+1] <= rows does not hold, its drafts lie outside of q, or an entry before row0[r] is larger.  scratch: pipesd_accept_scratch_bytes(rows) bytes, 8-byte aligned, one for
  * each of calls that may run at the same time. */
 uint64_t pipesd_accept_scratch_bytes(int32_t rows);
 int32_t pipesd_accept(const void *logits, int32_t dtype, int64_t row_stride, int32_t n_req, int32_t rows, int32_t vocab,
@@ -384,9 +383,9 @@ int32_t pipesd_kv4_read(const pipesd_kv4_cfg *cfg, const void *pool, float *k, f
                         const int32_t *row0, const int32_t *base, const int32_t *table, void *cuda_stream);
 /* out[row] = softmax(scale * q . k) v over positions 0 .. base[r] + i of the request (its new rows appended before): a single
  * token, the k+1 rows of a verification, or a prompt.  q, out: [rows, n_q_heads, head_dim] of `dtype` with q_stride, out_stride;
- * n_q_heads a multiple of n_kv_heads; scale > 0, scale * |q| below 2^96 and every score below 2^120 in magnitude.  Sums are fp32.  bf16: q and codes enter the products as they
- * are, probabilities, probabilities times scales, and z + 8 s of V as fp16 (11 bits), so that about an eighth of the outputs lie one bf16
- * step beside the nearest one; fp32: q, probabilities and z + 8 s carry 22 bits of mantissa.  A row that sees no position gives 0, a head's
+ * n_q_heads a multiple of n_kv_heads; scale > 0, scale * |q| below 2^96 and every score below 2^120 in magnitude.  Sums are fp32.
+ * bf16: q and codes enter the products as they are, probabilities, probabilities times scales, and z + 8 s of V as fp16 (11 bits), so
+ * that about an eighth of the outputs lie one bf16 step beside the nearest one; fp32: q, probabilities and z + 8 s carry 22 bits of mantissa.  A row that sees no position gives 0, a head's
  * row whose q has a NaN or an infinity a NaN; rows of no request are left as they are.  out must not overlap q.  A value's bits are
  * kept relative to the largest of its request's: down to 2^-16 of it all of them, then fewer.  The order of sums goes by the lengths
  * and by max_pages.  scratch: pipesd_kv4_attend_scratch_bytes(cfg) bytes, 16-byte aligned; it holds nothing between calls, but two

@@ -67,7 +67,8 @@ int attend_row_tiles(int64_t rows) { return (rows + 15) / 16 * 16 * 5 <= (rows +
 // That where there is work for the CTAs of two: `units` of the page table (what the host knows of the lengths) times the row groups that read each,
 // `rows` of a KV head in the mean.  us with one and two tiles, bf16, one request, by units * groups: 9 rows of 32 heads behind 2048 positions
 // (8 thousand) 25 29; behind 8192 (33) 39 39; behind 16384 (66) 57 51; 9 rows over 8 heads behind 16384 (41) 43 47; 64 rows of 32 heads behind
-// 2048 (34) 39 41; 128 rows (70) 61 55; prompts of 512 rows (66) 78 68, of 2000 (1000) 620 430.
+// 2048 (34) 39 41; 128 rows (70) 61 55; prompts of 64 rows (1) 18 25, of 512 (66) 78 68, of 2000 (1000) 620 430.  (A prompt of 128 rows (4) 25 18,
+// whose triples of eight units need no merge with either.)
 constexpr int64_t kAttendTwoTiles = 49152;
 int attend_tiles(int64_t units, int64_t rows) { return units * ((rows + 7) / 8) < kAttendTwoTiles ? 1 : attend_row_tiles(rows); }
 
