@@ -395,6 +395,93 @@ int32_t pipesd_kv4_attend(const pipesd_kv4_cfg *cfg, const void *pool, const voi
                           int64_t out_stride, int32_t n_q_heads, float scale, int32_t n_req, int32_t rows, const int32_t *row0,
                           const int32_t *base, const int32_t *table, void *scratch, void *cuda_stream);
 
+/* ---- trees of drafts: prompts, a K/V cache in bf16, and its pages ----
+ *
+ * What a server needs whose edges draft trees instead of chains: attention of whole prompts, which fills the cache; attention of a tree's
+ * nodes over the cache; and the pages' life: reserved for rows to come, forked for candidates that share a prefix, compacted to the
+ * accepted path, released.  Calls, streams, threads and graphs as for pipesd_sample; all arrays are in device memory. */
+
+/* out[row] = softmax(scale * q . k) v over the rows of the same prompt up to itself.  Prompt r has the rows row0[r] .. row0[r+1]-1 (row0:
+ * n_req + 1 ascending entries within 0 .. rows; a prompt without rows is one); rows of no prompt are neither read into any result nor written.
+ * bf16 throughout: q, out [rows, n_q_heads, head_dim], k, v [rows, n_kv_heads, head_dim], head_dim 64 or 128, n_q_heads a multiple of
+ * n_kv_heads, up to 128 times as many; strides in elements between rows, multiples of 8, pointers 16-byte aligned; scale > 0, every score
+ * times scale below 2^120 in magnitude.  Scores, their maximum and their sums are fp32, probabilities enter the second product in bf16.  A NaN or an
+ * infinity in a row of k or v reaches the rows that see it (what is not finite in v makes that column NaN or infinite) and no others.  out must
+ * not overlap the inputs. */
+int32_t pipesd_attend_packed(const void *q, const void *k, const void *v, void *out, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                             int64_t out_stride, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, float scale, int32_t n_req,
+                             int32_t rows, const int32_t *row0, void *cuda_stream);
+
+/* Mask rows of drafted trees.  Request r has the nodes row0[r] .. row0[r+1]-1; parent[row] is the index within its request of the node's
+ * parent, below its own (-1, or anything that is not: a child of the prefix).  mask: [rows, words], bit j of a row = node j is the node itself or an
+ * ancestor; depth: [rows], ancestors among the nodes (the row's position is base + depth).  words: 1..256; a node with an index of 32 * words
+ * or more has no bits and depth -1.  Rows of no request are left as they are. */
+int32_t pipesd_tree_mask(int32_t n_req, int32_t rows, const int32_t *row0, const int32_t *parent, int32_t words, uint32_t *mask,
+                         int32_t *depth, void *cuda_stream);
+
+/* The pool has the layout of a context's own: [layer][page][K, V][KV head][position / 8][column / 8][position % 8][column % 8], bf16.
+ * Requests, rows, base and table as for the 4-bit cache, one table for all layers. */
+typedef struct pipesd_kv16_cfg {
+    int32_t n_layers;
+    int32_t n_kv_heads;
+    int32_t head_dim;  /* 64 or 128                                            */
+    int32_t page_size; /* positions: a multiple of 8, up to 4096               */
+    int32_t n_pages;   /* in the pool; n_pages * page_size < 2^31              */
+    int32_t max_pages; /* columns of the table; max_pages * page_size <= 2^30  */
+    int32_t reserved;  /* must be 0                                            */
+} pipesd_kv16_cfg;
+
+/* Bytes of a pool (16-byte aligned, contents irrelevant at first; 0 for a bad cfg). */
+uint64_t pipesd_kv16_pool_bytes(const pipesd_kv16_cfg *cfg);
+/* Rows of K and V ([rows, n_kv_heads, head_dim] of `dtype`, rounded to bf16 where they are fp32) into their positions of one layer. */
+int32_t pipesd_kv16_append(const pipesd_kv16_cfg *cfg, void *pool, int32_t layer, const void *k, const void *v, int32_t dtype,
+                           int64_t k_stride, int64_t v_stride, int32_t n_req, int32_t rows, const int32_t *row0, const int32_t *base,
+                           const int32_t *table, void *cuda_stream);
+/* The rows' positions of one layer: bf16 [rows, n_kv_heads, head_dim] each, 16-byte aligned; 0 where no page is, and for rows of no request. */
+int32_t pipesd_kv16_read(const pipesd_kv16_cfg *cfg, const void *pool, int32_t layer, void *k, void *v, int32_t n_req, int32_t rows,
+                         const int32_t *row0, const int32_t *base, const int32_t *table, void *cuda_stream);
+/* out[row] = softmax(scale * q . k) v over what the row sees (its request's new rows appended before): positions 0 .. base[r]-1, and of the
+ * new rows those whose bit is set in its row of mask ([rows, words], words 1..256, as pipesd_tree_mask writes them; any other set will do, none
+ * at all too); without a mask (null) those up to itself.  q, out: [rows, n_q_heads, head_dim] of `dtype` with q_stride, out_stride;
+ * n_q_heads a multiple of n_kv_heads, up to 128 times as many; scale > 0, every score times scale below 2^120 in magnitude.  Sums are fp32.  bf16:
+ * q as it is, probabilities in bf16; fp32: q and probabilities as three bf16 terms each (24 bits).  A row that sees no position gives 0, a
+ * head's row whose q has a NaN a NaN; rows of no request are left as they are.  A NaN or an infinity in the cache reaches the rows that
+ * see it, as for prompts.  out must not overlap q.  The order of sums goes by the lengths and by the number of rows.  scratch:
+ * pipesd_kv16_attend_scratch_bytes bytes (0 for arguments that are refused), 16-byte aligned; it holds nothing between calls, but two
+ * calls that may run at the same time need one each. */
+uint64_t pipesd_kv16_attend_scratch_bytes(const pipesd_kv16_cfg *cfg, int32_t rows, int32_t n_q_heads);
+int32_t pipesd_kv16_attend(const pipesd_kv16_cfg *cfg, const void *pool, int32_t layer, const void *q, void *out, int32_t dtype,
+                           int64_t q_stride, int64_t out_stride, int32_t n_q_heads, float scale, int32_t n_req, int32_t rows,
+                           const int32_t *row0, const int32_t *base, const int32_t *table, const uint32_t *mask, int32_t words,
+                           void *scratch, void *cuda_stream);
+
+/* Pages.  refs: [n_pages], how many entries of tables hold a page; 0: it is free (all 0 at first).  These calls keep it so, and pages are
+ * handed out lowest id first, in the order of the requests.  A request that does not get all its pages gets none, its row of the table stays
+ * as it was and its entry of pages is -1 (as where its numbers make no sense); those behind it are still served where they fit.  Calls on one
+ * refs or table are made one after the other.  scratch: pipesd_kv16_plan_scratch_bytes(cfg, n) bytes, 4-byte aligned, one for each of
+ * calls that may run at the same time.
+ * reserve: pages for positions 0 .. length[r]-1 of request r = row r of table ([n_req, max_pages]) where the table has none; pages[r]: their
+ * number, those that were there included. */
+uint64_t pipesd_kv16_plan_scratch_bytes(const pipesd_kv16_cfg *cfg, int32_t n);
+int32_t pipesd_kv16_reserve(const pipesd_kv16_cfg *cfg, int32_t n_req, const int32_t *length, int32_t *table, int32_t *refs, int32_t *pages,
+                            void *scratch, void *cuda_stream);
+/* fork: row dst[i] of table ([n_slots, max_pages]) becomes a continuation of row src[i], which has length[i] positions: pages that hold only
+ * positions below own[i] are shared, those behind, up to length[i], are copied in all layers into new ones, so that both may write from
+ * position own[i] on.  Entries of the row dst[i] are overwritten (release its pages first); no dst is a src or twice a dst within a call. */
+int32_t pipesd_kv16_fork(const pipesd_kv16_cfg *cfg, void *pool, int32_t n, const int32_t *src, const int32_t *dst, const int32_t *length,
+                         const int32_t *own, int32_t n_slots, int32_t *table, int32_t *refs, int32_t *pages, void *scratch,
+                         void *cuda_stream);
+/* compact: of the rows behind base[r], those whose bit is set in keep[r] ([n_req, words]; the accepted leaf's row of a mask keeps a path) move
+ * together, in their order, to base[r], base[r] + 1, ..., in all layers; kept[r]: how many.  Rows behind them hold leavings.  The pages
+ * that hold these rows are in one request's row, once; a row whose page (or whose new position's) is not there does not move; bits of positions
+ * behind the table's last are not counted. */
+int32_t pipesd_kv16_compact(const pipesd_kv16_cfg *cfg, void *pool, int32_t n_req, const uint32_t *keep, int32_t words, const int32_t *base,
+                            const int32_t *table, int32_t *kept, void *cuda_stream);
+/* release: pages that hold only positions from length[r] on leave row r of table ([n_req, max_pages]); the last one to hold a page frees it.
+ * A length below 0 leaves the row as it is. */
+int32_t pipesd_kv16_release(const pipesd_kv16_cfg *cfg, int32_t n_req, const int32_t *length, int32_t *table, int32_t *refs,
+                            void *cuda_stream);
+
 /* ---- the edge-side scheduling model (host code only; no device work) ----
  *
  * The verify pass above is what the cloud runs; what decides WHEN it runs and how the draft tokens reach it is the

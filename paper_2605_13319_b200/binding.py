@@ -69,6 +69,10 @@ class Kv4Cfg(ctypes.Structure):
     _fields_ = [(n, i32) for n in ("n_kv_heads", "head_dim", "page_size", "n_pages", "max_pages", "reserved")]
 
 
+class Kv16Cfg(ctypes.Structure):
+    _fields_ = [(n, i32) for n in ("n_layers", "n_kv_heads", "head_dim", "page_size", "n_pages", "max_pages", "reserved")]
+
+
 # name -> (restype, argtypes); mirrors include/pipesd.h one to one
 _SIGNATURES = {
     "pipesd_strerror": (ctypes.c_char_p, [i32]),
@@ -104,6 +108,18 @@ _SIGNATURES = {
     "pipesd_kv4_read": (i32, [ctypes.POINTER(Kv4Cfg), vp, vp, vp, i32, i32, vp, vp, vp, vp]),
     "pipesd_kv4_attend_scratch_bytes": (u64, [ctypes.POINTER(Kv4Cfg)]),
     "pipesd_kv4_attend": (i32, [ctypes.POINTER(Kv4Cfg), vp, vp, vp, i32, i64, i64, i32, f32, i32, i32, vp, vp, vp, vp, vp]),
+    "pipesd_attend_packed": (i32, [vp, vp, vp, vp, i64, i64, i64, i64, i32, i32, i32, f32, i32, i32, vp, vp]),
+    "pipesd_tree_mask": (i32, [i32, i32, vp, vp, i32, vp, vp, vp]),
+    "pipesd_kv16_pool_bytes": (u64, [ctypes.POINTER(Kv16Cfg)]),
+    "pipesd_kv16_append": (i32, [ctypes.POINTER(Kv16Cfg), vp, i32, vp, vp, i32, i64, i64, i32, i32, vp, vp, vp, vp]),
+    "pipesd_kv16_read": (i32, [ctypes.POINTER(Kv16Cfg), vp, i32, vp, vp, i32, i32, vp, vp, vp, vp]),
+    "pipesd_kv16_attend_scratch_bytes": (u64, [ctypes.POINTER(Kv16Cfg), i32, i32]),
+    "pipesd_kv16_attend": (i32, [ctypes.POINTER(Kv16Cfg), vp, i32, vp, vp, i32, i64, i64, i32, f32, i32, i32, vp, vp, vp, vp, i32, vp, vp]),
+    "pipesd_kv16_plan_scratch_bytes": (u64, [ctypes.POINTER(Kv16Cfg), i32]),
+    "pipesd_kv16_reserve": (i32, [ctypes.POINTER(Kv16Cfg), i32, vp, vp, vp, vp, vp, vp]),
+    "pipesd_kv16_fork": (i32, [ctypes.POINTER(Kv16Cfg), vp, i32, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp]),
+    "pipesd_kv16_compact": (i32, [ctypes.POINTER(Kv16Cfg), vp, i32, vp, i32, vp, vp, vp, vp]),
+    "pipesd_kv16_release": (i32, [ctypes.POINTER(Kv16Cfg), i32, vp, vp, vp, vp]),
     "pipesd_sched_round_time": (i32, [i32, ctypes.c_double, ctypes.c_double, ctypes.c_double, vp, i32,
                                       ctypes.POINTER(ctypes.c_double)]),
     "pipesd_sched_optimal_batching": (i32, [i32, ctypes.c_double, ctypes.c_double, ctypes.c_double, vp,
@@ -656,6 +672,213 @@ class Kv4Cache:
         if rc != OK:
             raise PipesdError(rc, "pipesd_kv4_attend")
         return out
+
+
+# ---- trees of drafts: prompts, a bf16 cache and its pages, on device tensors (no context)
+def attend_packed(q, k, v, row0, *, scale=None, out=None, stream=None):
+    """pipesd_attend_packed: causal attention of prompts packed one behind the other.  q [rows, query heads, head_dim], k, v [rows, KV
+    heads, head_dim] in bf16, row strides of their own (views of a fused projection will do); row0: int32 [prompts + 1].  scale: head_dim ** -0.5
+    unless given.  Returns out, like q (made here: rows of no prompt are not written)."""
+    import torch
+    dev = q.device
+    assert q.dim() == 3 and k.dim() == 3 and k.shape == v.shape and k.shape[0] == q.shape[0] and k.shape[2] == q.shape[2], "q, k, v: [rows, heads, head_dim]"
+    assert q.dtype is k.dtype is v.dtype is torch.bfloat16 and k.device == dev == v.device, "q, k, v: bf16 on one device"
+    rows, heads, hd = q.shape
+    n_req = row0.numel() - 1
+    on = _on(dev, stream, q, k, v, row0, out)
+    with on as st:
+        if out is None:
+            out = torch.empty_like(q, memory_format=torch.contiguous_format)
+            on.made(out)
+        else:
+            assert out.shape == q.shape and out.dtype is q.dtype and out.device == dev, "out: like q"
+        rc = lib().pipesd_attend_packed(q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), _rows_of(q, "q"), _rows_of(k, "k"), _rows_of(v, "v"),
+                                        _rows_of(out, "out"), heads, k.shape[1], hd, hd ** -0.5 if scale is None else scale, n_req, rows,
+                                        _vector(row0, n_req + 1, torch.int32, dev, "row0"), st)
+    if rc != OK:
+        raise PipesdError(rc, "pipesd_attend_packed")
+    return out
+
+
+def tree_mask(parent, row0, words: int, *, stream=None):
+    """pipesd_tree_mask: (mask int32 [rows, words], depth int32 [rows]) of drafted trees.  parent: int32 [rows], indices within the request, -1
+    below the prefix; row0: int32 [n_req + 1].  Rows of no request: no bits, depth 0."""
+    import torch
+    dev, rows, n_req = parent.device, parent.numel(), row0.numel() - 1
+    on = _on(dev, stream, parent, row0)
+    with on as st:
+        both = torch.zeros(rows * (words + 1), dtype=torch.int32, device=dev)
+        mask, depth = both[rows:].view(rows, words), both[:rows]
+        on.made(both)
+        rc = lib().pipesd_tree_mask(n_req, rows, _vector(row0, n_req + 1, torch.int32, dev, "row0"), _vector(parent, rows, torch.int32, dev, "parent"), words,
+                                    mask.data_ptr(), depth.data_ptr(), st)
+    if rc != OK:
+        raise PipesdError(rc, "pipesd_tree_mask")
+    return mask, depth
+
+
+class Kv16Cache:
+    """A paged K/V cache in bf16 (pipesd_kv16_*), all layers of it.  The pool is a bf16 tensor [layers, pages, 2, KV heads, page_size / 8,
+    head_dim / 8, 8, 8], the caller's or one of n_pages pages made here; requests, positions, tables and references are the caller's, as int32
+    device tensors: row0, base and table as for Kv4Cache, and
+
+      refs   [n_pages]      entries of tables that hold a page; zeros at first
+      keep   [n_req, words] rows of tree_mask
+    """
+
+    def __init__(self, n_kv_heads: int, head_dim: int, *, n_layers: int | None = None, n_pages: int | None = None, pool=None, page_size: int = 16, device="cuda"):
+        import torch
+        if pool is not None:
+            assert pool.is_cuda and pool.dtype is torch.bfloat16 and pool.is_contiguous(), "pool: contiguous bf16 on a CUDA device"
+            if pool.dim() == 8:
+                n_layers, n_pages = n_layers or pool.shape[0], n_pages or pool.shape[1]
+        self.n_kv_heads, self.head_dim, self.page_size = n_kv_heads, head_dim, page_size
+        self.n_layers, self.n_pages = 1 if n_layers is None else n_layers, n_pages or 0
+        self._cfgs = {}        # by the width of the page table
+        size = int(lib().pipesd_kv16_pool_bytes(ctypes.byref(self._cfg(1))))
+        if size == 0:
+            raise PipesdError(E_INVALID, "pipesd_kv16_pool_bytes")
+        if pool is None:
+            pool = torch.zeros((self.n_layers, self.n_pages, 2, n_kv_heads, page_size // 8, head_dim // 8, 8, 8), dtype=torch.bfloat16, device=device)
+        assert pool.numel() * 2 == size, f"pool: {size} bytes expected"
+        self.pool = pool
+
+    def _cfg(self, max_pages):
+        cfg = self._cfgs.get(max_pages)
+        if cfg is None:
+            cfg = self._cfgs[max_pages] = Kv16Cfg(self.n_layers, self.n_kv_heads, self.head_dim, self.page_size, self.n_pages, max_pages, 0)
+        return cfg
+
+    def _ints(self, t, n, name):
+        import torch
+        return _vector(t, n, torch.int32, self.pool.device, name)
+
+    def _where(self, rows, row0, base, table):
+        n_req = base.numel()
+        assert table.dim() == 2 and table.shape[0] == n_req, "table: [n_req, max_pages]"
+        return self._cfg(table.shape[1]), (n_req, rows, self._ints(row0, n_req + 1, "row0"), self._ints(base, n_req, "base"),
+                                           self._ints(table, table.numel(), "table"))
+
+    def append(self, k, v, row0, base, table, *, layer: int = 0, stream=None):
+        """Writes the rows k, v [rows, KV heads, head_dim] (fp32 or bf16) into their positions of a layer."""
+        dev = self.pool.device
+        shape = (k.shape[0], self.n_kv_heads, self.head_dim)
+        assert k.shape == shape == v.shape and k.dtype is v.dtype and k.get_device() == dev.index == v.get_device(), f"k, v: two alike of {shape} on {dev}"
+        cfg, where = self._where(k.shape[0], row0, base, table)
+        with _on(dev, stream, self.pool, k, v, row0, base, table) as st:
+            rc = lib().pipesd_kv16_append(ctypes.byref(cfg), self.pool.data_ptr(), layer, k.data_ptr(), v.data_ptr(), _dtype_of(k, "k"), _rows_of(k, "k"),
+                                          _rows_of(v, "v"), *where, st)
+        if rc != OK:
+            raise PipesdError(rc, "pipesd_kv16_append")
+
+    def read(self, rows: int, row0, base, table, *, layer: int = 0, stream=None):
+        """The rows' positions of a layer, bf16 [rows, KV heads, head_dim] of K and of V."""
+        import torch
+        dev = self.pool.device
+        cfg, where = self._where(rows, row0, base, table)
+        on = _on(dev, stream, self.pool, row0, base, table)
+        with on as st:
+            k = torch.empty((rows, self.n_kv_heads, self.head_dim), dtype=torch.bfloat16, device=dev)
+            v = torch.empty_like(k)
+            on.made(k, v)
+            rc = lib().pipesd_kv16_read(ctypes.byref(cfg), self.pool.data_ptr(), layer, k.data_ptr(), v.data_ptr(), *where, st)
+        if rc != OK:
+            raise PipesdError(rc, "pipesd_kv16_read")
+        return k, v
+
+    def attend(self, q, row0, base, table, *, mask=None, layer: int = 0, scale=None, out=None, stream=None):
+        """Attention of the rows q [rows, query heads, head_dim] (fp32 or bf16; appended before): over their requests' positions below base,
+        and the new rows that mask (int32 [rows, words], from tree_mask) names, or, without one, those up to themselves.  scale: head_dim ** -0.5
+        unless given."""
+        import torch
+        dev = self.pool.device
+        assert q.dim() == 3 and q.shape[2] == self.head_dim and q.get_device() == dev.index, f"q: [rows, query heads, {self.head_dim}] on {dev}"
+        rows, heads = q.shape[:2]
+        cfg, where = self._where(rows, row0, base, table)
+        words, bits = 0, None
+        if mask is not None:
+            assert mask.dim() == 2 and mask.shape[0] == rows, "mask: [rows, words]"
+            words, bits = mask.shape[1], self._ints(mask, mask.numel(), "mask")
+        on = _on(dev, stream, self.pool, q, row0, base, table, mask, out)
+        with on as st:
+            if out is None:
+                out = torch.empty_like(q, memory_format=torch.contiguous_format)
+                on.made(out)
+            else:
+                assert out.shape == q.shape and out.dtype is q.dtype and out.get_device() == dev.index, "out: like q"
+            scratch = torch.empty(int(lib().pipesd_kv16_attend_scratch_bytes(ctypes.byref(cfg), rows, heads)) or 16, dtype=torch.uint8, device=dev)
+            rc = lib().pipesd_kv16_attend(ctypes.byref(cfg), self.pool.data_ptr(), layer, q.data_ptr(), out.data_ptr(), _dtype_of(q, "q"), _rows_of(q, "q"),
+                                          _rows_of(out, "out"), heads, self.head_dim ** -0.5 if scale is None else scale, *where, bits, words, scratch.data_ptr(), st)
+        if rc != OK:
+            raise PipesdError(rc, "pipesd_kv16_attend")
+        return out
+
+    def _plan(self, n, table, refs, stream, *given):
+        """(configuration, addresses of table and refs, a stream scope and what makes pages and scratch within it)."""
+        import torch
+        dev = self.pool.device
+        assert table.dim() == 2, "table: [requests, max_pages]"
+        cfg, on = self._cfg(table.shape[1]), _on(dev, stream, self.pool, table, refs, *given)
+
+        def room():
+            pages = torch.empty(n, dtype=torch.int32, device=dev)
+            on.made(pages)
+            return pages, torch.empty(int(lib().pipesd_kv16_plan_scratch_bytes(ctypes.byref(cfg), n)) or 16, dtype=torch.uint8, device=dev)
+
+        return cfg, self._ints(table, table.numel(), "table"), self._ints(refs, self.n_pages, "refs"), on, room
+
+    def reserve(self, length, table, refs, *, stream=None):
+        """Pages for the positions below length [n_req] where the requests' rows of table have none.  Returns how many pages each then has there,
+        -1 where there were not enough (int32 [n_req])."""
+        n = length.numel()
+        assert table.shape[0] == n, "table: [n_req, max_pages]"
+        cfg, tab, ref, on, room = self._plan(n, table, refs, stream, length)
+        with on as st:
+            pages, scratch = room()
+            rc = lib().pipesd_kv16_reserve(ctypes.byref(cfg), n, self._ints(length, n, "length"), tab, ref, pages.data_ptr(), scratch.data_ptr(), st)
+        if rc != OK:
+            raise PipesdError(rc, "pipesd_kv16_reserve")
+        return pages
+
+    def fork(self, src, dst, length, own, table, refs, *, stream=None):
+        """Rows dst of table become continuations of rows src, which hold length positions: pages of positions below own are shared, the others
+        copied.  All int32 [n].  Returns the pages that each has, -1 where there were not enough (int32 [n])."""
+        n = src.numel()
+        cfg, tab, ref, on, room = self._plan(n, table, refs, stream, src, dst, length, own)
+        with on as st:
+            pages, scratch = room()
+            rc = lib().pipesd_kv16_fork(ctypes.byref(cfg), self.pool.data_ptr(), n, *(self._ints(t, n, name) for t, name in
+                                        ((src, "src"), (dst, "dst"), (length, "length"), (own, "own"))), table.shape[0], tab, ref, pages.data_ptr(),
+                                        scratch.data_ptr(), st)
+        if rc != OK:
+            raise PipesdError(rc, "pipesd_kv16_fork")
+        return pages
+
+    def compact(self, keep, base, table, *, stream=None):
+        """Of the rows behind base [n_req], those whose bits are set in keep [n_req, words] move together to base, base + 1, ..., in all layers.
+        Returns how many there are (int32 [n_req])."""
+        import torch
+        dev, n = self.pool.device, base.numel()
+        assert table.dim() == 2 and table.shape[0] == n and keep.dim() == 2 and keep.shape[0] == n, "keep: [n_req, words], table: [n_req, max_pages]"
+        on = _on(dev, stream, self.pool, keep, base, table)
+        with on as st:
+            kept = torch.empty(n, dtype=torch.int32, device=dev)
+            on.made(kept)
+            rc = lib().pipesd_kv16_compact(ctypes.byref(self._cfg(table.shape[1])), self.pool.data_ptr(), n, self._ints(keep, keep.numel(), "keep"), keep.shape[1],
+                                           self._ints(base, n, "base"), self._ints(table, table.numel(), "table"), kept.data_ptr(), st)
+        if rc != OK:
+            raise PipesdError(rc, "pipesd_kv16_compact")
+        return kept
+
+    def release(self, length, table, refs, *, stream=None):
+        """Pages that hold only positions from length [n_req] on leave their rows of table."""
+        n = length.numel()
+        assert table.dim() == 2 and table.shape[0] == n, "table: [n_req, max_pages]"
+        with _on(self.pool.device, stream, self.pool, length, table, refs) as st:
+            rc = lib().pipesd_kv16_release(ctypes.byref(self._cfg(table.shape[1])), n, self._ints(length, n, "length"), self._ints(table, table.numel(), "table"),
+                                           self._ints(refs, self.n_pages, "refs"), st)
+        if rc != OK:
+            raise PipesdError(rc, "pipesd_kv16_release")
 
 
 # ---- the edge-side scheduling model (host code of the library)

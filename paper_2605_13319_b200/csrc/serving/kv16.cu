@@ -1,0 +1,199 @@
+// C entries of the bf16 K/V cache, its pages, and attention in bf16.
+#include <algorithm>
+#include <mutex>
+
+#include "../../../include/pipesd.h"
+#include "attend16.cuh"
+#include "kv16_pages.cuh"
+
+using namespace pipesd;
+
+namespace {
+
+bool cfg_ok(const pipesd_kv16_cfg* c) {
+    return c && (c->head_dim == 64 || c->head_dim == 128) && c->n_kv_heads >= 1 && c->n_kv_heads <= 65535 && c->page_size >= 8 && c->page_size % 8 == 0 &&
+           c->page_size <= 4096 && c->n_pages >= 1 && (int64_t)c->n_pages * c->page_size <= INT32_MAX && c->max_pages >= 1 &&
+           (int64_t)c->max_pages * c->page_size <= (1 << 30) && c->n_layers >= 1 && c->n_layers <= 65535 && c->reserved == 0 &&
+           (double)c->n_layers * c->n_pages * c->page_size * c->n_kv_heads * c->head_dim < 0x1p60;
+}
+bool pool_ok(const pipesd_kv16_cfg* c, const void* pool) { return cfg_ok(c) && pool && (uintptr_t)pool % 16 == 0; }
+bool where_ok(const pipesd_kv16_cfg* c, const void* pool, int32_t layer, int32_t n_req, int32_t rows, const int32_t* row0, const int32_t* base,
+              const int32_t* table) {
+    return pool_ok(c, pool) && layer >= 0 && layer < c->n_layers && n_req >= 1 && rows >= 1 && row0 && base && table;
+}
+Kv4Where where_of(const pipesd_kv16_cfg* c, int n_req, int rows, const int32_t* row0, const int32_t* base, const int32_t* table) {
+    return Kv4Where{row0, base, table, n_req, rows, c->n_pages, c->max_pages, c->page_size, c->n_kv_heads};
+}
+Kv16Pool pool_of(const pipesd_kv16_cfg* c, const void* pool, int layer) {
+    return Kv16Pool{static_cast<uint16_t*>(const_cast<void*>(pool)), c->n_layers, layer, c->head_dim};
+}
+int size_of(int32_t dtype) { return dtype == PIPESD_F32 ? 4 : 2; }
+bool dtype_ok(int32_t dtype) { return dtype == PIPESD_F32 || dtype == PIPESD_BF16; }
+bool aligned(const void* p, int32_t dtype) { return (uintptr_t)p % size_of(dtype) == 0; }
+bool wide(const void* p, int64_t stride, int32_t rows, int32_t dtype) { return (uintptr_t)p % 16 == 0 && (rows == 1 || stride * size_of(dtype) % 16 == 0); }
+int32_t launched() { return cudaGetLastError() == cudaSuccess ? PIPESD_OK : PIPESD_E_CUDA; }
+
+int plan_cap(const pipesd_kv16_cfg* c, int32_t n) { return (int)std::min<int64_t>((int64_t)n * c->max_pages, c->n_pages); }
+
+}  // namespace
+
+extern "C" {
+
+uint64_t pipesd_kv16_pool_bytes(const pipesd_kv16_cfg* cfg) {
+    if (!cfg_ok(cfg)) return 0;
+    return (uint64_t)cfg->n_layers * cfg->n_pages * 2 * cfg->n_kv_heads * cfg->page_size * cfg->head_dim * 2;
+}
+
+int32_t pipesd_kv16_append(const pipesd_kv16_cfg* cfg, void* pool, int32_t layer, const void* k, const void* v, int32_t dtype, int64_t k_stride,
+                           int64_t v_stride, int32_t n_req, int32_t rows, const int32_t* row0, const int32_t* base, const int32_t* table,
+                           void* cuda_stream) {
+    if (!where_ok(cfg, pool, layer, n_req, rows, row0, base, table) || !k || !v || !dtype_ok(dtype) || !aligned(k, dtype) || !aligned(v, dtype))
+        return PIPESD_E_INVALID;
+    const int64_t width = (int64_t)cfg->n_kv_heads * cfg->head_dim;
+    if (rows > 1 && (k_stride < width || v_stride < width)) return PIPESD_E_INVALID;
+    const Kv16RowsArgs a = {where_of(cfg, n_req, rows, row0, base, table), pool_of(cfg, pool, layer), k, v, k_stride, v_stride,
+                            wide(k, k_stride, rows, dtype) && wide(v, v_stride, rows, dtype)};
+    const dim3 grid((unsigned)((rows + kKv16RowWarps - 1) / kKv16RowWarps), (unsigned)cfg->n_kv_heads);
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (cfg->head_dim == 128) {
+        if (dtype == PIPESD_F32) kv16_append_kernel<128, float><<<grid, 32 * kKv16RowWarps, 0, st>>>(a);
+        else kv16_append_kernel<128, uint16_t><<<grid, 32 * kKv16RowWarps, 0, st>>>(a);
+    } else {
+        if (dtype == PIPESD_F32) kv16_append_kernel<64, float><<<grid, 32 * kKv16RowWarps, 0, st>>>(a);
+        else kv16_append_kernel<64, uint16_t><<<grid, 32 * kKv16RowWarps, 0, st>>>(a);
+    }
+    return launched();
+}
+
+int32_t pipesd_kv16_read(const pipesd_kv16_cfg* cfg, const void* pool, int32_t layer, void* k, void* v, int32_t n_req, int32_t rows, const int32_t* row0,
+                         const int32_t* base, const int32_t* table, void* cuda_stream) {
+    if (!where_ok(cfg, pool, layer, n_req, rows, row0, base, table) || !k || !v || (uintptr_t)k % 16 || (uintptr_t)v % 16) return PIPESD_E_INVALID;
+    const Kv16RowsArgs a = {where_of(cfg, n_req, rows, row0, base, table), pool_of(cfg, pool, layer), k, v, 0, 0, 1};
+    const dim3 grid((unsigned)((rows + kKv16RowWarps - 1) / kKv16RowWarps), (unsigned)cfg->n_kv_heads);
+    if (cfg->head_dim == 128) kv16_read_kernel<128><<<grid, 32 * kKv16RowWarps, 0, (cudaStream_t)cuda_stream>>>(a);
+    else kv16_read_kernel<64><<<grid, 32 * kKv16RowWarps, 0, (cudaStream_t)cuda_stream>>>(a);
+    return launched();
+}
+
+int32_t pipesd_tree_mask(int32_t n_req, int32_t rows, const int32_t* row0, const int32_t* parent, int32_t words, uint32_t* mask, int32_t* depth,
+                         void* cuda_stream) {
+    if (n_req < 1 || rows < 1 || !row0 || !parent || !mask || !depth || words < 1 || words > kTreeWords) return PIPESD_E_INVALID;
+    tree_mask_kernel<<<n_req, 256, 0, (cudaStream_t)cuda_stream>>>(row0, parent, n_req, rows, words, mask, depth);
+    return launched();
+}
+
+int32_t pipesd_kv16_compact(const pipesd_kv16_cfg* cfg, void* pool, int32_t n_req, const uint32_t* keep, int32_t words, const int32_t* base,
+                            const int32_t* table, int32_t* kept, void* cuda_stream) {
+    if (!pool_ok(cfg, pool) || n_req < 1 || !keep || words < 1 || words > (1 << 25) || !base || !table || !kept) return PIPESD_E_INVALID;
+    const Kv16CompactArgs a = {where_of(cfg, n_req, 0, nullptr, base, table), pool_of(cfg, pool, 0), keep, words, kept};
+    const int64_t blocks = (int64_t)cfg->n_layers * 2 * cfg->n_kv_heads;
+    if (blocks > INT32_MAX) return PIPESD_E_INVALID;
+    const dim3 grid((unsigned)n_req, (unsigned)std::min<int64_t>((blocks + 7) / 8, 65535));
+    if (cfg->head_dim == 128) kv16_compact_kernel<128><<<grid, 256, 0, (cudaStream_t)cuda_stream>>>(a);
+    else kv16_compact_kernel<64><<<grid, 256, 0, (cudaStream_t)cuda_stream>>>(a);
+    return launched();
+}
+
+uint64_t pipesd_kv16_plan_scratch_bytes(const pipesd_kv16_cfg* cfg, int32_t n) {
+    if (!cfg_ok(cfg) || n < 1) return 0;
+    return 4 * (1 + 2 * (uint64_t)n + 3 * (uint64_t)plan_cap(cfg, n));
+}
+
+int32_t pipesd_kv16_reserve(const pipesd_kv16_cfg* cfg, int32_t n_req, const int32_t* length, int32_t* table, int32_t* refs, int32_t* pages, void* scratch,
+                            void* cuda_stream) {
+    if (!cfg_ok(cfg) || n_req < 1 || !length || !table || !refs || !pages || !scratch || (uintptr_t)scratch % 4) return PIPESD_E_INVALID;
+    const Kv16PlanArgs a = {nullptr, nullptr, length, nullptr, table, refs, pages, n_req, n_req, cfg->n_pages, cfg->max_pages, cfg->page_size,
+                            static_cast<int32_t*>(scratch), plan_cap(cfg, n_req)};
+    kv16_plan_kernel<<<1, kPlanThreads, 0, (cudaStream_t)cuda_stream>>>(a);
+    return launched();
+}
+
+int32_t pipesd_kv16_fork(const pipesd_kv16_cfg* cfg, void* pool, int32_t n, const int32_t* src, const int32_t* dst, const int32_t* length,
+                         const int32_t* own, int32_t n_slots, int32_t* table, int32_t* refs, int32_t* pages, void* scratch, void* cuda_stream) {
+    if (!pool_ok(cfg, pool) || n < 1 || n_slots < 1 || !src || !dst || !length || !own || !table || !refs || !pages || !scratch || (uintptr_t)scratch % 4)
+        return PIPESD_E_INVALID;
+    const Kv16PlanArgs a = {src, dst, length, own, table, refs, pages, n, n_slots, cfg->n_pages, cfg->max_pages, cfg->page_size,
+                            static_cast<int32_t*>(scratch), plan_cap(cfg, n)};
+    kv16_plan_kernel<<<1, kPlanThreads, 0, (cudaStream_t)cuda_stream>>>(a);
+    if (cudaGetLastError() != cudaSuccess) return PIPESD_E_CUDA;
+    const Kv16CopyArgs c = {static_cast<uint4*>(pool), a.scratch, n, a.cap, cfg->n_layers, cfg->n_pages,
+                            (long long)cfg->n_kv_heads * cfg->page_size * cfg->head_dim / 4};
+    if (launch_pdl(kv16_copy_kernel, dim3(148 * 8), dim3(kCopyThreads), 0, (cudaStream_t)cuda_stream, c) != cudaSuccess) return PIPESD_E_CUDA;
+    return launched();
+}
+
+int32_t pipesd_kv16_release(const pipesd_kv16_cfg* cfg, int32_t n_req, const int32_t* length, int32_t* table, int32_t* refs, void* cuda_stream) {
+    if (!cfg_ok(cfg) || n_req < 1 || !length || !table || !refs) return PIPESD_E_INVALID;
+    kv16_release_kernel<<<n_req, 128, 0, (cudaStream_t)cuda_stream>>>(length, table, refs, cfg->n_pages, cfg->max_pages, cfg->page_size);
+    return launched();
+}
+
+uint64_t pipesd_kv16_attend_scratch_bytes(const pipesd_kv16_cfg* cfg, int32_t rows, int32_t n_q_heads) {
+    if (!cfg_ok(cfg) || rows < 1 || n_q_heads < 1 || n_q_heads % cfg->n_kv_heads || n_q_heads / cfg->n_kv_heads > 128) return 0;
+    return 16;
+}
+
+int32_t pipesd_kv16_attend(const pipesd_kv16_cfg* cfg, const void* pool, int32_t layer, const void* q, void* out, int32_t dtype, int64_t q_stride,
+                           int64_t out_stride, int32_t n_q_heads, float scale, int32_t n_req, int32_t rows, const int32_t* row0, const int32_t* base,
+                           const int32_t* table, const uint32_t* mask, int32_t words, void* scratch, void* cuda_stream) {
+    if (!where_ok(cfg, pool, layer, n_req, rows, row0, base, table) || !q || !out || !scratch || (uintptr_t)scratch % 16 || !dtype_ok(dtype) ||
+        !aligned(q, dtype) || !aligned(out, dtype) || n_q_heads < 1 || n_q_heads % cfg->n_kv_heads || n_q_heads / cfg->n_kv_heads > 128 ||
+        !(scale > 0.f && scale < INFINITY) || (mask && (words < 1 || words > kTreeWords)))
+        return PIPESD_E_INVALID;
+    const int64_t width = (int64_t)n_q_heads * cfg->head_dim;
+    if (rows > 1 && (q_stride < width || out_stride < width)) return PIPESD_E_INVALID;
+    if ((int64_t)rows * n_q_heads > INT32_MAX) return PIPESD_E_INVALID;
+    Attend16Args a = {};
+    a.w = where_of(cfg, n_req, rows, row0, base, table);
+    a.p = pool_of(cfg, pool, layer);
+    a.q = q;
+    a.out = out;
+    a.q_stride = q_stride;
+    a.out_stride = out_stride;
+    a.Hq = n_q_heads;
+    a.scale = scale * 1.4426950408889634f;
+    a.mask = mask;
+    a.words = mask ? words : 0;
+    const unsigned grid = (unsigned)(((int64_t)rows * n_q_heads + 3) / 4);
+    cudaStream_t st = (cudaStream_t)cuda_stream;
+    if (cfg->head_dim == 128) {
+        if (dtype == PIPESD_F32) attend16_simple_kernel<128, float, true><<<grid, 128, 0, st>>>(a);
+        else attend16_simple_kernel<128, uint16_t, true><<<grid, 128, 0, st>>>(a);
+    } else {
+        if (dtype == PIPESD_F32) attend16_simple_kernel<64, float, true><<<grid, 128, 0, st>>>(a);
+        else attend16_simple_kernel<64, uint16_t, true><<<grid, 128, 0, st>>>(a);
+    }
+    return launched();
+}
+
+int32_t pipesd_attend_packed(const void* q, const void* k, const void* v, void* out, int64_t q_stride, int64_t k_stride, int64_t v_stride,
+                             int64_t out_stride, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, float scale, int32_t n_req, int32_t rows,
+                             const int32_t* row0, void* cuda_stream) {
+    if (!q || !k || !v || !out || !row0 || (head_dim != 64 && head_dim != 128) || n_kv_heads < 1 || n_kv_heads > 65535 || n_q_heads < 1 ||
+        n_q_heads % n_kv_heads || n_q_heads / n_kv_heads > 128 || !(scale > 0.f && scale < INFINITY) || n_req < 1 || rows < 1)
+        return PIPESD_E_INVALID;
+    const int64_t wq = (int64_t)n_q_heads * head_dim, wkv = (int64_t)n_kv_heads * head_dim;
+    if ((int64_t)rows * n_q_heads > INT32_MAX) return PIPESD_E_INVALID;
+    for (const void* p : {q, k, v, (const void*)out})
+        if ((uintptr_t)p % 16) return PIPESD_E_INVALID;
+    if (rows > 1 && (q_stride < wq || k_stride < wkv || v_stride < wkv || out_stride < wq || q_stride % 8 || k_stride % 8 || v_stride % 8 || out_stride % 8))
+        return PIPESD_E_INVALID;
+    Attend16Args a = {};
+    a.w = Kv4Where{row0, nullptr, nullptr, n_req, rows, 0, 0, 0, n_kv_heads};
+    a.k = static_cast<const uint16_t*>(k);
+    a.v = static_cast<const uint16_t*>(v);
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    a.q = q;
+    a.out = out;
+    a.q_stride = q_stride;
+    a.out_stride = out_stride;
+    a.Hq = n_q_heads;
+    a.scale = scale * 1.4426950408889634f;
+    const unsigned grid = (unsigned)(((int64_t)rows * n_q_heads + 3) / 4);
+    if (head_dim == 128) attend16_simple_kernel<128, uint16_t, false><<<grid, 128, 0, (cudaStream_t)cuda_stream>>>(a);
+    else attend16_simple_kernel<64, uint16_t, false><<<grid, 128, 0, (cudaStream_t)cuda_stream>>>(a);
+    return launched();
+}
+
+}  // extern "C"

@@ -15,7 +15,7 @@
 // times 2^-24 (subnormals: the exponent fields 0 and 1 are one linear range), so that a code needs one AND (and a shift for
 // every second one) and no conversion.  The factor 16 of the odd nibbles goes into Q, or into the step that centres V's codes.
 #pragma once
-#include "../common.cuh"
+#include "where.cuh"
 
 namespace pipesd {
 
@@ -27,21 +27,6 @@ __host__ __device__ constexpr int kv4_unit_bytes(int hd) { return 20 * hd; }
 __host__ __device__ constexpr int kv4_k_scales(int hd) { return 8 * hd; }
 __host__ __device__ constexpr int kv4_v_codes(int hd) { return 10 * hd; }
 __host__ __device__ constexpr int kv4_v_scales(int hd) { return 18 * hd; }
-
-// Where the requests of a call are: request r has the rows row0[r] .. row0[r + 1] - 1, at the positions base[r] ... of its pages.
-struct Kv4Where {
-    const int32_t *row0, *base, *table;
-    int n_req, rows, n_pages, max_pages, page_size, Hkv;
-};
-
-// New rows and base of a request; a request whose numbers make no sense has none.
-__device__ __forceinline__ int kv4_rows(const Kv4Where& w, int r, int& first, int& base) {
-    first = w.row0[r];
-    base = w.base[r];
-    const int end = w.row0[r + 1];
-    if (first < 0 || end < first || end > w.rows || base < 0) return 0;
-    return min(end - first, max(0, w.max_pages * w.page_size - base));      // rows behind the table's last position are dropped
-}
 
 // Address of a unit of a request, or null where no page is mapped.
 __device__ __forceinline__ unsigned char* kv4_unit(unsigned char* pool, const Kv4Where& w, int r, int head, int unit, int hd) {
