@@ -1,0 +1,330 @@
+// Causal attention of prompts packed one behind the other: out[i] = sum over j <= i of the prompt of softmax_j(scale q_i.k_j) v_j.
+//
+// Rows of a tile are (token, query head of the KV head's group) pairs, so that every tile reads one KV head's keys once for all of the group: T = 128 / G
+// tokens by G heads, rounded down (G = 3: 126 rows of 128).  A job is two such tiles, 2 T consecutive tokens of a prompt by one KV head, each with a
+// stream of its own (attend16_tile.cuh); both read the same keys and values, 128 at a time, from the first up to their last token.
+// A CTA per SM takes jobs in turn: sorted by length (block of tokens, last first; then prompts, then heads), dealt out back and forth, so that the CTAs'
+// sums differ by less than a job.  Nothing is shared between CTAs: no atomics, no scratch.
+// Warps: 0-3 and 4-7 the streams' rows, 8 fetches (copy engine, 128-byte swizzle), 9 issues the products.
+#pragma once
+#include "attend16_tile.cuh"
+
+namespace pipesd {
+
+struct PromptArgs {
+    const int32_t* row0;
+    const uint16_t* v;
+    uint16_t* out;
+    long long v_stride, out_stride;
+    int n_req, rows, Hq, Hkv;
+    float scale;                // times log2(e)
+    int ctas;
+};
+struct PromptJob {
+    int first, n, t0, head;     // the prompt's first row and length (0: no more jobs), the job's first token
+};
+constexpr int kPromptThreads = 320, kPromptJobs = 2;
+
+struct PromptControl {
+    unsigned long long q_full, q_empty, full[16], empty[16], s_full[2], p_full[2], o_full[2], done;
+    PromptJob jobs[kPromptJobs];
+    int flags[kPromptJobs];     // a value of the job's last tiles was not finite
+    uint32_t tmem;
+    int dead;
+};
+template <int HD>
+struct PromptShape {
+    static constexpr int kTile = 128 * HD * 2, kStages = HD == 128 ? 5 : 8;
+    static constexpr int kSmem = 1024 + (2 + kStages) * kTile + (int)sizeof(PromptControl);
+};
+
+__device__ __forceinline__ void tensor3_g2s(uint32_t dst_smem, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst_smem), "l"(map),
+                 "r"(bar), "r"(x), "r"(y), "r"(z)
+                 : "memory");
+}
+
+// Tokens of prompt r (0 where its entries make no sense).
+__device__ __forceinline__ int prompt_len(const PromptArgs& a, int r, int& first) {
+    first = a.row0[r];
+    const int end = a.row0[r + 1];
+    return first < 0 || end < first || end > a.rows ? 0 : end - first;
+}
+// Blocks of `block` tokens with an index of `level` or more, over all prompts (whole warp).
+__device__ __forceinline__ int prompt_blocks_from(const PromptArgs& a, int level, int block) {
+    int sum = 0;
+    for (int r = threadIdx.x & 31; r < a.n_req; r += 32) {
+        int first;
+        const int b = (prompt_len(a, r, first) + block - 1) / block;
+        sum += max(0, b - level);
+    }
+    return __reduce_add_sync(0xffffffffu, sum);
+}
+// Job of a rank, longest first (whole warp).  n = 0: there are not as many.
+__device__ __forceinline__ PromptJob prompt_job(const PromptArgs& a, long long rank, int block, int levels) {
+    PromptJob job = {0, 0, 0, 0};
+    const int lane = threadIdx.x & 31;
+    int lo = 0, hi = levels;                       // the largest level that at least rank + 1 jobs reach
+    if ((long long)prompt_blocks_from(a, 0, block) * a.Hkv <= rank) return job;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if ((long long)prompt_blocks_from(a, mid, block) * a.Hkv > rank) lo = mid;
+        else hi = mid;
+    }
+    const int index = (int)(rank - (long long)prompt_blocks_from(a, lo + 1, block) * a.Hkv);
+    int left = index / a.Hkv;
+    job.head = index % a.Hkv;
+    for (int r0 = 0; r0 < a.n_req; r0 += 32) {
+        int first = 0, n = 0;
+        if (r0 + lane < a.n_req) n = prompt_len(a, r0 + lane, first);
+        const unsigned reach = __ballot_sync(0xffffffffu, n > lo * block);
+        if (left < __popc(reach)) {
+            const unsigned mine = __ballot_sync(0xffffffffu, (reach >> lane & 1u) && __popc(reach & ((1u << lane) - 1)) == left);
+            const int l = __ffs(mine) - 1;
+            job.first = __shfl_sync(0xffffffffu, first, l);
+            job.n = __shfl_sync(0xffffffffu, n, l);
+            job.t0 = lo * block;
+            return job;
+        }
+        left -= __popc(reach);
+    }
+    return job;
+}
+// Tiles of 128 keys that stream s of a job goes through.
+__device__ __forceinline__ int prompt_tiles(const PromptJob& job, int s, int T) {
+    const int t = job.t0 + s * T;
+    return t >= job.n ? 0 : (min(t + T, job.n) + 127) >> 7;
+}
+
+template <int HD>
+__global__ void __launch_bounds__(kPromptThreads, 1)
+    prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const PromptArgs a) {
+    using Shape = PromptShape<HD>;
+    constexpr int kTile = Shape::kTile, kStages = Shape::kStages, kAtom = 128 * 128;      // an atom: 128 rows of 64 columns
+    constexpr uint32_t kIdescS = umma_idesc_bf16(128, 128, 0, 0), kIdescO = umma_idesc_bf16(128, HD, 0, 1);
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    unsigned char* const ring = smem + 2 * kTile;
+    PromptControl& c = *reinterpret_cast<PromptControl*>(ring + kStages * kTile);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int G = a.Hq / a.Hkv, T = 128 / G;
+    volatile int* const dead = &c.dead;
+
+    if (tid == 0) {
+        mbar_init(smem_u32(&c.q_full), 1);
+        mbar_init(smem_u32(&c.q_empty), 9);      // the products, and the streams' warps when they have read the job
+        mbar_init(smem_u32(&c.done), 1);
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(smem_u32(&c.full[i]), 1);
+            mbar_init(smem_u32(&c.empty[i]), 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(smem_u32(&c.s_full[s]), 1);
+            mbar_init(smem_u32(&c.p_full[s]), 4);
+            mbar_init(smem_u32(&c.o_full[s]), 1);
+        }
+        c.dead = 0;
+        fence_mbar_init();
+    }
+    if (warp == 9) tmem_alloc(smem_u32(&c.tmem), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = c.tmem;                  // stream s: scores and weights at 128 s, sums at 256 + HD s
+
+    if (warp == 8) {                               // ---- fetches
+        int levels = 0;
+        for (int r = lane; r < a.n_req; r += 32) {
+            int first;
+            levels = max(levels, (prompt_len(a, r, first) + 2 * T - 1) / (2 * T));
+        }
+        levels = __reduce_max_sync(0xffffffffu, levels);
+        uint32_t entry = 0;                        // of the ring, over all jobs
+        bool ok = true;
+        for (int i = 0; ok; ++i) {
+            const long long round = (long long)i * a.ctas;
+            const PromptJob job = prompt_job(a, i & 1 ? round + a.ctas - 1 - blockIdx.x : round + blockIdx.x, 2 * T, levels);
+            if (i > 0) ok = warp_wait(smem_u32(&c.q_empty), (i - 1) & 1, dead);
+            if (lane == 0 && ok) {
+                c.jobs[i % kPromptJobs] = job;
+                c.flags[i % kPromptJobs] = 0;
+                if (job.n == 0) {
+                    mbar_arrive(smem_u32(&c.q_full));
+                } else {
+                    const int tiles[2] = {prompt_tiles(job, 0, T), prompt_tiles(job, 1, T)};
+                    const uint32_t bar = smem_u32(&c.q_full);
+                    mbar_expect_tx(bar, (uint32_t)((tiles[1] ? 2 : 1) * (HD / 64) * T * G * 128));
+                    for (int s = 0; s < 2; ++s)
+                        for (int x = 0; tiles[s] && x < HD / 64; ++x)
+                            tensor3_g2s(smem_u32(smem + s * kTile + x * kAtom), &map_q, 64 * x, job.head * G, job.first + job.t0 + s * T, bar);
+                    const int n = max(tiles[0], tiles[1]);
+                    for (int e = 0; e < 2 * n && ok; ++e, ++entry) {
+                        const int st = entry % kStages;
+                        if (entry >= kStages) ok = role_wait(smem_u32(&c.empty[st]), (entry / kStages - 1) & 1, dead);
+                        if (!ok) break;
+                        const uint32_t full = smem_u32(&c.full[st]);
+                        mbar_expect_tx(full, kTile);
+                        for (int x = 0; x < HD / 64; ++x)
+                            tensor3_g2s(smem_u32(ring + st * kTile + x * kAtom), e & 1 ? &map_v : &map_k, 64 * x, job.head, job.first + (e >> 1) * 128, full);
+                    }
+                }
+            }
+            ok = __shfl_sync(0xffffffffu, ok, 0);
+            entry = __shfl_sync(0xffffffffu, entry, 0);
+            if (job.n == 0) break;
+        }
+        if (!ok && lane == 0) {                    // given up: the copies in flight are waited for
+            for (uint32_t e = entry > kStages ? entry - kStages : 0; e < entry; ++e) mbar_wait(smem_u32(&c.full[e % kStages]), (e / kStages) & 1);
+        }
+    } else if (warp == 9) {                        // ---- products
+        if (lane == 0) {
+            uint32_t entry = 0;
+            bool ok = true;
+            auto scores = [&](int s, uint32_t e) {
+                const uint32_t q = smem_u32(smem + s * kTile), k = smem_u32(ring + e % kStages * kTile);
+#pragma unroll
+                for (int x = 0; x < HD / 16; ++x) {
+                    const uint32_t at = (x >> 2) * kAtom + (x & 3) * 32;
+                    umma_bf16(tmem + 128 * s, umma_desc_swizzled(q + at, 16, 1024), umma_desc_swizzled(k + at, 16, 1024), kIdescS, x > 0);
+                }
+                umma_commit(smem_u32(&c.s_full[s]));
+            };
+            uint32_t p_phase[2] = {0, 0};
+            auto sums = [&](int s, uint32_t e, bool first, bool last) {
+                ok = ok && role_wait(smem_u32(&c.p_full[s]), p_phase[s], dead);
+                p_phase[s] ^= 1;
+                if (!ok) return;
+                tc_fence_after();
+                const uint32_t v = smem_u32(ring + e % kStages * kTile);
+#pragma unroll
+                for (int x = 0; x < 8; ++x)
+                    umma_bf16_ta(tmem + 256 + HD * s, tmem + 128 * s + 8 * x, umma_desc_swizzled(v + x * 2048, kAtom, 1024), kIdescO, !first || x > 0);
+                if (last) umma_commit(smem_u32(&c.o_full[s]));
+            };
+            auto arrived = [&](uint32_t e) { ok = ok && role_wait(smem_u32(&c.full[e % kStages]), (e / kStages) & 1, dead); };
+            for (int i = 0; ok; ++i) {
+                ok = role_wait(smem_u32(&c.q_full), i & 1, dead);
+                if (!ok) break;
+                const PromptJob job = c.jobs[i % kPromptJobs];
+                if (job.n == 0) break;
+                const int n0 = prompt_tiles(job, 0, T), n1 = prompt_tiles(job, 1, T), n = max(n0, n1);
+                arrived(entry);
+                if (!ok) break;
+                tc_fence_after();
+                scores(0, entry);
+                if (n1) scores(1, entry);
+                umma_commit(smem_u32(&c.empty[entry % kStages]));
+                if (n == 1) umma_commit(smem_u32(&c.q_empty));
+                for (int j = 0; j < n && ok; ++j) {
+                    const uint32_t ev = entry + 2 * j + 1, ek = ev + 1;
+                    arrived(ev);
+                    if (ok && j < n0) sums(0, ev, j == 0, j == n0 - 1);
+                    if (j + 1 < n) arrived(ek);
+                    if (ok && j + 1 < n0) scores(0, ek);
+                    if (ok && j < n1) sums(1, ev, j == 0, j == n1 - 1);
+                    if (!ok) break;
+                    umma_commit(smem_u32(&c.empty[ev % kStages]));
+                    if (j + 1 < n1) scores(1, ek);
+                    if (j + 1 < n) umma_commit(smem_u32(&c.empty[ek % kStages]));
+                    if (j + 2 == n) umma_commit(smem_u32(&c.q_empty));
+                }
+                entry += 2 * n;
+            }
+        }
+        __syncwarp();
+    } else {                                       // ---- a stream's rows
+        const int s = warp >> 2, row = tid & 127, token = row / G, g = row % G;
+        const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16, s_tmem = tmem + 128 * s + lanes, o_tmem = tmem + 256 + HD * s + lanes;
+        uint32_t entry = 0, s_phase = 0, o_phase = 0;
+        for (int i = 0;; ++i) {
+            if (!warp_wait(smem_u32(&c.q_full), i & 1, dead)) break;
+            const PromptJob job = c.jobs[i % kPromptJobs];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&c.q_empty));
+            if (job.n == 0) break;
+            const int tiles = prompt_tiles(job, s, T), all = max(prompt_tiles(job, 0, T), prompt_tiles(job, 1, T));
+            const int t = job.t0 + s * T + token;  // this row's token
+            const int clear = (job.t0 + s * T + 1) >> 7;                       // tiles that every row sees whole
+            float ref = -INFINITY, sum = 0.f;
+            bool ok = true;
+            for (int j = 0; j < tiles; ++j) {
+                uint32_t see[4];
+                const bool masked = j >= clear;
+                if (masked) {
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const int n = t + 1 - (j * 128 + 32 * w);
+                        see[w] = n >= 32 ? 0xffffffffu : (n <= 0 ? 0u : (1u << n) - 1u);
+                    }
+                }
+                ok = warp_wait(smem_u32(&c.s_full[s]), s_phase, dead);
+                s_phase ^= 1;
+                if (!ok) break;
+                tc_fence_after();
+                softmax_tile<HD, 128, 1>(s_tmem, o_tmem, a.scale, j == 0, masked, see, ref, sum);
+                if (masked) {
+                    const uint32_t ev = entry + 2 * j + 1;
+                    ok = warp_wait(smem_u32(&c.full[ev % kStages]), (ev / kStages) & 1, dead);
+                    if (!ok) break;
+                    if (clean_values(ring + ev % kStages * kTile, kTile / 16, job.n - j * 128, row, 128, [](int p) { return (p >> 3) & 127; })) {
+                        *(volatile int*)&c.flags[i % kPromptJobs] = 1;
+                        __threadfence_block();
+                    }
+                    fence_proxy_async_smem();
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&c.p_full[s]));
+            }
+            entry += 2 * all;
+            if (tiles == 0) continue;
+            if (ok) {
+                ok = warp_wait(smem_u32(&c.o_full[s]), o_phase, dead);
+                o_phase ^= 1;
+            }
+            const bool mine = token < T && t < job.n;
+            uint16_t* const out = a.out + (long long)(job.first + t) * a.out_stride + (job.head * G + g) * HD;
+            if (!ok) {                             // a copy or a product that never came: no result
+                if (mine)
+                    for (int d = 0; d < HD; ++d) out[d] = 0x7fff;
+                break;
+            }
+            tc_fence_after();
+            const bool fix = *(volatile int*)&c.flags[i % kPromptJobs];
+            const float inv = sum > 0.f ? 1.f / sum : sum;
+#pragma unroll 1
+            for (int d = 0; d < HD; d += 32) {
+                uint32_t o[32];
+                tmem_ld32(o_tmem + d, o);
+                tmem_ld_wait32(o);
+                if (mine) {
+                    uint32_t bad = 0;
+                    if (fix)
+                        for (int p = job.t0 >> 7 << 7; p <= t; ++p) bad |= not_finite32(a.v + (long long)(job.first + p) * a.v_stride + job.head * HD + d, 8);
+#pragma unroll
+                    for (int x = 0; x < 32; x += 8) {
+                        float y[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) y[e] = bad >> (x + e) & 1u ? __uint_as_float(0x7fffffffu) : __uint_as_float(o[x + e]) * inv;
+                        *reinterpret_cast<uint4*>(out + d + x) =
+                            make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
+                    }
+                }
+                __syncwarp();
+            }
+            tc_fence_before();
+        }
+    }
+    __syncthreads();
+    if (warp == 9) {
+        if (c.dead && lane == 0) {                 // products in flight end before their memory is given back
+            umma_commit(smem_u32(&c.done));
+            mbar_wait(smem_u32(&c.done), 0);
+        }
+        __syncwarp();
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+}  // namespace pipesd

@@ -1,0 +1,201 @@
+// What both bf16 attention kernels (prompts, pages) do with a tile of 128 query rows by kKeys keys on the 5th-generation tensor cores.
+//
+//   S[128 x kKeys] = Q K^T        both operands in shared memory, fp32 scores in tensor memory, a lane per query row
+//   P = exp2(scale S - ref)       one thread per row: its scores in registers, no exchange between threads.  ref is the row's running
+//                                 maximum as of the last time it rose by more than 2^8 in weight: O and the sum are rescaled only then, so that
+//                                 P <= 2^8, and hardly ever behind a row's first tile
+//   O[128 x HD] += P V            P as bf16 in tensor memory (over the scores it was made of), V in shared memory, fp32 sums in tensor memory
+//
+// Two such streams per CTA, each with four warps of its own, keep the tensor cores at the one's products while the other's exponentials are taken.
+#pragma once
+#include "../tcgen05.cuh"
+
+namespace pipesd {
+
+// ---- instructions that tcgen05.cuh does not have
+// Shared-memory operand descriptor of tiles in the copy engine's 128-byte swizzle: rows of 128 bytes in groups of eight (1024 bytes), 16-byte pieces
+// exchanged by the row's number in its group.  K-major: sbo = bytes between groups of eight rows (lbo is not used).  MN-major: a row holds
+// 64 neighbouring columns of one k; lbo = bytes between blocks of 64 columns, sbo = between groups of eight k.
+__device__ __forceinline__ uint64_t umma_desc_swizzled(uint32_t saddr, uint32_t lbo_bytes, uint32_t sbo_bytes) {
+    return umma_desc(saddr, lbo_bytes, sbo_bytes) | (2ull << 61);
+}
+// D[tmem] (+)= A[tmem] . B[smem], one k16 step (A: 8 columns of bf16 pairs); issued by ONE thread.
+__device__ __forceinline__ void umma_bf16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t"
+        ".reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t"
+        "}\n"
+        :
+        : "r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+#define PIPESD_R8(u, i) "=r"(u[i]), "=r"(u[i + 1]), "=r"(u[i + 2]), "=r"(u[i + 3]), "=r"(u[i + 4]), "=r"(u[i + 5]), "=r"(u[i + 6]), "=r"(u[i + 7])
+#define PIPESD_IN8(u, i) "r"(u[i]), "r"(u[i + 1]), "r"(u[i + 2]), "r"(u[i + 3]), "r"(u[i + 4]), "r"(u[i + 5]), "r"(u[i + 6]), "r"(u[i + 7])
+#define PIPESD_RW8(u, i) "+r"(u[i]), "+r"(u[i + 1]), "+r"(u[i + 2]), "+r"(u[i + 3]), "+r"(u[i + 4]), "+r"(u[i + 5]), "+r"(u[i + 6]), "+r"(u[i + 7])
+// 32 consecutive columns of this thread's lane, as bits; whole warp, same address.
+__device__ __forceinline__ void tmem_ld32(uint32_t taddr, uint32_t* u) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, "
+        "%23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : PIPESD_R8(u, 0), PIPESD_R8(u, 8), PIPESD_R8(u, 16), PIPESD_R8(u, 24)
+        : "r"(taddr));
+}
+__device__ __forceinline__ void tmem_st32(uint32_t taddr, const uint32_t* u) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, %22, "
+        "%23, %24, %25, %26, %27, %28, %29, %30, %31, %32};" ::"r"(taddr),
+        PIPESD_IN8(u, 0), PIPESD_IN8(u, 8), PIPESD_IN8(u, 16), PIPESD_IN8(u, 24)
+        : "memory");
+}
+// Waits for the loads before it; u names registers of theirs, so that no use of these moves ahead of the wait.
+__device__ __forceinline__ void tmem_ld_wait32(uint32_t* u) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : PIPESD_RW8(u, 0), PIPESD_RW8(u, 8), PIPESD_RW8(u, 16), PIPESD_RW8(u, 24)::"memory");
+}
+__device__ __forceinline__ float exp2_approx(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float x, float y) {      // the first in the low half
+    const __nv_bfloat162 h = __floats2bfloat162_rn(x, y);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+// ---- waits: bounded, and given up at once when another role of the CTA has given up
+__device__ __forceinline__ bool role_wait(uint32_t bar, uint32_t parity, volatile int* dead) {
+    uint64_t t0 = 0;
+    for (uint32_t it = 0;; ++it) {
+        uint32_t ok;
+        asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n selp.u32 %0, 1, 0, p;\n}"
+                     : "=r"(ok)
+                     : "r"(bar), "r"(parity)
+                     : "memory");
+        if (ok) return true;
+        if ((it & 255u) == 255u) {
+            if (*dead) return false;
+            const uint64_t now = global_ns();
+            if (t0 == 0) t0 = now;
+            else if (now - t0 > 2000000000ull) {
+                *dead = 1;
+                return false;
+            }
+        }
+    }
+}
+
+// The same for a whole warp, which goes on together.
+__device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* dead) { return __all_sync(0xffffffffu, role_wait(bar, parity, dead)); }
+
+constexpr float kRefExcess = 8.f;                  // log2 units by which a weight may exceed 1
+
+// One row's share of a tile.  `o_tmem`: the row's running sums, rescaled here if they have to be; `first`: there are none yet.  masked: bit c of `see`
+// says whether key c is seen; the others' scores are replaced, whatever they are.
+template <int HD, int kKeys, int kTerms>
+__device__ __forceinline__ void softmax_tile(uint32_t s_tmem, uint32_t o_tmem, float scale, bool first, bool masked, const uint32_t (&see)[kKeys / 32], float& ref,
+                                             float& sum) {
+    uint32_t s[kKeys];
+#pragma unroll
+    for (int i = 0; i < kKeys; i += 32) tmem_ld32(s_tmem + i, s + i);
+#pragma unroll
+    for (int i = 0; i < kKeys; i += 32) tmem_ld_wait32(s + i);
+    if (masked) {
+#pragma unroll
+        for (int i = 0; i < kKeys; ++i)
+            if (!(see[i / 32] >> (i % 32) & 1u)) s[i] = 0xff800000u;
+    }
+    float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+    for (int i = 0; i < kKeys; ++i) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(s[i]));
+    const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
+    const bool up = top > ref + kRefExcess || (ref == -INFINITY && top > ref);
+    if (__any_sync(0xffffffffu, up)) {
+        const float next = up ? top : ref, factor = up ? exp2_approx(ref - next) : 1.f;
+        ref = next;
+        sum *= factor;
+        if (!first) {
+#pragma unroll 1
+            for (int c = 0; c < HD; c += 32) {
+                uint32_t o[32];
+                tmem_ld32(o_tmem + c, o);
+                tmem_ld_wait32(o);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * factor);
+                tmem_st32(o_tmem + c, o);
+            }
+        }
+    }
+    const float shift = ref == -INFINITY ? 0.f : -ref;
+    float part[4] = {};
+#pragma unroll
+    for (int i = 0; i < kKeys; ++i) {
+        const float p = exp2_approx(fmaf(__uint_as_float(s[i]), scale, shift));
+        part[i & 3] += p;
+        s[i] = __float_as_uint(p);
+    }
+    sum += (part[0] + part[1]) + (part[2] + part[3]);
+#pragma unroll
+    for (int t = 0; t < kTerms; ++t) {
+        uint32_t p[kKeys / 2];
+#pragma unroll
+        for (int i = 0; i < kKeys / 2; ++i) {
+            const float x = __uint_as_float(s[2 * i]), y = __uint_as_float(s[2 * i + 1]);
+            p[i] = pack_bf16(x, y);
+            if (t + 1 < kTerms) {                  // what the term leaves, exactly
+                s[2 * i] = __float_as_uint(x - __uint_as_float(p[i] << 16));
+                s[2 * i + 1] = __float_as_uint(y - __uint_as_float(p[i] & 0xffff0000u));
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kKeys / 2; i += 32) tmem_st32(s_tmem + t * (kKeys / 2) + i, p + i);
+    }
+    tmem_st_wait();
+}
+
+// Values of a tile that no row may take into its products: rows from `limit` on, and what is not finite.  A weight of 0 does not keep them out, so they
+// are 0 in shared memory.  `pieces` 16-byte pieces, key_of(piece) its row; threads of one stream.  True if something was not finite.
+template <typename KeyOf>
+__device__ __forceinline__ bool clean_values(unsigned char* tile, int pieces, int limit, int tid, int n_thr, KeyOf key_of) {
+    bool found = false;
+    for (int i = tid; i < pieces; i += n_thr) {
+        uint4* const at = reinterpret_cast<uint4*>(tile) + i;
+        if (key_of(i) >= limit) {
+            *at = make_uint4(0, 0, 0, 0);
+            continue;
+        }
+        uint4 x = *at;
+        uint32_t* const w = reinterpret_cast<uint32_t*>(&x);
+        uint32_t bad = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) bad |= ((w[j] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+        if (bad) {
+            found = true;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t b = ((w[j] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+                if (b & 0x8000u) w[j] &= 0xffff0000u;
+                if (b & 0x80000000u) w[j] &= 0x0000ffffu;
+            }
+            *at = x;
+        }
+    }
+    return found;
+}
+// Bits of the 32 columns behind p whose value is not finite.
+__device__ __forceinline__ uint32_t not_finite32(const uint16_t* p, int piece_stride) {
+    uint32_t bits = 0;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        const uint4 x = *reinterpret_cast<const uint4*>(p + c * piece_stride);
+        const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            if ((w[j] & 0x7f80u) == 0x7f80u) bits |= 1u << (8 * c + 2 * j);
+            if ((w[j] & 0x7f800000u) == 0x7f800000u) bits |= 2u << (8 * c + 2 * j);
+        }
+    }
+    return bits;
+}
+
+}  // namespace pipesd

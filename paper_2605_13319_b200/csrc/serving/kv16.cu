@@ -4,6 +4,7 @@
 
 #include "../../../include/pipesd.h"
 #include "attend16.cuh"
+#include "attend16_prompt.cuh"
 #include "kv16_pages.cuh"
 
 using namespace pipesd;
@@ -34,6 +35,37 @@ bool wide(const void* p, int64_t stride, int32_t rows, int32_t dtype) { return (
 int32_t launched() { return cudaGetLastError() == cudaSuccess ? PIPESD_OK : PIPESD_E_CUDA; }
 
 int plan_cap(const pipesd_kv16_cfg* c, int32_t n) { return (int)std::min<int64_t>((int64_t)n * c->max_pages, c->n_pages); }
+
+// [rows, heads, head_dim] with `stride` elements between rows, fetched in boxes of 64 columns x box_heads x box_rows; rows behind the last read as 0.
+bool rows_map(CUtensorMap* m, const void* base, int hd, int heads, int64_t rows, int64_t stride, int box_heads, int box_rows) {
+    using Encode = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+    static const Encode encode = [] {
+        void* fn = nullptr;
+        cudaDriverEntryPointQueryResult found;
+        const cudaError_t e = cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &fn, 12000, cudaEnableDefault, &found);
+        return e == cudaSuccess && found == cudaDriverEntryPointSuccess ? (Encode)fn : (Encode) nullptr;
+    }();
+    if (!encode) return false;
+    const cuuint64_t dims[3] = {(cuuint64_t)hd, (cuuint64_t)heads, (cuuint64_t)rows}, strides[2] = {(cuuint64_t)hd * 2, (cuuint64_t)stride * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_rows}, ones[3] = {1, 1, 1};
+    return encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                  CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+// Shared-memory limits belong to a device: set once for each, with that device current.
+constexpr int kDevices = 64, kSms = 148;
+std::mutex g_mu;
+bool g_ready[kDevices] = {false};
+bool device_ready() {
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices) return false;
+    std::lock_guard<std::mutex> lock(g_mu);
+    if (!g_ready[dev])
+        g_ready[dev] = cudaFuncSetAttribute((const void*)prompt_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, PromptShape<64>::kSmem) == cudaSuccess &&
+                       cudaFuncSetAttribute((const void*)prompt_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, PromptShape<128>::kSmem) == cudaSuccess;
+    return g_ready[dev];
+}
 
 }  // namespace
 
@@ -178,21 +210,19 @@ int32_t pipesd_attend_packed(const void* q, const void* k, const void* v, void* 
         if ((uintptr_t)p % 16) return PIPESD_E_INVALID;
     if (rows > 1 && (q_stride < wq || k_stride < wkv || v_stride < wkv || out_stride < wq || q_stride % 8 || k_stride % 8 || v_stride % 8 || out_stride % 8))
         return PIPESD_E_INVALID;
-    Attend16Args a = {};
-    a.w = Kv4Where{row0, nullptr, nullptr, n_req, rows, 0, 0, 0, n_kv_heads};
-    a.k = static_cast<const uint16_t*>(k);
-    a.v = static_cast<const uint16_t*>(v);
-    a.k_stride = k_stride;
-    a.v_stride = v_stride;
-    a.q = q;
-    a.out = out;
-    a.q_stride = q_stride;
-    a.out_stride = out_stride;
-    a.Hq = n_q_heads;
-    a.scale = scale * 1.4426950408889634f;
-    const unsigned grid = (unsigned)(((int64_t)rows * n_q_heads + 3) / 4);
-    if (head_dim == 128) attend16_simple_kernel<128, uint16_t, false><<<grid, 128, 0, (cudaStream_t)cuda_stream>>>(a);
-    else attend16_simple_kernel<64, uint16_t, false><<<grid, 128, 0, (cudaStream_t)cuda_stream>>>(a);
+    if (!device_ready()) return PIPESD_E_CUDA;
+    if (rows == 1) { q_stride = out_stride = wq; k_stride = v_stride = wkv; }
+    const int G = n_q_heads / n_kv_heads, T = 128 / G;
+    CUtensorMap mq, mk, mv;
+    if (!rows_map(&mq, q, head_dim, n_q_heads, rows, q_stride, G, T) || !rows_map(&mk, k, head_dim, n_kv_heads, rows, k_stride, 1, 128) ||
+        !rows_map(&mv, v, head_dim, n_kv_heads, rows, v_stride, 1, 128))
+        return PIPESD_E_INVALID;
+    // the jobs there can be: a prompt's last one may be short
+    const int64_t jobs = ((int64_t)rows / (2 * T) + std::min(n_req, rows)) * n_kv_heads;
+    const PromptArgs a = {row0,    static_cast<const uint16_t*>(v), static_cast<uint16_t*>(out), v_stride, out_stride, n_req, rows, n_q_heads, n_kv_heads,
+                          scale * 1.4426950408889634f, (int)std::min<int64_t>(jobs, kSms)};
+    if (head_dim == 128) prompt_kernel<128><<<a.ctas, kPromptThreads, PromptShape<128>::kSmem, (cudaStream_t)cuda_stream>>>(mq, mk, mv, a);
+    else prompt_kernel<64><<<a.ctas, kPromptThreads, PromptShape<64>::kSmem, (cudaStream_t)cuda_stream>>>(mq, mk, mv, a);
     return launched();
 }
 
