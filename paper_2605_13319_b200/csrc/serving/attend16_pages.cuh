@@ -1,0 +1,659 @@
+// Attention of every request's new rows over its pages: positions in front of base, and of the new rows those that the row's mask names.
+//
+// Rows of a tile are (new row, query head of the KV head's group) pairs.  Work: the key tiles of all (request, KV head, row group) triples in a
+// row, cut into equal ranges, one per CTA (one CTA per SM).  A triple that one CTA has whole is finished there; of others each CTA leaves its sums, which
+// pages_merge_kernel adds up in CTA order.  No atomics, no state between calls.
+// A row group has up to 256 rows in bf16.  More than 128: the CTA's two streams (attend16_tile.cuh) have 128 rows each and go through the same
+// tiles; fewer: both have the same rows and take the tiles in turn, and their sums are joined at the end -- in tensor memory, where each stream
+// reads the other's, half of the columns each.  fp32: q and weights as three bf16 terms, groups of 128 rows and tiles of 64 keys, since the
+// terms of q fill shared memory and those of the weights tensor memory.
+// Blocks of pages are operands of the products as they are (kv16.cuh): a bulk copy per page and tile, by the lanes of one warp.
+#pragma once
+#include "attend16_tile.cuh"
+#include "kv16.cuh"
+
+namespace pipesd {
+
+constexpr int kPagesSms = 148, kPagesThreads = 320, kPagesMinTiles = 1;
+
+template <int HD, typename T>
+struct PagesShape {
+    static constexpr bool kWide = sizeof(T) == 4;
+    static constexpr int kTerms = kWide ? 3 : 1, kKeys = kWide ? 64 : 128, kRows = kWide ? 128 : 256;
+    static constexpr int kQTile = 128 * HD * 2, kQ = (kWide ? 3 : 2) * kQTile, kTile = kKeys * HD * 2;
+    static constexpr int kStages = kWide ? (HD == 128 ? 8 : 16) : (HD == 128 ? 5 : 10);
+};
+struct PagesArgs {
+    Kv4Where w;
+    Kv16Pool p;
+    const void* q;
+    void* out;
+    long long q_stride, out_stride;
+    int Hq, q_wide, out_wide;   // wide: 16-byte loads and stores
+    float scale;                // times log2(e)
+    const uint32_t* mask;       // [rows][words], null: a row sees the new rows up to itself
+    int words;
+    float* parts;               // [2 * CTAs] of {sums [HD / 4][cap][4], references [cap], denominators [cap]}
+    int ctas, cap, keys, rows;  // cap: query rows that a slot has room for; keys, rows: of a tile and a row group
+};
+struct PagesJob {
+    int req, n, first, base, head, rho0, n_rows, tiles;      // tiles: 0 = no more jobs
+    int u0, u1, units;          // the range's tiles (u1 <= units; tiles of them are seen by some row), of all the triple's
+    int slot;
+};
+struct PagesControl {
+    unsigned long long job_full, job_read, q_full, q_empty, full[16], empty[16], s_full[2], p_full[2], o_full[2], joint, done;
+    PagesJob jobs[2];
+    int bad_lo[2], bad_hi[2];   // tiles in which a value was not finite
+    uint32_t present[32];       // eight positions a bit
+    float ref[2][128], sum[2][128];
+    uint32_t tmem;
+    int dead;
+};
+template <int HD, typename T>
+constexpr int pages_smem() { return 128 + PagesShape<HD, T>::kQ + PagesShape<HD, T>::kStages * PagesShape<HD, T>::kTile + (int)sizeof(PagesControl); }
+
+// What a request adds to the sequence of tiles: tiles per triple and row groups.
+__device__ __forceinline__ void pages_load(const PagesArgs& a, int r, int& n, int& first, int& base, int& units, int& groups) {
+    n = first = base = units = groups = 0;
+    if (r >= a.w.n_req) return;
+    n = kv4_rows(a.w, r, first, base);
+    if (n <= 0) { n = 0; return; }
+    units = (base + n + a.keys - 1) / a.keys;
+    groups = (n * (a.Hq / a.w.Hkv) + a.rows - 1) / a.rows;
+}
+__device__ __forceinline__ long long pages_scan(long long v) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long t = __shfl_up_sync(0xffffffffu, v, o);
+        if (lane >= o) v += t;
+    }
+    return v;
+}
+// Tiles of all requests, and of those before request `upto` (whole warp).
+__device__ __forceinline__ long long pages_total(const PagesArgs& a, int upto, long long& before) {
+    const int lane = threadIdx.x & 31;
+    long long all = 0;
+    before = 0;
+    for (int r0 = 0; r0 < a.w.n_req; r0 += 32) {
+        int n, first, base, units, groups;
+        pages_load(a, r0 + lane, n, first, base, units, groups);
+        const long long mine = (long long)units * groups * a.w.Hkv, inc = pages_scan(mine);
+        if (upto >= r0 && upto < r0 + 32) before = all + __shfl_sync(0xffffffffu, inc - mine, upto - r0);
+        all += __shfl_sync(0xffffffffu, inc, 31);
+    }
+    return all;
+}
+__device__ __forceinline__ long long pages_share(const PagesArgs& a, long long all) {
+    const long long per = (all + a.ctas - 1) / a.ctas;
+    return per < kPagesMinTiles ? kPagesMinTiles : per;
+}
+// Request that tile `at` of the sequence belongs to, and how far into it (whole warp; at < the total).
+__device__ __forceinline__ int pages_find(const PagesArgs& a, long long at, long long& off) {
+    const int lane = threadIdx.x & 31;
+    for (int r0 = 0; r0 < a.w.n_req; r0 += 32) {
+        int n, first, base, units, groups;
+        pages_load(a, r0 + lane, n, first, base, units, groups);
+        const long long mine = (long long)units * groups * a.w.Hkv, inc = pages_scan(mine);
+        const unsigned hit = __ballot_sync(0xffffffffu, at < inc);
+        if (hit) {
+            const int l = __ffs(hit) - 1;
+            off = at - __shfl_sync(0xffffffffu, inc - mine, l);
+            return r0 + l;
+        }
+        at -= __shfl_sync(0xffffffffu, inc, 31);
+    }
+    off = 0;
+    return a.w.n_req;
+}
+
+// Entries of the ring in the order they are used: K0 K1 V0 K2 V1 K3 ... V(n-1).
+__device__ __forceinline__ uint32_t pages_k(int j) { return j == 0 ? 0 : 2 * j - 1; }
+__device__ __forceinline__ uint32_t pages_v(int j, int n) { return min(j + 2, n) + j; }
+
+// Which of the 32 positions from `start` on row i of a request sees (bit 0: the first).
+__device__ __forceinline__ uint32_t pages_see(const PagesArgs& a, const PagesJob& job, int i, int start) {
+    const int total = job.base + job.n;
+    auto below = [](int n) { return n >= 32 ? 0xffffffffu : (n <= 0 ? 0u : (1u << n) - 1u); };
+    if (!a.mask) return below(min(job.base + i + 1, total) - start);
+    const int j = start - job.base;                // the first's new row; below 0: the prefix
+    if (j <= -32) return 0xffffffffu;
+    const uint32_t* const m = a.mask + (size_t)(job.first + i) * a.words;
+    const int w = j >> 5, sh = j & 31;             // (w is -1 where the border lies within)
+    const uint32_t lo = w < 0 ? 0xffffffffu : (w < a.words ? m[w] : 0u), hi = w + 1 < a.words ? m[w + 1] : 0u;
+    return __funnelshift_r(lo, hi, sh) & below(total - start);
+}
+
+__device__ __forceinline__ void pages_load8(const uint16_t* p, bool wide, uint4 (&x)[1]) {
+    if (wide) x[0] = *reinterpret_cast<const uint4*>(p);
+    else x[0] = make_uint4(pack2(p[0], p[1]), pack2(p[2], p[3]), pack2(p[4], p[5]), pack2(p[6], p[7]));
+}
+// Three terms of eight fp32 values: what a term leaves is exact.
+__device__ __forceinline__ void pages_load8(const float* p, bool wide, uint4 (&x)[3]) {
+    float v[8];
+    if (wide) {
+        *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(p);
+        *reinterpret_cast<float4*>(v + 4) = *reinterpret_cast<const float4*>(p + 4);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = p[i];
+    }
+#pragma unroll
+    for (int t = 0; t < 3; ++t) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+            v[2 * i] -= __uint_as_float(w[i] << 16);
+            v[2 * i + 1] -= __uint_as_float(w[i] & 0xffff0000u);
+        }
+        x[t] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+// 32 neighbouring outputs.
+__device__ __forceinline__ void pages_store32(uint16_t* p, bool wide, const float* y) {
+    if (wide) {
+#pragma unroll
+        for (int x = 0; x < 32; x += 8)
+            *reinterpret_cast<uint4*>(p + x) =
+                make_uint4(pack_bf16(y[x], y[x + 1]), pack_bf16(y[x + 2], y[x + 3]), pack_bf16(y[x + 4], y[x + 5]), pack_bf16(y[x + 6], y[x + 7]));
+    } else {
+#pragma unroll
+        for (int x = 0; x < 32; ++x) p[x] = f32_to_bf16_bits(y[x]);
+    }
+}
+__device__ __forceinline__ void pages_store32(float* p, bool wide, const float* y) {
+    if (wide) {
+#pragma unroll
+        for (int x = 0; x < 32; x += 4) *reinterpret_cast<float4*>(p + x) = make_float4(y[x], y[x + 1], y[x + 2], y[x + 3]);
+    } else {
+#pragma unroll
+        for (int x = 0; x < 32; ++x) p[x] = y[x];
+    }
+}
+__device__ __forceinline__ void pages_store(uint16_t* p, float y) { *p = f32_to_bf16_bits(y); }
+__device__ __forceinline__ void pages_store(float* p, float y) { *p = y; }
+
+template <int HD, typename T>
+__global__ void __launch_bounds__(kPagesThreads, 1) pages_attend_kernel(const PagesArgs a) {
+    using Shape = PagesShape<HD, T>;
+    constexpr int kKeys = Shape::kKeys, kTile = Shape::kTile, kStages = Shape::kStages, kTerms = Shape::kTerms, kPieces = HD / 8;
+    constexpr uint32_t kIdescS = umma_idesc_bf16(128, kKeys, 0, 0), kIdescO = umma_idesc_bf16(128, HD, 0, 1);
+    extern __shared__ unsigned char smem_raw[];
+    unsigned char* const smem = smem_raw + ((128u - (smem_u32(smem_raw) & 127u)) & 127u);
+    unsigned char* const ring = smem + Shape::kQ;
+    PagesControl& c = *reinterpret_cast<PagesControl*>(ring + kStages * kTile);
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int G = a.Hq / a.w.Hkv;
+    volatile int* const dead = &c.dead;
+    pdl_launch_dependents();
+
+    if (tid == 0) {
+        mbar_init(smem_u32(&c.job_full), 1);
+        mbar_init(smem_u32(&c.job_read), 9);
+        mbar_init(smem_u32(&c.q_full), 8);
+        mbar_init(smem_u32(&c.q_empty), 1);
+        mbar_init(smem_u32(&c.joint), 8);
+        mbar_init(smem_u32(&c.done), 1);
+        for (int i = 0; i < kStages; ++i) {
+            mbar_init(smem_u32(&c.full[i]), 1);
+            mbar_init(smem_u32(&c.empty[i]), 1);
+        }
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(smem_u32(&c.s_full[s]), 1);
+            mbar_init(smem_u32(&c.p_full[s]), 4);
+            mbar_init(smem_u32(&c.o_full[s]), 1);
+        }
+        c.dead = 0;
+        fence_mbar_init();
+    }
+    if (warp == 9) tmem_alloc(smem_u32(&c.tmem), 512);
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = c.tmem;                  // stream s: scores and weights at 128 s, sums at 256 + HD s
+
+    if (warp == 8) {                               // ---- what there is to do, and fetches
+        long long before;
+        const long long all = pages_total(a, -1, before), share = pages_share(a, all);
+        long long f = (long long)blockIdx.x * share, off = 0;
+        const long long f_cta = f, f_end = min(f + share, all);
+        int req = f < f_end ? pages_find(a, f, off) : a.w.n_req;
+        uint32_t entry = 0, tile_no = 0;
+        bool ok = true;
+        for (int i = 0; ok; ++i) {
+            PagesJob job = {};
+            while (f < f_end && req < a.w.n_req) {
+                int n, first, base, units, groups;
+                pages_load(a, req, n, first, base, units, groups);
+                if (off >= (long long)units * groups * a.w.Hkv) { ++req; off = 0; continue; }      // (requests without rows have no tiles)
+                const int triple = (int)(off / units);
+                job.req = req; job.n = n; job.first = first; job.base = base; job.units = units;
+                job.head = triple / groups;
+                job.rho0 = triple % groups * Shape::kRows;
+                job.n_rows = min(Shape::kRows, n * G - job.rho0);
+                job.u0 = (int)(off % units);
+                job.u1 = (int)min((long long)units, job.u0 + (f_end - f));
+                job.slot = 2 * blockIdx.x + (f - job.u0 > f_cta ? 1 : 0);
+                // without a mask no row of the group sees what lies behind its last one
+                const int seen = a.mask ? units : min(units, (base + (job.rho0 + job.n_rows - 1) / G) / kKeys + 1);
+                job.tiles = max(1, min(job.u1, seen) - job.u0);                // (a tile at least: the others' sums are none)
+                f += job.u1 - job.u0;
+                off += job.u1 - job.u0;
+                break;
+            }
+            if (i > 0) ok = warp_wait(smem_u32(&c.job_read), (i - 1) & 1, dead);
+            if (!ok) break;
+            if (lane == 0) {
+                c.jobs[i & 1] = job;
+                c.bad_lo[i & 1] = INT32_MAX;
+                c.bad_hi[i & 1] = -1;
+                mbar_arrive(smem_u32(&c.job_full));
+            }
+            if (job.tiles == 0) break;
+            // a lane per page of a tile; the pages of tile j + 1 are looked up ahead of tile j's copies
+            const int total = job.base + job.n, total8 = (total + 7) & ~7;
+            const uint16_t* block[2] = {nullptr, nullptr};                     // where the lane's piece of K begins (tile j even, odd)
+            uint32_t bytes[2] = {0, 0}, to[2] = {0, 0};
+            const size_t v_off = (size_t)a.w.Hkv * kv16_block_elems(a.w, HD);  // from a K block to its V block
+            auto locate = [&](int j) {
+                const int p0 = (job.u0 + j) * kKeys, page_no = p0 / a.w.page_size + lane;
+                const int start = max(p0, page_no * a.w.page_size), end = min(min(p0 + kKeys, (page_no + 1) * a.w.page_size), total8);
+                int page = -1;
+                if (start < end) page = kv16_page(a.w, job.req, start);
+                block[j & 1] = nullptr;
+                bytes[j & 1] = 0;
+                if (page >= 0) {
+                    block[j & 1] = kv16_block(a.p, a.w, a.p.layer, page, 0, job.head) + (size_t)(start % a.w.page_size) * HD;
+                    bytes[j & 1] = (uint32_t)(end - start) * HD * 2;
+                    to[j & 1] = (uint32_t)(start - p0) * HD * 2;
+                }
+            };
+            auto fetch = [&](int j, int v) {
+                const int st = entry % kStages;
+                if (entry >= kStages) ok = warp_wait(smem_u32(&c.empty[st]), (entry / kStages - 1) & 1, dead);
+                if (!ok) return;
+                const uint32_t bar = smem_u32(&c.full[st]), sum = __reduce_add_sync(0xffffffffu, bytes[j & 1]);
+                if (v == 0) {
+                    const uint32_t groups = bytes[j & 1] / (HD * 16), bits = groups ? ((1u << groups) - 1u) << (to[j & 1] / (HD * 16)) : 0u;
+                    const uint32_t present = __reduce_or_sync(0xffffffffu, bits);
+                    if (lane == 0) c.present[(tile_no + j) & 31] = present;
+                }
+                if (lane == 0) mbar_expect_tx(bar, sum);
+                __syncwarp();
+                if (block[j & 1]) bulk_g2s(smem_u32(ring + st * kTile) + to[j & 1], block[j & 1] + (v ? v_off : 0), bytes[j & 1], bar);
+                ++entry;
+            };
+            locate(0);
+            fetch(0, 0);
+            for (int j = 0; j < job.tiles && ok; ++j) {
+                if (j + 1 < job.tiles) {
+                    locate(j + 1);
+                    fetch(j + 1, 0);
+                }
+                if (ok) fetch(j, 1);
+            }
+            tile_no += job.tiles;
+        }
+        if (!ok && lane == 0) {                    // given up: the copies in flight are waited for
+            for (uint32_t e = entry > kStages ? entry - kStages : 0; e < entry; ++e) mbar_wait(smem_u32(&c.full[e % kStages]), (e / kStages) & 1);
+        }
+        __syncwarp();
+    } else if (warp == 9) {                        // ---- products
+        if (lane == 0) {
+            uint32_t entry = 0;
+            bool ok = true;
+            auto scores = [&](int s, int q_tile, uint32_t e) {
+                const uint32_t q = smem_u32(smem + q_tile * Shape::kQTile), k = smem_u32(ring + e % kStages * kTile);
+#pragma unroll
+                for (int t = 0; t < kTerms; ++t)
+#pragma unroll
+                    for (int x = 0; x < HD / 16; ++x)
+                        umma_bf16(tmem + 128 * s, umma_desc(q + t * Shape::kQTile + x * 256, 128, HD * 16), umma_desc(k + x * 256, 128, HD * 16), kIdescS, t + x > 0);
+                umma_commit(smem_u32(&c.s_full[s]));
+            };
+            uint32_t p_phase[2] = {0, 0};
+            auto sums = [&](int s, uint32_t e, bool first, bool last) {
+                ok = ok && role_wait(smem_u32(&c.p_full[s]), p_phase[s], dead);
+                p_phase[s] ^= 1;
+                if (!ok) return;
+                tc_fence_after();
+                const uint32_t v = smem_u32(ring + e % kStages * kTile);
+#pragma unroll
+                for (int t = 0; t < kTerms; ++t)
+#pragma unroll
+                    for (int x = 0; x < kKeys / 16; ++x)
+                        umma_bf16_ta(tmem + 256 + HD * s, tmem + 128 * s + t * (kKeys / 2) + 8 * x, umma_desc(v + x * HD * 32, HD * 16, 128), kIdescO, !first || t + x > 0);
+                if (last) umma_commit(smem_u32(&c.o_full[s]));
+            };
+            auto arrived = [&](uint32_t e) {
+                ok = ok && role_wait(smem_u32(&c.full[e % kStages]), (e / kStages) & 1, dead);
+                if (ok) tc_fence_after();
+                return ok;
+            };
+            auto release = [&](uint32_t e) { umma_commit(smem_u32(&c.empty[e % kStages])); };
+            for (int i = 0; ok; ++i) {
+                ok = role_wait(smem_u32(&c.job_full), i & 1, dead);
+                if (!ok) break;
+                const int n = c.jobs[i & 1].tiles;
+                const bool both = c.jobs[i & 1].n_rows > 128;
+                mbar_arrive(smem_u32(&c.job_read));
+                if (n == 0) break;
+                ok = role_wait(smem_u32(&c.q_full), i & 1, dead);
+                if (!ok || !arrived(entry)) break;
+                if (both) {
+                    scores(0, 0, entry);
+                    scores(1, 1, entry);
+                    release(entry);
+                    if (n == 1) umma_commit(smem_u32(&c.q_empty));
+                    for (int j = 0; j < n; ++j) {
+                        const uint32_t ev = entry + pages_v(j, n), ek = entry + pages_k(j + 1);
+                        const bool more = j + 1 < n;
+                        if (!arrived(ev)) break;
+                        sums(0, ev, j == 0, !more);
+                        if (!ok) break;
+                        if (more) {
+                            if (!arrived(ek)) break;
+                            scores(0, 0, ek);
+                        }
+                        sums(1, ev, j == 0, !more);
+                        if (!ok) break;
+                        release(ev);
+                        if (more) {
+                            scores(1, 1, ek);
+                            release(ek);
+                            if (j + 2 == n) umma_commit(smem_u32(&c.q_empty));
+                        }
+                    }
+                } else {
+                    scores(0, 0, entry);
+                    release(entry);
+                    if (n > 1) {
+                        if (!arrived(entry + 1)) break;
+                        scores(1, 0, entry + 1);
+                        release(entry + 1);
+                    }
+                    if (n <= 2) umma_commit(smem_u32(&c.q_empty));
+                    for (int j = 0; j < n; ++j) {
+                        const uint32_t ev = entry + pages_v(j, n);
+                        if (!arrived(ev)) break;
+                        sums(j & 1, ev, j < 2, j + 2 >= n);
+                        if (!ok) break;
+                        release(ev);
+                        if (j + 2 < n) {
+                            const uint32_t ek = entry + pages_k(j + 2);
+                            if (!arrived(ek)) break;
+                            scores(j & 1, 0, ek);
+                            release(ek);
+                            if (j + 3 == n) umma_commit(smem_u32(&c.q_empty));
+                        }
+                    }
+                }
+                entry += 2 * n;
+            }
+        }
+        __syncwarp();
+    } else {                                       // ---- a stream's rows
+        const int s = warp >> 2, row = tid & 127;
+        const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16, s_tmem = tmem + 128 * s + lanes, o_tmem = tmem + 256 + HD * s + lanes;
+        uint32_t entry = 0, tile_no = 0, s_phase = 0, o_phase[2] = {0, 0}, joint_phase = 0;
+        auto joint = [&] {                         // both streams' warps
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&c.joint));
+            const bool there = warp_wait(smem_u32(&c.joint), joint_phase, dead);
+            joint_phase ^= 1;
+            return there;
+        };
+        for (int i = 0;; ++i) {
+            if (!warp_wait(smem_u32(&c.job_full), i & 1, dead)) break;
+            const PagesJob job = c.jobs[i & 1];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&c.job_read));
+            if (job.tiles == 0) break;
+            const int n = job.tiles;
+            const bool both = job.n_rows > 128;
+            // ---- queries, in the products' order: 8 x 4 pieces of 8 columns a warp and step
+            bool ok = i == 0 || warp_wait(smem_u32(&c.q_empty), (i - 1) & 1, dead);
+            if (ok) {
+                const int steps = (job.n_rows + 7) / 8 * (kPieces / 4);
+                for (int x = warp; x < steps; x += 8) {
+                    const int rho = x / (kPieces / 4) * 8 + (lane & 7), piece = x % (kPieces / 4) * 4 + (lane >> 3);
+                    if (rho < job.n_rows) {
+                        const int at = job.rho0 + rho;
+                        uint4 v[kTerms];
+                        pages_load8(static_cast<const T*>(a.q) + (job.first + at / G) * a.q_stride + (size_t)(job.head * G + at % G) * HD + piece * 8, a.q_wide, v);
+#pragma unroll
+                        for (int t = 0; t < kTerms; ++t)
+                            *reinterpret_cast<uint4*>(smem + (t + (rho >> 7)) * Shape::kQTile + ((rho & 127) >> 3) * HD * 16 + piece * 128 + (rho & 7) * 16) = v[t];
+                    }
+                }
+                fence_proxy_async_smem();
+            }
+            __syncwarp();
+            if (ok && lane == 0) mbar_arrive(smem_u32(&c.q_full));
+            const int local = both ? 128 * s + row : row;                      // of the group's rows
+            const bool mine = local < job.n_rows, any = (both ? 128 * s : 0) + 32 * (warp & 3) < job.n_rows;
+            const int at = job.rho0 + (mine ? local : 0), node = at / G;
+            // tiles that every row of the stream sees whole
+            const int clear = (a.mask ? job.base : job.base + (job.rho0 + (both ? 128 * s : 0)) / G + 1) / kKeys;
+            float ref = -INFINITY, sum = 0.f;
+            for (int j = both ? 0 : s; j < n && ok; j += both ? 1 : 2) {
+                const int u = job.u0 + j;
+                uint32_t see[kKeys / 32];
+                bool masked = u >= clear;
+                if (masked) {
+#pragma unroll
+                    for (int w = 0; w < kKeys / 32; ++w) see[w] = pages_see(a, job, node, u * kKeys + 32 * w);
+                }
+                ok = warp_wait(smem_u32(&c.s_full[s]), s_phase, dead);
+                s_phase ^= 1;
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t present = c.present[(tile_no + j) & 31];
+                if (present != (kKeys == 128 ? 0xffffu : 0xffu)) {
+#pragma unroll
+                    for (int w = 0; w < kKeys / 32; ++w) {
+                        const uint32_t x = present >> (4 * w);
+                        const uint32_t there = (x & 1u ? 0xffu : 0u) | (x & 2u ? 0xff00u : 0u) | (x & 4u ? 0xff0000u : 0u) | (x & 8u ? 0xff000000u : 0u);
+                        see[w] = (masked ? see[w] : 0xffffffffu) & there;
+                    }
+                    masked = true;
+                }
+                if (any) softmax_tile<HD, kKeys, kTerms>(s_tmem, o_tmem, a.scale, both ? j == 0 : j < 2, masked, see, ref, sum);
+                if (masked) {
+                    const uint32_t ev = entry + pages_v(j, n);
+                    ok = warp_wait(smem_u32(&c.full[ev % kStages]), (ev / kStages) & 1, dead);
+                    if (!ok) break;
+                    const int keys = job.base + job.n - u * kKeys;
+                    if (clean_values(ring + ev % kStages * kTile, kTile / 16, row, 128, [&](int p) {
+                            const int key = p / kPieces / 8 * 8 + p % 8;
+                            return key < keys && (present >> (key >> 3) & 1u);
+                        })) {
+                        atomicMin(&c.bad_lo[i & 1], u);
+                        atomicMax(&c.bad_hi[i & 1], u);
+                        __threadfence_block();
+                    }
+                    fence_proxy_async_smem();
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&c.p_full[s]));
+            }
+            if (sum != sum) ref = INFINITY;        // (not what a row that sees nothing has: every factor of it is then a NaN)
+            // ---- the range's sums
+            const bool has[2] = {true, both || n > 1};
+            if (ok && (both ? s == 0 : true)) ok = warp_wait(smem_u32(&c.o_full[0]), o_phase[0], dead);
+            if (ok && has[1] && (both ? s == 1 : true)) ok = warp_wait(smem_u32(&c.o_full[1]), o_phase[1], dead);
+            o_phase[0] ^= 1;
+            if (has[1]) o_phase[1] ^= 1;
+            entry += 2 * n;
+            tile_no += n;
+            T* const out = static_cast<T*>(a.out) + (job.first + node) * a.out_stride + (size_t)(job.head * G + at % G) * HD;
+            const bool whole = job.u0 == 0 && job.u1 == job.units;
+            float* const part = a.parts + (size_t)job.slot * a.cap * (HD + 2);
+            if (ok && !both) {
+                c.ref[s][row] = ref;
+                c.sum[s][row] = sum;
+                ok = joint();
+            }
+            if (!ok) {                             // a copy or a product that never came: no result
+                if (mine && whole)
+                    for (int d = 0; d < HD; ++d) pages_store(out + d, NAN);
+                if (mine && !whole) part[a.cap * HD + local] = NAN;
+                break;
+            }
+            tc_fence_after();
+            float f0 = 1.f, f1 = 1.f;              // what stream 0's and stream 1's sums are multiplied with
+            bool none0 = ref == -INFINITY, none1 = true;                       // a stream that has seen nothing has none
+            if (!both) {
+                const float r0 = c.ref[0][row], r1 = c.ref[1][row];
+                none0 = r0 == -INFINITY;
+                none1 = r1 == -INFINITY;
+                ref = fmaxf(r0, r1);
+                f0 = none0 ? 0.f : exp2_approx(r0 - ref);
+                f1 = none1 ? 0.f : exp2_approx(r1 - ref);
+                sum = c.sum[0][row] * f0 + c.sum[1][row] * f1;
+            }
+            const int lo = *(volatile int*)&c.bad_lo[i & 1], hi = *(volatile int*)&c.bad_hi[i & 1];
+            const float inv = !whole ? 1.f : (sum > 0.f ? 1.f / sum : sum);
+            const int d0 = both ? 0 : s * (HD / 2), d1 = both ? HD : d0 + HD / 2;
+#pragma unroll 1
+            for (int d = d0; d < d1; d += 32) {
+                if (any) {
+                    float y[32];
+                    uint32_t o[32];
+                    tmem_ld32(tmem + 256 + HD * (both ? s : 0) + lanes + d, o);
+                    tmem_ld_wait32(o);
+#pragma unroll
+                    for (int x = 0; x < 32; ++x) y[x] = none0 ? 0.f : __uint_as_float(o[x]) * f0;
+                    if (!both && n > 1) {
+                        tmem_ld32(tmem + 256 + HD + lanes + d, o);
+                        tmem_ld_wait32(o);
+#pragma unroll
+                        for (int x = 0; x < 32; ++x) y[x] = none1 ? y[x] : fmaf(__uint_as_float(o[x]), f1, y[x]);
+                    }
+                    if (mine) {
+                        if (lo <= hi) {            // columns of what the row sees whose values are not finite
+                            uint32_t bad = 0;
+                            for (int p0 = lo * kKeys; p0 < (hi + 1) * kKeys; p0 += 32) {
+                                uint32_t bits = pages_see(a, job, node, p0);
+                                while (bits) {
+                                    const int p = p0 + __ffs(bits) - 1, page = kv16_page(a.w, job.req, p);
+                                    bits &= bits - 1;
+                                    if (page >= 0) bad |= not_finite32(kv16_block(a.p, a.w, a.p.layer, page, 1, job.head) + kv16_piece(p % a.w.page_size, d / 8, HD), 64);
+                                }
+                            }
+#pragma unroll
+                            for (int x = 0; x < 32; ++x)
+                                if (bad >> x & 1u) y[x] = NAN;
+                        }
+                        if (whole) {
+#pragma unroll
+                            for (int x = 0; x < 32; ++x) y[x] *= inv;
+                            pages_store32(out + d, a.out_wide, y);
+                        } else {
+#pragma unroll
+                            for (int x = 0; x < 32; x += 4)
+                                *reinterpret_cast<float4*>(part + ((size_t)(d + x) * a.cap + 4 * local)) = make_float4(y[x], y[x + 1], y[x + 2], y[x + 3]);
+                        }
+                    }
+                }
+                __syncwarp();
+            }
+            if (mine && !whole && (both || s == 0)) {
+                part[a.cap * HD + local] = ref;
+                part[a.cap * (HD + 1) + local] = sum;
+            }
+            tc_fence_before();
+            if (!both && !joint()) break;          // both streams' sums have been read
+        }
+    }
+    __syncthreads();
+    if (warp == 9) {
+        if (c.dead && lane == 0) {                 // products in flight end before their memory is given back
+            umma_commit(smem_u32(&c.done));
+            mbar_wait(smem_u32(&c.done), 0);
+        }
+        __syncwarp();
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+// Adds up the shares of triples that several CTAs had, a CTA per (row, query head): warp w the shares w, w + 4, ..., then the warps' sums in order.
+constexpr int kPagesMergeWarps = 4;
+template <int HD, typename T>
+__global__ void __launch_bounds__(32 * kPagesMergeWarps) pages_merge_kernel(const PagesArgs a) {
+    constexpr int kE = HD / 32;                    // neighbouring columns of a lane
+    __shared__ float s_v[kPagesMergeWarps][HD], s_sum[kPagesMergeWarps];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, G = a.Hq / a.w.Hkv;
+    const int row = blockIdx.x / a.Hq, qh = blockIdx.x % a.Hq;
+    int req = -1;
+    for (int r0 = 0; r0 < a.w.n_req && req < 0; r0 += 32) {
+        const int r = min(r0 + lane, a.w.n_req - 1);
+        const unsigned hit = __ballot_sync(0xffffffffu, a.w.row0[r] <= row && row < a.w.row0[r + 1]);
+        if (hit) req = min(r0 + __ffs(hit) - 1, a.w.n_req - 1);
+    }
+    int n, first, base, units, groups;
+    pages_load(a, req < 0 ? a.w.n_req : req, n, first, base, units, groups);
+    long long before;
+    const long long all = pages_total(a, req, before), share = pages_share(a, all);
+    // Launched with programmatic serialisation: behind this the shares are complete.  Every thread waits, those without work too.
+    pdl_wait();
+    if (req < 0) return;
+    T* const out = static_cast<T*>(a.out) + row * a.out_stride + (size_t)qh * HD + lane * kE;
+    if (row - first >= n) {                        // a row without a position: nothing to see
+        if (warp == 0)
+#pragma unroll
+            for (int i = 0; i < kE; ++i) pages_store(out + i, 0.f);
+        return;
+    }
+    const int rho = (row - first) * G + qh % G;
+    const long long start = before + (long long)(qh / G * groups + rho / a.rows) * units;
+    const int c0 = (int)(start / share), c1 = (int)((start + units - 1) / share);
+    if (c0 == c1) return;
+    const int local = rho % a.rows;
+    auto slot = [&](int c) { return a.parts + (size_t)(2 * c + (start > (long long)c * share ? 1 : 0)) * a.cap * (HD + 2); };
+    float top = -INFINITY;
+    for (int c = c0 + lane; c <= c1; c += 32) {
+        const float r = slot(c)[a.cap * HD + local];
+        top = r == r ? fmaxf(top, r) : INFINITY;
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    float v[kE] = {}, sum = 0.f;
+#pragma unroll 4
+    for (int c = c0 + warp; c <= c1; c += kPagesMergeWarps) {
+        const float* p = slot(c);
+        const float r = p[a.cap * HD + local], factor = r == -INFINITY ? 0.f : exp2_approx(r - top);      // (NaN where a share is missing)
+        float x[kE];
+#pragma unroll
+        for (int i = 0; i < kE; ++i) {
+            const int d = lane * kE + i;
+            x[i] = p[(size_t)(d & ~3) * a.cap + 4 * local + (d & 3)];
+        }
+        const float part = p[a.cap * (HD + 1) + local];
+        if (r != -INFINITY) {
+#pragma unroll
+            for (int i = 0; i < kE; ++i) v[i] = fmaf(factor, x[i], v[i]);
+            sum = fmaf(factor, part, sum);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kE; ++i) s_v[warp][lane * kE + i] = v[i];
+    if (lane == 0) s_sum[warp] = sum;
+    __syncthreads();
+    if (warp) return;
+#pragma unroll
+    for (int w = 1; w < kPagesMergeWarps; ++w) {
+        sum += s_sum[w];
+#pragma unroll
+        for (int i = 0; i < kE; ++i) v[i] += s_v[w][lane * kE + i];
+    }
+    const float inv = sum > 0.f ? 1.f / sum : sum;
+#pragma unroll
+    for (int i = 0; i < kE; ++i) pages_store(out + i, v[i] * inv);
+}
+
+}  // namespace pipesd

@@ -266,7 +266,7 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
                     const uint32_t ev = entry + 2 * j + 1;
                     ok = warp_wait(smem_u32(&c.full[ev % kStages]), (ev / kStages) & 1, dead);
                     if (!ok) break;
-                    if (clean_values(ring + ev % kStages * kTile, kTile / 16, job.n - j * 128, row, 128, [](int p) { return (p >> 3) & 127; })) {
+                    if (clean_values(ring + ev % kStages * kTile, kTile / 16, row, 128, [&](int p) { return j * 128 + ((p >> 3) & 127) < job.n; })) {
                         *(volatile int*)&c.flags[i % kPromptJobs] = 1;
                         __threadfence_block();
                     }

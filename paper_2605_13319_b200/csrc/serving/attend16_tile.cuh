@@ -153,14 +153,14 @@ __device__ __forceinline__ void softmax_tile(uint32_t s_tmem, uint32_t o_tmem, f
     tmem_st_wait();
 }
 
-// Values of a tile that no row may take into its products: rows from `limit` on, and what is not finite.  A weight of 0 does not keep them out, so they
-// are 0 in shared memory.  `pieces` 16-byte pieces, key_of(piece) its row; threads of one stream.  True if something was not finite.
-template <typename KeyOf>
-__device__ __forceinline__ bool clean_values(unsigned char* tile, int pieces, int limit, int tid, int n_thr, KeyOf key_of) {
+// Values of a tile that no row may take into its products: pieces that are no key's, and what is not finite.  A weight of 0 does not keep them out, so
+// they become 0 in shared memory.  `pieces` 16-byte pieces, is_key(piece); threads of one stream.  True if something was not finite.
+template <typename IsKey>
+__device__ __forceinline__ bool clean_values(unsigned char* tile, int pieces, int tid, int n_thr, IsKey is_key) {
     bool found = false;
     for (int i = tid; i < pieces; i += n_thr) {
         uint4* const at = reinterpret_cast<uint4*>(tile) + i;
-        if (key_of(i) >= limit) {
+        if (!is_key(i)) {
             *at = make_uint4(0, 0, 0, 0);
             continue;
         }

@@ -3,7 +3,7 @@
 #include <mutex>
 
 #include "../../../include/pipesd.h"
-#include "attend16.cuh"
+#include "attend16_pages.cuh"
 #include "attend16_prompt.cuh"
 #include "kv16_pages.cuh"
 
@@ -34,6 +34,20 @@ bool aligned(const void* p, int32_t dtype) { return (uintptr_t)p % size_of(dtype
 bool wide(const void* p, int64_t stride, int32_t rows, int32_t dtype) { return (uintptr_t)p % 16 == 0 && (rows == 1 || stride * size_of(dtype) % 16 == 0); }
 int32_t launched() { return cudaGetLastError() == cudaSuccess ? PIPESD_OK : PIPESD_E_CUDA; }
 
+// Query rows that a share has room for.
+int pages_cap(const pipesd_kv16_cfg* c, int32_t rows, int32_t n_q_heads) {
+    return (int)std::min<int64_t>(256, ((int64_t)rows * (n_q_heads / c->n_kv_heads) + 3) / 4 * 4);
+}
+template <int HD, typename T>
+int32_t pages_run(PagesArgs& a, cudaStream_t st) {
+    a.keys = PagesShape<HD, T>::kKeys;
+    a.rows = PagesShape<HD, T>::kRows;
+    pages_attend_kernel<HD, T><<<a.ctas, kPagesThreads, pages_smem<HD, T>(), st>>>(a);
+    if (cudaGetLastError() != cudaSuccess) return PIPESD_E_CUDA;
+    if (launch_pdl(pages_merge_kernel<HD, T>, dim3((unsigned)(a.w.rows * a.Hq)), dim3(32 * kPagesMergeWarps), 0, st, a) != cudaSuccess) return PIPESD_E_CUDA;
+    return launched();
+}
+
 int plan_cap(const pipesd_kv16_cfg* c, int32_t n) { return (int)std::min<int64_t>((int64_t)n * c->max_pages, c->n_pages); }
 
 // [rows, heads, head_dim] with `stride` elements between rows, fetched in boxes of 64 columns x box_heads x box_rows; rows behind the last read as 0.
@@ -57,13 +71,19 @@ bool rows_map(CUtensorMap* m, const void* base, int hd, int heads, int64_t rows,
 constexpr int kDevices = 64, kSms = 148;
 std::mutex g_mu;
 bool g_ready[kDevices] = {false};
+template <int HD, typename T>
+bool pages_attrs() {
+    static_assert(pages_smem<HD, T>() <= 232448, "a CTA's shared memory");
+    return cudaFuncSetAttribute((const void*)pages_attend_kernel<HD, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, pages_smem<HD, T>()) == cudaSuccess;
+}
 bool device_ready() {
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices) return false;
     std::lock_guard<std::mutex> lock(g_mu);
     if (!g_ready[dev])
         g_ready[dev] = cudaFuncSetAttribute((const void*)prompt_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, PromptShape<64>::kSmem) == cudaSuccess &&
-                       cudaFuncSetAttribute((const void*)prompt_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, PromptShape<128>::kSmem) == cudaSuccess;
+                       cudaFuncSetAttribute((const void*)prompt_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, PromptShape<128>::kSmem) == cudaSuccess &&
+                       pages_attrs<64, float>() && pages_attrs<64, uint16_t>() && pages_attrs<128, float>() && pages_attrs<128, uint16_t>();
     return g_ready[dev];
 }
 
@@ -162,7 +182,7 @@ int32_t pipesd_kv16_release(const pipesd_kv16_cfg* cfg, int32_t n_req, const int
 
 uint64_t pipesd_kv16_attend_scratch_bytes(const pipesd_kv16_cfg* cfg, int32_t rows, int32_t n_q_heads) {
     if (!cfg_ok(cfg) || rows < 1 || n_q_heads < 1 || n_q_heads % cfg->n_kv_heads || n_q_heads / cfg->n_kv_heads > 128) return 0;
-    return 16;
+    return (uint64_t)2 * kPagesSms * pages_cap(cfg, rows, n_q_heads) * (cfg->head_dim + 2) * 4;
 }
 
 int32_t pipesd_kv16_attend(const pipesd_kv16_cfg* cfg, const void* pool, int32_t layer, const void* q, void* out, int32_t dtype, int64_t q_stride,
@@ -175,7 +195,8 @@ int32_t pipesd_kv16_attend(const pipesd_kv16_cfg* cfg, const void* pool, int32_t
     const int64_t width = (int64_t)n_q_heads * cfg->head_dim;
     if (rows > 1 && (q_stride < width || out_stride < width)) return PIPESD_E_INVALID;
     if ((int64_t)rows * n_q_heads > INT32_MAX) return PIPESD_E_INVALID;
-    Attend16Args a = {};
+    if (!device_ready()) return PIPESD_E_CUDA;
+    PagesArgs a = {};
     a.w = where_of(cfg, n_req, rows, row0, base, table);
     a.p = pool_of(cfg, pool, layer);
     a.q = q;
@@ -183,19 +204,17 @@ int32_t pipesd_kv16_attend(const pipesd_kv16_cfg* cfg, const void* pool, int32_t
     a.q_stride = q_stride;
     a.out_stride = out_stride;
     a.Hq = n_q_heads;
+    a.q_wide = wide(q, q_stride, rows, dtype);
+    a.out_wide = wide(out, out_stride, rows, dtype);
     a.scale = scale * 1.4426950408889634f;
     a.mask = mask;
     a.words = mask ? words : 0;
-    const unsigned grid = (unsigned)(((int64_t)rows * n_q_heads + 3) / 4);
+    a.parts = static_cast<float*>(scratch);
+    a.ctas = kPagesSms;
+    a.cap = pages_cap(cfg, rows, n_q_heads);
     cudaStream_t st = (cudaStream_t)cuda_stream;
-    if (cfg->head_dim == 128) {
-        if (dtype == PIPESD_F32) attend16_simple_kernel<128, float, true><<<grid, 128, 0, st>>>(a);
-        else attend16_simple_kernel<128, uint16_t, true><<<grid, 128, 0, st>>>(a);
-    } else {
-        if (dtype == PIPESD_F32) attend16_simple_kernel<64, float, true><<<grid, 128, 0, st>>>(a);
-        else attend16_simple_kernel<64, uint16_t, true><<<grid, 128, 0, st>>>(a);
-    }
-    return launched();
+    if (cfg->head_dim == 128) return dtype == PIPESD_F32 ? pages_run<128, float>(a, st) : pages_run<128, uint16_t>(a, st);
+    return dtype == PIPESD_F32 ? pages_run<64, float>(a, st) : pages_run<64, uint16_t>(a, st);
 }
 
 int32_t pipesd_attend_packed(const void* q, const void* k, const void* v, void* out, int64_t q_stride, int64_t k_stride, int64_t v_stride,
