@@ -14,14 +14,15 @@
 
 namespace pipesd {
 
-constexpr int kPagesSms = 148, kPagesThreads = 320, kPagesMinTiles = 1;
+constexpr int kPagesSms = 148, kPagesMinTiles = 1;
 
 template <int HD, typename T>
 struct PagesShape {
     static constexpr bool kWide = sizeof(T) == 4;
     static constexpr int kTerms = kWide ? 3 : 1, kKeys = kWide ? 64 : 128, kRows = kWide ? 128 : 256;
     static constexpr int kQTile = 128 * HD * 2, kQ = (kWide ? 3 : 2) * kQTile, kTile = kKeys * HD * 2;
-    static constexpr int kStages = kWide ? (HD == 128 ? 8 : 16) : (HD == 128 ? 5 : 10);
+    static constexpr int kKSlots = kWide ? (HD == 128 ? 4 : 8) : (HD == 128 ? 2 : 4), kVSlots = kWide ? (HD == 128 ? 4 : 8) : (HD == 128 ? 3 : 6);
+    static constexpr int kSlots = kKSlots + kVSlots;
 };
 struct PagesArgs {
     Kv4Where w;
@@ -42,7 +43,7 @@ struct PagesJob {
     int slot;
 };
 struct PagesControl {
-    unsigned long long job_full, job_read, q_full, q_empty, full[16], empty[16], s_full[2], p_full[2], o_full[2], joint, done;
+    unsigned long long job_full, job_read, q_full, q_empty, k_full[8], k_empty[8], v_full[8], v_empty[8], s_full[2], p_full[2], o_full[2], joint, done;
     PagesJob jobs[2];
     int bad_lo[2], bad_hi[2];   // tiles in which a value was not finite
     uint32_t present[32];       // eight positions a bit
@@ -51,7 +52,7 @@ struct PagesControl {
     int dead;
 };
 template <int HD, typename T>
-constexpr int pages_smem() { return 128 + PagesShape<HD, T>::kQ + PagesShape<HD, T>::kStages * PagesShape<HD, T>::kTile + (int)sizeof(PagesControl); }
+constexpr int pages_smem() { return 128 + PagesShape<HD, T>::kQ + PagesShape<HD, T>::kSlots * PagesShape<HD, T>::kTile + (int)sizeof(PagesControl); }
 
 // What a request adds to the sequence of tiles: tiles per triple and row groups.
 __device__ __forceinline__ void pages_load(const PagesArgs& a, int r, int& n, int& first, int& base, int& units, int& groups) {
@@ -107,10 +108,6 @@ __device__ __forceinline__ int pages_find(const PagesArgs& a, long long at, long
     off = 0;
     return a.w.n_req;
 }
-
-// Entries of the ring in the order they are used: K0 K1 V0 K2 V1 K3 ... V(n-1).
-__device__ __forceinline__ uint32_t pages_k(int j) { return j == 0 ? 0 : 2 * j - 1; }
-__device__ __forceinline__ uint32_t pages_v(int j, int n) { return min(j + 2, n) + j; }
 
 // Which of the 32 positions from `start` on row i of a request sees (bit 0: the first).
 __device__ __forceinline__ uint32_t pages_see(const PagesArgs& a, const PagesJob& job, int i, int start) {
@@ -175,15 +172,68 @@ __device__ __forceinline__ void pages_store32(float* p, bool wide, const float* 
 __device__ __forceinline__ void pages_store(uint16_t* p, float y) { *p = f32_to_bf16_bits(y); }
 __device__ __forceinline__ void pages_store(float* p, float y) { *p = y; }
 
+// A warp's copies of one kind (kv 0: keys, 1: values) into a ring of its own, tile after tile over all jobs.  A lane per page that a tile touches; page
+// ids come by windows of 32, looked up a window ahead.
+template <int HD, int kKeys, int kSlots>
+struct PagesFetch {
+    static constexpr int kTile = kKeys * HD * 2;
+    RingPlace<kSlots> place;
+    uint32_t count = 0;
+
+    // said(tile, present): which groups of eight positions of a tile are there, said before its copies.
+    template <typename Say>
+    __device__ __forceinline__ bool run(const PagesArgs& a, const PagesJob& job, int kv, unsigned char* ring, unsigned long long* full, unsigned long long* empty,
+                                        volatile int* dead, Say say) {
+        const int lane = threadIdx.x & 31, ps = a.w.page_size, total8 = (job.base + job.n + 7) & ~7;
+        const size_t page_elems = (size_t)2 * a.w.Hkv * kv16_block_elems(a.w, HD);
+        const uint16_t* const block = kv16_block(a.p, a.w, a.p.layer, 0, kv, job.head);
+        const int32_t* const table = a.w.table + (size_t)job.req * a.w.max_pages;
+        const int pages = (total8 - 1) / ps + 1, per = kKeys / ps, over = kKeys % ps;
+        auto look = [&](int c) { return c < pages ? table[c] : -1; };
+        int p0 = job.u0 * kKeys, page0 = p0 / ps, off0 = p0 % ps;              // the tile's first position, its page, and where it lies in it
+        int window = page0, ids = look(window + lane), ids_next = look(window + 32 + lane);
+        for (int j = 0; j < job.tiles; ++j) {
+            const int start = max(0, lane * ps - off0), end = min(min(kKeys, (lane + 1) * ps - off0), total8 - p0), at = page0 - window + lane;
+            const int x = __shfl_sync(0xffffffffu, ids, at & 31), y = __shfl_sync(0xffffffffu, ids_next, at & 31), id = at < 32 ? x : y;
+            const bool there = start < end && id >= 0 && id < a.w.n_pages;
+            const uint16_t* const src = block + (there ? id * page_elems + (size_t)(start + off0 - lane * ps) * HD : 0);
+            const uint32_t groups = there ? ((1u << ((end - start) >> 3)) - 1u) << (start >> 3) : 0u, present = __reduce_or_sync(0xffffffffu, groups);
+            say(j, present);
+            if (count >= kSlots && !warp_wait(smem_u32(&empty[place.slot]), place.phase ^ 1, dead)) return false;
+            const uint32_t bar = smem_u32(&full[place.slot]);
+            if (lane == 0) mbar_expect_tx(bar, (uint32_t)__popc(present) * (HD * 16));
+            __syncwarp();
+            if (there) bulk_g2s(smem_u32(ring + place.slot * kTile) + (uint32_t)start * (HD * 2), src, (uint32_t)(end - start) * (HD * 2), bar);
+            place.next();
+            ++count;
+            p0 += kKeys;
+            page0 += per;
+            off0 += over;
+            if (off0 >= ps) { off0 -= ps; ++page0; }
+            if (page0 - window >= 32) {
+                window += 32;
+                ids = ids_next;
+                ids_next = look(window + 32 + lane);
+            }
+        }
+        return true;
+    }
+    // Given up: the copies in flight are waited for.
+    __device__ __forceinline__ void drain(unsigned long long* full) {
+        for (uint32_t i = count > kSlots ? count - kSlots : 0; i < count; ++i) mbar_wait(smem_u32(&full[i % kSlots]), i / kSlots & 1);
+    }
+};
+
 template <int HD, typename T>
-__global__ void __launch_bounds__(kPagesThreads, 1) pages_attend_kernel(const PagesArgs a) {
+__global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const PagesArgs a) {
     using Shape = PagesShape<HD, T>;
-    constexpr int kKeys = Shape::kKeys, kTile = Shape::kTile, kStages = Shape::kStages, kTerms = Shape::kTerms, kPieces = HD / 8;
+    constexpr int kKeys = Shape::kKeys, kTile = Shape::kTile, kKSlots = Shape::kKSlots, kVSlots = Shape::kVSlots, kTerms = Shape::kTerms, kPieces = HD / 8;
     constexpr uint32_t kIdescS = umma_idesc_bf16(128, kKeys, 0, 0), kIdescO = umma_idesc_bf16(128, HD, 0, 1);
     extern __shared__ unsigned char smem_raw[];
     unsigned char* const smem = smem_raw + ((128u - (smem_u32(smem_raw) & 127u)) & 127u);
-    unsigned char* const ring = smem + Shape::kQ;
-    PagesControl& c = *reinterpret_cast<PagesControl*>(ring + kStages * kTile);
+    unsigned char* const k_ring = smem + Shape::kQ;
+    unsigned char* const v_ring = k_ring + kKSlots * kTile;
+    PagesControl& c = *reinterpret_cast<PagesControl*>(v_ring + kVSlots * kTile);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int G = a.Hq / a.w.Hkv;
     volatile int* const dead = &c.dead;
@@ -191,14 +241,18 @@ __global__ void __launch_bounds__(kPagesThreads, 1) pages_attend_kernel(const Pa
 
     if (tid == 0) {
         mbar_init(smem_u32(&c.job_full), 1);
-        mbar_init(smem_u32(&c.job_read), 9);
+        mbar_init(smem_u32(&c.job_read), 10);   // all other roles' warps
         mbar_init(smem_u32(&c.q_full), 8);
         mbar_init(smem_u32(&c.q_empty), 1);
         mbar_init(smem_u32(&c.joint), 8);
         mbar_init(smem_u32(&c.done), 1);
-        for (int i = 0; i < kStages; ++i) {
-            mbar_init(smem_u32(&c.full[i]), 1);
-            mbar_init(smem_u32(&c.empty[i]), 1);
+        for (int i = 0; i < kKSlots; ++i) {
+            mbar_init(smem_u32(&c.k_full[i]), 1);
+            mbar_init(smem_u32(&c.k_empty[i]), 1);
+        }
+        for (int i = 0; i < kVSlots; ++i) {
+            mbar_init(smem_u32(&c.v_full[i]), 1);
+            mbar_init(smem_u32(&c.v_empty[i]), 1);
         }
         for (int s = 0; s < 2; ++s) {
             mbar_init(smem_u32(&c.s_full[s]), 1);
@@ -214,190 +268,177 @@ __global__ void __launch_bounds__(kPagesThreads, 1) pages_attend_kernel(const Pa
     tc_fence_after();
     const uint32_t tmem = c.tmem;                  // stream s: scores and weights at 128 s, sums at 256 + HD s
 
-    if (warp == 8) {                               // ---- what there is to do, and fetches
-        long long before;
-        const long long all = pages_total(a, -1, before), share = pages_share(a, all);
-        long long f = (long long)blockIdx.x * share, off = 0;
-        const long long f_cta = f, f_end = min(f + share, all);
-        int req = f < f_end ? pages_find(a, f, off) : a.w.n_req;
-        uint32_t entry = 0, tile_no = 0;
-        bool ok = true;
-        for (int i = 0; ok; ++i) {
-            PagesJob job = {};
-            while (f < f_end && req < a.w.n_req) {
-                int n, first, base, units, groups;
-                pages_load(a, req, n, first, base, units, groups);
-                if (off >= (long long)units * groups * a.w.Hkv) { ++req; off = 0; continue; }      // (requests without rows have no tiles)
-                const int triple = (int)(off / units);
-                job.req = req; job.n = n; job.first = first; job.base = base; job.units = units;
-                job.head = triple / groups;
-                job.rho0 = triple % groups * Shape::kRows;
-                job.n_rows = min(Shape::kRows, n * G - job.rho0);
-                job.u0 = (int)(off % units);
-                job.u1 = (int)min((long long)units, job.u0 + (f_end - f));
-                job.slot = 2 * blockIdx.x + (f - job.u0 > f_cta ? 1 : 0);
-                // without a mask no row of the group sees what lies behind its last one
-                const int seen = a.mask ? units : min(units, (base + (job.rho0 + job.n_rows - 1) / G) / kKeys + 1);
-                job.tiles = max(1, min(job.u1, seen) - job.u0);                // (a tile at least: the others' sums are none)
-                f += job.u1 - job.u0;
-                off += job.u1 - job.u0;
-                break;
-            }
-            if (i > 0) ok = warp_wait(smem_u32(&c.job_read), (i - 1) & 1, dead);
-            if (!ok) break;
-            if (lane == 0) {
-                c.jobs[i & 1] = job;
-                c.bad_lo[i & 1] = INT32_MAX;
-                c.bad_hi[i & 1] = -1;
-                mbar_arrive(smem_u32(&c.job_full));
-            }
-            if (job.tiles == 0) break;
-            // a lane per page of a tile; the pages of tile j + 1 are looked up ahead of tile j's copies
-            const int total = job.base + job.n, total8 = (total + 7) & ~7;
-            const uint16_t* block[2] = {nullptr, nullptr};                     // where the lane's piece of K begins (tile j even, odd)
-            uint32_t bytes[2] = {0, 0}, to[2] = {0, 0};
-            const size_t v_off = (size_t)a.w.Hkv * kv16_block_elems(a.w, HD);  // from a K block to its V block
-            auto locate = [&](int j) {
-                const int p0 = (job.u0 + j) * kKeys, page_no = p0 / a.w.page_size + lane;
-                const int start = max(p0, page_no * a.w.page_size), end = min(min(p0 + kKeys, (page_no + 1) * a.w.page_size), total8);
-                int page = -1;
-                if (start < end) page = kv16_page(a.w, job.req, start);
-                block[j & 1] = nullptr;
-                bytes[j & 1] = 0;
-                if (page >= 0) {
-                    block[j & 1] = kv16_block(a.p, a.w, a.p.layer, page, 0, job.head) + (size_t)(start % a.w.page_size) * HD;
-                    bytes[j & 1] = (uint32_t)(end - start) * HD * 2;
-                    to[j & 1] = (uint32_t)(start - p0) * HD * 2;
-                }
-            };
-            auto fetch = [&](int j, int v) {
-                const int st = entry % kStages;
-                if (entry >= kStages) ok = warp_wait(smem_u32(&c.empty[st]), (entry / kStages - 1) & 1, dead);
-                if (!ok) return;
-                const uint32_t bar = smem_u32(&c.full[st]), sum = __reduce_add_sync(0xffffffffu, bytes[j & 1]);
-                if (v == 0) {
-                    const uint32_t groups = bytes[j & 1] / (HD * 16), bits = groups ? ((1u << groups) - 1u) << (to[j & 1] / (HD * 16)) : 0u;
-                    const uint32_t present = __reduce_or_sync(0xffffffffu, bits);
-                    if (lane == 0) c.present[(tile_no + j) & 31] = present;
-                }
-                if (lane == 0) mbar_expect_tx(bar, sum);
-                __syncwarp();
-                if (block[j & 1]) bulk_g2s(smem_u32(ring + st * kTile) + to[j & 1], block[j & 1] + (v ? v_off : 0), bytes[j & 1], bar);
-                ++entry;
-            };
-            locate(0);
-            fetch(0, 0);
-            for (int j = 0; j < job.tiles && ok; ++j) {
-                if (j + 1 < job.tiles) {
-                    locate(j + 1);
-                    fetch(j + 1, 0);
-                }
-                if (ok) fetch(j, 1);
-            }
-            tile_no += job.tiles;
-        }
-        if (!ok && lane == 0) {                    // given up: the copies in flight are waited for
-            for (uint32_t e = entry > kStages ? entry - kStages : 0; e < entry; ++e) mbar_wait(smem_u32(&c.full[e % kStages]), (e / kStages) & 1);
-        }
-        __syncwarp();
-    } else if (warp == 9) {                        // ---- products
-        if (lane == 0) {
-            uint32_t entry = 0;
+    if (warp >= 8) {
+        registers_fewer();
+        if (warp == 8) {                               // ---- what there is to do, and keys
+            long long before;
+            const long long all = pages_total(a, -1, before), share = pages_share(a, all);
+            long long f = (long long)blockIdx.x * share, off = 0;
+            const long long f_cta = f, f_end = min(f + share, all);
+            int req = f < f_end ? pages_find(a, f, off) : a.w.n_req;
+            PagesFetch<HD, kKeys, kKSlots> fetch;
+            uint32_t tile_no = 0;
             bool ok = true;
-            auto scores = [&](int s, int q_tile, uint32_t e) {
-                const uint32_t q = smem_u32(smem + q_tile * Shape::kQTile), k = smem_u32(ring + e % kStages * kTile);
-#pragma unroll
-                for (int t = 0; t < kTerms; ++t)
-#pragma unroll
-                    for (int x = 0; x < HD / 16; ++x)
-                        umma_bf16(tmem + 128 * s, umma_desc(q + t * Shape::kQTile + x * 256, 128, HD * 16), umma_desc(k + x * 256, 128, HD * 16), kIdescS, t + x > 0);
-                umma_commit(smem_u32(&c.s_full[s]));
-            };
-            uint32_t p_phase[2] = {0, 0};
-            auto sums = [&](int s, uint32_t e, bool first, bool last) {
-                ok = ok && role_wait(smem_u32(&c.p_full[s]), p_phase[s], dead);
-                p_phase[s] ^= 1;
-                if (!ok) return;
-                tc_fence_after();
-                const uint32_t v = smem_u32(ring + e % kStages * kTile);
-#pragma unroll
-                for (int t = 0; t < kTerms; ++t)
-#pragma unroll
-                    for (int x = 0; x < kKeys / 16; ++x)
-                        umma_bf16_ta(tmem + 256 + HD * s, tmem + 128 * s + t * (kKeys / 2) + 8 * x, umma_desc(v + x * HD * 32, HD * 16, 128), kIdescO, !first || t + x > 0);
-                if (last) umma_commit(smem_u32(&c.o_full[s]));
-            };
-            auto arrived = [&](uint32_t e) {
-                ok = ok && role_wait(smem_u32(&c.full[e % kStages]), (e / kStages) & 1, dead);
-                if (ok) tc_fence_after();
-                return ok;
-            };
-            auto release = [&](uint32_t e) { umma_commit(smem_u32(&c.empty[e % kStages])); };
             for (int i = 0; ok; ++i) {
-                ok = role_wait(smem_u32(&c.job_full), i & 1, dead);
+                PagesJob job = {};
+                while (f < f_end && req < a.w.n_req) {
+                    int n, first, base, units, groups;
+                    pages_load(a, req, n, first, base, units, groups);
+                    if (off >= (long long)units * groups * a.w.Hkv) { ++req; off = 0; continue; }      // (requests without rows have no tiles)
+                    const int triple = (int)(off / units);
+                    job.req = req; job.n = n; job.first = first; job.base = base; job.units = units;
+                    job.head = triple / groups;
+                    job.rho0 = triple % groups * Shape::kRows;
+                    job.n_rows = min(Shape::kRows, n * G - job.rho0);
+                    job.u0 = (int)(off % units);
+                    job.u1 = (int)min((long long)units, job.u0 + (f_end - f));
+                    job.slot = 2 * blockIdx.x + (f - job.u0 > f_cta ? 1 : 0);
+                    // without a mask no row of the group sees what lies behind its last one
+                    const int seen = a.mask ? units : min(units, (base + (job.rho0 + job.n_rows - 1) / G) / kKeys + 1);
+                    job.tiles = max(1, min(job.u1, seen) - job.u0);                // (a tile at least: the others' sums are none)
+                    f += job.u1 - job.u0;
+                    off += job.u1 - job.u0;
+                    break;
+                }
+                if (i > 0) ok = warp_wait(smem_u32(&c.job_read), (i - 1) & 1, dead);
                 if (!ok) break;
-                const int n = c.jobs[i & 1].tiles;
-                const bool both = c.jobs[i & 1].n_rows > 128;
-                mbar_arrive(smem_u32(&c.job_read));
-                if (n == 0) break;
-                ok = role_wait(smem_u32(&c.q_full), i & 1, dead);
-                if (!ok || !arrived(entry)) break;
-                if (both) {
-                    scores(0, 0, entry);
-                    scores(1, 1, entry);
-                    release(entry);
-                    if (n == 1) umma_commit(smem_u32(&c.q_empty));
-                    for (int j = 0; j < n; ++j) {
-                        const uint32_t ev = entry + pages_v(j, n), ek = entry + pages_k(j + 1);
-                        const bool more = j + 1 < n;
-                        if (!arrived(ev)) break;
-                        sums(0, ev, j == 0, !more);
-                        if (!ok) break;
-                        if (more) {
-                            if (!arrived(ek)) break;
-                            scores(0, 0, ek);
+                if (lane == 0) {
+                    c.jobs[i & 1] = job;
+                    c.bad_lo[i & 1] = INT32_MAX;
+                    c.bad_hi[i & 1] = -1;
+                    mbar_arrive(smem_u32(&c.job_full));
+                }
+                if (job.tiles == 0) break;
+                ok = fetch.run(a, job, 0, k_ring, c.k_full, c.k_empty, dead, [&](int j, uint32_t present) {
+                    if (lane == 0) c.present[(tile_no + j) & 31] = present;
+                });
+                tile_no += job.tiles;
+            }
+            if (!ok) fetch.drain(c.k_full);
+        } else if (warp == 10) {                       // ---- values
+            PagesFetch<HD, kKeys, kVSlots> fetch;
+            bool ok = true;
+            for (int i = 0; ok; ++i) {
+                ok = warp_wait(smem_u32(&c.job_full), i & 1, dead);
+                if (!ok) break;
+                const PagesJob job = c.jobs[i & 1];
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&c.job_read));
+                if (job.tiles == 0) break;
+                ok = fetch.run(a, job, 1, v_ring, c.v_full, c.v_empty, dead, [](int, uint32_t) {});
+            }
+            if (!ok) fetch.drain(c.v_full);
+        } else if (warp == 9) {                        // ---- products
+            if (elect_one()) {
+                RingPlace<kKSlots> kp;
+                RingPlace<kVSlots> vp;
+                bool ok = true;
+                const uint64_t q_desc = umma_desc(smem_u32(smem), 128, HD * 16), k_desc = umma_desc(smem_u32(k_ring), 128, HD * 16),
+                               v_desc = umma_desc(smem_u32(v_ring), HD * 16, 128);
+                uint32_t p_phase[2] = {0, 0};
+                // The next keys have come / the scores of stream s against them / their slot is free when what was issued so far is done; and so for values.
+                auto k_there = [&] {
+                    ok = ok && role_wait(smem_u32(&c.k_full[kp.slot]), kp.phase, dead);
+                    if (ok) tc_fence_after();
+                    return ok;
+                };
+                auto v_there = [&] {
+                    ok = ok && role_wait(smem_u32(&c.v_full[vp.slot]), vp.phase, dead);
+                    return ok;
+                };
+                auto scores = [&](int s, int q_tile) {
+                    const uint64_t q = q_desc + (uint32_t)(q_tile * (Shape::kQTile >> 4)), k = k_desc + kp.slot * (uint32_t)(kTile >> 4);
+#pragma unroll
+                    for (int t = 0; t < kTerms; ++t)
+#pragma unroll
+                        for (int x = 0; x < HD / 16; ++x)
+                            umma_bf16(tmem + 128 * s, q + ((kTerms - 1 - t) * (Shape::kQTile >> 4) + x * 16), k + x * 16, kIdescS, t + x > 0);
+                    umma_commit(smem_u32(&c.s_full[s]));
+                };
+                auto k_done = [&] {
+                    umma_commit(smem_u32(&c.k_empty[kp.slot]));
+                    kp.next();
+                };
+                auto sums = [&](int s, bool first, bool last) {
+                    ok = ok && role_wait(smem_u32(&c.p_full[s]), p_phase[s], dead);
+                    p_phase[s] ^= 1;
+                    if (!ok) return false;
+                    tc_fence_after();
+                    const uint64_t v = v_desc + vp.slot * (uint32_t)(kTile >> 4);
+#pragma unroll
+                    for (int t = 0; t < kTerms; ++t)
+#pragma unroll
+                        for (int x = 0; x < kKeys / 16; ++x)
+                            umma_bf16_ta(tmem + 256 + HD * s, tmem + 128 * s + (kTerms - 1 - t) * (kKeys / 2) + 8 * x, v + x * HD * 2, kIdescO, !first || t + x > 0);
+                    if (last) umma_commit(smem_u32(&c.o_full[s]));
+                    return true;
+                };
+                auto v_done = [&] {
+                    umma_commit(smem_u32(&c.v_empty[vp.slot]));
+                    vp.next();
+                };
+                for (int i = 0; ok; ++i) {
+                    ok = role_wait(smem_u32(&c.job_full), i & 1, dead);
+                    if (!ok) break;
+                    const int n = c.jobs[i & 1].tiles;
+                    const bool both = c.jobs[i & 1].n_rows > 128;
+                    mbar_arrive(smem_u32(&c.job_read));
+                    if (n == 0) break;
+                    ok = role_wait(smem_u32(&c.q_full), i & 1, dead);
+                    if (!k_there()) break;
+                    if (both) {
+                        scores(0, 0);
+                        scores(1, 1);
+                        k_done();
+                        if (n == 1) umma_commit(smem_u32(&c.q_empty));
+                        for (int j = 0; j < n; ++j) {
+                            const bool more = j + 1 < n;
+                            if (!v_there() || !sums(0, j == 0, !more)) break;
+                            if (more) {
+                                if (!k_there()) break;
+                                scores(0, 0);
+                            }
+                            if (!sums(1, j == 0, !more)) break;
+                            v_done();
+                            if (more) {
+                                scores(1, 1);
+                                k_done();
+                                if (j + 2 == n) umma_commit(smem_u32(&c.q_empty));
+                            }
                         }
-                        sums(1, ev, j == 0, !more);
-                        if (!ok) break;
-                        release(ev);
-                        if (more) {
-                            scores(1, 1, ek);
-                            release(ek);
-                            if (j + 2 == n) umma_commit(smem_u32(&c.q_empty));
+                    } else {
+                        scores(0, 0);
+                        k_done();
+                        if (n > 1) {
+                            if (!k_there()) break;
+                            scores(1, 0);
+                            k_done();
                         }
-                    }
-                } else {
-                    scores(0, 0, entry);
-                    release(entry);
-                    if (n > 1) {
-                        if (!arrived(entry + 1)) break;
-                        scores(1, 0, entry + 1);
-                        release(entry + 1);
-                    }
-                    if (n <= 2) umma_commit(smem_u32(&c.q_empty));
-                    for (int j = 0; j < n; ++j) {
-                        const uint32_t ev = entry + pages_v(j, n);
-                        if (!arrived(ev)) break;
-                        sums(j & 1, ev, j < 2, j + 2 >= n);
-                        if (!ok) break;
-                        release(ev);
-                        if (j + 2 < n) {
-                            const uint32_t ek = entry + pages_k(j + 2);
-                            if (!arrived(ek)) break;
-                            scores(j & 1, 0, ek);
-                            release(ek);
-                            if (j + 3 == n) umma_commit(smem_u32(&c.q_empty));
+                        if (n <= 2) umma_commit(smem_u32(&c.q_empty));
+                        for (int j = 0; j < n; ++j) {
+                            if (!v_there() || !sums(j & 1, j < 2, j + 2 >= n)) break;
+                            v_done();
+                            if (j + 2 < n) {
+                                if (!k_there()) break;
+                                scores(j & 1, 0);
+                                k_done();
+                                if (j + 3 == n) umma_commit(smem_u32(&c.q_empty));
+                            }
                         }
                     }
                 }
-                entry += 2 * n;
+                if (!ok) {                             // products in flight end before their memory is given back
+                    umma_commit(smem_u32(&c.done));
+                    mbar_wait(smem_u32(&c.done), 0);
+                }
             }
+            __syncwarp();
         }
-        __syncwarp();
     } else {                                       // ---- a stream's rows
+        registers_more();
         const int s = warp >> 2, row = tid & 127;
         const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16, s_tmem = tmem + 128 * s + lanes, o_tmem = tmem + 256 + HD * s + lanes;
-        uint32_t entry = 0, tile_no = 0, s_phase = 0, o_phase[2] = {0, 0}, joint_phase = 0;
+        uint32_t tile_no = 0, s_phase = 0, o_phase[2] = {0, 0}, joint_phase = 0;
         auto joint = [&] {                         // both streams' warps
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&c.joint));
@@ -416,16 +457,23 @@ __global__ void __launch_bounds__(kPagesThreads, 1) pages_attend_kernel(const Pa
             // ---- queries, in the products' order: 8 x 4 pieces of 8 columns a warp and step
             bool ok = i == 0 || warp_wait(smem_u32(&c.q_empty), (i - 1) & 1, dead);
             if (ok) {
+                constexpr int kBatch = 8 / (int)(sizeof(T) / 2);               // loads of a thread at once
                 const int steps = (job.n_rows + 7) / 8 * (kPieces / 4);
-                for (int x = warp; x < steps; x += 8) {
-                    const int rho = x / (kPieces / 4) * 8 + (lane & 7), piece = x % (kPieces / 4) * 4 + (lane >> 3);
-                    if (rho < job.n_rows) {
-                        const int at = job.rho0 + rho;
-                        uint4 v[kTerms];
-                        pages_load8(static_cast<const T*>(a.q) + (job.first + at / G) * a.q_stride + (size_t)(job.head * G + at % G) * HD + piece * 8, a.q_wide, v);
+                for (int x0 = warp; x0 < steps; x0 += 8 * kBatch) {
+                    uint4 v[kBatch][kTerms];
 #pragma unroll
-                        for (int t = 0; t < kTerms; ++t)
-                            *reinterpret_cast<uint4*>(smem + (t + (rho >> 7)) * Shape::kQTile + ((rho & 127) >> 3) * HD * 16 + piece * 128 + (rho & 7) * 16) = v[t];
+                    for (int y = 0; y < kBatch; ++y) {
+                        const int x = x0 + 8 * y, r = x / (kPieces / 4) * 8 + (lane & 7), at = job.rho0 + r, piece = x % (kPieces / 4) * 4 + (lane >> 3);
+                        if (r < job.n_rows)
+                            pages_load8(static_cast<const T*>(a.q) + (job.first + at / G) * a.q_stride + (size_t)(job.head * G + at % G) * HD + piece * 8, a.q_wide, v[y]);
+                    }
+#pragma unroll
+                    for (int y = 0; y < kBatch; ++y) {
+                        const int x = x0 + 8 * y, r = x / (kPieces / 4) * 8 + (lane & 7), piece = x % (kPieces / 4) * 4 + (lane >> 3);
+                        if (r < job.n_rows)
+#pragma unroll
+                            for (int t = 0; t < kTerms; ++t)
+                                *reinterpret_cast<uint4*>(smem + (t + (r >> 7)) * Shape::kQTile + ((r & 127) >> 3) * HD * 16 + piece * 128 + (r & 7) * 16) = v[y][t];
                     }
                 }
                 fence_proxy_async_smem();
@@ -434,7 +482,7 @@ __global__ void __launch_bounds__(kPagesThreads, 1) pages_attend_kernel(const Pa
             if (ok && lane == 0) mbar_arrive(smem_u32(&c.q_full));
             const int local = both ? 128 * s + row : row;                      // of the group's rows
             const bool mine = local < job.n_rows, any = (both ? 128 * s : 0) + 32 * (warp & 3) < job.n_rows;
-            const int at = job.rho0 + (mine ? local : 0), node = at / G;
+            const int rho = job.rho0 + (mine ? local : 0), node = rho / G;
             // tiles that every row of the stream sees whole
             const int clear = (a.mask ? job.base : job.base + (job.rho0 + (both ? 128 * s : 0)) / G + 1) / kKeys;
             float ref = -INFINITY, sum = 0.f;
@@ -462,11 +510,11 @@ __global__ void __launch_bounds__(kPagesThreads, 1) pages_attend_kernel(const Pa
                 }
                 if (any) softmax_tile<HD, kKeys, kTerms>(s_tmem, o_tmem, a.scale, both ? j == 0 : j < 2, masked, see, ref, sum);
                 if (masked) {
-                    const uint32_t ev = entry + pages_v(j, n);
-                    ok = warp_wait(smem_u32(&c.full[ev % kStages]), (ev / kStages) & 1, dead);
+                    const uint32_t at = tile_no + j;                           // of the values fetched by this CTA
+                    ok = warp_wait(smem_u32(&c.v_full[at % kVSlots]), at / kVSlots & 1, dead);
                     if (!ok) break;
                     const int keys = job.base + job.n - u * kKeys;
-                    if (clean_values(ring + ev % kStages * kTile, kTile / 16, row, 128, [&](int p) {
+                    if (clean_values(v_ring + at % kVSlots * kTile, kTile / 16, row, 128, [&](int p) {
                             const int key = p / kPieces / 8 * 8 + p % 8;
                             return key < keys && (present >> (key >> 3) & 1u);
                         })) {
@@ -487,9 +535,8 @@ __global__ void __launch_bounds__(kPagesThreads, 1) pages_attend_kernel(const Pa
             if (ok && has[1] && (both ? s == 1 : true)) ok = warp_wait(smem_u32(&c.o_full[1]), o_phase[1], dead);
             o_phase[0] ^= 1;
             if (has[1]) o_phase[1] ^= 1;
-            entry += 2 * n;
             tile_no += n;
-            T* const out = static_cast<T*>(a.out) + (job.first + node) * a.out_stride + (size_t)(job.head * G + at % G) * HD;
+            T* const out = static_cast<T*>(a.out) + (job.first + node) * a.out_stride + (size_t)(job.head * G + rho % G) * HD;
             const bool whole = job.u0 == 0 && job.u1 == job.units;
             float* const part = a.parts + (size_t)job.slot * a.cap * (HD + 2);
             if (ok && !both) {
@@ -571,11 +618,6 @@ __global__ void __launch_bounds__(kPagesThreads, 1) pages_attend_kernel(const Pa
     }
     __syncthreads();
     if (warp == 9) {
-        if (c.dead && lane == 0) {                 // products in flight end before their memory is given back
-            umma_commit(smem_u32(&c.done));
-            mbar_wait(smem_u32(&c.done), 0);
-        }
-        __syncwarp();
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }

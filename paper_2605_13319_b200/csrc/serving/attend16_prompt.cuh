@@ -23,7 +23,7 @@ struct PromptArgs {
 struct PromptJob {
     int first, n, t0, head;     // the prompt's first row and length (0: no more jobs), the job's first token
 };
-constexpr int kPromptThreads = 320, kPromptJobs = 2;
+constexpr int kPromptJobs = 2;
 
 struct PromptControl {
     unsigned long long q_full, q_empty, full[16], empty[16], s_full[2], p_full[2], o_full[2], done;
@@ -97,7 +97,7 @@ __device__ __forceinline__ int prompt_tiles(const PromptJob& job, int s, int T) 
 }
 
 template <int HD>
-__global__ void __launch_bounds__(kPromptThreads, 1)
+__global__ void __launch_bounds__(kAttendThreads16, 1)
     prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const PromptArgs a) {
     using Shape = PromptShape<HD>;
     constexpr int kTile = Shape::kTile, kStages = Shape::kStages, kAtom = 128 * 128;      // an atom: 128 rows of 64 columns
@@ -132,107 +132,115 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
     tc_fence_after();
     const uint32_t tmem = c.tmem;                  // stream s: scores and weights at 128 s, sums at 256 + HD s
 
-    if (warp == 8) {                               // ---- fetches
-        int levels = 0;
-        for (int r = lane; r < a.n_req; r += 32) {
-            int first;
-            levels = max(levels, (prompt_len(a, r, first) + 2 * T - 1) / (2 * T));
-        }
-        levels = __reduce_max_sync(0xffffffffu, levels);
-        uint32_t entry = 0;                        // of the ring, over all jobs
-        bool ok = true;
-        for (int i = 0; ok; ++i) {
-            const long long round = (long long)i * a.ctas;
-            const PromptJob job = prompt_job(a, i & 1 ? round + a.ctas - 1 - blockIdx.x : round + blockIdx.x, 2 * T, levels);
-            if (i > 0) ok = warp_wait(smem_u32(&c.q_empty), (i - 1) & 1, dead);
-            if (lane == 0 && ok) {
-                c.jobs[i % kPromptJobs] = job;
-                c.flags[i % kPromptJobs] = 0;
-                if (job.n == 0) {
-                    mbar_arrive(smem_u32(&c.q_full));
-                } else {
-                    const int tiles[2] = {prompt_tiles(job, 0, T), prompt_tiles(job, 1, T)};
-                    const uint32_t bar = smem_u32(&c.q_full);
-                    mbar_expect_tx(bar, (uint32_t)((tiles[1] ? 2 : 1) * (HD / 64) * T * G * 128));
-                    for (int s = 0; s < 2; ++s)
-                        for (int x = 0; tiles[s] && x < HD / 64; ++x)
-                            tensor3_g2s(smem_u32(smem + s * kTile + x * kAtom), &map_q, 64 * x, job.head * G, job.first + job.t0 + s * T, bar);
-                    const int n = max(tiles[0], tiles[1]);
-                    for (int e = 0; e < 2 * n && ok; ++e, ++entry) {
-                        const int st = entry % kStages;
-                        if (entry >= kStages) ok = role_wait(smem_u32(&c.empty[st]), (entry / kStages - 1) & 1, dead);
-                        if (!ok) break;
-                        const uint32_t full = smem_u32(&c.full[st]);
-                        mbar_expect_tx(full, kTile);
-                        for (int x = 0; x < HD / 64; ++x)
-                            tensor3_g2s(smem_u32(ring + st * kTile + x * kAtom), e & 1 ? &map_v : &map_k, 64 * x, job.head, job.first + (e >> 1) * 128, full);
+    if (warp >= 8) {
+        registers_fewer();
+        if (warp == 8) {                               // ---- fetches
+            int levels = 0;
+            for (int r = lane; r < a.n_req; r += 32) {
+                int first;
+                levels = max(levels, (prompt_len(a, r, first) + 2 * T - 1) / (2 * T));
+            }
+            levels = __reduce_max_sync(0xffffffffu, levels);
+            uint32_t entry = 0;                        // of the ring, over all jobs
+            bool ok = true;
+            for (int i = 0; ok; ++i) {
+                const long long round = (long long)i * a.ctas;
+                const PromptJob job = prompt_job(a, i & 1 ? round + a.ctas - 1 - blockIdx.x : round + blockIdx.x, 2 * T, levels);
+                if (i > 0) ok = warp_wait(smem_u32(&c.q_empty), (i - 1) & 1, dead);
+                if (lane == 0 && ok) {
+                    c.jobs[i % kPromptJobs] = job;
+                    c.flags[i % kPromptJobs] = 0;
+                    if (job.n == 0) {
+                        mbar_arrive(smem_u32(&c.q_full));
+                    } else {
+                        const int tiles[2] = {prompt_tiles(job, 0, T), prompt_tiles(job, 1, T)};
+                        const uint32_t bar = smem_u32(&c.q_full);
+                        mbar_expect_tx(bar, (uint32_t)((tiles[1] ? 2 : 1) * (HD / 64) * T * G * 128));
+                        for (int s = 0; s < 2; ++s)
+                            for (int x = 0; tiles[s] && x < HD / 64; ++x)
+                                tensor3_g2s(smem_u32(smem + s * kTile + x * kAtom), &map_q, 64 * x, job.head * G, job.first + job.t0 + s * T, bar);
+                        const int n = max(tiles[0], tiles[1]);
+                        for (int e = 0; e < 2 * n && ok; ++e, ++entry) {
+                            const int st = entry % kStages;
+                            if (entry >= kStages) ok = role_wait(smem_u32(&c.empty[st]), (entry / kStages - 1) & 1, dead);
+                            if (!ok) break;
+                            const uint32_t full = smem_u32(&c.full[st]);
+                            mbar_expect_tx(full, kTile);
+                            for (int x = 0; x < HD / 64; ++x)
+                                tensor3_g2s(smem_u32(ring + st * kTile + x * kAtom), e & 1 ? &map_v : &map_k, 64 * x, job.head, job.first + (e >> 1) * 128, full);
+                        }
                     }
                 }
-            }
-            ok = __shfl_sync(0xffffffffu, ok, 0);
-            entry = __shfl_sync(0xffffffffu, entry, 0);
-            if (job.n == 0) break;
-        }
-        if (!ok && lane == 0) {                    // given up: the copies in flight are waited for
-            for (uint32_t e = entry > kStages ? entry - kStages : 0; e < entry; ++e) mbar_wait(smem_u32(&c.full[e % kStages]), (e / kStages) & 1);
-        }
-    } else if (warp == 9) {                        // ---- products
-        if (lane == 0) {
-            uint32_t entry = 0;
-            bool ok = true;
-            auto scores = [&](int s, uint32_t e) {
-                const uint32_t q = smem_u32(smem + s * kTile), k = smem_u32(ring + e % kStages * kTile);
-#pragma unroll
-                for (int x = 0; x < HD / 16; ++x) {
-                    const uint32_t at = (x >> 2) * kAtom + (x & 3) * 32;
-                    umma_bf16(tmem + 128 * s, umma_desc_swizzled(q + at, 16, 1024), umma_desc_swizzled(k + at, 16, 1024), kIdescS, x > 0);
-                }
-                umma_commit(smem_u32(&c.s_full[s]));
-            };
-            uint32_t p_phase[2] = {0, 0};
-            auto sums = [&](int s, uint32_t e, bool first, bool last) {
-                ok = ok && role_wait(smem_u32(&c.p_full[s]), p_phase[s], dead);
-                p_phase[s] ^= 1;
-                if (!ok) return;
-                tc_fence_after();
-                const uint32_t v = smem_u32(ring + e % kStages * kTile);
-#pragma unroll
-                for (int x = 0; x < 8; ++x)
-                    umma_bf16_ta(tmem + 256 + HD * s, tmem + 128 * s + 8 * x, umma_desc_swizzled(v + x * 2048, kAtom, 1024), kIdescO, !first || x > 0);
-                if (last) umma_commit(smem_u32(&c.o_full[s]));
-            };
-            auto arrived = [&](uint32_t e) { ok = ok && role_wait(smem_u32(&c.full[e % kStages]), (e / kStages) & 1, dead); };
-            for (int i = 0; ok; ++i) {
-                ok = role_wait(smem_u32(&c.q_full), i & 1, dead);
-                if (!ok) break;
-                const PromptJob job = c.jobs[i % kPromptJobs];
+                ok = __shfl_sync(0xffffffffu, ok, 0);
+                entry = __shfl_sync(0xffffffffu, entry, 0);
                 if (job.n == 0) break;
-                const int n0 = prompt_tiles(job, 0, T), n1 = prompt_tiles(job, 1, T), n = max(n0, n1);
-                arrived(entry);
-                if (!ok) break;
-                tc_fence_after();
-                scores(0, entry);
-                if (n1) scores(1, entry);
-                umma_commit(smem_u32(&c.empty[entry % kStages]));
-                if (n == 1) umma_commit(smem_u32(&c.q_empty));
-                for (int j = 0; j < n && ok; ++j) {
-                    const uint32_t ev = entry + 2 * j + 1, ek = ev + 1;
-                    arrived(ev);
-                    if (ok && j < n0) sums(0, ev, j == 0, j == n0 - 1);
-                    if (j + 1 < n) arrived(ek);
-                    if (ok && j + 1 < n0) scores(0, ek);
-                    if (ok && j < n1) sums(1, ev, j == 0, j == n1 - 1);
-                    if (!ok) break;
-                    umma_commit(smem_u32(&c.empty[ev % kStages]));
-                    if (j + 1 < n1) scores(1, ek);
-                    if (j + 1 < n) umma_commit(smem_u32(&c.empty[ek % kStages]));
-                    if (j + 2 == n) umma_commit(smem_u32(&c.q_empty));
-                }
-                entry += 2 * n;
             }
+            if (!ok && lane == 0) {                    // given up: the copies in flight are waited for
+                for (uint32_t e = entry > kStages ? entry - kStages : 0; e < entry; ++e) mbar_wait(smem_u32(&c.full[e % kStages]), (e / kStages) & 1);
+            }
+        } else if (warp == 9) {                        // ---- products
+            if (elect_one()) {
+                uint32_t entry = 0;
+                bool ok = true;
+                auto scores = [&](int s, uint32_t e) {
+                    const uint32_t q = smem_u32(smem + s * kTile), k = smem_u32(ring + e % kStages * kTile);
+#pragma unroll
+                    for (int x = 0; x < HD / 16; ++x) {
+                        const uint32_t at = (x >> 2) * kAtom + (x & 3) * 32;
+                        umma_bf16(tmem + 128 * s, umma_desc_swizzled(q + at, 16, 1024), umma_desc_swizzled(k + at, 16, 1024), kIdescS, x > 0);
+                    }
+                    umma_commit(smem_u32(&c.s_full[s]));
+                };
+                uint32_t p_phase[2] = {0, 0};
+                auto sums = [&](int s, uint32_t e, bool first, bool last) {
+                    ok = ok && role_wait(smem_u32(&c.p_full[s]), p_phase[s], dead);
+                    p_phase[s] ^= 1;
+                    if (!ok) return;
+                    tc_fence_after();
+                    const uint32_t v = smem_u32(ring + e % kStages * kTile);
+#pragma unroll
+                    for (int x = 0; x < 8; ++x)
+                        umma_bf16_ta(tmem + 256 + HD * s, tmem + 128 * s + 8 * x, umma_desc_swizzled(v + x * 2048, kAtom, 1024), kIdescO, !first || x > 0);
+                    if (last) umma_commit(smem_u32(&c.o_full[s]));
+                };
+                auto arrived = [&](uint32_t e) { ok = ok && role_wait(smem_u32(&c.full[e % kStages]), (e / kStages) & 1, dead); };
+                for (int i = 0; ok; ++i) {
+                    ok = role_wait(smem_u32(&c.q_full), i & 1, dead);
+                    if (!ok) break;
+                    const PromptJob job = c.jobs[i % kPromptJobs];
+                    if (job.n == 0) break;
+                    const int n0 = prompt_tiles(job, 0, T), n1 = prompt_tiles(job, 1, T), n = max(n0, n1);
+                    arrived(entry);
+                    if (!ok) break;
+                    tc_fence_after();
+                    scores(0, entry);
+                    if (n1) scores(1, entry);
+                    umma_commit(smem_u32(&c.empty[entry % kStages]));
+                    if (n == 1) umma_commit(smem_u32(&c.q_empty));
+                    for (int j = 0; j < n && ok; ++j) {
+                        const uint32_t ev = entry + 2 * j + 1, ek = ev + 1;
+                        arrived(ev);
+                        if (ok && j < n0) sums(0, ev, j == 0, j == n0 - 1);
+                        if (j + 1 < n) arrived(ek);
+                        if (ok && j + 1 < n0) scores(0, ek);
+                        if (ok && j < n1) sums(1, ev, j == 0, j == n1 - 1);
+                        if (!ok) break;
+                        umma_commit(smem_u32(&c.empty[ev % kStages]));
+                        if (j + 1 < n1) scores(1, ek);
+                        if (j + 1 < n) umma_commit(smem_u32(&c.empty[ek % kStages]));
+                        if (j + 2 == n) umma_commit(smem_u32(&c.q_empty));
+                    }
+                    entry += 2 * n;
+                }
+                if (!ok) {                             // products in flight end before their memory is given back
+                    umma_commit(smem_u32(&c.done));
+                    mbar_wait(smem_u32(&c.done), 0);
+                }
+            }
+            __syncwarp();
         }
-        __syncwarp();
     } else {                                       // ---- a stream's rows
+        registers_more();
         const int s = warp >> 2, row = tid & 127, token = row / G, g = row % G;
         const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16, s_tmem = tmem + 128 * s + lanes, o_tmem = tmem + 256 + HD * s + lanes;
         uint32_t entry = 0, s_phase = 0, o_phase = 0;
@@ -317,11 +325,6 @@ __global__ void __launch_bounds__(kPromptThreads, 1)
     }
     __syncthreads();
     if (warp == 9) {
-        if (c.dead && lane == 0) {                 // products in flight end before their memory is given back
-            umma_commit(smem_u32(&c.done));
-            mbar_wait(smem_u32(&c.done), 0);
-        }
-        __syncwarp();
         tc_fence_after();
         tmem_dealloc(tmem, 512);
     }

@@ -88,6 +88,23 @@ __device__ __forceinline__ bool role_wait(uint32_t bar, uint32_t parity, volatil
 // The same for a whole warp, which goes on together.
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* dead) { return __all_sync(0xffffffffu, role_wait(bar, parity, dead)); }
 
+// Registers: twelve warps are launched with 168 each; the four that fetch and issue hand over to the eight of the streams (8 x 208 + 4 x 88 = 12 x 168).
+constexpr int kAttendThreads16 = 384, kLaunchRegisters = 168;
+__device__ __forceinline__ void registers_more() { asm volatile("setmaxnreg.inc.sync.aligned.u32 208;"); }
+__device__ __forceinline__ void registers_fewer() { asm volatile("setmaxnreg.dec.sync.aligned.u32 88;"); }
+
+// A place in a ring of n slots.
+template <int n>
+struct RingPlace {
+    uint32_t slot = 0, phase = 0;
+    __device__ __forceinline__ void next() {
+        if (++slot == n) {
+            slot = 0;
+            phase ^= 1;
+        }
+    }
+};
+
 constexpr float kRefExcess = 8.f;                  // log2 units by which a weight may exceed 1
 
 // One row's share of a tile.  `o_tmem`: the row's running sums, rescaled here if they have to be; `first`: there are none yet.  masked: bit c of `see`

@@ -42,7 +42,7 @@ template <int HD, typename T>
 int32_t pages_run(PagesArgs& a, cudaStream_t st) {
     a.keys = PagesShape<HD, T>::kKeys;
     a.rows = PagesShape<HD, T>::kRows;
-    pages_attend_kernel<HD, T><<<a.ctas, kPagesThreads, pages_smem<HD, T>(), st>>>(a);
+    pages_attend_kernel<HD, T><<<a.ctas, kAttendThreads16, pages_smem<HD, T>(), st>>>(a);
     if (cudaGetLastError() != cudaSuccess) return PIPESD_E_CUDA;
     if (launch_pdl(pages_merge_kernel<HD, T>, dim3((unsigned)(a.w.rows * a.Hq)), dim3(32 * kPagesMergeWarps), 0, st, a) != cudaSuccess) return PIPESD_E_CUDA;
     return launched();
@@ -71,19 +71,24 @@ bool rows_map(CUtensorMap* m, const void* base, int hd, int heads, int64_t rows,
 constexpr int kDevices = 64, kSms = 148;
 std::mutex g_mu;
 bool g_ready[kDevices] = {false};
+// The kernels' warps exchange registers: what they take together must be what they are launched with.
+bool attend_ready(const void* kernel, int smem) {
+    cudaFuncAttributes at;
+    return cudaFuncGetAttributes(&at, kernel) == cudaSuccess && at.numRegs == kLaunchRegisters &&
+           cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) == cudaSuccess;
+}
 template <int HD, typename T>
-bool pages_attrs() {
+bool pages_ready() {
     static_assert(pages_smem<HD, T>() <= 232448, "a CTA's shared memory");
-    return cudaFuncSetAttribute((const void*)pages_attend_kernel<HD, T>, cudaFuncAttributeMaxDynamicSharedMemorySize, pages_smem<HD, T>()) == cudaSuccess;
+    return attend_ready((const void*)pages_attend_kernel<HD, T>, pages_smem<HD, T>());
 }
 bool device_ready() {
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= kDevices) return false;
     std::lock_guard<std::mutex> lock(g_mu);
     if (!g_ready[dev])
-        g_ready[dev] = cudaFuncSetAttribute((const void*)prompt_kernel<64>, cudaFuncAttributeMaxDynamicSharedMemorySize, PromptShape<64>::kSmem) == cudaSuccess &&
-                       cudaFuncSetAttribute((const void*)prompt_kernel<128>, cudaFuncAttributeMaxDynamicSharedMemorySize, PromptShape<128>::kSmem) == cudaSuccess &&
-                       pages_attrs<64, float>() && pages_attrs<64, uint16_t>() && pages_attrs<128, float>() && pages_attrs<128, uint16_t>();
+        g_ready[dev] = attend_ready((const void*)prompt_kernel<64>, PromptShape<64>::kSmem) && attend_ready((const void*)prompt_kernel<128>, PromptShape<128>::kSmem) &&
+                       pages_ready<64, float>() && pages_ready<64, uint16_t>() && pages_ready<128, float>() && pages_ready<128, uint16_t>();
     return g_ready[dev];
 }
 
@@ -240,8 +245,8 @@ int32_t pipesd_attend_packed(const void* q, const void* k, const void* v, void* 
     const int64_t jobs = ((int64_t)rows / (2 * T) + std::min(n_req, rows)) * n_kv_heads;
     const PromptArgs a = {row0,    static_cast<const uint16_t*>(v), static_cast<uint16_t*>(out), v_stride, out_stride, n_req, rows, n_q_heads, n_kv_heads,
                           scale * 1.4426950408889634f, (int)std::min<int64_t>(jobs, kSms)};
-    if (head_dim == 128) prompt_kernel<128><<<a.ctas, kPromptThreads, PromptShape<128>::kSmem, (cudaStream_t)cuda_stream>>>(mq, mk, mv, a);
-    else prompt_kernel<64><<<a.ctas, kPromptThreads, PromptShape<64>::kSmem, (cudaStream_t)cuda_stream>>>(mq, mk, mv, a);
+    if (head_dim == 128) prompt_kernel<128><<<a.ctas, kAttendThreads16, PromptShape<128>::kSmem, (cudaStream_t)cuda_stream>>>(mq, mk, mv, a);
+    else prompt_kernel<64><<<a.ctas, kAttendThreads16, PromptShape<64>::kSmem, (cudaStream_t)cuda_stream>>>(mq, mk, mv, a);
     return launched();
 }
 
