@@ -63,6 +63,64 @@ __device__ __forceinline__ uint32_t pack_bf16(float x, float y) {      // the fi
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
+// Two fp32 values in one register pair, and what is done with both at once.
+__device__ __forceinline__ uint64_t pair_of(uint32_t x, uint32_t y) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(x), "r"(y));
+    return r;
+}
+__device__ __forceinline__ uint64_t pair_of(float x, float y) { return pair_of(__float_as_uint(x), __float_as_uint(y)); }
+__device__ __forceinline__ void pair_split(uint64_t v, float& x, float& y) {
+    uint32_t a, b;
+    asm("mov.b64 {%0, %1}, %2;" : "=r"(a), "=r"(b) : "l"(v));
+    x = __uint_as_float(a);
+    y = __uint_as_float(b);
+}
+__device__ __forceinline__ uint64_t pair_fma(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t pair_add(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t pair_mul(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+// 2^x of two values up to 127 on the multiply-add pipe, for a part of the weights, since the special-function unit alone would take as long as the
+// products: x = n + f, |f| <= 1/2, 2^f by the polynomial of degree 4 with the smallest relative error there (Remez exchange: 2.6e-6, against
+// 2^-9 of a rounding to bf16), times 2^n put together from its bits.  0 below 2^-127; a NaN stays one.
+__device__ __forceinline__ uint64_t pair_exp2(uint64_t x) {
+    float a, b;
+    pair_split(x, a, b);
+    x = pair_of(max_nan(a, -127.f), max_nan(b, -127.f));
+    const uint64_t big = pair_of(12583039.f, 12583039.f);                      // 1.5 * 2^23 + 127: the sum's low bits are n + 127
+    const uint64_t t = pair_add(x, big);
+    const uint64_t f = pair_add(x, pair_mul(pair_add(t, pair_of(-12583039.f, -12583039.f)), pair_of(-1.f, -1.f)));
+    uint64_t y = pair_of(0.009570102207362652f, 0.009570102207362652f);
+    y = pair_fma(y, f, pair_of(0.05591785907745361f, 0.05591785907745361f));
+    y = pair_fma(y, f, pair_of(0.240247443318367f, 0.240247443318367f));
+    y = pair_fma(y, f, pair_of(0.6931217908859253f, 0.6931217908859253f));
+    y = pair_fma(y, f, pair_of(0.9999992847442627f, 0.9999992847442627f));
+    float n0, n1;
+    pair_split(t, n0, n1);
+    return pair_mul(y, pair_of(__float_as_uint(n0) << 23, __float_as_uint(n1) << 23));
+}
+
 // ---- waits: bounded, and given up at once when another role of the CTA has given up
 __device__ __forceinline__ bool role_wait(uint32_t bar, uint32_t parity, volatile int* dead) {
     uint64_t t0 = 0;
@@ -105,6 +163,7 @@ struct RingPlace {
     }
 };
 
+constexpr int kPoly = 1, kPolyOf = 4;              // of so many pairs of weights, those whose exponentials are polynomials
 constexpr float kRefExcess = 8.f;                  // log2 units by which a weight may exceed 1
 
 // One row's share of a tile.  `o_tmem`: the row's running sums, rescaled here if they have to be; `first`: there are none yet.  masked: bit c of `see`
@@ -124,7 +183,7 @@ __device__ __forceinline__ void softmax_tile(uint32_t s_tmem, uint32_t o_tmem, f
     }
     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-    for (int i = 0; i < kKeys; ++i) mx[i & 3] = fmaxf(mx[i & 3], __uint_as_float(s[i]));
+    for (int i = 0; i < kKeys; i += 2) mx[(i >> 1) & 3] = max3(mx[(i >> 1) & 3], __uint_as_float(s[i]), __uint_as_float(s[i + 1]));
     const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
     const bool up = top > ref + kRefExcess || (ref == -INFINITY && top > ref);
     if (__any_sync(0xffffffffu, up)) {
@@ -144,14 +203,28 @@ __device__ __forceinline__ void softmax_tile(uint32_t s_tmem, uint32_t o_tmem, f
         }
     }
     const float shift = ref == -INFINITY ? 0.f : -ref;
-    float part[4] = {};
+    const uint64_t scale2 = pair_of(scale, scale), shift2 = pair_of(shift, shift);
+    uint64_t part[2] = {0, 0};
 #pragma unroll
-    for (int i = 0; i < kKeys; ++i) {
-        const float p = exp2_approx(fmaf(__uint_as_float(s[i]), scale, shift));
-        part[i & 3] += p;
-        s[i] = __float_as_uint(p);
+    for (int i = 0; i < kKeys; i += 2) {
+        uint64_t p = pair_fma(pair_of(s[i], s[i + 1]), scale2, shift2);
+        float x, y;
+        if (kTerms == 1 && (i / 2) % kPolyOf < kPoly) {
+            p = pair_exp2(p);
+            pair_split(p, x, y);
+        } else {
+            pair_split(p, x, y);
+            x = exp2_approx(x);
+            y = exp2_approx(y);
+            p = pair_of(x, y);
+        }
+        part[(i >> 1) & 1] = pair_add(part[(i >> 1) & 1], p);
+        s[i] = __float_as_uint(x);
+        s[i + 1] = __float_as_uint(y);
     }
-    sum += (part[0] + part[1]) + (part[2] + part[3]);
+    float even, odd;
+    pair_split(pair_add(part[0], part[1]), even, odd);
+    sum += even + odd;
 #pragma unroll
     for (int t = 0; t < kTerms; ++t) {
         uint32_t p[kKeys / 2];
