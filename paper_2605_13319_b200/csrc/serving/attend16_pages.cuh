@@ -19,7 +19,7 @@ constexpr int kPagesSms = 148, kPagesMinTiles = 1;
 template <int HD, typename T>
 struct PagesShape {
     static constexpr bool kWide = sizeof(T) == 4;
-    static constexpr int kTerms = kWide ? 3 : 1, kKeys = kWide ? 64 : 128, kRows = kWide ? 128 : 256;
+    static constexpr int kTerms = kWide ? 3 : 1, kHalves = kWide ? 1 : 2, kKeys = kWide ? 64 : 128, kRows = kWide ? 128 : 256;
     static constexpr int kQTile = 128 * HD * 2, kQ = (kWide ? 3 : 2) * kQTile, kTile = kKeys * HD * 2;
     static constexpr int kKSlots = kWide ? (HD == 128 ? 4 : 8) : (HD == 128 ? 2 : 4), kVSlots = kWide ? (HD == 128 ? 4 : 8) : (HD == 128 ? 3 : 6);
     static constexpr int kSlots = kKSlots + kVSlots;
@@ -43,7 +43,7 @@ struct PagesJob {
     int slot;
 };
 struct PagesControl {
-    unsigned long long job_full, job_read, q_full, q_empty, k_full[8], k_empty[8], v_full[8], v_empty[8], s_full[2], p_full[2], o_full[2], joint, done;
+    unsigned long long job_full, job_read, q_full, q_empty, k_full[8], k_empty[8], v_full[8], v_empty[8], s_full[2][2], p_full[2][2], o_done[2], o_full[2], joint, done;     // o_done: a step's products; o_full: a job's
     PagesJob jobs[2];
     int bad_lo[2], bad_hi[2];   // tiles in which a value was not finite
     uint32_t present[32];       // eight positions a bit
@@ -52,7 +52,7 @@ struct PagesControl {
     int dead;
 };
 template <int HD, typename T>
-constexpr int pages_smem() { return 128 + PagesShape<HD, T>::kQ + PagesShape<HD, T>::kSlots * PagesShape<HD, T>::kTile + (int)sizeof(PagesControl); }
+constexpr int pages_smem() { return PagesShape<HD, T>::kQ + PagesShape<HD, T>::kSlots * PagesShape<HD, T>::kTile + (int)sizeof(PagesControl); }
 
 // What a request adds to the sequence of tiles: tiles per triple and row groups.
 __device__ __forceinline__ void pages_load(const PagesArgs& a, int r, int& n, int& first, int& base, int& units, int& groups) {
@@ -148,29 +148,43 @@ __device__ __forceinline__ void pages_load8(const float* p, bool wide, uint4 (&x
         x[t] = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
-// 32 neighbouring outputs.
-__device__ __forceinline__ void pages_store32(uint16_t* p, bool wide, const float* y) {
+// 16 neighbouring outputs.
+__device__ __forceinline__ void pages_store16(uint16_t* p, bool wide, const float* y) {
     if (wide) {
 #pragma unroll
-        for (int x = 0; x < 32; x += 8)
-            *reinterpret_cast<uint4*>(p + x) =
-                make_uint4(pack_bf16(y[x], y[x + 1]), pack_bf16(y[x + 2], y[x + 3]), pack_bf16(y[x + 4], y[x + 5]), pack_bf16(y[x + 6], y[x + 7]));
+        for (int x = 0; x < 16; x += 8) *reinterpret_cast<uint4*>(p + x) = bf16x8(y + x);
     } else {
 #pragma unroll
-        for (int x = 0; x < 32; ++x) p[x] = f32_to_bf16_bits(y[x]);
+        for (int x = 0; x < 16; ++x) p[x] = f32_to_bf16_bits(y[x]);
     }
 }
-__device__ __forceinline__ void pages_store32(float* p, bool wide, const float* y) {
+__device__ __forceinline__ void pages_store16(float* p, bool wide, const float* y) {
     if (wide) {
 #pragma unroll
-        for (int x = 0; x < 32; x += 4) *reinterpret_cast<float4*>(p + x) = make_float4(y[x], y[x + 1], y[x + 2], y[x + 3]);
+        for (int x = 0; x < 16; x += 4) *reinterpret_cast<float4*>(p + x) = make_float4(y[x], y[x + 1], y[x + 2], y[x + 3]);
     } else {
 #pragma unroll
-        for (int x = 0; x < 32; ++x) p[x] = y[x];
+        for (int x = 0; x < 16; ++x) p[x] = y[x];
     }
 }
 __device__ __forceinline__ void pages_store(uint16_t* p, float y) { *p = f32_to_bf16_bits(y); }
 __device__ __forceinline__ void pages_store(float* p, float y) { *p = y; }
+
+// Which of the 16 columns from d on hold something that is not finite in the values of tiles lo .. hi that row i sees (0 in shared memory, where these
+// tiles were cleaned).
+template <int HD, int kKeys>
+__device__ __noinline__ uint32_t pages_bad(const PagesArgs& a, const PagesJob& job, int i, int lo, int hi, int d) {
+    uint32_t bad = 0;
+    for (int p0 = lo * kKeys; p0 < (hi + 1) * kKeys; p0 += 32) {
+        uint32_t bits = pages_see(a, job, i, p0);
+        while (bits) {
+            const int p = p0 + __ffs(bits) - 1, page = kv16_page(a.w, job.req, p);
+            bits &= bits - 1;
+            if (page >= 0) bad |= not_finite16(kv16_block(a.p, a.w, a.p.layer, page, 1, job.head) + kv16_piece(p % a.w.page_size, d / 8, HD), 64);
+        }
+    }
+    return bad;
+}
 
 // A warp's copies of one kind (kv 0: keys, 1: values) into a ring of its own, tile after tile over all jobs.  A lane per page that a tile touches; page
 // ids come by windows of 32, looked up a window ahead.
@@ -225,12 +239,13 @@ struct PagesFetch {
 };
 
 template <int HD, typename T>
-__global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const PagesArgs a) {
+__global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const __grid_constant__ PagesArgs a) {
     using Shape = PagesShape<HD, T>;
     constexpr int kKeys = Shape::kKeys, kTile = Shape::kTile, kKSlots = Shape::kKSlots, kVSlots = Shape::kVSlots, kTerms = Shape::kTerms, kPieces = HD / 8;
-    constexpr uint32_t kIdescS = umma_idesc_bf16(128, kKeys, 0, 0), kIdescO = umma_idesc_bf16(128, HD, 0, 1);
-    extern __shared__ unsigned char smem_raw[];
-    unsigned char* const smem = smem_raw + ((128u - (smem_u32(smem_raw) & 127u)) & 127u);
+    constexpr int kHalves = Shape::kHalves;        // steps of a tile, and places for a stream's scores
+    constexpr bool kOwn = Shape::kWide;            // the threads add up the tiles' sums
+    constexpr uint32_t kIdescS = umma_idesc_bf16(128, kStep, 0, 0), kIdescO = umma_idesc_bf16(128, HD, 0, 1);
+    extern __shared__ __align__(128) unsigned char smem[];
     unsigned char* const k_ring = smem + Shape::kQ;
     unsigned char* const v_ring = k_ring + kKSlots * kTile;
     PagesControl& c = *reinterpret_cast<PagesControl*>(v_ring + kVSlots * kTile);
@@ -255,8 +270,11 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
             mbar_init(smem_u32(&c.v_empty[i]), 1);
         }
         for (int s = 0; s < 2; ++s) {
-            mbar_init(smem_u32(&c.s_full[s]), 1);
-            mbar_init(smem_u32(&c.p_full[s]), 4);
+            for (int h = 0; h < 2; ++h) {
+                mbar_init(smem_u32(&c.s_full[s][h]), 1);
+                mbar_init(smem_u32(&c.p_full[s][h]), 4);
+            }
+            mbar_init(smem_u32(&c.o_done[s]), 1);
             mbar_init(smem_u32(&c.o_full[s]), 1);
         }
         c.dead = 0;
@@ -335,8 +353,9 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                 bool ok = true;
                 const uint64_t q_desc = umma_desc(smem_u32(smem), 128, HD * 16), k_desc = umma_desc(smem_u32(k_ring), 128, HD * 16),
                                v_desc = umma_desc(smem_u32(v_ring), HD * 16, 128);
-                uint32_t p_phase[2] = {0, 0};
-                // The next keys have come / the scores of stream s against them / their slot is free when what was issued so far is done; and so for values.
+                uint32_t p_phase = 0;              // bit 2 s + h
+                // The next keys have come / the scores of stream s against half of them / their slot is free when what was issued so far is done; and so
+                // for values.
                 auto k_there = [&] {
                     ok = ok && role_wait(smem_u32(&c.k_full[kp.slot]), kp.phase, dead);
                     if (ok) tc_fence_after();
@@ -346,30 +365,31 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                     ok = ok && role_wait(smem_u32(&c.v_full[vp.slot]), vp.phase, dead);
                     return ok;
                 };
-                auto scores = [&](int s, int q_tile) {
-                    const uint64_t q = q_desc + (uint32_t)(q_tile * (Shape::kQTile >> 4)), k = k_desc + kp.slot * (uint32_t)(kTile >> 4);
+                auto scores = [&](int s, int q_tile, int h) {
+                    const uint64_t q = q_desc + (uint32_t)(q_tile * (Shape::kQTile >> 4)), k = k_desc + (kp.slot * (kTile >> 4) + h * kStep * HD * 2 / 16);
 #pragma unroll
                     for (int t = 0; t < kTerms; ++t)
 #pragma unroll
                         for (int x = 0; x < HD / 16; ++x)
-                            umma_bf16(tmem + 128 * s, q + ((kTerms - 1 - t) * (Shape::kQTile >> 4) + x * 16), k + x * 16, kIdescS, t + x > 0);
-                    umma_commit(smem_u32(&c.s_full[s]));
+                            umma_bf16(tmem + 128 * s + kStep * h, q + ((kTerms - 1 - t) * (Shape::kQTile >> 4) + x * 16), k + x * 16, kIdescS, t + x > 0);
+                    umma_commit(smem_u32(&c.s_full[s][h]));
                 };
                 auto k_done = [&] {
                     umma_commit(smem_u32(&c.k_empty[kp.slot]));
                     kp.next();
                 };
-                auto sums = [&](int s, bool first, bool last) {
-                    ok = ok && role_wait(smem_u32(&c.p_full[s]), p_phase[s], dead);
-                    p_phase[s] ^= 1;
+                auto sums = [&](int s, int h, bool first, bool last) {
+                    ok = ok && role_wait(smem_u32(&c.p_full[s][h]), p_phase >> (2 * s + h) & 1u, dead);
+                    p_phase ^= 1u << (2 * s + h);
                     if (!ok) return false;
                     tc_fence_after();
-                    const uint64_t v = v_desc + vp.slot * (uint32_t)(kTile >> 4);
+                    const uint64_t v = v_desc + (vp.slot * (kTile >> 4) + h * kStep * HD * 2 / 16);
 #pragma unroll
                     for (int t = 0; t < kTerms; ++t)
 #pragma unroll
-                        for (int x = 0; x < kKeys / 16; ++x)
-                            umma_bf16_ta(tmem + 256 + HD * s, tmem + 128 * s + (kTerms - 1 - t) * (kKeys / 2) + 8 * x, v + x * HD * 2, kIdescO, !first || t + x > 0);
+                        for (int x = 0; x < kStep / 16; ++x)
+                            umma_bf16_ta(tmem + 256 + HD * s, tmem + 128 * s + kStep * h + (kTerms - 1 - t) * (kStep / 2) + 8 * x, v + x * HD * 2, kIdescO, (!kOwn && !first) || t + x > 0);
+                    umma_commit(smem_u32(&c.o_done[s]));
                     if (last) umma_commit(smem_u32(&c.o_full[s]));
                     return true;
                 };
@@ -386,44 +406,44 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                     if (n == 0) break;
                     ok = role_wait(smem_u32(&c.q_full), i & 1, dead);
                     if (!k_there()) break;
-                    if (both) {
-                        scores(0, 0);
-                        scores(1, 1);
+                    if (both) {                    // stream s: rows of q tile s, every tile of keys
+                        for (int h = 0; h < kHalves; ++h)
+                            for (int s = 0; s < 2; ++s) scores(s, s, h);
                         k_done();
                         if (n == 1) umma_commit(smem_u32(&c.q_empty));
-                        for (int j = 0; j < n; ++j) {
+                        for (int j = 0; j < n && ok; ++j) {
                             const bool more = j + 1 < n;
-                            if (!v_there() || !sums(0, j == 0, !more)) break;
-                            if (more) {
-                                if (!k_there()) break;
-                                scores(0, 0);
-                            }
-                            if (!sums(1, j == 0, !more)) break;
+                            if (!v_there() || (more && !k_there())) break;
+                            for (int h = 0; h < kHalves && ok; ++h)
+                                for (int s = 0; s < 2; ++s) {
+                                    if (!sums(s, h, j + h == 0, !more && h == kHalves - 1)) break;
+                                    if (more) scores(s, s, h);
+                                }
+                            if (!ok) break;
                             v_done();
-                            if (more) {
-                                scores(1, 1);
-                                k_done();
-                                if (j + 2 == n) umma_commit(smem_u32(&c.q_empty));
-                            }
+                            if (more) k_done();
+                            if (j + 2 == n) umma_commit(smem_u32(&c.q_empty));
                         }
-                    } else {
-                        scores(0, 0);
+                    } else {                       // the same rows, tiles in turn
+                        for (int h = 0; h < kHalves; ++h) scores(0, 0, h);
                         k_done();
                         if (n > 1) {
                             if (!k_there()) break;
-                            scores(1, 0);
+                            for (int h = 0; h < kHalves; ++h) scores(1, 0, h);
                             k_done();
                         }
                         if (n <= 2) umma_commit(smem_u32(&c.q_empty));
-                        for (int j = 0; j < n; ++j) {
-                            if (!v_there() || !sums(j & 1, j < 2, j + 2 >= n)) break;
-                            v_done();
-                            if (j + 2 < n) {
-                                if (!k_there()) break;
-                                scores(j & 1, 0);
-                                k_done();
-                                if (j + 3 == n) umma_commit(smem_u32(&c.q_empty));
+                        for (int j = 0; j < n && ok; ++j) {
+                            const bool more = j + 2 < n;
+                            if (!v_there() || (more && !k_there())) break;
+                            for (int h = 0; h < kHalves; ++h) {
+                                if (!sums(j & 1, h, j < 2 && h == 0, !more && h == kHalves - 1)) break;
+                                if (more) scores(j & 1, 0, h);
                             }
+                            if (!ok) break;
+                            v_done();
+                            if (more) k_done();
+                            if (j + 3 == n) umma_commit(smem_u32(&c.q_empty));
                         }
                     }
                 }
@@ -438,7 +458,8 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
         registers_more();
         const int s = warp >> 2, row = tid & 127;
         const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16, s_tmem = tmem + 128 * s + lanes, o_tmem = tmem + 256 + HD * s + lanes;
-        uint32_t tile_no = 0, s_phase = 0, o_phase[2] = {0, 0}, joint_phase = 0;
+        // phases: s_phase bit h, o_phase of the last step's products; tile_no: tiles fetched by this CTA before the job's
+        uint32_t tile_no = 0, s_phase = 0, o_phase = 0, full_phase = 0, joint_phase = 0;
         auto joint = [&] {                         // both streams' warps
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&c.joint));
@@ -446,9 +467,10 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
             joint_phase ^= 1;
             return there;
         };
+        auto products_done = [&] { return warp_wait(smem_u32(&c.o_done[s]), o_phase ^ 1u, dead); };
         for (int i = 0;; ++i) {
             if (!warp_wait(smem_u32(&c.job_full), i & 1, dead)) break;
-            const PagesJob job = c.jobs[i & 1];
+            const PagesJob& job = c.jobs[i & 1];           // (as it is until the next but one is said, when both streams have read the next)
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&c.job_read));
             if (job.tiles == 0) break;
@@ -463,9 +485,9 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                     uint4 v[kBatch][kTerms];
 #pragma unroll
                     for (int y = 0; y < kBatch; ++y) {
-                        const int x = x0 + 8 * y, r = x / (kPieces / 4) * 8 + (lane & 7), at = job.rho0 + r, piece = x % (kPieces / 4) * 4 + (lane >> 3);
+                        const int x = x0 + 8 * y, r = x / (kPieces / 4) * 8 + (lane & 7), rho = job.rho0 + r, piece = x % (kPieces / 4) * 4 + (lane >> 3);
                         if (r < job.n_rows)
-                            pages_load8(static_cast<const T*>(a.q) + (job.first + at / G) * a.q_stride + (size_t)(job.head * G + at % G) * HD + piece * 8, a.q_wide, v[y]);
+                            pages_load8(static_cast<const T*>(a.q) + (job.first + rho / G) * a.q_stride + (size_t)(job.head * G + rho % G) * HD + piece * 8, a.q_wide, v[y]);
                     }
 #pragma unroll
                     for (int y = 0; y < kBatch; ++y) {
@@ -483,74 +505,89 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
             const int local = both ? 128 * s + row : row;                      // of the group's rows
             const bool mine = local < job.n_rows, any = (both ? 128 * s : 0) + 32 * (warp & 3) < job.n_rows;
             const int rho = job.rho0 + (mine ? local : 0), node = rho / G;
-            // tiles that every row of the stream sees whole
-            const int clear = (a.mask ? job.base : job.base + (job.rho0 + (both ? 128 * s : 0)) / G + 1) / kKeys;
-            float ref = -INFINITY, sum = 0.f;
+            // positions that every row of the stream sees
+            const int clear = a.mask ? job.base : job.base + (job.rho0 + (both ? 128 * s : 0)) / G + 1;
+            float ref = -INFINITY, sum = 0.f, own[kOwn ? HD : 1] = {};
             for (int j = both ? 0 : s; j < n && ok; j += both ? 1 : 2) {
                 const int u = job.u0 + j;
-                uint32_t see[kKeys / 32];
-                bool masked = u >= clear;
-                if (masked) {
+#pragma unroll 1
+                for (int h = 0; h < kHalves && ok; ++h) {
+                    const int p0 = u * kKeys + h * kStep;
+                    uint32_t see[2];
+                    bool masked = p0 + kStep > clear;
+                    if (masked) {
 #pragma unroll
-                    for (int w = 0; w < kKeys / 32; ++w) see[w] = pages_see(a, job, node, u * kKeys + 32 * w);
-                }
-                ok = warp_wait(smem_u32(&c.s_full[s]), s_phase, dead);
-                s_phase ^= 1;
-                if (!ok) break;
-                tc_fence_after();
-                const uint32_t present = c.present[(tile_no + j) & 31];
-                if (present != (kKeys == 128 ? 0xffffu : 0xffu)) {
-#pragma unroll
-                    for (int w = 0; w < kKeys / 32; ++w) {
-                        const uint32_t x = present >> (4 * w);
-                        const uint32_t there = (x & 1u ? 0xffu : 0u) | (x & 2u ? 0xff00u : 0u) | (x & 4u ? 0xff0000u : 0u) | (x & 8u ? 0xff000000u : 0u);
-                        see[w] = (masked ? see[w] : 0xffffffffu) & there;
+                        for (int w = 0; w < 2; ++w) see[w] = pages_see(a, job, node, p0 + 32 * w);
                     }
-                    masked = true;
-                }
-                if (any) softmax_tile<HD, kKeys, kTerms>(s_tmem, o_tmem, a.scale, both ? j == 0 : j < 2, masked, see, ref, sum);
-                if (masked) {
-                    const uint32_t at = tile_no + j;                           // of the values fetched by this CTA
-                    ok = warp_wait(smem_u32(&c.v_full[at % kVSlots]), at / kVSlots & 1, dead);
+                    ok = warp_wait(smem_u32(&c.s_full[s][h]), s_phase >> h & 1u, dead);
+                    s_phase ^= 1u << h;
                     if (!ok) break;
-                    const int keys = job.base + job.n - u * kKeys;
-                    if (clean_values(v_ring + at % kVSlots * kTile, kTile / 16, row, 128, [&](int p) {
-                            const int key = p / kPieces / 8 * 8 + p % 8;
-                            return key < keys && (present >> (key >> 3) & 1u);
-                        })) {
-                        atomicMin(&c.bad_lo[i & 1], u);
-                        atomicMax(&c.bad_hi[i & 1], u);
-                        __threadfence_block();
+                    tc_fence_after();
+                    const uint32_t there = c.present[(tile_no + j) & 31] >> (8 * h) & 0xffu;       // eight positions a bit
+                    if (there != 0xffu) {
+#pragma unroll
+                        for (int w = 0; w < 2; ++w) {
+                            const uint32_t x = there >> (4 * w);
+                            const uint32_t bits = (x & 1u ? 0xffu : 0u) | (x & 2u ? 0xff00u : 0u) | (x & 4u ? 0xff0000u : 0u) | (x & 8u ? 0xff000000u : 0u);
+                            see[w] = (masked ? see[w] : 0xffffffffu) & bits;
+                        }
+                        masked = true;
                     }
-                    fence_proxy_async_smem();
+                    const bool first = (both ? j : j >> 1) + h == 0;
+                    if (any) ok = softmax_step<HD, kTerms, kOwn>(s_tmem + kStep * h, o_tmem, a.scale, first, masked, see, ref, sum, own, products_done);
+                    if (!ok) break;
+                    o_phase ^= 1;
+                    if (masked) {
+                        const uint32_t v = tile_no + j;
+                        ok = warp_wait(smem_u32(&c.v_full[v % kVSlots]), v / kVSlots & 1, dead);
+                        if (!ok) break;
+                        const int keys = job.base + job.n - p0;
+                        if (clean_values(v_ring + v % kVSlots * kTile + h * kStep * HD * 2, kStep * kPieces, row, 128, [&](int p) {
+                                const int key = p / kPieces / 8 * 8 + p % 8;
+                                return key < keys && (there >> (key >> 3) & 1u);
+                            })) {
+                            atomicMin(&c.bad_lo[i & 1], u);
+                            atomicMax(&c.bad_hi[i & 1], u);
+                            __threadfence_block();
+                        }
+                        fence_proxy_async_smem();
+                    }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&c.p_full[s][h]));
                 }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&c.p_full[s]));
             }
-            if (sum != sum) ref = INFINITY;        // (not what a row that sees nothing has: every factor of it is then a NaN)
             // ---- the range's sums
-            const bool has[2] = {true, both || n > 1};
-            if (ok && (both ? s == 0 : true)) ok = warp_wait(smem_u32(&c.o_full[0]), o_phase[0], dead);
-            if (ok && has[1] && (both ? s == 1 : true)) ok = warp_wait(smem_u32(&c.o_full[1]), o_phase[1], dead);
-            o_phase[0] ^= 1;
-            if (has[1]) o_phase[1] ^= 1;
+            const bool mine_has = both || s < n;
+            if (ok && mine_has) ok = warp_wait(smem_u32(&c.o_full[s]), full_phase, dead);      // (not o_done, which may still be two steps behind)
+            if (mine_has) full_phase ^= 1;
             tile_no += n;
-            T* const out = static_cast<T*>(a.out) + (job.first + node) * a.out_stride + (size_t)(job.head * G + rho % G) * HD;
-            const bool whole = job.u0 == 0 && job.u1 == job.units;
-            float* const part = a.parts + (size_t)job.slot * a.cap * (HD + 2);
+            tc_fence_after();
+            if constexpr (kOwn)
+                if (ok && any && mine_has) {       // (the other stream reads them too)
+                    own_sums<HD>(o_tmem, own);
+#pragma unroll
+                    for (int d = 0; d < HD; d += 16) tmem_st16(o_tmem + d, *reinterpret_cast<const float(*)[16]>(own + d));
+                    tmem_st_wait();
+                    tc_fence_before();
+                }
+            if (sum != sum) ref = INFINITY;        // (not what a row that sees nothing has: every factor of it is then a NaN)
             if (ok && !both) {
                 c.ref[s][row] = ref;
                 c.sum[s][row] = sum;
+                tc_fence_before();
                 ok = joint();
+                tc_fence_after();
             }
+            T* const out = static_cast<T*>(a.out) + (job.first + node) * a.out_stride + (size_t)(job.head * G + rho % G) * HD;
+            const bool whole = job.u0 == 0 && job.u1 == job.units;
+            float* const part = a.parts + (size_t)job.slot * a.cap * (HD + 2);
             if (!ok) {                             // a copy or a product that never came: no result
                 if (mine && whole)
                     for (int d = 0; d < HD; ++d) pages_store(out + d, NAN);
                 if (mine && !whole) part[a.cap * HD + local] = NAN;
                 break;
             }
-            tc_fence_after();
             float f0 = 1.f, f1 = 1.f;              // what stream 0's and stream 1's sums are multiplied with
             bool none0 = ref == -INFINITY, none1 = true;                       // a stream that has seen nothing has none
             if (!both) {
@@ -565,45 +602,35 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
             const int lo = *(volatile int*)&c.bad_lo[i & 1], hi = *(volatile int*)&c.bad_hi[i & 1];
             const float inv = !whole ? 1.f : (sum > 0.f ? 1.f / sum : sum);
             const int d0 = both ? 0 : s * (HD / 2), d1 = both ? HD : d0 + HD / 2;
+            const uint32_t o0 = tmem + 256 + HD * (both ? s : 0) + lanes;
 #pragma unroll 1
-            for (int d = d0; d < d1; d += 32) {
-                if (any) {
-                    float y[32];
-                    uint32_t o[32];
-                    tmem_ld32(tmem + 256 + HD * (both ? s : 0) + lanes + d, o);
-                    tmem_ld_wait32(o);
+            for (int d = d0; d < d1 && any; d += 16) {
+                float y[16], o[16];
+                tmem_ld16(o0 + d, y);
+                tmem_ld_wait16(y);
 #pragma unroll
-                    for (int x = 0; x < 32; ++x) y[x] = none0 ? 0.f : __uint_as_float(o[x]) * f0;
-                    if (!both && n > 1) {
-                        tmem_ld32(tmem + 256 + HD + lanes + d, o);
-                        tmem_ld_wait32(o);
+                for (int x = 0; x < 16; ++x) y[x] = none0 ? 0.f : y[x] * f0;
+                if (!both && n > 1) {
+                    tmem_ld16(o0 + HD + d, o);
+                    tmem_ld_wait16(o);
 #pragma unroll
-                        for (int x = 0; x < 32; ++x) y[x] = none1 ? y[x] : fmaf(__uint_as_float(o[x]), f1, y[x]);
+                    for (int x = 0; x < 16; ++x) y[x] = none1 ? y[x] : fmaf(o[x], f1, y[x]);
+                }
+                if (mine) {
+                    if (lo <= hi) {
+                        const uint32_t bad = pages_bad<HD, kKeys>(a, job, node, lo, hi, d);
+#pragma unroll
+                        for (int x = 0; x < 16; ++x)
+                            if (bad >> x & 1u) y[x] = NAN;
                     }
-                    if (mine) {
-                        if (lo <= hi) {            // columns of what the row sees whose values are not finite
-                            uint32_t bad = 0;
-                            for (int p0 = lo * kKeys; p0 < (hi + 1) * kKeys; p0 += 32) {
-                                uint32_t bits = pages_see(a, job, node, p0);
-                                while (bits) {
-                                    const int p = p0 + __ffs(bits) - 1, page = kv16_page(a.w, job.req, p);
-                                    bits &= bits - 1;
-                                    if (page >= 0) bad |= not_finite32(kv16_block(a.p, a.w, a.p.layer, page, 1, job.head) + kv16_piece(p % a.w.page_size, d / 8, HD), 64);
-                                }
-                            }
+                    if (whole) {
 #pragma unroll
-                            for (int x = 0; x < 32; ++x)
-                                if (bad >> x & 1u) y[x] = NAN;
-                        }
-                        if (whole) {
+                        for (int x = 0; x < 16; ++x) y[x] *= inv;
+                        pages_store16(out + d, a.out_wide, y);
+                    } else {
 #pragma unroll
-                            for (int x = 0; x < 32; ++x) y[x] *= inv;
-                            pages_store32(out + d, a.out_wide, y);
-                        } else {
-#pragma unroll
-                            for (int x = 0; x < 32; x += 4)
-                                *reinterpret_cast<float4*>(part + ((size_t)(d + x) * a.cap + 4 * local)) = make_float4(y[x], y[x + 1], y[x + 2], y[x + 3]);
-                        }
+                        for (int x = 0; x < 16; x += 4)
+                            *reinterpret_cast<float4*>(part + ((size_t)(d + x) * a.cap + 4 * local)) = make_float4(y[x], y[x + 1], y[x + 2], y[x + 3]);
                     }
                 }
                 __syncwarp();

@@ -2,10 +2,10 @@
 //
 // Rows of a tile are (token, query head of the KV head's group) pairs, so that every tile reads one KV head's keys once for all of the group: T = 128 / G
 // tokens by G heads, rounded down (G = 3: 126 rows of 128).  A job is two such tiles, 2 T consecutive tokens of a prompt by one KV head, each with a
-// stream of its own (attend16_tile.cuh); both read the same keys and values, 128 at a time, from the first up to their last token.
+// stream of its own (attend16_tile.cuh); both go through the same keys, from the first up to their last token, in steps of 64.
 // A CTA per SM takes jobs in turn: sorted by length (block of tokens, last first; then prompts, then heads), dealt out back and forth, so that the CTAs'
 // sums differ by less than a job.  Nothing is shared between CTAs: no atomics, no scratch.
-// Warps: 0-3 and 4-7 the streams' rows, 8 fetches (copy engine, 128-byte swizzle), 9 issues the products.
+// Warps: 0-3 and 4-7 the streams' rows, 8 fetches (copy engine, 128-byte swizzle; 128 keys at a time), 9 issues the products.
 #pragma once
 #include "attend16_tile.cuh"
 
@@ -26,7 +26,7 @@ struct PromptJob {
 constexpr int kPromptJobs = 2;
 
 struct PromptControl {
-    unsigned long long q_full, q_empty, full[16], empty[16], s_full[2], p_full[2], o_full[2], done;
+    unsigned long long q_full, q_empty, full[16], empty[16], s_full[2][2], p_full[2][2], o_done[2], o_full[2], done;      // o_done: a step's products; o_full: a job's
     PromptJob jobs[kPromptJobs];
     int flags[kPromptJobs];     // a value of the job's last tiles was not finite
     uint32_t tmem;
@@ -35,7 +35,7 @@ struct PromptControl {
 template <int HD>
 struct PromptShape {
     static constexpr int kTile = 128 * HD * 2, kStages = HD == 128 ? 5 : 8;
-    static constexpr int kSmem = 1024 + (2 + kStages) * kTile + (int)sizeof(PromptControl);
+    static constexpr int kSmem = (2 + kStages) * kTile + (int)sizeof(PromptControl);
 };
 
 __device__ __forceinline__ void tensor3_g2s(uint32_t dst_smem, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
@@ -90,20 +90,27 @@ __device__ __forceinline__ PromptJob prompt_job(const PromptArgs& a, long long r
     }
     return job;
 }
-// Tiles of 128 keys that stream s of a job goes through.
-__device__ __forceinline__ int prompt_tiles(const PromptJob& job, int s, int T) {
+// Steps that stream s of a job goes through.
+__device__ __forceinline__ int prompt_steps(const PromptJob& job, int s, int T) {
     const int t = job.t0 + s * T;
-    return t >= job.n ? 0 : (min(t + T, job.n) + 127) >> 7;
+    return t >= job.n ? 0 : (min(t + T, job.n) + kStep - 1) / kStep;
+}
+
+// Which of 16 columns hold something that is not finite in n rows of v (0 in shared memory, where the job's last tiles had it).
+template <int HD>
+__device__ __noinline__ uint32_t prompt_bad(const uint16_t* v, long long stride, int n) {
+    uint32_t bad = 0;
+    for (int i = 0; i < n; ++i) bad |= not_finite16(v + i * stride, 8);
+    return bad;
 }
 
 template <int HD>
 __global__ void __launch_bounds__(kAttendThreads16, 1)
-    prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const PromptArgs a) {
+    prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ PromptArgs a) {
     using Shape = PromptShape<HD>;
     constexpr int kTile = Shape::kTile, kStages = Shape::kStages, kAtom = 128 * 128;      // an atom: 128 rows of 64 columns
-    constexpr uint32_t kIdescS = umma_idesc_bf16(128, 128, 0, 0), kIdescO = umma_idesc_bf16(128, HD, 0, 1);
-    extern __shared__ unsigned char smem_raw[];
-    unsigned char* const smem = smem_raw + ((1024u - (smem_u32(smem_raw) & 1023u)) & 1023u);
+    constexpr uint32_t kIdescS = umma_idesc_bf16(128, kStep, 0, 0), kIdescO = umma_idesc_bf16(128, HD, 0, 1);
+    extern __shared__ __align__(1024) unsigned char smem[];
     unsigned char* const ring = smem + 2 * kTile;
     PromptControl& c = *reinterpret_cast<PromptControl*>(ring + kStages * kTile);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -119,8 +126,11 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
             mbar_init(smem_u32(&c.empty[i]), 1);
         }
         for (int s = 0; s < 2; ++s) {
-            mbar_init(smem_u32(&c.s_full[s]), 1);
-            mbar_init(smem_u32(&c.p_full[s]), 4);
+            for (int h = 0; h < 2; ++h) {
+                mbar_init(smem_u32(&c.s_full[s][h]), 1);
+                mbar_init(smem_u32(&c.p_full[s][h]), 4);
+            }
+            mbar_init(smem_u32(&c.o_done[s]), 1);
             mbar_init(smem_u32(&c.o_full[s]), 1);
         }
         c.dead = 0;
@@ -153,13 +163,13 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
                     if (job.n == 0) {
                         mbar_arrive(smem_u32(&c.q_full));
                     } else {
-                        const int tiles[2] = {prompt_tiles(job, 0, T), prompt_tiles(job, 1, T)};
+                        const int steps[2] = {prompt_steps(job, 0, T), prompt_steps(job, 1, T)};
                         const uint32_t bar = smem_u32(&c.q_full);
-                        mbar_expect_tx(bar, (uint32_t)((tiles[1] ? 2 : 1) * (HD / 64) * T * G * 128));
+                        mbar_expect_tx(bar, (uint32_t)((steps[1] ? 2 : 1) * (HD / 64) * T * G * 128));
                         for (int s = 0; s < 2; ++s)
-                            for (int x = 0; tiles[s] && x < HD / 64; ++x)
+                            for (int x = 0; steps[s] && x < HD / 64; ++x)
                                 tensor3_g2s(smem_u32(smem + s * kTile + x * kAtom), &map_q, 64 * x, job.head * G, job.first + job.t0 + s * T, bar);
-                        const int n = max(tiles[0], tiles[1]);
+                        const int n = (max(steps[0], steps[1]) + 1) >> 1;                // tiles of 128 keys
                         for (int e = 0; e < 2 * n && ok; ++e, ++entry) {
                             const int st = entry % kStages;
                             if (entry >= kStages) ok = role_wait(smem_u32(&c.empty[st]), (entry / kStages - 1) & 1, dead);
@@ -180,57 +190,74 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
             }
         } else if (warp == 9) {                        // ---- products
             if (elect_one()) {
-                uint32_t entry = 0;
+                RingPlace<kStages> place;          // the next of the ring that has not come yet
+                uint32_t k_slot = 0, v_slot = 0;
                 bool ok = true;
-                auto scores = [&](int s, uint32_t e) {
-                    const uint32_t q = smem_u32(smem + s * kTile), k = smem_u32(ring + e % kStages * kTile);
+                const uint64_t q_desc = umma_desc_swizzled(smem_u32(smem), 16, 1024), k_desc = umma_desc_swizzled(smem_u32(ring), 16, 1024),
+                               v_desc = umma_desc_swizzled(smem_u32(ring), kAtom, 1024);
+                uint32_t p_phase = 0;              // bit 2 s + h
+                auto arrived = [&](uint32_t& slot) {
+                    ok = ok && role_wait(smem_u32(&c.full[place.slot]), place.phase, dead);
+                    slot = place.slot;
+                    place.next();
+                    return ok;
+                };
+                auto release = [&](uint32_t slot) { umma_commit(smem_u32(&c.empty[slot])); };
+                auto scores = [&](int s, int h) {
+                    const uint64_t q = q_desc + (uint32_t)(s * (kTile >> 4)), k = k_desc + (k_slot * (kTile >> 4) + h * (kStep * 128 >> 4));
 #pragma unroll
                     for (int x = 0; x < HD / 16; ++x) {
-                        const uint32_t at = (x >> 2) * kAtom + (x & 3) * 32;
-                        umma_bf16(tmem + 128 * s, umma_desc_swizzled(q + at, 16, 1024), umma_desc_swizzled(k + at, 16, 1024), kIdescS, x > 0);
+                        const uint32_t at = ((x >> 2) * kAtom + (x & 3) * 32) >> 4;
+                        umma_bf16(tmem + 128 * s + kStep * h, q + at, k + at, kIdescS, x > 0);
                     }
-                    umma_commit(smem_u32(&c.s_full[s]));
+                    umma_commit(smem_u32(&c.s_full[s][h]));
                 };
-                uint32_t p_phase[2] = {0, 0};
-                auto sums = [&](int s, uint32_t e, bool first, bool last) {
-                    ok = ok && role_wait(smem_u32(&c.p_full[s]), p_phase[s], dead);
-                    p_phase[s] ^= 1;
-                    if (!ok) return;
+                auto sums = [&](int s, int h, bool first, bool last) {
+                    ok = ok && role_wait(smem_u32(&c.p_full[s][h]), p_phase >> (2 * s + h) & 1u, dead);
+                    p_phase ^= 1u << (2 * s + h);
+                    if (!ok) return false;
                     tc_fence_after();
-                    const uint32_t v = smem_u32(ring + e % kStages * kTile);
+                    const uint64_t v = v_desc + (v_slot * (kTile >> 4) + h * (kStep * 128 >> 4));
 #pragma unroll
-                    for (int x = 0; x < 8; ++x)
-                        umma_bf16_ta(tmem + 256 + HD * s, tmem + 128 * s + 8 * x, umma_desc_swizzled(v + x * 2048, kAtom, 1024), kIdescO, !first || x > 0);
+                    for (int x = 0; x < kStep / 16; ++x)
+                        umma_bf16_ta(tmem + 256 + HD * s, tmem + 128 * s + kStep * h + 8 * x, v + x * (2048 >> 4), kIdescO, !first || x > 0);
+                    umma_commit(smem_u32(&c.o_done[s]));
                     if (last) umma_commit(smem_u32(&c.o_full[s]));
+                    return true;
                 };
-                auto arrived = [&](uint32_t e) { ok = ok && role_wait(smem_u32(&c.full[e % kStages]), (e / kStages) & 1, dead); };
                 for (int i = 0; ok; ++i) {
                     ok = role_wait(smem_u32(&c.q_full), i & 1, dead);
                     if (!ok) break;
                     const PromptJob job = c.jobs[i % kPromptJobs];
                     if (job.n == 0) break;
-                    const int n0 = prompt_tiles(job, 0, T), n1 = prompt_tiles(job, 1, T), n = max(n0, n1);
-                    arrived(entry);
-                    if (!ok) break;
+                    const int n0 = prompt_steps(job, 0, T), n1 = prompt_steps(job, 1, T), n = max(n0, n1);
+                    // The scores of step j (both streams' where they go so far); the last of a tile of keys lets go of it, the last of all of q too.
+                    auto all_scores = [&](int j, int s) {
+                        if (j < (s ? n1 : n0)) scores(s, j & 1);
+                        if (s == 0) return;
+                        if ((j & 1) || j + 1 == n) release(k_slot);
+                        if (j + 1 == n) umma_commit(smem_u32(&c.q_empty));
+                    };
+                    if (!arrived(k_slot)) break;
                     tc_fence_after();
-                    scores(0, entry);
-                    if (n1) scores(1, entry);
-                    umma_commit(smem_u32(&c.empty[entry % kStages]));
-                    if (n == 1) umma_commit(smem_u32(&c.q_empty));
-                    for (int j = 0; j < n && ok; ++j) {
-                        const uint32_t ev = entry + 2 * j + 1, ek = ev + 1;
-                        arrived(ev);
-                        if (ok && j < n0) sums(0, ev, j == 0, j == n0 - 1);
-                        if (j + 1 < n) arrived(ek);
-                        if (ok && j + 1 < n0) scores(0, ek);
-                        if (ok && j < n1) sums(1, ev, j == 0, j == n1 - 1);
-                        if (!ok) break;
-                        umma_commit(smem_u32(&c.empty[ev % kStages]));
-                        if (j + 1 < n1) scores(1, ek);
-                        if (j + 1 < n) umma_commit(smem_u32(&c.empty[ek % kStages]));
-                        if (j + 2 == n) umma_commit(smem_u32(&c.q_empty));
+                    all_scores(0, 0);
+                    all_scores(0, 1);
+                    if (n > 1) {
+                        all_scores(1, 0);
+                        all_scores(1, 1);
                     }
-                    entry += 2 * n;
+                    for (int j = 0; j < n; ++j) {
+                        const bool more = j + 2 < n;
+                        if (!(j & 1)) {
+                            if (!arrived(v_slot)) break;
+                            if (more && !arrived(k_slot)) break;
+                        }
+                        if (j < n0 && !sums(0, j & 1, j == 0, j + 1 == n0)) break;
+                        if (more) all_scores(j + 2, 0);
+                        if (j < n1 && !sums(1, j & 1, j == 0, j + 1 == n1)) break;
+                        if (more) all_scores(j + 2, 1);
+                        if ((j & 1) || j + 1 == n) release(v_slot);
+                    }
                 }
                 if (!ok) {                             // products in flight end before their memory is given back
                     umma_commit(smem_u32(&c.done));
@@ -243,38 +270,47 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
         registers_more();
         const int s = warp >> 2, row = tid & 127, token = row / G, g = row % G;
         const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16, s_tmem = tmem + 128 * s + lanes, o_tmem = tmem + 256 + HD * s + lanes;
-        uint32_t entry = 0, s_phase = 0, o_phase = 0;
+        uint32_t entry = 0, s_phase = 0, o_phase = 0, full_phase = 0;          // s_phase: bit h; o_phase: of the last step's products
         for (int i = 0;; ++i) {
             if (!warp_wait(smem_u32(&c.q_full), i & 1, dead)) break;
             const PromptJob job = c.jobs[i % kPromptJobs];
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&c.q_empty));
             if (job.n == 0) break;
-            const int tiles = prompt_tiles(job, s, T), all = max(prompt_tiles(job, 0, T), prompt_tiles(job, 1, T));
+            const int steps = prompt_steps(job, s, T), all = (max(prompt_steps(job, 0, T), prompt_steps(job, 1, T)) + 1) >> 1;
             const int t = job.t0 + s * T + token;  // this row's token
-            const int clear = (job.t0 + s * T + 1) >> 7;                       // tiles that every row sees whole
-            float ref = -INFINITY, sum = 0.f;
+            const int clear = (job.t0 + s * T + 1) / kStep;                    // steps that every row sees whole
+            float ref = -INFINITY, sum = 0.f, none[1];
             bool ok = true;
-            for (int j = 0; j < tiles; ++j) {
-                uint32_t see[4];
+            auto products_done = [&] { return warp_wait(smem_u32(&c.o_done[s]), o_phase ^ 1, dead); };
+            for (int j = 0; j < steps; ++j) {
+                const int h = j & 1;
+                uint32_t see[2];
                 const bool masked = j >= clear;
                 if (masked) {
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) {
-                        const int n = t + 1 - (j * 128 + 32 * w);
+                    for (int w = 0; w < 2; ++w) {
+                        const int n = t + 1 - (j * kStep + 32 * w);
                         see[w] = n >= 32 ? 0xffffffffu : (n <= 0 ? 0u : (1u << n) - 1u);
                     }
                 }
-                ok = warp_wait(smem_u32(&c.s_full[s]), s_phase, dead);
-                s_phase ^= 1;
+                ok = warp_wait(smem_u32(&c.s_full[s][h]), s_phase >> h & 1u, dead);
+                s_phase ^= 1u << h;
                 if (!ok) break;
                 tc_fence_after();
-                softmax_tile<HD, 128, 1>(s_tmem, o_tmem, a.scale, j == 0, masked, see, ref, sum);
+                ok = softmax_step<HD, 1, false>(s_tmem + kStep * h, o_tmem, a.scale, j == 0, masked, see, ref, sum, none, products_done);
+                if (!ok) break;
+                o_phase ^= 1;
                 if (masked) {
-                    const uint32_t ev = entry + 2 * j + 1;
+                    const uint32_t ev = entry + 2 * (j >> 1) + 1;
                     ok = warp_wait(smem_u32(&c.full[ev % kStages]), (ev / kStages) & 1, dead);
                     if (!ok) break;
-                    if (clean_values(ring + ev % kStages * kTile, kTile / 16, row, 128, [&](int p) { return j * 128 + ((p >> 3) & 127) < job.n; })) {
+                    // half of a tile of 128 keys: 64 rows of 128 bytes of each block of 64 columns
+                    unsigned char* const half = ring + ev % kStages * kTile + h * kStep * 128;
+                    bool bad = false;
+                    for (int x = 0; x < HD / 64; ++x)
+                        bad |= clean_values(half + x * kAtom, kStep * 8, row, 128, [&](int p) { return j * kStep + (p >> 3) < job.n; });
+                    if (bad) {
                         *(volatile int*)&c.flags[i % kPromptJobs] = 1;
                         __threadfence_block();
                     }
@@ -282,16 +318,14 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
                 }
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&c.p_full[s]));
+                if (lane == 0) mbar_arrive(smem_u32(&c.p_full[s][h]));
             }
             entry += 2 * all;
-            if (tiles == 0) continue;
-            if (ok) {
-                ok = warp_wait(smem_u32(&c.o_full[s]), o_phase, dead);
-                o_phase ^= 1;
-            }
+            if (steps == 0) continue;
             const bool mine = token < T && t < job.n;
             uint16_t* const out = a.out + (long long)(job.first + t) * a.out_stride + (job.head * G + g) * HD;
+            if (ok) ok = warp_wait(smem_u32(&c.o_full[s]), full_phase, dead);      // (not o_done, which may still be two steps behind)
+            full_phase ^= 1;
             if (!ok) {                             // a copy or a product that never came: no result
                 if (mine)
                     for (int d = 0; d < HD; ++d) out[d] = 0x7fff;
@@ -300,23 +334,23 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
             tc_fence_after();
             const bool fix = *(volatile int*)&c.flags[i % kPromptJobs];
             const float inv = sum > 0.f ? 1.f / sum : sum;
-#pragma unroll 1
-            for (int d = 0; d < HD; d += 32) {
-                uint32_t o[32];
-                tmem_ld32(o_tmem + d, o);
-                tmem_ld_wait32(o);
+#pragma unroll 2
+            for (int d = 0; d < HD; d += 16) {
+                float o[16];
+                tmem_ld16(o_tmem + d, o);
+                tmem_ld_wait16(o);
                 if (mine) {
-                    uint32_t bad = 0;
-                    if (fix)
-                        for (int p = job.t0 >> 7 << 7; p <= t; ++p) bad |= not_finite32(a.v + (long long)(job.first + p) * a.v_stride + job.head * HD + d, 8);
 #pragma unroll
-                    for (int x = 0; x < 32; x += 8) {
-                        float y[8];
+                    for (int x = 0; x < 16; ++x) o[x] *= inv;
+                    if (fix) {
+                        const int p = job.t0 >> 7 << 7;
+                        const uint32_t bad = prompt_bad<HD>(a.v + (long long)(job.first + p) * a.v_stride + job.head * HD + d, a.v_stride, t + 1 - p);
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) y[e] = bad >> (x + e) & 1u ? __uint_as_float(0x7fffffffu) : __uint_as_float(o[x + e]) * inv;
-                        *reinterpret_cast<uint4*>(out + d + x) =
-                            make_uint4(pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3]), pack_bf16(y[4], y[5]), pack_bf16(y[6], y[7]));
+                        for (int x = 0; x < 16; ++x)
+                            if (bad >> x & 1u) o[x] = NAN;
                     }
+#pragma unroll
+                    for (int x = 0; x < 16; x += 8) *reinterpret_cast<uint4*>(out + d + x) = bf16x8(o + x);
                 }
                 __syncwarp();
             }

@@ -1,12 +1,15 @@
-// What both bf16 attention kernels (prompts, pages) do with a tile of 128 query rows by kKeys keys on the 5th-generation tensor cores.
+// What both bf16 attention kernels (prompts, pages) do with 128 query rows by 64 keys (a step) on the 5th-generation tensor cores.
 //
-//   S[128 x kKeys] = Q K^T        both operands in shared memory, fp32 scores in tensor memory, a lane per query row
+//   S[128 x 64] = Q K^T           both operands in shared memory, fp32 scores in tensor memory, a lane per query row
 //   P = exp2(scale S - ref)       one thread per row: its scores in registers, no exchange between threads.  ref is the row's running
 //                                 maximum as of the last time it rose by more than 2^8 in weight: O and the sum are rescaled only then, so that
-//                                 P <= 2^8, and hardly ever behind a row's first tile
+//                                 P <= 2^8, and hardly ever behind a row's first step
 //   O[128 x HD] += P V            P as bf16 in tensor memory (over the scores it was made of), V in shared memory, fp32 sums in tensor memory
 //
-// Two such streams per CTA, each with four warps of its own, keep the tensor cores at the one's products while the other's exponentials are taken.
+// Two such streams per CTA, each with four warps of its own; in bf16 each has two places for scores, so that its warps take one step's
+// exponentials while the tensor cores do the products of the step before and the scores of the next but one.  (Steps of 128 keys, of which tensor memory
+// holds one a stream: the warps waited for 1250 of 3740 cycles a pair of steps, and both streams at the same time.  The same with two
+// threads a row, in sixteen warps: 3900.)
 #pragma once
 #include "../tcgen05.cuh"
 
@@ -110,7 +113,7 @@ __device__ __forceinline__ uint64_t pair_exp2(uint64_t x) {
     x = pair_of(max_nan(a, -127.f), max_nan(b, -127.f));
     const uint64_t big = pair_of(12583039.f, 12583039.f);                      // 1.5 * 2^23 + 127: the sum's low bits are n + 127
     const uint64_t t = pair_add(x, big);
-    const uint64_t f = pair_add(x, pair_mul(pair_add(t, pair_of(-12583039.f, -12583039.f)), pair_of(-1.f, -1.f)));
+    const uint64_t f = pair_fma(pair_add(t, pair_of(-12583039.f, -12583039.f)), pair_of(-1.f, -1.f), x);
     uint64_t y = pair_of(0.009570102207362652f, 0.009570102207362652f);
     y = pair_fma(y, f, pair_of(0.05591785907745361f, 0.05591785907745361f));
     y = pair_fma(y, f, pair_of(0.240247443318367f, 0.240247443318367f));
@@ -146,7 +149,8 @@ __device__ __forceinline__ bool role_wait(uint32_t bar, uint32_t parity, volatil
 // The same for a whole warp, which goes on together.
 __device__ __forceinline__ bool warp_wait(uint32_t bar, uint32_t parity, volatile int* dead) { return __all_sync(0xffffffffu, role_wait(bar, parity, dead)); }
 
-// Registers: twelve warps are launched with 168 each; the four that fetch and issue hand over to the eight of the streams (8 x 208 + 4 x 88 = 12 x 168).
+// Warps 0-3 and 4-7: the streams'; 8-11 fetch and issue.  Twelve warps are launched with 168 registers each; the last four hand over to the others
+// (8 x 208 + 4 x 88 = 12 x 168).
 constexpr int kAttendThreads16 = 384, kLaunchRegisters = 168;
 __device__ __forceinline__ void registers_more() { asm volatile("setmaxnreg.inc.sync.aligned.u32 208;"); }
 __device__ __forceinline__ void registers_fewer() { asm volatile("setmaxnreg.dec.sync.aligned.u32 88;"); }
@@ -166,39 +170,63 @@ struct RingPlace {
 constexpr int kPoly = 1, kPolyOf = 4;              // of so many pairs of weights, those whose exponentials are polynomials
 constexpr float kRefExcess = 8.f;                  // log2 units by which a weight may exceed 1
 
-// One row's share of a tile.  `o_tmem`: the row's running sums, rescaled here if they have to be; `first`: there are none yet.  masked: bit c of `see`
-// says whether key c is seen; the others' scores are replaced, whatever they are.
-template <int HD, int kKeys, int kTerms>
-__device__ __forceinline__ void softmax_tile(uint32_t s_tmem, uint32_t o_tmem, float scale, bool first, bool masked, const uint32_t (&see)[kKeys / 32], float& ref,
-                                             float& sum) {
-    uint32_t s[kKeys];
+constexpr int kStep = 64;                          // keys
+
+// Adds a tile's sums to a row's.
+template <int HD>
+__device__ __forceinline__ void own_sums(uint32_t o_tmem, float (&own)[HD]) {
 #pragma unroll
-    for (int i = 0; i < kKeys; i += 32) tmem_ld32(s_tmem + i, s + i);
+    for (int c = 0; c < HD; c += 16) {
+        float o[16];
+        tmem_ld16(o_tmem + c, o);
+        tmem_ld_wait16(o);
 #pragma unroll
-    for (int i = 0; i < kKeys; i += 32) tmem_ld_wait32(s + i);
+        for (int i = 0; i < 16; ++i) own[c + i] += o[i];
+    }
+}
+
+// One row's step.  `first`: there are no sums yet.  masked: bit c of `see` says whether key c is seen; the others' scores are replaced, whatever they are.
+// products_done(): waits for the sums of the step before (false: given up, and so is this).
+// kOwn: the products of a step are sums of their own, which the thread adds to `own`: the tensor cores' additions truncate, which in bf16 does not
+// count, but would cost fp32 two bits over a long row.
+template <int HD, int kTerms, bool kOwn, typename Done>
+__device__ __forceinline__ bool softmax_step(uint32_t s_tmem, uint32_t o_tmem, float scale, bool first, bool masked, const uint32_t (&see)[2], float& ref, float& sum,
+                                             float (&own)[kOwn ? HD : 1], Done products_done) {
+    uint32_t s[kStep];
+#pragma unroll
+    for (int i = 0; i < kStep; i += 32) tmem_ld32(s_tmem + i, s + i);
+    if constexpr (kOwn)
+        if (!first) own_sums<HD>(o_tmem, own);
+#pragma unroll
+    for (int i = 0; i < kStep; i += 32) tmem_ld_wait32(s + i);
     if (masked) {
 #pragma unroll
-        for (int i = 0; i < kKeys; ++i)
+        for (int i = 0; i < kStep; ++i)
             if (!(see[i / 32] >> (i % 32) & 1u)) s[i] = 0xff800000u;
     }
     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-    for (int i = 0; i < kKeys; i += 2) mx[(i >> 1) & 3] = max3(mx[(i >> 1) & 3], __uint_as_float(s[i]), __uint_as_float(s[i + 1]));
+    for (int i = 0; i < kStep; i += 2) mx[(i >> 1) & 3] = max3(mx[(i >> 1) & 3], __uint_as_float(s[i]), __uint_as_float(s[i + 1]));
     const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
     const bool up = top > ref + kRefExcess || (ref == -INFINITY && top > ref);
     if (__any_sync(0xffffffffu, up)) {
         const float next = up ? top : ref, factor = up ? exp2_approx(ref - next) : 1.f;
         ref = next;
         sum *= factor;
-        if (!first) {
-#pragma unroll 1
-            for (int c = 0; c < HD; c += 32) {
-                uint32_t o[32];
-                tmem_ld32(o_tmem + c, o);
-                tmem_ld_wait32(o);
+        if constexpr (kOwn) {
 #pragma unroll
-                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * factor);
-                tmem_st32(o_tmem + c, o);
+            for (int i = 0; i < HD; ++i) own[i] *= factor;
+        } else if (!first) {
+            if (!products_done()) return false;
+            tc_fence_after();
+#pragma unroll 1
+            for (int c = 0; c < HD; c += 16) {
+                float o[16];
+                tmem_ld16(o_tmem + c, o);
+                tmem_ld_wait16(o);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[i] *= factor;
+                tmem_st16(o_tmem + c, o);
             }
         }
     }
@@ -206,7 +234,7 @@ __device__ __forceinline__ void softmax_tile(uint32_t s_tmem, uint32_t o_tmem, f
     const uint64_t scale2 = pair_of(scale, scale), shift2 = pair_of(shift, shift);
     uint64_t part[2] = {0, 0};
 #pragma unroll
-    for (int i = 0; i < kKeys; i += 2) {
+    for (int i = 0; i < kStep; i += 2) {
         uint64_t p = pair_fma(pair_of(s[i], s[i + 1]), scale2, shift2);
         float x, y;
         if (kTerms == 1 && (i / 2) % kPolyOf < kPoly) {
@@ -227,9 +255,9 @@ __device__ __forceinline__ void softmax_tile(uint32_t s_tmem, uint32_t o_tmem, f
     sum += even + odd;
 #pragma unroll
     for (int t = 0; t < kTerms; ++t) {
-        uint32_t p[kKeys / 2];
+        uint32_t p[kStep / 2];
 #pragma unroll
-        for (int i = 0; i < kKeys / 2; ++i) {
+        for (int i = 0; i < kStep / 2; ++i) {
             const float x = __uint_as_float(s[2 * i]), y = __uint_as_float(s[2 * i + 1]);
             p[i] = pack_bf16(x, y);
             if (t + 1 < kTerms) {                  // what the term leaves, exactly
@@ -237,10 +265,10 @@ __device__ __forceinline__ void softmax_tile(uint32_t s_tmem, uint32_t o_tmem, f
                 s[2 * i + 1] = __float_as_uint(y - __uint_as_float(p[i] & 0xffff0000u));
             }
         }
-#pragma unroll
-        for (int i = 0; i < kKeys / 2; i += 32) tmem_st32(s_tmem + t * (kKeys / 2) + i, p + i);
+        tmem_st32(s_tmem + t * (kStep / 2), p);
     }
     tmem_st_wait();
+    return true;
 }
 
 // Values of a tile that no row may take into its products: pieces that are no key's, and what is not finite.  A weight of 0 does not keep them out, so
@@ -272,11 +300,11 @@ __device__ __forceinline__ bool clean_values(unsigned char* tile, int pieces, in
     }
     return found;
 }
-// Bits of the 32 columns behind p whose value is not finite.
-__device__ __forceinline__ uint32_t not_finite32(const uint16_t* p, int piece_stride) {
+// Bits of the 16 columns behind p whose value is not finite.
+__device__ __forceinline__ uint32_t not_finite16(const uint16_t* p, int piece_stride) {
     uint32_t bits = 0;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
+    for (int c = 0; c < 2; ++c) {
         const uint4 x = *reinterpret_cast<const uint4*>(p + c * piece_stride);
         const uint32_t w[4] = {x.x, x.y, x.z, x.w};
 #pragma unroll

@@ -77,6 +77,7 @@ bool attend_ready(const void* kernel, int smem) {
     return cudaFuncGetAttributes(&at, kernel) == cudaSuccess && at.numRegs == kLaunchRegisters &&
            cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) == cudaSuccess;
 }
+static_assert(PromptShape<128>::kSmem <= 232448 && PromptShape<64>::kSmem <= 232448, "a CTA's shared memory");
 template <int HD, typename T>
 bool pages_ready() {
     static_assert(pages_smem<HD, T>() <= 232448, "a CTA's shared memory");
