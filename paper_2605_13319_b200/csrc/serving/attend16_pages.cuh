@@ -43,7 +43,7 @@ struct PagesJob {
     int slot;
 };
 struct PagesControl {
-    unsigned long long job_full, job_read, q_full, q_empty, k_full[8], k_empty[8], v_full[8], v_empty[8], s_full[2][2], p_full[2][2], o_done[2], o_full[2], joint, done;     // o_done: a step's products; o_full: a job's
+    unsigned long long job_full, job_read, q_full, q_empty, k_full[8], k_empty[8], v_full[8], v_empty[8], s_full[2][2], p_full[2][2], o_done[2], o_full[2], joint, done[2];  // o_done: products of a job's last step but one; o_full: of all
     PagesJob jobs[2];
     int bad_lo[2], bad_hi[2];   // tiles in which a value was not finite
     uint32_t present[32];       // eight positions a bit
@@ -191,7 +191,6 @@ __device__ __noinline__ uint32_t pages_bad(const PagesArgs& a, const PagesJob& j
 template <int HD, int kKeys, int kSlots>
 struct PagesFetch {
     static constexpr int kTile = kKeys * HD * 2;
-    RingPlace<kSlots> place;
     uint32_t count = 0;
 
     // said(tile, present): which groups of eight positions of a tile are there, said before its copies.
@@ -213,12 +212,12 @@ struct PagesFetch {
             const uint16_t* const src = block + (there ? id * page_elems + (size_t)(start + off0 - lane * ps) * HD : 0);
             const uint32_t groups = there ? ((1u << ((end - start) >> 3)) - 1u) << (start >> 3) : 0u, present = __reduce_or_sync(0xffffffffu, groups);
             say(j, present);
+            const RingPlace<kSlots> place(count);
             if (count >= kSlots && !warp_wait(smem_u32(&empty[place.slot]), place.phase ^ 1, dead)) return false;
             const uint32_t bar = smem_u32(&full[place.slot]);
             if (lane == 0) mbar_expect_tx(bar, (uint32_t)__popc(present) * (HD * 16));
             __syncwarp();
             if (there) bulk_g2s(smem_u32(ring + place.slot * kTile) + (uint32_t)start * (HD * 2), src, (uint32_t)(end - start) * (HD * 2), bar);
-            place.next();
             ++count;
             p0 += kKeys;
             page0 += per;
@@ -256,18 +255,17 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
 
     if (tid == 0) {
         mbar_init(smem_u32(&c.job_full), 1);
-        mbar_init(smem_u32(&c.job_read), 10);   // all other roles' warps
+        mbar_init(smem_u32(&c.job_read), 11);   // all other roles' warps
         mbar_init(smem_u32(&c.q_full), 8);
-        mbar_init(smem_u32(&c.q_empty), 1);
+        mbar_init(smem_u32(&c.q_empty), 2);
         mbar_init(smem_u32(&c.joint), 8);
-        mbar_init(smem_u32(&c.done), 1);
         for (int i = 0; i < kKSlots; ++i) {
             mbar_init(smem_u32(&c.k_full[i]), 1);
-            mbar_init(smem_u32(&c.k_empty[i]), 1);
+            mbar_init(smem_u32(&c.k_empty[i]), 2);
         }
         for (int i = 0; i < kVSlots; ++i) {
             mbar_init(smem_u32(&c.v_full[i]), 1);
-            mbar_init(smem_u32(&c.v_empty[i]), 1);
+            mbar_init(smem_u32(&c.v_empty[i]), 2);
         }
         for (int s = 0; s < 2; ++s) {
             for (int h = 0; h < 2; ++h) {
@@ -276,6 +274,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
             }
             mbar_init(smem_u32(&c.o_done[s]), 1);
             mbar_init(smem_u32(&c.o_full[s]), 1);
+            mbar_init(smem_u32(&c.done[s]), 1);
         }
         c.dead = 0;
         fence_mbar_init();
@@ -346,56 +345,44 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                 ok = fetch.run(a, job, 1, v_ring, c.v_full, c.v_empty, dead, [](int, uint32_t) {});
             }
             if (!ok) fetch.drain(c.v_full);
-        } else if (warp == 9) {                        // ---- products
+        } else if (warp == 9 || warp == 11) {      // ---- a stream's products
             if (elect_one()) {
-                RingPlace<kKSlots> kp;
-                RingPlace<kVSlots> vp;
+                const int s = warp == 9 ? 0 : 1;
+                using KPlace = RingPlace<kKSlots>;
+                using VPlace = RingPlace<kVSlots>;
+                uint32_t tile_no = 0;              // tiles of the jobs before
                 bool ok = true;
                 const uint64_t q_desc = umma_desc(smem_u32(smem), 128, HD * 16), k_desc = umma_desc(smem_u32(k_ring), 128, HD * 16),
                                v_desc = umma_desc(smem_u32(v_ring), HD * 16, 128);
-                uint32_t p_phase = 0;              // bit 2 s + h
-                // The next keys have come / the scores of stream s against half of them / their slot is free when what was issued so far is done; and so
-                // for values.
-                auto k_there = [&] {
-                    ok = ok && role_wait(smem_u32(&c.k_full[kp.slot]), kp.phase, dead);
+                uint32_t p_phase = 0;              // bit h
+                auto k_there = [&](const KPlace& k) {
+                    ok = ok && role_wait(smem_u32(&c.k_full[k.slot]), k.phase, dead);
                     if (ok) tc_fence_after();
                     return ok;
                 };
-                auto v_there = [&] {
-                    ok = ok && role_wait(smem_u32(&c.v_full[vp.slot]), vp.phase, dead);
-                    return ok;
-                };
-                auto scores = [&](int s, int q_tile, int h) {
-                    const uint64_t q = q_desc + (uint32_t)(q_tile * (Shape::kQTile >> 4)), k = k_desc + (kp.slot * (kTile >> 4) + h * kStep * HD * 2 / 16);
+                auto v_there = [&](const VPlace& v) { return ok = ok && role_wait(smem_u32(&c.v_full[v.slot]), v.phase, dead); };
+                auto scores = [&](const KPlace& k, int q_tile, int h) {
+                    const uint64_t q = q_desc + (uint32_t)(q_tile * (Shape::kQTile >> 4)), half = k_desc + (k.slot * (kTile >> 4) + h * kStep * HD * 2 / 16);
 #pragma unroll
                     for (int t = 0; t < kTerms; ++t)
 #pragma unroll
                         for (int x = 0; x < HD / 16; ++x)
-                            umma_bf16(tmem + 128 * s + kStep * h, q + ((kTerms - 1 - t) * (Shape::kQTile >> 4) + x * 16), k + x * 16, kIdescS, t + x > 0);
+                            umma_bf16(tmem + 128 * s + kStep * h, q + ((kTerms - 1 - t) * (Shape::kQTile >> 4) + x * 16), half + x * 16, kIdescS, t + x > 0);
                     umma_commit(smem_u32(&c.s_full[s][h]));
                 };
-                auto k_done = [&] {
-                    umma_commit(smem_u32(&c.k_empty[kp.slot]));
-                    kp.next();
-                };
-                auto sums = [&](int s, int h, bool first, bool last) {
-                    ok = ok && role_wait(smem_u32(&c.p_full[s][h]), p_phase >> (2 * s + h) & 1u, dead);
-                    p_phase ^= 1u << (2 * s + h);
+                auto sums = [&](const VPlace& v, int h, bool first) {
+                    ok = ok && role_wait(smem_u32(&c.p_full[s][h]), p_phase >> h & 1u, dead);
+                    p_phase ^= 1u << h;
                     if (!ok) return false;
                     tc_fence_after();
-                    const uint64_t v = v_desc + (vp.slot * (kTile >> 4) + h * kStep * HD * 2 / 16);
+                    const uint64_t half = v_desc + (v.slot * (kTile >> 4) + h * kStep * HD * 2 / 16);
 #pragma unroll
                     for (int t = 0; t < kTerms; ++t)
 #pragma unroll
                         for (int x = 0; x < kStep / 16; ++x)
-                            umma_bf16_ta(tmem + 256 + HD * s, tmem + 128 * s + kStep * h + (kTerms - 1 - t) * (kStep / 2) + 8 * x, v + x * HD * 2, kIdescO, (!kOwn && !first) || t + x > 0);
-                    umma_commit(smem_u32(&c.o_done[s]));
-                    if (last) umma_commit(smem_u32(&c.o_full[s]));
+                            umma_bf16_ta(tmem + 256 + HD * s, tmem + 128 * s + kStep * h + (kTerms - 1 - t) * (kStep / 2) + 8 * x, half + x * HD * 2, kIdescO,
+                                         (!kOwn && !first) || t + x > 0);
                     return true;
-                };
-                auto v_done = [&] {
-                    umma_commit(smem_u32(&c.v_empty[vp.slot]));
-                    vp.next();
                 };
                 for (int i = 0; ok; ++i) {
                     ok = role_wait(smem_u32(&c.job_full), i & 1, dead);
@@ -404,52 +391,43 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                     const bool both = c.jobs[i & 1].n_rows > 128;
                     mbar_arrive(smem_u32(&c.job_read));
                     if (n == 0) break;
+                    // both: rows of q tile s, every tile of keys; else the same rows, tiles in turn
+                    const int step = both ? 1 : 2, q_tile = both ? s : 0, j0 = both ? 0 : s;
+                    // A slot is free when what was issued so far is done, for both streams: the only one that uses it says so twice.
+                    auto release = [&](unsigned long long* bar) {
+                        umma_commit(smem_u32(bar));
+                        if (!both) umma_commit(smem_u32(bar));
+                    };
                     ok = role_wait(smem_u32(&c.q_full), i & 1, dead);
-                    if (!k_there()) break;
-                    if (both) {                    // stream s: rows of q tile s, every tile of keys
-                        for (int h = 0; h < kHalves; ++h)
-                            for (int s = 0; s < 2; ++s) scores(s, s, h);
-                        k_done();
-                        if (n == 1) umma_commit(smem_u32(&c.q_empty));
-                        for (int j = 0; j < n && ok; ++j) {
-                            const bool more = j + 1 < n;
-                            if (!v_there() || (more && !k_there())) break;
-                            for (int h = 0; h < kHalves && ok; ++h)
-                                for (int s = 0; s < 2; ++s) {
-                                    if (!sums(s, h, j + h == 0, !more && h == kHalves - 1)) break;
-                                    if (more) scores(s, s, h);
-                                }
-                            if (!ok) break;
-                            v_done();
-                            if (more) k_done();
-                            if (j + 2 == n) umma_commit(smem_u32(&c.q_empty));
-                        }
-                    } else {                       // the same rows, tiles in turn
-                        for (int h = 0; h < kHalves; ++h) scores(0, 0, h);
-                        k_done();
-                        if (n > 1) {
-                            if (!k_there()) break;
-                            for (int h = 0; h < kHalves; ++h) scores(1, 0, h);
-                            k_done();
-                        }
-                        if (n <= 2) umma_commit(smem_u32(&c.q_empty));
-                        for (int j = 0; j < n && ok; ++j) {
-                            const bool more = j + 2 < n;
-                            if (!v_there() || (more && !k_there())) break;
-                            for (int h = 0; h < kHalves; ++h) {
-                                if (!sums(j & 1, h, j < 2 && h == 0, !more && h == kHalves - 1)) break;
-                                if (more) scores(j & 1, 0, h);
-                            }
-                            if (!ok) break;
-                            v_done();
-                            if (more) k_done();
-                            if (j + 3 == n) umma_commit(smem_u32(&c.q_empty));
-                        }
+                    if (!ok) break;
+                    if (j0 < n) {
+                        const KPlace k(tile_no + j0);
+                        if (!k_there(k)) break;
+                        for (int h = 0; h < kHalves; ++h) scores(k, q_tile, h);
+                        release(&c.k_empty[k.slot]);
                     }
+                    if (j0 + step >= n) umma_commit(smem_u32(&c.q_empty));
+                    for (int j = j0; j < n && ok; j += step) {
+                        const bool more = j + step < n;
+                        const KPlace k(tile_no + j + step);
+                        const VPlace v(tile_no + j);
+                        if (!v_there(v) || (more && !k_there(k))) break;
+                        for (int h = 0; h < kHalves; ++h) {
+                            if (!sums(v, h, j == j0 && h == 0)) break;
+                            if (!more && h == kHalves - 2) umma_commit(smem_u32(&c.o_done[s]));
+                            if (!more && h == kHalves - 1) umma_commit(smem_u32(&c.o_full[s]));
+                            if (more) scores(k, q_tile, h);
+                        }
+                        if (!ok) break;
+                        release(&c.v_empty[v.slot]);
+                        if (more) release(&c.k_empty[k.slot]);
+                        if (more && j + 2 * step >= n) umma_commit(smem_u32(&c.q_empty));
+                    }
+                    tile_no += n;
                 }
-                if (!ok) {                             // products in flight end before their memory is given back
-                    umma_commit(smem_u32(&c.done));
-                    mbar_wait(smem_u32(&c.done), 0);
+                if (!ok) {                         // products in flight end before their memory is given back
+                    umma_commit(smem_u32(&c.done[s]));
+                    mbar_wait(smem_u32(&c.done[s]), 0);
                 }
             }
             __syncwarp();
@@ -458,8 +436,8 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
         registers_more();
         const int s = warp >> 2, row = tid & 127;
         const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16, s_tmem = tmem + 128 * s + lanes, o_tmem = tmem + 256 + HD * s + lanes;
-        // phases: s_phase bit h, o_phase of the last step's products; tile_no: tiles fetched by this CTA before the job's
-        uint32_t tile_no = 0, s_phase = 0, o_phase = 0, full_phase = 0, joint_phase = 0;
+        // s_phase: bit h; tile_no: tiles of the jobs before
+        uint32_t tile_no = 0, s_phase = 0, done_phase = 0, full_phase = 0, joint_phase = 0;
         auto joint = [&] {                         // both streams' warps
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&c.joint));
@@ -467,7 +445,6 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
             joint_phase ^= 1;
             return there;
         };
-        auto products_done = [&] { return warp_wait(smem_u32(&c.o_done[s]), o_phase ^ 1u, dead); };
         for (int i = 0;; ++i) {
             if (!warp_wait(smem_u32(&c.job_full), i & 1, dead)) break;
             const PagesJob& job = c.jobs[i & 1];           // (as it is until the next but one is said, when both streams have read the next)
@@ -534,9 +511,13 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                         masked = true;
                     }
                     const bool first = (both ? j : j >> 1) + h == 0;
+                    // The products of the step before are done when the scores issued behind them are, or, where no step follows, by a barrier of their own.
+                    auto products_done = [&] {
+                        return h == 0 || j + (both ? 1 : 2) < n ? warp_wait(smem_u32(&c.s_full[s][h ^ 1]), s_phase >> (h ^ 1) & 1u, dead)
+                                                                : warp_wait(smem_u32(&c.o_done[s]), done_phase, dead);
+                    };
                     if (any) ok = softmax_step<HD, kTerms, kOwn>(s_tmem + kStep * h, o_tmem, a.scale, first, masked, see, ref, sum, own, products_done);
                     if (!ok) break;
-                    o_phase ^= 1;
                     if (masked) {
                         const uint32_t v = tile_no + j;
                         ok = warp_wait(smem_u32(&c.v_full[v % kVSlots]), v / kVSlots & 1, dead);
@@ -559,8 +540,11 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
             }
             // ---- the range's sums
             const bool mine_has = both || s < n;
-            if (ok && mine_has) ok = warp_wait(smem_u32(&c.o_full[s]), full_phase, dead);      // (not o_done, which may still be two steps behind)
-            if (mine_has) full_phase ^= 1;
+            if (ok && mine_has) ok = warp_wait(smem_u32(&c.o_full[s]), full_phase, dead);
+            if (mine_has) {
+                full_phase ^= 1;
+                done_phase ^= 1;
+            }
             tile_no += n;
             tc_fence_after();
             if constexpr (kOwn)

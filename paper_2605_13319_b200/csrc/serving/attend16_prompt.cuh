@@ -5,7 +5,8 @@
 // stream of its own (attend16_tile.cuh); both go through the same keys, from the first up to their last token, in steps of 64.
 // A CTA per SM takes jobs in turn: sorted by length (block of tokens, last first; then prompts, then heads), dealt out back and forth, so that the CTAs'
 // sums differ by less than a job.  Nothing is shared between CTAs: no atomics, no scratch.
-// Warps: 0-3 and 4-7 the streams' rows, 8 fetches (copy engine, 128-byte swizzle; 128 keys at a time), 9 issues the products.
+// Warps: 0-3 and 4-7 the streams' rows, 8 fetches (copy engine, 128-byte swizzle; 128 keys at a time), 9 and 11 issue the
+// streams' products.
 #pragma once
 #include "attend16_tile.cuh"
 
@@ -26,7 +27,7 @@ struct PromptJob {
 constexpr int kPromptJobs = 2;
 
 struct PromptControl {
-    unsigned long long q_full, q_empty, full[16], empty[16], s_full[2][2], p_full[2][2], o_done[2], o_full[2], done;      // o_done: a step's products; o_full: a job's
+    unsigned long long q_full, q_empty, full[16], empty[16], s_full[2][2], p_full[2][2], o_done[2], o_full[2], done[2];   // o_done: products of a job's last step but one; o_full: of all
     PromptJob jobs[kPromptJobs];
     int flags[kPromptJobs];     // a value of the job's last tiles was not finite
     uint32_t tmem;
@@ -119,11 +120,10 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
 
     if (tid == 0) {
         mbar_init(smem_u32(&c.q_full), 1);
-        mbar_init(smem_u32(&c.q_empty), 9);      // the products, and the streams' warps when they have read the job
-        mbar_init(smem_u32(&c.done), 1);
+        mbar_init(smem_u32(&c.q_empty), 10);     // both streams' products, and their warps when they have read the job
         for (int i = 0; i < kStages; ++i) {
             mbar_init(smem_u32(&c.full[i]), 1);
-            mbar_init(smem_u32(&c.empty[i]), 1);
+            mbar_init(smem_u32(&c.empty[i]), 2);
         }
         for (int s = 0; s < 2; ++s) {
             for (int h = 0; h < 2; ++h) {
@@ -132,6 +132,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
             }
             mbar_init(smem_u32(&c.o_done[s]), 1);
             mbar_init(smem_u32(&c.o_full[s]), 1);
+            mbar_init(smem_u32(&c.done[s]), 1);
         }
         c.dead = 0;
         fence_mbar_init();
@@ -188,41 +189,35 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
             if (!ok && lane == 0) {                    // given up: the copies in flight are waited for
                 for (uint32_t e = entry > kStages ? entry - kStages : 0; e < entry; ++e) mbar_wait(smem_u32(&c.full[e % kStages]), (e / kStages) & 1);
             }
-        } else if (warp == 9) {                        // ---- products
+        } else if (warp == 9 || warp == 11) {      // ---- a stream's products
             if (elect_one()) {
-                RingPlace<kStages> place;          // the next of the ring that has not come yet
-                uint32_t k_slot = 0, v_slot = 0;
+                const int s = warp == 9 ? 0 : 1;
+                using Place = RingPlace<kStages>;
+                uint32_t entry = 0;                // of the ring, over all jobs: tile t's keys at entry + 2 t, its values behind them
                 bool ok = true;
-                const uint64_t q_desc = umma_desc_swizzled(smem_u32(smem), 16, 1024), k_desc = umma_desc_swizzled(smem_u32(ring), 16, 1024),
+                const uint64_t q_desc = umma_desc_swizzled(smem_u32(smem + s * kTile), 16, 1024), k_desc = umma_desc_swizzled(smem_u32(ring), 16, 1024),
                                v_desc = umma_desc_swizzled(smem_u32(ring), kAtom, 1024);
-                uint32_t p_phase = 0;              // bit 2 s + h
-                auto arrived = [&](uint32_t& slot) {
-                    ok = ok && role_wait(smem_u32(&c.full[place.slot]), place.phase, dead);
-                    slot = place.slot;
-                    place.next();
-                    return ok;
-                };
-                auto release = [&](uint32_t slot) { umma_commit(smem_u32(&c.empty[slot])); };
-                auto scores = [&](int s, int h) {
-                    const uint64_t q = q_desc + (uint32_t)(s * (kTile >> 4)), k = k_desc + (k_slot * (kTile >> 4) + h * (kStep * 128 >> 4));
+                uint32_t p_phase = 0;              // bit h
+                auto arrived = [&](const Place& at) { return ok = ok && role_wait(smem_u32(&c.full[at.slot]), at.phase, dead); };
+                auto release = [&](const Place& at) { umma_commit(smem_u32(&c.empty[at.slot])); };      // free when what was issued so far is done
+                auto scores = [&](const Place& k, int h) {
+                    const uint64_t half = k_desc + (k.slot * (kTile >> 4) + h * (kStep * 128 >> 4));
 #pragma unroll
                     for (int x = 0; x < HD / 16; ++x) {
                         const uint32_t at = ((x >> 2) * kAtom + (x & 3) * 32) >> 4;
-                        umma_bf16(tmem + 128 * s + kStep * h, q + at, k + at, kIdescS, x > 0);
+                        umma_bf16(tmem + 128 * s + kStep * h, q_desc + at, half + at, kIdescS, x > 0);
                     }
                     umma_commit(smem_u32(&c.s_full[s][h]));
                 };
-                auto sums = [&](int s, int h, bool first, bool last) {
-                    ok = ok && role_wait(smem_u32(&c.p_full[s][h]), p_phase >> (2 * s + h) & 1u, dead);
-                    p_phase ^= 1u << (2 * s + h);
+                auto sums = [&](const Place& v, int h, bool first) {
+                    ok = ok && role_wait(smem_u32(&c.p_full[s][h]), p_phase >> h & 1u, dead);
+                    p_phase ^= 1u << h;
                     if (!ok) return false;
                     tc_fence_after();
-                    const uint64_t v = v_desc + (v_slot * (kTile >> 4) + h * (kStep * 128 >> 4));
+                    const uint64_t half = v_desc + (v.slot * (kTile >> 4) + h * (kStep * 128 >> 4));
 #pragma unroll
                     for (int x = 0; x < kStep / 16; ++x)
-                        umma_bf16_ta(tmem + 256 + HD * s, tmem + 128 * s + kStep * h + 8 * x, v + x * (2048 >> 4), kIdescO, !first || x > 0);
-                    umma_commit(smem_u32(&c.o_done[s]));
-                    if (last) umma_commit(smem_u32(&c.o_full[s]));
+                        umma_bf16_ta(tmem + 256 + HD * s, tmem + 128 * s + kStep * h + 8 * x, half + x * (2048 >> 4), kIdescO, !first || x > 0);
                     return true;
                 };
                 for (int i = 0; ok; ++i) {
@@ -230,38 +225,41 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
                     if (!ok) break;
                     const PromptJob job = c.jobs[i % kPromptJobs];
                     if (job.n == 0) break;
-                    const int n0 = prompt_steps(job, 0, T), n1 = prompt_steps(job, 1, T), n = max(n0, n1);
-                    // The scores of step j (both streams' where they go so far); the last of a tile of keys lets go of it, the last of all of q too.
-                    auto all_scores = [&](int j, int s) {
-                        if (j < (s ? n1 : n0)) scores(s, j & 1);
-                        if (s == 0) return;
-                        if ((j & 1) || j + 1 == n) release(k_slot);
-                        if (j + 1 == n) umma_commit(smem_u32(&c.q_empty));
-                    };
-                    if (!arrived(k_slot)) break;
-                    tc_fence_after();
-                    all_scores(0, 0);
-                    all_scores(0, 1);
-                    if (n > 1) {
-                        all_scores(1, 0);
-                        all_scores(1, 1);
+                    const int n = prompt_steps(job, s, T), tiles = (max(n, prompt_steps(job, 1 - s, T)) + 1) >> 1;
+                    if (n > 0) {
+                        const Place k(entry);
+                        if (!arrived(k)) break;
+                        tc_fence_after();
+                        scores(k, 0);
+                        if (n > 1) scores(k, 1);
+                        release(k);
+                        if (n <= 2) umma_commit(smem_u32(&c.q_empty));
+                    } else {
+                        mbar_arrive(smem_u32(&c.q_empty));
                     }
                     for (int j = 0; j < n; ++j) {
+                        const Place v(entry + (j & ~1) + 1), k(entry + (j & ~1) + 2);      // of this step, and of the next but one
                         const bool more = j + 2 < n;
-                        if (!(j & 1)) {
-                            if (!arrived(v_slot)) break;
-                            if (more && !arrived(k_slot)) break;
+                        if (!(j & 1) && (!arrived(v) || (more && !arrived(k)))) break;
+                        if (!sums(v, j & 1, j == 0)) break;
+                        if (j + 2 == n) umma_commit(smem_u32(&c.o_done[s]));
+                        if (j + 1 == n) umma_commit(smem_u32(&c.o_full[s]));
+                        if (more) {
+                            scores(k, j & 1);
+                            if ((j & 1) || j + 3 == n) release(k);
+                            if (j + 3 == n) umma_commit(smem_u32(&c.q_empty));
                         }
-                        if (j < n0 && !sums(0, j & 1, j == 0, j + 1 == n0)) break;
-                        if (more) all_scores(j + 2, 0);
-                        if (j < n1 && !sums(1, j & 1, j == 0, j + 1 == n1)) break;
-                        if (more) all_scores(j + 2, 1);
-                        if ((j & 1) || j + 1 == n) release(v_slot);
+                        if ((j & 1) || j + 1 == n) release(v);
                     }
+                    for (int e = 2 * ((n + 1) >> 1); e < 2 * tiles && ok; ++e) {           // what the other stream alone goes through
+                        const Place at(entry + e);
+                        if (arrived(at)) mbar_arrive(smem_u32(&c.empty[at.slot]));
+                    }
+                    entry += 2 * tiles;
                 }
-                if (!ok) {                             // products in flight end before their memory is given back
-                    umma_commit(smem_u32(&c.done));
-                    mbar_wait(smem_u32(&c.done), 0);
+                if (!ok) {                         // products in flight end before their memory is given back
+                    umma_commit(smem_u32(&c.done[s]));
+                    mbar_wait(smem_u32(&c.done[s]), 0);
                 }
             }
             __syncwarp();
@@ -270,7 +268,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
         registers_more();
         const int s = warp >> 2, row = tid & 127, token = row / G, g = row % G;
         const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16, s_tmem = tmem + 128 * s + lanes, o_tmem = tmem + 256 + HD * s + lanes;
-        uint32_t entry = 0, s_phase = 0, o_phase = 0, full_phase = 0;          // s_phase: bit h; o_phase: of the last step's products
+        uint32_t entry = 0, s_phase = 0, done_phase = 0, full_phase = 0;       // s_phase: bit h
         for (int i = 0;; ++i) {
             if (!warp_wait(smem_u32(&c.q_full), i & 1, dead)) break;
             const PromptJob job = c.jobs[i % kPromptJobs];
@@ -282,8 +280,13 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
             const int clear = (job.t0 + s * T + 1) / kStep;                    // steps that every row sees whole
             float ref = -INFINITY, sum = 0.f, none[1];
             bool ok = true;
-            auto products_done = [&] { return warp_wait(smem_u32(&c.o_done[s]), o_phase ^ 1, dead); };
-            for (int j = 0; j < steps; ++j) {
+            int j = 0;
+            // The products of the step before are done when the scores issued behind them are, or, where no step follows, by a barrier of their own.
+            auto products_done = [&] {
+                const int h = (j + 1) & 1;
+                return j + 1 < steps ? warp_wait(smem_u32(&c.s_full[s][h]), s_phase >> h & 1u, dead) : warp_wait(smem_u32(&c.o_done[s]), done_phase, dead);
+            };
+            for (; j < steps; ++j) {
                 const int h = j & 1;
                 uint32_t see[2];
                 const bool masked = j >= clear;
@@ -300,7 +303,6 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
                 tc_fence_after();
                 ok = softmax_step<HD, 1, false>(s_tmem + kStep * h, o_tmem, a.scale, j == 0, masked, see, ref, sum, none, products_done);
                 if (!ok) break;
-                o_phase ^= 1;
                 if (masked) {
                     const uint32_t ev = entry + 2 * (j >> 1) + 1;
                     ok = warp_wait(smem_u32(&c.full[ev % kStages]), (ev / kStages) & 1, dead);
@@ -322,9 +324,10 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
             }
             entry += 2 * all;
             if (steps == 0) continue;
+            if (steps > 1) done_phase ^= 1;
             const bool mine = token < T && t < job.n;
             uint16_t* const out = a.out + (long long)(job.first + t) * a.out_stride + (job.head * G + g) * HD;
-            if (ok) ok = warp_wait(smem_u32(&c.o_full[s]), full_phase, dead);      // (not o_done, which may still be two steps behind)
+            if (ok) ok = warp_wait(smem_u32(&c.o_full[s]), full_phase, dead);
             full_phase ^= 1;
             if (!ok) {                             // a copy or a product that never came: no result
                 if (mine)

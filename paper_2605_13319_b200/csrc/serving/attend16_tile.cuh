@@ -6,10 +6,10 @@
 //                                 P <= 2^8, and hardly ever behind a row's first step
 //   O[128 x HD] += P V            P as bf16 in tensor memory (over the scores it was made of), V in shared memory, fp32 sums in tensor memory
 //
-// Two such streams per CTA, each with four warps of its own; in bf16 each has two places for scores, so that its warps take one step's
+// Two such streams per CTA, each with four warps of its own and a thread that issues its products; in bf16 each has two places for scores, so that its warps take one step's
 // exponentials while the tensor cores do the products of the step before and the scores of the next but one.  (Steps of 128 keys, of which tensor memory
 // holds one a stream: the warps waited for 1250 of 3740 cycles a pair of steps, and both streams at the same time.  The same with two
-// threads a row, in sixteen warps: 3900.)
+// threads a row, in sixteen warps: 3900.  One thread for both streams' products took 3900 cycles for what the tensor cores do in 2560.)
 #pragma once
 #include "../tcgen05.cuh"
 
@@ -155,16 +155,11 @@ constexpr int kAttendThreads16 = 384, kLaunchRegisters = 168;
 __device__ __forceinline__ void registers_more() { asm volatile("setmaxnreg.inc.sync.aligned.u32 208;"); }
 __device__ __forceinline__ void registers_fewer() { asm volatile("setmaxnreg.dec.sync.aligned.u32 88;"); }
 
-// A place in a ring of n slots.
+// Slot and phase of the at-th entry of a ring of n slots.
 template <int n>
 struct RingPlace {
-    uint32_t slot = 0, phase = 0;
-    __device__ __forceinline__ void next() {
-        if (++slot == n) {
-            slot = 0;
-            phase ^= 1;
-        }
-    }
+    uint32_t slot, phase;
+    __device__ __forceinline__ explicit RingPlace(uint32_t at) : slot(at % n), phase(at / n & 1u) {}
 };
 
 constexpr int kPoly = 1, kPolyOf = 4;              // of so many pairs of weights, those whose exponentials are polynomials
