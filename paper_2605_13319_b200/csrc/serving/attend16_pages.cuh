@@ -43,7 +43,7 @@ struct PagesJob {
     int slot;
 };
 struct PagesControl {
-    unsigned long long job_full, job_read, q_full, q_empty, k_full[8], k_empty[8], v_full[8], v_empty[8], s_full[2][2], p_full[2][2], o_done[2], o_full[2], joint, done[2];  // o_done: products of a job's last step but one; o_full: of all
+    unsigned long long job_full, job_read, q_full, q_empty, k_full[8], k_empty[8], v_full[8], v_empty[8], s_full[2], p_full[2][2], o_full[2], joint, done[2];
     PagesJob jobs[2];
     int bad_lo[2], bad_hi[2];   // tiles in which a value was not finite
     uint32_t present[32];       // eight positions a bit
@@ -241,9 +241,9 @@ template <int HD, typename T>
 __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const __grid_constant__ PagesArgs a) {
     using Shape = PagesShape<HD, T>;
     constexpr int kKeys = Shape::kKeys, kTile = Shape::kTile, kKSlots = Shape::kKSlots, kVSlots = Shape::kVSlots, kTerms = Shape::kTerms, kPieces = HD / 8;
-    constexpr int kHalves = Shape::kHalves;        // steps of a tile, and places for a stream's scores
+    constexpr int kHalves = Shape::kHalves;        // in which a tile's weights go over
     constexpr bool kOwn = Shape::kWide;            // the threads add up the tiles' sums
-    constexpr uint32_t kIdescS = umma_idesc_bf16(128, kStep, 0, 0), kIdescO = umma_idesc_bf16(128, HD, 0, 1);
+    constexpr uint32_t kIdescS = umma_idesc_bf16(128, kKeys, 0, 0), kIdescO = umma_idesc_bf16(128, HD, 0, 1);
     extern __shared__ __align__(128) unsigned char smem[];
     unsigned char* const k_ring = smem + Shape::kQ;
     unsigned char* const v_ring = k_ring + kKSlots * kTile;
@@ -268,11 +268,8 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
             mbar_init(smem_u32(&c.v_empty[i]), 2);
         }
         for (int s = 0; s < 2; ++s) {
-            for (int h = 0; h < 2; ++h) {
-                mbar_init(smem_u32(&c.s_full[s][h]), 1);
-                mbar_init(smem_u32(&c.p_full[s][h]), 4);
-            }
-            mbar_init(smem_u32(&c.o_done[s]), 1);
+            mbar_init(smem_u32(&c.s_full[s]), 1);
+            for (int h = 0; h < 2; ++h) mbar_init(smem_u32(&c.p_full[s][h]), 4);
             mbar_init(smem_u32(&c.o_full[s]), 1);
             mbar_init(smem_u32(&c.done[s]), 1);
         }
@@ -354,34 +351,36 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                 bool ok = true;
                 const uint64_t q_desc = umma_desc(smem_u32(smem), 128, HD * 16), k_desc = umma_desc(smem_u32(k_ring), 128, HD * 16),
                                v_desc = umma_desc(smem_u32(v_ring), HD * 16, 128);
-                uint32_t p_phase = 0;              // bit h
+                uint32_t p_phase = 0;              // of both halves
                 auto k_there = [&](const KPlace& k) {
                     ok = ok && role_wait(smem_u32(&c.k_full[k.slot]), k.phase, dead);
                     if (ok) tc_fence_after();
                     return ok;
                 };
                 auto v_there = [&](const VPlace& v) { return ok = ok && role_wait(smem_u32(&c.v_full[v.slot]), v.phase, dead); };
-                auto scores = [&](const KPlace& k, int q_tile, int h) {
-                    const uint64_t q = q_desc + (uint32_t)(q_tile * (Shape::kQTile >> 4)), half = k_desc + (k.slot * (kTile >> 4) + h * kStep * HD * 2 / 16);
+                auto scores = [&](const KPlace& k, int q_tile) {
+                    const uint64_t q = q_desc + (uint32_t)(q_tile * (Shape::kQTile >> 4)), tile = k_desc + k.slot * (kTile >> 4);
 #pragma unroll
                     for (int t = 0; t < kTerms; ++t)
 #pragma unroll
                         for (int x = 0; x < HD / 16; ++x)
-                            umma_bf16(tmem + 128 * s + kStep * h, q + ((kTerms - 1 - t) * (Shape::kQTile >> 4) + x * 16), half + x * 16, kIdescS, t + x > 0);
-                    umma_commit(smem_u32(&c.s_full[s][h]));
+                            umma_bf16(tmem + 128 * s, q + ((kTerms - 1 - t) * (Shape::kQTile >> 4) + x * 16), tile + x * 16, kIdescS, t + x > 0);
+                    umma_commit(smem_u32(&c.s_full[s]));
                 };
-                auto sums = [&](const VPlace& v, int h, bool first) {
-                    ok = ok && role_wait(smem_u32(&c.p_full[s][h]), p_phase >> h & 1u, dead);
-                    p_phase ^= 1u << h;
-                    if (!ok) return false;
-                    tc_fence_after();
-                    const uint64_t half = v_desc + (v.slot * (kTile >> 4) + h * kStep * HD * 2 / 16);
+                auto sums = [&](const VPlace& v, bool first) {
+                    const uint64_t tile = v_desc + v.slot * (kTile >> 4);
+                    for (int h = 0; h < kHalves; ++h) {
+                        ok = ok && role_wait(smem_u32(&c.p_full[s][h]), p_phase, dead);
+                        if (!ok) return false;
+                        tc_fence_after();
 #pragma unroll
-                    for (int t = 0; t < kTerms; ++t)
+                        for (int t = 0; t < kTerms; ++t)
 #pragma unroll
-                        for (int x = 0; x < kStep / 16; ++x)
-                            umma_bf16_ta(tmem + 256 + HD * s, tmem + 128 * s + kStep * h + (kTerms - 1 - t) * (kStep / 2) + 8 * x, half + x * HD * 2, kIdescO,
-                                         (!kOwn && !first) || t + x > 0);
+                            for (int x = 0; x < 4; ++x)
+                                umma_bf16_ta(tmem + 256 + HD * s, tmem + 128 * s + (kTerms - 1 - t) * (kKeys / 2) + 32 * h + 8 * x, tile + (4 * h + x) * HD * 2, kIdescO,
+                                             (!kOwn && !first) || t + h + x > 0);
+                    }
+                    p_phase ^= 1;
                     return true;
                 };
                 for (int i = 0; ok; ++i) {
@@ -403,22 +402,18 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                     if (j0 < n) {
                         const KPlace k(tile_no + j0);
                         if (!k_there(k)) break;
-                        for (int h = 0; h < kHalves; ++h) scores(k, q_tile, h);
+                        scores(k, q_tile);
                         release(&c.k_empty[k.slot]);
                     }
                     if (j0 + step >= n) umma_commit(smem_u32(&c.q_empty));
-                    for (int j = j0; j < n && ok; j += step) {
+                    for (int j = j0; j < n; j += step) {
                         const bool more = j + step < n;
                         const KPlace k(tile_no + j + step);
                         const VPlace v(tile_no + j);
                         if (!v_there(v) || (more && !k_there(k))) break;
-                        for (int h = 0; h < kHalves; ++h) {
-                            if (!sums(v, h, j == j0 && h == 0)) break;
-                            if (!more && h == kHalves - 2) umma_commit(smem_u32(&c.o_done[s]));
-                            if (!more && h == kHalves - 1) umma_commit(smem_u32(&c.o_full[s]));
-                            if (more) scores(k, q_tile, h);
-                        }
-                        if (!ok) break;
+                        if (!sums(v, j == j0)) break;
+                        if (more) scores(k, q_tile);
+                        else umma_commit(smem_u32(&c.o_full[s]));
                         release(&c.v_empty[v.slot]);
                         if (more) release(&c.k_empty[k.slot]);
                         if (more && j + 2 * step >= n) umma_commit(smem_u32(&c.q_empty));
@@ -436,8 +431,8 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
         registers_more();
         const int s = warp >> 2, row = tid & 127;
         const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16, s_tmem = tmem + 128 * s + lanes, o_tmem = tmem + 256 + HD * s + lanes;
-        // s_phase: bit h; tile_no: tiles of the jobs before
-        uint32_t tile_no = 0, s_phase = 0, done_phase = 0, full_phase = 0, joint_phase = 0;
+        using VPlace = RingPlace<kVSlots>;
+        uint32_t tile_no = 0, s_phase = 0, full_phase = 0, joint_phase = 0;    // tile_no: tiles of the jobs before
         auto joint = [&] {                         // both streams' warps
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&c.joint));
@@ -485,66 +480,59 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
             // positions that every row of the stream sees
             const int clear = a.mask ? job.base : job.base + (job.rho0 + (both ? 128 * s : 0)) / G + 1;
             float ref = -INFINITY, sum = 0.f, own[kOwn ? HD : 1] = {};
-            for (int j = both ? 0 : s; j < n && ok; j += both ? 1 : 2) {
-                const int u = job.u0 + j;
-#pragma unroll 1
-                for (int h = 0; h < kHalves && ok; ++h) {
-                    const int p0 = u * kKeys + h * kStep;
-                    uint32_t see[2];
-                    bool masked = p0 + kStep > clear;
-                    if (masked) {
+            for (int j = both ? 0 : s; j < n; j += both ? 1 : 2) {
+                const int u = job.u0 + j, p0 = u * kKeys;
+                uint32_t see[kKeys / 32];
+                bool masked = p0 + kKeys > clear;
+                if (masked) {
 #pragma unroll
-                        for (int w = 0; w < 2; ++w) see[w] = pages_see(a, job, node, p0 + 32 * w);
-                    }
-                    ok = warp_wait(smem_u32(&c.s_full[s][h]), s_phase >> h & 1u, dead);
-                    s_phase ^= 1u << h;
-                    if (!ok) break;
-                    tc_fence_after();
-                    const uint32_t there = c.present[(tile_no + j) & 31] >> (8 * h) & 0xffu;       // eight positions a bit
-                    if (there != 0xffu) {
+                    for (int w = 0; w < kKeys / 32; ++w) see[w] = pages_see(a, job, node, p0 + 32 * w);
+                }
+                ok = ok && warp_wait(smem_u32(&c.s_full[s]), s_phase, dead);
+                s_phase ^= 1;
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t present = c.present[(tile_no + j) & 31];        // eight positions a bit
+                if (present != (kKeys == 128 ? 0xffffu : 0xffu)) {
 #pragma unroll
-                        for (int w = 0; w < 2; ++w) {
-                            const uint32_t x = there >> (4 * w);
-                            const uint32_t bits = (x & 1u ? 0xffu : 0u) | (x & 2u ? 0xff00u : 0u) | (x & 4u ? 0xff0000u : 0u) | (x & 8u ? 0xff000000u : 0u);
-                            see[w] = (masked ? see[w] : 0xffffffffu) & bits;
-                        }
-                        masked = true;
+                    for (int w = 0; w < kKeys / 32; ++w) {
+                        const uint32_t x = present >> (4 * w);
+                        const uint32_t there = (x & 1u ? 0xffu : 0u) | (x & 2u ? 0xff00u : 0u) | (x & 4u ? 0xff0000u : 0u) | (x & 8u ? 0xff000000u : 0u);
+                        see[w] = (masked ? see[w] : 0xffffffffu) & there;
                     }
-                    const bool first = (both ? j : j >> 1) + h == 0;
-                    // The products of the step before are done when the scores issued behind them are, or, where no step follows, by a barrier of their own.
-                    auto products_done = [&] {
-                        return h == 0 || j + (both ? 1 : 2) < n ? warp_wait(smem_u32(&c.s_full[s][h ^ 1]), s_phase >> (h ^ 1) & 1u, dead)
-                                                                : warp_wait(smem_u32(&c.o_done[s]), done_phase, dead);
-                    };
-                    if (any) ok = softmax_step<HD, kTerms, kOwn>(s_tmem + kStep * h, o_tmem, a.scale, first, masked, see, ref, sum, own, products_done);
+                    masked = true;
+                }
+                if (masked) {
+                    const VPlace v(tile_no + j);
+                    ok = warp_wait(smem_u32(&c.v_full[v.slot]), v.phase, dead);
                     if (!ok) break;
-                    if (masked) {
-                        const uint32_t v = tile_no + j;
-                        ok = warp_wait(smem_u32(&c.v_full[v % kVSlots]), v / kVSlots & 1, dead);
-                        if (!ok) break;
-                        const int keys = job.base + job.n - p0;
-                        if (clean_values(v_ring + v % kVSlots * kTile + h * kStep * HD * 2, kStep * kPieces, row, 128, [&](int p) {
-                                const int key = p / kPieces / 8 * 8 + p % 8;
-                                return key < keys && (there >> (key >> 3) & 1u);
-                            })) {
-                            atomicMin(&c.bad_lo[i & 1], u);
-                            atomicMax(&c.bad_hi[i & 1], u);
-                            __threadfence_block();
-                        }
-                        fence_proxy_async_smem();
+                    const int keys = job.base + job.n - p0;
+                    if (clean_values(v_ring + v.slot * kTile, kTile / 16, row, 128, [&](int p) {
+                            const int key = p / kPieces / 8 * 8 + p % 8;
+                            return key < keys && (present >> (key >> 3) & 1u);
+                        })) {
+                        atomicMin(&c.bad_lo[i & 1], u);
+                        atomicMax(&c.bad_hi[i & 1], u);
+                        __threadfence_block();
                     }
+                    fence_proxy_async_smem();
+                }
+                auto given = [&](int h) {
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(smem_u32(&c.p_full[s][h]));
+                };
+                if (any) {
+                    softmax_tile<HD, kKeys, kTerms, kOwn>(s_tmem, o_tmem, a.scale, both ? j == 0 : j < 2, masked, see, ref, sum, own, given);
+                } else {
+#pragma unroll
+                    for (int h = 0; h < kHalves; ++h) given(h);
                 }
             }
             // ---- the range's sums
             const bool mine_has = both || s < n;
             if (ok && mine_has) ok = warp_wait(smem_u32(&c.o_full[s]), full_phase, dead);
-            if (mine_has) {
-                full_phase ^= 1;
-                done_phase ^= 1;
-            }
+            if (mine_has) full_phase ^= 1;
             tile_no += n;
             tc_fence_after();
             if constexpr (kOwn)

@@ -2,10 +2,10 @@
 //
 // Rows of a tile are (token, query head of the KV head's group) pairs, so that every tile reads one KV head's keys once for all of the group: T = 128 / G
 // tokens by G heads, rounded down (G = 3: 126 rows of 128).  A job is two such tiles, 2 T consecutive tokens of a prompt by one KV head, each with a
-// stream of its own (attend16_tile.cuh); both go through the same keys, from the first up to their last token, in steps of 64.
+// stream of its own (attend16_tile.cuh); both go through the same keys, 128 at a time, from the first up to their last token.
 // A CTA per SM takes jobs in turn: sorted by length (block of tokens, last first; then prompts, then heads), dealt out back and forth, so that the CTAs'
 // sums differ by less than a job.  Nothing is shared between CTAs: no atomics, no scratch.
-// Warps: 0-3 and 4-7 the streams' rows, 8 fetches (copy engine, 128-byte swizzle; 128 keys at a time), 9 and 11 issue the
+// Warps: 0-3 and 4-7 the streams' rows, 8 fetches (copy engine, 128-byte swizzle), 9 and 11 issue the
 // streams' products.
 #pragma once
 #include "attend16_tile.cuh"
@@ -27,7 +27,7 @@ struct PromptJob {
 constexpr int kPromptJobs = 2;
 
 struct PromptControl {
-    unsigned long long q_full, q_empty, full[16], empty[16], s_full[2][2], p_full[2][2], o_done[2], o_full[2], done[2];   // o_done: products of a job's last step but one; o_full: of all
+    unsigned long long q_full, q_empty, full[16], empty[16], s_full[2], p_full[2][2], o_full[2], done[2];
     PromptJob jobs[kPromptJobs];
     int flags[kPromptJobs];     // a value of the job's last tiles was not finite
     uint32_t tmem;
@@ -91,10 +91,10 @@ __device__ __forceinline__ PromptJob prompt_job(const PromptArgs& a, long long r
     }
     return job;
 }
-// Steps that stream s of a job goes through.
-__device__ __forceinline__ int prompt_steps(const PromptJob& job, int s, int T) {
+// Tiles of 128 keys that stream s of a job goes through.
+__device__ __forceinline__ int prompt_tiles(const PromptJob& job, int s, int T) {
     const int t = job.t0 + s * T;
-    return t >= job.n ? 0 : (min(t + T, job.n) + kStep - 1) / kStep;
+    return t >= job.n ? 0 : (min(t + T, job.n) + 127) >> 7;
 }
 
 // Which of 16 columns hold something that is not finite in n rows of v (0 in shared memory, where the job's last tiles had it).
@@ -110,7 +110,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
     prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ PromptArgs a) {
     using Shape = PromptShape<HD>;
     constexpr int kTile = Shape::kTile, kStages = Shape::kStages, kAtom = 128 * 128;      // an atom: 128 rows of 64 columns
-    constexpr uint32_t kIdescS = umma_idesc_bf16(128, kStep, 0, 0), kIdescO = umma_idesc_bf16(128, HD, 0, 1);
+    constexpr uint32_t kIdescS = umma_idesc_bf16(128, 128, 0, 0), kIdescO = umma_idesc_bf16(128, HD, 0, 1);
     extern __shared__ __align__(1024) unsigned char smem[];
     unsigned char* const ring = smem + 2 * kTile;
     PromptControl& c = *reinterpret_cast<PromptControl*>(ring + kStages * kTile);
@@ -126,11 +126,8 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
             mbar_init(smem_u32(&c.empty[i]), 2);
         }
         for (int s = 0; s < 2; ++s) {
-            for (int h = 0; h < 2; ++h) {
-                mbar_init(smem_u32(&c.s_full[s][h]), 1);
-                mbar_init(smem_u32(&c.p_full[s][h]), 4);
-            }
-            mbar_init(smem_u32(&c.o_done[s]), 1);
+            mbar_init(smem_u32(&c.s_full[s]), 1);
+            for (int h = 0; h < 2; ++h) mbar_init(smem_u32(&c.p_full[s][h]), 4);
             mbar_init(smem_u32(&c.o_full[s]), 1);
             mbar_init(smem_u32(&c.done[s]), 1);
         }
@@ -164,13 +161,13 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
                     if (job.n == 0) {
                         mbar_arrive(smem_u32(&c.q_full));
                     } else {
-                        const int steps[2] = {prompt_steps(job, 0, T), prompt_steps(job, 1, T)};
+                        const int tiles[2] = {prompt_tiles(job, 0, T), prompt_tiles(job, 1, T)};
                         const uint32_t bar = smem_u32(&c.q_full);
-                        mbar_expect_tx(bar, (uint32_t)((steps[1] ? 2 : 1) * (HD / 64) * T * G * 128));
+                        mbar_expect_tx(bar, (uint32_t)((tiles[1] ? 2 : 1) * (HD / 64) * T * G * 128));
                         for (int s = 0; s < 2; ++s)
-                            for (int x = 0; steps[s] && x < HD / 64; ++x)
+                            for (int x = 0; tiles[s] && x < HD / 64; ++x)
                                 tensor3_g2s(smem_u32(smem + s * kTile + x * kAtom), &map_q, 64 * x, job.head * G, job.first + job.t0 + s * T, bar);
-                        const int n = (max(steps[0], steps[1]) + 1) >> 1;                // tiles of 128 keys
+                        const int n = max(tiles[0], tiles[1]);
                         for (int e = 0; e < 2 * n && ok; ++e, ++entry) {
                             const int st = entry % kStages;
                             if (entry >= kStages) ok = role_wait(smem_u32(&c.empty[st]), (entry / kStages - 1) & 1, dead);
@@ -197,27 +194,29 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
                 bool ok = true;
                 const uint64_t q_desc = umma_desc_swizzled(smem_u32(smem + s * kTile), 16, 1024), k_desc = umma_desc_swizzled(smem_u32(ring), 16, 1024),
                                v_desc = umma_desc_swizzled(smem_u32(ring), kAtom, 1024);
-                uint32_t p_phase = 0;              // bit h
+                uint32_t p_phase = 0;              // of both halves
                 auto arrived = [&](const Place& at) { return ok = ok && role_wait(smem_u32(&c.full[at.slot]), at.phase, dead); };
                 auto release = [&](const Place& at) { umma_commit(smem_u32(&c.empty[at.slot])); };      // free when what was issued so far is done
-                auto scores = [&](const Place& k, int h) {
-                    const uint64_t half = k_desc + (k.slot * (kTile >> 4) + h * (kStep * 128 >> 4));
+                auto scores = [&](const Place& k) {
+                    const uint64_t tile = k_desc + k.slot * (kTile >> 4);
 #pragma unroll
                     for (int x = 0; x < HD / 16; ++x) {
                         const uint32_t at = ((x >> 2) * kAtom + (x & 3) * 32) >> 4;
-                        umma_bf16(tmem + 128 * s + kStep * h, q_desc + at, half + at, kIdescS, x > 0);
+                        umma_bf16(tmem + 128 * s, q_desc + at, tile + at, kIdescS, x > 0);
                     }
-                    umma_commit(smem_u32(&c.s_full[s][h]));
+                    umma_commit(smem_u32(&c.s_full[s]));
                 };
-                auto sums = [&](const Place& v, int h, bool first) {
-                    ok = ok && role_wait(smem_u32(&c.p_full[s][h]), p_phase >> h & 1u, dead);
-                    p_phase ^= 1u << h;
-                    if (!ok) return false;
-                    tc_fence_after();
-                    const uint64_t half = v_desc + (v.slot * (kTile >> 4) + h * (kStep * 128 >> 4));
+                auto sums = [&](const Place& v, bool first) {
+                    const uint64_t tile = v_desc + v.slot * (kTile >> 4);
+                    for (int h = 0; h < 2; ++h) {
+                        ok = ok && role_wait(smem_u32(&c.p_full[s][h]), p_phase, dead);
+                        if (!ok) return false;
+                        tc_fence_after();
 #pragma unroll
-                    for (int x = 0; x < kStep / 16; ++x)
-                        umma_bf16_ta(tmem + 256 + HD * s, tmem + 128 * s + kStep * h + 8 * x, half + x * (2048 >> 4), kIdescO, !first || x > 0);
+                        for (int x = 0; x < 4; ++x)
+                            umma_bf16_ta(tmem + 256 + HD * s, tmem + 128 * s + 32 * h + 8 * x, tile + (4 * h + x) * (2048 >> 4), kIdescO, !first || h + x > 0);
+                    }
+                    p_phase ^= 1;
                     return true;
                 };
                 for (int i = 0; ok; ++i) {
@@ -225,33 +224,29 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
                     if (!ok) break;
                     const PromptJob job = c.jobs[i % kPromptJobs];
                     if (job.n == 0) break;
-                    const int n = prompt_steps(job, s, T), tiles = (max(n, prompt_steps(job, 1 - s, T)) + 1) >> 1;
+                    const int n = prompt_tiles(job, s, T), tiles = max(n, prompt_tiles(job, 1 - s, T));
                     if (n > 0) {
                         const Place k(entry);
                         if (!arrived(k)) break;
                         tc_fence_after();
-                        scores(k, 0);
-                        if (n > 1) scores(k, 1);
+                        scores(k);
                         release(k);
-                        if (n <= 2) umma_commit(smem_u32(&c.q_empty));
+                        if (n == 1) umma_commit(smem_u32(&c.q_empty));
                     } else {
                         mbar_arrive(smem_u32(&c.q_empty));
                     }
                     for (int j = 0; j < n; ++j) {
-                        const Place v(entry + (j & ~1) + 1), k(entry + (j & ~1) + 2);      // of this step, and of the next but one
-                        const bool more = j + 2 < n;
-                        if (!(j & 1) && (!arrived(v) || (more && !arrived(k)))) break;
-                        if (!sums(v, j & 1, j == 0)) break;
-                        if (j + 2 == n) umma_commit(smem_u32(&c.o_done[s]));
-                        if (j + 1 == n) umma_commit(smem_u32(&c.o_full[s]));
-                        if (more) {
-                            scores(k, j & 1);
-                            if ((j & 1) || j + 3 == n) release(k);
-                            if (j + 3 == n) umma_commit(smem_u32(&c.q_empty));
-                        }
-                        if ((j & 1) || j + 1 == n) release(v);
+                        const Place v(entry + 2 * j + 1), k(entry + 2 * j + 2);
+                        const bool more = j + 1 < n;
+                        if (!arrived(v) || (more && !arrived(k))) break;
+                        if (!sums(v, j == 0)) break;
+                        if (more) scores(k);
+                        else umma_commit(smem_u32(&c.o_full[s]));
+                        release(v);
+                        if (more) release(k);
+                        if (j + 2 == n) umma_commit(smem_u32(&c.q_empty));
                     }
-                    for (int e = 2 * ((n + 1) >> 1); e < 2 * tiles && ok; ++e) {           // what the other stream alone goes through
+                    for (int e = 2 * n; e < 2 * tiles && ok; ++e) {            // what the other stream alone goes through
                         const Place at(entry + e);
                         if (arrived(at)) mbar_arrive(smem_u32(&c.empty[at.slot]));
                     }
@@ -268,63 +263,48 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
         registers_more();
         const int s = warp >> 2, row = tid & 127, token = row / G, g = row % G;
         const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16, s_tmem = tmem + 128 * s + lanes, o_tmem = tmem + 256 + HD * s + lanes;
-        uint32_t entry = 0, s_phase = 0, done_phase = 0, full_phase = 0;       // s_phase: bit h
+        uint32_t entry = 0, s_phase = 0, full_phase = 0;
         for (int i = 0;; ++i) {
             if (!warp_wait(smem_u32(&c.q_full), i & 1, dead)) break;
             const PromptJob job = c.jobs[i % kPromptJobs];
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&c.q_empty));
             if (job.n == 0) break;
-            const int steps = prompt_steps(job, s, T), all = (max(prompt_steps(job, 0, T), prompt_steps(job, 1, T)) + 1) >> 1;
+            const int tiles = prompt_tiles(job, s, T), all = max(prompt_tiles(job, 0, T), prompt_tiles(job, 1, T));
             const int t = job.t0 + s * T + token;  // this row's token
-            const int clear = (job.t0 + s * T + 1) / kStep;                    // steps that every row sees whole
+            const int clear = (job.t0 + s * T + 1) >> 7;                       // tiles that every row sees whole
             float ref = -INFINITY, sum = 0.f, none[1];
             bool ok = true;
-            int j = 0;
-            // The products of the step before are done when the scores issued behind them are, or, where no step follows, by a barrier of their own.
-            auto products_done = [&] {
-                const int h = (j + 1) & 1;
-                return j + 1 < steps ? warp_wait(smem_u32(&c.s_full[s][h]), s_phase >> h & 1u, dead) : warp_wait(smem_u32(&c.o_done[s]), done_phase, dead);
-            };
-            for (; j < steps; ++j) {
-                const int h = j & 1;
-                uint32_t see[2];
+            for (int j = 0; j < tiles; ++j) {
+                uint32_t see[4];
                 const bool masked = j >= clear;
                 if (masked) {
 #pragma unroll
-                    for (int w = 0; w < 2; ++w) {
-                        const int n = t + 1 - (j * kStep + 32 * w);
+                    for (int w = 0; w < 4; ++w) {
+                        const int n = t + 1 - (j * 128 + 32 * w);
                         see[w] = n >= 32 ? 0xffffffffu : (n <= 0 ? 0u : (1u << n) - 1u);
                     }
-                }
-                ok = warp_wait(smem_u32(&c.s_full[s][h]), s_phase >> h & 1u, dead);
-                s_phase ^= 1u << h;
-                if (!ok) break;
-                tc_fence_after();
-                ok = softmax_step<HD, 1, false>(s_tmem + kStep * h, o_tmem, a.scale, j == 0, masked, see, ref, sum, none, products_done);
-                if (!ok) break;
-                if (masked) {
-                    const uint32_t ev = entry + 2 * (j >> 1) + 1;
+                    const uint32_t ev = entry + 2 * j + 1;
                     ok = warp_wait(smem_u32(&c.full[ev % kStages]), (ev / kStages) & 1, dead);
                     if (!ok) break;
-                    // half of a tile of 128 keys: 64 rows of 128 bytes of each block of 64 columns
-                    unsigned char* const half = ring + ev % kStages * kTile + h * kStep * 128;
-                    bool bad = false;
-                    for (int x = 0; x < HD / 64; ++x)
-                        bad |= clean_values(half + x * kAtom, kStep * 8, row, 128, [&](int p) { return j * kStep + (p >> 3) < job.n; });
-                    if (bad) {
+                    if (clean_values(ring + ev % kStages * kTile, kTile / 16, row, 128, [&](int p) { return j * 128 + ((p >> 3) & 127) < job.n; })) {
                         *(volatile int*)&c.flags[i % kPromptJobs] = 1;
                         __threadfence_block();
                     }
                     fence_proxy_async_smem();
                 }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&c.p_full[s][h]));
+                ok = warp_wait(smem_u32(&c.s_full[s]), s_phase, dead);
+                s_phase ^= 1;
+                if (!ok) break;
+                tc_fence_after();
+                softmax_tile<HD, 128, 1, false>(s_tmem, o_tmem, a.scale, j == 0, masked, see, ref, sum, none, [&](int h) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&c.p_full[s][h]));
+                });
             }
             entry += 2 * all;
-            if (steps == 0) continue;
-            if (steps > 1) done_phase ^= 1;
+            if (tiles == 0) continue;
             const bool mine = token < T && t < job.n;
             uint16_t* const out = a.out + (long long)(job.first + t) * a.out_stride + (job.head * G + g) * HD;
             if (ok) ok = warp_wait(smem_u32(&c.o_full[s]), full_phase, dead);

@@ -1,15 +1,13 @@
-// What both bf16 attention kernels (prompts, pages) do with 128 query rows by 64 keys (a step) on the 5th-generation tensor cores.
+// What both bf16 attention kernels (prompts, pages) do with a tile of 128 query rows by kKeys keys on the 5th-generation tensor cores.
 //
-//   S[128 x 64] = Q K^T           both operands in shared memory, fp32 scores in tensor memory, a lane per query row
+//   S[128 x kKeys] = Q K^T        both operands in shared memory, fp32 scores in tensor memory, a lane per query row
 //   P = exp2(scale S - ref)       one thread per row: its scores in registers, no exchange between threads.  ref is the row's running
 //                                 maximum as of the last time it rose by more than 2^8 in weight: O and the sum are rescaled only then, so that
-//                                 P <= 2^8, and hardly ever behind a row's first step
+//                                 P <= 2^8, and hardly ever behind a row's first tile
 //   O[128 x HD] += P V            P as bf16 in tensor memory (over the scores it was made of), V in shared memory, fp32 sums in tensor memory
 //
-// Two such streams per CTA, each with four warps of its own and a thread that issues its products; in bf16 each has two places for scores, so that its warps take one step's
-// exponentials while the tensor cores do the products of the step before and the scores of the next but one.  (Steps of 128 keys, of which tensor memory
-// holds one a stream: the warps waited for 1250 of 3740 cycles a pair of steps, and both streams at the same time.  The same with two
-// threads a row, in sixteen warps: 3900.  One thread for both streams' products took 3900 cycles for what the tensor cores do in 2560.)
+// Two such streams per CTA, each with four warps of its own and a thread that issues its products: while one stream's exponentials are taken the tensor
+// cores do the other's products.  P goes over in halves, so that the first half's products run beside the second's exponentials.
 #pragma once
 #include "../tcgen05.cuh"
 
@@ -165,8 +163,6 @@ struct RingPlace {
 constexpr int kPoly = 1, kPolyOf = 4;              // of so many pairs of weights, those whose exponentials are polynomials
 constexpr float kRefExcess = 8.f;                  // log2 units by which a weight may exceed 1
 
-constexpr int kStep = 64;                          // keys
-
 // Adds a tile's sums to a row's.
 template <int HD>
 __device__ __forceinline__ void own_sums(uint32_t o_tmem, float (&own)[HD]) {
@@ -180,29 +176,30 @@ __device__ __forceinline__ void own_sums(uint32_t o_tmem, float (&own)[HD]) {
     }
 }
 
-// One row's step.  `first`: there are no sums yet.  masked: bit c of `see` says whether key c is seen; the others' scores are replaced, whatever they are.
-// products_done(): waits for the sums of the step before (false: given up, and so is this).
-// kOwn: the products of a step are sums of their own, which the thread adds to `own`: the tensor cores' additions truncate, which in bf16 does not
+// One row's share of a tile, whose scores have come (and the products of the tile before are done).  `first`: there are no sums yet.  masked: bit c of
+// `see` says whether key c is seen; the others' scores are replaced, whatever they are.  given(h): half h of the weights is where the products read it.
+// kOwn: the products of a tile are sums of their own, which the thread adds to `own`: the tensor cores' additions truncate, which in bf16 does not
 // count, but would cost fp32 two bits over a long row.
-template <int HD, int kTerms, bool kOwn, typename Done>
-__device__ __forceinline__ bool softmax_step(uint32_t s_tmem, uint32_t o_tmem, float scale, bool first, bool masked, const uint32_t (&see)[2], float& ref, float& sum,
-                                             float (&own)[kOwn ? HD : 1], Done products_done) {
-    uint32_t s[kStep];
+template <int HD, int kKeys, int kTerms, bool kOwn, typename Given>
+__device__ __forceinline__ void softmax_tile(uint32_t s_tmem, uint32_t o_tmem, float scale, bool first, bool masked, const uint32_t (&see)[kKeys / 32], float& ref,
+                                             float& sum, float (&own)[kOwn ? HD : 1], Given given) {
+    constexpr int kHalf = kTerms == 1 ? kKeys / 2 : kKeys;
+    uint32_t s[kKeys];
 #pragma unroll
-    for (int i = 0; i < kStep; i += 32) tmem_ld32(s_tmem + i, s + i);
+    for (int i = 0; i < kKeys; i += 32) tmem_ld32(s_tmem + i, s + i);
     if constexpr (kOwn)
         if (!first) own_sums<HD>(o_tmem, own);
 #pragma unroll
-    for (int i = 0; i < kStep; i += 32) tmem_ld_wait32(s + i);
+    for (int i = 0; i < kKeys; i += 32) tmem_ld_wait32(s + i);
     if (masked) {
 #pragma unroll
-        for (int i = 0; i < kStep; ++i)
+        for (int i = 0; i < kKeys; ++i)
             if (!(see[i / 32] >> (i % 32) & 1u)) s[i] = 0xff800000u;
     }
     float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-    for (int i = 0; i < kStep; i += 2) mx[(i >> 1) & 3] = max3(mx[(i >> 1) & 3], __uint_as_float(s[i]), __uint_as_float(s[i + 1]));
-    const float top = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * scale;
+    for (int i = 0; i < kKeys; i += 2) mx[(i >> 1) & 3] = max3(mx[(i >> 1) & 3], __uint_as_float(s[i]), __uint_as_float(s[i + 1]));
+    const float top = fmaxf(max3(mx[0], mx[1], mx[2]), mx[3]) * scale;
     const bool up = top > ref + kRefExcess || (ref == -INFINITY && top > ref);
     if (__any_sync(0xffffffffu, up)) {
         const float next = up ? top : ref, factor = up ? exp2_approx(ref - next) : 1.f;
@@ -212,8 +209,6 @@ __device__ __forceinline__ bool softmax_step(uint32_t s_tmem, uint32_t o_tmem, f
 #pragma unroll
             for (int i = 0; i < HD; ++i) own[i] *= factor;
         } else if (!first) {
-            if (!products_done()) return false;
-            tc_fence_after();
 #pragma unroll 1
             for (int c = 0; c < HD; c += 16) {
                 float o[16];
@@ -229,41 +224,45 @@ __device__ __forceinline__ bool softmax_step(uint32_t s_tmem, uint32_t o_tmem, f
     const uint64_t scale2 = pair_of(scale, scale), shift2 = pair_of(shift, shift);
     uint64_t part[2] = {0, 0};
 #pragma unroll
-    for (int i = 0; i < kStep; i += 2) {
-        uint64_t p = pair_fma(pair_of(s[i], s[i + 1]), scale2, shift2);
-        float x, y;
-        if (kTerms == 1 && (i / 2) % kPolyOf < kPoly) {
-            p = pair_exp2(p);
-            pair_split(p, x, y);
-        } else {
-            pair_split(p, x, y);
-            x = exp2_approx(x);
-            y = exp2_approx(y);
-            p = pair_of(x, y);
+    for (int h = 0; h < kKeys / kHalf; ++h) {
+        uint32_t* const x = s + h * kHalf;
+#pragma unroll
+        for (int i = 0; i < kHalf; i += 2) {
+            uint64_t p = pair_fma(pair_of(x[i], x[i + 1]), scale2, shift2);
+            float a, b;
+            if (kTerms == 1 && (i / 2) % kPolyOf < kPoly) {
+                p = pair_exp2(p);
+                pair_split(p, a, b);
+            } else {
+                pair_split(p, a, b);
+                a = exp2_approx(a);
+                b = exp2_approx(b);
+                p = pair_of(a, b);
+            }
+            part[(i >> 1) & 1] = pair_add(part[(i >> 1) & 1], p);
+            x[i] = __float_as_uint(a);
+            x[i + 1] = __float_as_uint(b);
         }
-        part[(i >> 1) & 1] = pair_add(part[(i >> 1) & 1], p);
-        s[i] = __float_as_uint(x);
-        s[i + 1] = __float_as_uint(y);
+#pragma unroll
+        for (int t = 0; t < kTerms; ++t) {
+            uint32_t p[kHalf / 2];
+#pragma unroll
+            for (int i = 0; i < kHalf / 2; ++i) {
+                const float a = __uint_as_float(x[2 * i]), b = __uint_as_float(x[2 * i + 1]);
+                p[i] = pack_bf16(a, b);
+                if (t + 1 < kTerms) {              // what the term leaves, exactly
+                    x[2 * i] = __float_as_uint(a - __uint_as_float(p[i] << 16));
+                    x[2 * i + 1] = __float_as_uint(b - __uint_as_float(p[i] & 0xffff0000u));
+                }
+            }
+            tmem_st32(s_tmem + t * (kKeys / 2) + h * (kHalf / 2), p);
+        }
+        tmem_st_wait();
+        given(h);
     }
     float even, odd;
     pair_split(pair_add(part[0], part[1]), even, odd);
     sum += even + odd;
-#pragma unroll
-    for (int t = 0; t < kTerms; ++t) {
-        uint32_t p[kStep / 2];
-#pragma unroll
-        for (int i = 0; i < kStep / 2; ++i) {
-            const float x = __uint_as_float(s[2 * i]), y = __uint_as_float(s[2 * i + 1]);
-            p[i] = pack_bf16(x, y);
-            if (t + 1 < kTerms) {                  // what the term leaves, exactly
-                s[2 * i] = __float_as_uint(x - __uint_as_float(p[i] << 16));
-                s[2 * i + 1] = __float_as_uint(y - __uint_as_float(p[i] & 0xffff0000u));
-            }
-        }
-        tmem_st32(s_tmem + t * (kStep / 2), p);
-    }
-    tmem_st_wait();
-    return true;
 }
 
 // Values of a tile that no row may take into its products: pieces that are no key's, and what is not finite.  A weight of 0 does not keep them out, so
