@@ -4,17 +4,19 @@
 // row, cut into equal ranges, one per CTA (one CTA per SM).  A triple that one CTA has whole is finished there; of others each CTA leaves its sums, which
 // pages_merge_kernel adds up in CTA order.  No atomics, no state between calls.
 // A row group has up to 256 rows in bf16.  More than 128: the CTA's two streams (attend16_tile.cuh) have 128 rows each and go through the same
-// tiles; fewer: both have the same rows and take the tiles in turn, and their sums are joined at the end -- in tensor memory, where each stream
-// reads the other's, half of the columns each.  fp32: q and weights as three bf16 terms, groups of 128 rows and tiles of 64 keys, since the
-// terms of q fill shared memory and those of the weights tensor memory.
-// Blocks of pages are operands of the products as they are (kv16.cuh): a bulk copy per page and tile, by the lanes of one warp.
+// tiles; fewer: both have the same rows and take the tiles in turn, and their sums are joined at the end -- by the merge, or, where the CTA has all of
+// the triple, in tensor memory, where each stream reads the other's, half of the columns each.  fp32: q and weights as three bf16 terms, groups of 128
+// rows and tiles of 64 keys, since the terms of q fill shared memory and those of the weights tensor memory.
+// Blocks of pages are operands of the products as they are (kv16.cuh): a bulk copy per page and tile, by the lanes of a warp for keys and one for values.
 #pragma once
 #include "attend16_tile.cuh"
 #include "kv16.cuh"
 
 namespace pipesd {
 
-constexpr int kPagesSms = 148, kPagesMinTiles = 1;
+constexpr int kPagesSms = 148;
+// What a triple counts in the ranges: a lead, and every tile; a tile whose rows fill both streams counts more.
+constexpr int kPagesLead = 6, kPagesTile = 3, kPagesWideTile = 4;
 
 template <int HD, typename T>
 struct PagesShape {
@@ -34,13 +36,19 @@ struct PagesArgs {
     float scale;                // times log2(e)
     const uint32_t* mask;       // [rows][words], null: a row sees the new rows up to itself
     int words;
-    float* parts;               // [2 * CTAs] of {sums [HD / 4][cap][4], references [cap], denominators [cap]}
-    int ctas, cap, keys, rows;  // cap: query rows that a slot has room for; keys, rows: of a tile and a row group
+    struct PagesSplit* splits;  // [CTAs]
+    float* parts;               // [4 * CTAs] of {sums [HD / 4][cap][4], references [cap], denominators [cap]}: of a CTA's first range and of a later one, by stream
+    int ctas, cap, keys, rows;  // cap: query rows that a share has room for; keys, rows: of a tile and a row group
+};
+// The triple that goes on behind a CTA's range, as the merge needs it (rows 0: none).
+struct PagesSplit {
+    int first, head, rho0, rows, last, share, both, pad;     // last: its last CTA; share: where this CTA's sums are
 };
 struct PagesJob {
     int req, n, first, base, head, rho0, n_rows, tiles;      // tiles: 0 = no more jobs
-    int u0, u1, units;          // the range's tiles (u1 <= units; tiles of them are seen by some row), of all the triple's
-    int slot;
+    int whole, share;           // whole: all of the triple's; share: where its sums go else
+    int u0;                     // the first of its tiles
+    int pad;
 };
 struct PagesControl {
     unsigned long long job_full, job_read, q_full, q_empty, k_full[8], k_empty[8], v_full[8], v_empty[8], s_full[2], p_full[2][2], o_full[2], joint, done[2];
@@ -54,14 +62,29 @@ struct PagesControl {
 template <int HD, typename T>
 constexpr int pages_smem() { return PagesShape<HD, T>::kQ + PagesShape<HD, T>::kSlots * PagesShape<HD, T>::kTile + (int)sizeof(PagesControl); }
 
-// What a request adds to the sequence of tiles: tiles per triple and row groups.
-__device__ __forceinline__ void pages_load(const PagesArgs& a, int r, int& n, int& first, int& base, int& units, int& groups) {
-    n = first = base = units = groups = 0;
-    if (r >= a.w.n_req) return;
-    n = kv4_rows(a.w, r, first, base);
-    if (n <= 0) { n = 0; return; }
-    units = (base + n + a.keys - 1) / a.keys;
-    groups = (n * (a.Hq / a.w.Hkv) + a.rows - 1) / a.rows;
+// What a request adds to the sequence: tiles per triple, row groups, and what a triple counts.
+struct PagesRequest {
+    int n, first, base, units, groups;
+    long long last;             // of the last row group, which may be narrower
+    int per;                    // of the others
+};
+__device__ __forceinline__ int pages_weight(int rows) { return rows > 128 ? kPagesWideTile : kPagesTile; }
+__device__ __forceinline__ long long pages_count(int units, int rows) { return kPagesLead + (long long)units * pages_weight(rows); }
+__device__ __forceinline__ PagesRequest pages_load(const PagesArgs& a, int r) {
+    PagesRequest q = {0, 0, 0, 0, 0, 0, 0};
+    if (r >= a.w.n_req) return q;
+    q.n = kv4_rows(a.w, r, q.first, q.base);
+    if (q.n <= 0) { q.n = 0; return q; }
+    const int rows = q.n * (a.Hq / a.w.Hkv);
+    q.units = (q.base + q.n + a.keys - 1) / a.keys;
+    q.groups = (rows + a.rows - 1) / a.rows;
+    return q;
+}
+__device__ __forceinline__ int pages_group_rows(const PagesArgs& a, const PagesRequest& q, int group) { return min(a.rows, q.n * (a.Hq / a.w.Hkv) - group * a.rows); }
+// All heads' triples of a request: group by group within a head.
+__device__ __forceinline__ long long pages_head(const PagesArgs& a, const PagesRequest& q) {
+    if (q.groups == 0) return 0;
+    return (q.groups - 1) * pages_count(q.units, a.rows) + pages_count(q.units, pages_group_rows(a, q, q.groups - 1));
 }
 __device__ __forceinline__ long long pages_scan(long long v) {
     const int lane = threadIdx.x & 31;
@@ -72,31 +95,21 @@ __device__ __forceinline__ long long pages_scan(long long v) {
     }
     return v;
 }
-// Tiles of all requests, and of those before request `upto` (whole warp).
-__device__ __forceinline__ long long pages_total(const PagesArgs& a, int upto, long long& before) {
-    const int lane = threadIdx.x & 31;
+// The count of all requests (whole warp).
+__device__ __forceinline__ long long pages_total(const PagesArgs& a) {
     long long all = 0;
-    before = 0;
-    for (int r0 = 0; r0 < a.w.n_req; r0 += 32) {
-        int n, first, base, units, groups;
-        pages_load(a, r0 + lane, n, first, base, units, groups);
-        const long long mine = (long long)units * groups * a.w.Hkv, inc = pages_scan(mine);
-        if (upto >= r0 && upto < r0 + 32) before = all + __shfl_sync(0xffffffffu, inc - mine, upto - r0);
-        all += __shfl_sync(0xffffffffu, inc, 31);
-    }
-    return all;
+    for (int r = threadIdx.x & 31; r < a.w.n_req; r += 32) all += pages_head(a, pages_load(a, r)) * a.w.Hkv;
+    return __shfl_sync(0xffffffffu, pages_scan(all), 31);
 }
 __device__ __forceinline__ long long pages_share(const PagesArgs& a, long long all) {
     const long long per = (all + a.ctas - 1) / a.ctas;
-    return per < kPagesMinTiles ? kPagesMinTiles : per;
+    return max(per, (long long)(kPagesLead + kPagesWideTile));
 }
-// Request that tile `at` of the sequence belongs to, and how far into it (whole warp; at < the total).
+// Request that `at` of the sequence belongs to, and how far into it (whole warp; at < the total).
 __device__ __forceinline__ int pages_find(const PagesArgs& a, long long at, long long& off) {
     const int lane = threadIdx.x & 31;
     for (int r0 = 0; r0 < a.w.n_req; r0 += 32) {
-        int n, first, base, units, groups;
-        pages_load(a, r0 + lane, n, first, base, units, groups);
-        const long long mine = (long long)units * groups * a.w.Hkv, inc = pages_scan(mine);
+        const long long mine = pages_head(a, pages_load(a, r0 + lane)) * a.w.Hkv, inc = pages_scan(mine);
         const unsigned hit = __ballot_sync(0xffffffffu, at < inc);
         if (hit) {
             const int l = __ffs(hit) - 1;
@@ -108,6 +121,58 @@ __device__ __forceinline__ int pages_find(const PagesArgs& a, long long at, long
     off = 0;
     return a.w.n_req;
 }
+// A CTA's way through its range (whole warp).
+struct PagesWalk {
+    long long f, f0, f_end, share, off;
+    int req;
+    PagesSplit split;
+
+    __device__ __forceinline__ void begin(const PagesArgs& a) {
+        const long long all = pages_total(a);
+        share = pages_share(a, all);
+        f = f0 = (long long)blockIdx.x * share;
+        f_end = min(f + share, all);
+        off = 0;
+        req = f < f_end ? pages_find(a, f, off) : a.w.n_req;
+        split = {};
+    }
+    // The next triple of which the range has tiles; tiles 0: there is none.
+    __device__ __forceinline__ PagesJob next(const PagesArgs& a) {
+        PagesJob job = {};
+        const int G = a.Hq / a.w.Hkv;
+        while (f < f_end && req < a.w.n_req) {
+            const PagesRequest q = pages_load(a, req);
+            const long long head = pages_head(a, q);
+            if (off >= head * a.w.Hkv) { ++req; off = 0; continue; }           // (requests without rows have nothing)
+            const long long full = pages_count(q.units, a.rows), in_head = off % head;
+            job.head = (int)(off / head);
+            const int group = (int)min(in_head / full, (long long)q.groups - 1);
+            job.n_rows = pages_group_rows(a, q, group);
+            const int weight = pages_weight(job.n_rows);
+            const long long start = f - (in_head - group * full), count = pages_count(q.units, job.n_rows);      // of the triple
+            // tile t of it is the range's that start + lead + t * weight lies in
+            auto tiles_before = [&](long long at) { return (int)min((long long)q.units, max(0ll, (at - start - kPagesLead + weight - 1) / weight)); };
+            const int u0 = f > start ? tiles_before(f) : 0, u1 = tiles_before(f_end);
+            const long long step = min(start + count, f_end) - f;
+            off += step;
+            f += step;
+            if (u0 >= u1) continue;
+            job.req = req; job.n = q.n; job.first = q.first; job.base = q.base;
+            job.rho0 = group * a.rows;
+            job.u0 = u0;
+            job.whole = u0 == 0 && u1 == q.units;
+            job.share = 4 * blockIdx.x + (start > f0 ? 2 : 0);
+            // without a mask no row of the group sees what lies behind its last one
+            const int seen = a.mask ? q.units : min(q.units, (q.base + (job.rho0 + job.n_rows - 1) / G) / a.keys + 1);
+            job.tiles = max(1, min(u1, seen) - u0);                            // (a tile at least: the others' sums are none)
+            if (u0 == 0 && !job.whole)
+                split = {q.first, job.head, job.rho0, job.n_rows, (int)((start + kPagesLead + (long long)(q.units - 1) * weight) / share), job.share, job.n_rows > 128, 0};
+            return job;
+        }
+        job.tiles = 0;
+        return job;
+    }
+};
 
 // Which of the 32 positions from `start` on row i of a request sees (bit 0: the first).
 __device__ __forceinline__ uint32_t pages_see(const PagesArgs& a, const PagesJob& job, int i, int start) {
@@ -253,6 +318,12 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
     volatile int* const dead = &c.dead;
     pdl_launch_dependents();
 
+    PagesWalk walk;
+    PagesJob ahead;
+    if (warp == 8) {                               // (while the others set up)
+        walk.begin(a);
+        ahead = walk.next(a);
+    }
     if (tid == 0) {
         mbar_init(smem_u32(&c.job_full), 1);
         mbar_init(smem_u32(&c.job_read), 11);   // all other roles' warps
@@ -285,35 +356,11 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
     if (warp >= 8) {
         registers_fewer();
         if (warp == 8) {                               // ---- what there is to do, and keys
-            long long before;
-            const long long all = pages_total(a, -1, before), share = pages_share(a, all);
-            long long f = (long long)blockIdx.x * share, off = 0;
-            const long long f_cta = f, f_end = min(f + share, all);
-            int req = f < f_end ? pages_find(a, f, off) : a.w.n_req;
             PagesFetch<HD, kKeys, kKSlots> fetch;
             uint32_t tile_no = 0;
             bool ok = true;
             for (int i = 0; ok; ++i) {
-                PagesJob job = {};
-                while (f < f_end && req < a.w.n_req) {
-                    int n, first, base, units, groups;
-                    pages_load(a, req, n, first, base, units, groups);
-                    if (off >= (long long)units * groups * a.w.Hkv) { ++req; off = 0; continue; }      // (requests without rows have no tiles)
-                    const int triple = (int)(off / units);
-                    job.req = req; job.n = n; job.first = first; job.base = base; job.units = units;
-                    job.head = triple / groups;
-                    job.rho0 = triple % groups * Shape::kRows;
-                    job.n_rows = min(Shape::kRows, n * G - job.rho0);
-                    job.u0 = (int)(off % units);
-                    job.u1 = (int)min((long long)units, job.u0 + (f_end - f));
-                    job.slot = 2 * blockIdx.x + (f - job.u0 > f_cta ? 1 : 0);
-                    // without a mask no row of the group sees what lies behind its last one
-                    const int seen = a.mask ? units : min(units, (base + (job.rho0 + job.n_rows - 1) / G) / kKeys + 1);
-                    job.tiles = max(1, min(job.u1, seen) - job.u0);                // (a tile at least: the others' sums are none)
-                    f += job.u1 - job.u0;
-                    off += job.u1 - job.u0;
-                    break;
-                }
+                const PagesJob job = ahead;
                 if (i > 0) ok = warp_wait(smem_u32(&c.job_read), (i - 1) & 1, dead);
                 if (!ok) break;
                 if (lane == 0) {
@@ -327,8 +374,10 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                     if (lane == 0) c.present[(tile_no + j) & 31] = present;
                 });
                 tile_no += job.tiles;
+                ahead = walk.next(a);
             }
             if (!ok) fetch.drain(c.k_full);
+            if (lane == 0) a.splits[blockIdx.x] = walk.split;
         } else if (warp == 10) {                       // ---- values
             PagesFetch<HD, kKeys, kVSlots> fetch;
             bool ok = true;
@@ -521,6 +570,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(smem_u32(&c.p_full[s][h]));
+                    __syncwarp();
                 };
                 if (any) {
                     softmax_tile<HD, kKeys, kTerms, kOwn>(s_tmem, o_tmem, a.scale, both ? j == 0 : j < 2, masked, see, ref, sum, own, given);
@@ -535,16 +585,16 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
             if (mine_has) full_phase ^= 1;
             tile_no += n;
             tc_fence_after();
+            const bool whole = job.whole, join = whole && !both;               // join: both streams' sums are the triple's
             if constexpr (kOwn)
-                if (ok && any && mine_has) {       // (the other stream reads them too)
+                if (ok && any && mine_has) {
                     own_sums<HD>(o_tmem, own);
 #pragma unroll
                     for (int d = 0; d < HD; d += 16) tmem_st16(o_tmem + d, *reinterpret_cast<const float(*)[16]>(own + d));
                     tmem_st_wait();
-                    tc_fence_before();
                 }
             if (sum != sum) ref = INFINITY;        // (not what a row that sees nothing has: every factor of it is then a NaN)
-            if (ok && !both) {
+            if (ok && join) {
                 c.ref[s][row] = ref;
                 c.sum[s][row] = sum;
                 tc_fence_before();
@@ -552,17 +602,17 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                 tc_fence_after();
             }
             T* const out = static_cast<T*>(a.out) + (job.first + node) * a.out_stride + (size_t)(job.head * G + rho % G) * HD;
-            const bool whole = job.u0 == 0 && job.u1 == job.units;
-            float* const part = a.parts + (size_t)job.slot * a.cap * (HD + 2);
+            float* const part = a.parts + (size_t)(job.share + s) * a.cap * (HD + 2);
+            const int slot = both ? row : local;   // (a stream's rows: of 128)
             if (!ok) {                             // a copy or a product that never came: no result
                 if (mine && whole)
                     for (int d = 0; d < HD; ++d) pages_store(out + d, NAN);
-                if (mine && !whole) part[a.cap * HD + local] = NAN;
+                if (mine && !whole) part[a.cap * HD + slot] = NAN;
                 break;
             }
             float f0 = 1.f, f1 = 1.f;              // what stream 0's and stream 1's sums are multiplied with
             bool none0 = ref == -INFINITY, none1 = true;                       // a stream that has seen nothing has none
-            if (!both) {
+            if (join) {
                 const float r0 = c.ref[0][row], r1 = c.ref[1][row];
                 none0 = r0 == -INFINITY;
                 none1 = r1 == -INFINITY;
@@ -572,47 +622,50 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                 sum = c.sum[0][row] * f0 + c.sum[1][row] * f1;
             }
             const int lo = *(volatile int*)&c.bad_lo[i & 1], hi = *(volatile int*)&c.bad_hi[i & 1];
-            const float inv = !whole ? 1.f : (sum > 0.f ? 1.f / sum : sum);
-            const int d0 = both ? 0 : s * (HD / 2), d1 = both ? HD : d0 + HD / 2;
-            const uint32_t o0 = tmem + 256 + HD * (both ? s : 0) + lanes;
-#pragma unroll 1
-            for (int d = d0; d < d1 && any; d += 16) {
-                float y[16], o[16];
-                tmem_ld16(o0 + d, y);
-                tmem_ld_wait16(y);
-#pragma unroll
-                for (int x = 0; x < 16; ++x) y[x] = none0 ? 0.f : y[x] * f0;
-                if (!both && n > 1) {
-                    tmem_ld16(o0 + HD + d, o);
-                    tmem_ld_wait16(o);
-#pragma unroll
-                    for (int x = 0; x < 16; ++x) y[x] = none1 ? y[x] : fmaf(o[x], f1, y[x]);
-                }
-                if (mine) {
-                    if (lo <= hi) {
-                        const uint32_t bad = pages_bad<HD, kKeys>(a, job, node, lo, hi, d);
-#pragma unroll
-                        for (int x = 0; x < 16; ++x)
-                            if (bad >> x & 1u) y[x] = NAN;
-                    }
-                    if (whole) {
-#pragma unroll
-                        for (int x = 0; x < 16; ++x) y[x] *= inv;
-                        pages_store16(out + d, a.out_wide, y);
-                    } else {
-#pragma unroll
-                        for (int x = 0; x < 16; x += 4)
-                            *reinterpret_cast<float4*>(part + ((size_t)(d + x) * a.cap + 4 * local)) = make_float4(y[x], y[x + 1], y[x + 2], y[x + 3]);
-                    }
-                }
-                __syncwarp();
+            if (whole) {
+                const float inv = sum > 0.f ? 1.f / sum : sum;
+                f0 *= inv;
+                f1 *= inv;
             }
-            if (mine && !whole && (both || s == 0)) {
-                part[a.cap * HD + local] = ref;
-                part[a.cap * (HD + 1) + local] = sum;
+            const int d0 = join ? s * (HD / 2) : 0, d1 = join ? d0 + HD / 2 : HD;
+            const uint32_t from = tmem + 256 + HD * (join ? 0 : s) + lanes;
+            if (any)
+#pragma unroll 1
+                for (int d = d0; d < d1; d += 16) {
+                    float y[16], o[16];
+                    tmem_ld16(from + d, y);
+                    tmem_ld_wait16(y);
+#pragma unroll
+                    for (int x = 0; x < 16; ++x) y[x] = none0 ? 0.f : y[x] * f0;
+                    if (join && n > 1) {
+                        tmem_ld16(from + HD + d, o);
+                        tmem_ld_wait16(o);
+#pragma unroll
+                        for (int x = 0; x < 16; ++x) y[x] = none1 ? y[x] : fmaf(o[x], f1, y[x]);
+                    }
+                    if (mine) {
+                        if (lo <= hi) {
+                            const uint32_t bad = pages_bad<HD, kKeys>(a, job, node, lo, hi, d);
+#pragma unroll
+                            for (int x = 0; x < 16; ++x)
+                                if (bad >> x & 1u) y[x] = NAN;
+                        }
+                        if (whole) {
+                            pages_store16(out + d, a.out_wide, y);
+                        } else {
+#pragma unroll
+                            for (int x = 0; x < 16; x += 4)
+                                *reinterpret_cast<float4*>(part + ((size_t)(d + x) * a.cap + 4 * slot)) = make_float4(y[x], y[x + 1], y[x + 2], y[x + 3]);
+                        }
+                    }
+                    __syncwarp();
+                }
+            if (mine && !whole) {
+                part[a.cap * HD + slot] = ref;
+                part[a.cap * (HD + 1) + slot] = sum;
             }
             tc_fence_before();
-            if (!both && !joint()) break;          // both streams' sums have been read
+            if (join && !joint()) break;           // both streams' sums have been read
         }
     }
     __syncthreads();
@@ -622,79 +675,78 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
     }
 }
 
-// Adds up the shares of triples that several CTAs had, a CTA per (row, query head): warp w the shares w, w + 4, ..., then the warps' sums in order.
-constexpr int kPagesMergeWarps = 4;
+// Adds up the shares of triples that several CTAs had.  A CTA per (CTA whose range ends within a triple, 32 columns), rows by 32: a warp per eighth of the
+// shares, a lane per row, whose shares lie side by side; the warps' sums are added in order.  grid: CTAs, HD / 32, 2.
+constexpr int kPagesMergeWarps = 8;
 template <int HD, typename T>
-__global__ void __launch_bounds__(32 * kPagesMergeWarps) pages_merge_kernel(const PagesArgs a) {
-    constexpr int kE = HD / 32;                    // neighbouring columns of a lane
-    __shared__ float s_v[kPagesMergeWarps][HD], s_sum[kPagesMergeWarps];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, G = a.Hq / a.w.Hkv;
-    const int row = blockIdx.x / a.Hq, qh = blockIdx.x % a.Hq;
-    int req = -1;
-    for (int r0 = 0; r0 < a.w.n_req && req < 0; r0 += 32) {
-        const int r = min(r0 + lane, a.w.n_req - 1);
-        const unsigned hit = __ballot_sync(0xffffffffu, a.w.row0[r] <= row && row < a.w.row0[r + 1]);
-        if (hit) req = min(r0 + __ffs(hit) - 1, a.w.n_req - 1);
-    }
-    int n, first, base, units, groups;
-    pages_load(a, req < 0 ? a.w.n_req : req, n, first, base, units, groups);
-    long long before;
-    const long long all = pages_total(a, req, before), share = pages_share(a, all);
+__global__ void __launch_bounds__(32 * kPagesMergeWarps) pages_merge_kernel(const __grid_constant__ PagesArgs a) {
+    __shared__ float s_top[kPagesMergeWarps][32], s_sum[kPagesMergeWarps][32];
+    __shared__ float s_v[kPagesMergeWarps][32][33];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, G = a.Hq / a.w.Hkv;
     // Launched with programmatic serialisation: behind this the shares are complete.  Every thread waits, those without work too.
     pdl_wait();
-    if (req < 0) return;
-    T* const out = static_cast<T*>(a.out) + row * a.out_stride + (size_t)qh * HD + lane * kE;
-    if (row - first >= n) {                        // a row without a position: nothing to see
-        if (warp == 0)
-#pragma unroll
-            for (int i = 0; i < kE; ++i) pages_store(out + i, 0.f);
-        return;
-    }
-    const int rho = (row - first) * G + qh % G;
-    const long long start = before + (long long)(qh / G * groups + rho / a.rows) * units;
-    const int c0 = (int)(start / share), c1 = (int)((start + units - 1) / share);
-    if (c0 == c1) return;
-    const int local = rho % a.rows;
-    auto slot = [&](int c) { return a.parts + (size_t)(2 * c + (start > (long long)c * share ? 1 : 0)) * a.cap * (HD + 2); };
-    float top = -INFINITY;
-    for (int c = c0 + lane; c <= c1; c += 32) {
-        const float r = slot(c)[a.cap * HD + local];
-        top = r == r ? fmaxf(top, r) : INFINITY;
-    }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-    float v[kE] = {}, sum = 0.f;
-#pragma unroll 4
-    for (int c = c0 + warp; c <= c1; c += kPagesMergeWarps) {
-        const float* p = slot(c);
-        const float r = p[a.cap * HD + local], factor = r == -INFINITY ? 0.f : exp2_approx(r - top);      // (NaN where a share is missing)
-        float x[kE];
-#pragma unroll
-        for (int i = 0; i < kE; ++i) {
-            const int d = lane * kE + i;
-            x[i] = p[(size_t)(d & ~3) * a.cap + 4 * local + (d & 3)];
+    // rows of requests that have no position: nothing to see
+    if (blockIdx.y == 0 && blockIdx.z == 0)
+        for (int r = blockIdx.x * blockDim.x + tid; r < a.w.n_req; r += gridDim.x * blockDim.x) {
+            int first, base;
+            const int n = kv4_rows(a.w, r, first, base), end = min(a.w.row0[r + 1], a.w.rows);
+            for (int row = max(first, 0) + n; row < end; ++row)
+                for (int d = 0; d < a.Hq * HD; ++d) pages_store(static_cast<T*>(a.out) + row * a.out_stride + d, 0.f);
         }
-        const float part = p[a.cap * (HD + 1) + local];
-        if (r != -INFINITY) {
+    const PagesSplit split = a.splits[blockIdx.x];
+    const int c0 = blockIdx.x, streams = 2, shares = (split.last - c0 + 1) * (split.both ? 1 : streams), d0 = blockIdx.y * 32;
+    for (int r0 = blockIdx.z * 32; r0 < split.rows; r0 += 32 * gridDim.z) {
+        const int local = r0 + lane;
+        const bool mine = local < split.rows;
+        // A row's shares: of every CTA, and, unless each has rows of its own, of both streams.
+        const int slot = mine ? (split.both ? local & 127 : local) : 0;
+        auto share = [&](int i) {
+            const int c = split.both ? i : i >> 1, s = split.both ? local >> 7 : i & 1;
+            return a.parts + (size_t)((c == 0 ? split.share : 4 * (c0 + c)) + s) * a.cap * (HD + 2);
+        };
+        float top = -INFINITY;
+        for (int i = warp; i < shares; i += kPagesMergeWarps) {
+            const float r = share(i)[a.cap * HD + slot];
+            top = r == r ? fmaxf(top, r) : INFINITY;                           // (a NaN where a share never came)
+        }
+        s_top[warp][lane] = top;
+        __syncthreads();
 #pragma unroll
-            for (int i = 0; i < kE; ++i) v[i] = fmaf(factor, x[i], v[i]);
+        for (int w = 0; w < kPagesMergeWarps; ++w) top = fmaxf(top, s_top[w][lane]);
+        float v[32] = {}, sum = 0.f;
+        for (int i = warp; i < shares; i += kPagesMergeWarps) {
+            const float* const p = share(i);
+            const float r = p[a.cap * HD + slot], part = p[a.cap * (HD + 1) + slot];
+            if (r == -INFINITY) continue;          // a share that has seen nothing
+            const float factor = exp2_approx(r - top);
             sum = fmaf(factor, part, sum);
+#pragma unroll
+            for (int x = 0; x < 32; x += 4) {
+                const float4 y = *reinterpret_cast<const float4*>(p + (size_t)(d0 + x) * a.cap + 4 * slot);
+                v[x] = fmaf(factor, y.x, v[x]);
+                v[x + 1] = fmaf(factor, y.y, v[x + 1]);
+                v[x + 2] = fmaf(factor, y.z, v[x + 2]);
+                v[x + 3] = fmaf(factor, y.w, v[x + 3]);
+            }
         }
+        s_sum[warp][lane] = sum;
+#pragma unroll
+        for (int x = 0; x < 32; ++x) s_v[warp][lane][x] = v[x];
+        __syncthreads();
+        // four rows a warp, a lane per column
+        for (int r = warp; r < 32 && r0 + r < split.rows; r += kPagesMergeWarps) {
+            float y = 0.f, total = 0.f;
+#pragma unroll
+            for (int w = 0; w < kPagesMergeWarps; ++w) {
+                y += s_v[w][r][lane];
+                total += s_sum[w][r];
+            }
+            const int rho = split.rho0 + r0 + r;
+            const float inv = total > 0.f ? 1.f / total : total;
+            pages_store(static_cast<T*>(a.out) + (split.first + rho / G) * a.out_stride + (size_t)(split.head * G + rho % G) * HD + d0 + lane, y * inv);
+        }
+        __syncthreads();
     }
-#pragma unroll
-    for (int i = 0; i < kE; ++i) s_v[warp][lane * kE + i] = v[i];
-    if (lane == 0) s_sum[warp] = sum;
-    __syncthreads();
-    if (warp) return;
-#pragma unroll
-    for (int w = 1; w < kPagesMergeWarps; ++w) {
-        sum += s_sum[w];
-#pragma unroll
-        for (int i = 0; i < kE; ++i) v[i] += s_v[w][lane * kE + i];
-    }
-    const float inv = sum > 0.f ? 1.f / sum : sum;
-#pragma unroll
-    for (int i = 0; i < kE; ++i) pages_store(out + i, v[i] * inv);
 }
 
 }  // namespace pipesd

@@ -301,6 +301,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(smem_u32(&c.p_full[s][h]));
+                    __syncwarp();
                 });
             }
             entry += 2 * all;

@@ -87,39 +87,10 @@ __device__ __forceinline__ uint64_t pair_add(uint64_t a, uint64_t b) {
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
-__device__ __forceinline__ uint64_t pair_mul(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
 __device__ __forceinline__ float max3(float a, float b, float c) {
     float r;
     asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
     return r;
-}
-__device__ __forceinline__ float max_nan(float a, float b) {
-    float r;
-    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
-    return r;
-}
-// 2^x of two values up to 127 on the multiply-add pipe, for a part of the weights, since the special-function unit alone would take as long as the
-// products: x = n + f, |f| <= 1/2, 2^f by the polynomial of degree 4 with the smallest relative error there (Remez exchange: 2.6e-6, against
-// 2^-9 of a rounding to bf16), times 2^n put together from its bits.  0 below 2^-127; a NaN stays one.
-__device__ __forceinline__ uint64_t pair_exp2(uint64_t x) {
-    float a, b;
-    pair_split(x, a, b);
-    x = pair_of(max_nan(a, -127.f), max_nan(b, -127.f));
-    const uint64_t big = pair_of(12583039.f, 12583039.f);                      // 1.5 * 2^23 + 127: the sum's low bits are n + 127
-    const uint64_t t = pair_add(x, big);
-    const uint64_t f = pair_fma(pair_add(t, pair_of(-12583039.f, -12583039.f)), pair_of(-1.f, -1.f), x);
-    uint64_t y = pair_of(0.009570102207362652f, 0.009570102207362652f);
-    y = pair_fma(y, f, pair_of(0.05591785907745361f, 0.05591785907745361f));
-    y = pair_fma(y, f, pair_of(0.240247443318367f, 0.240247443318367f));
-    y = pair_fma(y, f, pair_of(0.6931217908859253f, 0.6931217908859253f));
-    y = pair_fma(y, f, pair_of(0.9999992847442627f, 0.9999992847442627f));
-    float n0, n1;
-    pair_split(t, n0, n1);
-    return pair_mul(y, pair_of(__float_as_uint(n0) << 23, __float_as_uint(n1) << 23));
 }
 
 // ---- waits: bounded, and given up at once when another role of the CTA has given up
@@ -160,7 +131,6 @@ struct RingPlace {
     __device__ __forceinline__ explicit RingPlace(uint32_t at) : slot(at % n), phase(at / n & 1u) {}
 };
 
-constexpr int kPoly = 1, kPolyOf = 4;              // of so many pairs of weights, those whose exponentials are polynomials
 constexpr float kRefExcess = 8.f;                  // log2 units by which a weight may exceed 1
 
 // Adds a tile's sums to a row's.
@@ -228,18 +198,12 @@ __device__ __forceinline__ void softmax_tile(uint32_t s_tmem, uint32_t o_tmem, f
         uint32_t* const x = s + h * kHalf;
 #pragma unroll
         for (int i = 0; i < kHalf; i += 2) {
-            uint64_t p = pair_fma(pair_of(x[i], x[i + 1]), scale2, shift2);
+            const uint64_t p = pair_fma(pair_of(x[i], x[i + 1]), scale2, shift2);
             float a, b;
-            if (kTerms == 1 && (i / 2) % kPolyOf < kPoly) {
-                p = pair_exp2(p);
-                pair_split(p, a, b);
-            } else {
-                pair_split(p, a, b);
-                a = exp2_approx(a);
-                b = exp2_approx(b);
-                p = pair_of(a, b);
-            }
-            part[(i >> 1) & 1] = pair_add(part[(i >> 1) & 1], p);
+            pair_split(p, a, b);
+            a = exp2_approx(a);
+            b = exp2_approx(b);
+            part[(i >> 1) & 1] = pair_add(part[(i >> 1) & 1], pair_of(a, b));
             x[i] = __float_as_uint(a);
             x[i + 1] = __float_as_uint(b);
         }

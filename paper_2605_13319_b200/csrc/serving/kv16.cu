@@ -34,9 +34,9 @@ bool aligned(const void* p, int32_t dtype) { return (uintptr_t)p % size_of(dtype
 bool wide(const void* p, int64_t stride, int32_t rows, int32_t dtype) { return (uintptr_t)p % 16 == 0 && (rows == 1 || stride * size_of(dtype) % 16 == 0); }
 int32_t launched() { return cudaGetLastError() == cudaSuccess ? PIPESD_OK : PIPESD_E_CUDA; }
 
-// Query rows that a share has room for.
+// Query rows that a share (of a stream) has room for.
 int pages_cap(const pipesd_kv16_cfg* c, int32_t rows, int32_t n_q_heads) {
-    return (int)std::min<int64_t>(256, ((int64_t)rows * (n_q_heads / c->n_kv_heads) + 3) / 4 * 4);
+    return (int)std::min<int64_t>(128, ((int64_t)rows * (n_q_heads / c->n_kv_heads) + 3) / 4 * 4);
 }
 template <int HD, typename T>
 int32_t pages_run(PagesArgs& a, cudaStream_t st) {
@@ -44,7 +44,7 @@ int32_t pages_run(PagesArgs& a, cudaStream_t st) {
     a.rows = PagesShape<HD, T>::kRows;
     pages_attend_kernel<HD, T><<<a.ctas, kAttendThreads16, pages_smem<HD, T>(), st>>>(a);
     if (cudaGetLastError() != cudaSuccess) return PIPESD_E_CUDA;
-    if (launch_pdl(pages_merge_kernel<HD, T>, dim3((unsigned)(a.w.rows * a.Hq)), dim3(32 * kPagesMergeWarps), 0, st, a) != cudaSuccess) return PIPESD_E_CUDA;
+    if (launch_pdl(pages_merge_kernel<HD, T>, dim3(a.ctas, HD / 32, 2), dim3(32 * kPagesMergeWarps), 0, st, a) != cudaSuccess) return PIPESD_E_CUDA;
     return launched();
 }
 
@@ -188,7 +188,7 @@ int32_t pipesd_kv16_release(const pipesd_kv16_cfg* cfg, int32_t n_req, const int
 
 uint64_t pipesd_kv16_attend_scratch_bytes(const pipesd_kv16_cfg* cfg, int32_t rows, int32_t n_q_heads) {
     if (!cfg_ok(cfg) || rows < 1 || n_q_heads < 1 || n_q_heads % cfg->n_kv_heads || n_q_heads / cfg->n_kv_heads > 128) return 0;
-    return (uint64_t)2 * kPagesSms * pages_cap(cfg, rows, n_q_heads) * (cfg->head_dim + 2) * 4;
+    return kPagesSms * (sizeof(PagesSplit) + (uint64_t)4 * pages_cap(cfg, rows, n_q_heads) * (cfg->head_dim + 2) * 4);
 }
 
 int32_t pipesd_kv16_attend(const pipesd_kv16_cfg* cfg, const void* pool, int32_t layer, const void* q, void* out, int32_t dtype, int64_t q_stride,
@@ -215,7 +215,8 @@ int32_t pipesd_kv16_attend(const pipesd_kv16_cfg* cfg, const void* pool, int32_t
     a.scale = scale * 1.4426950408889634f;
     a.mask = mask;
     a.words = mask ? words : 0;
-    a.parts = static_cast<float*>(scratch);
+    a.splits = static_cast<PagesSplit*>(scratch);
+    a.parts = reinterpret_cast<float*>(a.splits + kPagesSms);
     a.ctas = kPagesSms;
     a.cap = pages_cap(cfg, rows, n_q_heads);
     cudaStream_t st = (cudaStream_t)cuda_stream;
