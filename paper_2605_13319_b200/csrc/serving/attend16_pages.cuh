@@ -23,7 +23,10 @@ struct PagesShape {
     static constexpr bool kWide = sizeof(T) == 4;
     static constexpr int kTerms = kWide ? 3 : 1, kHalves = kWide ? 1 : 2, kKeys = kWide ? 64 : 128, kRows = kWide ? 128 : 256;
     static constexpr int kQTile = 128 * HD * 2, kQ = (kWide ? 3 : 2) * kQTile, kTile = kKeys * HD * 2;
-    static constexpr int kKSlots = kWide ? (HD == 128 ? 4 : 8) : (HD == 128 ? 2 : 4), kVSlots = kWide ? (HD == 128 ? 4 : 8) : (HD == 128 ? 3 : 6);
+    // An even number of places in either ring: where the streams take the tiles in turn each then has places of its own, and a wait for a place's next
+    // turn cannot take the other stream's turn before it, not yet come, for one that is over.
+    static constexpr int kKSlots = kWide ? (HD == 128 ? 4 : 8) : (HD == 128 ? 2 : 4), kVSlots = kWide ? (HD == 128 ? 4 : 8) : (HD == 128 ? 2 : 6);
+    static_assert(kKSlots % 2 == 0 && kVSlots % 2 == 0, "");
     static constexpr int kSlots = kKSlots + kVSlots;
 };
 struct PagesArgs {
@@ -103,7 +106,7 @@ __device__ __forceinline__ long long pages_total(const PagesArgs& a) {
 }
 __device__ __forceinline__ long long pages_share(const PagesArgs& a, long long all) {
     const long long per = (all + a.ctas - 1) / a.ctas;
-    return max(per, (long long)(kPagesLead + kPagesWideTile));
+    return max(per, (long long)kPagesWideTile);      // (every range within a triple has a tile of it)
 }
 // Request that `at` of the sequence belongs to, and how far into it (whole warp; at < the total).
 __device__ __forceinline__ int pages_find(const PagesArgs& a, long long at, long long& off) {
@@ -469,10 +472,9 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                     }
                     tile_no += n;
                 }
-                if (!ok) {                         // products in flight end before their memory is given back
-                    umma_commit(smem_u32(&c.done[s]));
-                    mbar_wait(smem_u32(&c.done[s]), 0);
-                }
+                // What was issued ends, and has arrived at its barriers, before the CTA goes.
+                umma_commit(smem_u32(&c.done[s]));
+                mbar_wait(smem_u32(&c.done[s]), 0);
             }
             __syncwarp();
         }
@@ -565,6 +567,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                         __threadfence_block();
                     }
                     fence_proxy_async_smem();
+                    __syncwarp();
                 }
                 auto given = [&](int h) {
                     tc_fence_before();
@@ -676,7 +679,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
 }
 
 // Adds up the shares of triples that several CTAs had.  A CTA per (CTA whose range ends within a triple, 32 columns), rows by 32: a warp per eighth of the
-// shares, a lane per row, whose shares lie side by side; the warps' sums are added in order.  grid: CTAs, HD / 32, 2.
+// shares, a lane per row, whose shares lie side by side; each warp keeps a maximum of its own, and their sums are added in order.  grid: CTAs, HD / 32, 1 to 4.
 constexpr int kPagesMergeWarps = 8;
 template <int HD, typename T>
 __global__ void __launch_bounds__(32 * kPagesMergeWarps) pages_merge_kernel(const __grid_constant__ PagesArgs a) {
@@ -704,42 +707,42 @@ __global__ void __launch_bounds__(32 * kPagesMergeWarps) pages_merge_kernel(cons
             const int c = split.both ? i : i >> 1, s = split.both ? local >> 7 : i & 1;
             return a.parts + (size_t)((c == 0 ? split.share : 4 * (c0 + c)) + s) * a.cap * (HD + 2);
         };
-        float top = -INFINITY;
-        for (int i = warp; i < shares; i += kPagesMergeWarps) {
-            const float r = share(i)[a.cap * HD + slot];
-            top = r == r ? fmaxf(top, r) : INFINITY;                           // (a NaN where a share never came)
-        }
-        s_top[warp][lane] = top;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < kPagesMergeWarps; ++w) top = fmaxf(top, s_top[w][lane]);
-        float v[32] = {}, sum = 0.f;
+        float top = -INFINITY, sum = 0.f, v[32] = {};
+#pragma unroll 2
         for (int i = warp; i < shares; i += kPagesMergeWarps) {
             const float* const p = share(i);
             const float r = p[a.cap * HD + slot], part = p[a.cap * (HD + 1) + slot];
-            if (r == -INFINITY) continue;          // a share that has seen nothing
-            const float factor = exp2_approx(r - top);
-            sum = fmaf(factor, part, sum);
+            float4 y[8];
 #pragma unroll
-            for (int x = 0; x < 32; x += 4) {
-                const float4 y = *reinterpret_cast<const float4*>(p + (size_t)(d0 + x) * a.cap + 4 * slot);
-                v[x] = fmaf(factor, y.x, v[x]);
-                v[x + 1] = fmaf(factor, y.y, v[x + 1]);
-                v[x + 2] = fmaf(factor, y.z, v[x + 2]);
-                v[x + 3] = fmaf(factor, y.w, v[x + 3]);
+            for (int x = 0; x < 8; ++x) y[x] = *reinterpret_cast<const float4*>(p + (size_t)(d0 + 4 * x) * a.cap + 4 * slot);
+            if (r == -INFINITY) continue;          // a share that has seen nothing
+            const float next = r == r ? fmaxf(top, r) : INFINITY;              // (a NaN where a share never came)
+            const float keep = top == -INFINITY ? 0.f : exp2_approx(top - next), factor = exp2_approx(r - next);
+            top = next;
+            sum = fmaf(factor, part, sum * keep);
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                v[4 * x] = fmaf(factor, y[x].x, v[4 * x] * keep);
+                v[4 * x + 1] = fmaf(factor, y[x].y, v[4 * x + 1] * keep);
+                v[4 * x + 2] = fmaf(factor, y[x].z, v[4 * x + 2] * keep);
+                v[4 * x + 3] = fmaf(factor, y[x].w, v[4 * x + 3] * keep);
             }
         }
+        s_top[warp][lane] = top;
         s_sum[warp][lane] = sum;
 #pragma unroll
         for (int x = 0; x < 32; ++x) s_v[warp][lane][x] = v[x];
         __syncthreads();
         // four rows a warp, a lane per column
         for (int r = warp; r < 32 && r0 + r < split.rows; r += kPagesMergeWarps) {
-            float y = 0.f, total = 0.f;
+            float most = -INFINITY, y = 0.f, total = 0.f;
+#pragma unroll
+            for (int w = 0; w < kPagesMergeWarps; ++w) most = fmaxf(most, s_top[w][r]);
 #pragma unroll
             for (int w = 0; w < kPagesMergeWarps; ++w) {
-                y += s_v[w][r][lane];
-                total += s_sum[w][r];
+                const float factor = s_top[w][r] == -INFINITY ? 0.f : exp2_approx(s_top[w][r] - most);
+                y = fmaf(factor, s_v[w][r][lane], y);
+                total = fmaf(factor, s_sum[w][r], total);
             }
             const int rho = split.rho0 + r0 + r;
             const float inv = total > 0.f ? 1.f / total : total;

@@ -252,10 +252,9 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
                     }
                     entry += 2 * tiles;
                 }
-                if (!ok) {                         // products in flight end before their memory is given back
-                    umma_commit(smem_u32(&c.done[s]));
-                    mbar_wait(smem_u32(&c.done[s]), 0);
-                }
+                // What was issued ends, and has arrived at its barriers, before the CTA goes.
+                umma_commit(smem_u32(&c.done[s]));
+                mbar_wait(smem_u32(&c.done[s]), 0);
             }
             __syncwarp();
         }
@@ -292,6 +291,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
                         __threadfence_block();
                     }
                     fence_proxy_async_smem();
+                    __syncwarp();
                 }
                 ok = warp_wait(smem_u32(&c.s_full[s]), s_phase, dead);
                 s_phase ^= 1;

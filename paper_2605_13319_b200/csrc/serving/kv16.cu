@@ -44,7 +44,7 @@ int32_t pages_run(PagesArgs& a, cudaStream_t st) {
     a.rows = PagesShape<HD, T>::kRows;
     pages_attend_kernel<HD, T><<<a.ctas, kAttendThreads16, pages_smem<HD, T>(), st>>>(a);
     if (cudaGetLastError() != cudaSuccess) return PIPESD_E_CUDA;
-    if (launch_pdl(pages_merge_kernel<HD, T>, dim3(a.ctas, HD / 32, 2), dim3(32 * kPagesMergeWarps), 0, st, a) != cudaSuccess) return PIPESD_E_CUDA;
+    if (launch_pdl(pages_merge_kernel<HD, T>, dim3(a.ctas, HD / 32, std::min<int64_t>(4, ((int64_t)a.w.rows * (a.Hq / a.w.Hkv) + 31) / 32)), dim3(32 * kPagesMergeWarps), 0, st, a) != cudaSuccess) return PIPESD_E_CUDA;
     return launched();
 }
 
