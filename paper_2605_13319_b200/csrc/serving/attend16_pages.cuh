@@ -16,7 +16,7 @@ namespace pipesd {
 
 constexpr int kPagesSms = 148;
 // What a triple counts in the ranges: a lead, and every tile; a tile whose rows fill both streams counts more.
-constexpr int kPagesLead = 6, kPagesTile = 3, kPagesWideTile = 4;
+constexpr int kPagesLead = 18, kPagesTile = 3, kPagesWideTile = 5;
 
 template <int HD, typename T>
 struct PagesShape {
@@ -41,6 +41,8 @@ struct PagesArgs {
     int words;
     struct PagesSplit* splits;  // [CTAs]
     float* parts;               // [4 * CTAs] of {sums [HD / 4][cap][4], references [cap], denominators [cap]}: of a CTA's first range and of a later one, by stream
+    uint32_t page_mul, page_shift;                       // position / page_size = position * page_mul >> page_shift, for positions below 2^30
+    int tile_pages, tile_over;  // keys / page_size and the remainder
     int ctas, cap, keys, rows;  // cap: query rows that a share has room for; keys, rows: of a tile and a row group
 };
 // The triple that goes on behind a CTA's range, as the merge needs it (rows 0: none).
@@ -54,9 +56,9 @@ struct PagesJob {
     int pad;
 };
 struct PagesControl {
-    unsigned long long job_full, job_read, q_full, q_empty, k_full[8], k_empty[8], v_full[8], v_empty[8], s_full[2], p_full[2][2], o_full[2], joint, done[2];
-    PagesJob jobs[2];
-    int bad_lo[2], bad_hi[2];   // tiles in which a value was not finite
+    unsigned long long job_full[2], job_read[2], q_full, q_empty, k_full[8], k_empty[8], v_full[8], v_empty[8], s_full[2], p_full[2][2], o_full[2], joint, done[2];
+    PagesJob jobs[4];           // the slot of job i is said again for job i + 4, when everyone has read job i + 2
+    int bad_lo[4], bad_hi[4];   // tiles in which a value was not finite
     uint32_t present[32];       // eight positions a bit
     float ref[2][128], sum[2][128];
     uint32_t tmem;
@@ -98,31 +100,9 @@ __device__ __forceinline__ long long pages_scan(long long v) {
     }
     return v;
 }
-// The count of all requests (whole warp).
-__device__ __forceinline__ long long pages_total(const PagesArgs& a) {
-    long long all = 0;
-    for (int r = threadIdx.x & 31; r < a.w.n_req; r += 32) all += pages_head(a, pages_load(a, r)) * a.w.Hkv;
-    return __shfl_sync(0xffffffffu, pages_scan(all), 31);
-}
 __device__ __forceinline__ long long pages_share(const PagesArgs& a, long long all) {
     const long long per = (all + a.ctas - 1) / a.ctas;
     return max(per, (long long)kPagesWideTile);      // (every range within a triple has a tile of it)
-}
-// Request that `at` of the sequence belongs to, and how far into it (whole warp; at < the total).
-__device__ __forceinline__ int pages_find(const PagesArgs& a, long long at, long long& off) {
-    const int lane = threadIdx.x & 31;
-    for (int r0 = 0; r0 < a.w.n_req; r0 += 32) {
-        const long long mine = pages_head(a, pages_load(a, r0 + lane)) * a.w.Hkv, inc = pages_scan(mine);
-        const unsigned hit = __ballot_sync(0xffffffffu, at < inc);
-        if (hit) {
-            const int l = __ffs(hit) - 1;
-            off = at - __shfl_sync(0xffffffffu, inc - mine, l);
-            return r0 + l;
-        }
-        at -= __shfl_sync(0xffffffffu, inc, 31);
-    }
-    off = 0;
-    return a.w.n_req;
 }
 // A CTA's way through its range (whole warp).
 struct PagesWalk {
@@ -131,16 +111,34 @@ struct PagesWalk {
     PagesSplit split;
 
     __device__ __forceinline__ void begin(const PagesArgs& a) {
-        const long long all = pages_total(a);
+        const int lane = threadIdx.x & 31;
+        const long long mine0 = pages_head(a, pages_load(a, lane)) * a.w.Hkv, inc0 = pages_scan(mine0);
+        long long all = __shfl_sync(0xffffffffu, inc0, 31);
+        for (int r0 = 32; r0 < a.w.n_req; r0 += 32) all += __shfl_sync(0xffffffffu, pages_scan(pages_head(a, pages_load(a, r0 + lane)) * a.w.Hkv), 31);
         share = pages_share(a, all);
         f = f0 = (long long)blockIdx.x * share;
         f_end = min(f + share, all);
-        off = 0;
-        req = f < f_end ? pages_find(a, f, off) : a.w.n_req;
         split = {};
+        off = f;
+        req = a.w.n_req;
+        for (int r0 = 0; f < f_end && r0 < a.w.n_req; r0 += 32) {
+            long long mine = mine0, inc = inc0;
+            if (r0 > 0) {
+                mine = pages_head(a, pages_load(a, r0 + lane)) * a.w.Hkv;
+                inc = pages_scan(mine);
+            }
+            const unsigned hit = __ballot_sync(0xffffffffu, off < inc);
+            if (hit) {
+                const int l = __ffs(hit) - 1;
+                off -= __shfl_sync(0xffffffffu, inc - mine, l);
+                req = r0 + l;
+                break;
+            }
+            off -= __shfl_sync(0xffffffffu, inc, 31);
+        }
     }
     // The next triple of which the range has tiles; tiles 0: there is none.
-    __device__ __forceinline__ PagesJob next(const PagesArgs& a) {
+    __device__ __noinline__ PagesJob next(const PagesArgs& a) {        // (one copy: what is run for the first time waits for its instructions)
         PagesJob job = {};
         const int G = a.Hq / a.w.Hkv;
         while (f < f_end && req < a.w.n_req) {
@@ -256,54 +254,59 @@ __device__ __noinline__ uint32_t pages_bad(const PagesArgs& a, const PagesJob& j
 
 // A warp's copies of one kind (kv 0: keys, 1: values) into a ring of its own, tile after tile over all jobs.  A lane per page that a tile touches; page
 // ids come by windows of 32, looked up a window ahead.
-template <int HD, int kKeys, int kSlots>
 struct PagesFetch {
-    static constexpr int kTile = kKeys * HD * 2;
-    uint32_t count = 0;
+    const uint16_t* block;      // of the pool's first page
+    const int32_t* table;
+    int total8, pages, p0, page0, off0, window, ids, ids_next;      // p0, page0, off0: the next tile's first position, its page, and where it lies in it
 
-    // said(tile, present): which groups of eight positions of a tile are there, said before its copies.
-    template <typename Say>
-    __device__ __forceinline__ bool run(const PagesArgs& a, const PagesJob& job, int kv, unsigned char* ring, unsigned long long* full, unsigned long long* empty,
-                                        volatile int* dead, Say say) {
-        const int lane = threadIdx.x & 31, ps = a.w.page_size, total8 = (job.base + job.n + 7) & ~7;
-        const size_t page_elems = (size_t)2 * a.w.Hkv * kv16_block_elems(a.w, HD);
-        const uint16_t* const block = kv16_block(a.p, a.w, a.p.layer, 0, kv, job.head);
-        const int32_t* const table = a.w.table + (size_t)job.req * a.w.max_pages;
-        const int pages = (total8 - 1) / ps + 1, per = kKeys / ps, over = kKeys % ps;
-        auto look = [&](int c) { return c < pages ? table[c] : -1; };
-        int p0 = job.u0 * kKeys, page0 = p0 / ps, off0 = p0 % ps;              // the tile's first position, its page, and where it lies in it
-        int window = page0, ids = look(window + lane), ids_next = look(window + 32 + lane);
-        for (int j = 0; j < job.tiles; ++j) {
-            const int start = max(0, lane * ps - off0), end = min(min(kKeys, (lane + 1) * ps - off0), total8 - p0), at = page0 - window + lane;
-            const int x = __shfl_sync(0xffffffffu, ids, at & 31), y = __shfl_sync(0xffffffffu, ids_next, at & 31), id = at < 32 ? x : y;
-            const bool there = start < end && id >= 0 && id < a.w.n_pages;
-            const uint16_t* const src = block + (there ? id * page_elems + (size_t)(start + off0 - lane * ps) * HD : 0);
-            const uint32_t groups = there ? ((1u << ((end - start) >> 3)) - 1u) << (start >> 3) : 0u, present = __reduce_or_sync(0xffffffffu, groups);
-            say(j, present);
-            const RingPlace<kSlots> place(count);
-            if (count >= kSlots && !warp_wait(smem_u32(&empty[place.slot]), place.phase ^ 1, dead)) return false;
-            const uint32_t bar = smem_u32(&full[place.slot]);
-            if (lane == 0) mbar_expect_tx(bar, (uint32_t)__popc(present) * (HD * 16));
-            __syncwarp();
-            if (there) bulk_g2s(smem_u32(ring + place.slot * kTile) + (uint32_t)start * (HD * 2), src, (uint32_t)(end - start) * (HD * 2), bar);
-            ++count;
-            p0 += kKeys;
-            page0 += per;
-            off0 += over;
-            if (off0 >= ps) { off0 -= ps; ++page0; }
-            if (page0 - window >= 32) {
-                window += 32;
-                ids = ids_next;
-                ids_next = look(window + 32 + lane);
-            }
+    __device__ __forceinline__ int look(int c) const { return c < pages ? table[c] : -1; }
+    __device__ __forceinline__ void begin(const PagesArgs& a, const PagesJob& job, int kv) {
+        const int lane = threadIdx.x & 31;
+        auto page_of = [&](int pos) { return (int)((unsigned long long)(uint32_t)pos * a.page_mul >> a.page_shift); };
+        table = a.w.table + (size_t)job.req * a.w.max_pages;
+        block = kv16_block(a.p, a.w, a.p.layer, 0, kv, job.head);
+        total8 = (job.base + job.n + 7) & ~7;
+        pages = page_of(total8 - 1) + 1;
+        p0 = job.u0 * a.keys;
+        page0 = window = page_of(p0);
+        off0 = p0 - page0 * a.w.page_size;
+        ids = look(window + lane);
+        ids_next = look(window + 32 + lane);
+    }
+    // The count-th tile that this warp fetches: which groups of eight positions of it are there.  Nothing: given up.
+    template <int HD, int kKeys, int kSlots, typename Say>
+    __device__ __forceinline__ bool tile(const PagesArgs& a, uint32_t count, unsigned char* ring, unsigned long long* full, unsigned long long* empty, volatile int* dead,
+                                         Say say) {
+        const int lane = threadIdx.x & 31, ps = a.w.page_size;
+        const int start = max(0, lane * ps - off0), end = min(min(kKeys, (lane + 1) * ps - off0), total8 - p0), at = page0 - window + lane;
+        const int x = __shfl_sync(0xffffffffu, ids, at & 31), y = __shfl_sync(0xffffffffu, ids_next, at & 31), id = at < 32 ? x : y;
+        const bool there = start < end && id >= 0 && id < a.w.n_pages;
+        const uint16_t* const src = block + (there ? id * ((size_t)2 * a.w.Hkv * kv16_block_elems(a.w, HD)) + (size_t)(start + off0 - lane * ps) * HD : 0);
+        const uint32_t groups = there ? ((1u << ((end - start) >> 3)) - 1u) << (start >> 3) : 0u, present = __reduce_or_sync(0xffffffffu, groups);
+        say(present);
+        const RingPlace<kSlots> place(count);
+        if (count >= kSlots && !warp_wait(smem_u32(&empty[place.slot]), place.phase ^ 1, dead)) return false;
+        const uint32_t bar = smem_u32(&full[place.slot]);
+        if (lane == 0) mbar_expect_tx(bar, (uint32_t)__popc(present) * (HD * 16));
+        __syncwarp();
+        if (there) bulk_g2s(smem_u32(ring + place.slot * (kKeys * HD * 2)) + (uint32_t)start * (HD * 2), src, (uint32_t)(end - start) * (HD * 2), bar);
+        p0 += kKeys;
+        page0 += a.tile_pages;
+        off0 += a.tile_over;
+        if (off0 >= ps) { off0 -= ps; ++page0; }
+        if (page0 - window >= 32) {
+            window += 32;
+            ids = ids_next;
+            ids_next = look(window + 32 + lane);
         }
         return true;
     }
-    // Given up: the copies in flight are waited for.
-    __device__ __forceinline__ void drain(unsigned long long* full) {
-        for (uint32_t i = count > kSlots ? count - kSlots : 0; i < count; ++i) mbar_wait(smem_u32(&full[i % kSlots]), i / kSlots & 1);
-    }
 };
+// Given up: the copies in flight are waited for.
+template <int kSlots>
+__device__ __forceinline__ void pages_drain(uint32_t count, unsigned long long* full) {
+    for (uint32_t i = count > kSlots ? count - kSlots : 0; i < count; ++i) mbar_wait(smem_u32(&full[i % kSlots]), i / kSlots & 1);
+}
 
 template <int HD, typename T>
 __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const __grid_constant__ PagesArgs a) {
@@ -328,8 +331,10 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
         ahead = walk.next(a);
     }
     if (tid == 0) {
-        mbar_init(smem_u32(&c.job_full), 1);
-        mbar_init(smem_u32(&c.job_read), 11);   // all other roles' warps
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(smem_u32(&c.job_full[i]), 1);
+            mbar_init(smem_u32(&c.job_read[i]), 11);       // all other roles' warps
+        }
         mbar_init(smem_u32(&c.q_full), 8);
         mbar_init(smem_u32(&c.q_empty), 2);
         mbar_init(smem_u32(&c.joint), 8);
@@ -359,41 +364,58 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
     if (warp >= 8) {
         registers_fewer();
         if (warp == 8) {                               // ---- what there is to do, and keys
-            PagesFetch<HD, kKeys, kKSlots> fetch;
-            uint32_t tile_no = 0;
+            uint32_t count = 0;                    // tiles of all jobs
             bool ok = true;
-            for (int i = 0; ok; ++i) {
-                const PagesJob job = ahead;
-                if (i > 0) ok = warp_wait(smem_u32(&c.job_read), (i - 1) & 1, dead);
-                if (!ok) break;
-                if (lane == 0) {
-                    c.jobs[i & 1] = job;
-                    c.bad_lo[i & 1] = INT32_MAX;
-                    c.bad_hi[i & 1] = -1;
-                    mbar_arrive(smem_u32(&c.job_full));
+            auto say = [&](int i, const PagesJob& job) {
+                if (i >= 2) ok = warp_wait(smem_u32(&c.job_read[i & 1]), (i >> 1 & 1) ^ 1, dead);
+                if (ok && lane == 0) {
+                    c.jobs[i & 3] = job;
+                    c.bad_lo[i & 3] = INT32_MAX;
+                    c.bad_hi[i & 3] = -1;
+                    mbar_arrive(smem_u32(&c.job_full[i & 1]));
                 }
-                if (job.tiles == 0) break;
-                ok = fetch.run(a, job, 0, k_ring, c.k_full, c.k_empty, dead, [&](int j, uint32_t present) {
-                    if (lane == 0) c.present[(tile_no + j) & 31] = present;
-                });
-                tile_no += job.tiles;
-                ahead = walk.next(a);
+                __syncwarp();
+            };
+            say(0, ahead);
+            PagesFetch fetch, fetch_next;
+            if (ahead.tiles) fetch.begin(a, ahead, 0);
+            for (int i = 0; ok; ++i) {
+                const int n = ahead.tiles;
+                if (n == 0) break;
+                for (int j = 0; j < n && ok; ++j) {
+                    ok = fetch.tile<HD, kKeys, kKSlots>(a, count, k_ring, c.k_full, c.k_empty, dead, [&](uint32_t present) {
+                        if (lane == 0) c.present[count & 31] = present;
+                    });
+                    count += ok;
+                    if (ok && j == min(1, n - 1)) {                            // the next job is found and said while this one's tiles are fetched
+                        ahead = walk.next(a);
+                        say(i + 1, ahead);
+                        if (ahead.tiles) fetch_next.begin(a, ahead, 0);
+                    }
+                }
+                fetch = fetch_next;
             }
-            if (!ok) fetch.drain(c.k_full);
+            if (!ok) pages_drain<kKSlots>(count, c.k_full);
             if (lane == 0) a.splits[blockIdx.x] = walk.split;
-        } else if (warp == 10) {                       // ---- values
-            PagesFetch<HD, kKeys, kVSlots> fetch;
+        } else if (warp == 10) {                   // ---- values
+            uint32_t count = 0;
             bool ok = true;
             for (int i = 0; ok; ++i) {
-                ok = warp_wait(smem_u32(&c.job_full), i & 1, dead);
+                ok = warp_wait(smem_u32(&c.job_full[i & 1]), i >> 1 & 1, dead);
                 if (!ok) break;
-                const PagesJob job = c.jobs[i & 1];
+                const PagesJob& job = c.jobs[i & 3];
+                const int n = job.tiles;
+                PagesFetch fetch;
+                if (n) fetch.begin(a, job, 1);
                 __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&c.job_read));
-                if (job.tiles == 0) break;
-                ok = fetch.run(a, job, 1, v_ring, c.v_full, c.v_empty, dead, [](int, uint32_t) {});
+                if (lane == 0) mbar_arrive(smem_u32(&c.job_read[i & 1]));
+                if (n == 0) break;
+                for (int j = 0; j < n && ok; ++j) {
+                    ok = fetch.tile<HD, kKeys, kVSlots>(a, count, v_ring, c.v_full, c.v_empty, dead, [](uint32_t) {});
+                    count += ok;
+                }
             }
-            if (!ok) fetch.drain(c.v_full);
+            if (!ok) pages_drain<kVSlots>(count, c.v_full);
         } else if (warp == 9 || warp == 11) {      // ---- a stream's products
             if (elect_one()) {
                 const int s = warp == 9 ? 0 : 1;
@@ -436,11 +458,11 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                     return true;
                 };
                 for (int i = 0; ok; ++i) {
-                    ok = role_wait(smem_u32(&c.job_full), i & 1, dead);
+                    ok = role_wait(smem_u32(&c.job_full[i & 1]), i >> 1 & 1, dead);
                     if (!ok) break;
-                    const int n = c.jobs[i & 1].tiles;
-                    const bool both = c.jobs[i & 1].n_rows > 128;
-                    mbar_arrive(smem_u32(&c.job_read));
+                    const int n = c.jobs[i & 3].tiles;
+                    const bool both = c.jobs[i & 3].n_rows > 128;
+                    mbar_arrive(smem_u32(&c.job_read[i & 1]));
                     if (n == 0) break;
                     // both: rows of q tile s, every tile of keys; else the same rows, tiles in turn
                     const int step = both ? 1 : 2, q_tile = both ? s : 0, j0 = both ? 0 : s;
@@ -492,33 +514,40 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
             return there;
         };
         for (int i = 0;; ++i) {
-            if (!warp_wait(smem_u32(&c.job_full), i & 1, dead)) break;
-            const PagesJob& job = c.jobs[i & 1];           // (as it is until the next but one is said, when both streams have read the next)
+            if (!warp_wait(smem_u32(&c.job_full[i & 1]), i >> 1 & 1, dead)) break;
+            const PagesJob& job = c.jobs[i & 3];
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&c.job_read));
+            if (lane == 0) mbar_arrive(smem_u32(&c.job_read[i & 1]));
             if (job.tiles == 0) break;
             const int n = job.tiles;
             const bool both = job.n_rows > 128;
             // ---- queries, in the products' order: 8 x 4 pieces of 8 columns a warp and step
             bool ok = i == 0 || warp_wait(smem_u32(&c.q_empty), (i - 1) & 1, dead);
             if (ok) {
-                constexpr int kBatch = 8 / (int)(sizeof(T) / 2);               // loads of a thread at once
-                const int steps = (job.n_rows + 7) / 8 * (kPieces / 4);
-                for (int x0 = warp; x0 < steps; x0 += 8 * kBatch) {
+                // A thread has a piece of every kRowStep-th row.
+                constexpr int kBatch = kTerms == 1 ? 4 : 2, kRowStep = 256 / kPieces;          // loads at once
+                const int piece = warp % (kPieces / 4) * 4 + (lane >> 3), r0 = warp / (kPieces / 4) * 8 + (lane & 7);
+                int node = (job.rho0 + r0) / G, g = (job.rho0 + r0) % G;
+                const int node_step = kRowStep / G, g_step = kRowStep % G;
+                const T* const q = static_cast<const T*>(a.q) + (size_t)job.head * G * HD + piece * 8;
+                unsigned char* const to = smem + piece * 128 + (r0 & 7) * 16;
+#pragma unroll 1
+                for (int r = r0; r < job.n_rows; r += kBatch * kRowStep) {
                     uint4 v[kBatch][kTerms];
 #pragma unroll
                     for (int y = 0; y < kBatch; ++y) {
-                        const int x = x0 + 8 * y, r = x / (kPieces / 4) * 8 + (lane & 7), rho = job.rho0 + r, piece = x % (kPieces / 4) * 4 + (lane >> 3);
-                        if (r < job.n_rows)
-                            pages_load8(static_cast<const T*>(a.q) + (job.first + rho / G) * a.q_stride + (size_t)(job.head * G + rho % G) * HD + piece * 8, a.q_wide, v[y]);
+                        if (r + y * kRowStep < job.n_rows) pages_load8(q + (job.first + node) * a.q_stride + (size_t)g * HD, a.q_wide, v[y]);
+                        node += node_step;
+                        g += g_step;
+                        if (g >= G) { g -= G; ++node; }
                     }
 #pragma unroll
                     for (int y = 0; y < kBatch; ++y) {
-                        const int x = x0 + 8 * y, r = x / (kPieces / 4) * 8 + (lane & 7), piece = x % (kPieces / 4) * 4 + (lane >> 3);
-                        if (r < job.n_rows)
+                        const int at = r + y * kRowStep;
+                        if (at < job.n_rows)
 #pragma unroll
                             for (int t = 0; t < kTerms; ++t)
-                                *reinterpret_cast<uint4*>(smem + (t + (r >> 7)) * Shape::kQTile + ((r & 127) >> 3) * HD * 16 + piece * 128 + (r & 7) * 16) = v[y][t];
+                                *reinterpret_cast<uint4*>(to + (t + (at >> 7)) * Shape::kQTile + ((at & 127) >> 3) * HD * 16) = v[y][t];
                     }
                 }
                 fence_proxy_async_smem();
@@ -562,8 +591,8 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                             const int key = p / kPieces / 8 * 8 + p % 8;
                             return key < keys && (present >> (key >> 3) & 1u);
                         })) {
-                        atomicMin(&c.bad_lo[i & 1], u);
-                        atomicMax(&c.bad_hi[i & 1], u);
+                        atomicMin(&c.bad_lo[i & 3], u);
+                        atomicMax(&c.bad_hi[i & 3], u);
                         __threadfence_block();
                     }
                     fence_proxy_async_smem();
@@ -624,7 +653,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                 f1 = none1 ? 0.f : exp2_approx(r1 - ref);
                 sum = c.sum[0][row] * f0 + c.sum[1][row] * f1;
             }
-            const int lo = *(volatile int*)&c.bad_lo[i & 1], hi = *(volatile int*)&c.bad_hi[i & 1];
+            const int lo = *(volatile int*)&c.bad_lo[i & 3], hi = *(volatile int*)&c.bad_hi[i & 3];
             if (whole) {
                 const float inv = sum > 0.f ? 1.f / sum : sum;
                 f0 *= inv;

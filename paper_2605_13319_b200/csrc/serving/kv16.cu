@@ -42,6 +42,13 @@ template <int HD, typename T>
 int32_t pages_run(PagesArgs& a, cudaStream_t st) {
     a.keys = PagesShape<HD, T>::kKeys;
     a.rows = PagesShape<HD, T>::kRows;
+    a.tile_pages = a.keys / a.w.page_size;
+    a.tile_over = a.keys % a.w.page_size;
+    // ceil(2^(30 + L) / page_size) with 2^L >= page_size is off by less than page_size <= 2^L, so that the quotient of a position below 2^30 is exact
+    int log = 0;
+    while ((1 << log) < a.w.page_size) ++log;
+    a.page_shift = 30 + log;
+    a.page_mul = (uint32_t)(((1ull << a.page_shift) + a.w.page_size - 1) / a.w.page_size);
     pages_attend_kernel<HD, T><<<a.ctas, kAttendThreads16, pages_smem<HD, T>(), st>>>(a);
     if (cudaGetLastError() != cudaSuccess) return PIPESD_E_CUDA;
     if (launch_pdl(pages_merge_kernel<HD, T>, dim3(a.ctas, HD / 32, std::min<int64_t>(4, ((int64_t)a.w.rows * (a.Hq / a.w.Hkv) + 31) / 32)), dim3(32 * kPagesMergeWarps), 0, st, a) != cudaSuccess) return PIPESD_E_CUDA;
