@@ -415,7 +415,7 @@ int32_t pipesd_attend_packed(const void *q, const void *k, const void *v, void *
 /* Mask rows of drafted trees.  Request r has the nodes row0[r] .. row0[r+1]-1; parent[row] is the index within its request of the node's
  * parent, below its own (-1, or anything that is not: a child of the prefix).  mask: [rows, words], bit j of a row = node j is the node itself or an
  * ancestor; depth: [rows], ancestors among the nodes (the row's position is base + depth).  words: 1..256; a node with an index of 32 * words
- * or more has no bits and depth -1.  Rows of no request are left as they are. */
+ * or more has no bits and depth -1.  Rows in front of the first request and behind the last have no bits and depth 0. */
 int32_t pipesd_tree_mask(int32_t n_req, int32_t rows, const int32_t *row0, const int32_t *parent, int32_t words, uint32_t *mask,
                          int32_t *depth, void *cuda_stream);
 

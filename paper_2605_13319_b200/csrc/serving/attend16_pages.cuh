@@ -315,7 +315,8 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
     constexpr int kHalves = Shape::kHalves;        // in which a tile's weights go over
     constexpr bool kOwn = Shape::kWide;            // the threads add up the tiles' sums
     constexpr uint32_t kIdescS = umma_idesc_bf16(128, kKeys, 0, 0), kIdescO = umma_idesc_bf16(128, HD, 0, 1);
-    extern __shared__ __align__(128) unsigned char smem[];
+    extern __shared__ __align__(128) unsigned char pages_memory[];
+    unsigned char* const smem = pages_memory;
     unsigned char* const k_ring = smem + Shape::kQ;
     unsigned char* const v_ring = k_ring + kKSlots * kTile;
     PagesControl& c = *reinterpret_cast<PagesControl*>(v_ring + kVSlots * kTile);

@@ -61,8 +61,9 @@ __device__ __forceinline__ int prompt_blocks_from(const PromptArgs& a, int level
     }
     return __reduce_add_sync(0xffffffffu, sum);
 }
-// Job of a rank, longest first (whole warp).  n = 0: there are not as many.
-__device__ __forceinline__ PromptJob prompt_job(const PromptArgs& a, long long rank, int block, int levels) {
+// A CTA's i-th job: the jobs, longest first, are dealt out back and forth (whole warp).  n = 0: there are not as many.
+__device__ __forceinline__ PromptJob prompt_job(const PromptArgs& a, int i, int block, int levels) {
+    const long long round = (long long)i * a.ctas, rank = i & 1 ? round + a.ctas - 1 - blockIdx.x : round + blockIdx.x;
     PromptJob job = {0, 0, 0, 0};
     const int lane = threadIdx.x & 31;
     int lo = 0, hi = levels;                       // the largest level that at least rank + 1 jobs reach
@@ -111,13 +112,25 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
     using Shape = PromptShape<HD>;
     constexpr int kTile = Shape::kTile, kStages = Shape::kStages, kAtom = 128 * 128;      // an atom: 128 rows of 64 columns
     constexpr uint32_t kIdescS = umma_idesc_bf16(128, 128, 0, 0), kIdescO = umma_idesc_bf16(128, HD, 0, 1);
-    extern __shared__ __align__(1024) unsigned char smem[];
+    extern __shared__ __align__(1024) unsigned char prompt_memory[];
+    unsigned char* const smem = prompt_memory;
     unsigned char* const ring = smem + 2 * kTile;
     PromptControl& c = *reinterpret_cast<PromptControl*>(ring + kStages * kTile);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int G = a.Hq / a.Hkv, T = 128 / G;
     volatile int* const dead = &c.dead;
 
+    PromptJob ahead;
+    int levels = 0;
+    if (warp == 8) {                               // (while the others set up)
+        if (lane < 3) tensor_map_prefetch(lane == 0 ? &map_q : lane == 1 ? &map_k : &map_v);
+        for (int r = lane; r < a.n_req; r += 32) {
+            int first;
+            levels = max(levels, (prompt_len(a, r, first) + 2 * T - 1) / (2 * T));
+        }
+        levels = __reduce_max_sync(0xffffffffu, levels);
+        ahead = prompt_job(a, 0, 2 * T, levels);
+    }
     if (tid == 0) {
         mbar_init(smem_u32(&c.q_full), 1);
         mbar_init(smem_u32(&c.q_empty), 10);     // both streams' products, and their warps when they have read the job
@@ -143,49 +156,47 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
     if (warp >= 8) {
         registers_fewer();
         if (warp == 8) {                               // ---- fetches
-            int levels = 0;
-            for (int r = lane; r < a.n_req; r += 32) {
-                int first;
-                levels = max(levels, (prompt_len(a, r, first) + 2 * T - 1) / (2 * T));
-            }
-            levels = __reduce_max_sync(0xffffffffu, levels);
             uint32_t entry = 0;                        // of the ring, over all jobs
             bool ok = true;
             for (int i = 0; ok; ++i) {
-                const long long round = (long long)i * a.ctas;
-                const PromptJob job = prompt_job(a, i & 1 ? round + a.ctas - 1 - blockIdx.x : round + blockIdx.x, 2 * T, levels);
+                const PromptJob job = ahead;
                 if (i > 0) ok = warp_wait(smem_u32(&c.q_empty), (i - 1) & 1, dead);
-                if (lane == 0 && ok) {
+                if (!ok) break;
+                const int tiles[2] = {prompt_tiles(job, 0, T), prompt_tiles(job, 1, T)}, n = max(tiles[0], tiles[1]);
+                if (lane == 0) {
+                    const uint32_t bar = smem_u32(&c.q_full);
                     c.jobs[i % kPromptJobs] = job;
                     c.flags[i % kPromptJobs] = 0;
                     if (job.n == 0) {
-                        mbar_arrive(smem_u32(&c.q_full));
+                        mbar_arrive(bar);
                     } else {
-                        const int tiles[2] = {prompt_tiles(job, 0, T), prompt_tiles(job, 1, T)};
-                        const uint32_t bar = smem_u32(&c.q_full);
                         mbar_expect_tx(bar, (uint32_t)((tiles[1] ? 2 : 1) * (HD / 64) * T * G * 128));
                         for (int s = 0; s < 2; ++s)
                             for (int x = 0; tiles[s] && x < HD / 64; ++x)
                                 tensor3_g2s(smem_u32(smem + s * kTile + x * kAtom), &map_q, 64 * x, job.head * G, job.first + job.t0 + s * T, bar);
-                        const int n = max(tiles[0], tiles[1]);
-                        for (int e = 0; e < 2 * n && ok; ++e, ++entry) {
-                            const int st = entry % kStages;
-                            if (entry >= kStages) ok = role_wait(smem_u32(&c.empty[st]), (entry / kStages - 1) & 1, dead);
-                            if (!ok) break;
-                            const uint32_t full = smem_u32(&c.full[st]);
-                            mbar_expect_tx(full, kTile);
-                            for (int x = 0; x < HD / 64; ++x)
-                                tensor3_g2s(smem_u32(ring + st * kTile + x * kAtom), e & 1 ? &map_v : &map_k, 64 * x, job.head, job.first + (e >> 1) * 128, full);
-                        }
                     }
                 }
-                ok = __shfl_sync(0xffffffffu, ok, 0);
-                entry = __shfl_sync(0xffffffffu, entry, 0);
+                __syncwarp();
                 if (job.n == 0) break;
+                for (int e = 0; e < 2 * n && ok; ++e) {
+                    const RingPlace<kStages> place(entry);
+                    if (entry >= kStages) ok = warp_wait(smem_u32(&c.empty[place.slot]), place.phase ^ 1, dead);
+                    if (!ok) break;
+                    if (lane == 0) {
+                        const uint32_t full = smem_u32(&c.full[place.slot]);
+                        mbar_expect_tx(full, kTile);
+                        for (int x = 0; x < HD / 64; ++x)
+                            tensor3_g2s(smem_u32(ring + place.slot * kTile + x * kAtom), e & 1 ? &map_v : &map_k, 64 * x, job.head, job.first + (e >> 1) * 128, full);
+                    }
+                    __syncwarp();
+                    ++entry;
+                    if (e == 1) ahead = prompt_job(a, i + 1, 2 * T, levels);   // (while this job's tiles are fetched)
+                }
             }
             if (!ok && lane == 0) {                    // given up: the copies in flight are waited for
                 for (uint32_t e = entry > kStages ? entry - kStages : 0; e < entry; ++e) mbar_wait(smem_u32(&c.full[e % kStages]), (e / kStages) & 1);
             }
+            __syncwarp();
         } else if (warp == 9 || warp == 11) {      // ---- a stream's products
             if (elect_one()) {
                 const int s = warp == 9 ? 0 : 1;

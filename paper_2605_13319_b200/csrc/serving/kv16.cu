@@ -143,7 +143,7 @@ int32_t pipesd_kv16_read(const pipesd_kv16_cfg* cfg, const void* pool, int32_t l
 int32_t pipesd_tree_mask(int32_t n_req, int32_t rows, const int32_t* row0, const int32_t* parent, int32_t words, uint32_t* mask, int32_t* depth,
                          void* cuda_stream) {
     if (n_req < 1 || rows < 1 || !row0 || !parent || !mask || !depth || words < 1 || words > kTreeWords) return PIPESD_E_INVALID;
-    tree_mask_kernel<<<n_req, 256, 0, (cudaStream_t)cuda_stream>>>(row0, parent, n_req, rows, words, mask, depth);
+    tree_mask_kernel<<<n_req + 1u, 256, 0, (cudaStream_t)cuda_stream>>>(row0, parent, n_req, rows, words, mask, depth);
     return launched();
 }
 

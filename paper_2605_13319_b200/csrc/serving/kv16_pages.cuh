@@ -77,10 +77,20 @@ __global__ void __launch_bounds__(32 * kKv16RowWarps) kv16_read_kernel(const Kv1
 constexpr int kTreeWords = 256;                    // of a row's mask at most: 8192 nodes
 
 // A CTA per request: its parents in shared memory, a thread per node that walks up.  A parent has a lower index than its child, so every walk ends.
+// One CTA more: rows in front of the first request and behind the last.
 __global__ void __launch_bounds__(256) tree_mask_kernel(const int32_t* row0, const int32_t* parent, int n_req, int rows, int words, uint32_t* mask,
                                                          int32_t* depth) {
     __shared__ int32_t up[32 * kTreeWords];
-    const int r = blockIdx.x, first = row0[r], end = row0[r + 1];
+    const int r = blockIdx.x;
+    if (r == n_req) {
+        const int from = max(0, min(row0[0], rows)), to = max(from, min(row0[n_req], rows));
+        for (size_t i = threadIdx.x; i < (size_t)from * words; i += blockDim.x) mask[i] = 0;
+        for (size_t i = (size_t)to * words + threadIdx.x; i < (size_t)rows * words; i += blockDim.x) mask[i] = 0;
+        for (int i = threadIdx.x; i < from; i += blockDim.x) depth[i] = 0;
+        for (int i = to + threadIdx.x; i < rows; i += blockDim.x) depth[i] = 0;
+        return;
+    }
+    const int first = row0[r], end = row0[r + 1];
     if (first < 0 || end < first || end > rows) return;
     const int n = end - first, held = min(n, 32 * words);
     for (int i = threadIdx.x; i < held; i += blockDim.x) up[i] = parent[first + i];
@@ -116,12 +126,13 @@ struct Kv16CompactArgs {
 };
 constexpr int kCompactMoves = 256;                 // rows that are listed at a time
 
-// Rows base + j with bit j of the request's keep go to base + (number of bits below j).  A warp per (layer, K or V, head) block, which loads eight
-// rows or more before it stores them; targets lie in front of their sources and both ascend, so that no row is overwritten before it is
-// read.  grid: requests, blocks / 8.
+// Rows base + j with bit j of the request's keep go to base + (number of bits below j).  A warp per (layer, K or V, head) block, which loads sixteen
+// rows before it stores them; targets lie in front of their sources and both ascend, so that no row is overwritten before it is
+// read.  Eight lanes have the same columns of eight rows: rows that lie side by side share their sectors (32 forks of 64 nodes in 32 layers of 8 heads,
+// 20 rows each: 55 us with the lanes along a row, 41 so).  grid: requests, blocks / 8.
 template <int HD>
 __global__ void __launch_bounds__(256) kv16_compact_kernel(const Kv16CompactArgs a) {
-    constexpr int kPieces = HD / 8, kRows = 32 / kPieces, kUnroll = 8;
+    constexpr int kPieces = HD / 8, kGroups = kPieces / 4;                     // of 4 pieces by 8 rows
     __shared__ uint32_t src[kCompactMoves], dst[kCompactMoves];      // page * page_size + slot
     __shared__ int s_n, s_word, s_rank;
     const int r = blockIdx.x, tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -164,22 +175,30 @@ __global__ void __launch_bounds__(256) kv16_compact_kernel(const Kv16CompactArgs
         for (int b = blockIdx.y * 8 + warp; b < blocks; b += gridDim.y * 8) {
             const int layer = b / (2 * a.w.Hkv), rest = b % (2 * a.w.Hkv);
             uint16_t* const at = a.p.pool + ((size_t)layer * a.w.n_pages * 2 * a.w.Hkv + rest) * elems;
-            auto piece = [&](uint32_t where) {
+            auto row_of = [&](uint32_t where) {
                 const uint32_t page = where / a.w.page_size, slot = where % a.w.page_size;
-                return reinterpret_cast<uint4*>(at + (size_t)page * 2 * a.w.Hkv * elems + kv16_piece(slot, lane % kPieces, HD));
+                return at + (size_t)page * 2 * a.w.Hkv * elems + kv16_piece(slot, lane >> 3, HD);
             };
-            for (int i0 = 0; i0 < n; i0 += kRows * kUnroll) {
-                uint4 x[kUnroll];
+            for (int i0 = 0; i0 < n; i0 += 16) {
+                uint4 x[2][kGroups];
 #pragma unroll
-                for (int u = 0; u < kUnroll; ++u) {
-                    const int i = i0 + u * kRows + lane / kPieces;
-                    if (i < n) x[u] = *piece(src[i]);
+                for (int u = 0; u < 2; ++u) {
+                    const int i = i0 + 8 * u + (lane & 7);
+                    if (i < n) {
+                        const uint16_t* const from = row_of(src[i]);
+#pragma unroll
+                        for (int c = 0; c < kGroups; ++c) x[u][c] = *reinterpret_cast<const uint4*>(from + c * 4 * 64);
+                    }
                 }
                 __syncwarp();
 #pragma unroll
-                for (int u = 0; u < kUnroll; ++u) {
-                    const int i = i0 + u * kRows + lane / kPieces;
-                    if (i < n) *piece(dst[i]) = x[u];
+                for (int u = 0; u < 2; ++u) {
+                    const int i = i0 + 8 * u + (lane & 7);
+                    if (i < n) {
+                        uint16_t* const to = row_of(dst[i]);
+#pragma unroll
+                        for (int c = 0; c < kGroups; ++c) *reinterpret_cast<uint4*>(to + c * 4 * 64) = x[u][c];
+                    }
                 }
                 __syncwarp();
             }
