@@ -43,7 +43,8 @@ struct PagesArgs {
     float* parts;               // [4 * CTAs] of {sums [HD / 4][cap][4], references [cap], denominators [cap]}: of a CTA's first range and of a later one, by stream
     uint32_t page_mul, page_shift;                       // position / page_size = position * page_mul >> page_shift, for positions below 2^30
     int tile_pages, tile_over;  // keys / page_size and the remainder
-    int ctas, cap, keys, rows;  // cap: query rows that a share has room for; keys, rows: of a tile and a row group
+    int G, cap;                 // query heads per KV head; query rows that a share has room for
+    int log_keys, log_rows;     // of a tile and a row group
 };
 // The triple that goes on behind a CTA's range, as the merge needs it (rows 0: none).
 struct PagesSplit {
@@ -70,26 +71,23 @@ constexpr int pages_smem() { return PagesShape<HD, T>::kQ + PagesShape<HD, T>::k
 // What a request adds to the sequence: tiles per triple, row groups, and what a triple counts.
 struct PagesRequest {
     int n, first, base, units, groups;
-    long long last;             // of the last row group, which may be narrower
-    int per;                    // of the others
 };
 __device__ __forceinline__ int pages_weight(int rows) { return rows > 128 ? kPagesWideTile : kPagesTile; }
 __device__ __forceinline__ long long pages_count(int units, int rows) { return kPagesLead + (long long)units * pages_weight(rows); }
 __device__ __forceinline__ PagesRequest pages_load(const PagesArgs& a, int r) {
-    PagesRequest q = {0, 0, 0, 0, 0, 0, 0};
+    PagesRequest q = {0, 0, 0, 0, 0};
     if (r >= a.w.n_req) return q;
     q.n = kv4_rows(a.w, r, q.first, q.base);
     if (q.n <= 0) { q.n = 0; return q; }
-    const int rows = q.n * (a.Hq / a.w.Hkv);
-    q.units = (q.base + q.n + a.keys - 1) / a.keys;
-    q.groups = (rows + a.rows - 1) / a.rows;
+    q.units = (q.base + q.n + (1 << a.log_keys) - 1) >> a.log_keys;
+    q.groups = (q.n * a.G + (1 << a.log_rows) - 1) >> a.log_rows;
     return q;
 }
-__device__ __forceinline__ int pages_group_rows(const PagesArgs& a, const PagesRequest& q, int group) { return min(a.rows, q.n * (a.Hq / a.w.Hkv) - group * a.rows); }
+__device__ __forceinline__ int pages_group_rows(const PagesArgs& a, const PagesRequest& q, int group) { return min(1 << a.log_rows, q.n * a.G - (group << a.log_rows)); }
 // All heads' triples of a request: group by group within a head.
 __device__ __forceinline__ long long pages_head(const PagesArgs& a, const PagesRequest& q) {
     if (q.groups == 0) return 0;
-    return (q.groups - 1) * pages_count(q.units, a.rows) + pages_count(q.units, pages_group_rows(a, q, q.groups - 1));
+    return (q.groups - 1) * pages_count(q.units, 1 << a.log_rows) + pages_count(q.units, pages_group_rows(a, q, q.groups - 1));
 }
 __device__ __forceinline__ long long pages_scan(long long v) {
     const int lane = threadIdx.x & 31;
@@ -100,9 +98,16 @@ __device__ __forceinline__ long long pages_scan(long long v) {
     }
     return v;
 }
-__device__ __forceinline__ long long pages_share(const PagesArgs& a, long long all) {
-    const long long per = (all + a.ctas - 1) / a.ctas;
-    return max(per, (long long)kPagesWideTile);      // (every range within a triple has a tile of it)
+__device__ __forceinline__ long long pages_share(long long all) {
+    return max((all + kPagesSms - 1) / kPagesSms, (long long)kPagesWideTile);      // (every range within a triple has a tile of it)
+}
+// a / b of whole numbers, a >= 0, b > 0: the fp32 quotient is off by 2^-21 of itself and one, so that the loops run once at most below two
+// million.  (A division of 64-bit integers takes several times as long, and this is what everyone waits for first.)
+__device__ __forceinline__ long long pages_div(long long a, long long b) {
+    long long q = (long long)__fdividef((float)a, (float)b), r = a - q * b;
+    for (; r < 0; r += b) --q;
+    for (; r >= b; r -= b) ++q;
+    return q;
 }
 // A CTA's way through its range (whole warp).
 struct PagesWalk {
@@ -115,7 +120,7 @@ struct PagesWalk {
         const long long mine0 = pages_head(a, pages_load(a, lane)) * a.w.Hkv, inc0 = pages_scan(mine0);
         long long all = __shfl_sync(0xffffffffu, inc0, 31);
         for (int r0 = 32; r0 < a.w.n_req; r0 += 32) all += __shfl_sync(0xffffffffu, pages_scan(pages_head(a, pages_load(a, r0 + lane)) * a.w.Hkv), 31);
-        share = pages_share(a, all);
+        share = pages_share(all);
         f = f0 = (long long)blockIdx.x * share;
         f_end = min(f + share, all);
         split = {};
@@ -138,36 +143,38 @@ struct PagesWalk {
         }
     }
     // The next triple of which the range has tiles; tiles 0: there is none.
-    __device__ __noinline__ PagesJob next(const PagesArgs& a) {        // (one copy: what is run for the first time waits for its instructions)
+    __device__ __forceinline__ PagesJob next(const PagesArgs& a) {
         PagesJob job = {};
-        const int G = a.Hq / a.w.Hkv;
         while (f < f_end && req < a.w.n_req) {
             const PagesRequest q = pages_load(a, req);
             const long long head = pages_head(a, q);
             if (off >= head * a.w.Hkv) { ++req; off = 0; continue; }           // (requests without rows have nothing)
-            const long long full = pages_count(q.units, a.rows), in_head = off % head;
-            job.head = (int)(off / head);
-            const int group = (int)min(in_head / full, (long long)q.groups - 1);
+            job.head = (int)pages_div(off, head);
+            const long long full = pages_count(q.units, 1 << a.log_rows), in_head = off - job.head * head;
+            const int group = (int)min(pages_div(in_head, full), (long long)q.groups - 1);
             job.n_rows = pages_group_rows(a, q, group);
             const int weight = pages_weight(job.n_rows);
             const long long start = f - (in_head - group * full), count = pages_count(q.units, job.n_rows);      // of the triple
             // tile t of it is the range's that start + lead + t * weight lies in
-            auto tiles_before = [&](long long at) { return (int)min((long long)q.units, max(0ll, (at - start - kPagesLead + weight - 1) / weight)); };
+            auto tiles_before = [&](long long at) {
+                const unsigned long long x = max(0ll, at - start - kPagesLead);
+                return (int)min((unsigned long long)q.units, weight == kPagesTile ? (x + kPagesTile - 1) / kPagesTile : (x + kPagesWideTile - 1) / kPagesWideTile);
+            };
             const int u0 = f > start ? tiles_before(f) : 0, u1 = tiles_before(f_end);
             const long long step = min(start + count, f_end) - f;
             off += step;
             f += step;
             if (u0 >= u1) continue;
             job.req = req; job.n = q.n; job.first = q.first; job.base = q.base;
-            job.rho0 = group * a.rows;
+            job.rho0 = group << a.log_rows;
             job.u0 = u0;
             job.whole = u0 == 0 && u1 == q.units;
             job.share = 4 * blockIdx.x + (start > f0 ? 2 : 0);
             // without a mask no row of the group sees what lies behind its last one
-            const int seen = a.mask ? q.units : min(q.units, (q.base + (job.rho0 + job.n_rows - 1) / G) / a.keys + 1);
+            const int seen = a.mask ? q.units : min(q.units, ((q.base + (job.rho0 + job.n_rows - 1) / a.G) >> a.log_keys) + 1);
             job.tiles = max(1, min(u1, seen) - u0);                            // (a tile at least: the others' sums are none)
             if (u0 == 0 && !job.whole)
-                split = {q.first, job.head, job.rho0, job.n_rows, (int)((start + kPagesLead + (long long)(q.units - 1) * weight) / share), job.share, job.n_rows > 128, 0};
+                split = {q.first, job.head, job.rho0, job.n_rows, (int)pages_div(start + kPagesLead + (long long)(q.units - 1) * weight, share), job.share, job.n_rows > 128, 0};
             return job;
         }
         job.tiles = 0;
@@ -267,7 +274,7 @@ struct PagesFetch {
         block = kv16_block(a.p, a.w, a.p.layer, 0, kv, job.head);
         total8 = (job.base + job.n + 7) & ~7;
         pages = page_of(total8 - 1) + 1;
-        p0 = job.u0 * a.keys;
+        p0 = job.u0 << a.log_keys;
         page0 = window = page_of(p0);
         off0 = p0 - page0 * a.w.page_size;
         ids = look(window + lane);
@@ -321,16 +328,12 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
     unsigned char* const v_ring = k_ring + kKSlots * kTile;
     PagesControl& c = *reinterpret_cast<PagesControl*>(v_ring + kVSlots * kTile);
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const int G = a.Hq / a.w.Hkv;
+    const int G = a.G;
     volatile int* const dead = &c.dead;
     pdl_launch_dependents();
 
     PagesWalk walk;
-    PagesJob ahead;
-    if (warp == 8) {                               // (while the others set up)
-        walk.begin(a);
-        ahead = walk.next(a);
-    }
+    if (warp == 8) walk.begin(a);                  // (while the others set up)
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&c.job_full[i]), 1);
@@ -377,24 +380,28 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                 }
                 __syncwarp();
             };
-            say(0, ahead);
+            // A job is found and said while the tiles of the one before are fetched.
+            PagesJob ahead;
             PagesFetch fetch, fetch_next;
-            if (ahead.tiles) fetch.begin(a, ahead, 0);
-            for (int i = 0; ok; ++i) {
-                const int n = ahead.tiles;
-                if (n == 0) break;
-                for (int j = 0; j < n && ok; ++j) {
-                    ok = fetch.tile<HD, kKeys, kKSlots>(a, count, k_ring, c.k_full, c.k_empty, dead, [&](uint32_t present) {
-                        if (lane == 0) c.present[count & 31] = present;
-                    });
-                    count += ok;
-                    if (ok && j == min(1, n - 1)) {                            // the next job is found and said while this one's tiles are fetched
-                        ahead = walk.next(a);
-                        say(i + 1, ahead);
-                        if (ahead.tiles) fetch_next.begin(a, ahead, 0);
-                    }
+            bool find = true;
+            for (int i = 0, j = 0, n = 0; ok;) {
+                if (find) {
+                    ahead = walk.next(a);
+                    say(i++, ahead);
+                    if (ahead.tiles) fetch_next.begin(a, ahead, 0);
+                    find = false;
                 }
-                fetch = fetch_next;
+                if (j == n) {
+                    n = ahead.tiles;
+                    if (!ok || n == 0) break;
+                    fetch = fetch_next;
+                    j = 0;
+                }
+                ok = ok && fetch.tile<HD, kKeys, kKSlots>(a, count, k_ring, c.k_full, c.k_empty, dead, [&](uint32_t present) {
+                    if (lane == 0) c.present[count & 31] = present;
+                });
+                count += ok;
+                find = ++j == min(2, n);
             }
             if (!ok) pages_drain<kKSlots>(count, c.k_full);
             if (lane == 0) a.splits[blockIdx.x] = walk.split;
@@ -588,16 +595,16 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                     ok = warp_wait(smem_u32(&c.v_full[v.slot]), v.phase, dead);
                     if (!ok) break;
                     const int keys = job.base + job.n - p0;
-                    if (clean_values(v_ring + v.slot * kTile, kTile / 16, row, 128, [&](int p) {
+                    clean_values<kTile / 16>(
+                        v_ring + v.slot * kTile, row,
+                        [&](int p) {
                             const int key = p / kPieces / 8 * 8 + p % 8;
-                            return key < keys && (present >> (key >> 3) & 1u);
-                        })) {
-                        atomicMin(&c.bad_lo[i & 3], u);
-                        atomicMax(&c.bad_hi[i & 3], u);
-                        __threadfence_block();
-                    }
-                    fence_proxy_async_smem();
-                    __syncwarp();
+                            return key < keys && (present >> (key >> 3) & 1u) ? kSeenBySome : kNoKey;      // (who sees all is not worth asking here)
+                        },
+                        [&] {
+                            atomicMin(&c.bad_lo[i & 3], u);
+                            atomicMax(&c.bad_hi[i & 3], u);
+                        });
                 }
                 auto given = [&](int h) {
                     tc_fence_before();
@@ -715,7 +722,7 @@ template <int HD, typename T>
 __global__ void __launch_bounds__(32 * kPagesMergeWarps) pages_merge_kernel(const __grid_constant__ PagesArgs a) {
     __shared__ float s_top[kPagesMergeWarps][32], s_sum[kPagesMergeWarps][32];
     __shared__ float s_v[kPagesMergeWarps][32][33];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, G = a.Hq / a.w.Hkv;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, G = a.G;
     // Launched with programmatic serialisation: behind this the shares are complete.  Every thread waits, those without work too.
     pdl_wait();
     // rows of requests that have no position: nothing to see

@@ -51,10 +51,10 @@ __device__ __forceinline__ int prompt_len(const PromptArgs& a, int r, int& first
     const int end = a.row0[r + 1];
     return first < 0 || end < first || end > a.rows ? 0 : end - first;
 }
-// Blocks of `block` tokens with an index of `level` or more, over all prompts (whole warp).
-__device__ __forceinline__ int prompt_blocks_from(const PromptArgs& a, int level, int block) {
-    int sum = 0;
-    for (int r = threadIdx.x & 31; r < a.n_req; r += 32) {
+// Blocks of `block` tokens with an index of `level` or more, over all prompts (whole warp; mine: of the lane's own prompt, r = lane).
+__device__ __forceinline__ int prompt_blocks_from(const PromptArgs& a, int level, int block, int mine) {
+    int sum = max(0, mine - level);
+    for (int r = 32 + (threadIdx.x & 31); r < a.n_req; r += 32) {
         int first;
         const int b = (prompt_len(a, r, first) + block - 1) / block;
         sum += max(0, b - level);
@@ -62,27 +62,28 @@ __device__ __forceinline__ int prompt_blocks_from(const PromptArgs& a, int level
     return __reduce_add_sync(0xffffffffu, sum);
 }
 // A CTA's i-th job: the jobs, longest first, are dealt out back and forth (whole warp).  n = 0: there are not as many.
-__device__ __forceinline__ PromptJob prompt_job(const PromptArgs& a, int i, int block, int levels) {
+__device__ __forceinline__ PromptJob prompt_job(const PromptArgs& a, int i, int block, int levels, int n0, int first0) {
+    const int mine = (n0 + block - 1) / block;
     const long long round = (long long)i * a.ctas, rank = i & 1 ? round + a.ctas - 1 - blockIdx.x : round + blockIdx.x;
     PromptJob job = {0, 0, 0, 0};
     const int lane = threadIdx.x & 31;
     int lo = 0, hi = levels;                       // the largest level that at least rank + 1 jobs reach
-    if ((long long)prompt_blocks_from(a, 0, block) * a.Hkv <= rank) return job;
+    if ((long long)prompt_blocks_from(a, 0, block, mine) * a.Hkv <= rank) return job;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if ((long long)prompt_blocks_from(a, mid, block) * a.Hkv > rank) lo = mid;
+        if ((long long)prompt_blocks_from(a, mid, block, mine) * a.Hkv > rank) lo = mid;
         else hi = mid;
     }
-    const int index = (int)(rank - (long long)prompt_blocks_from(a, lo + 1, block) * a.Hkv);
+    const int index = (int)(rank - (long long)prompt_blocks_from(a, lo + 1, block, mine) * a.Hkv);
     int left = index / a.Hkv;
     job.head = index % a.Hkv;
     for (int r0 = 0; r0 < a.n_req; r0 += 32) {
-        int first = 0, n = 0;
-        if (r0 + lane < a.n_req) n = prompt_len(a, r0 + lane, first);
+        int first = first0, n = n0;
+        if (r0 > 0) n = r0 + lane < a.n_req ? prompt_len(a, r0 + lane, first) : 0;
         const unsigned reach = __ballot_sync(0xffffffffu, n > lo * block);
         if (left < __popc(reach)) {
-            const unsigned mine = __ballot_sync(0xffffffffu, (reach >> lane & 1u) && __popc(reach & ((1u << lane) - 1)) == left);
-            const int l = __ffs(mine) - 1;
+            const unsigned it = __ballot_sync(0xffffffffu, (reach >> lane & 1u) && __popc(reach & ((1u << lane) - 1)) == left);
+            const int l = __ffs(it) - 1;
             job.first = __shfl_sync(0xffffffffu, first, l);
             job.n = __shfl_sync(0xffffffffu, n, l);
             job.t0 = lo * block;
@@ -121,15 +122,17 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
     volatile int* const dead = &c.dead;
 
     PromptJob ahead;
-    int levels = 0;
+    int levels = 0, n0 = 0, first0 = 0;            // n0, first0: of prompt `lane`
     if (warp == 8) {                               // (while the others set up)
         if (lane < 3) tensor_map_prefetch(lane == 0 ? &map_q : lane == 1 ? &map_k : &map_v);
-        for (int r = lane; r < a.n_req; r += 32) {
+        if (lane < a.n_req) n0 = prompt_len(a, lane, first0);
+        int longest = n0;
+        for (int r = 32 + lane; r < a.n_req; r += 32) {
             int first;
-            levels = max(levels, (prompt_len(a, r, first) + 2 * T - 1) / (2 * T));
+            longest = max(longest, prompt_len(a, r, first));
         }
-        levels = __reduce_max_sync(0xffffffffu, levels);
-        ahead = prompt_job(a, 0, 2 * T, levels);
+        levels = (__reduce_max_sync(0xffffffffu, longest) + 2 * T - 1) / (2 * T);
+        ahead = prompt_job(a, 0, 2 * T, levels, n0, first0);
     }
     if (tid == 0) {
         mbar_init(smem_u32(&c.q_full), 1);
@@ -190,8 +193,8 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
                     }
                     __syncwarp();
                     ++entry;
-                    if (e == 1) ahead = prompt_job(a, i + 1, 2 * T, levels);   // (while this job's tiles are fetched)
                 }
+                if (ok) ahead = prompt_job(a, i + 1, 2 * T, levels, n0, first0);        // (while the ring's tiles are gone through)
             }
             if (!ok && lane == 0) {                    // given up: the copies in flight are waited for
                 for (uint32_t e = entry > kStages ? entry - kStages : 0; e < entry; ++e) mbar_wait(smem_u32(&c.full[e % kStages]), (e / kStages) & 1);
@@ -297,12 +300,14 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
                     const uint32_t ev = entry + 2 * j + 1;
                     ok = warp_wait(smem_u32(&c.full[ev % kStages]), (ev / kStages) & 1, dead);
                     if (!ok) break;
-                    if (clean_values(ring + ev % kStages * kTile, kTile / 16, row, 128, [&](int p) { return j * 128 + ((p >> 3) & 127) < job.n; })) {
-                        *(volatile int*)&c.flags[i % kPromptJobs] = 1;
-                        __threadfence_block();
-                    }
-                    fence_proxy_async_smem();
-                    __syncwarp();
+                    const int all = job.t0 + s * T - j * 128;                  // the last key that every row sees
+                    clean_values<kTile / 16>(
+                        ring + ev % kStages * kTile, row,
+                        [&](int p) {
+                            const int key = p >> 3 & 127;
+                            return key <= all ? kSeenByAll : j * 128 + key < job.n ? kSeenBySome : kNoKey;
+                        },
+                        [&] { *(volatile int*)&c.flags[i % kPromptJobs] = 1; });
                 }
                 ok = warp_wait(smem_u32(&c.s_full[s]), s_phase, dead);
                 s_phase ^= 1;
@@ -329,25 +334,36 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
             tc_fence_after();
             const bool fix = *(volatile int*)&c.flags[i % kPromptJobs];
             const float inv = sum > 0.f ? 1.f / sum : sum;
-#pragma unroll 2
-            for (int d = 0; d < HD; d += 16) {
-                float o[16];
-                tmem_ld16(o_tmem + d, o);
-                tmem_ld_wait16(o);
-                if (mine) {
+            // 64 bytes of each of four rows by four lanes: a store of a piece by every row's own lane would cost a pass per row (a job of 64 columns
+            // ends 1000 clocks sooner for it)
+            const unsigned rows = __ballot_sync(0xffffffffu, mine);
+            uint4* to[4];
 #pragma unroll
-                    for (int x = 0; x < 16; ++x) o[x] *= inv;
-                    if (fix) {
-                        const int p = job.t0 >> 7 << 7;
-                        const uint32_t bad = prompt_bad<HD>(a.v + (long long)(job.first + p) * a.v_stride + job.head * HD + d, a.v_stride, t + 1 - p);
+            for (int y = 0; y < 4; ++y) to[y] = reinterpret_cast<uint4*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(out), (lane & 28) + y)) + (lane & 3);
+#pragma unroll 1
+            for (int d = 0; d < HD; d += 32) {
+                uint32_t u[32];
+                tmem_ld32(o_tmem + d, u);
+                tmem_ld_wait32(u);
+                float o[32];
+#pragma unroll
+                for (int x = 0; x < 32; ++x) o[x] = __uint_as_float(u[x]) * inv;
+                if (fix && mine) {
+                    const int p = job.t0 >> 7 << 7;
+#pragma unroll
+                    for (int h = 0; h < 32; h += 16) {
+                        const uint32_t bad = prompt_bad<HD>(a.v + (long long)(job.first + p) * a.v_stride + job.head * HD + d + h, a.v_stride, t + 1 - p);
 #pragma unroll
                         for (int x = 0; x < 16; ++x)
-                            if (bad >> x & 1u) o[x] = NAN;
+                            if (bad >> x & 1u) o[h + x] = NAN;
                     }
-#pragma unroll
-                    for (int x = 0; x < 16; x += 8) *reinterpret_cast<uint4*>(out + d + x) = bf16x8(o + x);
                 }
                 __syncwarp();
+                uint4 x[4] = {bf16x8(o), bf16x8(o + 8), bf16x8(o + 16), bf16x8(o + 24)};
+                exchange_pieces(x);
+#pragma unroll
+                for (int y = 0; y < 4; ++y)
+                    if (rows >> ((lane & 28) + y) & 1u) to[y][d / 8] = x[y];
             }
             tc_fence_before();
         }

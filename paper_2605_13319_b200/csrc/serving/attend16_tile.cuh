@@ -229,34 +229,62 @@ __device__ __forceinline__ void softmax_tile(uint32_t s_tmem, uint32_t o_tmem, f
     sum += even + odd;
 }
 
-// Values of a tile that no row may take into its products: pieces that are no key's, and what is not finite.  A weight of 0 does not keep them out, so
-// they become 0 in shared memory.  `pieces` 16-byte pieces, is_key(piece); threads of one stream.  True if something was not finite.
-template <typename IsKey>
-__device__ __forceinline__ bool clean_values(unsigned char* tile, int pieces, int tid, int n_thr, IsKey is_key) {
-    bool found = false;
-    for (int i = tid; i < pieces; i += n_thr) {
+// Values of a tile that no row may take into its products: pieces that are no key's, and what is not finite where not every row sees it.  A weight of 0
+// does not keep them out, so they become 0 in shared memory.  Done by the 128 threads of a stream; kPieces pieces of 16 bytes.  kind(piece): what the
+// piece's key is.  found(): something is not finite, said before it goes, so that who reads the 0 instead finds it said.
+enum { kSeenByAll, kSeenBySome, kNoKey };
+template <int kPieces, typename Kind, typename Found>
+__device__ __forceinline__ void clean_values(unsigned char* tile, int tid, Kind kind, Found found) {
+    constexpr int kBatch = 4;                      // loads at once
+    static_assert(kPieces % (128 * kBatch) == 0, "");
+#pragma unroll 1
+    for (int i = tid; i < kPieces; i += 128 * kBatch) {
         uint4* const at = reinterpret_cast<uint4*>(tile) + i;
-        if (!is_key(i)) {
-            *at = make_uint4(0, 0, 0, 0);
-            continue;
+        uint4 x[kBatch];
+#pragma unroll
+        for (int y = 0; y < kBatch; ++y) {
+            const int k = kind(i + 128 * y);
+            x[y] = make_uint4(0, 0, 0, 0);
+            if (k == kSeenBySome) x[y] = at[128 * y];
+            if (k == kNoKey) at[128 * y] = x[y];
         }
-        uint4 x = *at;
-        uint32_t* const w = reinterpret_cast<uint32_t*>(&x);
-        uint32_t bad = 0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) bad |= ((w[j] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-        if (bad) {
-            found = true;
+        for (int y = 0; y < kBatch; ++y) {
+            uint32_t w[4] = {x[y].x, x[y].y, x[y].z, x[y].w}, bad = 0;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t b = ((w[j] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
-                if (b & 0x8000u) w[j] &= 0xffff0000u;
-                if (b & 0x80000000u) w[j] &= 0x0000ffffu;
+            for (int j = 0; j < 4; ++j) bad |= ((w[j] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+            if (bad) {
+                found();
+                __threadfence_block();
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t b = ((w[j] & 0x7f807f80u) + 0x00800080u) & 0x80008000u;
+                    if (b & 0x8000u) w[j] &= 0xffff0000u;
+                    if (b & 0x80000000u) w[j] &= 0x0000ffffu;
+                }
+                at[128 * y] = make_uint4(w[0], w[1], w[2], w[3]);
             }
-            *at = x;
         }
     }
-    return found;
+    fence_proxy_async_smem();
+    __syncwarp();
+}
+// Four lanes have four pieces each, of a row each: afterwards piece `lane & 3` of each of the four rows.
+__device__ __forceinline__ void exchange_pieces(uint4 (&x)[4]) {
+    auto swap = [](uint4& a, uint4& b, bool odd, int lanes) {                  // a stays where odd is false, b where it is true; the other goes
+        uint4 go = odd ? a : b;
+        go.x = __shfl_xor_sync(0xffffffffu, go.x, lanes);
+        go.y = __shfl_xor_sync(0xffffffffu, go.y, lanes);
+        go.z = __shfl_xor_sync(0xffffffffu, go.z, lanes);
+        go.w = __shfl_xor_sync(0xffffffffu, go.w, lanes);
+        if (odd) a = go;
+        else b = go;
+    };
+    const bool odd = threadIdx.x & 1, high = threadIdx.x & 2;
+    swap(x[0], x[1], odd, 1);
+    swap(x[2], x[3], odd, 1);
+    swap(x[0], x[2], high, 2);
+    swap(x[1], x[3], high, 2);
 }
 // Bits of the 16 columns behind p whose value is not finite.
 __device__ __forceinline__ uint32_t not_finite16(const uint16_t* p, int piece_stride) {

@@ -40,18 +40,19 @@ int pages_cap(const pipesd_kv16_cfg* c, int32_t rows, int32_t n_q_heads) {
 }
 template <int HD, typename T>
 int32_t pages_run(PagesArgs& a, cudaStream_t st) {
-    a.keys = PagesShape<HD, T>::kKeys;
-    a.rows = PagesShape<HD, T>::kRows;
-    a.tile_pages = a.keys / a.w.page_size;
-    a.tile_over = a.keys % a.w.page_size;
+    constexpr int keys = PagesShape<HD, T>::kKeys, rows = PagesShape<HD, T>::kRows;
+    a.log_keys = keys == 128 ? 7 : 6;
+    a.log_rows = rows == 256 ? 8 : 7;
+    a.tile_pages = keys / a.w.page_size;
+    a.tile_over = keys % a.w.page_size;
     // ceil(2^(30 + L) / page_size) with 2^L >= page_size is off by less than page_size <= 2^L, so that the quotient of a position below 2^30 is exact
     int log = 0;
     while ((1 << log) < a.w.page_size) ++log;
     a.page_shift = 30 + log;
     a.page_mul = (uint32_t)(((1ull << a.page_shift) + a.w.page_size - 1) / a.w.page_size);
-    pages_attend_kernel<HD, T><<<a.ctas, kAttendThreads16, pages_smem<HD, T>(), st>>>(a);
+    pages_attend_kernel<HD, T><<<kPagesSms, kAttendThreads16, pages_smem<HD, T>(), st>>>(a);
     if (cudaGetLastError() != cudaSuccess) return PIPESD_E_CUDA;
-    if (launch_pdl(pages_merge_kernel<HD, T>, dim3(a.ctas, HD / 32, std::min<int64_t>(4, ((int64_t)a.w.rows * (a.Hq / a.w.Hkv) + 31) / 32)), dim3(32 * kPagesMergeWarps), 0, st, a) != cudaSuccess) return PIPESD_E_CUDA;
+    if (launch_pdl(pages_merge_kernel<HD, T>, dim3(kPagesSms, HD / 32, std::min<int64_t>(4, ((int64_t)a.w.rows * a.G + 31) / 32)), dim3(32 * kPagesMergeWarps), 0, st, a) != cudaSuccess) return PIPESD_E_CUDA;
     return launched();
 }
 
@@ -224,7 +225,7 @@ int32_t pipesd_kv16_attend(const pipesd_kv16_cfg* cfg, const void* pool, int32_t
     a.words = mask ? words : 0;
     a.splits = static_cast<PagesSplit*>(scratch);
     a.parts = reinterpret_cast<float*>(a.splits + kPagesSms);
-    a.ctas = kPagesSms;
+    a.G = n_q_heads / cfg->n_kv_heads;
     a.cap = pages_cap(cfg, rows, n_q_heads);
     cudaStream_t st = (cudaStream_t)cuda_stream;
     if (cfg->head_dim == 128) return dtype == PIPESD_F32 ? pages_run<128, float>(a, st) : pages_run<128, uint16_t>(a, st);
