@@ -9,6 +9,8 @@
 // rows and tiles of 64 keys, since the terms of q fill shared memory and those of the weights tensor memory.
 // Blocks of pages are operands of the products as they are (kv16.cuh): a bulk copy per page and tile, by the lanes of a warp for keys and one for values.
 #pragma once
+#include <type_traits>
+
 #include "attend16_tile.cuh"
 #include "kv16.cuh"
 
@@ -195,20 +197,25 @@ __device__ __forceinline__ uint32_t pages_see(const PagesArgs& a, const PagesJob
     return __funnelshift_r(lo, hi, sh) & below(total - start);
 }
 
-__device__ __forceinline__ void pages_load8(const uint16_t* p, bool wide, uint4 (&x)[1]) {
-    if (wide) x[0] = *reinterpret_cast<const uint4*>(p);
-    else x[0] = make_uint4(pack2(p[0], p[1]), pack2(p[2], p[3]), pack2(p[4], p[5]), pack2(p[6], p[7]));
-}
-// Three terms of eight fp32 values: what a term leaves is exact.
-__device__ __forceinline__ void pages_load8(const float* p, bool wide, uint4 (&x)[3]) {
-    float v[8];
+// Eight neighbouring values of a query row as they are (wide: aligned to 16 bytes), and as the products take them.
+template <int n, typename T>
+__device__ __forceinline__ void pages_load8(const T* p, bool wide, uint4 (&x)[n]) {
     if (wide) {
-        *reinterpret_cast<float4*>(v) = *reinterpret_cast<const float4*>(p);
-        *reinterpret_cast<float4*>(v + 4) = *reinterpret_cast<const float4*>(p + 4);
-    } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = p[i];
+        for (int h = 0; h < n; ++h) x[h] = reinterpret_cast<const uint4*>(p)[h];
+    } else if constexpr (n == 1) {
+        x[0] = make_uint4(pack2(p[0], p[1]), pack2(p[2], p[3]), pack2(p[4], p[5]), pack2(p[6], p[7]));
+    } else {
+        const uint32_t* const w = reinterpret_cast<const uint32_t*>(p);
+#pragma unroll
+        for (int h = 0; h < n; ++h) x[h] = make_uint4(w[4 * h], w[4 * h + 1], w[4 * h + 2], w[4 * h + 3]);
     }
+}
+__device__ __forceinline__ void pages_terms(const uint4 (&x)[1], uint4 (&terms)[1]) { terms[0] = x[0]; }
+// Three terms of fp32 values: what a term leaves is exact.
+__device__ __forceinline__ void pages_terms(const uint4 (&x)[2], uint4 (&terms)[3]) {
+    float v[8] = {__uint_as_float(x[0].x), __uint_as_float(x[0].y), __uint_as_float(x[0].z), __uint_as_float(x[0].w),
+                  __uint_as_float(x[1].x), __uint_as_float(x[1].y), __uint_as_float(x[1].z), __uint_as_float(x[1].w)};
 #pragma unroll
     for (int t = 0; t < 3; ++t) {
         uint32_t w[4];
@@ -218,7 +225,7 @@ __device__ __forceinline__ void pages_load8(const float* p, bool wide, uint4 (&x
             v[2 * i] -= __uint_as_float(w[i] << 16);
             v[2 * i + 1] -= __uint_as_float(w[i] & 0xffff0000u);
         }
-        x[t] = make_uint4(w[0], w[1], w[2], w[3]);
+        terms[t] = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
 // 16 neighbouring outputs.
@@ -521,47 +528,60 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
             joint_phase ^= 1;
             return there;
         };
-        for (int i = 0;; ++i) {
-            if (!warp_wait(smem_u32(&c.job_full[i & 1]), i >> 1 & 1, dead)) break;
+        // The queries of job i, in the products' order: 8 x 4 pieces of 8 columns a warp and step.  1: they are there, 0: there is no such job, -1: given up.
+        auto queries = [&](int i) {
+            if (!warp_wait(smem_u32(&c.job_full[i & 1]), i >> 1 & 1, dead)) return -1;
             const PagesJob& job = c.jobs[i & 3];
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&c.job_read[i & 1]));
-            if (job.tiles == 0) break;
-            const int n = job.tiles;
-            const bool both = job.n_rows > 128;
-            // ---- queries, in the products' order: 8 x 4 pieces of 8 columns a warp and step
-            bool ok = i == 0 || warp_wait(smem_u32(&c.q_empty), (i - 1) & 1, dead);
-            if (ok) {
-                // A thread has a piece of every kRowStep-th row.
-                constexpr int kBatch = kTerms == 1 ? 4 : 2, kRowStep = 256 / kPieces;          // loads at once
-                const int piece = warp % (kPieces / 4) * 4 + (lane >> 3), r0 = warp / (kPieces / 4) * 8 + (lane & 7);
-                int node = (job.rho0 + r0) / G, g = (job.rho0 + r0) % G;
-                const int node_step = kRowStep / G, g_step = kRowStep % G;
-                const T* const q = static_cast<const T*>(a.q) + (size_t)job.head * G * HD + piece * 8;
-                unsigned char* const to = smem + piece * 128 + (r0 & 7) * 16;
+            if (job.tiles == 0) return 0;
+            // A thread has a piece of every kRowStep-th row, several of them on their way at once.
+            constexpr int kRowStep = 256 / kPieces;
+            const int piece = warp % (kPieces / 4) * 4 + (lane >> 3), r0 = warp / (kPieces / 4) * 8 + (lane & 7);
+            int node = (job.rho0 + r0) / G, g = (job.rho0 + r0) % G;
+            const int node_step = kRowStep / G, g_step = kRowStep % G;
+            const T* const q = static_cast<const T*>(a.q) + (size_t)job.head * G * HD + piece * 8;
+            unsigned char* const to = smem + piece * 128 + (r0 & 7) * 16;
+            bool empty = i == 0;
+            auto rows = [&](auto batch, bool wide) {
+                constexpr int kBatch = decltype(batch)::value;
 #pragma unroll 1
-                for (int r = r0; r < job.n_rows; r += kBatch * kRowStep) {
-                    uint4 v[kBatch][kTerms];
+                for (int r = r0; r - r0 < job.n_rows; r += kBatch * kRowStep) {          // (as often for all of a warp)
+                    uint4 v[kBatch][sizeof(T) / 2];
 #pragma unroll
                     for (int y = 0; y < kBatch; ++y) {
-                        if (r + y * kRowStep < job.n_rows) pages_load8(q + (job.first + node) * a.q_stride + (size_t)g * HD, a.q_wide, v[y]);
+                        if (r + y * kRowStep < job.n_rows) pages_load8(q + (job.first + node) * a.q_stride + (size_t)g * HD, wide, v[y]);
                         node += node_step;
                         g += g_step;
                         if (g >= G) { g -= G; ++node; }
                     }
+                    if (!empty && !(empty = warp_wait(smem_u32(&c.q_empty), (i - 1) & 1, dead))) return;
 #pragma unroll
                     for (int y = 0; y < kBatch; ++y) {
                         const int at = r + y * kRowStep;
-                        if (at < job.n_rows)
+                        if (at < job.n_rows) {
+                            uint4 terms[kTerms];
+                            pages_terms(v[y], terms);
 #pragma unroll
-                            for (int t = 0; t < kTerms; ++t)
-                                *reinterpret_cast<uint4*>(to + (t + (at >> 7)) * Shape::kQTile + ((at & 127) >> 3) * HD * 16) = v[y][t];
+                            for (int t = 0; t < kTerms; ++t) *reinterpret_cast<uint4*>(to + (t + (at >> 7)) * Shape::kQTile + ((at & 127) >> 3) * HD * 16) = terms[t];
+                        }
                     }
                 }
-                fence_proxy_async_smem();
-            }
+            };
+            if (a.q_wide) rows(std::integral_constant<int, 4>{}, true);        // (eight at once: more code to fetch, a chain of 32 x 4096 79 -> 84 us)
+            else rows(std::integral_constant<int, 1>{}, false);
+            if (!empty) return -1;
+            fence_proxy_async_smem();
             __syncwarp();
-            if (ok && lane == 0) mbar_arrive(smem_u32(&c.q_full));
+            if (lane == 0) mbar_arrive(smem_u32(&c.q_full));
+            return 1;
+        };
+        int next = 1;                              // of the job behind the present one
+        for (int i = -1; next == 1; ++i) {         // (-1: nothing yet)
+            const PagesJob& job = c.jobs[i & 3];
+            const int n = i < 0 ? 0 : job.tiles;
+            const bool both = job.n_rows > 128;
+            bool ok = true;
             const int local = both ? 128 * s + row : row;                      // of the group's rows
             const bool mine = local < job.n_rows, any = (both ? 128 * s : 0) + 32 * (warp & 3) < job.n_rows;
             const int rho = job.rho0 + (mine ? local : 0), node = rho / G;
@@ -619,6 +639,10 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                     for (int h = 0; h < kHalves; ++h) given(h);
                 }
             }
+            // ---- the next job's queries, whose products begin while this one's sums are read
+            next = ok ? queries(i + 1) : -1;
+            if (i < 0) continue;
+            ok = next >= 0;
             // ---- the range's sums
             const bool mine_has = both || s < n;
             if (ok && mine_has) ok = warp_wait(smem_u32(&c.o_full[s]), full_phase, dead);
