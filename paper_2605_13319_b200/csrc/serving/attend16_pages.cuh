@@ -118,27 +118,31 @@ struct PagesWalk {
     PagesSplit split;
 
     __device__ __forceinline__ void begin(const PagesArgs& a) {
-        const int lane = threadIdx.x & 31;
-        const long long mine0 = pages_head(a, pages_load(a, lane)) * a.w.Hkv, inc0 = pages_scan(mine0);
-        long long all = __shfl_sync(0xffffffffu, inc0, 31);
-        for (int r0 = 32; r0 < a.w.n_req; r0 += 32) all += __shfl_sync(0xffffffffu, pages_scan(pages_head(a, pages_load(a, r0 + lane)) * a.w.Hkv), 31);
+        const int lane = threadIdx.x & 31, per = (a.w.n_req + 31) / 32;        // a lane adds up `per` neighbouring requests
+        long long mine = pages_head(a, pages_load(a, lane * per));
+#pragma unroll 4
+        for (int x = 1; x < per; ++x) mine += pages_head(a, pages_load(a, lane * per + x));
+        mine *= a.w.Hkv;
+        long long inc = pages_scan(mine);
+        const long long all = __shfl_sync(0xffffffffu, inc, 31);
         share = pages_share(all);
         f = f0 = (long long)blockIdx.x * share;
         f_end = min(f + share, all);
         split = {};
         off = f;
         req = a.w.n_req;
-        for (int r0 = 0; f < f_end && r0 < a.w.n_req; r0 += 32) {
-            long long mine = mine0, inc = inc0;
-            if (r0 > 0) {
-                mine = pages_head(a, pages_load(a, r0 + lane)) * a.w.Hkv;
-                inc = pages_scan(mine);
-            }
+        if (f >= f_end) return;
+        int l = __ffs(__ballot_sync(0xffffffffu, off < inc)) - 1;
+        off -= __shfl_sync(0xffffffffu, inc - mine, l);
+        req = l * per;
+        for (int x = 0; per > 1 && x < per; x += 32) {                         // among that lane's
+            mine = x + lane < per ? pages_head(a, pages_load(a, l * per + x + lane)) * a.w.Hkv : 0;
+            inc = pages_scan(mine);
             const unsigned hit = __ballot_sync(0xffffffffu, off < inc);
             if (hit) {
-                const int l = __ffs(hit) - 1;
-                off -= __shfl_sync(0xffffffffu, inc - mine, l);
-                req = r0 + l;
+                const int h = __ffs(hit) - 1;
+                off -= __shfl_sync(0xffffffffu, inc - mine, h);
+                req = l * per + x + h;
                 break;
             }
             off -= __shfl_sync(0xffffffffu, inc, 31);
@@ -751,11 +755,18 @@ __global__ void __launch_bounds__(32 * kPagesMergeWarps) pages_merge_kernel(cons
     pdl_wait();
     // rows of requests that have no position: nothing to see
     if (blockIdx.y == 0 && blockIdx.z == 0)
-        for (int r = blockIdx.x * blockDim.x + tid; r < a.w.n_req; r += gridDim.x * blockDim.x) {
-            int first, base;
-            const int n = kv4_rows(a.w, r, first, base), end = min(a.w.row0[r + 1], a.w.rows);
-            for (int row = max(first, 0) + n; row < end; ++row)
-                for (int d = 0; d < a.Hq * HD; ++d) pages_store(static_cast<T*>(a.out) + row * a.out_stride + d, 0.f);
+        for (int r0 = blockIdx.x * 32; r0 < a.w.n_req; r0 += gridDim.x * 32) {
+            int first = 0, base, n = 0, end = 0;
+            if (r0 + lane < a.w.n_req) {
+                n = kv4_rows(a.w, r0 + lane, first, base);
+                end = min(a.w.row0[r0 + lane + 1], a.w.rows);
+            }
+            first = max(first, 0) + n;
+            for (unsigned some = __ballot_sync(0xffffffffu, first < end); some; some &= some - 1) {
+                const int l = __ffs(some) - 1, from = __shfl_sync(0xffffffffu, first, l), to = __shfl_sync(0xffffffffu, end, l);
+                for (int row = from + warp; row < to; row += kPagesMergeWarps)
+                    for (int d = lane; d < a.Hq * HD; d += 32) pages_store(static_cast<T*>(a.out) + row * a.out_stride + d, 0.f);
+            }
         }
     const PagesSplit split = a.splits[blockIdx.x];
     const int c0 = blockIdx.x, streams = 2, shares = (split.last - c0 + 1) * (split.both ? 1 : streams), d0 = blockIdx.y * 32;

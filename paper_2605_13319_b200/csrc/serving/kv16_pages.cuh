@@ -298,7 +298,10 @@ __global__ void __launch_bounds__(kPlanThreads) kv16_plan_kernel(const Kv16PlanA
         int total, to = found + block_scan(mine, s_warp, total);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            if (f[i] && to < wanted) free_ids[to++] = p + i;
+            if (f[i] && to < wanted) {
+                copies[2 * to + 1] = -1;           // (none yet)
+                free_ids[to++] = p + i;
+            }
         found += total;
     }
     found = min(found, wanted);
@@ -367,9 +370,10 @@ __global__ void __launch_bounds__(kCopyThreads) kv16_copy_kernel(const Kv16CopyA
     const long long chunks = (a.page_pieces + kStep - 1) / kStep, items = chunks * a.n_layers * count;
     for (long long it = blockIdx.x; it < items; it += gridDim.x) {
         const long long chunk = it % chunks, rest = it / chunks;
-        const int layer = (int)(rest % a.n_layers), e = (int)(rest / a.n_layers);
-        const uint4* src = a.pool + ((long long)layer * a.n_pages + copies[2 * e]) * a.page_pieces;
-        uint4* dst = a.pool + ((long long)layer * a.n_pages + copies[2 * e + 1]) * a.page_pieces;
+        const int layer = (int)(rest % a.n_layers), e = (int)(rest / a.n_layers), from = copies[2 * e], to = copies[2 * e + 1];
+        if (to < 0 || from < 0 || from >= a.n_pages) continue;       // (a table that changed under the plan)
+        const uint4* src = a.pool + ((long long)layer * a.n_pages + from) * a.page_pieces;
+        uint4* dst = a.pool + ((long long)layer * a.n_pages + to) * a.page_pieces;
         uint4 x[kCopyUnroll];
 #pragma unroll
         for (int u = 0; u < kCopyUnroll; ++u) {
