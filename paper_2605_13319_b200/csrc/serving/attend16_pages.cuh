@@ -47,6 +47,8 @@ struct PagesArgs {
     int tile_pages, tile_over;  // keys / page_size and the remainder
     int G, cap;                 // query heads per KV head; query rows that a share has room for
     int log_keys, log_rows;     // of a tile and a row group
+    int ranges, lead;           // into which the tiles are cut; what a triple counts beside its tiles
+    int own_shares;             // of a range: two for each stream that goes through it
 };
 // The triple that goes on behind a CTA's range, as the merge needs it (rows 0: none).
 struct PagesSplit {
@@ -75,7 +77,7 @@ struct PagesRequest {
     int n, first, base, units, groups;
 };
 __device__ __forceinline__ int pages_weight(int rows) { return rows > 128 ? kPagesWideTile : kPagesTile; }
-__device__ __forceinline__ long long pages_count(int units, int rows) { return kPagesLead + (long long)units * pages_weight(rows); }
+__device__ __forceinline__ long long pages_count(const PagesArgs& a, int units, int rows) { return a.lead + (long long)units * pages_weight(rows); }
 __device__ __forceinline__ PagesRequest pages_load(const PagesArgs& a, int r) {
     PagesRequest q = {0, 0, 0, 0, 0};
     if (r >= a.w.n_req) return q;
@@ -89,7 +91,7 @@ __device__ __forceinline__ int pages_group_rows(const PagesArgs& a, const PagesR
 // All heads' triples of a request: group by group within a head.
 __device__ __forceinline__ long long pages_head(const PagesArgs& a, const PagesRequest& q) {
     if (q.groups == 0) return 0;
-    return (q.groups - 1) * pages_count(q.units, 1 << a.log_rows) + pages_count(q.units, pages_group_rows(a, q, q.groups - 1));
+    return (q.groups - 1) * pages_count(a, q.units, 1 << a.log_rows) + pages_count(a, q.units, pages_group_rows(a, q, q.groups - 1));
 }
 __device__ __forceinline__ long long pages_scan(long long v) {
     const int lane = threadIdx.x & 31;
@@ -100,8 +102,8 @@ __device__ __forceinline__ long long pages_scan(long long v) {
     }
     return v;
 }
-__device__ __forceinline__ long long pages_share(long long all) {
-    return max((all + kPagesSms - 1) / kPagesSms, (long long)kPagesWideTile);      // (every range within a triple has a tile of it)
+__device__ __forceinline__ long long pages_share(const PagesArgs& a, long long all) {
+    return max((all + a.ranges - 1) / a.ranges, (long long)kPagesWideTile);      // (every range within a triple has a tile of it)
 }
 // a / b of whole numbers, a >= 0, b > 0: the fp32 quotient is off by 2^-21 of itself and one, so that the loops run once at most below two
 // million.  (A division of 64-bit integers takes several times as long, and this is what everyone waits for first.)
@@ -111,13 +113,13 @@ __device__ __forceinline__ long long pages_div(long long a, long long b) {
     for (; r >= b; r -= b) ++q;
     return q;
 }
-// A CTA's way through its range (whole warp).
+// The way through a range (whole warp).
 struct PagesWalk {
     long long f, f0, f_end, share, off;
-    int req;
+    int req, range;
     PagesSplit split;
 
-    __device__ __forceinline__ void begin(const PagesArgs& a) {
+    __device__ __forceinline__ void begin(const PagesArgs& a, int which) {
         const int lane = threadIdx.x & 31, per = (a.w.n_req + 31) / 32;        // a lane adds up `per` neighbouring requests
         long long mine = pages_head(a, pages_load(a, lane * per));
 #pragma unroll 4
@@ -125,8 +127,9 @@ struct PagesWalk {
         mine *= a.w.Hkv;
         long long inc = pages_scan(mine);
         const long long all = __shfl_sync(0xffffffffu, inc, 31);
-        share = pages_share(all);
-        f = f0 = (long long)blockIdx.x * share;
+        share = pages_share(a, all);
+        range = which;
+        f = f0 = (long long)which * share;
         f_end = min(f + share, all);
         split = {};
         off = f;
@@ -156,14 +159,14 @@ struct PagesWalk {
             const long long head = pages_head(a, q);
             if (off >= head * a.w.Hkv) { ++req; off = 0; continue; }           // (requests without rows have nothing)
             job.head = (int)pages_div(off, head);
-            const long long full = pages_count(q.units, 1 << a.log_rows), in_head = off - job.head * head;
+            const long long full = pages_count(a, q.units, 1 << a.log_rows), in_head = off - job.head * head;
             const int group = (int)min(pages_div(in_head, full), (long long)q.groups - 1);
             job.n_rows = pages_group_rows(a, q, group);
             const int weight = pages_weight(job.n_rows);
-            const long long start = f - (in_head - group * full), count = pages_count(q.units, job.n_rows);      // of the triple
+            const long long start = f - (in_head - group * full), count = pages_count(a, q.units, job.n_rows);      // of the triple
             // tile t of it is the range's that start + lead + t * weight lies in
             auto tiles_before = [&](long long at) {
-                const unsigned long long x = max(0ll, at - start - kPagesLead);
+                const unsigned long long x = max(0ll, at - start - a.lead);
                 return (int)min((unsigned long long)q.units, weight == kPagesTile ? (x + kPagesTile - 1) / kPagesTile : (x + kPagesWideTile - 1) / kPagesWideTile);
             };
             const int u0 = f > start ? tiles_before(f) : 0, u1 = tiles_before(f_end);
@@ -175,12 +178,12 @@ struct PagesWalk {
             job.rho0 = group << a.log_rows;
             job.u0 = u0;
             job.whole = u0 == 0 && u1 == q.units;
-            job.share = 4 * blockIdx.x + (start > f0 ? 2 : 0);
+            job.share = a.own_shares * range + (start > f0 ? a.own_shares / 2 : 0);
             // without a mask no row of the group sees what lies behind its last one
             const int seen = a.mask ? q.units : min(q.units, ((q.base + (job.rho0 + job.n_rows - 1) / a.G) >> a.log_keys) + 1);
             job.tiles = max(1, min(u1, seen) - u0);                            // (a tile at least: the others' sums are none)
             if (u0 == 0 && !job.whole)
-                split = {q.first, job.head, job.rho0, job.n_rows, (int)pages_div(start + kPagesLead + (long long)(q.units - 1) * weight, share), job.share, job.n_rows > 128, 0};
+                split = {q.first, job.head, job.rho0, job.n_rows, (int)pages_div(start + a.lead + (long long)(q.units - 1) * weight, share), job.share, job.n_rows > 128, 0};
             return job;
         }
         job.tiles = 0;
@@ -291,45 +294,122 @@ struct PagesFetch {
         ids = look(window + lane);
         ids_next = look(window + 32 + lane);
     }
-    // The count-th tile that this warp fetches: which groups of eight positions of it are there.  Nothing: given up.
-    template <int HD, int kKeys, int kSlots, typename Say>
-    __device__ __forceinline__ bool tile(const PagesArgs& a, uint32_t count, unsigned char* ring, unsigned long long* full, unsigned long long* empty, volatile int* dead,
-                                         Say say) {
+    // The next tile's pages, one per lane: positions start .. end of the tile, and which groups of eight of the tile are there at all.
+    struct Piece {
+        int start, end;
+        bool there;
+        const uint16_t* src;
+        uint32_t present;
+    };
+    template <int HD, int kKeys>
+    __device__ __forceinline__ Piece look_up(const PagesArgs& a) const {
         const int lane = threadIdx.x & 31, ps = a.w.page_size;
-        const int start = max(0, lane * ps - off0), end = min(min(kKeys, (lane + 1) * ps - off0), total8 - p0), at = page0 - window + lane;
+        Piece t;
+        t.start = max(0, lane * ps - off0);
+        t.end = min(min(kKeys, (lane + 1) * ps - off0), total8 - p0);
+        const int at = page0 - window + lane;
         const int x = __shfl_sync(0xffffffffu, ids, at & 31), y = __shfl_sync(0xffffffffu, ids_next, at & 31), id = at < 32 ? x : y;
-        const bool there = start < end && id >= 0 && id < a.w.n_pages;
-        const uint16_t* const src = block + (there ? id * ((size_t)2 * a.w.Hkv * kv16_block_elems(a.w, HD)) + (size_t)(start + off0 - lane * ps) * HD : 0);
-        const uint32_t groups = there ? ((1u << ((end - start) >> 3)) - 1u) << (start >> 3) : 0u, present = __reduce_or_sync(0xffffffffu, groups);
-        say(present);
-        const RingPlace<kSlots> place(count);
-        if (count >= kSlots && !warp_wait(smem_u32(&empty[place.slot]), place.phase ^ 1, dead)) return false;
-        const uint32_t bar = smem_u32(&full[place.slot]);
-        if (lane == 0) mbar_expect_tx(bar, (uint32_t)__popc(present) * (HD * 16));
-        __syncwarp();
-        if (there) bulk_g2s(smem_u32(ring + place.slot * (kKeys * HD * 2)) + (uint32_t)start * (HD * 2), src, (uint32_t)(end - start) * (HD * 2), bar);
+        t.there = t.start < t.end && id >= 0 && id < a.w.n_pages;
+        t.src = block + (t.there ? id * ((size_t)2 * a.w.Hkv * kv16_block_elems(a.w, HD)) + (size_t)(t.start + off0 - lane * ps) * HD : 0);
+        t.present = __reduce_or_sync(0xffffffffu, t.there ? ((1u << ((t.end - t.start) >> 3)) - 1u) << (t.start >> 3) : 0u);
+        return t;
+    }
+    template <int kKeys>
+    __device__ __forceinline__ void go_on(const PagesArgs& a) {
         p0 += kKeys;
         page0 += a.tile_pages;
         off0 += a.tile_over;
-        if (off0 >= ps) { off0 -= ps; ++page0; }
+        if (off0 >= a.w.page_size) { off0 -= a.w.page_size; ++page0; }
         if (page0 - window >= 32) {
             window += 32;
             ids = ids_next;
-            ids_next = look(window + 32 + lane);
+            ids_next = look(window + 32 + (threadIdx.x & 31));
         }
-        return true;
     }
 };
+// The count-th tile that comes into a ring, when its place is free.  False: given up.
+template <int HD, int kKeys, int kSlots>
+__device__ __forceinline__ bool pages_copy(const PagesFetch::Piece& t, const uint16_t* src, uint32_t count, unsigned char* ring, unsigned long long* full,
+                                           unsigned long long* empty, volatile int* dead) {
+    const RingPlace<kSlots> place(count);
+    if (count >= kSlots && !warp_wait(smem_u32(&empty[place.slot]), place.phase ^ 1, dead)) return false;
+    const uint32_t bar = smem_u32(&full[place.slot]);
+    if ((threadIdx.x & 31) == 0) mbar_expect_tx(bar, (uint32_t)__popc(t.present) * (HD * 16));
+    __syncwarp();
+    if (t.there) bulk_g2s(smem_u32(ring + place.slot * (kKeys * HD * 2)) + (uint32_t)t.start * (HD * 2), src, (uint32_t)(t.end - t.start) * (HD * 2), bar);
+    return true;
+}
 // Given up: the copies in flight are waited for.
 template <int kSlots>
 __device__ __forceinline__ void pages_drain(uint32_t count, unsigned long long* full) {
     for (uint32_t i = count > kSlots ? count - kSlots : 0; i < count; ++i) mbar_wait(smem_u32(&full[i % kSlots]), i / kSlots & 1);
 }
 
+// Keys of pages that are not there are not seen.
+template <int kWords>
+__device__ __forceinline__ void pages_present(uint32_t present, bool masked, uint32_t (&see)[kWords]) {
+#pragma unroll
+    for (int w = 0; w < kWords; ++w) {
+        const uint32_t x = present >> (4 * w);
+        const uint32_t there = (x & 1u ? 0xffu : 0u) | (x & 2u ? 0xff00u : 0u) | (x & 4u ? 0xff0000u : 0u) | (x & 8u ? 0xff000000u : 0u);
+        see[w] = (masked ? see[w] : 0xffffffffu) & there;
+    }
+}
+template <int HD, int kKeys, typename Found>
+__device__ __forceinline__ void pages_clean(unsigned char* tile, int row, int keys, uint32_t present, Found found) {
+    clean_values<kKeys * HD / 8>(
+        tile, row,
+        [&](int p) {
+            const int key = p / HD * 8 + p % 8;    // (a group of eight keys: HD pieces)
+            return key < keys && (present >> (key >> 3) & 1u) ? kSeenBySome : kNoKey;    // (who sees all is not worth asking here)
+        },
+        found);
+}
+
+// A job's queries in the products' order, by kWarps warps: 8 x 4 pieces of 8 columns a warp and step.  empty, wait(): the place is free, wait for that.
+template <int HD, typename T, int kWarps, typename Wait>
+__device__ __forceinline__ bool pages_queries(const PagesArgs& a, const PagesJob& job, int warp, unsigned char* place, bool empty, Wait wait) {
+    // A thread has a piece of every kRowStep-th row, several of them on their way at once.
+    constexpr int kPieces = HD / 8, kTerms = PagesShape<HD, T>::kTerms, kQTile = PagesShape<HD, T>::kQTile, kRowStep = 32 * kWarps / kPieces;
+    const int lane = threadIdx.x & 31, piece = warp % (kPieces / 4) * 4 + (lane >> 3), r0 = warp / (kPieces / 4) * 8 + (lane & 7);
+    int node = (job.rho0 + r0) / a.G, g = (job.rho0 + r0) % a.G;
+    const int node_step = kRowStep / a.G, g_step = kRowStep % a.G;
+    const T* const q = static_cast<const T*>(a.q) + (size_t)job.head * a.G * HD + piece * 8;
+    unsigned char* const to = place + piece * 128 + (r0 & 7) * 16;
+    auto rows = [&](auto batch, bool wide) {
+        constexpr int kBatch = decltype(batch)::value;
+#pragma unroll 1
+        for (int r = r0; r - r0 < job.n_rows; r += kBatch * kRowStep) {        // (as often for all of a warp)
+            uint4 v[kBatch][sizeof(T) / 2];
+#pragma unroll
+            for (int y = 0; y < kBatch; ++y) {
+                if (r + y * kRowStep < job.n_rows) pages_load8(q + (job.first + node) * a.q_stride + (size_t)g * HD, wide, v[y]);
+                node += node_step;
+                g += g_step;
+                if (g >= a.G) { g -= a.G; ++node; }
+            }
+            if (!empty && !(empty = wait())) return;
+#pragma unroll
+            for (int y = 0; y < kBatch; ++y) {
+                const int at = r + y * kRowStep;
+                if (at < job.n_rows) {
+                    uint4 terms[kTerms];
+                    pages_terms(v[y], terms);
+#pragma unroll
+                    for (int t = 0; t < kTerms; ++t) *reinterpret_cast<uint4*>(to + (t + (at >> 7)) * kQTile + ((at & 127) >> 3) * HD * 16) = terms[t];
+                }
+            }
+        }
+    };
+    if (a.q_wide) rows(std::integral_constant<int, 4>{}, true);                // (eight at once: more code to fetch, a chain of 32 x 4096 79 -> 84 us)
+    else rows(std::integral_constant<int, 1>{}, false);
+    return empty;
+}
+
 template <int HD, typename T>
 __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const __grid_constant__ PagesArgs a) {
     using Shape = PagesShape<HD, T>;
-    constexpr int kKeys = Shape::kKeys, kTile = Shape::kTile, kKSlots = Shape::kKSlots, kVSlots = Shape::kVSlots, kTerms = Shape::kTerms, kPieces = HD / 8;
+    constexpr int kKeys = Shape::kKeys, kTile = Shape::kTile, kKSlots = Shape::kKSlots, kVSlots = Shape::kVSlots, kTerms = Shape::kTerms;
     constexpr int kHalves = Shape::kHalves;        // in which a tile's weights go over
     constexpr bool kOwn = Shape::kWide;            // the threads add up the tiles' sums
     constexpr uint32_t kIdescS = umma_idesc_bf16(128, kKeys, 0, 0), kIdescO = umma_idesc_bf16(128, HD, 0, 1);
@@ -344,7 +424,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
     pdl_launch_dependents();
 
     PagesWalk walk;
-    if (warp == 8) walk.begin(a);                  // (while the others set up)
+    if (warp == 8) walk.begin(a, blockIdx.x);                  // (while the others set up)
     if (tid == 0) {
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&c.job_full[i]), 1);
@@ -408,9 +488,10 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                     fetch = fetch_next;
                     j = 0;
                 }
-                ok = ok && fetch.tile<HD, kKeys, kKSlots>(a, count, k_ring, c.k_full, c.k_empty, dead, [&](uint32_t present) {
-                    if (lane == 0) c.present[count & 31] = present;
-                });
+                const PagesFetch::Piece t = fetch.look_up<HD, kKeys>(a);
+                if (lane == 0) c.present[count & 31] = t.present;
+                ok = ok && pages_copy<HD, kKeys, kKSlots>(t, t.src, count, k_ring, c.k_full, c.k_empty, dead);
+                fetch.go_on<kKeys>(a);
                 count += ok;
                 find = ++j == min(2, n);
             }
@@ -430,7 +511,9 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                 if (lane == 0) mbar_arrive(smem_u32(&c.job_read[i & 1]));
                 if (n == 0) break;
                 for (int j = 0; j < n && ok; ++j) {
-                    ok = fetch.tile<HD, kKeys, kVSlots>(a, count, v_ring, c.v_full, c.v_empty, dead, [](uint32_t) {});
+                    const PagesFetch::Piece t = fetch.look_up<HD, kKeys>(a);
+                    ok = pages_copy<HD, kKeys, kVSlots>(t, t.src, count, v_ring, c.v_full, c.v_empty, dead);
+                    fetch.go_on<kKeys>(a);
                     count += ok;
                 }
             }
@@ -539,42 +622,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&c.job_read[i & 1]));
             if (job.tiles == 0) return 0;
-            // A thread has a piece of every kRowStep-th row, several of them on their way at once.
-            constexpr int kRowStep = 256 / kPieces;
-            const int piece = warp % (kPieces / 4) * 4 + (lane >> 3), r0 = warp / (kPieces / 4) * 8 + (lane & 7);
-            int node = (job.rho0 + r0) / G, g = (job.rho0 + r0) % G;
-            const int node_step = kRowStep / G, g_step = kRowStep % G;
-            const T* const q = static_cast<const T*>(a.q) + (size_t)job.head * G * HD + piece * 8;
-            unsigned char* const to = smem + piece * 128 + (r0 & 7) * 16;
-            bool empty = i == 0;
-            auto rows = [&](auto batch, bool wide) {
-                constexpr int kBatch = decltype(batch)::value;
-#pragma unroll 1
-                for (int r = r0; r - r0 < job.n_rows; r += kBatch * kRowStep) {          // (as often for all of a warp)
-                    uint4 v[kBatch][sizeof(T) / 2];
-#pragma unroll
-                    for (int y = 0; y < kBatch; ++y) {
-                        if (r + y * kRowStep < job.n_rows) pages_load8(q + (job.first + node) * a.q_stride + (size_t)g * HD, wide, v[y]);
-                        node += node_step;
-                        g += g_step;
-                        if (g >= G) { g -= G; ++node; }
-                    }
-                    if (!empty && !(empty = warp_wait(smem_u32(&c.q_empty), (i - 1) & 1, dead))) return;
-#pragma unroll
-                    for (int y = 0; y < kBatch; ++y) {
-                        const int at = r + y * kRowStep;
-                        if (at < job.n_rows) {
-                            uint4 terms[kTerms];
-                            pages_terms(v[y], terms);
-#pragma unroll
-                            for (int t = 0; t < kTerms; ++t) *reinterpret_cast<uint4*>(to + (t + (at >> 7)) * Shape::kQTile + ((at & 127) >> 3) * HD * 16) = terms[t];
-                        }
-                    }
-                }
-            };
-            if (a.q_wide) rows(std::integral_constant<int, 4>{}, true);        // (eight at once: more code to fetch, a chain of 32 x 4096 79 -> 84 us)
-            else rows(std::integral_constant<int, 1>{}, false);
-            if (!empty) return -1;
+            if (!pages_queries<HD, T, 8>(a, job, warp, smem, i == 0, [&] { return warp_wait(smem_u32(&c.q_empty), (i - 1) & 1, dead); })) return -1;
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&c.q_full));
@@ -606,12 +654,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                 tc_fence_after();
                 const uint32_t present = c.present[(tile_no + j) & 31];        // eight positions a bit
                 if (present != (kKeys == 128 ? 0xffffu : 0xffu)) {
-#pragma unroll
-                    for (int w = 0; w < kKeys / 32; ++w) {
-                        const uint32_t x = present >> (4 * w);
-                        const uint32_t there = (x & 1u ? 0xffu : 0u) | (x & 2u ? 0xff00u : 0u) | (x & 4u ? 0xff0000u : 0u) | (x & 8u ? 0xff000000u : 0u);
-                        see[w] = (masked ? see[w] : 0xffffffffu) & there;
-                    }
+                    pages_present(present, masked, see);
                     masked = true;
                 }
                 if (masked) {
@@ -619,16 +662,10 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                     ok = warp_wait(smem_u32(&c.v_full[v.slot]), v.phase, dead);
                     if (!ok) break;
                     const int keys = job.base + job.n - p0;
-                    clean_values<kTile / 16>(
-                        v_ring + v.slot * kTile, row,
-                        [&](int p) {
-                            const int key = p / kPieces / 8 * 8 + p % 8;
-                            return key < keys && (present >> (key >> 3) & 1u) ? kSeenBySome : kNoKey;      // (who sees all is not worth asking here)
-                        },
-                        [&] {
-                            atomicMin(&c.bad_lo[i & 3], u);
-                            atomicMax(&c.bad_hi[i & 3], u);
-                        });
+                    pages_clean<HD, kKeys>(v_ring + v.slot * kTile, row, keys, present, [&] {
+                        atomicMin(&c.bad_lo[i & 3], u);
+                        atomicMax(&c.bad_hi[i & 3], u);
+                    });
                 }
                 auto given = [&](int h) {
                     tc_fence_before();
@@ -769,15 +806,15 @@ __global__ void __launch_bounds__(32 * kPagesMergeWarps) pages_merge_kernel(cons
             }
         }
     const PagesSplit split = a.splits[blockIdx.x];
-    const int c0 = blockIdx.x, streams = 2, shares = (split.last - c0 + 1) * (split.both ? 1 : streams), d0 = blockIdx.y * 32;
+    const int c0 = blockIdx.x, streams = split.both ? 1 : a.own_shares / 2, shares = (split.last - c0 + 1) * streams, d0 = blockIdx.y * 32;
     for (int r0 = blockIdx.z * 32; r0 < split.rows; r0 += 32 * gridDim.z) {
         const int local = r0 + lane;
         const bool mine = local < split.rows;
         // A row's shares: of every CTA, and, unless each has rows of its own, of both streams.
         const int slot = mine ? (split.both ? local & 127 : local) : 0;
         auto share = [&](int i) {
-            const int c = split.both ? i : i >> 1, s = split.both ? local >> 7 : i & 1;
-            return a.parts + (size_t)((c == 0 ? split.share : 4 * (c0 + c)) + s) * a.cap * (HD + 2);
+            const int c = i / streams, s = split.both ? local >> 7 : i % streams;
+            return a.parts + (size_t)((c == 0 ? split.share : a.own_shares * (c0 + c)) + s) * a.cap * (HD + 2);
         };
         float top = -INFINITY, sum = 0.f, v[32] = {};
 #pragma unroll 2

@@ -3,6 +3,7 @@
 #include <mutex>
 
 #include "../../../include/pipesd.h"
+#include "attend16_apart.cuh"
 #include "attend16_pages.cuh"
 #include "attend16_prompt.cuh"
 #include "kv16_pages.cuh"
@@ -43,6 +44,9 @@ int32_t pages_run(PagesArgs& a, cudaStream_t st) {
     constexpr int keys = PagesShape<HD, T>::kKeys, rows = PagesShape<HD, T>::kRows;
     a.log_keys = keys == 128 ? 7 : 6;
     a.log_rows = rows == 256 ? 8 : 7;
+    a.ranges = kPagesSms;
+    a.lead = kPagesLead;
+    a.own_shares = 4;
     a.tile_pages = keys / a.w.page_size;
     a.tile_over = keys % a.w.page_size;
     // ceil(2^(30 + L) / page_size) with 2^L >= page_size is off by less than page_size <= 2^L, so that the quotient of a position below 2^30 is exact
@@ -50,9 +54,23 @@ int32_t pages_run(PagesArgs& a, cudaStream_t st) {
     while ((1 << log) < a.w.page_size) ++log;
     a.page_shift = 30 + log;
     a.page_mul = (uint32_t)(((1ull << a.page_shift) + a.w.page_size - 1) / a.w.page_size);
-    pages_attend_kernel<HD, T><<<kPagesSms, kAttendThreads16, pages_smem<HD, T>(), st>>>(a);
+    bool apart = false;
+    if constexpr (keys == 128) {
+        // Streams with triples of their own where requests have up to 64 query rows by KV head on average.  Together and apart, us, 8 KV heads of 128:
+        // 4 rows, 256 requests behind 512 positions 203 and 147, 8 behind 16384 95 and 92; 32 rows, 8 behind 4096 39.5 and 38; 64 rows, 4 behind
+        // 8192 41 and 42, one behind 2048 (32 KV heads) 25 and 23.5; 128 rows, 16 behind 2048 58 and 62.
+        apart = (int64_t)a.w.rows * a.G <= 64 * (int64_t)a.w.n_req;
+        if (apart) {
+            a.log_rows = 7;
+            a.ranges = 2 * kPagesSms;
+            a.lead = kApartLead;
+            a.own_shares = 2;
+            pages_apart_kernel<HD><<<kPagesSms, kAttendThreads16, apart_smem<HD>(), st>>>(a);
+        }
+    }
+    if (!apart) pages_attend_kernel<HD, T><<<kPagesSms, kAttendThreads16, pages_smem<HD, T>(), st>>>(a);
     if (cudaGetLastError() != cudaSuccess) return PIPESD_E_CUDA;
-    if (launch_pdl(pages_merge_kernel<HD, T>, dim3(kPagesSms, HD / 32, std::min<int64_t>(4, ((int64_t)a.w.rows * a.G + 31) / 32)), dim3(32 * kPagesMergeWarps), 0, st, a) != cudaSuccess) return PIPESD_E_CUDA;
+    if (launch_pdl(pages_merge_kernel<HD, T>, dim3(a.ranges, HD / 32, std::min<int64_t>(4, ((int64_t)a.w.rows * a.G + 31) / 32)), dim3(32 * kPagesMergeWarps), 0, st, a) != cudaSuccess) return PIPESD_E_CUDA;
     return launched();
 }
 
@@ -85,7 +103,7 @@ bool attend_ready(const void* kernel, int smem) {
     return cudaFuncGetAttributes(&at, kernel) == cudaSuccess && at.numRegs == kLaunchRegisters &&
            cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) == cudaSuccess;
 }
-static_assert(PromptShape<128>::kSmem <= 232448 && PromptShape<64>::kSmem <= 232448, "a CTA's shared memory");
+static_assert(apart_smem<64>() <= 232448 && apart_smem<128>() <= 232448 && PromptShape<128>::kSmem <= 232448 && PromptShape<64>::kSmem <= 232448, "a CTA's shared memory");
 template <int HD, typename T>
 bool pages_ready() {
     static_assert(pages_smem<HD, T>() <= 232448, "a CTA's shared memory");
@@ -97,7 +115,8 @@ bool device_ready() {
     std::lock_guard<std::mutex> lock(g_mu);
     if (!g_ready[dev])
         g_ready[dev] = attend_ready((const void*)prompt_kernel<64>, PromptShape<64>::kSmem) && attend_ready((const void*)prompt_kernel<128>, PromptShape<128>::kSmem) &&
-                       pages_ready<64, float>() && pages_ready<64, uint16_t>() && pages_ready<128, float>() && pages_ready<128, uint16_t>();
+                       pages_ready<64, float>() && pages_ready<64, uint16_t>() && pages_ready<128, float>() && pages_ready<128, uint16_t>() &&
+                       attend_ready((const void*)pages_apart_kernel<64>, apart_smem<64>()) && attend_ready((const void*)pages_apart_kernel<128>, apart_smem<128>());
     return g_ready[dev];
 }
 
@@ -196,7 +215,7 @@ int32_t pipesd_kv16_release(const pipesd_kv16_cfg* cfg, int32_t n_req, const int
 
 uint64_t pipesd_kv16_attend_scratch_bytes(const pipesd_kv16_cfg* cfg, int32_t rows, int32_t n_q_heads) {
     if (!cfg_ok(cfg) || rows < 1 || n_q_heads < 1 || n_q_heads % cfg->n_kv_heads || n_q_heads / cfg->n_kv_heads > 128) return 0;
-    return kPagesSms * (sizeof(PagesSplit) + (uint64_t)4 * pages_cap(cfg, rows, n_q_heads) * (cfg->head_dim + 2) * 4);
+    return kPagesSms * (2 * sizeof(PagesSplit) + (uint64_t)4 * pages_cap(cfg, rows, n_q_heads) * (cfg->head_dim + 2) * 4);
 }
 
 int32_t pipesd_kv16_attend(const pipesd_kv16_cfg* cfg, const void* pool, int32_t layer, const void* q, void* out, int32_t dtype, int64_t q_stride,
@@ -224,7 +243,7 @@ int32_t pipesd_kv16_attend(const pipesd_kv16_cfg* cfg, const void* pool, int32_t
     a.mask = mask;
     a.words = mask ? words : 0;
     a.splits = static_cast<PagesSplit*>(scratch);
-    a.parts = reinterpret_cast<float*>(a.splits + kPagesSms);
+    a.parts = reinterpret_cast<float*>(a.splits + 2 * kPagesSms);
     a.G = n_q_heads / cfg->n_kv_heads;
     a.cap = pages_cap(cfg, rows, n_q_heads);
     cudaStream_t st = (cudaStream_t)cuda_stream;

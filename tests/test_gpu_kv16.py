@@ -434,6 +434,71 @@ def test_attend_strides_streams_and_graphs():
         c.fill()
 
 
+@pytest.mark.parametrize("new,base,heads,kvh,hd,page", [
+    ([1] * 400, [int(x) for x in np.linspace(0, 800, 400)], 8, 2, 64, 16), ([100] + [1] * 40, [300] + [129] * 40, 8, 2, 128, 16),
+    ([0] * 70 + [3] * 70, [50] * 70 + [int(x) for x in np.linspace(0, 500, 70)], 6, 2, 128, 24), ([16] * 9, [200] * 9, 4, 1, 128, 8),
+    ([17] * 9, [200] * 9, 4, 1, 128, 8), ([2] * 1500, [30] * 1500, 2, 1, 64, 16), ([0, 0, 1, 0], [5, 6000, 5000, 0], 32, 8, 128, 64),
+    ([64], [1000], 8, 8, 128, 16), ([65], [1000], 8, 8, 128, 16), ([1], [0], 64, 1, 64, 16)])
+def test_many_requests_with_few_rows(new, base, heads, kvh, hd, page):
+    """Up to 64 query rows by KV head a request on average, and just beyond; groups of more than 128 rows among them; requests without rows."""
+    import torch
+    c = Case(len(new), new, base, heads, kvh, hd, page)
+    c.fill()
+    for mask in (None, c.trees(-(-max(new) // 32))):
+        q = c.queries(torch.bfloat16)
+        out = c.attend(q, mask)
+        c.check(q, mask, out)
+        assert all(torch.equal(out, c.attend(q, mask)) for _ in range(5))
+        side = torch.cuda.Stream()
+        torch.cuda.synchronize()
+        both = [c.attend(q, mask, stream=st) for _ in range(4) for st in (None, side)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(out, x) for x in both)
+
+
+def test_few_rows_scores_that_grow_and_graphs():
+    import torch
+    c = Case(17, [20, 1, 0, 5], [700, 30, 0, 256], 4, 2, 128)
+    c.k[0] *= (torch.arange(720, device="cuda") * 0.05)[:, None, None]
+    c.fill()
+    q, mask = c.queries(torch.bfloat16), c.trees(1)
+    bits = _ints(mask.view(np.int32))
+    c.check(q, mask, c.attend(q, mask))
+    odd = torch.full((c.rows, 4 * 128 + 1), 3.0, device="cuda", dtype=q.dtype)[:, 1:].unflatten(1, (4, 128))       # rows at odd addresses
+    want = c.attend(q, mask)
+    assert torch.equal(c.attend(q, mask, out=odd), want) and torch.equal(c.attend(odd.copy_(q), mask), want)
+    graphs, outs = [], []
+    for _ in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(c.cache.attend(q, *c.where, mask=bits))
+        graphs.append(g)
+    for shift in (0, -25, -30):
+        c.where[1].copy_(_ints([700 + shift, 30 + shift, 0, 256 + shift]))
+        for g in (graphs[1], graphs[0], graphs[1]):
+            g.replay()
+        torch.cuda.synchronize()
+        want = c.cache.attend(q, *c.where, mask=bits)
+        assert torch.equal(outs[0], want) and torch.equal(outs[1], want)
+
+
+def test_rows_of_requests_without_positions():
+    """A base below 0 or behind the table: zeros, however many rows; the other requests' rows are theirs."""
+    import torch
+    for heads in (4, 8):                           # few rows and many
+        c = Case(19, [7] * 40 + [30], [100] * 41, heads, 2, 64)
+        c.fill()
+        q = c.queries(torch.bfloat16)
+        want = c.attend(q, None)
+        c.where[1][[3, 20, 40]] = _ints([-1, 10 ** 6, -2 ** 31])
+        out = c.attend(q, None, out=torch.full_like(q, 5.0))
+        gone = [*range(21, 28), *range(140, 147), *range(280, 310)]
+        assert (out[gone] == 0).all()
+        want[gone] = 0
+        c.where[1][[3, 20, 40]] = 100
+        assert torch.equal(out == 0, want == 0) and ((out.double() - want.double()).norm() < 2.0 ** -7 * want.double().norm())
+
+
 def test_offsets_beyond_32_bits():
     """A pool of 10 GB, 5 * 10^9 values: a request whose pages lie at its end."""
     import torch

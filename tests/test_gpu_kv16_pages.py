@@ -95,6 +95,21 @@ def test_fork_without_enough_pages():
     p.fork([0, 0], [2, 3], [64, 40], [0, 32])
 
 
+def test_fork_of_slots_that_are_targets_too():
+    """Not served in any set way (no dst is a src within a call), but pages of other slots stay what they were."""
+    import torch
+    p = Pages(8, 9, 6, 60)
+    p.reserve([96, 96, 80, 0, 0, 0, 0, 0, 50])
+    before = p.cache.pool.clone()
+    for src, dst in (([0, 1, 2, 3, 4], [1, 2, 3, 4, 5]), ([3, 2, 1], [2, 1, 0]), ([0, 0], [3, 3])):
+        pages = p.cache.fork(_ints(src), _ints(dst), _ints([90] * len(src)), _ints([20] * len(src)), p.d_table, p.d_refs)
+        assert ((pages == -1) | (pages == 6)).all()
+    table = p.d_table.cpu().numpy()
+    assert ((table >= -1) & (table < 60)).all() and np.array_equal(table[8], p.table[8])
+    for page in table[8][:4]:
+        assert torch.equal(p.cache.pool[:, page].view(torch.int16), before[:, page].view(torch.int16))
+
+
 def test_fork_of_many_and_large_pools():
     import torch
     p = Pages(3, 300, 3, 3000, page=8, layers=1, kvh=1)
