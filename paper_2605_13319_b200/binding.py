@@ -707,9 +707,8 @@ def tree_mask(parent, row0, words: int, *, stream=None):
     dev, rows, n_req = parent.device, parent.numel(), row0.numel() - 1
     on = _on(dev, stream, parent, row0)
     with on as st:
-        both = torch.empty(rows * (words + 1), dtype=torch.int32, device=dev)
-        mask, depth = both[rows:].view(rows, words), both[:rows]
-        on.made(both)
+        mask, depth = torch.empty((rows, words), dtype=torch.int32, device=dev), torch.empty(rows, dtype=torch.int32, device=dev)
+        on.made(mask, depth)
         rc = lib().pipesd_tree_mask(n_req, rows, _vector(row0, n_req + 1, torch.int32, dev, "row0"), _vector(parent, rows, torch.int32, dev, "parent"), words,
                                     mask.data_ptr(), depth.data_ptr(), st)
     if rc != OK:
@@ -821,9 +820,9 @@ class Kv16Cache:
         cfg, on = self._cfg(table.shape[1]), _on(dev, stream, self.pool, table, refs, *given)
 
         def room():
-            whole = torch.empty(n + int(lib().pipesd_kv16_plan_scratch_bytes(ctypes.byref(cfg), n)) // 4 + 4, dtype=torch.int32, device=dev)
-            on.made(whole)
-            return whole[:n], whole[n:]
+            pages = torch.empty(n, dtype=torch.int32, device=dev)
+            on.made(pages)
+            return pages, torch.empty(int(lib().pipesd_kv16_plan_scratch_bytes(ctypes.byref(cfg), n)) or 16, dtype=torch.uint8, device=dev)
 
         return cfg, self._ints(table, table.numel(), "table"), self._ints(refs, self.n_pages, "refs"), on, room
 

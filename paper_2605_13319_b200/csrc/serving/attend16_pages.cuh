@@ -103,7 +103,7 @@ __device__ __forceinline__ long long pages_scan(long long v) {
     return v;
 }
 __device__ __forceinline__ long long pages_share(const PagesArgs& a, long long all) {
-    return max((all + a.ranges - 1) / a.ranges, (long long)kPagesWideTile);      // (every range within a triple has a tile of it)
+    return max((all + a.ranges - 1) / a.ranges, a.log_rows > 7 ? (long long)kPagesWideTile : (long long)kPagesTile);      // (every range within a triple has a tile of it)
 }
 // a / b of whole numbers, a >= 0, b > 0: the fp32 quotient is off by 2^-21 of itself and one, so that the loops run once at most below two
 // million.  (A division of 64-bit integers takes several times as long, and this is what everyone waits for first.)
