@@ -446,7 +446,7 @@ int32_t pipesd_kv16_read(const pipesd_kv16_cfg *cfg, const void *pool, int32_t l
  * n_q_heads a multiple of n_kv_heads, up to 128 times as many; scale > 0, every score times scale below 2^120 in magnitude.  Sums are fp32.  bf16:
  * q as it is, probabilities in bf16; fp32: q and probabilities as three bf16 terms each (24 bits).  A row that sees no position gives 0, a
  * head's row whose q has a NaN a NaN; rows of no request are left as they are.  A NaN or an infinity in the cache reaches the rows that
- * see it, as for prompts.  out must not overlap q.  The order of sums goes by the lengths and by the number of rows.  scratch:
+ * see it, as for prompts.  out must not overlap q.  The order of sums goes by the lengths and by the numbers of rows and requests.  scratch:
  * pipesd_kv16_attend_scratch_bytes bytes (0 for arguments that are refused), 16-byte aligned; it holds nothing between calls, but two
  * calls that may run at the same time need one each. */
 uint64_t pipesd_kv16_attend_scratch_bytes(const pipesd_kv16_cfg *cfg, int32_t rows, int32_t n_q_heads);

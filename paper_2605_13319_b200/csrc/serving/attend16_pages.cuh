@@ -8,6 +8,10 @@
 // the triple, in tensor memory, where each stream reads the other's, half of the columns each.  fp32: q and weights as three bf16 terms, groups of 128
 // rows and tiles of 64 keys, since the terms of q fill shared memory and those of the weights tensor memory.
 // Blocks of pages are operands of the products as they are (kv16.cuh): a bulk copy per page and tile, by the lanes of a warp for keys and one for values.
+//
+// Bound by the cache's bytes where rows are few and caches long: 32 rows behind 131040 positions (128 query rows by KV head) 109 us, 4.9 TB/s; by the chain
+// of a triple's beginning and end where they are short: until the first scores 9000 clocks, 4500 from the last weights to the sums' end, 3300 to 3900 a tile of
+// 256 rows between them (16 requests of 8 to 64 nodes behind 256 to 8192 positions: 120 us, 52 of bytes).  The merge adds 6 to 10.
 #pragma once
 #include <type_traits>
 
@@ -17,7 +21,8 @@
 namespace pipesd {
 
 constexpr int kPagesSms = 148;
-// What a triple counts in the ranges: a lead, and every tile; a tile whose rows fill both streams counts more.
+// What a triple counts in the ranges: a lead, and every tile; a tile whose rows fill both streams counts more.  As measured: 13000 clocks, 2200 and 3900.
+// (No lead: 32 single tokens behind up to 4096 positions took 117 us instead of 83; 12 or 24 instead of 18: 16 ragged trees 122 instead of 120.)
 constexpr int kPagesLead = 18, kPagesTile = 3, kPagesWideTile = 5;
 
 template <int HD, typename T>
@@ -41,8 +46,8 @@ struct PagesArgs {
     float scale;                // times log2(e)
     const uint32_t* mask;       // [rows][words], null: a row sees the new rows up to itself
     int words;
-    struct PagesSplit* splits;  // [CTAs]
-    float* parts;               // [4 * CTAs] of {sums [HD / 4][cap][4], references [cap], denominators [cap]}: of a CTA's first range and of a later one, by stream
+    struct PagesSplit* splits;  // [ranges]
+    float* parts;               // [own_shares * ranges] of {sums [HD / 4][cap][4], references [cap], denominators [cap]}: of a range's first triple and of a later one, by stream
     uint32_t page_mul, page_shift;                       // position / page_size = position * page_mul >> page_shift, for positions below 2^30
     int tile_pages, tile_over;  // keys / page_size and the remainder
     int G, cap;                 // query heads per KV head; query rows that a share has room for
@@ -50,9 +55,9 @@ struct PagesArgs {
     int ranges, lead;           // into which the tiles are cut; what a triple counts beside its tiles
     int own_shares;             // of a range: two for each stream that goes through it
 };
-// The triple that goes on behind a CTA's range, as the merge needs it (rows 0: none).
+// The triple that goes on behind a range, as the merge needs it (rows 0: none).
 struct PagesSplit {
-    int first, head, rho0, rows, last, share, both, pad;     // last: its last CTA; share: where this CTA's sums are
+    int first, head, rho0, rows, last, share, both, pad;     // last: its last range; share: where this one's sums are
 };
 struct PagesJob {
     int req, n, first, base, head, rho0, n_rows, tiles;      // tiles: 0 = no more jobs
@@ -401,7 +406,7 @@ __device__ __forceinline__ bool pages_queries(const PagesArgs& a, const PagesJob
             }
         }
     };
-    if (a.q_wide) rows(std::integral_constant<int, 4>{}, true);                // (eight at once: more code to fetch, a chain of 32 x 4096 79 -> 84 us)
+    if (a.q_wide) rows(std::integral_constant<int, 4>{}, true);                // (eight at once: more code to fetch, 32 single tokens behind up to 4096 positions 79 -> 84 us)
     else rows(std::integral_constant<int, 1>{}, false);
     return empty;
 }
@@ -780,8 +785,9 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
     }
 }
 
-// Adds up the shares of triples that several CTAs had.  A CTA per (CTA whose range ends within a triple, 32 columns), rows by 32: a warp per eighth of the
-// shares, a lane per row, whose shares lie side by side; each warp keeps a maximum of its own, and their sums are added in order.  grid: CTAs, HD / 32, 1 to 4.
+// Adds up the shares of triples that several ranges had.  A CTA per (range that ends within a triple, 32 columns), rows by 32: a warp per eighth of the
+// shares, a lane per row, whose shares lie side by side; each warp keeps a maximum of its own, and their sums are added in order.  grid: ranges, HD / 32, 1 to 4.  A
+// chain of loads (record, shares) behind the last range: 6 to 10 us.  A warp per 32 rows where shares are few: 113 registers instead of 80, 3 to 8 us slower.
 constexpr int kPagesMergeWarps = 8;
 template <int HD, typename T>
 __global__ void __launch_bounds__(32 * kPagesMergeWarps) pages_merge_kernel(const __grid_constant__ PagesArgs a) {

@@ -1,4 +1,4 @@
-// What both bf16 attention kernels (prompts, pages) do with a tile of 128 query rows by kKeys keys on the 5th-generation tensor cores.
+// What the bf16 attention kernels (prompts; pages, together and apart) do with a tile of 128 query rows by kKeys keys on the 5th-generation tensor cores.
 //
 //   S[128 x kKeys] = Q K^T        both operands in shared memory, fp32 scores in tensor memory, a lane per query row
 //   P = exp2(scale S - ref)       one thread per row: its scores in registers, no exchange between threads.  ref is the row's running
@@ -8,6 +8,12 @@
 //
 // Two such streams per CTA, each with four warps of its own and a thread that issues its products: while one stream's exponentials are taken the tensor
 // cores do the other's products.  P goes over in halves, so that the first half's products run beside the second's exponentials.
+//
+// What bounds it, for two streams of 128 rows by 128 keys with heads of 128: the products 2048 clocks (S = Q K^T of 64 clocks a k16 step, P V the same), the
+// exponentials 2048 clocks too (the special-function units take 16 a clock), 3500 measured in a long prompt: the hand-over from one to the other, some
+// 1000 clocks a tile and stream, is covered by the other stream only in part.  A tile of one stream with few rows, so with one warp at work, takes that warp
+// 3300 clocks.  Steps of 64 keys with two places for the scores: a prompt of 16384 2133 us instead of 1984; two threads a row: 2222; a quarter of
+// the exponentials as polynomials on the FMA pipe: 1830 instead of 1728 (short runs).
 #pragma once
 #include "../tcgen05.cuh"
 
