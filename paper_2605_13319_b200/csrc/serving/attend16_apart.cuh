@@ -5,6 +5,10 @@
 // read, joined and written, the next queries) than on tiles.  Here a stream has a range, a ring and a warp that fetches for it, and nothing to
 // wait for in the other, so that one stream's tiles come in while the other ends a triple.
 // Warps: 0-3 and 4-7 the streams' rows, 8 and 10 fetch a stream's keys and values, 9 and 11 issue its products.
+//
+// Bound by the cache's bytes behind long contexts (32 single tokens behind 256 to 4096 positions 73 us, 4.5 TB/s, 6.9 while tiles flow; one behind 131072 93 us,
+// 5.8 TB/s), else by a stream's own chain: 3300 clocks of one warp for a tile's 128 exponentials a row and what goes with them, 1200 until the next
+// scores, 6000 for a triple's end and the next one's beginning (256 behind 512: 128 us, 4.2 TB/s).
 #pragma once
 #include "attend16_pages.cuh"
 
@@ -187,14 +191,16 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_apart_kernel(const 
         }
     } else {                                       // ---- a stream's rows
         registers_more();
-        const int row = tid & 127;
+        // Few rows are one warp's work: those of stream 1 lie 64 lanes further on, so that it is a warp of another scheduler
+        // (256 single tokens behind 512 positions 146 -> 128 us).
+        const int turn = 64 * s, row = (tid & 127) ^ turn;
         const uint32_t lanes = (uint32_t)(32 * (warp & 3)) << 16, s_tmem = s_tile + lanes, o_tmem = o_tile + lanes;
         uint32_t tile_no = 0, s_phase = 0, full_phase = 0;                     // tile_no: tiles of the jobs before
         int next = 1;                              // of the job behind the present one: 1: its queries are there, 0: there is none, -1: given up
         for (int i = -1; next == 1; ++i) {         // (-1: nothing yet)
             const PagesJob& job = c.jobs[i & 3];
             const int n = i < 0 ? 0 : job.tiles;
-            const bool mine = row < job.n_rows, any = 32 * (warp & 3) < job.n_rows;
+            const bool mine = row < job.n_rows, any = (row & ~31) < job.n_rows;
             const int rho = job.rho0 + (mine ? row : 0), node = rho / a.G;
             const int clear = a.mask ? job.base : job.base + job.rho0 / a.G + 1;         // positions that every row sees
             float ref = -INFINITY, sum = 0.f, none[1];
@@ -247,7 +253,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_apart_kernel(const 
                     if (lane == 0) mbar_arrive(smem_u32(&c.job_read[(i + 1) & 1]));
                     if (then.tiles == 0) {
                         next = 0;
-                    } else if (pages_queries<HD, uint16_t, 4>(a, then, warp & 3, queries, i < 0, [&] { return warp_wait(smem_u32(&c.q_empty), i & 1, dead); })) {
+                    } else if (pages_queries<HD, uint16_t, 4>(a, then, warp & 3, queries, turn, i < 0, [&] { return warp_wait(smem_u32(&c.q_empty), i & 1, dead); })) {
                         next = 1;
                         fence_proxy_async_smem();
                         __syncwarp();

@@ -371,9 +371,10 @@ __device__ __forceinline__ void pages_clean(unsigned char* tile, int row, int ke
         found);
 }
 
-// A job's queries in the products' order, by kWarps warps: 8 x 4 pieces of 8 columns a warp and step.  empty, wait(): the place is free, wait for that.
+// A job's queries in the products' order, by kWarps warps: 8 x 4 pieces of 8 columns a warp and step.  Row r comes to row r ^ turn of the operand (turn: 0 or 64).
+// empty, wait(): the place is free, wait for that.
 template <int HD, typename T, int kWarps, typename Wait>
-__device__ __forceinline__ bool pages_queries(const PagesArgs& a, const PagesJob& job, int warp, unsigned char* place, bool empty, Wait wait) {
+__device__ __forceinline__ bool pages_queries(const PagesArgs& a, const PagesJob& job, int warp, unsigned char* place, int turn, bool empty, Wait wait) {
     // A thread has a piece of every kRowStep-th row, several of them on their way at once.
     constexpr int kPieces = HD / 8, kTerms = PagesShape<HD, T>::kTerms, kQTile = PagesShape<HD, T>::kQTile, kRowStep = 32 * kWarps / kPieces;
     const int lane = threadIdx.x & 31, piece = warp % (kPieces / 4) * 4 + (lane >> 3), r0 = warp / (kPieces / 4) * 8 + (lane & 7);
@@ -401,7 +402,7 @@ __device__ __forceinline__ bool pages_queries(const PagesArgs& a, const PagesJob
                     uint4 terms[kTerms];
                     pages_terms(v[y], terms);
 #pragma unroll
-                    for (int t = 0; t < kTerms; ++t) *reinterpret_cast<uint4*>(to + (t + (at >> 7)) * kQTile + ((at & 127) >> 3) * HD * 16) = terms[t];
+                    for (int t = 0; t < kTerms; ++t) *reinterpret_cast<uint4*>(to + (t + (at >> 7)) * kQTile + (((at & 127) ^ turn) >> 3) * HD * 16) = terms[t];
                 }
             }
         }
@@ -627,7 +628,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&c.job_read[i & 1]));
             if (job.tiles == 0) return 0;
-            if (!pages_queries<HD, T, 8>(a, job, warp, smem, i == 0, [&] { return warp_wait(smem_u32(&c.q_empty), (i - 1) & 1, dead); })) return -1;
+            if (!pages_queries<HD, T, 8>(a, job, warp, smem, 0, i == 0, [&] { return warp_wait(smem_u32(&c.q_empty), (i - 1) & 1, dead); })) return -1;
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&c.q_full));

@@ -57,8 +57,8 @@ int32_t pages_run(PagesArgs& a, cudaStream_t st) {
     bool apart = false;
     if constexpr (keys == 128) {
         // Streams with triples of their own where requests have up to 64 query rows by KV head on average.  Together and apart, us, 8 KV heads of 128:
-        // 4 rows, 256 requests behind 512 positions 203 and 147, 8 behind 16384 95 and 92; 32 rows, 8 behind 4096 39.5 and 38; 64 rows, 4 behind
-        // 8192 41 and 42, one behind 2048 (32 KV heads) 25 and 23.5; 128 rows, 16 behind 2048 58 and 62.
+        // 4 rows, 256 requests behind 512 positions 203 and 128, 8 behind 16384 95 and 91; 32 rows, 8 behind 4096 39.5 and 36.5; 64 rows, 4 behind
+        // 8192 41 and 41.5, one behind 2048 (32 KV heads) 25 and 23; 128 rows, 16 behind 2048 58 and 62.
         apart = (int64_t)a.w.rows * a.G <= 64 * (int64_t)a.w.n_req;
         if (apart) {
             a.log_rows = 7;
