@@ -7,9 +7,9 @@
 // sums differ by less than a job.  Nothing is shared between CTAs: no atomics, no scratch.
 // Warps: 0-3 and 4-7 the streams' rows, 8 fetches (copy engine, 128-byte swizzle), 9 and 11 issue the streams' products.
 //
-// Bound by the products and the exponentials alike (attend16_tile.cuh): 16384 tokens, 32 heads over 8 of 128, 2.2 TFLOP: 1.78 ms (1.24 PFLOP/s) in a
-// short run, 2.0 under the power limit, the tensor pipe 62 % busy; 2048 tokens 49 us (0.70 PFLOP/s), of which 4 until the first tile and, for every job, 2000
-// clocks for its outputs and 1300 more for the tile with the border; 8 prompts of 100 to 2000 tokens in heads of 64 169 us, where the exponentials weigh twice
+// Bound by the products and the exponentials alike (attend16_tile.cuh): 16384 tokens, 32 heads over 8 of 128, 2.2 TFLOP: 1.74 ms (1.26 PFLOP/s) in a
+// short run, 2.0 under the power limit, the tensor pipe 62 % busy; 2048 tokens 45 us (0.76 PFLOP/s), of which 4 until the first tile and, for every job, 2000
+// clocks for its outputs and 1300 more for the tile with the border; 8 prompts of 100 to 2000 tokens in heads of 64 166 us, where the exponentials weigh twice
 // as much against the products.  Jobs of 2 T tokens: both streams share what is fetched, 128 bytes a clock and SM of shared memory are what
 // S = Q K^T takes already.  Finding a job goes through all prompts' lengths some ten times: beside the tiles of the job before up to some
 // hundred prompts, but 2000 prompts of three tokens take 1.3 ms.
