@@ -730,6 +730,8 @@ class Kv16Cache:
         if pool is not None:
             assert pool.is_cuda and pool.dtype is torch.bfloat16 and pool.is_contiguous(), "pool: contiguous bf16 on a CUDA device"
             if pool.dim() == 8:
+                shape = (2, n_kv_heads, page_size // 8, head_dim // 8, 8, 8)
+                assert tuple(pool.shape[2:]) == shape, f"pool: [layers, pages, {', '.join(map(str, shape))}] expected"
                 n_layers, n_pages = n_layers or pool.shape[0], n_pages or pool.shape[1]
         self.n_kv_heads, self.head_dim, self.page_size = n_kv_heads, head_dim, page_size
         self.n_layers, self.n_pages = 1 if n_layers is None else n_layers, n_pages or 0

@@ -499,6 +499,19 @@ def test_rows_of_requests_without_positions():
         assert torch.equal(out == 0, want == 0) and ((out.double() - want.double()).norm() < 2.0 ** -7 * want.double().norm())
 
 
+def test_pools_of_another_shape_are_refused():
+    import torch
+    from paper_2605_13319_b200 import binding
+    pool = torch.zeros((1, 4, 2, 2, 2, 8, 8, 8), dtype=torch.bfloat16, device="cuda")       # two heads of 64, 16 positions a page
+    assert binding.Kv16Cache(2, 64, pool=pool).n_pages == 4
+    for kvh, hd, page in ((4, 64, 8), (1, 64, 32), (1, 128, 16), (2, 64, 8)):
+        with pytest.raises(AssertionError):
+            binding.Kv16Cache(kvh, hd, pool=pool, page_size=page)
+    with pytest.raises(AssertionError):
+        binding.Kv16Cache(2, 64, pool=pool.flatten(), n_pages=3)
+    assert binding.Kv16Cache(2, 64, pool=pool.flatten(), n_pages=4).n_layers == 1
+
+
 def test_offsets_beyond_32_bits():
     """A pool of 10 GB, 5 * 10^9 values: a request whose pages lie at its end."""
     import torch
