@@ -7,8 +7,8 @@
 // Warps: 0-3 and 4-7 the streams' rows, 8 and 10 fetch a stream's keys and values, 9 and 11 issue its products.
 //
 // Bound by the cache's bytes behind long contexts (32 single tokens behind 256 to 4096 positions 71 us, 4.7 TB/s, 6.9 while tiles flow; one behind 131072 93 us,
-// 5.8 TB/s), else by a stream's own chain: 3300 clocks of one warp for a tile's 128 exponentials a row and what goes with them, 1200 until the next
-// scores, 6000 for a triple's end and the next one's beginning (256 behind 512: 128 us, 4.2 TB/s).
+// 5.8 TB/s), else by a stream's own chain: 2000 to 2700 clocks of one warp for a tile's 128 exponentials a row and what goes with them, 4500 for the one with the
+// border, 1000 to 3000 until the next scores (heads of 128 leave a stream one place for keys), 6000 for a triple's end and the next one's beginning (256 behind 512: 128 us, 4.2 TB/s).
 #pragma once
 #include "attend16_pages.cuh"
 

@@ -12,8 +12,8 @@
 // What bounds it, for two streams of 128 rows by 128 keys with heads of 128: the products 2048 clocks (S = Q K^T of 64 clocks a k16 step, P V the same), the
 // exponentials 2048 clocks too (the special-function units take 16 a clock), 3500 measured in a long prompt: the hand-over from one to the other, some
 // 1000 clocks a tile and stream, is covered by the other stream only in part.  A tile of one stream with few rows, so with one warp at work, takes that warp
-// 3300 clocks.  Steps of 64 keys with two places for the scores: a prompt of 16384 2133 us instead of 1984; two threads a row: 2222; a quarter of
-// the exponentials as polynomials on the FMA pipe: 1830 instead of 1728 (short runs).
+// 2000 to 2700 clocks, 3300 with the other stream's on the same scheduler.  Steps of 64 keys with two places for the scores: a prompt of 16384 2133 us
+// instead of 1984; two threads a row: 2222; a quarter of the exponentials as polynomials on the FMA pipe: 1830 instead of 1728 (short runs).
 #pragma once
 #include "../tcgen05.cuh"
 
