@@ -30,10 +30,12 @@ struct PagesShape {
     static constexpr bool kWide = sizeof(T) == 4;
     static constexpr int kTerms = kWide ? 3 : 1, kHalves = kWide ? 1 : 2, kKeys = kWide ? 64 : 128, kRows = kWide ? 128 : 256;
     static constexpr int kQTile = 128 * HD * 2, kQ = (kWide ? 3 : 2) * kQTile, kTile = kKeys * HD * 2;
-    // An even number of places in either ring: where the streams take the tiles in turn each then has places of its own, and a wait for a place's next
-    // turn cannot take the other stream's turn before it, not yet come, for one that is over.
+    // A wait for a place's turn returns while the turn before it is still to come, too: who waits has to know that one to be over.  Keys: an even number of
+    // places gives each stream places of its own where the streams take a job's tiles in turn, and behind a job all its keys have come before the next
+    // one's queries are given.  Values, which a job's rows need not have waited for: each stream waits for all of them in order, the other stream's too,
+    // and gives a place back when it has seen that it came, so that no place is two turns ahead of a wait.
     static constexpr int kKSlots = kWide ? (HD == 128 ? 4 : 8) : (HD == 128 ? 2 : 4), kVSlots = kWide ? (HD == 128 ? 4 : 8) : (HD == 128 ? 2 : 6);
-    static_assert(kKSlots % 2 == 0 && kVSlots % 2 == 0, "");
+    static_assert(kKSlots % 2 == 0, "");
     static constexpr int kSlots = kKSlots + kVSlots;
 };
 struct PagesArgs {
@@ -549,6 +551,9 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                             umma_bf16(tmem + 128 * s, q + ((kTerms - 1 - t) * (Shape::kQTile >> 4) + x * 16), tile + x * 16, kIdescS, t + x > 0);
                     umma_commit(smem_u32(&c.s_full[s]));
                 };
+                auto see = [&](const VPlace& v) {          // a tile that the other stream takes
+                    if (v_there(v)) mbar_arrive(smem_u32(&c.v_empty[v.slot]));
+                };
                 auto sums = [&](const VPlace& v, bool first) {
                     const uint64_t tile = v_desc + v.slot * (kTile >> 4);
                     for (int h = 0; h < kHalves; ++h) {
@@ -574,10 +579,10 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                     if (n == 0) break;
                     // both: rows of q tile s, every tile of keys; else the same rows, tiles in turn
                     const int step = both ? 1 : 2, q_tile = both ? s : 0, j0 = both ? 0 : s;
-                    // A slot is free when what was issued so far is done, for both streams: the only one that uses it says so twice.
-                    auto release = [&](unsigned long long* bar) {
-                        umma_commit(smem_u32(bar));
-                        if (!both) umma_commit(smem_u32(bar));
+                    // A place is free when what was issued so far is done, for both streams: of keys, the only one that uses it says so twice.
+                    auto release_keys = [&](const KPlace& k) {
+                        umma_commit(smem_u32(&c.k_empty[k.slot]));
+                        if (!both) umma_commit(smem_u32(&c.k_empty[k.slot]));
                     };
                     ok = role_wait(smem_u32(&c.q_full), i & 1, dead);
                     if (!ok) break;
@@ -585,9 +590,10 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                         const KPlace k(tile_no + j0);
                         if (!k_there(k)) break;
                         scores(k, q_tile);
-                        release(&c.k_empty[k.slot]);
+                        release_keys(k);
                     }
                     if (j0 + step >= n) umma_commit(smem_u32(&c.q_empty));
+                    if (!both && s == 1) see(VPlace(tile_no));
                     for (int j = j0; j < n; j += step) {
                         const bool more = j + step < n;
                         const KPlace k(tile_no + j + step);
@@ -596,9 +602,10 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                         if (!sums(v, j == j0)) break;
                         if (more) scores(k, q_tile);
                         else umma_commit(smem_u32(&c.o_full[s]));
-                        release(&c.v_empty[v.slot]);
-                        if (more) release(&c.k_empty[k.slot]);
+                        umma_commit(smem_u32(&c.v_empty[v.slot]));
+                        if (more) release_keys(k);
                         if (more && j + 2 * step >= n) umma_commit(smem_u32(&c.q_empty));
+                        if (!both && j + 1 < n) see(VPlace(tile_no + j + 1));
                     }
                     tile_no += n;
                 }
