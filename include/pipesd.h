@@ -459,7 +459,7 @@ int32_t pipesd_kv16_attend(const pipesd_kv16_cfg *cfg, const void *pool, int32_t
  * handed out lowest id first, in the order of the requests.  A request that does not get all its pages gets none, its row of the table stays
  * as it was and its entry of pages is -1 (as where its numbers make no sense); those behind it are still served where they fit.  Calls on one
  * refs or table are made one after the other.  scratch: pipesd_kv16_plan_scratch_bytes(cfg, n) bytes, 4-byte aligned, one for each of
- * calls that may run at the same time.
+ * calls that may run at the same time.  At most 2^30 requests or forks in a call.
  * reserve: pages for positions 0 .. length[r]-1 of request r = row r of table ([n_req, max_pages]) where the table has none; pages[r]: their
  * number, those that were there included. */
 uint64_t pipesd_kv16_plan_scratch_bytes(const pipesd_kv16_cfg *cfg, int32_t n);

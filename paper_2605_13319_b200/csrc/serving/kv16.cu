@@ -74,6 +74,7 @@ int32_t pages_run(PagesArgs& a, cudaStream_t st) {
     return launched();
 }
 
+constexpr int32_t kPlanRequests = 1 << 30;         // (indices that step by a CTA's threads are 32-bit)
 int plan_cap(const pipesd_kv16_cfg* c, int32_t n) { return (int)std::min<int64_t>((int64_t)n * c->max_pages, c->n_pages); }
 
 // [rows, heads, head_dim] with `stride` elements between rows, fetched in boxes of 64 columns x box_heads x box_rows; rows behind the last read as 0.
@@ -180,13 +181,13 @@ int32_t pipesd_kv16_compact(const pipesd_kv16_cfg* cfg, void* pool, int32_t n_re
 }
 
 uint64_t pipesd_kv16_plan_scratch_bytes(const pipesd_kv16_cfg* cfg, int32_t n) {
-    if (!cfg_ok(cfg) || n < 1) return 0;
+    if (!cfg_ok(cfg) || n < 1 || n > kPlanRequests) return 0;
     return 4 * (1 + 2 * (uint64_t)n + 3 * (uint64_t)plan_cap(cfg, n));
 }
 
 int32_t pipesd_kv16_reserve(const pipesd_kv16_cfg* cfg, int32_t n_req, const int32_t* length, int32_t* table, int32_t* refs, int32_t* pages, void* scratch,
                             void* cuda_stream) {
-    if (!cfg_ok(cfg) || n_req < 1 || !length || !table || !refs || !pages || !scratch || (uintptr_t)scratch % 4) return PIPESD_E_INVALID;
+    if (!cfg_ok(cfg) || n_req < 1 || n_req > kPlanRequests || !length || !table || !refs || !pages || !scratch || (uintptr_t)scratch % 4) return PIPESD_E_INVALID;
     const Kv16PlanArgs a = {nullptr, nullptr, length, nullptr, table, refs, pages, n_req, n_req, cfg->n_pages, cfg->max_pages, cfg->page_size,
                             static_cast<int32_t*>(scratch), plan_cap(cfg, n_req)};
     kv16_plan_kernel<<<1, kPlanThreads, 0, (cudaStream_t)cuda_stream>>>(a);
@@ -195,7 +196,7 @@ int32_t pipesd_kv16_reserve(const pipesd_kv16_cfg* cfg, int32_t n_req, const int
 
 int32_t pipesd_kv16_fork(const pipesd_kv16_cfg* cfg, void* pool, int32_t n, const int32_t* src, const int32_t* dst, const int32_t* length,
                          const int32_t* own, int32_t n_slots, int32_t* table, int32_t* refs, int32_t* pages, void* scratch, void* cuda_stream) {
-    if (!pool_ok(cfg, pool) || n < 1 || n_slots < 1 || !src || !dst || !length || !own || !table || !refs || !pages || !scratch || (uintptr_t)scratch % 4)
+    if (!pool_ok(cfg, pool) || n < 1 || n > kPlanRequests || n_slots < 1 || !src || !dst || !length || !own || !table || !refs || !pages || !scratch || (uintptr_t)scratch % 4)
         return PIPESD_E_INVALID;
     const Kv16PlanArgs a = {src, dst, length, own, table, refs, pages, n, n_slots, cfg->n_pages, cfg->max_pages, cfg->page_size,
                             static_cast<int32_t*>(scratch), plan_cap(cfg, n)};

@@ -221,21 +221,23 @@ struct Kv16PlanArgs {
 };
 constexpr int kPlanThreads = 1024;
 
-__device__ __forceinline__ int block_scan(int v, int* s_warp, int& total) {      // sum in front of the thread's v; whole CTA
+// Sum in front of the thread's v; whole CTA.  N: int where the sum of all threads' fits, else long long.
+template <typename N>
+__device__ __forceinline__ N block_scan(N v, N* s_warp, N& total) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int inc = v;
+    N inc = v;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int t = __shfl_up_sync(0xffffffffu, inc, o);
+        const N t = __shfl_up_sync(0xffffffffu, inc, o);
         if (lane >= o) inc += t;
     }
     __syncthreads();
     if (lane == 31) s_warp[warp] = inc;
     __syncthreads();
-    int w = s_warp[lane], s = w;
+    N w = s_warp[lane], s = w;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-        const int t = __shfl_up_sync(0xffffffffu, s, o);
+        const N t = __shfl_up_sync(0xffffffffu, s, o);
         if (lane >= o) s += t;
     }
     total = __shfl_sync(0xffffffffu, s, 31);
@@ -246,6 +248,7 @@ __device__ __forceinline__ int block_scan(int v, int* s_warp, int& total) {     
 // Bound by its chain of loads and barriers: 7.6 us for 32 requests over 2048 pages, hidden by nothing; one CTA, since ids go out in order.
 __global__ void __launch_bounds__(kPlanThreads) kv16_plan_kernel(const Kv16PlanArgs a) {
     __shared__ int s_warp[32];
+    __shared__ long long s_wide[32];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     int32_t* const need = a.scratch + 1;
     int32_t* const at = need + a.n;
@@ -268,20 +271,20 @@ __global__ void __launch_bounds__(kPlanThreads) kv16_plan_kernel(const Kv16PlanA
         return true;
     };
     auto wants = [&](int from, int c) { return there(a.table[(size_t)from * a.max_pages + c]) == (a.src != nullptr); };
-    // pages that every request needs
+    // pages that every request needs, counted no further than the pool could serve; their sum is one of 64 bits
     for (int i = warp; i < a.n; i += kPlanThreads / 32) {
         int from, to, share, end, n = -1;
         if (range(i, from, to, share, end)) {
             n = 0;
-            for (int c0 = share; c0 < end; c0 += 32) n += __popc(__ballot_sync(0xffffffffu, c0 + lane < end && wants(from, c0 + lane)));
+            for (int c0 = share; c0 < end && n <= a.n_pages; c0 += 32) n += __popc(__ballot_sync(0xffffffffu, c0 + lane < end && wants(from, c0 + lane)));
         }
         if (lane == 0) need[i] = n;
     }
     __syncthreads();
     long long all = 0;
     for (int i0 = 0; i0 < a.n; i0 += kPlanThreads) {
-        int total;
-        const int before = block_scan(i0 + tid < a.n ? max(need[i0 + tid], 0) : 0, s_warp, total);
+        long long total;
+        const long long before = block_scan<long long>(i0 + tid < a.n ? max(need[i0 + tid], 0) : 0, s_wide, total);
         if (i0 + tid < a.n) at[i0 + tid] = (int)min(all + before, (long long)INT32_MAX);
         all += total;
     }
@@ -297,7 +300,7 @@ __global__ void __launch_bounds__(kPlanThreads) kv16_plan_kernel(const Kv16PlanA
             f[i] = p + i < a.n_pages && a.refs[p + i] == 0;
             mine += f[i];
         }
-        int total, to = found + block_scan(mine, s_warp, total);
+        int total, to = found + block_scan<int>(mine, s_warp, total);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             if (f[i] && to < wanted) {
@@ -368,7 +371,7 @@ constexpr int kCopyThreads = 256, kCopyUnroll = 4;
 __global__ void __launch_bounds__(kCopyThreads) kv16_copy_kernel(const Kv16CopyArgs a) {
     pdl_wait();
     const int count = a.scratch[0];
-    const int32_t* const copies = a.scratch + 1 + 2 * a.n + a.cap;
+    const int32_t* const copies = a.scratch + 1 + 2 * (size_t)a.n + a.cap;
     constexpr int kStep = kCopyThreads * kCopyUnroll;
     const long long chunks = (a.page_pieces + kStep - 1) / kStep, items = chunks * a.n_layers * count;
     for (long long it = blockIdx.x; it < items; it += gridDim.x) {

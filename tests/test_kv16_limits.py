@@ -1,0 +1,16 @@
+"""Limits of the bf16 cache's calls, found on the host: nothing here launches anything."""
+import ctypes
+
+import pytest
+
+from paper_2605_13319_b200 import binding
+from test_kv16_arguments import INVALID, call, cfg
+
+
+@pytest.mark.parametrize("name,many", [("reserve", "n_req"), ("fork", "n")])
+def test_more_requests_than_an_index_counts(name, many):
+    for n in ((1 << 30) + 1, 2 ** 31 - 1):
+        assert call(name, **{many: n}) == INVALID
+        assert binding.lib().pipesd_kv16_plan_scratch_bytes(ctypes.byref(cfg()), n) == 0
+    assert binding.lib().pipesd_kv16_plan_scratch_bytes(ctypes.byref(cfg()), 1 << 30) == 4 * (1 + (2 << 30) + 3 * 10)
+
