@@ -406,8 +406,8 @@ int32_t pipesd_kv4_attend(const pipesd_kv4_cfg *cfg, const void *pool, const voi
  * bf16 throughout: q, out [rows, n_q_heads, head_dim], k, v [rows, n_kv_heads, head_dim], head_dim 64 or 128, n_q_heads a multiple of
  * n_kv_heads, up to 128 times as many; strides in elements between rows, multiples of 8, pointers 16-byte aligned; scale > 0, every score
  * times scale below 2^120 in magnitude.  Scores, their maximum and their sums are fp32, probabilities enter the second product in bf16.  A NaN or an
- * infinity in a row of k or v reaches the rows that see it (what is not finite in v makes that column NaN or infinite) and no others.  out must
- * not overlap the inputs. */
+ * infinity in a row of k or v reaches the rows that see it (what is not finite in v makes that column NaN or infinite) and no others; a
+ * score of minus infinity has no weight, and a head's row that has no other is NaN.  out must not overlap the inputs. */
 int32_t pipesd_attend_packed(const void *q, const void *k, const void *v, void *out, int64_t q_stride, int64_t k_stride, int64_t v_stride,
                              int64_t out_stride, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, float scale, int32_t n_req,
                              int32_t rows, const int32_t *row0, void *cuda_stream);
@@ -446,7 +446,7 @@ int32_t pipesd_kv16_read(const pipesd_kv16_cfg *cfg, const void *pool, int32_t l
  * n_q_heads a multiple of n_kv_heads, up to 128 times as many; scale > 0, every score times scale below 2^120 in magnitude.  Sums are fp32.  bf16:
  * q as it is, probabilities in bf16; fp32: q and probabilities as three bf16 terms each (24 bits).  A row that sees no position gives 0, a
  * head's row whose q has a NaN a NaN; rows of no request are left as they are.  A NaN or an infinity in the cache reaches the rows that
- * see it, as for prompts.  out must not overlap q.  The order of sums goes by the lengths and by the numbers of rows and requests.  scratch:
+ * see it, as for prompts; fp32: an infinity in k as a NaN, since q's terms may differ in sign.  out must not overlap q.  The order of sums goes by the lengths and by the numbers of rows and requests.  scratch:
  * pipesd_kv16_attend_scratch_bytes bytes (0 for arguments that are refused), 16-byte aligned; it holds nothing between calls, but two
  * calls that may run at the same time need one each. */
 uint64_t pipesd_kv16_attend_scratch_bytes(const pipesd_kv16_cfg *cfg, int32_t rows, int32_t n_q_heads);

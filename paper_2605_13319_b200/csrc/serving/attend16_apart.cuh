@@ -204,7 +204,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_apart_kernel(const 
             const int rho = job.rho0 + (mine ? row : 0), node = rho / a.G;
             const int clear = a.mask ? job.base : job.base + job.rho0 / a.G + 1;         // positions that every row sees
             float ref = -INFINITY, sum = 0.f, none[1];
-            bool ok = true;
+            bool ok = true, saw = false;           // saw: the row has seen a position
             for (int j = 0; j < n; ++j) {
                 const int u = job.u0 + j, p0 = u * kKeys;
                 uint32_t see[kKeys / 32];
@@ -222,6 +222,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_apart_kernel(const 
                     pages_present(present, masked, see);
                     masked = true;
                 }
+                saw = saw || pages_any(masked, see);
                 if (masked) {
                     const VPlace v(tile_no + j);
                     ok = warp_wait(smem_u32(&c.v_full[v.slot]), v.phase, dead);
@@ -272,6 +273,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_apart_kernel(const 
             tc_fence_after();
             const bool whole = job.whole;
             if (sum != sum) ref = INFINITY;        // (not what a row that sees nothing has: every factor of it is then a NaN)
+            if (ref == -INFINITY) sum = saw ? kBlind : 0.f;
             uint16_t* const out = static_cast<uint16_t*>(a.out) + (job.first + node) * a.out_stride + (size_t)(job.head * a.G + rho % a.G) * HD;
             float* const part = a.parts + (size_t)job.share * a.cap * (HD + 2);
             if (!ok) {                             // a copy or a product that never came: no result
@@ -281,8 +283,8 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_apart_kernel(const 
                 break;
             }
             const int lo = *(volatile int*)&c.bad_lo[i & 3], hi = *(volatile int*)&c.bad_hi[i & 3];
-            const bool nothing = ref == -INFINITY;
-            const float factor = !whole ? 1.f : sum > 0.f ? 1.f / sum : sum;
+            const bool none_seen = ref == -INFINITY;
+            const float nothing = sum == kBlind ? NAN : 0.f, factor = !whole ? 1.f : sum > 0.f ? 1.f / sum : sum;
             if (any)
 #pragma unroll 1
                 for (int d = 0; d < HD; d += 32) {
@@ -292,7 +294,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_apart_kernel(const 
                     if (mine) {
                         float y[32];
 #pragma unroll
-                        for (int x = 0; x < 32; ++x) y[x] = nothing ? 0.f : __uint_as_float(u[x]) * factor;
+                        for (int x = 0; x < 32; ++x) y[x] = none_seen ? nothing : __uint_as_float(u[x]) * factor;
                         if (lo <= hi)
 #pragma unroll 1
                             for (int h = 0; h < 32; h += 16) {

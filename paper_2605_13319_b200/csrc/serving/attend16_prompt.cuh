@@ -339,7 +339,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
             }
             tc_fence_after();
             const bool fix = *(volatile int*)&c.flags[i % kPromptJobs];
-            const float inv = sum > 0.f ? 1.f / sum : sum;
+            const float inv = sum > 0.f ? 1.f / sum : NAN;      // (0: every score that the row sees is minus infinity; it sees itself)
             // 64 bytes of each of four rows by four lanes: a store of a piece by every row's own lane would cost a pass per row (a job of 64 columns
             // ends 1000 clocks sooner for it)
             const unsigned rows = __ballot_sync(0xffffffffu, mine);

@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 
 from oracle import trees
-from test_gpu_kv16 import Case, _ints, _row0
+from test_gpu_kv16 import Case, Packed, _close, _ints
 
 pytestmark = pytest.mark.gpu
 
@@ -47,3 +47,63 @@ def test_more_pages_wanted_than_32_bits_count():
     copied = torch.zeros(n_pages, dtype=torch.bool, device="cuda")
     copied[6:9] = True
     assert torch.equal(cache.pool[:, ~copied], before[:, ~copied]) and torch.equal(cache.pool[:, copied], before[:, 5:6].expand(-1, 3, *before.shape[2:]))
+
+
+def _blind(k, keys):
+    """Keys whose score is minus infinity for a query with a positive first column."""
+    k[keys, :, 0] = -float("inf")
+
+
+@pytest.mark.parametrize("heads,kvh,hd", [(4, 2, 128), (8, 2, 64), (64, 2, 128)])
+@pytest.mark.parametrize("new,base", [([9], [40]), ([1], [0]), ([5], [0]), ([1], [9000]), ([40], [20000]), ([3] * 60, [300] * 60), ([1] * 300, [100] * 300)])
+def test_rows_that_see_nothing_but_minus_infinity(new, base, heads, kvh, hd):
+    """A softmax of minus infinities alone has no value: NaN.  One finite score among them takes all the weight, and a row that sees nothing gives 0."""
+    import torch
+    nan = float("nan")
+    c = Case(heads + sum(new), new, base, heads, kvh, hd)
+    for r, (n, b) in enumerate(zip(new, base)):
+        _blind(c.k[r], slice(0, b + n))
+    c.fill()
+    words = 2
+    some = c.trees(words)
+    some[c.rng.random(c.rows) < 0.3] = 0
+    for dtype in (torch.bfloat16, torch.float32):
+        q = c.queries(dtype)
+        q[:, :, 0] = q[:, :, 0].abs() + 0.25
+        for mask in (None, some):
+            out = c.attend(q, mask)
+            for r in range(len(new)):
+                rows = slice(int(c.row0[r]), int(c.row0[r + 1]))
+                sees = c.seen(r, mask).any(1)
+                assert torch.isnan(out[rows][sees]).all() and (out[rows][~sees] == 0).all()
+    # every third request has one key with a score of its own, early, in the middle or the last one
+    for r, (n, b) in enumerate(zip(new, base)):
+        if r % 3 == 0:
+            c.k[r][[0, (b + n) // 2, b + n - 1][r // 3 % 3], :, 0] = 1.0
+    c.fill()
+    q = c.queries(torch.bfloat16)
+    q[:, :, 0] = q[:, :, 0].abs() + 0.25
+    for mask in (None, some):
+        out = c.attend(q, mask)
+        for r in range(len(new)):
+            rows, seen = slice(int(c.row0[r]), int(c.row0[r + 1])), c.seen(r, mask)
+            want, size, mag = trees.attend(q[rows], c.k[r], c.v[r], seen, hd ** -0.5)
+            finite = torch.isfinite(c.k[r][:, 0, 0])
+            want[seen.any(1) & ~(seen & finite).any(1)] = nan
+            _close(out[rows], (want, size, mag), q.dtype, base[r] + new[r])
+
+
+@pytest.mark.parametrize("heads,kvh,hd", [(4, 2, 128), (8, 1, 64)])
+def test_prompts_that_begin_with_minus_infinity(heads, kvh, hd):
+    import torch
+    from paper_2605_13319_b200 import binding
+    c = Packed(5, [300, 1, 40, 7], heads, kvh, hd)
+    c.q[:, :, 0] = c.q[:, :, 0].abs() + 0.25
+    for (rows, _), blind in zip(c.spans(), (200, 1, 0, 7)):
+        _blind(c.k, slice(rows.start, rows.start + blind))
+    out = binding.attend_packed(c.q, c.k, c.v, c.row0)
+    for (rows, n), blind in zip(c.spans(), (200, 1, 0, 7)):
+        seen = torch.ones((n, n), dtype=torch.bool, device="cuda").tril()
+        want, size, mag = trees.attend(c.q[rows], c.k[rows], c.v[rows], seen, c.scale)
+        want[:blind] = float("nan")
+        _close(out[rows], (want, size, mag), out.dtype, n)
