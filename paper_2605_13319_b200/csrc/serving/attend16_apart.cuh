@@ -273,7 +273,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_apart_kernel(const 
             tc_fence_after();
             const bool whole = job.whole;
             if (sum != sum) ref = INFINITY;        // (not what a row that sees nothing has: every factor of it is then a NaN)
-            if (ref == -INFINITY) sum = saw ? kBlind : 0.f;
+            if (saw) ref = fmaxf(ref, kBlind);
             uint16_t* const out = static_cast<uint16_t*>(a.out) + (job.first + node) * a.out_stride + (size_t)(job.head * a.G + rho % a.G) * HD;
             float* const part = a.parts + (size_t)job.share * a.cap * (HD + 2);
             if (!ok) {                             // a copy or a product that never came: no result
@@ -283,8 +283,8 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_apart_kernel(const 
                 break;
             }
             const int lo = *(volatile int*)&c.bad_lo[i & 3], hi = *(volatile int*)&c.bad_hi[i & 3];
-            const bool none_seen = ref == -INFINITY;
-            const float nothing = sum == kBlind ? NAN : 0.f, factor = !whole ? 1.f : sum > 0.f ? 1.f / sum : sum;
+            const bool nothing = ref == -INFINITY;
+            const float factor = !whole ? 1.f : sum > 0.f ? 1.f / sum : NAN;
             if (any)
 #pragma unroll 1
                 for (int d = 0; d < HD; d += 32) {
@@ -294,7 +294,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_apart_kernel(const 
                     if (mine) {
                         float y[32];
 #pragma unroll
-                        for (int x = 0; x < 32; ++x) y[x] = none_seen ? nothing : __uint_as_float(u[x]) * factor;
+                        for (int x = 0; x < 32; ++x) y[x] = nothing ? 0.f : __uint_as_float(u[x]) * factor;
                         if (lo <= hi)
 #pragma unroll 1
                             for (int h = 0; h < 32; h += 16) {

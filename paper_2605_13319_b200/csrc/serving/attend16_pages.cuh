@@ -369,9 +369,9 @@ __device__ __forceinline__ bool pages_any(bool masked, const uint32_t (&see)[kWo
     for (int w = 0; w < kWords; ++w) any |= see[w];
     return !masked || any;
 }
-// The sum of a share without a reference: 0 where the row has seen nothing, which is what it gives; else all that it saw had a score of minus
-// infinity, so that the row is a NaN unless another share has a reference.
-constexpr float kBlind = 1.f;
+// The reference of a row that has seen scores of minus infinity alone, with a sum of 0: any other reference outweighs it, and where there is none the row
+// is a NaN.  (A row that has seen nothing has minus infinity, and gives 0.)
+constexpr float kBlind = -3.402823466e38f;
 template <int HD, int kKeys, typename Found>
 __device__ __forceinline__ void pages_clean(unsigned char* tile, int row, int keys, uint32_t present, Found found) {
     clean_values<kKeys * HD / 8>(
@@ -724,7 +724,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                     tmem_st_wait();
                 }
             if (sum != sum) ref = INFINITY;        // (not what a row that sees nothing has: every factor of it is then a NaN)
-            if (ref == -INFINITY) sum = saw ? kBlind : 0.f;
+            if (saw) ref = fmaxf(ref, kBlind);
             if (ok && join) {
                 c.ref[s][row] = ref;
                 c.sum[s][row] = sum;
@@ -750,12 +750,11 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                 ref = fmaxf(r0, r1);
                 f0 = none0 ? 0.f : exp2_approx(r0 - ref);
                 f1 = none1 ? 0.f : exp2_approx(r1 - ref);
-                sum = none0 && none1 ? fmaxf(c.sum[0][row], c.sum[1][row]) : c.sum[0][row] * f0 + c.sum[1][row] * f1;
+                sum = c.sum[0][row] * f0 + c.sum[1][row] * f1;
             }
-            const float nothing = ref == -INFINITY && sum == kBlind ? NAN : 0.f;
             const int lo = *(volatile int*)&c.bad_lo[i & 3], hi = *(volatile int*)&c.bad_hi[i & 3];
             if (whole) {
-                const float inv = sum > 0.f ? 1.f / sum : sum;
+                const float inv = sum > 0.f ? 1.f / sum : ref == -INFINITY ? 0.f : NAN;
                 f0 *= inv;
                 f1 *= inv;
             }
@@ -768,7 +767,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                     tmem_ld16(from + d, y);
                     tmem_ld_wait16(y);
 #pragma unroll
-                    for (int x = 0; x < 16; ++x) y[x] = none0 ? nothing : y[x] * f0;
+                    for (int x = 0; x < 16; ++x) y[x] = none0 ? 0.f : y[x] * f0;
                     if (join && n > 1) {
                         tmem_ld16(from + HD + d, o);
                         tmem_ld_wait16(o);
@@ -852,10 +851,7 @@ __global__ void __launch_bounds__(32 * kPagesMergeWarps) pages_merge_kernel(cons
             float4 y[8];
 #pragma unroll
             for (int x = 0; x < 8; ++x) y[x] = *reinterpret_cast<const float4*>(p + (size_t)(d0 + 4 * x) * a.cap + 4 * slot);
-            if (r == -INFINITY) {                  // a share that has seen nothing, or no score above minus infinity (kBlind)
-                if (top == -INFINITY) sum = fmaxf(sum, part);
-                continue;
-            }
+            if (r == -INFINITY) continue;          // a share that has seen nothing
             const float next = r == r ? fmaxf(top, r) : INFINITY;              // (a NaN where a share never came)
             const float keep = top == -INFINITY ? 0.f : exp2_approx(top - next), factor = exp2_approx(r - next);
             top = next;
@@ -880,12 +876,12 @@ __global__ void __launch_bounds__(32 * kPagesMergeWarps) pages_merge_kernel(cons
             for (int w = 0; w < kPagesMergeWarps; ++w) most = fmaxf(most, s_top[w][r]);
 #pragma unroll
             for (int w = 0; w < kPagesMergeWarps; ++w) {
-                const float factor = most == -INFINITY ? 1.f : exp2_approx(s_top[w][r] - most);
+                const float factor = s_top[w][r] == -INFINITY ? 0.f : exp2_approx(s_top[w][r] - most);
                 y = fmaf(factor, s_v[w][r][lane], y);
                 total = fmaf(factor, s_sum[w][r], total);
             }
             const int rho = split.rho0 + r0 + r;
-            const float inv = most == -INFINITY && total > 0.f ? NAN : total > 0.f ? 1.f / total : total;
+            const float inv = total > 0.f ? 1.f / total : most == -INFINITY ? 0.f : NAN;
             pages_store(static_cast<T*>(a.out) + (split.first + rho / G) * a.out_stride + (size_t)(split.head * G + rho % G) * HD + d0 + lane, y * inv);
         }
         __syncthreads();
