@@ -399,7 +399,9 @@ int32_t pipesd_kv4_attend(const pipesd_kv4_cfg *cfg, const void *pool, const voi
  *
  * What a server needs whose edges draft trees instead of chains: attention of whole prompts, which fills the cache; attention of a tree's
  * nodes over the cache; and the pages' life: reserved for rows to come, forked for candidates that share a prefix, compacted to the
- * accepted path, released.  Calls, streams, threads and graphs as for pipesd_sample; all arrays are in device memory. */
+ * accepted path, released.  Calls, streams, threads and graphs as for pipesd_sample; all arrays are in device memory.
+ * Attention's kernels wait for copies and products at most two seconds at a time.  Where such a wait runs out, which no valid call brings about, all
+ * rows of which that CTA has a part are NaN in the heads that it had, and the call's other rows what they should be. */
 
 /* out[row] = softmax(scale * q . k) v over the rows of the same prompt up to itself.  Prompt r has the rows row0[r] .. row0[r+1]-1 (row0:
  * n_req + 1 ascending entries within 0 .. rows; a prompt without rows is one); rows of no prompt are neither read into any result nor written.
@@ -418,6 +420,10 @@ int32_t pipesd_attend_packed(const void *q, const void *k, const void *v, void *
  * or more has no bits and depth -1.  Rows in front of the first request and behind the last have no bits and depth 0. */
 int32_t pipesd_tree_mask(int32_t n_req, int32_t rows, const int32_t *row0, const int32_t *parent, int32_t words, uint32_t *mask,
                          int32_t *depth, void *cuda_stream);
+
+/* Self-test of what a wait that ran out leaves: of the attention calls that follow, in every thread, block `cta` (0..147; -1, as at first: none) has
+ * given up when it starts. */
+int32_t pipesd_debug_attend_gives_up(int32_t cta);
 
 /* The pool has the layout of a context's own: [layer][page][K, V][KV head][position / 8][column / 8][position % 8][column % 8], bf16.
  * Requests, rows, base and table as for the 4-bit cache, one table for all layers. */

@@ -110,6 +110,7 @@ _SIGNATURES = {
     "pipesd_kv4_attend": (i32, [ctypes.POINTER(Kv4Cfg), vp, vp, vp, i32, i64, i64, i32, f32, i32, i32, vp, vp, vp, vp, vp]),
     "pipesd_attend_packed": (i32, [vp, vp, vp, vp, i64, i64, i64, i64, i32, i32, i32, f32, i32, i32, vp, vp]),
     "pipesd_tree_mask": (i32, [i32, i32, vp, vp, i32, vp, vp, vp]),
+    "pipesd_debug_attend_gives_up": (i32, [i32]),
     "pipesd_kv16_pool_bytes": (u64, [ctypes.POINTER(Kv16Cfg)]),
     "pipesd_kv16_append": (i32, [ctypes.POINTER(Kv16Cfg), vp, i32, vp, vp, i32, i64, i64, i32, i32, vp, vp, vp, vp]),
     "pipesd_kv16_read": (i32, [ctypes.POINTER(Kv16Cfg), vp, i32, vp, vp, i32, i32, vp, vp, vp, vp]),

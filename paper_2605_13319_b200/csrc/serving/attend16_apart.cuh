@@ -81,7 +81,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_apart_kernel(const 
             mbar_init(smem_u32(&b.o_full), 1);
             mbar_init(smem_u32(&b.done), 1);
         }
-        control.dead = 0;
+        control.dead = blockIdx.x == a.gives_up;
         fence_mbar_init();
     }
     if (warp == 9) tmem_alloc(smem_u32(&control.tmem), 512);
@@ -276,12 +276,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_apart_kernel(const 
             if (saw) ref = fmaxf(ref, kBlind);
             uint16_t* const out = static_cast<uint16_t*>(a.out) + (job.first + node) * a.out_stride + (size_t)(job.head * a.G + rho % a.G) * HD;
             float* const part = a.parts + (size_t)job.share * a.cap * (HD + 2);
-            if (!ok) {                             // a copy or a product that never came: no result
-                if (mine && whole)
-                    for (int d = 0; d < HD; ++d) pages_store(out + d, NAN);
-                if (mine && !whole) part[a.cap * HD + row] = NAN;
-                break;
-            }
+            if (!ok) break;                        // a copy or a product that never came
             const int lo = *(volatile int*)&c.bad_lo[i & 3], hi = *(volatile int*)&c.bad_hi[i & 3];
             const bool nothing = ref == -INFINITY;
             const float factor = !whole ? 1.f : sum > 0.f ? 1.f / sum : NAN;
@@ -322,6 +317,8 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_apart_kernel(const 
         }
     }
     __syncthreads();
+    if (warp < 8 && *dead)
+        for (int x = 0; x < 2; ++x) pages_gave_up<HD, uint16_t>(a, 2 * blockIdx.x + x);
     if (warp == 9) {
         tc_fence_after();
         tmem_dealloc(control.tmem, 512);

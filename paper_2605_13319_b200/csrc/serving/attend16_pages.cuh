@@ -56,6 +56,7 @@ struct PagesArgs {
     int log_keys, log_rows;     // of a tile and a row group
     int ranges, lead;           // into which the tiles are cut; what a triple counts beside its tiles
     int own_shares;             // of a range: two for each stream that goes through it
+    int gives_up;               // a CTA that has given up from the start (tests; -1: none)
 };
 // The triple that goes on behind a range, as the merge needs it (rows 0: none).
 struct PagesSplit {
@@ -424,6 +425,28 @@ __device__ __forceinline__ bool pages_queries(const PagesArgs& a, const PagesJob
     return empty;
 }
 
+// A CTA that gave up has no results: NaN for all that its range holds, what was finished among it, and as the references of its shares, so that the
+// merge gives NaN too.  By the streams' warps, when all roles have ended.
+template <int HD, typename T>
+__device__ __noinline__ void pages_gave_up(const PagesArgs& a, int range) {
+    PagesWalk walk;
+    walk.begin(a, range);
+    for (;;) {
+        const PagesJob job = walk.next(a);
+        if (job.tiles == 0) break;
+        for (int local = threadIdx.x; local < job.n_rows; local += 256) {
+            const int rho = job.rho0 + local, slot = job.n_rows > 128 ? local & 127 : local;
+            if (job.whole) {
+                T* const out = static_cast<T*>(a.out) + (job.first + rho / a.G) * a.out_stride + (size_t)(job.head * a.G + rho % a.G) * HD;
+                for (int d = 0; d < HD; ++d) pages_store(out + d, NAN);
+            } else {
+                for (int s = 0; s < a.own_shares / 2; ++s) a.parts[(size_t)(job.share + s) * a.cap * (HD + 2) + a.cap * HD + slot] = NAN;
+            }
+        }
+    }
+    if (threadIdx.x == 0) a.splits[range] = walk.split;
+}
+
 template <int HD, typename T>
 __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const __grid_constant__ PagesArgs a) {
     using Shape = PagesShape<HD, T>;
@@ -465,7 +488,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
             mbar_init(smem_u32(&c.o_full[s]), 1);
             mbar_init(smem_u32(&c.done[s]), 1);
         }
-        c.dead = 0;
+        c.dead = blockIdx.x == a.gives_up;
         fence_mbar_init();
     }
     if (warp == 9) tmem_alloc(smem_u32(&c.tmem), 512);
@@ -735,12 +758,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
             T* const out = static_cast<T*>(a.out) + (job.first + node) * a.out_stride + (size_t)(job.head * G + rho % G) * HD;
             float* const part = a.parts + (size_t)(job.share + s) * a.cap * (HD + 2);
             const int slot = both ? row : local;   // (a stream's rows: of 128)
-            if (!ok) {                             // a copy or a product that never came: no result
-                if (mine && whole)
-                    for (int d = 0; d < HD; ++d) pages_store(out + d, NAN);
-                if (mine && !whole) part[a.cap * HD + slot] = NAN;
-                break;
-            }
+            if (!ok) break;                        // a copy or a product that never came
             float f0 = 1.f, f1 = 1.f;              // what stream 0's and stream 1's sums are multiplied with
             bool none0 = ref == -INFINITY, none1 = true;                       // a stream that has seen nothing has none
             if (join) {
@@ -800,6 +818,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
         }
     }
     __syncthreads();
+    if (warp < 8 && *dead) pages_gave_up<HD, T>(a, blockIdx.x);
     if (warp == 9) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);

@@ -26,6 +26,7 @@ struct PromptArgs {
     int n_req, rows, Hq, Hkv;
     float scale;                // times log2(e)
     int ctas;
+    int gives_up;               // a CTA that has given up from the start (tests; -1: none)
 };
 struct PromptJob {
     int first, n, t0, head;     // the prompt's first row and length (0: no more jobs), the job's first token
@@ -66,6 +67,18 @@ __device__ __forceinline__ int prompt_blocks_from(const PromptArgs& a, int level
         sum += max(0, b - level);
     }
     return __reduce_add_sync(0xffffffffu, sum);
+}
+// Levels that there are, and the length and first row of prompt `lane` (whole warp).
+__device__ __forceinline__ int prompt_levels(const PromptArgs& a, int block, int& n0, int& first0) {
+    const int lane = threadIdx.x & 31;
+    n0 = first0 = 0;
+    if (lane < a.n_req) n0 = prompt_len(a, lane, first0);
+    int longest = n0;
+    for (int r = 32 + lane; r < a.n_req; r += 32) {
+        int first;
+        longest = max(longest, prompt_len(a, r, first));
+    }
+    return (__reduce_max_sync(0xffffffffu, longest) + block - 1) / block;
 }
 // A CTA's i-th job: the jobs, longest first, are dealt out back and forth (whole warp).  n = 0: there are not as many.
 __device__ __forceinline__ PromptJob prompt_job(const PromptArgs& a, int i, int block, int levels, int n0, int first0) {
@@ -113,6 +126,22 @@ __device__ __noinline__ uint32_t prompt_bad(const uint16_t* v, long long stride,
     return bad;
 }
 
+// A CTA that gave up has no results: NaN for all of its jobs, those that were finished among them.  By the streams' warps, when all roles have ended.
+template <int HD>
+__device__ __noinline__ void prompt_gave_up(const PromptArgs& a) {
+    const int G = a.Hq / a.Hkv, block = 2 * (128 / G);
+    int n0, first0;
+    const int levels = prompt_levels(a, block, n0, first0);
+    for (int i = 0;; ++i) {
+        const PromptJob job = prompt_job(a, i, block, levels, n0, first0);
+        if (job.n == 0) break;
+        for (int x = threadIdx.x; x < min(block, job.n - job.t0) * G; x += 256) {
+            uint16_t* const out = a.out + (long long)(job.first + job.t0 + x / G) * a.out_stride + (job.head * G + x % G) * HD;
+            for (int d = 0; d < HD; ++d) out[d] = 0x7fff;
+        }
+    }
+}
+
 template <int HD>
 __global__ void __launch_bounds__(kAttendThreads16, 1)
     prompt_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ PromptArgs a) {
@@ -131,13 +160,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
     int levels = 0, n0 = 0, first0 = 0;            // n0, first0: of prompt `lane`
     if (warp == 8) {                               // (while the others set up)
         if (lane < 3) tensor_map_prefetch(lane == 0 ? &map_q : lane == 1 ? &map_k : &map_v);
-        if (lane < a.n_req) n0 = prompt_len(a, lane, first0);
-        int longest = n0;
-        for (int r = 32 + lane; r < a.n_req; r += 32) {
-            int first;
-            longest = max(longest, prompt_len(a, r, first));
-        }
-        levels = (__reduce_max_sync(0xffffffffu, longest) + 2 * T - 1) / (2 * T);
+        levels = prompt_levels(a, 2 * T, n0, first0);
         ahead = prompt_job(a, 0, 2 * T, levels, n0, first0);
     }
     if (tid == 0) {
@@ -153,7 +176,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
             mbar_init(smem_u32(&c.o_full[s]), 1);
             mbar_init(smem_u32(&c.done[s]), 1);
         }
-        c.dead = 0;
+        c.dead = blockIdx.x == a.gives_up;
         fence_mbar_init();
     }
     if (warp == 9) tmem_alloc(smem_u32(&c.tmem), 512);
@@ -332,11 +355,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
             uint16_t* const out = a.out + (long long)(job.first + t) * a.out_stride + (job.head * G + g) * HD;
             if (ok) ok = warp_wait(smem_u32(&c.o_full[s]), full_phase, dead);
             full_phase ^= 1;
-            if (!ok) {                             // a copy or a product that never came: no result
-                if (mine)
-                    for (int d = 0; d < HD; ++d) out[d] = 0x7fff;
-                break;
-            }
+            if (!ok) break;                        // a copy or a product that never came
             tc_fence_after();
             const bool fix = *(volatile int*)&c.flags[i % kPromptJobs];
             const float inv = sum > 0.f ? 1.f / sum : NAN;      // (0: every score that the row sees is minus infinity; it sees itself)
@@ -375,6 +394,7 @@ __global__ void __launch_bounds__(kAttendThreads16, 1)
         }
     }
     __syncthreads();
+    if (warp < 8 && *dead) prompt_gave_up<HD>(a);
     if (warp == 9) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);

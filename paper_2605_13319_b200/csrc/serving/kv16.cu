@@ -1,5 +1,6 @@
 // C entries of the bf16 K/V cache, its pages, and attention in bf16.
 #include <algorithm>
+#include <atomic>
 #include <mutex>
 
 #include "../../../include/pipesd.h"
@@ -11,6 +12,8 @@
 using namespace pipesd;
 
 namespace {
+
+std::atomic<int32_t> g_gives_up{-1};               // pipesd_debug_attend_gives_up
 
 bool cfg_ok(const pipesd_kv16_cfg* c) {
     return c && (c->head_dim == 64 || c->head_dim == 128) && c->n_kv_heads >= 1 && c->n_kv_heads <= 65535 && c->page_size >= 8 && c->page_size % 8 == 0 &&
@@ -47,6 +50,7 @@ int32_t pages_run(PagesArgs& a, cudaStream_t st) {
     a.ranges = kPagesSms;
     a.lead = kPagesLead;
     a.own_shares = 4;
+    a.gives_up = g_gives_up.load(std::memory_order_relaxed);
     a.tile_pages = keys / a.w.page_size;
     a.tile_over = keys % a.w.page_size;
     // ceil(2^(30 + L) / page_size) with 2^L >= page_size is off by less than page_size <= 2^L, so that the quotient of a position below 2^30 is exact
@@ -124,6 +128,12 @@ bool device_ready() {
 }  // namespace
 
 extern "C" {
+
+int32_t pipesd_debug_attend_gives_up(int32_t cta) {
+    if (cta < -1 || cta >= kSms) return PIPESD_E_INVALID;
+    g_gives_up.store(cta, std::memory_order_relaxed);
+    return PIPESD_OK;
+}
 
 uint64_t pipesd_kv16_pool_bytes(const pipesd_kv16_cfg* cfg) {
     if (!cfg_ok(cfg)) return 0;
@@ -274,7 +284,7 @@ int32_t pipesd_attend_packed(const void* q, const void* k, const void* v, void* 
     // the jobs there can be: a prompt's last one may be short
     const int64_t jobs = ((int64_t)rows / (2 * T) + std::min(n_req, rows)) * n_kv_heads;
     const PromptArgs a = {row0,    static_cast<const uint16_t*>(v), static_cast<uint16_t*>(out), v_stride, out_stride, n_req, rows, n_q_heads, n_kv_heads,
-                          scale * 1.4426950408889634f, (int)std::min<int64_t>(jobs, kSms)};
+                          scale * 1.4426950408889634f, (int)std::min<int64_t>(jobs, kSms), g_gives_up.load(std::memory_order_relaxed)};
     if (head_dim == 128) prompt_kernel<128><<<a.ctas, kAttendThreads16, PromptShape<128>::kSmem, (cudaStream_t)cuda_stream>>>(mq, mk, mv, a);
     else prompt_kernel<64><<<a.ctas, kAttendThreads16, PromptShape<64>::kSmem, (cudaStream_t)cuda_stream>>>(mq, mk, mv, a);
     return launched();

@@ -107,3 +107,51 @@ def test_prompts_that_begin_with_minus_infinity(heads, kvh, hd):
         want, size, mag = trees.attend(c.q[rows], c.k[rows], c.v[rows], seen, c.scale)
         want[:blind] = float("nan")
         _close(out[rows], (want, size, mag), out.dtype, n)
+
+
+def _blocks_that_give_up(call, clean):
+    """call() with each block having given up in turn: what it had is NaN, all of a row's head or nothing, the rest what it is without.  Returns
+    how many blocks had a part of each [row, head]."""
+    import torch
+    from paper_2605_13319_b200 import binding
+    parts = torch.zeros(clean.shape[:2], dtype=torch.int32, device="cuda")
+    try:
+        for block in range(148):
+            assert binding.lib().pipesd_debug_attend_gives_up(block) == 0
+            out = call()
+            gone = torch.isnan(out)
+            assert torch.equal(gone.all(2), gone.any(2))
+            assert torch.equal(torch.where(gone, clean, out), clean)
+            parts += gone.all(2)
+    finally:
+        assert binding.lib().pipesd_debug_attend_gives_up(-1) == 0
+    assert torch.equal(call(), clean)
+    return parts
+
+
+@pytest.mark.parametrize("heads,kvh,hd", [(8, 2, 128), (4, 4, 64), (40, 1, 128)])
+@pytest.mark.parametrize("new,base", [([1], [40000]), ([40, 3, 0, 7], [2000, 100, 4, 0]), ([1] * 200, [300] * 200), ([100], [5000])])
+def test_a_block_that_gives_up_leaves_nan(new, base, heads, kvh, hd):
+    import torch
+    c = Case(heads + sum(new), new, base, heads, kvh, hd)
+    c.fill()
+    mask = c.trees(-(-max(new) // 32))
+    bits = _ints(mask.view(np.int32))
+    for dtype in (torch.bfloat16, torch.float32):
+        q = c.queries(dtype)
+        clean = c.attend(q, mask)
+        c.check(q, mask, clean)
+        parts = _blocks_that_give_up(lambda: c.cache.attend(q, *c.where, mask=bits, out=torch.full_like(q, 5.0)), clean)
+        assert (parts > 0).all()
+
+
+@pytest.mark.parametrize("lengths,heads,kvh,hd", [([37], 8, 2, 128), ([3000, 1, 200], 8, 2, 128), ([64] * 100, 4, 4, 64)])
+def test_a_block_that_gives_up_leaves_nan_in_prompts(lengths, heads, kvh, hd):
+    import torch
+    from paper_2605_13319_b200 import binding
+    c = Packed(8, lengths, heads, kvh, hd, pad=3)
+    n = sum(lengths)
+    clean = binding.attend_packed(c.q, c.k, c.v, c.row0, out=torch.full(c.q.shape, 5.0, dtype=torch.bfloat16, device="cuda"))
+    c.check(clean)
+    parts = _blocks_that_give_up(lambda: binding.attend_packed(c.q, c.k, c.v, c.row0, out=torch.full_like(clean, 5.0)), clean)
+    assert (parts[:n] == 1).all() and (parts[n:] == 0).all() and (clean[n:] == 5).all()

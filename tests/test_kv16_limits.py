@@ -14,3 +14,9 @@ def test_more_requests_than_an_index_counts(name, many):
         assert binding.lib().pipesd_kv16_plan_scratch_bytes(ctypes.byref(cfg()), n) == 0
     assert binding.lib().pipesd_kv16_plan_scratch_bytes(ctypes.byref(cfg()), 1 << 30) == 4 * (1 + (2 << 30) + 3 * 10)
 
+
+def test_blocks_that_give_up_are_blocks():
+    L = binding.lib()
+    for block in (-2, 148, 2 ** 31 - 1):
+        assert L.pipesd_debug_attend_gives_up(block) == INVALID
+    assert L.pipesd_debug_attend_gives_up(-1) == 0
