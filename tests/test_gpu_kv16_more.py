@@ -4,6 +4,7 @@ import pytest
 
 from oracle import trees
 from test_gpu_kv16 import Case, Packed, _close, _ints
+from test_kv16_bounds import marked, marked_queries, marked_result, marked_tolerance, norm_bound, norm_error
 
 pytestmark = pytest.mark.gpu
 
@@ -155,3 +156,97 @@ def test_a_block_that_gives_up_leaves_nan_in_prompts(lengths, heads, kvh, hd):
     c.check(clean)
     parts = _blocks_that_give_up(lambda: binding.attend_packed(c.q, c.k, c.v, c.row0, out=torch.full_like(clean, 5.0)), clean)
     assert (parts[:n] == 1).all() and (parts[n:] == 0).all() and (clean[n:] == 5).all()
+
+
+# --------------------------------------------------------------------------- long contexts
+LONG = [([1], [40000]), ([9], [20055]), ([1], [131071]), ([17, 3, 60], [8000, 100, 30500]), ([64] * 3, [20000, 4000, 9990]), ([1] * 40, [int(x) for x in np.linspace(100, 9000, 40)]),
+        ([512], [3000])]
+
+
+@pytest.mark.parametrize("heads,kvh,hd", [(8, 2, 128), (8, 2, 64), (48, 1, 128)])
+@pytest.mark.parametrize("new,base", LONG)
+def test_long_contexts_in_norm(new, base, heads, kvh, hd):
+    import torch
+    c = Case(heads + sum(new) + hd, new, base, heads, kvh, hd)
+    c.fill()
+    for dtype in (torch.bfloat16, torch.float32):
+        for mask in (None, c.trees(-(-max(new) // 32))):
+            q = c.queries(dtype)
+            out = c.attend(q, mask)
+            want = torch.cat([trees.attend(q[a:b], c.k[r], c.v[r], c.seen(r, mask), hd ** -0.5)[0] for r, (a, b) in enumerate(zip(c.row0[:-1].tolist(), c.row0[1:].tolist()))])
+            assert norm_error(out, want) < norm_bound(dtype)
+            for a, b in zip(c.row0[:-1].tolist(), c.row0[1:].tolist()):      # a request's alone: few values, whose roundings may all be near half a step
+                assert norm_error(out[a:b], want[a:b]) < 2 * norm_bound(dtype)
+
+
+@pytest.mark.parametrize("heads,kvh,hd", [(8, 2, 128), (8, 2, 64), (48, 1, 128)])
+@pytest.mark.parametrize("new,base", LONG)
+@pytest.mark.parametrize("every", [1, 16])
+def test_long_contexts_key_by_key(new, base, heads, kvh, hd, every):
+    """Every key, or one of each page, counts alike: a lost or a doubled one shows."""
+    import torch
+    c = Case(heads + sum(new) + hd, new, base, heads, kvh, hd)
+    for r, (n, b) in enumerate(zip(new, base)):
+        c.k[r], c.v[r] = marked(b + n, np.arange(5 % every, b + n, every), hd, kvh, "cuda")
+    c.fill()
+    for dtype in (torch.bfloat16, torch.float32):
+        if dtype is torch.bfloat16 and every == 1 and max(base) > 20000:
+            continue                               # (one key is less than half a step)
+        q = marked_queries(c.rows, heads, hd, dtype, "cuda")
+        out = c.attend(q, None)
+        for r, (n, b) in enumerate(zip(new, base)):
+            rows = slice(int(c.row0[r]), int(c.row0[r + 1]))
+            seen = b + 1 + np.arange(n)            # positions of each row
+            want = marked_result((seen - 1 - 5 % every) // every + 1, hd, heads, kvh).cuda()
+            assert ((out[rows].double() - want).abs() <= marked_tolerance(dtype) * want).all()
+
+
+@pytest.mark.parametrize("lengths,heads,kvh,hd", [([5000], 8, 2, 128), ([3000, 1, 2049, 700], 4, 4, 64), ([4100], 6, 2, 128)])
+def test_long_prompts_in_norm_and_key_by_key(lengths, heads, kvh, hd):
+    import torch
+    from paper_2605_13319_b200 import binding
+    c = Packed(sum(lengths), lengths, heads, kvh, hd)
+    out = binding.attend_packed(c.q, c.k, c.v, c.row0)
+    for rows, n in c.spans():
+        seen = torch.ones((n, n), dtype=torch.bool, device="cuda").tril()
+        want = trees.attend(c.q[rows], c.k[rows], c.v[rows], seen, c.scale)[0]
+        assert norm_error(out[rows], want) < norm_bound(out.dtype)
+        if n > 2000:                               # (the last rows alone, which see most)
+            assert norm_error(out[rows][-512:], want[-512:]) < norm_bound(out.dtype)
+    for every in (1, 16):
+        for rows, n in c.spans():
+            c.k[rows], c.v[rows] = marked(n, np.arange(0, n, every), hd, kvh, "cuda")
+        c.q[:] = marked_queries(c.rows, heads, hd, torch.bfloat16, "cuda")
+        out = binding.attend_packed(c.q, c.k, c.v, c.row0)
+        for rows, n in c.spans():
+            want = marked_result(np.arange(n) // every + 1, hd, heads, kvh).cuda()
+            assert ((out[rows].double() - want).abs() <= marked_tolerance(out.dtype) * want).all()
+
+
+# --------------------------------------------------------------------------- long pages
+def _ends(page):
+    """Numbers of positions in front of, at and behind a page's end, a tile's, and both."""
+    return [page - 1, page, page + 1, 2 * page + 127, 3 * page, 127, 128, 129]
+
+
+@pytest.mark.parametrize("heads,kvh,hd", [(4, 2, 128), (4, 2, 64), (40, 1, 128)])
+@pytest.mark.parametrize("page", [72, 128, 136, 256, 4096])
+def test_pages_as_long_as_tiles(page, heads, kvh, hd):
+    import torch
+    new = [1, 2, 5, 1, 9, 3, 1, 4]
+    base = [max(0, e - n) for e, n in zip(_ends(page), new)]
+    many = ([1] * 24 + [20], [_ends(page)[i % 8] - 1 for i in range(24)] + [page + 60])
+    for new, base in ((new, base), many, ([30], [2 * page + 20])):
+        c = Case(page + heads + len(new), new, base, heads, kvh, hd, page)
+        c.fill()
+        for dtype in (torch.bfloat16, torch.float32):
+            for mask in (None, c.trees(1)):
+                q = c.queries(dtype)
+                out = c.attend(q, mask)
+                c.check(q, mask, out)
+                assert torch.equal(out, c.attend(q, mask))
+    hidden = Case(page, [3, 40], [3 * page - 3, page + 7], heads, kvh, hd, page, hide=[(0, 1, -1), (1, 0, 10 ** 9)])
+    hidden.fill()
+    for dtype in (torch.bfloat16, torch.float32):
+        q = hidden.queries(dtype)
+        hidden.check(q, None, hidden.attend(q, None))
