@@ -400,8 +400,8 @@ int32_t pipesd_kv4_attend(const pipesd_kv4_cfg *cfg, const void *pool, const voi
  * What a server needs whose edges draft trees instead of chains: attention of whole prompts, which fills the cache; attention of a tree's
  * nodes over the cache; and the pages' life: reserved for rows to come, forked for candidates that share a prefix, compacted to the
  * accepted path, released.  Calls, streams, threads and graphs as for pipesd_sample; all arrays are in device memory.
- * Attention's kernels wait for copies and products at most two seconds at a time.  Where such a wait runs out, which no valid call brings about, all
- * rows of which that CTA has a part are NaN in the heads that it had, and the call's other rows what they should be. */
+ * Attention's kernels wait for copies and products at most two seconds at a time.  Where such a wait runs out, all rows of which
+ * that CTA has a part are NaN in the heads that it had, and the call's other rows what they should be. */
 
 /* out[row] = softmax(scale * q . k) v over the rows of the same prompt up to itself.  Prompt r has the rows row0[r] .. row0[r+1]-1 (row0:
  * n_req + 1 ascending entries within 0 .. rows; a prompt without rows is one); rows of no prompt are neither read into any result nor written.

@@ -250,3 +250,31 @@ def test_pages_as_long_as_tiles(page, heads, kvh, hd):
     for dtype in (torch.bfloat16, torch.float32):
         q = hidden.queries(dtype)
         hidden.check(q, None, hidden.attend(q, None))
+
+
+def test_a_long_way_between_values_that_are_not_finite():
+    """Two tiles with a border, each with a NaN, two million positions apart: rows see the NaN in its column, and the search for it takes no
+    block so long that its waits run out."""
+    import torch
+    from paper_2605_13319_b200 import binding
+    page, hd, n_req = 4088, 128, 450
+    n_pages = (1 << 21) // page
+    total = n_pages * page - 50
+    g = torch.Generator("cuda").manual_seed(0)
+    cache = binding.Kv16Cache(1, hd, n_pages=n_pages, page_size=page)
+    k, v = (torch.randn((total, 1, hd), generator=g, device="cuda").bfloat16() for _ in range(2))
+    v[page + 2, 0, 3] = float("nan")               # beside the page that is not there, and near the last position
+    v[total - 3, 0, 40] = float("nan")
+    table = torch.arange(n_pages, dtype=torch.int32, device="cuda")[None]
+    cache.append(k, v, _ints([0, total]), _ints([0]), table)
+    table = table.expand(n_req, -1).contiguous()   # read by all
+    table[:, 0] = -1
+    q = torch.randn((n_req, 1, hd), generator=g, device="cuda").bfloat16()
+    out = cache.attend(q, _ints(range(n_req + 1)), _ints([total - 1] * n_req), table)
+    assert torch.isnan(out[..., [3, 40]]).all() and torch.isfinite(out[:, 0, [i for i in range(hd) if i not in (3, 40)]]).all()
+    clean = v.clone()
+    clean[page + 2, 0, 3] = clean[total - 3, 0, 40] = 0.0
+    rows = [0, 1, n_req // 2, n_req - 1]
+    want = trees.attend(q[rows], k[page:], clean[page:], torch.ones((4, total - page), dtype=torch.bool, device="cuda"), hd ** -0.5)[0]
+    keep = [i for i in range(hd) if i not in (3, 40)]
+    assert norm_error(out[rows][..., keep], want[..., keep]) < 2 * norm_bound(q.dtype)
