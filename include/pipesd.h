@@ -406,8 +406,8 @@ int32_t pipesd_kv4_attend(const pipesd_kv4_cfg *cfg, const void *pool, const voi
 /* out[row] = softmax(scale * q . k) v over the rows of the same prompt up to itself.  Prompt r has the rows row0[r] .. row0[r+1]-1 (row0:
  * n_req + 1 ascending entries within 0 .. rows; a prompt without rows is one); rows of no prompt are neither read into any result nor written.
  * bf16 throughout: q, out [rows, n_q_heads, head_dim], k, v [rows, n_kv_heads, head_dim], head_dim 64 or 128, n_q_heads a multiple of
- * n_kv_heads, up to 128 times as many; strides in elements between rows, multiples of 8, pointers 16-byte aligned; scale > 0, every score
- * times scale below 2^120 in magnitude.  Scores, their maximum and their sums are fp32, probabilities enter the second product in bf16.  A NaN or an
+ * n_kv_heads, up to 128 times as many; strides in elements between rows, multiples of 8, pointers 16-byte aligned; scale of (0, 2^127], every
+ * score times scale below 2^120 in magnitude.  Scores, their maximum and their sums are fp32, probabilities enter the second product in bf16.  A NaN or an
  * infinity in a row of k or v reaches the rows that see it (what is not finite in v makes that column NaN or infinite) and no others; a
  * score of minus infinity has no weight, and a head's row that has no other is NaN.  out must not overlap the inputs. */
 int32_t pipesd_attend_packed(const void *q, const void *k, const void *v, void *out, int64_t q_stride, int64_t k_stride, int64_t v_stride,
@@ -449,7 +449,7 @@ int32_t pipesd_kv16_read(const pipesd_kv16_cfg *cfg, const void *pool, int32_t l
 /* out[row] = softmax(scale * q . k) v over what the row sees (its request's new rows appended before): positions 0 .. base[r]-1, and of the
  * new rows those whose bit is set in its row of mask ([rows, words], words 1..256, as pipesd_tree_mask writes them; any other set will do, none
  * at all too); without a mask (null) those up to itself.  q, out: [rows, n_q_heads, head_dim] of `dtype` with q_stride, out_stride;
- * n_q_heads a multiple of n_kv_heads, up to 128 times as many; scale > 0, every score times scale below 2^120 in magnitude.  Sums are fp32.  bf16:
+ * n_q_heads a multiple of n_kv_heads, up to 128 times as many; scale of (0, 2^127], every score times scale below 2^120 in magnitude.  Sums are fp32.  bf16:
  * q as it is, probabilities in bf16; fp32: q and probabilities as three bf16 terms each (24 bits).  A row that sees no position gives 0, a
  * head's row whose q has a NaN a NaN; rows of no request are left as they are.  A NaN or an infinity in the cache reaches the rows that
  * see it, as for prompts; fp32: an infinity in k as a NaN, since q's terms may differ in sign.  out must not overlap q.  The order of sums goes by the lengths and by the numbers of rows and requests.  scratch:

@@ -36,6 +36,8 @@ int size_of(int32_t dtype) { return dtype == PIPESD_F32 ? 4 : 2; }
 bool dtype_ok(int32_t dtype) { return dtype == PIPESD_F32 || dtype == PIPESD_BF16; }
 bool aligned(const void* p, int32_t dtype) { return (uintptr_t)p % size_of(dtype) == 0; }
 bool wide(const void* p, int64_t stride, int32_t rows, int32_t dtype) { return (uintptr_t)p % 16 == 0 && (rows == 1 || stride * size_of(dtype) % 16 == 0); }
+// The kernels take it times log2(e).
+bool scale_ok(float scale) { return scale > 0.f && scale * 1.4426950408889634f < INFINITY; }
 int32_t launched() { return cudaGetLastError() == cudaSuccess ? PIPESD_OK : PIPESD_E_CUDA; }
 
 // Query rows that a share (of a stream) has room for.
@@ -234,7 +236,7 @@ int32_t pipesd_kv16_attend(const pipesd_kv16_cfg* cfg, const void* pool, int32_t
                            const int32_t* table, const uint32_t* mask, int32_t words, void* scratch, void* cuda_stream) {
     if (!where_ok(cfg, pool, layer, n_req, rows, row0, base, table) || !q || !out || !scratch || (uintptr_t)scratch % 16 || !dtype_ok(dtype) ||
         !aligned(q, dtype) || !aligned(out, dtype) || n_q_heads < 1 || n_q_heads % cfg->n_kv_heads || n_q_heads / cfg->n_kv_heads > 128 ||
-        !(scale > 0.f && scale < INFINITY) || (mask && (words < 1 || words > kTreeWords)))
+        !scale_ok(scale) || (mask && (words < 1 || words > kTreeWords)))
         return PIPESD_E_INVALID;
     const int64_t width = (int64_t)n_q_heads * cfg->head_dim;
     if (rows > 1 && (q_stride < width || out_stride < width)) return PIPESD_E_INVALID;
@@ -266,7 +268,7 @@ int32_t pipesd_attend_packed(const void* q, const void* k, const void* v, void* 
                              int64_t out_stride, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, float scale, int32_t n_req, int32_t rows,
                              const int32_t* row0, void* cuda_stream) {
     if (!q || !k || !v || !out || !row0 || (head_dim != 64 && head_dim != 128) || n_kv_heads < 1 || n_kv_heads > 65535 || n_q_heads < 1 ||
-        n_q_heads % n_kv_heads || n_q_heads / n_kv_heads > 128 || !(scale > 0.f && scale < INFINITY) || n_req < 1 || rows < 1)
+        n_q_heads % n_kv_heads || n_q_heads / n_kv_heads > 128 || !scale_ok(scale) || n_req < 1 || rows < 1)
         return PIPESD_E_INVALID;
     const int64_t wq = (int64_t)n_q_heads * head_dim, wkv = (int64_t)n_kv_heads * head_dim;
     if ((int64_t)rows * n_q_heads > INT32_MAX) return PIPESD_E_INVALID;

@@ -278,3 +278,28 @@ def test_a_long_way_between_values_that_are_not_finite():
     want = trees.attend(q[rows], k[page:], clean[page:], torch.ones((4, total - page), dtype=torch.bool, device="cuda"), hd ** -0.5)[0]
     keep = [i for i in range(hd) if i not in (3, 40)]
     assert norm_error(out[rows][..., keep], want[..., keep]) < 2 * norm_bound(q.dtype)
+
+
+@pytest.mark.parametrize("scale", [2.0 ** 127, 2.0 ** -100])
+def test_largest_and_smallest_scales(scale):
+    import torch
+    from paper_2605_13319_b200 import binding
+    c = Case(3, [9, 1], [200, 30], 4, 2, 64)
+    c.fill()
+    for dtype in (torch.bfloat16, torch.float32):
+        q = c.queries(torch.float32) * (2.0 ** -64 if scale > 1 else 2.0 ** 50)
+        if scale > 1:                              # (keys' part of it, so that a score's products are normal numbers)
+            for k in c.k:
+                k *= 2.0 ** -62
+            c.fill()
+        q = q.to(dtype)
+        out = c.attend(q, None, scale=scale)
+        c.check(q, None, out, scale)
+        if scale > 1:
+            for k in c.k:
+                k *= 2.0 ** 62
+    p = Packed(4, [100, 5], 4, 2, 128)
+    p.q *= 2.0 ** -64 if scale > 1 else 2.0 ** 50
+    p.k *= 2.0 ** -62 if scale > 1 else 1.0
+    p.scale = scale
+    p.check(binding.attend_packed(p.q, p.k, p.v, p.row0, scale=scale))

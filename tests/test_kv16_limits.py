@@ -4,7 +4,7 @@ import ctypes
 import pytest
 
 from paper_2605_13319_b200 import binding
-from test_kv16_arguments import INVALID, call, cfg
+from test_kv16_arguments import INVALID, PACKED, call, cfg
 
 
 @pytest.mark.parametrize("name,many", [("reserve", "n_req"), ("fork", "n")])
@@ -20,3 +20,9 @@ def test_blocks_that_give_up_are_blocks():
     for block in (-2, 148, 2 ** 31 - 1):
         assert L.pipesd_debug_attend_gives_up(block) == INVALID
     assert L.pipesd_debug_attend_gives_up(-1) == 0
+
+
+@pytest.mark.parametrize("scale", [2.5e38, 3.4e38])
+def test_scales_that_overflow_in_powers_of_two(scale):
+    assert call("attend", scale=scale) == INVALID
+    assert binding.lib().pipesd_attend_packed(*(PACKED | dict(scale=scale)).values(), None) == INVALID
