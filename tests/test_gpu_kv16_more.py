@@ -303,3 +303,38 @@ def test_largest_and_smallest_scales(scale):
     p.k *= 2.0 ** -62 if scale > 1 else 1.0
     p.scale = scale
     p.check(binding.attend_packed(p.q, p.k, p.v, p.row0, scale=scale))
+
+
+@pytest.mark.parametrize("heads,new", [(4, [7, 1, 30]), (32, [20, 40, 3])])
+def test_padded_batches(heads, new):
+    """Rows in front of the first request and behind the last: not read into anything, left as they were, in every call that takes rows."""
+    import torch
+    from paper_2605_13319_b200 import binding
+    c = Case(heads, new, [300, 0, 77], heads, 2, 128)
+    c.fill()
+    mask = c.trees(2)
+    lead, pad = 3, 60
+    inside = slice(lead, lead + c.rows)
+    where = [c.where[0] + lead, *c.where[1:]]
+    for dtype in (torch.bfloat16, torch.float32):
+        q = c.queries(dtype)
+        wide = torch.full((lead + c.rows + pad, heads, 128), float("nan"), dtype=dtype, device="cuda")
+        wide[inside] = q
+        bits = torch.full((len(wide), 2), -1, dtype=torch.int32, device="cuda")
+        bits[inside] = _ints(mask.view(np.int32))
+        for m, b in ((None, None), (mask, bits)):
+            out = c.cache.attend(wide, *where, mask=b, out=torch.full_like(wide, 5.0))
+            c.check(q, m, out[inside])
+            assert (out[:lead] == 5).all() and (out[inside.stop:] == 5).all()
+    k, v = (torch.randn((len(wide), 2, 128), device="cuda").bfloat16() for _ in range(2))
+    before = c.cache.pool.clone()
+    c.cache.append(k, v, *where)
+    got = c.cache.read(len(wide), *where)
+    for x, y in zip((k, v), got):
+        assert torch.equal(y[inside], x[inside]) and (y[:lead] == 0).all() and (y[inside.stop:] == 0).all()
+    new_pages = {int(c.table[r, p // c.page]) for r, (n, b) in enumerate(zip(c.new, c.base)) for p in range(b, b + n)}
+    rest = [p for p in range(c.cache.n_pages) if p not in new_pages]
+    assert torch.equal(c.cache.pool[:, rest].view(torch.int16), before[:, rest].view(torch.int16))
+    parent = _ints([-1, 0] * ((len(wide) + 1) // 2))[:len(wide)].contiguous()
+    trees_mask, depth = binding.tree_mask(parent, where[0], 2)
+    assert (trees_mask[:lead] == 0).all() and (trees_mask[inside.stop:] == 0).all() and (depth[:lead] == 0).all() and (depth[inside.stop:] == 0).all()
