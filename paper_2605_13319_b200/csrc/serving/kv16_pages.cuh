@@ -45,11 +45,9 @@ __global__ void __launch_bounds__(32 * kKv16RowWarps) kv16_append_kernel(const K
     if (r < 0) return;
     const int pos = base + row - first, page = kv16_page(a.w, r, pos);
     if (page < 0 || kv >= 2) return;
-    for (int head = blockIdx.y; head < a.w.Hkv; head += gridDim.y) {
-        const T* src = kv == 0 ? static_cast<const T*>(a.k) + row * a.k_stride : static_cast<const T*>(a.v) + row * a.v_stride;
-        const uint4 x = kv16_load8(src + head * HD + c * 8, a.wide);
-        *reinterpret_cast<uint4*>(kv16_block(a.p, a.w, a.p.layer, page, kv, head) + kv16_piece(pos % a.w.page_size, c, HD)) = x;
-    }
+    const int head = blockIdx.y;
+    const T* src = kv == 0 ? static_cast<const T*>(a.k) + row * a.k_stride : static_cast<const T*>(a.v) + row * a.v_stride;
+    *reinterpret_cast<uint4*>(kv16_block(a.p, a.w, a.p.layer, page, kv, head) + kv16_piece(pos % a.w.page_size, c, HD)) = kv16_load8(src + head * HD + c * 8, a.wide);
 }
 
 // The same the other way; 0 where no page is and for rows of no request.
@@ -65,12 +63,11 @@ __global__ void __launch_bounds__(32 * kKv16RowWarps) kv16_read_kernel(const Kv1
         page = kv16_page(a.w, r, pos);
     }
     if (kv >= 2) return;
-    for (int head = blockIdx.y; head < a.w.Hkv; head += gridDim.y) {
-        uint4 x = make_uint4(0, 0, 0, 0);
-        if (page >= 0) x = *reinterpret_cast<const uint4*>(kv16_block(a.p, a.w, a.p.layer, page, kv, head) + kv16_piece(pos % a.w.page_size, c, HD));
-        uint16_t* dst = static_cast<uint16_t*>(const_cast<void*>(kv == 0 ? a.k : a.v)) + ((size_t)row * a.w.Hkv + head) * HD + c * 8;
-        *reinterpret_cast<uint4*>(dst) = x;
-    }
+    const int head = blockIdx.y;
+    uint4 x = make_uint4(0, 0, 0, 0);
+    if (page >= 0) x = *reinterpret_cast<const uint4*>(kv16_block(a.p, a.w, a.p.layer, page, kv, head) + kv16_piece(pos % a.w.page_size, c, HD));
+    uint16_t* dst = static_cast<uint16_t*>(const_cast<void*>(kv == 0 ? a.k : a.v)) + ((size_t)row * a.w.Hkv + head) * HD + c * 8;
+    *reinterpret_cast<uint4*>(dst) = x;
 }
 
 // ---- the ancestors of a tree's nodes
