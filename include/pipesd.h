@@ -450,11 +450,11 @@ int32_t pipesd_kv16_read(const pipesd_kv16_cfg *cfg, const void *pool, int32_t l
  * new rows those whose bit is set in its row of mask ([rows, words], words 1..256, as pipesd_tree_mask writes them; any other set will do, none
  * at all too); without a mask (null) those up to itself.  q, out: [rows, n_q_heads, head_dim] of `dtype` with q_stride, out_stride;
  * n_q_heads a multiple of n_kv_heads, up to 128 times as many; scale of (0, 2^127], every score times scale below 2^120 in magnitude.  Sums are fp32.  bf16:
- * q as it is, probabilities in bf16; fp32: q and probabilities as three bf16 terms each (24 bits).  A row that sees no position gives 0, a
+ * q as it is, probabilities in bf16; fp32: q, below 2^127 in magnitude, and probabilities as three bf16 terms each (24 bits).  A row that sees no position gives 0, a
  * head's row whose q has a NaN a NaN; rows of no request are left as they are.  A NaN or an infinity in the cache reaches the rows that
  * see it, as for prompts; fp32: an infinity in k as a NaN, since q's terms may differ in sign.  out must not overlap q.  The order of sums goes by the lengths and by the numbers of rows and requests.  scratch:
- * pipesd_kv16_attend_scratch_bytes bytes (0 for arguments that are refused), 16-byte aligned; it holds nothing between calls, but two
- * calls that may run at the same time need one each. */
+ * pipesd_kv16_attend_scratch_bytes bytes (0 for arguments that are refused; about 2400 * min(128, rows * n_q_heads / n_kv_heads) * (head_dim + 2), 39 MB at
+ * most), 16-byte aligned; it holds nothing between calls, but two calls that may run at the same time need one each. */
 uint64_t pipesd_kv16_attend_scratch_bytes(const pipesd_kv16_cfg *cfg, int32_t rows, int32_t n_q_heads);
 int32_t pipesd_kv16_attend(const pipesd_kv16_cfg *cfg, const void *pool, int32_t layer, const void *q, void *out, int32_t dtype,
                            int64_t q_stride, int64_t out_stride, int32_t n_q_heads, float scale, int32_t n_req, int32_t rows,
