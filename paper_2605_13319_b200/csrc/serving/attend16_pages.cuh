@@ -639,11 +639,11 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                         release_keys(k);
                     }
                     if (j0 + step >= n) umma_commit(smem_u32(&c.q_empty));
-                    if (!both && s == 1) see(VPlace(tile_no));
                     for (int j = j0; j < n; j += step) {
                         const bool more = j + step < n;
                         const KPlace k(tile_no + j + step);
                         const VPlace v(tile_no + j);
+                        if (!both && j > 0) see(VPlace(tile_no + j - 1));
                         if (!v_there(v) || (more && !k_there(k))) break;
                         if (!sums(v, j == j0)) break;
                         if (more) scores(k, q_tile);
@@ -651,8 +651,9 @@ __global__ void __launch_bounds__(kAttendThreads16, 1) pages_attend_kernel(const
                         umma_commit(smem_u32(&c.v_empty[v.slot]));
                         if (more) release_keys(k);
                         if (more && j + 2 * step >= n) umma_commit(smem_u32(&c.q_empty));
-                        if (!both && j + 1 < n) see(VPlace(tile_no + j + 1));
+                        if (!both && j + 2 == n) see(VPlace(tile_no + j + 1));
                     }
+                    if (!both && j0 >= n) see(VPlace(tile_no));
                     tile_no += n;
                 }
                 // What was issued ends, and has arrived at its barriers, before the CTA goes.

@@ -101,10 +101,10 @@ class Cta:
                 yield v_wait(c)
                 self.v_empty[c % self.v_slots].arrive()
 
-            if self.sees_all and not both and s == 1:
-                yield from see(first)
             for j in range(j0, n, step):
                 more, c = j + step < n, first + j
+                if self.sees_all and not both and j > 0:
+                    yield from see(c - 1)
                 yield v_wait(c)
                 if more:
                     yield k_wait(c + step)
@@ -121,8 +121,10 @@ class Cta:
                     release(self.k_empty[(c + step) % self.k_slots], both)
                 if more and j + 2 * step >= n:
                     commit(self.q_empty)
-                if self.sees_all and not both and j + 1 < n:
+                if self.sees_all and not both and j + 2 == n:
                     yield from see(c + 1)
+            if self.sees_all and not both and j0 >= n:
+                yield from see(first)
             first += n
 
     def rows(self, s):
@@ -214,6 +216,6 @@ def test_the_kernel_waits_so():
     body = body[:body.find("registers_more()")]
     see = re.search(r"auto see = \[&\]\(const VPlace& v\) \{([^}]*)\}", body)
     assert see and re.search(r"v_there\(v\)", see.group(1)) and re.search(r"mbar_arrive\(smem_u32\(&c\.v_empty\[v\.slot\]\)\)", see.group(1))
-    assert re.search(r"if \(!both && s == 1\) see\(VPlace\(tile_no\)\);\s*for \(int j = j0; j < n; j \+= step\)", body)
-    assert re.search(r"if \(!both && j \+ 1 < n\) see\(VPlace\(tile_no \+ j \+ 1\)\);\s*\}\s*tile_no \+= n;", body)
+    assert re.search(r"if \(!both && j > 0\) see\(VPlace\(tile_no \+ j - 1\)\);\s*if \(!v_there\(v\)", body)
+    assert re.search(r"if \(!both && j \+ 2 == n\) see\(VPlace\(tile_no \+ j \+ 1\)\);\s*\}\s*if \(!both && j0 >= n\) see\(VPlace\(tile_no\)\);\s*tile_no \+= n;", body)
     assert re.search(r"umma_commit\(smem_u32\(&c\.v_empty\[v\.slot\]\)\);", body) and not re.search(r"release\(&c\.v_empty", body)
