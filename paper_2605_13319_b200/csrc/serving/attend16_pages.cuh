@@ -9,9 +9,9 @@
 // rows and tiles of 64 keys, since the terms of q fill shared memory and those of the weights tensor memory.
 // Blocks of pages are operands of the products as they are (kv16.cuh): a bulk copy per page and tile, by the lanes of a warp for keys and one for values.
 //
-// Bound by the cache's bytes where rows are few and caches long: 32 rows behind 131040 positions (128 query rows by KV head) 109 us, 4.9 TB/s; by the chain
+// Bound by the cache's bytes where rows are few and caches long: 32 rows behind 131040 positions (128 query rows by KV head) 108 us, 5.0 TB/s; by the chain
 // of a triple's beginning and end where they are short: until the first scores 9000 clocks, 4500 from the last weights to the sums' end, 3300 to 3900 a tile of
-// 256 rows between them (16 requests of 8 to 64 nodes behind 256 to 8192 positions: 117 us, 52 of bytes).  The merge adds 6 to 10.
+// 256 rows between them (16 requests of 8 to 64 nodes behind 256 to 8192 positions: 118 us, 52 of bytes).  The merge adds 6 to 10.
 #pragma once
 #include <type_traits>
 
